@@ -387,6 +387,96 @@ l2a_status l2a_decode(const l2a_params* p, const void* q, const void* K, const v
                       void* O, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * ---------------------------------------------------------------------------------------------------------------------
+ * Paged key/value cache.  For serving, where sequences of different lengths grow side by side: keys and values are kept in
+ * pages of page_size tokens from a common pool, each sequence has a row of page numbers, and a page may hold bf16 or 8-bit
+ * values.  l2a_cache_append writes new tokens, l2a_cache_forward attends from them, l2a_cache_read gives them back.
+ *
+ * L2A_CACHE_E4M3: a row of D values x (one token, one KV head, K or V) is held as D e4m3 codes and one exponent e, the least
+ * whole number with max|x| <= 448 * 2^e (e >= -126; 0 for a row of zeros); code_i = x_i / 2^e rounded to e4m3, to nearest even.
+ * It stands for code_i * 2^e.  The scale is a power of two, so that this product is exact in bf16 and fp32; a float
+ * scale would gain nothing, since the spacing of e4m3 values is relative.  Relative error of a value at most 2^-4, of
+ * values below 2^-14 of the row's largest half a step of 2^-9 * 2^e.  Infinite values become +-448 * 2^e, NaN stays NaN (neither
+ * counts for max|x|).
+ */
+#define L2A_CACHE_BF16 0
+#define L2A_CACHE_E4M3 1
+
+typedef struct l2a_cache {
+  void *K, *V;               /* pools [n_pages, Hkv, page_size, D] of bf16 or e4m3, 16-byte aligned               */
+  uint8_t *k_scale, *v_scale; /* E4M3: [n_pages, Hkv, page_size] exponents e + 127, 16-byte aligned; BF16: NULL     */
+  int64_t page_stride;       /* elements from a page of K (of V) to the next; 0 = Hkv * page_size * D; multiple of   */
+                             /* 16 bytes.  K and V may lie in one allocation, page by page                           */
+  int64_t scale_stride;      /* the same for k_scale and v_scale; 0 = Hkv * page_size; multiple of 16                */
+  int32_t kind;              /* L2A_CACHE_*                                                                       */
+  int32_t n_pages;
+  int32_t page_size;         /* tokens of a page: 16, 32, 64 or 128                                               */
+  int32_t table_stride;      /* entries of a row of page_table                                                    */
+  const int32_t* page_table; /* device [B, table_stride]: entry i of row b is the page of positions               */
+                             /* i * page_size .. of sequence b.  Entries that no position in use falls into are    */
+                             /* not read; one outside 0 .. n_pages - 1 is never followed                         */
+  const int32_t* lengths;    /* device [B]: tokens of each sequence, its new ones included.  At most p->Lk          */
+} l2a_cache;
+
+/*
+ * What the three calls have in common.
+ *   p           : B sequences; Lq = the most new tokens of a sequence, Lk = the most tokens of a sequence (both bounds for
+ *                 the host; Lk <= table_stride * page_size); Hq, Hkv, D, window, softmax_scale as elsewhere.
+ *                 q_pos_offset and seq_bounds are not used (seq_bounds must be NULL).
+ *   cu_new      : device int32 [B + 1], ascending from 0: the new tokens of sequence b are rows cu_new[b] ..
+ *                 cu_new[b + 1] - 1 of a token axis of n_tokens rows; a sequence may have none.  NULL: every sequence has
+ *                 Lq of them (n_tokens = B * Lq).  New token i of n of sequence b sits at position lengths[b] - n + i.
+ * Tensors on the token axis are [n_tokens, H, D] with their token stride in p (k_stride[1] and so on; the batch stride is 0).
+ * The lengths, tables and cu_new are read on the device only: a captured call follows them when they change.  Values that break
+ * the bounds above give results of no meaning, but no access outside the tensors.
+ */
+
+/*
+ * Writes the keys and values of the new tokens into their pages (and quantises them).
+ *   K, V        in : bf16 [n_tokens, Hkv, D] (token strides k_stride[1], v_stride[1]).
+ * HBM-bound: one pass over K and V.  n_tokens = 0 is no work.  Two tokens never share a slot; slots of other tokens keep their
+ * bits.  Errors: L2A_ERR_INVALID_ARG, L2A_ERR_UNSUPPORTED (D, page_size, kind), L2A_ERR_CUDA.
+ */
+l2a_status l2a_cache_append(const l2a_params* p, const l2a_cache* c, const void* K, const void* V, const int32_t* cu_new,
+                            int n_tokens, void* stream);
+
+/*
+ * Reads the cache back.  Row t of sequence b of the outputs is position first[b] + t (first: device int32 [B], NULL = 0):
+ *   K_out, V_out out : bf16 [B, Lk, Hkv, D] (k_stride, v_stride), what the cache stands for, rounded to bf16 (exact unless it
+ *                      overflows or underflows); rows of positions below 0 or from lengths[b] on are zeros.
+ * HBM-bound.  The layout is that of K and V in l2a_forward and l2a_decode.
+ */
+l2a_status l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t* first, void* K_out, void* V_out,
+                          void* stream);
+
+/*
+ * The layer's attention of the new tokens over the cache, which holds their own keys and values already (l2a_cache_append).
+ * The token at position p attends to the keys max(0, p - window) .. p (Local Attention, s) and, if its routing decision
+ * is 1, to all keys 0 .. p (Global Attention, a); o = s + d * a, rounded to bf16 once.  From one new token per sequence (decode)
+ * to thousands (the next chunk of a prompt), mixed in one call.
+ *
+ *   Q           in : bf16 [n_tokens, Hq, D] (token stride q_stride[1]).
+ *   d           in : uint8 [n_tokens], non-zero = routed; NULL = none is.
+ *   O           out: bf16 [n_tokens, Hq, D] (token stride o_stride[1]).  Rows at positions below 0 get zeros.
+ *   ws             : device workspace of l2a_cache_workspace_bytes, 256-byte aligned, its first word a status
+ *                    (l2a_workspace_status).  The size follows from p, page size and n_tokens; it is enough for every smaller
+ *                    n_tokens, Lq and Lk (other fields alike).
+ *   p->flags       : L2A_FLAG_SKIP_GLOBAL: s only (as d = NULL).  L2A_FLAG_SKIP_LOCAL: o = d * a.  L2A_FLAG_GLOBAL_PHASE: O holds
+ *                    s already (from an L2A_FLAG_SKIP_GLOBAL call on another cache, say), and d * a is added for the routed
+ *                    rows; others are not touched.  That is the layer whose Global Attention has projections, and so
+ *                    a cache, of its own.  L2A_FLAG_SHARED_WINDOW is implied (one cache feeds both modules, the window's scores
+ *                    are computed once) and ignored.  Other flags: L2A_ERR_INVALID_ARG.
+ * Positions before every window of a sequence whose tokens are not routed are not read, nor are their table entries: a layer without
+ * Global Attention may give those pages back.  Slots without a token may hold anything.  Keys and values that some
+ * new token of the sequence attends to must be finite for all of them.
+ * Scores, soft-max statistics and sums are fp32.  Results are bit-reproducible; how the keys of a row are divided follows from
+ * all the call's lengths, so that the same sequence in another batch can differ by fp32 rounding.
+ */
+l2a_status l2a_cache_workspace_bytes(const l2a_params* p, const l2a_cache* c, int n_tokens, size_t* ws_bytes);
+l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c, const void* Q, const int32_t* cu_new, int n_tokens,
+                             const uint8_t* d, void* O, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * One whole step for callers that hold HOST buffers, so that end-to-end time including the
  * transfers can be measured through the C ABI: copies Q, K, V, the router input (and dO) to the
  * device buffers the caller supplies, runs l2a_route_compact + l2a_forward (+ l2a_backward when

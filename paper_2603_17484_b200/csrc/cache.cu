@@ -1,0 +1,285 @@
+// Paged key/value cache: argument checks, the write of new tokens (l2a_cache_append) and the read back (l2a_cache_read).
+#include <math.h>
+
+#include "cache_common.cuh"
+#include "sm100_prims.cuh"
+
+namespace l2a {
+
+l2a_status cache_view(const l2a_params* p, const l2a_cache* c, const int32_t* cu_new, int n_tokens, CacheView* v) {
+  if (!p || !c) return L2A_ERR_INVALID_ARG;
+  if (p->B <= 0 || p->Lq <= 0 || p->Lk <= 0 || p->Hq <= 0 || p->Hkv <= 0 || p->D <= 0 || n_tokens < 0) return L2A_ERR_INVALID_ARG;
+  if (p->Hq % p->Hkv != 0 || p->window < 0 || p->seq_bounds != nullptr) return L2A_ERR_INVALID_ARG;
+  if (!(p->softmax_scale >= 0.f) || isinf(p->softmax_scale)) return L2A_ERR_INVALID_ARG;
+  if (p->D != 64 && p->D != 128) return L2A_ERR_UNSUPPORTED;
+  if (c->kind != L2A_CACHE_BF16 && c->kind != L2A_CACHE_E4M3) return L2A_ERR_UNSUPPORTED;
+  if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128) return L2A_ERR_UNSUPPORTED;
+  if (c->n_pages <= 0 || c->table_stride <= 0 || (int64_t)c->table_stride * c->page_size < p->Lk) return L2A_ERR_INVALID_ARG;
+  if (!c->K || !c->V || !c->page_table || !c->lengths) return L2A_ERR_INVALID_ARG;
+  const bool e4m3 = c->kind == L2A_CACHE_E4M3;
+  const int64_t elem = e4m3 ? 1 : 2, page = (int64_t)p->Hkv * c->page_size * p->D, scales = (int64_t)p->Hkv * c->page_size;
+  const int64_t ps = c->page_stride ? c->page_stride : page, ss = c->scale_stride ? c->scale_stride : scales;
+  if (ps < page || ps * elem % 16 != 0 || ss < scales || ss % 16 != 0) return L2A_ERR_INVALID_ARG;
+  uintptr_t bits = reinterpret_cast<uintptr_t>(c->K) | reinterpret_cast<uintptr_t>(c->V);
+  if (e4m3) {
+    if (!c->k_scale || !c->v_scale) return L2A_ERR_INVALID_ARG;
+    bits |= reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale);
+  }
+  if (bits & 15) return L2A_ERR_INVALID_ARG;
+  if (!cu_new && (int64_t)p->B * p->Lq != n_tokens) return L2A_ERR_INVALID_ARG;
+  v->K = static_cast<uint8_t*>(c->K); v->V = static_cast<uint8_t*>(c->V);
+  v->ks = c->k_scale; v->vs = c->v_scale;
+  v->page_bytes = ps * elem;
+  v->scale_stride = ss;
+  v->kind = c->kind;
+  v->n_pages = c->n_pages;
+  v->page_shift = c->page_size == 16 ? 4 : c->page_size == 32 ? 5 : c->page_size == 64 ? 6 : 7;
+  v->table_stride = c->table_stride;
+  v->max_keys = p->Lk;
+  v->table = c->page_table; v->lengths = c->lengths;
+  v->cu_new = cu_new;
+  v->B = p->B; v->Lq = p->Lq; v->Hkv = p->Hkv; v->D = p->D; v->n_tokens = n_tokens;
+  return L2A_OK;
+}
+
+namespace {
+
+constexpr int kRowsThreads = 256;
+
+// Token stride of a tensor on the token axis, 0: not usable
+int64_t token_stride(const int64_t (&s)[2], int row_elems) {
+  if (s[0] != 0 || s[1] < 0) return 0;
+  const int64_t t = s[1] ? s[1] : row_elems;
+  return t >= row_elems && t % 8 == 0 ? t : 0;
+}
+
+struct AppendArgs {
+  CacheView c;
+  const bf16 *K, *V;
+  int64_t k_t, v_t;
+};
+
+// Biased exponent of the least 2^e with amax <= 448 * 2^e = 1.75 * 2^(8 + e), from the bits of the bf16 amax
+__device__ __forceinline__ uint32_t exponent_for(uint32_t amax) {
+  const int e = (int)(amax >> 7) - 8 + ((amax & 0x7fu) > 0x60u ? 1 : 0);
+  return amax == 0 ? 127u : (uint32_t)max(e, 1);
+}
+// The two magnitudes of a bf16 pair, 0 for those that are not finite
+__device__ __forceinline__ uint32_t finite_magnitudes(uint32_t x) {
+  x &= 0x7fff7fffu;
+  return __vcmpltu2(x, 0x7f807f80u) & x;
+}
+__device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// A lane holds 16 values of a row, D / 16 lanes a row, a warp 512 / D tokens of one head of K or V at a time, kSteps times: the
+// warps of a CTA take the heads of the same tokens, so that it reads whole token rows, and the exponents of
+// a warp's tokens, neighbours in a page, leave in one sector.
+template <int D, bool kE4M3, int kSteps>
+__global__ void __launch_bounds__(kRowsThreads) cache_append_kernel(const AppendArgs a) {
+  constexpr int kLanes = D / 16, kRows = 32 / kLanes, kTokens = kRows * kSteps;
+  const CacheView& c = a.c;
+  const int lane = threadIdx.x & 31;
+  const int64_t item = ((int64_t)blockIdx.x * kRowsThreads + threadIdx.x) >> 5;
+  const int heads = 2 * c.Hkv, hv = (int)(item % heads), h = hv >> 1;
+  const bool value = hv & 1;
+  const int64_t t0 = item / heads * kTokens;
+  if (t0 >= c.n_tokens) return;
+  const bf16* src = value ? a.V : a.K;
+  const int64_t stride = value ? a.v_t : a.k_t;
+  const int sub = lane % kLanes;
+  uint4 x[kSteps][2];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int64_t t = t0 + i * kRows + lane / kLanes;
+    const uint4* row = reinterpret_cast<const uint4*>(src + min(t, (int64_t)c.n_tokens - 1) * stride + h * D + sub * 16);
+    x[i][0] = row[0];
+    x[i][1] = row[1];
+  }
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int t = (int)t0 + i * kRows + lane / kLanes;
+    // the sequence of the token: the last b with cu_new[b] <= t
+    int b = 0, first = 0, n = 0;
+    if (c.cu_new == nullptr) {
+      b = t / c.Lq;
+    } else {
+      for (int b0 = 0; b0 < c.B; b0 += 32) {
+        const int cu = b0 + lane <= c.B ? c.cu_new[b0 + lane] : 0x7fffffff;
+        int seen = 0;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+          const uint32_t below = __ballot_sync(0xffffffffu, cu <= (int)t0 + i * kRows + r);
+          if (lane / kLanes == r) seen = __popc(below);
+        }
+        b += seen;
+        if (__all_sync(0xffffffffu, seen < 32)) break;
+      }
+      b = max(b - 1, 0);
+    }
+    int page = -1, pos = 0;
+    if (t < c.n_tokens && b < c.B) {
+      n = cache_new(c, b, first);
+      pos = c.lengths[b] - n + (t - first);
+      if (t - first < n && pos >= 0 && pos < c.max_keys) page = cache_page(c, b, pos);
+    }
+    const int64_t slot = ((int64_t)h << c.page_shift) + (pos & ((1 << c.page_shift) - 1));
+    uint8_t* dst = (value ? c.V : c.K) + page * c.page_bytes + slot * (kE4M3 ? D : 2 * D);
+    if (kE4M3) {
+      const uint32_t w[8] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w, x[i][1].x, x[i][1].y, x[i][1].z, x[i][1].w};
+      uint32_t m = 0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) m = __vmaxu2(m, finite_magnitudes(w[k]));
+      m = max(m & 0xffffu, m >> 16);
+#pragma unroll
+      for (int o = kLanes / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+      const uint32_t e = exponent_for(m);
+      const float inv = __uint_as_float((254u - e) << 23);       // 2^-e; e + 127 is 1 .. 247
+      uint32_t code[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t u = w[2 * k], v = w[2 * k + 1];
+        code[k] = to_e4m3x2(__uint_as_float(u << 16) * inv, __uint_as_float(u & 0xffff0000u) * inv) |
+                  to_e4m3x2(__uint_as_float(v << 16) * inv, __uint_as_float(v & 0xffff0000u) * inv) << 16;
+      }
+      if (page >= 0) {
+        *reinterpret_cast<uint4*>(dst + sub * 16) = make_uint4(code[0], code[1], code[2], code[3]);
+        if (sub == 0) (value ? c.vs : c.ks)[page * c.scale_stride + slot] = (uint8_t)e;
+      }
+    } else if (page >= 0) {
+      reinterpret_cast<uint4*>(dst + sub * 32)[0] = x[i][0];
+      reinterpret_cast<uint4*>(dst + sub * 32)[1] = x[i][1];
+    }
+  }
+}
+
+struct ReadArgs {
+  CacheView c;
+  const int32_t* first;
+  bf16 *K, *V;
+  RowStrides k_st, v_st;
+};
+
+// The same shape for the way back: a lane brings 16 values of a position, a warp 512 / D positions of a head at a time.
+template <int D, bool kE4M3, int kSteps>
+__global__ void __launch_bounds__(kRowsThreads) cache_read_kernel(const ReadArgs a) {
+  constexpr int kLanes = D / 16, kRows = 32 / kLanes, kTokens = kRows * kSteps;
+  const CacheView& c = a.c;
+  const int lane = threadIdx.x & 31, b = blockIdx.y, sub = lane % kLanes;
+  const int64_t item = ((int64_t)blockIdx.x * kRowsThreads + threadIdx.x) >> 5;
+  const int heads = 2 * c.Hkv, hv = (int)(item % heads), h = hv >> 1;
+  const bool value = hv & 1;
+  const int64_t t0 = item / heads * kTokens + lane / kLanes;
+  if (item / heads * kTokens >= c.max_keys) return;
+  const int start = a.first ? a.first[b] : 0, length = cache_length(c, b);
+  uint4 x[kSteps][kE4M3 ? 1 : 2];
+  uint32_t e[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int64_t pos = start + t0 + i * kRows;
+    x[i][0] = make_uint4(0, 0, 0, 0);
+    if (!kE4M3) x[i][kE4M3 ? 0 : 1] = make_uint4(0, 0, 0, 0);
+    e[i] = 127;
+    if (pos < 0 || pos >= length) continue;
+    const int page = cache_page(c, b, (int)pos);
+    if (page < 0) continue;
+    const int64_t slot = ((int64_t)h << c.page_shift) + (pos & ((1 << c.page_shift) - 1));
+    const uint8_t* src = (value ? c.V : c.K) + page * c.page_bytes + slot * (kE4M3 ? D : 2 * D);
+    if (kE4M3) {
+      x[i][0] = *reinterpret_cast<const uint4*>(src + sub * 16);
+      e[i] = (value ? c.vs : c.ks)[page * c.scale_stride + slot];
+    } else {
+      x[i][0] = reinterpret_cast<const uint4*>(src + sub * 32)[0];
+      x[i][kE4M3 ? 0 : 1] = reinterpret_cast<const uint4*>(src + sub * 32)[1];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int64_t t = t0 + i * kRows;
+    if (t >= c.max_keys) continue;
+    const RowStrides st = value ? a.v_st : a.k_st;
+    uint4* dst = reinterpret_cast<uint4*>((value ? a.V : a.K) + b * st.b + t * st.t + h * D + sub * 16);
+    if (kE4M3) {
+      const float s = scale_of_exponent(e[i]);
+      const uint32_t w[4] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w};
+      uint32_t o[8];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 lo = f16x2_to_float2(e4m3x2_to_f16x2(w[k] & 0xffffu)), hi = f16x2_to_float2(e4m3x2_to_f16x2(w[k] >> 16));
+        o[2 * k] = pack_bf16(lo.x * s, lo.y * s);
+        o[2 * k + 1] = pack_bf16(hi.x * s, hi.y * s);
+      }
+      dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
+      dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+    } else {
+      dst[0] = x[i][0];
+      dst[1] = x[i][kE4M3 ? 0 : 1];
+    }
+  }
+}
+
+template <int D, bool kE4M3>
+cudaError_t launch_append(const AppendArgs& a, cudaStream_t s) {
+  constexpr int kSteps = 2, kTokens = 512 / D * kSteps;
+  const int64_t warps = ((int64_t)a.c.n_tokens + kTokens - 1) / kTokens * 2 * a.c.Hkv;
+  cache_append_kernel<D, kE4M3, kSteps><<<(unsigned)((warps * 32 + kRowsThreads - 1) / kRowsThreads), kRowsThreads, 0, s>>>(a);
+  return cudaGetLastError();
+}
+template <int D, bool kE4M3>
+cudaError_t launch_read(const ReadArgs& a, cudaStream_t s) {
+  constexpr int kSteps = 4, kTokens = 512 / D * kSteps;
+  const int64_t warps = ((int64_t)a.c.max_keys + kTokens - 1) / kTokens * 2 * a.c.Hkv;
+  const dim3 grid((unsigned)((warps * 32 + kRowsThreads - 1) / kRowsThreads), a.c.B);
+  cache_read_kernel<D, kE4M3, kSteps><<<grid, kRowsThreads, 0, s>>>(a);
+  return cudaGetLastError();
+}
+
+bool misaligned(const void* p, const void* q) { return (reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & 15; }
+
+}  // namespace
+}  // namespace l2a
+
+using namespace l2a;
+
+extern "C" l2a_status l2a_cache_append(const l2a_params* p, const l2a_cache* c, const void* K, const void* V,
+                                       const int32_t* cu_new, int n_tokens, void* stream) {
+  AppendArgs a;
+  const l2a_status st = cache_view(p, c, cu_new, n_tokens, &a.c);
+  if (st != L2A_OK) return st;
+  if (n_tokens == 0) return L2A_OK;
+  a.k_t = token_stride(p->k_stride, p->Hkv * p->D);
+  a.v_t = token_stride(p->v_stride, p->Hkv * p->D);
+  if (!K || !V || misaligned(K, V) || a.k_t == 0 || a.v_t == 0) return L2A_ERR_INVALID_ARG;
+  a.K = static_cast<const bf16*>(K);
+  a.V = static_cast<const bf16*>(V);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const bool e4m3 = c->kind == L2A_CACHE_E4M3;
+  const cudaError_t e = p->D == 128 ? (e4m3 ? launch_append<128, true>(a, s) : launch_append<128, false>(a, s))
+                                    : (e4m3 ? launch_append<64, true>(a, s) : launch_append<64, false>(a, s));
+  return e == cudaSuccess ? L2A_OK : L2A_ERR_CUDA;
+}
+
+extern "C" l2a_status l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t* first, void* K_out, void* V_out,
+                                     void* stream) {
+  ReadArgs a;
+  const int32_t no_tokens = 0;      // (the new tokens play no part)
+  const l2a_status st = cache_view(p, c, &no_tokens, 0, &a.c);
+  if (st != L2A_OK) return st;
+  if (!K_out || !V_out || misaligned(K_out, V_out)) return L2A_ERR_INVALID_ARG;
+  if (!strides_ok(p->k_stride, p->Lk, p->Hkv * p->D) || !strides_ok(p->v_stride, p->Lk, p->Hkv * p->D)) return L2A_ERR_INVALID_ARG;
+  if (p->B > 65535) return L2A_ERR_UNSUPPORTED;
+  a.c.cu_new = nullptr;
+  a.first = first;
+  a.K = static_cast<bf16*>(K_out);
+  a.V = static_cast<bf16*>(V_out);
+  a.k_st = resolve_strides(p->k_stride, p->Lk, p->Hkv * p->D);
+  a.v_st = resolve_strides(p->v_stride, p->Lk, p->Hkv * p->D);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const bool e4m3 = c->kind == L2A_CACHE_E4M3;
+  const cudaError_t e = p->D == 128 ? (e4m3 ? launch_read<128, true>(a, s) : launch_read<128, false>(a, s))
+                                    : (e4m3 ? launch_read<64, true>(a, s) : launch_read<64, false>(a, s));
+  return e == cudaSuccess ? L2A_OK : L2A_ERR_CUDA;
+}

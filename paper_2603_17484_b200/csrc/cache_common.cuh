@@ -1,0 +1,55 @@
+// What the kernels of the paged key/value cache share: the cache as the device sees it, positions of the new tokens, the
+// conversion of 8-bit rows.
+#pragma once
+#include "l2a_common.cuh"
+
+namespace l2a {
+
+struct CacheView {
+  uint8_t *K, *V;              // pools, as bytes
+  uint8_t *ks, *vs;            // exponents + 127 (E4M3)
+  int64_t page_bytes, scale_stride;
+  int kind, n_pages, page_shift, table_stride;
+  int max_keys;                // positions that the table and p->Lk allow
+  const int32_t *table, *lengths;
+  const int32_t* cu_new;       // NULL: every sequence has Lq new tokens
+  int B, Lq, Hkv, D, n_tokens;
+};
+
+// Host side: checks a cache call's parameters and fills the view.
+l2a_status cache_view(const l2a_params* p, const l2a_cache* c, const int32_t* cu_new, int n_tokens, CacheView* v);
+
+__device__ __forceinline__ int cache_length(const CacheView& c, int b) { return min(max(c.lengths[b], 0), c.max_keys); }
+
+// New tokens of sequence b: first row of the token axis and their number (0 where cu_new breaks its bounds)
+__device__ __forceinline__ int cache_new(const CacheView& c, int b, int& first) {
+  if (c.cu_new == nullptr) {
+    first = b * c.Lq;
+    return c.Lq;
+  }
+  first = c.cu_new[b];
+  const int n = c.cu_new[b + 1] - first;
+  return first >= 0 && n > 0 && n <= c.Lq && first <= c.n_tokens - n ? n : 0;
+}
+
+// Page of a position of sequence b, -1: none
+__device__ __forceinline__ int cache_page(const CacheView& c, int b, int pos) {
+  const int page = c.table[(int64_t)b * c.table_stride + (pos >> c.page_shift)];
+  return page >= 0 && page < c.n_pages ? page : -1;
+}
+
+// Two e4m3 codes as fp16, exactly
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t codes) {
+  uint32_t r;
+  asm("{\n .reg .b16 c;\n cvt.u16.u32 c, %1;\n cvt.rn.f16x2.e4m3x2 %0, c;\n}" : "=r"(r) : "r"(codes));
+  return r;
+}
+__device__ __forceinline__ float2 f16x2_to_float2(uint32_t v) {
+  float2 f;
+  asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}" : "=f"(f.x), "=f"(f.y) : "r"(v));
+  return f;
+}
+// 2^e of a stored exponent (0 and 255, which no row is written with, stand for 0 and infinity)
+__device__ __forceinline__ float scale_of_exponent(uint32_t biased) { return __uint_as_float(biased << 23); }
+
+}  // namespace l2a

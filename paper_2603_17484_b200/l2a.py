@@ -25,6 +25,8 @@ FLAG_SHARED_WINDOW = 64
 ROUTER_MASK_U8 = 0
 ROUTER_LOGITS_F32 = 1
 ROUTER_LOGITS_BF16 = 2
+CACHE_BF16 = 0
+CACHE_E4M3 = 1
 
 EXPORTS = (
     "l2a_version", "l2a_status_string", "l2a_workspace_bytes", "l2a_workspace_status",
@@ -32,6 +34,7 @@ EXPORTS = (
     "l2a_route_compact_static", "l2a_router_logits", "l2a_decode_workspace_bytes", "l2a_decode",
     "l2a_backward_split", "l2a_router_backward", "l2a_forward_routed", "l2a_selftest_wait_timeout",
     "l2a_forward_sets", "l2a_backward_sets", "l2a_pack_sequences", "l2a_step_host_async", "l2a_step_host_wait",
+    "l2a_cache_append", "l2a_cache_read", "l2a_cache_workspace_bytes", "l2a_cache_forward",
 )
 
 
@@ -44,6 +47,16 @@ class L2AParams(ctypes.Structure):
         ("q_stride", ctypes.c_int64 * 2), ("k_stride", ctypes.c_int64 * 2),
         ("v_stride", ctypes.c_int64 * 2), ("o_stride", ctypes.c_int64 * 2),
         ("seq_bounds", ctypes.c_void_p),
+    ]
+
+
+class L2ACache(ctypes.Structure):
+    """l2a_cache of include/l2a.h; made by `cache`, which keeps the tensors alive."""
+    _fields_ = [
+        ("K", ctypes.c_void_p), ("V", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("page_stride", ctypes.c_int64), ("scale_stride", ctypes.c_int64),
+        ("kind", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+        ("table_stride", ctypes.c_int32), ("page_table", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
     ]
 
 
@@ -66,6 +79,10 @@ _SIGNATURES = {
     "l2a_forward_sets": "ppppppp" + "pppp" + "ppppp" + "pzp",
     "l2a_backward_sets": "ppppppp" + "pppp" + "ppppp" + "ppppppp" + "pzp",
     "l2a_router_backward": "ppppp" + "f" + "pppppp",
+    "l2a_cache_append": "ppppp" + "ip",
+    "l2a_cache_read": "pppppp",
+    "l2a_cache_workspace_bytes": "ppip",
+    "l2a_cache_forward": "pppp" + "i" + "pp" + "pzp",
 }
 
 _lib = None
@@ -108,6 +125,32 @@ def params(B, Lq, Lk, Hq, Hkv, D, window, q_pos_offset=None, softmax_scale=0.0, 
     st = [two(*(s if s is not None else (0, 0))) for s in (q_stride, k_stride, v_stride, o_stride)]
     return L2AParams(B, Lq, Lk, Hq, Hkv, D, window, Lk - Lq if q_pos_offset is None else q_pos_offset,
                      softmax_scale, flags, *st, None if seq_bounds is None else seq_bounds.data_ptr())
+
+
+def cache(K, V, page_table, lengths, k_scale=None, v_scale=None) -> L2ACache:
+    """Description of a paged cache (see include/l2a.h).  K, V: pools [pages, Hkv, page size, D], bf16, or 8-bit codes
+    (torch.float8_e4m3fn or uint8) with the exponents k_scale, v_scale (uint8 [pages, Hkv, page size]); a page itself is dense, the
+    pages may be further apart.  page_table: int32 [B, pages of a sequence], lengths: int32 [B]."""
+    def stride(x, y):
+        dense = tuple(torch.empty(x.shape[1:], device="meta").stride())
+        if x.shape != y.shape or x.stride() != y.stride() or x.stride()[1:] != dense:
+            raise ValueError("K and V (and their scales) have the same shape and strides, and dense pages")
+        return x.stride(0) if x.shape[0] > 1 else 0
+
+    kind = CACHE_BF16 if K.dtype == torch.bfloat16 else CACHE_E4M3
+    if K.dtype != V.dtype or K.element_size() != (2 if kind == CACHE_BF16 else 1):
+        raise ValueError("a cache holds bf16 values or 8-bit codes, K and V alike")
+    if (kind == CACHE_E4M3) != (k_scale is not None and v_scale is not None):
+        raise ValueError("8-bit codes need their exponents, bf16 values have none")
+    if kind == CACHE_E4M3 and (k_scale.dtype != torch.uint8 or v_scale.dtype != torch.uint8 or k_scale.shape != K.shape[:3]):
+        raise ValueError("k_scale, v_scale: uint8 [pages, Hkv, page size]")
+    if page_table.dtype != torch.int32 or lengths.dtype != torch.int32 or page_table.stride(-1) != 1:
+        raise ValueError("page_table [B, n] and lengths [B] are int32")
+    c = L2ACache(_addr(K), _addr(V), _addr(k_scale), _addr(v_scale), stride(K, V),
+                 0 if kind == CACHE_BF16 else stride(k_scale, v_scale), kind, K.shape[0], K.shape[2],
+                 page_table.stride(0) if page_table.shape[0] > 1 else page_table.shape[1], _addr(page_table), _addr(lengths))
+    c.tensors = (K, V, k_scale, v_scale, page_table, lengths)
+    return c
 
 
 def _addr(t):
@@ -199,6 +242,40 @@ def l2a_decode(p, q, K, V, d, O, ws, stream=None, check=True) -> int:
                             _bytes(ws), _raw_stream(stream))
     if check:
         _check(code, "l2a_decode")
+    return code
+
+
+def l2a_cache_append(p, cache, K, V, cu_new, n_tokens, stream=None, check=True) -> int:
+    """Writes the new tokens' keys and values [n_tokens, Hkv, D] into their pages, quantised where the cache is."""
+    code = lib().l2a_cache_append(ctypes.byref(p), ctypes.byref(cache), _addr(K), _addr(V), _addr(cu_new), n_tokens,
+                                  _raw_stream(stream))
+    if check:
+        _check(code, "l2a_cache_append")
+    return code
+
+
+def l2a_cache_read(p, cache, first, K_out, V_out, stream=None, check=True) -> int:
+    """Reads the cache back as dense bf16 [B, Lk, Hkv, D], from position first[b] on (None: 0)."""
+    code = lib().l2a_cache_read(ctypes.byref(p), ctypes.byref(cache), _addr(first), _addr(K_out), _addr(V_out),
+                                _raw_stream(stream))
+    if check:
+        _check(code, "l2a_cache_read")
+    return code
+
+
+def l2a_cache_workspace_bytes(p, cache, n_tokens) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().l2a_cache_workspace_bytes(ctypes.byref(p), ctypes.byref(cache), n_tokens, ctypes.byref(n)),
+           "l2a_cache_workspace_bytes")
+    return n.value
+
+
+def l2a_cache_forward(p, cache, Q, cu_new, n_tokens, d, O, ws, stream=None, check=True) -> int:
+    """Attention of the new tokens over the cache: the window for all, every key for the routed ones (d), o = s + d * a."""
+    code = lib().l2a_cache_forward(ctypes.byref(p), ctypes.byref(cache), _addr(Q), _addr(cu_new), n_tokens, _addr(d), _addr(O),
+                                   _addr(ws), _bytes(ws), _raw_stream(stream))
+    if check:
+        _check(code, "l2a_cache_forward")
     return code
 
 
