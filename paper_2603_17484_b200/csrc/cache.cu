@@ -42,6 +42,20 @@ l2a_status cache_view(const l2a_params* p, const l2a_cache* c, const int32_t* cu
   return L2A_OK;
 }
 
+bool encode_pool_map(CUtensorMap* map, const CacheView& c, const void* pool, int box_rows, int box_pieces) {
+  const cuuint64_t page = 1ull << c.page_shift, D = c.D, pages = c.n_pages, stride = c.page_bytes;
+  const cuuint32_t rows = box_rows;
+  if (c.kind == L2A_CACHE_E4M3) {
+    const cuuint64_t dims[4] = {D, page, (cuuint64_t)c.Hkv, pages}, strides[3] = {D, page * D, stride};
+    const cuuint32_t box[4] = {(cuuint32_t)c.D, rows, 1, 1};
+    return encode_tiled_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, pool, dims, strides, box,
+                            c.D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+  }
+  const cuuint64_t dims[5] = {64, page, D / 64, (cuuint64_t)c.Hkv, pages}, strides[4] = {2 * D, 128, 2 * page * D, stride};
+  const cuuint32_t box[5] = {64, rows, (cuuint32_t)box_pieces, 1, 1};
+  return encode_tiled_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, pool, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
 namespace {
 
 constexpr int kRowsThreads = 256;

@@ -2,6 +2,7 @@
 // conversion of 8-bit rows.
 #pragma once
 #include "l2a_common.cuh"
+#include "sm100_prims.cuh"
 
 namespace l2a {
 
@@ -38,6 +39,32 @@ __device__ __forceinline__ int cache_page(const CacheView& c, int b, int pos) {
   return page >= 0 && page < c.n_pages ? page : -1;
 }
 
+// A forward call over the cache.
+struct CacheFwdArgs {
+  CacheView c;
+  int Hq, G, window;
+  float scale_log2;
+  int local, global, add;      // which modules run; add: O holds s already
+  int shift;                   // a routed row at position p sees the keys 0 .. p - shift besides what Local Attention sees:
+                               // window + 1 where that runs, else 0
+  const bf16* q;               // [n_tokens, Hq, D], token strides q_t, o_t
+  int64_t q_t, o_t;
+  const uint8_t* d;            // routing decisions, NULL: none
+  bf16* O;
+  int* status;                 // workspace: status word,
+  int* plan;                   // few rows: tiles of a CTA, first tile of every sequence;
+  float* part;                 // rows of the parts
+};
+
+// Sequences whose new tokens have at most kFewRows rows (tokens x heads of a KV group): cache_few.cu
+constexpr int kFewRows = 16;
+size_t cache_few_ws_bytes(const l2a_params* p);     // plan and parts
+cudaError_t launch_cache_few(CacheFwdArgs& a, void* ws, cudaStream_t s);
+
+// Tensor map over a pool: {elements of 128 bytes at most, tokens, (pieces of a row,) heads, pages}; one copy brings box_rows
+// tokens of one head of one page, box_pieces * 64 elements of each (bf16) or the whole row of codes.
+bool encode_pool_map(CUtensorMap* map, const CacheView& c, const void* pool, int box_rows, int box_pieces);
+
 // Two e4m3 codes as fp16, exactly
 __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t codes) {
   uint32_t r;
@@ -48,6 +75,23 @@ __device__ __forceinline__ float2 f16x2_to_float2(uint32_t v) {
   float2 f;
   asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}" : "=f"(f.x), "=f"(f.y) : "r"(v));
   return f;
+}
+// Copies from one page: K or V rows of a head; untiled for their exponents (16 bytes or a multiple, 16-byte aligned)
+__device__ __forceinline__ void tma_load_page(void* dst, const CUtensorMap* map, uint64_t* bar, bool e4m3, int piece, int row,
+                                              int head, int page) {
+  if (e4m3) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+        ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(0), "r"(row), "r"(head), "r"(page) : "memory");
+  } else {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];"
+        ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(0), "r"(row), "r"(piece), "r"(head), "r"(page) : "memory");
+  }
+}
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
 // 2^e of a stored exponent (0 and 255, which no row is written with, stand for 0 and infinity)
 __device__ __forceinline__ float scale_of_exponent(uint32_t biased) { return __uint_as_float(biased << 23); }

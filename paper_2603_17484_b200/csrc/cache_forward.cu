@@ -8,18 +8,6 @@ namespace l2a {
 
 namespace {
 
-struct CacheFwdArgs {
-  CacheView c;
-  int Hq, G, window;
-  float scale_log2;
-  int local, global, add;      // which modules run; add: O holds s already
-  const bf16* q;
-  int64_t q_t, o_t;
-  const uint8_t* d;
-  bf16* O;
-  int* status;
-};
-
 constexpr int kWarps = 4;
 
 // One CTA = one query row of one head; a warp takes every fourth key, a lane D / 32 elements.
@@ -28,11 +16,12 @@ __global__ void __launch_bounds__(kWarps * 32) cache_forward_kernel(const CacheF
   constexpr int kE = D / 32;
   const CacheView& c = a.c;
   const int t = blockIdx.x, h = blockIdx.y, g = h / a.G, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  if (t == 0 && h == 0 && threadIdx.x == 0) *a.status = 0;
+  if (a.G > kFewRows && t == 0 && h == 0 && threadIdx.x == 0) *a.status = 0;
   int b = 0, first, n = 0;
   if (c.cu_new == nullptr) b = t / c.Lq;
   else while (b + 1 < c.B && c.cu_new[b + 1] <= t) ++b;
   n = cache_new(c, b, first);
+  if (n * a.G <= kFewRows) return;
   const int i = t - first;
   const int pos = i >= 0 && i < n ? cache_length(c, b) - n + i : -1;
   const bool routed = a.global && a.d != nullptr && a.d[t] != 0;
@@ -124,7 +113,7 @@ extern "C" l2a_status l2a_cache_workspace_bytes(const l2a_params* p, const l2a_c
   const l2a_status st = check_forward(p, c, n_tokens, &v);
   if (st != L2A_OK) return st;
   if (!ws_bytes) return L2A_ERR_INVALID_ARG;
-  *ws_bytes = kWsHeaderBytes;
+  *ws_bytes = kWsHeaderBytes + cache_few_ws_bytes(p);
   return L2A_OK;
 }
 
@@ -137,20 +126,29 @@ extern "C" l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c,
   a.q_t = row_stride(p->q_stride, p->Hq * p->D);
   a.o_t = row_stride(p->o_stride, p->Hq * p->D);
   if (a.q_t == 0 || a.o_t == 0) return L2A_ERR_INVALID_ARG;
-  if (!ws || (reinterpret_cast<uintptr_t>(ws) % 256) != 0 || ws_bytes < kWsHeaderBytes) return L2A_ERR_WORKSPACE;
+  size_t need = 0;
+  st = l2a_cache_workspace_bytes(p, c, n_tokens, &need);
+  if (st != L2A_OK) return st;
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) % 256) != 0 || ws_bytes < need) return L2A_ERR_WORKSPACE;
   if (n_tokens == 0) return L2A_OK;
   if (!Q || !O || ((reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(O)) & 15)) return L2A_ERR_INVALID_ARG;
   a.Hq = p->Hq; a.G = p->Hq / p->Hkv;
-  a.window = p->window;
+  a.window = p->window < p->Lk ? p->window : p->Lk;       // (no key is further away)
   a.scale_log2 = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->D)) * 1.4426950408889634f;
   a.add = (p->flags & L2A_FLAG_GLOBAL_PHASE) != 0;
   a.local = !a.add && !(p->flags & L2A_FLAG_SKIP_LOCAL);
   a.global = !(p->flags & L2A_FLAG_SKIP_GLOBAL);
+  a.shift = a.local ? a.window + 1 : 0;
   a.q = static_cast<const bf16*>(Q);
   a.d = d;
   a.O = static_cast<bf16*>(O);
   a.status = static_cast<int*>(ws);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (a.G <= kFewRows) {
+    const cudaError_t e = launch_cache_few(a, static_cast<uint8_t*>(ws) + kWsHeaderBytes, s);
+    if (e != cudaSuccess) return L2A_ERR_CUDA;
+    if ((int64_t)p->Lq * a.G <= kFewRows) return L2A_OK;
+  }
   const dim3 grid(n_tokens, p->Hq);
   if (p->D == 128) cache_forward_kernel<128><<<grid, kWarps * 32, 0, s>>>(a);
   else cache_forward_kernel<64><<<grid, kWarps * 32, 0, s>>>(a);

@@ -62,6 +62,10 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 bool encode_rows_map(CUtensorMap* map, const void* base, int batch, int rows, int row_elems, int box_rows,
                      int head_dim, int64_t batch_stride = 0, int64_t token_stride = 0);   // strides in elements; 0 = dense
 
+// The driver's cuTensorMapEncodeTiled (128-bytes-swizzled or, for rows of 64 bytes, 64-bytes-swizzled boxes); false on failure.
+bool encode_tiled_map(CUtensorMap* map, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims,
+                      const cuuint64_t* strides, const cuuint32_t* box, CUtensorMapSwizzle swizzle);
+
 // Strides of a [B, L, H, D] tensor in elements ({batch, token}); heads and head values are contiguous.
 struct RowStrides {
   int64_t b, t;
