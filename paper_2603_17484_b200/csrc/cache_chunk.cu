@@ -1,0 +1,984 @@
+// Attention over the paged cache for sequences with more query rows (the next chunk of a prompt): rows are the new tokens of
+// a sequence times the G heads of a KV group, packed (row i * G + h), 256 of them to a group.  Two kinds of groups:
+//   segment 0: all rows; keys max(0, p - W) .. p (Local Attention)
+//   segment 1: the rows of routed tokens, compacted; keys 0 .. p - W - 1 (with segment 0 what Global Attention sees)
+// so that the scores inside a window are computed once.  s and a are weighted sums of both segments' results.
+//
+// cache_plan_kernel   : one CTA.  Compacts the routed tokens, lists the groups with their key blocks (of 128), and divides the key
+//                       blocks of all groups and KV heads, laid end to end, evenly among the CTAs.
+// cache_chunk_kernel  : one CTA an SM takes its range, a few pieces of (group, KV head).  A row whose piece is all there is leaves
+//                       finished; other rows go to the piece's slot of the workspace, unnormalised.
+// cache_join_kernel   : joins the slots of a row.
+//
+// A piece: two query tiles of 128 rows share the stream of key blocks; a group of at most 128 rows is in both tiles, which then
+// take every other key block each.
+//   warps 0-7   : soft-max, correction and epilogue, one thread a row; they also gather the rows of Q
+//   warp 8      : TMA producer, one copy a page (and 64 columns in bf16)
+//   warp 9      : tcgen05 MMA issuer and TMEM owner
+//   warps 12-15 : one thread a key.  e4m3: decode the codes that arrive in a raw ring to bf16 times the key's power of
+//                 two, which is exact, in the layout the MMA operands have; the products then run as for a bf16 cache.
+//                 Both kinds: zeros for the values of keys that no row of the group sees (their slots may hold anything).
+#include <math.h>
+
+#include <algorithm>
+
+#include "cache_common.cuh"
+
+namespace l2a {
+
+namespace {
+
+constexpr int kStages = 2;
+constexpr int kSoftmaxWarps = 8, kTmaWarp = 8, kMmaWarp = 9, kConvWarp = 12, kConvWarps = 4;
+constexpr int kChunkThreads = 512;
+// The launch has 16 warps of 128 registers; the two warpgroups that do not compute rows give most of theirs away.
+constexpr int kSoftmaxRegs = 200, kOtherRegs = 56;
+static_assert(kSoftmaxWarps * kSoftmaxRegs + 8 * kOtherRegs <= 16 * 128, "register shares exceed the launch allocation");
+constexpr float kRescaleThreshold = 8.0f;  // log2 units
+constexpr int kBoxBytes = 128 * 128;       // 128 rows of 128 bytes
+constexpr int kPlanThreads = 1024;
+constexpr int kCtas = kSplitSms;
+constexpr int kItemCost = 3;               // key blocks' time that a piece costs besides its blocks
+constexpr int kMinCost = 8;                // of a CTA
+constexpr int kMinPiece = 2;
+
+// A group of rows
+struct alignas(16) Group {
+  int b, seg, first, off;        // sequence, segment, its first row of the token axis, position of that row
+  int list, row0, n_rows, dual;  // segment 1: its list of routed tokens starts here; first packed row; rows; one tile twice
+  int key_lo, key_hi, jlo, jhi;  // keys that some row sees, and their blocks (jhi < jlo: none)
+  int base, hi0, lo1, pad;       // first key block of the group's heads in the call; last block of tile 0, first of tile 1
+  int min_hi[2], max_lo[2];      // of each tile: keys from max_lo to min_hi are seen by all its rows
+};
+struct alignas(16) Start { int at, group, head, block; };   // where a CTA's range begins
+
+struct Plan {
+  int n_groups, ctas;
+  Start start[kCtas + 1];
+};
+
+// Workspace: plan, groups, then per token: sequence (-1: none here), rank among the routed of its sequence (-1: no
+// keys before its window to see), list of routed tokens; per sequence: first group of both segments, its part of the list.
+struct ChunkWs {
+  Plan* plan;
+  Group* groups;
+  int *seq, *rank, *list;
+  int *first_group, *list_start, *list_end;   // [2][B], [B], [B]
+  float* part;
+};
+
+__host__ __device__ inline int64_t most_groups(int n_tokens, int G, int B) {
+  return 2 * (((int64_t)n_tokens * G + kRowsPerCta - 1) / kRowsPerCta + B);
+}
+__host__ __device__ constexpr size_t slot_floats(int D) { return (size_t)kRowsPerCta * (D + 2); }
+
+struct ChunkArgs {
+  CacheFwdArgs f;
+  ChunkWs w;
+};
+
+// ------------------------------------------------------------------------------------------------------------- plan
+__device__ __forceinline__ bool is_chunk(const CacheFwdArgs& a, int n) { return (int64_t)n * a.G > kFewRows || (n > 0 && a.G > kFewRows); }
+
+// Inclusive scan over the CTA's threads; `all`: the sum.  Two barriers.
+__device__ __forceinline__ int block_scan(int x, int* sums, int& all) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();
+  if (lane == 31) sums[warp] = x;
+  __syncthreads();
+  int before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 32; ++w) {
+    if (w < warp) before += sums[w];
+    total += sums[w];
+  }
+  all = total;
+  return x + before;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const ChunkArgs p) {
+  const CacheFwdArgs& a = p.f;
+  const CacheView& c = a.c;
+  const ChunkWs& w = p.w;
+  __shared__ int sums[kPlanThreads / 32];
+  const int tid = threadIdx.x;
+  dependents_release();
+  if (a.G > kFewRows && tid == 0) *a.status = 0;       // (else the kernel of the few rows has)
+  // ---- sequence of every token.  (Lists of new tokens that do not ascend: no groups, nothing is stored.)
+  bool bad = false;
+  if (c.cu_new != nullptr)
+    for (int b = tid; b < c.B; b += kPlanThreads) bad |= c.cu_new[b] > c.cu_new[b + 1];
+  bad = __syncthreads_or(bad);
+  for (int t = tid; t < c.n_tokens; t += kPlanThreads) { w.seq[t] = -1; w.rank[t] = -1; }
+  __syncthreads();
+  for (int b = tid >> 5; b < c.B; b += kPlanThreads / 32) {
+    int first;
+    const int n = bad ? 0 : cache_new(c, b, first);
+    if (is_chunk(a, n))
+      for (int i = tid & 31; i < n; i += 32) w.seq[first + i] = b;
+  }
+  __syncthreads();
+  // ---- compact the routed tokens that see keys before their windows
+  int base = 0;
+  for (int t0 = 0; t0 < c.n_tokens; t0 += kPlanThreads) {
+    const int t = t0 + tid, b = t < c.n_tokens ? w.seq[t] : -1;
+    int first = 0, n = 0, take = 0, all;
+    if (b >= 0) {
+      n = cache_new(c, b, first);
+      take = a.global && a.d != nullptr && a.d[t] != 0 && cache_length(c, b) - n + (t - first) - a.shift >= 0;
+    }
+    const int at = base + block_scan(take, sums, all) - take;
+    if (b >= 0 && t == first) w.list_start[b] = at;
+    if (b >= 0 && t == first + n - 1) w.list_end[b] = at + take;
+    if (take) { w.list[at] = t; w.rank[t] = at; }
+    base += all;
+  }
+  __syncthreads();
+  // ---- groups of both segments, sequence by sequence
+  base = 0;
+  for (int b0 = 0; b0 < c.B; b0 += kPlanThreads) {
+    const int b = b0 + tid;
+    int first, n = 0, loc = 0, out = 0, all;
+    if (b < c.B && !bad) n = cache_new(c, b, first);
+    if (is_chunk(a, n)) {
+      loc = a.local ? (int)compact_groups(n, a.G) : 0;
+      out = (int)compact_groups(w.list_end[b] - w.list_start[b], a.G);
+    }
+    const int at = base + block_scan(loc + out, sums, all) - loc - out;
+    if (b < c.B) { w.first_group[b] = at; w.first_group[c.B + b] = at + loc; }
+    base += all;
+  }
+  const int n_groups = base;
+  __syncthreads();
+  for (int q = tid; q < n_groups; q += kPlanThreads) {
+    int b = 0, end = c.B;                              // the last sequence whose groups start at or before q
+    while (end - b > 1) {
+      const int mid = (b + end) >> 1;
+      if (w.first_group[mid] <= q) b = mid; else end = mid;
+    }
+    Group g;
+    const int n = cache_new(c, b, g.first), out0 = w.first_group[c.B + b];
+    g.b = b;
+    g.seg = q >= out0;
+    g.off = cache_length(c, b) - n;
+    g.list = g.seg ? w.list_start[b] : 0;
+    g.row0 = (q - (g.seg ? out0 : w.first_group[b])) * kRowsPerCta;
+    g.n_rows = min(kRowsPerCta, (g.seg ? w.list_end[b] - g.list : n) * a.G - g.row0);
+    g.dual = g.n_rows <= kTileM;
+    const int shift = g.seg ? a.shift : 0;
+    auto pos = [&](int r) {                            // position of packed row r of the group
+      const int i = (g.row0 + r) / a.G;
+      return g.off + (g.seg ? w.list[g.list + i] - g.first : i);
+    };
+    auto low = [&](int x) { return g.seg ? 0 : max(0, x - a.window); };
+    const int p0 = pos(0), p1 = pos(g.dual ? g.n_rows - 1 : kTileM - 1), p2 = g.dual ? p0 : pos(kTileM), p3 = pos(g.n_rows - 1);
+    g.key_lo = low(p0);
+    g.key_hi = p3 - shift;
+    g.jlo = g.key_lo / kTileN;
+    g.jhi = g.key_hi >= 0 ? g.key_hi / kTileN : g.jlo - 1;
+    g.hi0 = g.dual ? g.jhi : p1 - shift >= 0 ? (p1 - shift) / kTileN : g.jlo - 1;
+    g.lo1 = g.dual ? g.jlo : low(p2) / kTileN;
+    g.min_hi[0] = p0 - shift;
+    g.min_hi[1] = p2 - shift;
+    g.max_lo[0] = low(p1);
+    g.max_lo[1] = low(p3);
+    g.base = g.pad = 0;
+    w.groups[q] = g;
+  }
+  __syncthreads();
+  // ---- key blocks and costs, laid end to end: a thread sums a run of groups
+  const int run = (n_groups + kPlanThreads - 1) / kPlanThreads, q0 = min(n_groups, tid * run), q1 = min(n_groups, q0 + run);
+  int blocks = 0, cost = 0, all_blocks, all_cost;
+  for (int k = q0; k < q1; ++k) {
+    const int x = w.groups[k].jhi - w.groups[k].jlo + 1;
+    blocks += x * c.Hkv;
+    cost += x > 0 ? (x + kItemCost) * c.Hkv : 0;
+  }
+  int at = block_scan(blocks, sums, all_blocks) - blocks, cost_at = block_scan(cost, sums, all_cost) - cost;
+  const int ctas = max(1, min(kCtas, all_cost / kMinCost));
+  if (tid == 0) { w.plan->n_groups = n_groups; w.plan->ctas = ctas; }
+  for (int k = tid; k <= kCtas; k += kPlanThreads)
+    if (k == 0 || k >= ctas) w.plan->start[k] = Start{k == 0 ? 0 : all_blocks, 0, 0, 0};
+  for (int k = q0; k < q1; ++k) {
+    const int x = w.groups[k].jhi - w.groups[k].jlo + 1, per = x + kItemCost;
+    w.groups[k].base = at;
+    if (x <= 0) continue;
+    // the ranges that start in this group
+    const int64_t lo = cost_at, hi = lo + (int64_t)per * c.Hkv;
+    for (int64_t i = max((int64_t)1, (lo * ctas + all_cost - 1) / all_cost); i < ctas && i * all_cost / ctas < hi; ++i) {
+      const int in = (int)(i * all_cost / ctas - lo);
+      Start s;
+      s.group = k;
+      s.head = in / per;
+      s.block = max(0, in % per - kItemCost);
+      if (s.block < kMinPiece) s.block = 0;
+      if (s.block > 0 && x - s.block < kMinPiece) { s.block = 0; ++s.head; }
+      s.at = at + s.head * x + s.block;                // (head Hkv, block 0: the start of the next group)
+      w.plan->start[i] = s;
+    }
+    at += x * c.Hkv;
+    cost_at += per * c.Hkv;
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------- pieces
+struct ChunkPiece {
+  int head, j0, j1;        // KV head; key blocks j0 .. j1
+  bool whole;              // all of the group's blocks
+  int item;                // group * Hkv + head
+};
+// The pieces of a CTA's range in order; every warp walks through them by itself.
+struct ChunkWalk {
+  int at, end, group, head, block, n_groups;
+  Group g;
+  __device__ __forceinline__ void load(const ChunkWs& w) {
+    const uint4* src = reinterpret_cast<const uint4*>(w.groups + group);
+    uint4* dst = reinterpret_cast<uint4*>(&g);
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(Group) / 16; ++i) dst[i] = __ldcg(src + i);
+  }
+  __device__ __forceinline__ bool init(const ChunkWs& w) {
+    const int cta = blockIdx.x;
+    n_groups = w.plan->n_groups;
+    const int4 s = __ldcg(reinterpret_cast<const int4*>(&w.plan->start[cta]));
+    at = s.x;
+    group = s.y;
+    head = s.z;
+    block = s.w;
+    end = __ldcg(&w.plan->start[cta + 1].at);
+    if (cta >= w.plan->ctas || at >= end || group >= n_groups) return false;
+    load(w);
+    return true;
+  }
+  __device__ __forceinline__ bool next(const ChunkWs& w, int Hkv, ChunkPiece& p) {
+    if (at >= end) return false;
+    for (;;) {
+      const int n = g.jhi - g.jlo + 1;
+      if (head < Hkv && block < n) break;
+      block = 0;
+      if (++head >= Hkv || n <= 0) {
+        head = 0;
+        if (++group >= n_groups) return false;
+        load(w);
+      }
+    }
+    const int n = g.jhi - g.jlo + 1, take = min(n - block, end - at);
+    p.head = head;
+    p.j0 = g.jlo + block;
+    p.j1 = p.j0 + take - 1;
+    p.whole = take == n;
+    p.item = group * Hkv + head;
+    at += take;
+    block += take;
+    return true;
+  }
+};
+// Whether tile t takes key block j of the piece
+__device__ __forceinline__ bool tile_takes(const Group& g, int t, int j) {
+  return g.dual ? (j & 1) == t : t ? j >= g.lo1 : j <= g.hi0;
+}
+// First and last block of tile t in the piece (first > last: none), and their distance
+struct TileBlocks { int first, last, step; };
+__device__ __forceinline__ TileBlocks tile_blocks(const Group& g, const ChunkPiece& p, int t) {
+  TileBlocks x;
+  if (g.dual) {
+    x.first = p.j0 + ((p.j0 ^ t) & 1);
+    x.last = p.j1 - ((p.j1 ^ t) & 1);
+    x.step = 2;
+  } else {
+    x.first = t ? max(p.j0, g.lo1) : p.j0;
+    x.last = t ? p.j1 : min(p.j1, g.hi0);
+    x.step = 1;
+  }
+  return x;
+}
+
+template <int D, bool kE4M3>
+struct ChunkSmem {
+  static constexpr int kQTileBytes = kTileM * D * 2;
+  static constexpr int kKVTileBytes = kTileN * D * 2;
+  static constexpr int kRawBytes = 64 * D;               // codes of 64 keys
+  static constexpr int kKOff = 2 * kQTileBytes;
+  static constexpr int kVOff = kKOff + kStages * kKVTileBytes;
+  static constexpr int kRawOff = kVOff + kStages * kKVTileBytes;      // K: two halves of a block, V: two
+  static constexpr int kBarOff = kRawOff + (kE4M3 ? 4 * kRawBytes : 0);
+  static constexpr int kTotal = kBarOff + 256 + 1024 /* alignment slack */;
+};
+
+struct ChunkBars {
+  uint64_t q_full[2];
+  uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
+  uint64_t s_full[2], p_half[2], p_full[2], o_final[2];
+  uint64_t raw_full[4], raw_empty[4];     // e4m3: halves of K, of V; bf16: raw_full[stage] of V
+  uint32_t tmem_base;
+  int abort_flag;
+};
+static_assert(sizeof(ChunkBars) <= 256, "barriers");
+
+// 16 codes times a power of two as bf16, exactly (overflow and underflow aside)
+__device__ __forceinline__ void codes_to_bf16(const float4& codes, float scale, uint32_t (&o)[8]) {
+  const uint32_t w[4] = {__float_as_uint(codes.x), __float_as_uint(codes.y), __float_as_uint(codes.z), __float_as_uint(codes.w)};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 lo = f16x2_to_float2(e4m3x2_to_f16x2(w[k] & 0xffffu)), hi = f16x2_to_float2(e4m3x2_to_f16x2(w[k] >> 16));
+    const float2 s = make_float2(scale, scale);
+    const float2 a = __fmul2_rn(lo, s), b = __fmul2_rn(hi, s);
+    o[2 * k] = pack_bf16(a.x, a.y);
+    o[2 * k + 1] = pack_bf16(b.x, b.y);
+  }
+}
+__device__ __forceinline__ void sts128(uint32_t saddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(saddr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+template <int D, bool kE4M3>
+__global__ void __launch_bounds__(kChunkThreads, 1)
+cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const ChunkArgs p) {
+  using SM = ChunkSmem<D, kE4M3>;
+  constexpr int kKSteps = D / 16;      // MMA k-steps of Q*K^T
+  constexpr int kOCol0 = 2 * kTileN;   // first TMEM column of the O accumulators
+  const CacheFwdArgs& a = p.f;
+  const CacheView& c = a.c;
+  const ChunkWs& w = p.w;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sQ = smem;
+  uint8_t* sK = smem + SM::kKOff;
+  uint8_t* sV = smem + SM::kVOff;
+  uint8_t* sRaw = smem + SM::kRawOff;
+  ChunkBars* bar = reinterpret_cast<ChunkBars*>(smem + SM::kBarOff);
+  volatile int* abort_flag = &bar->abort_flag;
+
+  if (tid == kTmaWarp * 32) {
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&bar->q_full[t], kTileM);
+      mbar_init(&bar->s_full[t], 1);
+      mbar_init(&bar->p_half[t], kTileM);
+      mbar_init(&bar->p_full[t], kTileM);
+      mbar_init(&bar->o_final[t], 1);
+    }
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&bar->k_full[s], kE4M3 ? kConvWarps * 32 : 1);
+      mbar_init(&bar->k_empty[s], 1);
+      mbar_init(&bar->v_full[s], kConvWarps * 32);
+      mbar_init(&bar->v_empty[s], 1);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&bar->raw_full[i], 1);
+      mbar_init(&bar->raw_empty[i], kConvWarps / 2);
+    }
+    bar->abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == kMmaWarp) {
+    tmem_alloc(&bar->tmem_base, 512);
+    tmem_relinquish();
+  }
+  dependency_wait();
+  dependents_release();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bar->tmem_base;
+  if (tmem != 0) {
+    // all 512 columns were requested, so the allocation must start at column 0 (the MMA warp relies on it)
+    __syncthreads();
+    if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+    if (tid == 0) atomicExch(a.status, 3);
+    return;
+  }
+
+  if (warp == kTmaWarp) {
+    // =========================================================================== TMA producer
+    setmaxnreg_dec<kOtherRegs>();
+    if (lane == 0) {
+      tma_prefetch_desc(&mapK);
+      tma_prefetch_desc(&mapV);
+    }
+    ChunkWalk walk;
+    ChunkPiece pc;
+    bool ok = walk.init(w);
+    // rows of a copy; a lane copies page `u` (bf16: columns `piece`) of a block, e4m3: of half a block
+    const int rows_shift = min(c.page_shift, kE4M3 ? 6 : 7), rows = 1 << rows_shift;
+    const int copies = (kE4M3 ? 64 : 128) >> rows_shift, u = lane % copies, piece = lane / copies;
+    const bool active = piece < (kE4M3 ? 1 : D / 64);
+    const uint32_t bytes = rows * (kE4M3 ? D : 128);
+    uint32_t it = 0;
+    while (ok && walk.next(w, c.Hkv, pc)) {
+      const Group& g = walk.g;
+      const int first_entry = g.key_lo >> c.page_shift, last_entry = g.key_hi >> c.page_shift;
+      int entry0 = -512, page_ids = -1;
+      for (int j = pc.j0; ok && j <= pc.j1; ++j, ++it) {
+        const int s = it & 1;
+        const uint32_t ph = kE4M3 ? it & 1 : (it >> 1) & 1;
+#pragma unroll
+        for (int i = 0; i < (kE4M3 ? 4 : 2); ++i) {      // e4m3: halves of K, of V; bf16: K, V
+          const bool value = kE4M3 ? i >= 2 : i == 1;
+          const int key = j * kTileN + (kE4M3 ? (i & 1) * 64 : 0) + u * rows, entry = key >> c.page_shift;
+          if (((j * kTileN + kTileN - 1) >> c.page_shift) - entry0 >= 32) {
+            entry0 = (j * kTileN) >> c.page_shift;
+            const int e = entry0 + lane;
+            page_ids = e >= first_entry && e <= last_entry ? cache_page(c, g.b, e << c.page_shift) : -1;
+          }
+          const int page = __shfl_sync(0xffffffffu, page_ids, entry - entry0);
+          const bool load = active && page >= 0 && key <= g.key_hi && key + rows > g.key_lo;
+          const uint32_t expect = __popc(__ballot_sync(0xffffffffu, load)) * bytes;
+          uint64_t* full = kE4M3 ? &bar->raw_full[i] : value ? &bar->raw_full[s] : &bar->k_full[s];
+          uint64_t* empty = kE4M3 ? &bar->raw_empty[i] : value ? &bar->v_empty[s] : &bar->k_empty[s];
+          if (!mbar_wait_warp(empty, ph ^ 1, abort_flag)) { ok = false; break; }
+          if (lane == 0) mbar_expect_tx(full, expect);
+          __syncwarp();
+          if (load) {
+            uint8_t* dst = kE4M3 ? sRaw + i * SM::kRawBytes + u * rows * D
+                                 : (value ? sV : sK) + s * SM::kKVTileBytes + piece * kBoxBytes + u * rows * 128;
+            tma_load_page(dst, value ? &mapV : &mapK, full, kE4M3, piece, key & ((1 << c.page_shift) - 1), pc.head, page);
+          }
+        }
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    // =========================================================================== MMA issuer
+    setmaxnreg_dec<kOtherRegs>();
+    if (elect_one()) {
+      constexpr uint32_t tmem = 0;   // checked above: TMEM operand addresses are immediates in this loop
+      constexpr uint32_t idesc_qk = idesc_bf16_f32(kTileM, kTileN, 0, 0);
+      constexpr uint32_t idesc_pv = idesc_bf16_f32(kTileM, D, 0, 1);
+      const uint64_t dq0 = smem_desc_sw128(smem_u32(sQ), 16, 1024);
+      const uint64_t dq1 = smem_desc_sw128(smem_u32(sQ + SM::kQTileBytes), 16, 1024);
+      const uint64_t dk0 = smem_desc_sw128(smem_u32(sK), 16, 1024);
+      const uint64_t dk1 = smem_desc_sw128(smem_u32(sK + SM::kKVTileBytes), 16, 1024);
+      const uint64_t dv0 = smem_desc_sw128(smem_u32(sV), kBoxBytes, 1024);
+      const uint64_t dv1 = smem_desc_sw128(smem_u32(sV + SM::kKVTileBytes), kBoxBytes, 1024);
+      uint32_t p_cnt[2] = {0, 0}, q_cnt[2] = {0, 0};
+      bool started[2];
+
+      auto issue_qk = [&](int t, int s) {
+        const uint64_t qd = t ? dq1 : dq0, kd = s ? dk1 : dk0;
+        const uint32_t d = tmem + t * kTileN;
+#pragma unroll
+        for (int kk = 0; kk < kKSteps; ++kk) {
+          const uint32_t o = ((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4;
+          mma_ss(d, qd + o, kd + o, idesc_qk, kk > 0);
+        }
+        tc_commit(&bar->s_full[t]);
+      };
+      auto issue_pv = [&](int t, int s, int half, uint32_t acc) {   // P*V of 64 keys
+        const uint64_t vd = s ? dv1 : dv0;
+        const uint32_t d = tmem + kOCol0 + t * D, q = tmem + t * kTileN + half * 64;
+#pragma unroll
+        for (int kk = 0; kk < kTileN / 32; ++kk)
+          mma_ts(d, q + kk * 8, vd + (((half * 4 + kk) * 2048) >> 4), idesc_pv, kk > 0 ? 1u : acc);
+      };
+
+      ChunkWalk walk;
+      ChunkPiece pc;
+      bool ok = walk.init(w);
+      uint32_t it = 0;
+      while (ok && walk.next(w, c.Hkv, pc)) {
+        const TileBlocks tb[2] = {tile_blocks(walk.g, pc, 0), tile_blocks(walk.g, pc, 1)};
+        const bool dual = walk.g.dual;
+        auto takes = [&](int t, int j) {
+          return t ? j >= tb[1].first && j <= tb[1].last && (!dual || (j & 1)) : j >= tb[0].first && j <= tb[0].last && (!dual || !(j & 1));
+        };
+        // scores of block j for tile t; the tile's rows of Q arrive with its first block
+        auto scores = [&](int t, int j, int s) {
+          if (!started[t]) {
+            if (!mbar_spin(&bar->q_full[t], q_cnt[t] & 1, abort_flag)) { ok = false; return; }
+            ++q_cnt[t];
+            started[t] = true;
+            tc_fence_after();
+          }
+          issue_qk(t, s);
+        };
+        started[0] = started[1] = false;
+        {
+          const int s = it & 1;
+          if (!mbar_spin(&bar->k_full[s], (it >> 1) & 1, abort_flag)) ok = false;
+          tc_fence_after();
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            if (ok && takes(t, pc.j0)) scores(t, pc.j0, s);
+          if (ok) tc_commit(&bar->k_empty[s]);
+        }
+        for (int j = pc.j0; ok && j <= pc.j1; ++j, ++it) {
+          const int s = it & 1, sn = s ^ 1;
+          // both operand blocks of this step are waited for ahead of the probabilities
+          if (!mbar_spin(&bar->v_full[s], (it >> 1) & 1, abort_flag)) { ok = false; break; }
+          if (j < pc.j1 && !mbar_spin(&bar->k_full[sn], ((it + 1) >> 1) & 1, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (ok && takes(t, j)) {
+              const uint32_t pp = p_cnt[t] & 1;
+              if (!mbar_spin(&bar->p_half[t], pp, abort_flag)) { ok = false; break; }
+              tc_fence_after();
+              issue_pv(t, s, 0, j > tb[t].first ? 1u : 0u);
+              if (!mbar_spin(&bar->p_full[t], pp, abort_flag)) { ok = false; break; }
+              ++p_cnt[t];
+              tc_fence_after();
+              issue_pv(t, s, 1, 1u);
+              if (j == tb[t].last) tc_commit(&bar->o_final[t]);
+            }
+            if (ok && j < pc.j1 && takes(t, j + 1)) scores(t, j + 1, sn);
+          }
+          if (!ok) break;
+          tc_commit(&bar->v_empty[s]);
+          if (j < pc.j1) tc_commit(&bar->k_empty[sn]);
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp >= kConvWarp) {
+    // =========================================================================== decoding and clearing
+    setmaxnreg_dec<kOtherRegs>();
+    const int row = (warp - kConvWarp) * 32 + lane, half = (warp - kConvWarp) >> 1;      // this thread's key of a block
+    ChunkWalk walk;
+    ChunkPiece pc;
+    bool ok = walk.init(w);
+    uint32_t it = 0;
+    while (ok && walk.next(w, c.Hkv, pc)) {
+      const Group& g = walk.g;
+      // exponents of the key's rows of K and V, fetched a block ahead
+      auto fetch = [&](int j) -> uint32_t {
+        const int key = j * kTileN + row;
+        if (!kE4M3 || key < g.key_lo || key > g.key_hi) return 0u;
+        const int page = cache_page(c, g.b, key);
+        if (page < 0) return 0u;
+        const int64_t at = page * c.scale_stride + ((int64_t)pc.head << c.page_shift) + (key & ((1 << c.page_shift) - 1));
+        return c.ks[at] | (uint32_t)c.vs[at] << 8;
+      };
+      uint32_t exps = fetch(pc.j0);
+      for (int j = pc.j0; ok && j <= pc.j1; ++j, ++it) {
+        const int s = it & 1, key = j * kTileN + row;
+        const uint32_t ph = (it >> 1) & 1;
+        const bool seen = key >= g.key_lo && key <= g.key_hi;
+        const uint32_t ahead = j < pc.j1 ? fetch(j + 1) : 0u;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {                    // K, V
+          uint8_t* tile = (i ? sV : sK) + s * SM::kKVTileBytes;
+          const uint32_t dst = smem_u32(tile) + row * 128;
+          if (kE4M3) {
+            const int slot = 2 * i + half;
+            if (!mbar_wait_warp(&bar->raw_full[slot], it & 1, abort_flag)) { ok = false; break; }
+            const uint32_t src = smem_u32(sRaw + slot * SM::kRawBytes) + (row & 63) * D;
+            const float scale = scale_of_exponent(i ? exps >> 8 : exps & 0xffu);
+            float4 x[D / 16];
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) x[k] = lds128(src + ((D == 128 ? k ^ (row & 7) : k ^ ((row >> 1) & 3)) << 4));
+            if (!mbar_wait_warp(i ? &bar->v_empty[s] : &bar->k_empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+              uint32_t o[8];
+              codes_to_bf16(x[k], scale, o);
+              if (!seen) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = 0u;
+              }
+              const uint32_t at = dst + (k >> 2) * kBoxBytes;
+              sts128(at + (((2 * k) & 7 ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
+              sts128(at + (((2 * k + 1) & 7 ^ (row & 7)) << 4), o[4], o[5], o[6], o[7]);
+            }
+            fence_async_smem();
+            mbar_arrive(i ? &bar->v_full[s] : &bar->k_full[s]);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar->raw_empty[slot]);
+          } else if (i == 1) {
+            if (!mbar_wait_warp(&bar->raw_full[s], ph, abort_flag)) { ok = false; break; }
+            if (!seen) {
+#pragma unroll
+              for (int k = 0; k < D / 8; ++k) sts128(dst + (k >> 3) * kBoxBytes + ((k & 7) << 4), 0u, 0u, 0u, 0u);
+              fence_async_smem();
+            }
+            mbar_arrive(&bar->v_full[s]);
+          }
+        }
+        exps = ahead;
+      }
+    }
+  } else if (warp > kMmaWarp) {
+    setmaxnreg_dec<kOtherRegs>();     // idle warps of the third warpgroup
+  } else {
+    // =========================================================================== soft-max warpgroups
+    setmaxnreg_inc<kSoftmaxRegs>();
+    const int t = warp >> 2;                 // tile of this warpgroup
+    const int r = (warp & 3) * 32 + lane;    // row inside the tile == TMEM lane
+    const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_addr = tmem + lane_base + t * kTileN;        // this row's 128 score columns
+    const uint32_t o_addr = tmem + lane_base + kOCol0 + t * D;    // its D accumulator columns
+    ChunkWalk walk;
+    ChunkPiece pc;
+    bool ok = walk.init(w);
+    uint32_t s_cnt = 0, o_cnt = 0;
+    while (ok && walk.next(w, c.Hkv, pc)) {
+      const Group& g = walk.g;
+      const TileBlocks tb = tile_blocks(g, pc, t);
+      const int tile_row = (g.dual ? 0 : t * kTileM) + r;          // row of the group
+      const bool valid = tile_row < g.n_rows;
+      const bool any = tb.first <= tb.last;
+      int token = g.first, head = 0, row_lo = 0x3fffffff, row_hi = -1;
+      if (valid) {
+        const int x = g.row0 + tile_row, i = x / a.G;
+        token = g.seg ? __ldcg(w.list + g.list + i) : g.first + i;
+        head = pc.head * a.G + x - i * a.G;
+        const int pos = g.off + token - g.first;
+        row_hi = pos - (g.seg ? a.shift : 0);
+        row_lo = g.seg ? 0 : pos - a.window;
+      }
+      float m_use = -INFINITY;   // reference maximum, exp2 domain
+      float l = 0.f;             // row sum
+      if (any) {
+        // ---- the warp's 32 rows of Q, 16-byte pieces, in the layout a TMA copy would leave
+        constexpr int kPieces = D / 8, kRowsPerStep = 32 / kPieces;
+        const bf16* src = valid ? a.q + token * a.q_t + (int64_t)head * D : nullptr;
+        const int piece = lane % kPieces;
+        uint4 x[kPieces];
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+          const bf16* q = reinterpret_cast<const bf16*>(
+              __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), k * kRowsPerStep + lane / kPieces));
+          x[k] = q != nullptr ? __ldcg(reinterpret_cast<const uint4*>(q) + piece) : make_uint4(0, 0, 0, 0);
+        }
+        const uint32_t dst = smem_u32(sQ + t * SM::kQTileBytes) + (piece >> 3) * kBoxBytes;
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+          const int rr = (warp & 3) * 32 + k * kRowsPerStep + lane / kPieces;
+          sts128(dst + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4), x[k].x, x[k].y, x[k].z, x[k].w);
+        }
+        fence_async_smem();
+        mbar_arrive(&bar->q_full[t]);
+      }
+
+      for (int j = tb.first; j <= tb.last; j += tb.step) {
+        // warp-uniform outcome: the TMEM loads/stores below are warp-collective
+        if (!mbar_wait_warp(&bar->s_full[t], s_cnt & 1, abort_flag)) { ok = false; break; }
+        ++s_cnt;
+        tc_fence_after();
+        const int k0 = j * kTileN;
+        const bool partial = k0 + kTileN - 1 > g.min_hi[t] || k0 < g.max_lo[t];
+        uint32_t v[4][32];       // the row's scores of this key block
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_ld32(s_addr + q * 32, v[q]);
+        tmem_ld_wait();
+        if (partial) {
+          // the row's visible keys are one range, hence one bit per column; a masked score becomes -inf whatever it was
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const uint32_t visible = bit_range(row_lo - k0 - q * 32, row_hi + 1 - k0 - q * 32);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[q][e] = (visible >> e) & 1u ? v[q][e] : 0xff800000u;
+          }
+        }
+        float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+          mx0 = fmax3(mx0, __uint_as_float(v[0][e]), __uint_as_float(v[0][e + 1]));
+          mx1 = fmax3(mx1, __uint_as_float(v[1][e]), __uint_as_float(v[1][e + 1]));
+          mx2 = fmax3(mx2, __uint_as_float(v[2][e]), __uint_as_float(v[2][e + 1]));
+          mx3 = fmax3(mx3, __uint_as_float(v[3][e]), __uint_as_float(v[3][e + 1]));
+        }
+        const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
+        const float m_new = fmaxf(m_use, mx * a.scale_log2);
+        // rescale the running sum and the TMEM accumulator only when the maximum moved a lot
+        const bool need = j == tb.first ? false : m_new - m_use > kRescaleThreshold;
+        if (j == tb.first) m_use = m_new;
+        if (__any_sync(0xffffffffu, need)) {
+          const float alpha = need ? fast_exp2(m_use - m_new) : 1.0f;
+          l *= alpha;
+#pragma unroll 1
+          for (int q = 0; q < D / 32; ++q) {
+            uint32_t o[32];
+            tmem_ld32(o_addr + q * 32, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+            tmem_st32(o_addr + q * 32, o);
+          }
+          if (need) m_use = m_new;
+        }
+        const float neg_m = m_use == -INFINITY ? 0.f : -m_use;
+        // probabilities; the bf16 P of keys 64h .. 64h+63 overwrites score columns 64h .. 64h+31, a quarter of the
+        // exponentials on the FMA pipe, and the first half is handed over while the second is computed
+        float2 sum2 = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[q][2 * e]), __uint_as_float(v[q][2 * e + 1])),
+                                        make_float2(a.scale_log2, a.scale_log2), make_float2(neg_m, neg_m));
+            const float2 z = e % 4 == 3 ? exp2_fma2(y) : make_float2(fast_exp2(y.x), fast_exp2(y.y));
+            sum2 = __fadd2_rn(sum2, z);
+            pk[e] = pack_bf16(z.x, z.y);
+          }
+          tmem_st16(s_addr + (q >> 1) * 64 + (q & 1) * 16, pk);
+          if (q == 1) {
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(&bar->p_half[t]);
+          }
+        }
+        l += sum2.x + sum2.y;
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(&bar->p_full[t]);
+      }
+      if (ok && any) {
+        if (!mbar_wait_warp(&bar->o_final[t], o_cnt & 1, abort_flag)) ok = false;
+        ++o_cnt;
+      }
+      if (!ok) break;
+      tc_fence_after();
+
+      // ---- a row that has nothing else to be joined with leaves finished, others go to the piece's slot
+      const bool complete = pc.whole && !g.dual;
+      const bool finished = complete && (g.seg ? !a.local : valid && __ldcg(w.rank + token) < 0);
+      float* slot = w.part + (size_t)(pc.item + blockIdx.x) * slot_floats(D) + t * kTileM * (D + 2);
+      bf16* dst = nullptr;
+      float inv_l = 0.f;
+      if (finished && valid) {
+        const bool routed = a.global && a.d != nullptr && a.d[token] != 0;
+        dst = a.O + token * a.o_t + (int64_t)head * D;
+        inv_l = l > 0.f ? (g.seg || !routed ? 1.f : 2.f) / l : 0.f;      // (no key before the window: a = s)
+      }
+#pragma unroll 1
+      for (int q = 0; q < D / 32; ++q) {
+        uint32_t o[32];
+        if (any) {
+          tmem_ld32(o_addr + q * 32, o);
+          tmem_ld_wait();
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0u;                      // no block of this tile: the accumulator was never written
+        }
+        if (dst != nullptr) {
+          uint4* d4 = reinterpret_cast<uint4*>(dst + q * 32);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(o[8 * x + e]) * inv_l;
+            if (a.add) {
+              const uint4 old = d4[x];
+              const uint32_t ow[4] = {old.x, old.y, old.z, old.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                f[2 * e] += __uint_as_float(ow[e] << 16);
+                f[2 * e + 1] += __uint_as_float(ow[e] & 0xffff0000u);
+              }
+            }
+            d4[x] = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+          }
+        } else if (valid) {
+#pragma unroll
+          for (int x = 0; x < 8; ++x)
+            *reinterpret_cast<uint4*>(slot + ((q * 8 + x) * kTileM + r) * 4) =
+                make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+        }
+      }
+      if (dst == nullptr && valid) {
+        slot[kTileM * D + r] = m_use;
+        slot[kTileM * (D + 1) + r] = any ? l : 0.f;
+      }
+      tc_fence_before();       // the accumulators have been read; the next piece's products come behind this warp's arrivals
+    }
+  }
+
+  // ---- teardown
+  tc_fence_before();
+  __syncthreads();
+  if (bar->abort_flag) {
+    // a bounded wait ran out: give copies still in flight time to land before shared memory is released
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
+    if (tid == 0) atomicExch(a.status, 1);
+    __syncthreads();
+  }
+  if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+}
+
+// ------------------------------------------------------------------------------------------------------------- join
+// The parts of one row in the slots of its (group, KV head)
+struct RowParts {
+  const float* tile;     // half of the first slot that has the row,
+  int r;                 // its lane
+  int n, tiles;          // slots, halves of each
+};
+template <int D>
+__device__ __forceinline__ RowParts row_parts(const ChunkWs& w, const Group& g, int group, int Hkv, int head, int row,
+                                              const int* starts, int ctas, bool& complete) {
+  RowParts x;
+  const int n = g.jhi - g.jlo + 1;
+  x.tiles = g.dual ? 2 : 1;
+  x.n = x.r = 0;
+  x.tile = nullptr;
+  complete = false;
+  if (n <= 0) return x;
+  const int lo = g.base + head * n, hi = lo + n - 1;
+  auto cta_of = [&](int at) {              // the last CTA whose range starts at or before this block
+    int i = 0, k = ctas;
+    while (k - i > 1) {
+      const int mid = (i + k) >> 1;
+      if (starts[mid] <= at) i = mid; else k = mid;
+    }
+    return i;
+  };
+  const int c0 = cta_of(lo), c1 = cta_of(hi);
+  x.n = c1 - c0 + 1;
+  complete = x.n == 1 && !g.dual;
+  x.r = row % kTileM;
+  x.tile = w.part + (size_t)(group * Hkv + head + c0) * slot_floats(D) + row / kTileM * (kTileM * (D + 2));
+  return x;
+}
+
+// A CTA takes 32 packed rows of the token axis and one KV head, a thread D / 8 columns of a row.
+template <int D>
+__global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
+  constexpr int kCols = D / 8;
+  const CacheFwdArgs& a = p.f;
+  const ChunkWs& w = p.w;
+  __shared__ int starts[kCtas];
+  dependency_wait();
+  const int ctas = w.plan->ctas;
+  if (threadIdx.x < ctas) starts[threadIdx.x] = w.plan->start[threadIdx.x].at;
+  __syncthreads();
+  if (*a.status != 0) return;              // a wait ran out: nothing more is stored
+  const int64_t row = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
+  const int col = (threadIdx.x >> 5) * kCols, head = blockIdx.y;
+  const int t = (int)(row / a.G);
+  if (t >= a.c.n_tokens) return;
+  const int b = w.seq[t];
+  if (b < 0) return;
+  const int h = (int)(row - (int64_t)t * a.G), rank = w.rank[t];
+  const bool routed = a.global && a.d != nullptr && a.d[t] != 0;
+  if (a.add && !routed) return;
+  RowParts part[2] = {};
+  bool complete[2] = {false, false};
+  if (a.local) {
+    int first;
+    cache_new(a.c, b, first);
+    const int x = (t - first) * a.G + h, group = w.first_group[b] + x / kRowsPerCta;
+    part[0] = row_parts<D>(w, w.groups[group], group, a.c.Hkv, head, x % kRowsPerCta, starts, ctas, complete[0]);
+    if (complete[0] && rank < 0) return;
+  }
+  if (rank >= 0) {
+    const int x = (rank - w.list_start[b]) * a.G + h, group = w.first_group[a.c.B + b] + x / kRowsPerCta;
+    part[1] = row_parts<D>(w, w.groups[group], group, a.c.Hkv, head, x % kRowsPerCta, starts, ctas, complete[1]);
+    if (complete[1] && !a.local) return;
+  }
+  // maxima, then sums and accumulators, of the window and of what lies before it
+  constexpr size_t kSlot = (size_t)kRowsPerCta * (D + 2), kHalf = (size_t)kTileM * (D + 2);
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, f[2][kCols] = {};
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+    for (int i = 0; i < part[s].n * part[s].tiles; ++i) {
+      const float* x = part[s].tile + i / part[s].tiles * kSlot + i % part[s].tiles * kHalf + part[s].r;
+      if (x[kTileM * (D + 1)] != 0.f) m[s] = fmaxf(m[s], x[kTileM * D]);
+    }
+  const float m_all = fmaxf(m[0], m[1]);
+#pragma unroll
+  for (int s = 0; s < 2; ++s)
+    for (int i = 0; i < part[s].n * part[s].tiles; ++i) {
+      const float* x = part[s].tile + i / part[s].tiles * kSlot + i % part[s].tiles * kHalf;
+      const float ls = x[kTileM * (D + 1) + part[s].r];
+      if (ls == 0.f) continue;             // no key of that part is visible to the row
+      const float k = fast_exp2(x[kTileM * D + part[s].r] - m[s]);
+      l[s] = fmaf(ls, k, l[s]);
+#pragma unroll
+      for (int e = 0; e < kCols / 4; ++e) {
+        const float4 v = *reinterpret_cast<const float4*>(x + ((col / 4 + e) * kTileM + part[s].r) * 4);
+        f[s][4 * e] = fmaf(k, v.x, f[s][4 * e]);
+        f[s][4 * e + 1] = fmaf(k, v.y, f[s][4 * e + 1]);
+        f[s][4 * e + 2] = fmaf(k, v.z, f[s][4 * e + 2]);
+        f[s][4 * e + 3] = fmaf(k, v.w, f[s][4 * e + 3]);
+      }
+    }
+  const float k0 = l[0] > 0.f ? fast_exp2(m[0] - m_all) : 0.f, k1 = l[1] > 0.f ? fast_exp2(m[1] - m_all) : 0.f;
+  const float l_all = fmaf(k0, l[0], k1 * l[1]);
+  const float g_all = routed && l_all > 0.f ? 1.f / l_all : 0.f;
+  const float w0 = (a.local && l[0] > 0.f ? 1.f / l[0] : 0.f) + g_all * k0, w1 = g_all * k1;
+  bf16* dst = a.O + t * a.o_t + (int64_t)(head * a.G + h) * D + col;
+#pragma unroll
+  for (int q = 0; q < kCols / 8; ++q) {
+    float o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = fmaf(w0, f[0][8 * q + e], w1 * f[1][8 * q + e]);
+    uint4* d4 = reinterpret_cast<uint4*>(dst) + q;
+    if (a.add) {
+      const uint4 old = *d4;
+      const uint32_t ow[4] = {old.x, old.y, old.z, old.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        o[2 * e] += __uint_as_float(ow[e] << 16);
+        o[2 * e + 1] += __uint_as_float(ow[e] & 0xffff0000u);
+      }
+    }
+    *d4 = make_uint4(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7]));
+  }
+}
+
+// ------------------------------------------------------------------------------------------------------------- host
+size_t layout(int B, int n_tokens, int G, int Hkv, int D, uint8_t* base, ChunkWs* w) {
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    uint8_t* p = base + at;
+    at += align_up(bytes, 256);
+    return p;
+  };
+  const size_t groups = (size_t)most_groups(n_tokens, G, B), tokens = n_tokens;
+  ChunkWs x;
+  x.plan = reinterpret_cast<Plan*>(take(sizeof(Plan)));
+  x.groups = reinterpret_cast<Group*>(take(groups * sizeof(Group)));
+  x.seq = reinterpret_cast<int*>(take(tokens * 4));
+  x.rank = reinterpret_cast<int*>(take(tokens * 4));
+  x.list = reinterpret_cast<int*>(take(tokens * 4));
+  x.first_group = reinterpret_cast<int*>(take((size_t)B * 8));
+  x.list_start = reinterpret_cast<int*>(take((size_t)B * 4));
+  x.list_end = reinterpret_cast<int*>(take((size_t)B * 4));
+  x.part = reinterpret_cast<float*>(take((groups * Hkv + kCtas) * slot_floats(D) * sizeof(float)));
+  if (w) *w = x;
+  return at;
+}
+
+template <int D, bool kE4M3>
+cudaError_t launch_chunk(const ChunkArgs& p, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t s) {
+  constexpr int smem = ChunkSmem<D, kE4M3>::kTotal;
+  static PerDeviceOnce once;
+  cudaError_t e = once.run([] {
+    return cudaFuncSetAttribute(cache_chunk_kernel<D, kE4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  });
+  if (e != cudaSuccess) return e;
+  cache_plan_kernel<<<1, kPlanThreads, 0, s>>>(p);
+  e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  e = launch_dependent(cache_chunk_kernel<D, kE4M3>, dim3(kCtas), kChunkThreads, smem, s, true, mapK, mapV, p);
+  if (e != cudaSuccess) return e;
+  const dim3 grid((unsigned)(((int64_t)p.f.c.n_tokens * p.f.G + 31) / 32), p.f.c.Hkv);
+  return launch_dependent(cache_join_kernel<D>, grid, 256, 0, s, true, p);
+}
+
+}  // namespace
+
+size_t cache_chunk_ws_bytes(const l2a_params* p, int n_tokens) {
+  return layout(p->B, n_tokens, p->Hq / p->Hkv, p->Hkv, p->D, nullptr, nullptr);
+}
+
+cudaError_t launch_cache_chunk(const CacheFwdArgs& a, void* ws, cudaStream_t s) {
+  ChunkArgs p;
+  p.f = a;
+  layout(a.c.B, a.c.n_tokens, a.G, a.c.Hkv, a.c.D, static_cast<uint8_t*>(ws), &p.w);
+  const bool e4m3 = a.c.kind == L2A_CACHE_E4M3;
+  CUtensorMap mapK, mapV;
+  const int rows = std::min(1 << a.c.page_shift, e4m3 ? 64 : 128);
+  if (!encode_pool_map(&mapK, a.c, a.c.K, rows, 1) || !encode_pool_map(&mapV, a.c, a.c.V, rows, 1)) return cudaErrorUnknown;
+  if (a.c.D == 128) return e4m3 ? launch_chunk<128, true>(p, mapK, mapV, s) : launch_chunk<128, false>(p, mapK, mapV, s);
+  return e4m3 ? launch_chunk<64, true>(p, mapK, mapV, s) : launch_chunk<64, false>(p, mapK, mapV, s);
+}
+
+}  // namespace l2a

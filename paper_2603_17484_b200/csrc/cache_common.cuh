@@ -61,6 +61,10 @@ constexpr int kFewRows = 16;
 size_t cache_few_ws_bytes(const l2a_params* p);     // plan and parts
 cudaError_t launch_cache_few(CacheFwdArgs& a, void* ws, cudaStream_t s);
 
+// All others: cache_chunk.cu
+size_t cache_chunk_ws_bytes(const l2a_params* p, int n_tokens);
+cudaError_t launch_cache_chunk(const CacheFwdArgs& a, void* ws, cudaStream_t s);
+
 // Tensor map over a pool: {elements of 128 bytes at most, tokens, (pieces of a row,) heads, pages}; one copy brings box_rows
 // tokens of one head of one page, box_pieces * 64 elements of each (bf16) or the whole row of codes.
 bool encode_pool_map(CUtensorMap* map, const CacheView& c, const void* pool, int box_rows, int box_pieces);
