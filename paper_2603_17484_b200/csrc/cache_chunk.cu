@@ -36,6 +36,7 @@ constexpr int kSoftmaxRegs = 200, kOtherRegs = 56;
 static_assert(kSoftmaxWarps * kSoftmaxRegs + 8 * kOtherRegs <= 16 * 128, "register shares exceed the launch allocation");
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr int kBoxBytes = 128 * 128;       // 128 rows of 128 bytes
+constexpr float kWeightTop = 7.0f;         // e4m3: weights lie at 2^7 and, while the reference lags, up to 2^15 (fp16 operands)
 constexpr int kPlanThreads = 1024;
 constexpr int kCtas = kSplitSms;
 constexpr int kItemCost = 3;               // key blocks' time that a piece costs besides its blocks
@@ -48,7 +49,7 @@ struct alignas(16) Group {
   int list, row0, n_rows, dual;  // segment 1: its list of routed tokens starts here; first packed row; rows; one tile twice
   int key_lo, key_hi, jlo, jhi;  // keys that some row sees, and their blocks (jhi < jlo: none)
   int base, hi0, lo1, pad;       // first key block of the group's heads in the call; last block of tile 0, first of tile 1
-  int min_hi[2], max_lo[2];      // of each tile: keys from max_lo to min_hi are seen by all its rows
+  int min_hi0, min_hi1, max_lo0, max_lo1;      // of each tile: keys from max_lo to min_hi are seen by all its rows
 };
 struct alignas(16) Start { int at, group, head, block; };   // where a CTA's range begins
 
@@ -64,6 +65,7 @@ struct ChunkWs {
   Group* groups;
   int *seq, *rank, *list;
   int *first_group, *list_start, *list_end;   // [2][B], [B], [B]
+  int* group_cost;                 // of the groups before each
   float* part;
 };
 
@@ -80,62 +82,99 @@ struct ChunkArgs {
 // ------------------------------------------------------------------------------------------------------------- plan
 __device__ __forceinline__ bool is_chunk(const CacheFwdArgs& a, int n) { return (int64_t)n * a.G > kFewRows || (n > 0 && a.G > kFewRows); }
 
-// Inclusive scan over the CTA's threads; `all`: the sum.  Two barriers.
-__device__ __forceinline__ int block_scan(int x, int* sums, int& all) {
+// Inclusive scans of two values over the CTA's threads; all_x, all_y: the sums.  Two barriers.
+__device__ __forceinline__ int2 block_scan(int x, int y, int2* sums, int& all_x, int& all_y) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
+    const int u = __shfl_up_sync(0xffffffffu, x, o), v = __shfl_up_sync(0xffffffffu, y, o);
+    if (lane >= o) { x += u; y += v; }
   }
   __syncthreads();
-  if (lane == 31) sums[warp] = x;
+  if (lane == 31) sums[warp] = make_int2(x, y);
   __syncthreads();
-  int before = 0, total = 0;
+  const int2 mine = sums[lane];                        // (as many warps as lanes)
+  int u = mine.x, v = mine.y;
 #pragma unroll
-  for (int w = 0; w < kPlanThreads / 32; ++w) {
-    if (w < warp) before += sums[w];
-    total += sums[w];
+  for (int o = 1; o < 32; o <<= 1) {
+    const int i = __shfl_up_sync(0xffffffffu, u, o), k = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) { u += i; v += k; }
   }
-  all = total;
-  return x + before;
+  all_x = __shfl_sync(0xffffffffu, u, 31);
+  all_y = __shfl_sync(0xffffffffu, v, 31);
+  x += __shfl_sync(0xffffffffu, u - mine.x, warp);
+  y += __shfl_sync(0xffffffffu, v - mine.y, warp);
+  return make_int2(x, y);
+}
+// The last i with v[i] <= x, of n > 0 ascending ones with v[0] <= x
+__device__ __forceinline__ int last_not_above(const int* v, int n, int x) {
+  int lo = 0;
+  while (n - lo > 1) {
+    const int mid = (lo + n) >> 1;
+    if (v[mid] <= x) lo = mid; else n = mid;
+  }
+  return lo;
 }
 
+// Bound by latencies: what is searched lies in shared memory where it fits (kKeep sequences or groups), else in the workspace.
+constexpr int kKeep = 1024;
 __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const ChunkArgs p) {
   const CacheFwdArgs& a = p.f;
   const CacheView& c = a.c;
   const ChunkWs& w = p.w;
-  __shared__ int sums[kPlanThreads / 32];
+  __shared__ int2 sums[kPlanThreads / 32];
+  __shared__ int keep_first[kKeep], keep_n[kKeep], keep_length[kKeep], keep_group[2 * kKeep], keep_start[kKeep], keep_end[kKeep];
+  __shared__ int keep_cost[kKeep], keep_base[kKeep], keep_blocks[kKeep];
+  static_assert(kPlanThreads == 1024, "block_scan");
   const int tid = threadIdx.x;
+  dependency_wait();
   dependents_release();
   if (a.G > kFewRows && tid == 0) *a.status = 0;       // (else the kernel of the few rows has)
-  // ---- sequence of every token.  (Lists of new tokens that do not ascend: no groups, nothing is stored.)
+  const bool small = c.B <= kKeep;
+  int* first_group = small ? keep_group : w.first_group;
+  int* list_start = small ? keep_start : w.list_start;
+  int* list_end = small ? keep_end : w.list_end;
+  // ---- the sequences.  (Lists of new tokens that do not ascend: no groups, nothing is stored.)
   bool bad = false;
   if (c.cu_new != nullptr)
     for (int b = tid; b < c.B; b += kPlanThreads) bad |= c.cu_new[b] > c.cu_new[b + 1];
   bad = __syncthreads_or(bad);
-  for (int t = tid; t < c.n_tokens; t += kPlanThreads) { w.seq[t] = -1; w.rank[t] = -1; }
-  __syncthreads();
-  for (int b = tid >> 5; b < c.B; b += kPlanThreads / 32) {
-    int first;
+  auto sequence = [&](int b, int& first, int& length) -> int {       // new tokens, 0: none here
     const int n = bad ? 0 : cache_new(c, b, first);
-    if (is_chunk(a, n))
-      for (int i = tid & 31; i < n; i += 32) w.seq[first + i] = b;
+    length = cache_length(c, b);
+    return is_chunk(a, n) ? n : 0;
+  };
+  if (small && tid < c.B) {
+    int first = 0, length = 0;
+    keep_n[tid] = sequence(tid, first, length);
+    keep_first[tid] = c.cu_new != nullptr ? c.cu_new[tid] : first;   // (ascending, whatever else is wrong with a sequence)
+    keep_length[tid] = length;
   }
   __syncthreads();
-  // ---- compact the routed tokens that see keys before their windows
-  int base = 0;
-  for (int t0 = 0; t0 < c.n_tokens; t0 += kPlanThreads) {
-    const int t = t0 + tid, b = t < c.n_tokens ? w.seq[t] : -1;
-    int first = 0, n = 0, take = 0, all;
-    if (b >= 0) {
-      n = cache_new(c, b, first);
-      take = a.global && a.d != nullptr && a.d[t] != 0 && cache_length(c, b) - n + (t - first) - a.shift >= 0;
+  auto sequence_of = [&](int t, int& first, int& n, int& length) -> int {      // -1: of none here
+    const int b = c.cu_new == nullptr ? t / c.Lq : small ? last_not_above(keep_first, c.B, t) : last_not_above(c.cu_new, c.B, t);
+    if (small) {
+      first = keep_first[b];
+      n = keep_n[b];
+      length = keep_length[b];
+    } else {
+      n = sequence(b, first, length);
     }
-    const int at = base + block_scan(take, sums, all) - take;
-    if (b >= 0 && t == first) w.list_start[b] = at;
-    if (b >= 0 && t == first + n - 1) w.list_end[b] = at + take;
-    if (take) { w.list[at] = t; w.rank[t] = at; }
+    return n > 0 && t >= first && t < first + n ? b : -1;
+  };
+  // ---- compact the routed tokens that see keys before their windows
+  int base = 0, all, unused;
+  for (int t0 = 0; t0 < c.n_tokens; t0 += kPlanThreads) {
+    const int t = t0 + tid;
+    int b = -1, first = 0, n = 0, length = 0;
+    const bool routed = a.global && a.d != nullptr && t < c.n_tokens && a.d[t] != 0;
+    if (t < c.n_tokens && !bad && (c.cu_new == nullptr || t >= (small ? keep_first[0] : c.cu_new[0]))) b = sequence_of(t, first, n, length);
+    const int take = b >= 0 && routed && length - n + (t - first) - a.shift >= 0;
+    const int at = base + block_scan(take, 0, sums, all, unused).x - take;
+    if (t < c.n_tokens) { w.seq[t] = b; w.rank[t] = take ? at : -1; }
+    if (b >= 0 && t == first) { list_start[b] = at; w.list_start[b] = at; }
+    if (b >= 0 && t == first + n - 1) list_end[b] = at + take;
+    if (take) w.list[at] = t;
     base += all;
   }
   __syncthreads();
@@ -143,86 +182,99 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const ChunkArg
   base = 0;
   for (int b0 = 0; b0 < c.B; b0 += kPlanThreads) {
     const int b = b0 + tid;
-    int first, n = 0, loc = 0, out = 0, all;
-    if (b < c.B && !bad) n = cache_new(c, b, first);
-    if (is_chunk(a, n)) {
+    int first, length, n = 0, loc = 0, out = 0;
+    if (b < c.B) n = small ? keep_n[b] : sequence(b, first, length);
+    if (n > 0) {
       loc = a.local ? (int)compact_groups(n, a.G) : 0;
-      out = (int)compact_groups(w.list_end[b] - w.list_start[b], a.G);
+      out = (int)compact_groups(list_end[b] - list_start[b], a.G);
     }
-    const int at = base + block_scan(loc + out, sums, all) - loc - out;
-    if (b < c.B) { w.first_group[b] = at; w.first_group[c.B + b] = at + loc; }
+    const int at = base + block_scan(loc + out, 0, sums, all, unused).x - loc - out;
+    if (b < c.B) {
+      first_group[b] = w.first_group[b] = at;
+      first_group[c.B + b] = w.first_group[c.B + b] = at + loc;
+    }
     base += all;
   }
   const int n_groups = base;
   __syncthreads();
-  for (int q = tid; q < n_groups; q += kPlanThreads) {
-    int b = 0, end = c.B;                              // the last sequence whose groups start at or before q
-    while (end - b > 1) {
-      const int mid = (b + end) >> 1;
-      if (w.first_group[mid] <= q) b = mid; else end = mid;
-    }
+  // ---- the groups, their key blocks and costs laid end to end
+  const bool few_groups = n_groups <= kKeep;
+  int* group_cost = few_groups ? keep_cost : w.group_cost;
+  int base_blocks = 0, base_cost = 0;
+  for (int q0 = 0; q0 < n_groups; q0 += kPlanThreads) {
+    const int q = q0 + tid;
     Group g;
-    const int n = cache_new(c, b, g.first), out0 = w.first_group[c.B + b];
-    g.b = b;
-    g.seg = q >= out0;
-    g.off = cache_length(c, b) - n;
-    g.list = g.seg ? w.list_start[b] : 0;
-    g.row0 = (q - (g.seg ? out0 : w.first_group[b])) * kRowsPerCta;
-    g.n_rows = min(kRowsPerCta, (g.seg ? w.list_end[b] - g.list : n) * a.G - g.row0);
-    g.dual = g.n_rows <= kTileM;
-    const int shift = g.seg ? a.shift : 0;
-    auto pos = [&](int r) {                            // position of packed row r of the group
-      const int i = (g.row0 + r) / a.G;
-      return g.off + (g.seg ? w.list[g.list + i] - g.first : i);
-    };
-    auto low = [&](int x) { return g.seg ? 0 : max(0, x - a.window); };
-    const int p0 = pos(0), p1 = pos(g.dual ? g.n_rows - 1 : kTileM - 1), p2 = g.dual ? p0 : pos(kTileM), p3 = pos(g.n_rows - 1);
-    g.key_lo = low(p0);
-    g.key_hi = p3 - shift;
-    g.jlo = g.key_lo / kTileN;
-    g.jhi = g.key_hi >= 0 ? g.key_hi / kTileN : g.jlo - 1;
-    g.hi0 = g.dual ? g.jhi : p1 - shift >= 0 ? (p1 - shift) / kTileN : g.jlo - 1;
-    g.lo1 = g.dual ? g.jlo : low(p2) / kTileN;
-    g.min_hi[0] = p0 - shift;
-    g.min_hi[1] = p2 - shift;
-    g.max_lo[0] = low(p1);
-    g.max_lo[1] = low(p3);
-    g.base = g.pad = 0;
-    w.groups[q] = g;
+    int x = 0;
+    if (q < n_groups) {
+      const int b = last_not_above(first_group, c.B, q), out0 = first_group[c.B + b];      // (the last: it has groups)
+      int length;
+      int n;
+      if (small) {
+        g.first = keep_first[b];
+        n = keep_n[b];
+        length = keep_length[b];
+      } else {
+        n = sequence(b, g.first, length);
+      }
+      g.b = b;
+      g.seg = q >= out0;
+      g.off = length - n;
+      g.list = g.seg ? list_start[b] : 0;
+      g.row0 = (q - (g.seg ? out0 : first_group[b])) * kRowsPerCta;
+      g.n_rows = min(kRowsPerCta, (g.seg ? list_end[b] - g.list : n) * a.G - g.row0);
+      g.dual = g.n_rows <= kTileM;
+      const int shift = g.seg ? a.shift : 0;
+      auto pos = [&](int r) {                          // position of packed row r of the group
+        const int i = (g.row0 + r) / a.G;
+        return g.off + (g.seg ? w.list[g.list + i] - g.first : i);
+      };
+      auto low = [&](int y) { return g.seg ? 0 : max(0, y - a.window); };
+      const int i1 = g.dual ? g.n_rows - 1 : kTileM - 1, i2 = g.dual ? 0 : kTileM;
+      const int p0 = pos(0), p1 = pos(i1), p2 = pos(i2), p3 = pos(g.n_rows - 1);
+      g.key_lo = low(p0);
+      g.key_hi = p3 - shift;
+      g.jlo = g.key_lo / kTileN;
+      g.jhi = g.key_hi >= 0 ? g.key_hi / kTileN : g.jlo - 1;
+      g.hi0 = g.dual ? g.jhi : p1 - shift >= 0 ? (p1 - shift) / kTileN : g.jlo - 1;
+      g.lo1 = g.dual ? g.jlo : low(p2) / kTileN;
+      g.min_hi0 = p0 - shift;
+      g.min_hi1 = p2 - shift;
+      g.max_lo0 = low(p1);
+      g.max_lo1 = low(p3);
+      g.pad = 0;
+      x = g.jhi - g.jlo + 1;
+    }
+    const int blocks = x * c.Hkv, cost = x > 0 ? (x + kItemCost) * c.Hkv : 0;
+    int all_cost;
+    const int2 at = block_scan(blocks, cost, sums, all, all_cost);
+    if (q < n_groups) {
+      g.base = base_blocks + at.x - blocks;
+      w.groups[q] = g;
+      group_cost[q] = base_cost + at.y - cost;
+      if (few_groups) { keep_base[q] = g.base; keep_blocks[q] = x; }
+    }
+    base_blocks += all;
+    base_cost += all_cost;
   }
   __syncthreads();
-  // ---- key blocks and costs, laid end to end: a thread sums a run of groups
-  const int run = (n_groups + kPlanThreads - 1) / kPlanThreads, q0 = min(n_groups, tid * run), q1 = min(n_groups, q0 + run);
-  int blocks = 0, cost = 0, all_blocks, all_cost;
-  for (int k = q0; k < q1; ++k) {
-    const int x = w.groups[k].jhi - w.groups[k].jlo + 1;
-    blocks += x * c.Hkv;
-    cost += x > 0 ? (x + kItemCost) * c.Hkv : 0;
-  }
-  int at = block_scan(blocks, sums, all_blocks) - blocks, cost_at = block_scan(cost, sums, all_cost) - cost;
-  const int ctas = max(1, min(kCtas, all_cost / kMinCost));
+  // ---- where the CTAs' ranges start
+  const int ctas = max(1, min(kCtas, base_cost / kMinCost));
   if (tid == 0) { w.plan->n_groups = n_groups; w.plan->ctas = ctas; }
-  for (int k = tid; k <= kCtas; k += kPlanThreads)
-    if (k == 0 || k >= ctas) w.plan->start[k] = Start{k == 0 ? 0 : all_blocks, 0, 0, 0};
-  for (int k = q0; k < q1; ++k) {
-    const int x = w.groups[k].jhi - w.groups[k].jlo + 1, per = x + kItemCost;
-    w.groups[k].base = at;
-    if (x <= 0) continue;
-    // the ranges that start in this group
-    const int64_t lo = cost_at, hi = lo + (int64_t)per * c.Hkv;
-    for (int64_t i = max((int64_t)1, (lo * ctas + all_cost - 1) / all_cost); i < ctas && i * all_cost / ctas < hi; ++i) {
-      const int in = (int)(i * all_cost / ctas - lo);
-      Start s;
-      s.group = k;
+  if (tid <= kCtas) {
+    Start s = {tid == 0 ? 0 : base_blocks, 0, 0, 0};
+    if (tid > 0 && tid < ctas) {
+      const int cost = (int)((int64_t)tid * base_cost / ctas);
+      s.group = last_not_above(group_cost, n_groups, cost);              // (the last: it has blocks)
+      const int x = few_groups ? keep_blocks[s.group] : w.groups[s.group].jhi - w.groups[s.group].jlo + 1;
+      const int first = few_groups ? keep_base[s.group] : w.groups[s.group].base;
+      const int in = cost - group_cost[s.group], per = x + kItemCost;
       s.head = in / per;
       s.block = max(0, in % per - kItemCost);
       if (s.block < kMinPiece) s.block = 0;
       if (s.block > 0 && x - s.block < kMinPiece) { s.block = 0; ++s.head; }
-      s.at = at + s.head * x + s.block;                // (head Hkv, block 0: the start of the next group)
-      w.plan->start[i] = s;
+      s.at = first + s.head * x + s.block;             // (head Hkv, block 0: the start of the next group)
     }
-    at += x * c.Hkv;
-    cost_at += per * c.Hkv;
+    w.plan->start[tid] = s;
   }
 }
 
@@ -298,6 +350,7 @@ __device__ __forceinline__ TileBlocks tile_blocks(const Group& g, const ChunkPie
   return x;
 }
 
+constexpr int kBarBytes = 512, kScaleSlots = 4;
 template <int D, bool kE4M3>
 struct ChunkSmem {
   static constexpr int kQTileBytes = kTileM * D * 2;
@@ -307,7 +360,7 @@ struct ChunkSmem {
   static constexpr int kVOff = kKOff + kStages * kKVTileBytes;
   static constexpr int kRawOff = kVOff + kStages * kKVTileBytes;      // K: two halves of a block, V: two
   static constexpr int kBarOff = kRawOff + (kE4M3 ? 4 * kRawBytes : 0);
-  static constexpr int kTotal = kBarOff + 256 + 1024 /* alignment slack */;
+  static constexpr int kTotal = kBarOff + kBarBytes + 1024 /* alignment slack */;
 };
 
 struct ChunkBars {
@@ -315,22 +368,30 @@ struct ChunkBars {
   uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
   uint64_t s_full[2], p_half[2], p_full[2], o_final[2];
   uint64_t raw_full[4], raw_empty[4];     // e4m3: halves of K, of V; bf16: raw_full[stage] of V
+  uint64_t scale_full[kScaleSlots];
+  float4 k_scale[kScaleSlots], v_exp[kScaleSlots];       // of the 32 keys of each decoding warp: 2^e of K, e of V
   uint32_t tmem_base;
   int abort_flag;
 };
-static_assert(sizeof(ChunkBars) <= 256, "barriers");
+static_assert(sizeof(ChunkBars) <= kBarBytes, "barriers");
 
-// 16 codes times a power of two as bf16, exactly (overflow and underflow aside)
-__device__ __forceinline__ void codes_to_bf16(const float4& codes, float scale, uint32_t (&o)[8]) {
+// 16 codes times a power of two (two of it) as fp16
+__device__ __forceinline__ void scaled_codes(const float4& codes, uint32_t scale2, uint32_t (&o)[8]) {
   const uint32_t w[4] = {__float_as_uint(codes.x), __float_as_uint(codes.y), __float_as_uint(codes.z), __float_as_uint(codes.w)};
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float2 lo = f16x2_to_float2(e4m3x2_to_f16x2(w[k] & 0xffffu)), hi = f16x2_to_float2(e4m3x2_to_f16x2(w[k] >> 16));
-    const float2 s = make_float2(scale, scale);
-    const float2 a = __fmul2_rn(lo, s), b = __fmul2_rn(hi, s);
-    o[2 * k] = pack_bf16(a.x, a.y);
-    o[2 * k + 1] = pack_bf16(b.x, b.y);
+  for (int k = 0; k < 8; ++k) {
+    const uint32_t h = e4m3x2_to_f16x2(k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffffu);
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[k]) : "r"(h), "r"(scale2));
   }
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// Instruction descriptor as idesc_bf16_f32, of fp16 operands
+__host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, int a_mn_major, int b_mn_major) {
+  return idesc_bf16_f32(M, N, a_mn_major, b_mn_major) & ~((1u << 7) | (1u << 10));
 }
 __device__ __forceinline__ void sts128(uint32_t saddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(saddr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -370,6 +431,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       mbar_init(&bar->v_full[s], kConvWarps * 32);
       mbar_init(&bar->v_empty[s], 1);
     }
+    for (int i = 0; i < kScaleSlots; ++i) mbar_init(&bar->scale_full[i], kConvWarps);
     for (int i = 0; i < 4; ++i) {
       mbar_init(&bar->raw_full[i], 1);
       mbar_init(&bar->raw_empty[i], kConvWarps / 2);
@@ -448,8 +510,8 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     setmaxnreg_dec<kOtherRegs>();
     if (elect_one()) {
       constexpr uint32_t tmem = 0;   // checked above: TMEM operand addresses are immediates in this loop
-      constexpr uint32_t idesc_qk = idesc_bf16_f32(kTileM, kTileN, 0, 0);
-      constexpr uint32_t idesc_pv = idesc_bf16_f32(kTileM, D, 0, 1);
+      constexpr uint32_t idesc_qk = kE4M3 ? idesc_f16_f32(kTileM, kTileN, 0, 0) : idesc_bf16_f32(kTileM, kTileN, 0, 0);
+      constexpr uint32_t idesc_pv = kE4M3 ? idesc_f16_f32(kTileM, D, 0, 1) : idesc_bf16_f32(kTileM, D, 0, 1);
       const uint64_t dq0 = smem_desc_sw128(smem_u32(sQ), 16, 1024);
       const uint64_t dq1 = smem_desc_sw128(smem_u32(sQ + SM::kQTileBytes), 16, 1024);
       const uint64_t dk0 = smem_desc_sw128(smem_u32(sK), 16, 1024);
@@ -498,20 +560,24 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
           issue_qk(t, s);
         };
         started[0] = started[1] = false;
-        {
-          const int s = it & 1;
-          if (!mbar_spin(&bar->k_full[s], (it >> 1) & 1, abort_flag)) ok = false;
+        // Each tile has the scores of one block under way: the next block's, or where the tiles take turns those of
+        // the two next blocks.
+        const int step = dual ? 2 : 1;
+        for (int i = 0; ok && i < step && pc.j0 + i <= pc.j1; ++i) {
+          const int s = (it + i) & 1;
+          if (!mbar_spin(&bar->k_full[s], ((it + i) >> 1) & 1, abort_flag)) { ok = false; break; }
           tc_fence_after();
 #pragma unroll
           for (int t = 0; t < 2; ++t)
-            if (ok && takes(t, pc.j0)) scores(t, pc.j0, s);
+            if (ok && takes(t, pc.j0 + i)) scores(t, pc.j0 + i, s);
           if (ok) tc_commit(&bar->k_empty[s]);
         }
         for (int j = pc.j0; ok && j <= pc.j1; ++j, ++it) {
-          const int s = it & 1, sn = s ^ 1;
+          const int s = it & 1, sn = (it + step) & 1;
+          const bool more = j + step <= pc.j1;
           // both operand blocks of this step are waited for ahead of the probabilities
           if (!mbar_spin(&bar->v_full[s], (it >> 1) & 1, abort_flag)) { ok = false; break; }
-          if (j < pc.j1 && !mbar_spin(&bar->k_full[sn], ((it + 1) >> 1) & 1, abort_flag)) { ok = false; break; }
+          if (more && !mbar_spin(&bar->k_full[sn], ((it + step) >> 1) & 1, abort_flag)) { ok = false; break; }
           tc_fence_after();
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
@@ -526,11 +592,11 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
               issue_pv(t, s, 1, 1u);
               if (j == tb[t].last) tc_commit(&bar->o_final[t]);
             }
-            if (ok && j < pc.j1 && takes(t, j + 1)) scores(t, j + 1, sn);
+            if (ok && more && takes(t, j + step)) scores(t, j + step, sn);
           }
           if (!ok) break;
           tc_commit(&bar->v_empty[s]);
-          if (j < pc.j1) tc_commit(&bar->k_empty[sn]);
+          if (more) tc_commit(&bar->k_empty[sn]);
         }
       }
     }
@@ -545,21 +611,44 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     uint32_t it = 0;
     while (ok && walk.next(w, c.Hkv, pc)) {
       const Group& g = walk.g;
-      // exponents of the key's rows of K and V, fetched a block ahead
-      auto fetch = [&](int j) -> uint32_t {
+      // page of this thread's key two blocks ahead, the exponents of its rows of K and V one block ahead
+      auto page_of = [&](int j) -> int {
         const int key = j * kTileN + row;
-        if (!kE4M3 || key < g.key_lo || key > g.key_hi) return 0u;
-        const int page = cache_page(c, g.b, key);
+        return kE4M3 && key >= g.key_lo && key <= g.key_hi ? cache_page(c, g.b, key) : -1;
+      };
+      auto exponents = [&](int j, int page) -> uint32_t {
         if (page < 0) return 0u;
-        const int64_t at = page * c.scale_stride + ((int64_t)pc.head << c.page_shift) + (key & ((1 << c.page_shift) - 1));
+        const int64_t at = page * c.scale_stride + ((int64_t)pc.head << c.page_shift) + ((j * kTileN + row) & ((1 << c.page_shift) - 1));
         return c.ks[at] | (uint32_t)c.vs[at] << 8;
       };
-      uint32_t exps = fetch(pc.j0);
+      uint32_t exps = exponents(pc.j0, page_of(pc.j0));
+      int page = page_of(pc.j0 + 1);
       for (int j = pc.j0; ok && j <= pc.j1; ++j, ++it) {
         const int s = it & 1, key = j * kTileN + row;
         const uint32_t ph = (it >> 1) & 1;
         const bool seen = key >= g.key_lo && key <= g.key_hi;
-        const uint32_t ahead = j < pc.j1 ? fetch(j + 1) : 0u;
+        const uint32_t ahead = exponents(j + 1, page);
+        page = page_of(j + 2);
+        uint32_t scale2[2];
+        if (kE4M3) {
+          // A warp's 32 keys get the scale of the largest among them: the codes of the others times a power of two below one, exact in
+          // fp16 down to 2^-24, which is 2^-33 of the largest value.
+          const int e[2] = {(int)(exps & 0xffu), (int)(exps >> 8)};
+          int top[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            top[i] = __reduce_max_sync(0xffffffffu, e[i]);
+            if (top[i] == 0) top[i] = 127;
+            const float f = __uint_as_float((uint32_t)max(e[i] - top[i] + 127, 0) << 23);
+            scale2[i] = pack_f16(f, f);
+          }
+          if (lane == 0) {
+            const int slot = it & (kScaleSlots - 1);
+            reinterpret_cast<float*>(&bar->k_scale[slot])[warp - kConvWarp] = __uint_as_float((uint32_t)top[0] << 23);
+            reinterpret_cast<float*>(&bar->v_exp[slot])[warp - kConvWarp] = (float)(top[1] - 127);
+            mbar_arrive(&bar->scale_full[slot]);
+          }
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {                    // K, V
           uint8_t* tile = (i ? sV : sK) + s * SM::kKVTileBytes;
@@ -568,15 +657,16 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
             const int slot = 2 * i + half;
             if (!mbar_wait_warp(&bar->raw_full[slot], it & 1, abort_flag)) { ok = false; break; }
             const uint32_t src = smem_u32(sRaw + slot * SM::kRawBytes) + (row & 63) * D;
-            const float scale = scale_of_exponent(i ? exps >> 8 : exps & 0xffu);
             float4 x[D / 16];
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) x[k] = lds128(src + ((D == 128 ? k ^ (row & 7) : k ^ ((row >> 1) & 3)) << 4));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar->raw_empty[slot]);
             if (!mbar_wait_warp(i ? &bar->v_empty[s] : &bar->k_empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
               uint32_t o[8];
-              codes_to_bf16(x[k], scale, o);
+              scaled_codes(x[k], scale2[i], o);
               if (!seen) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] = 0u;
@@ -587,8 +677,6 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
             }
             fence_async_smem();
             mbar_arrive(i ? &bar->v_full[s] : &bar->k_full[s]);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bar->raw_empty[slot]);
           } else if (i == 1) {
             if (!mbar_wait_warp(&bar->raw_full[s], ph, abort_flag)) { ok = false; break; }
             if (!seen) {
@@ -615,10 +703,11 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     ChunkWalk walk;
     ChunkPiece pc;
     bool ok = walk.init(w);
-    uint32_t s_cnt = 0, o_cnt = 0;
+    uint32_t s_cnt = 0, o_cnt = 0, it0 = 0;            // it0: block count of the piece's first block
     while (ok && walk.next(w, c.Hkv, pc)) {
       const Group& g = walk.g;
       const TileBlocks tb = tile_blocks(g, pc, t);
+      const int min_hi = t ? g.min_hi1 : g.min_hi0, max_lo = t ? g.max_lo1 : g.max_lo0;
       const int tile_row = (g.dual ? 0 : t * kTileM) + r;          // row of the group
       const bool valid = tile_row < g.n_rows;
       const bool any = tb.first <= tb.last;
@@ -633,6 +722,8 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       }
       float m_use = -INFINITY;   // reference maximum, exp2 domain
       float l = 0.f;             // row sum
+      float row_scale = a.scale_log2;
+      float v_first = 0.f;       // e4m3: exponent of the first values, which the sum's terms are taken relative to
       if (any) {
         // ---- the warp's 32 rows of Q, 16-byte pieces, in the layout a TMA copy would leave
         constexpr int kPieces = D / 8, kRowsPerStep = 32 / kPieces;
@@ -645,6 +736,30 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
               __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), k * kRowsPerStep + lane / kPieces));
           x[k] = q != nullptr ? __ldcg(reinterpret_cast<const uint4*>(q) + piece) : make_uint4(0, 0, 0, 0);
         }
+        if (kE4M3) {
+          // fp16, the row's largest element scaled to 2^14 .. 2^15: the others keep all their bits down to 2^-28 of it
+          uint32_t mine = 0;
+#pragma unroll
+          for (int k = 0; k < kPieces; ++k) {
+            const uint32_t u[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
+            uint32_t top = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = __vmaxu2(top, u[e] & 0x7fff7fffu);
+            top = max(top & 0xffffu, top >> 16);
+#pragma unroll
+            for (int o = kPieces / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const int up = min(max(14 + 127 - (int)(top >> 7), -113), 100);
+            const float f = __uint_as_float((uint32_t)(up + 127) << 23);
+            uint32_t h[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = pack_f16(__uint_as_float(u[e] << 16) * f, __uint_as_float(u[e] & 0xffff0000u) * f);
+            x[k] = make_uint4(h[0], h[1], h[2], h[3]);
+            // this thread's own row, its lane: step lane / kRowsPerStep, lanes of row lane % kRowsPerStep
+            const uint32_t theirs = __shfl_sync(0xffffffffu, (uint32_t)(127 - up), (lane % kRowsPerStep) * kPieces);
+            if (lane / kRowsPerStep == k) mine = theirs;
+          }
+          row_scale = a.scale_log2 * __uint_as_float(mine << 23);
+        }
         const uint32_t dst = smem_u32(sQ + t * SM::kQTileBytes) + (piece >> 3) * kBoxBytes;
 #pragma unroll
         for (int k = 0; k < kPieces; ++k) {
@@ -656,12 +771,21 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       }
 
       for (int j = tb.first; j <= tb.last; j += tb.step) {
+        float sc[4], ev[4];      // e4m3, of each 32 keys: factor of the scores, exponent of the values
+        if (kE4M3) {
+          const uint32_t it = it0 + (j - pc.j0), slot = it & (kScaleSlots - 1);
+          if (!mbar_wait_warp(&bar->scale_full[slot], (it / kScaleSlots) & 1, abort_flag)) { ok = false; break; }
+          const float4 x = lds128(smem_u32(&bar->k_scale[slot])), y = lds128(smem_u32(&bar->v_exp[slot]));
+          sc[0] = x.x * row_scale; sc[1] = x.y * row_scale; sc[2] = x.z * row_scale; sc[3] = x.w * row_scale;
+          ev[0] = y.x; ev[1] = y.y; ev[2] = y.z; ev[3] = y.w;
+          if (j == tb.first) v_first = ev[0];
+        }
         // warp-uniform outcome: the TMEM loads/stores below are warp-collective
         if (!mbar_wait_warp(&bar->s_full[t], s_cnt & 1, abort_flag)) { ok = false; break; }
         ++s_cnt;
         tc_fence_after();
         const int k0 = j * kTileN;
-        const bool partial = k0 + kTileN - 1 > g.min_hi[t] || k0 < g.max_lo[t];
+        const bool partial = k0 + kTileN - 1 > min_hi || k0 < max_lo;
         uint32_t v[4][32];       // the row's scores of this key block
 #pragma unroll
         for (int q = 0; q < 4; ++q) tmem_ld32(s_addr + q * 32, v[q]);
@@ -675,16 +799,16 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
             for (int e = 0; e < 32; ++e) v[q][e] = (visible >> e) & 1u ? v[q][e] : 0xff800000u;
           }
         }
-        float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
-          mx0 = fmax3(mx0, __uint_as_float(v[0][e]), __uint_as_float(v[0][e + 1]));
-          mx1 = fmax3(mx1, __uint_as_float(v[1][e]), __uint_as_float(v[1][e + 1]));
-          mx2 = fmax3(mx2, __uint_as_float(v[2][e]), __uint_as_float(v[2][e + 1]));
-          mx3 = fmax3(mx3, __uint_as_float(v[3][e]), __uint_as_float(v[3][e + 1]));
+#pragma unroll
+          for (int q = 0; q < 4; ++q) mx[q] = fmax3(mx[q], __uint_as_float(v[q][e]), __uint_as_float(v[q][e + 1]));
         }
-        const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
-        const float m_new = fmaxf(m_use, mx * a.scale_log2);
+        float top;
+        if (kE4M3) top = fmaxf(fmaxf(fmaf(mx[0], sc[0], ev[0]), fmaf(mx[1], sc[1], ev[1])), fmaxf(fmaf(mx[2], sc[2], ev[2]), fmaf(mx[3], sc[3], ev[3])));
+        else top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
+        const float m_new = fmaxf(m_use, top);
         // rescale the running sum and the TMEM accumulator only when the maximum moved a lot
         const bool need = j == tb.first ? false : m_new - m_use > kRescaleThreshold;
         if (j == tb.first) m_use = m_new;
@@ -702,20 +826,27 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
           }
           if (need) m_use = m_new;
         }
-        const float neg_m = m_use == -INFINITY ? 0.f : -m_use;
-        // probabilities; the bf16 P of keys 64h .. 64h+63 overwrites score columns 64h .. 64h+31, a quarter of the
+        const float neg_m = (m_use == -INFINITY ? 0.f : -m_use) + (kE4M3 ? kWeightTop : 0.f);
+        // probabilities; the 16-bit P of keys 64h .. 64h+63 overwrites score columns 64h .. 64h+31, a quarter of the
         // exponentials on the FMA pipe, and the first half is handed over while the second is computed
         float2 sum2 = make_float2(0.f, 0.f);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           uint32_t pk[16];
+          const float mul = kE4M3 ? sc[q] : a.scale_log2, add = kE4M3 ? ev[q] + neg_m : neg_m;
+          float2 part = make_float2(0.f, 0.f);
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[q][2 * e]), __uint_as_float(v[q][2 * e + 1])),
-                                        make_float2(a.scale_log2, a.scale_log2), make_float2(neg_m, neg_m));
+                                        make_float2(mul, mul), make_float2(add, add));
             const float2 z = e % 4 == 3 ? exp2_fma2(y) : make_float2(fast_exp2(y.x), fast_exp2(y.y));
-            sum2 = __fadd2_rn(sum2, z);
-            pk[e] = pack_bf16(z.x, z.y);
+            if (kE4M3) part = __fadd2_rn(part, z);
+            else sum2 = __fadd2_rn(sum2, z);
+            pk[e] = kE4M3 ? pack_f16(z.x, z.y) : pack_bf16(z.x, z.y);
+          }
+          if (kE4M3) {           // (the weights hold 2^e of the values, their sum must not)
+            const float f = fast_exp2(v_first - ev[q]);
+            sum2 = __ffma2_rn(part, make_float2(f, f), sum2);
           }
           tmem_st16(s_addr + (q >> 1) * 64 + (q & 1) * 16, pk);
           if (q == 1) {
@@ -729,6 +860,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         tc_fence_before();
         mbar_arrive(&bar->p_full[t]);
       }
+      it0 += pc.j1 - pc.j0 + 1;
       if (ok && any) {
         if (!mbar_wait_warp(&bar->o_final[t], o_cnt & 1, abort_flag)) ok = false;
         ++o_cnt;
@@ -741,11 +873,12 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       const bool finished = complete && (g.seg ? !a.local : valid && __ldcg(w.rank + token) < 0);
       float* slot = w.part + (size_t)(pc.item + blockIdx.x) * slot_floats(D) + t * kTileM * (D + 2);
       bf16* dst = nullptr;
+      const float back = kE4M3 ? fast_exp2(v_first) : 1.f;           // the accumulators lack the exponent of the first values
       float inv_l = 0.f;
       if (finished && valid) {
         const bool routed = a.global && a.d != nullptr && a.d[token] != 0;
         dst = a.O + token * a.o_t + (int64_t)head * D;
-        inv_l = l > 0.f ? (g.seg || !routed ? 1.f : 2.f) / l : 0.f;      // (no key before the window: a = s)
+        inv_l = l > 0.f ? back * (g.seg || !routed ? 1.f : 2.f) / l : 0.f;      // (no key before the window: a = s)
       }
 #pragma unroll 1
       for (int q = 0; q < D / 32; ++q) {
@@ -776,6 +909,10 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
             d4[x] = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
           }
         } else if (valid) {
+          if (kE4M3) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * back);
+          }
 #pragma unroll
           for (int x = 0; x < 8; ++x)
             *reinterpret_cast<uint4*>(slot + ((q * 8 + x) * kTileM + r) * 4) =
@@ -783,7 +920,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         }
       }
       if (dst == nullptr && valid) {
-        slot[kTileM * D + r] = m_use;
+        slot[kTileM * D + r] = kE4M3 ? m_use - v_first - kWeightTop : m_use;
         slot[kTileM * (D + 1) + r] = any ? l : 0.f;
       }
       tc_fence_before();       // the accumulators have been read; the next piece's products come behind this warp's arrivals
@@ -935,6 +1072,7 @@ size_t layout(int B, int n_tokens, int G, int Hkv, int D, uint8_t* base, ChunkWs
   ChunkWs x;
   x.plan = reinterpret_cast<Plan*>(take(sizeof(Plan)));
   x.groups = reinterpret_cast<Group*>(take(groups * sizeof(Group)));
+  x.group_cost = reinterpret_cast<int*>(take(groups * 4));
   x.seq = reinterpret_cast<int*>(take(tokens * 4));
   x.rank = reinterpret_cast<int*>(take(tokens * 4));
   x.list = reinterpret_cast<int*>(take(tokens * 4));
@@ -954,8 +1092,7 @@ cudaError_t launch_chunk(const ChunkArgs& p, const CUtensorMap& mapK, const CUte
     return cudaFuncSetAttribute(cache_chunk_kernel<D, kE4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   });
   if (e != cudaSuccess) return e;
-  cache_plan_kernel<<<1, kPlanThreads, 0, s>>>(p);
-  e = cudaGetLastError();
+  e = launch_dependent(cache_plan_kernel, dim3(1), kPlanThreads, 0, s, p.f.G <= kFewRows, p);
   if (e != cudaSuccess) return e;
   e = launch_dependent(cache_chunk_kernel<D, kE4M3>, dim3(kCtas), kChunkThreads, smem, s, true, mapK, mapV, p);
   if (e != cudaSuccess) return e;

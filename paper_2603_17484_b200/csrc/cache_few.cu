@@ -621,6 +621,7 @@ __global__ void __launch_bounds__(kCombineThreads) cache_few_combine_kernel(cons
   const int h = blockIdx.x, b = blockIdx.y, i = blockIdx.z, g = h / a.G;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c4 = tid % kLanes, grp = tid / kLanes;
   dependency_wait();
+  dependents_release();
   const FewSeq s = few_seq(a, b);
   if (i >= s.n) return;
   const int per_cta = a.plan[0], at = a.plan[1 + b] + g * s.tiles();
