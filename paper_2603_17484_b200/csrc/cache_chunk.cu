@@ -15,9 +15,12 @@
 //   warps 0-7   : soft-max, correction and epilogue, one thread a row; they also gather the rows of Q
 //   warp 8      : TMA producer, one copy a page (and 64 columns in bf16)
 //   warp 9      : tcgen05 MMA issuer and TMEM owner
-//   warps 12-15 : one thread a key.  e4m3: decode the codes that arrive in a raw ring to bf16 times the key's power of
-//                 two, which is exact, in the layout the MMA operands have; the products then run as for a bf16 cache.
-//                 Both kinds: zeros for the values of keys that no row of the group sees (their slots may hold anything).
+//   warps 12-15 : one thread a key.  e4m3: decode the values to fp16 tiles.  Both kinds: zeros for the values of keys that no row
+//                 of the group sees (their slots may hold anything).
+// e4m3: the codes of K are an operand as they are.  Q is the sum of two e4m3 numbers, exactly (8 bits in two terms of 4 and a sign,
+// elements below 2^-10 of the row's largest to 2^-18 of that), so Q K^T is two products at twice the rate of bf16; the soft-max
+// warps multiply the scores by the keys' scales.  The values' scales would have to be known to the weights, key by key; instead they
+// are decoded, times their power of two relative to the largest of 32 keys, which goes into the exponent of the weights.
 #include <math.h>
 
 #include <algorithm>
@@ -28,7 +31,7 @@ namespace l2a {
 
 namespace {
 
-constexpr int kStages = 2;
+constexpr int kKStages = 3, kVStages = 2;
 constexpr int kSoftmaxWarps = 8, kTmaWarp = 8, kMmaWarp = 9, kConvWarp = 12, kConvWarps = 4;
 constexpr int kChunkThreads = 512;
 // The launch has 16 warps of 128 registers; the two warpgroups that do not compute rows give most of theirs away.
@@ -284,44 +287,38 @@ struct ChunkPiece {
   bool whole;              // all of the group's blocks
   int item;                // group * Hkv + head
 };
-// The pieces of a CTA's range in order; every warp walks through them by itself.
+// The pieces of a CTA's range in order; every warp walks through them by itself, and reads of a group what it needs (few
+// registers: those of the soft-max warps are taken by the scores).
 struct ChunkWalk {
   int at, end, group, head, block, n_groups;
-  Group g;
-  __device__ __forceinline__ void load(const ChunkWs& w) {
-    const uint4* src = reinterpret_cast<const uint4*>(w.groups + group);
-    uint4* dst = reinterpret_cast<uint4*>(&g);
-#pragma unroll
-    for (int i = 0; i < (int)sizeof(Group) / 16; ++i) dst[i] = __ldcg(src + i);
-  }
   __device__ __forceinline__ bool init(const ChunkWs& w) {
     const int cta = blockIdx.x;
     n_groups = w.plan->n_groups;
-    const int4 s = __ldcg(reinterpret_cast<const int4*>(&w.plan->start[cta]));
+    const int4 s = *reinterpret_cast<const int4*>(&w.plan->start[cta]);
     at = s.x;
     group = s.y;
     head = s.z;
     block = s.w;
-    end = __ldcg(&w.plan->start[cta + 1].at);
-    if (cta >= w.plan->ctas || at >= end || group >= n_groups) return false;
-    load(w);
-    return true;
+    end = w.plan->start[cta + 1].at;
+    return cta < w.plan->ctas && at < end && group < n_groups;
   }
   __device__ __forceinline__ bool next(const ChunkWs& w, int Hkv, ChunkPiece& p) {
     if (at >= end) return false;
+    int n, jlo;
     for (;;) {
-      const int n = g.jhi - g.jlo + 1;
+      const int2 j = *reinterpret_cast<const int2*>(&w.groups[group].jlo);
+      jlo = j.x;
+      n = j.y - j.x + 1;
       if (head < Hkv && block < n) break;
       block = 0;
       if (++head >= Hkv || n <= 0) {
         head = 0;
         if (++group >= n_groups) return false;
-        load(w);
       }
     }
-    const int n = g.jhi - g.jlo + 1, take = min(n - block, end - at);
+    const int take = min(n - block, end - at);
     p.head = head;
-    p.j0 = g.jlo + block;
+    p.j0 = jlo + block;
     p.j1 = p.j0 + take - 1;
     p.whole = take == n;
     p.item = group * Hkv + head;
@@ -330,10 +327,6 @@ struct ChunkWalk {
     return true;
   }
 };
-// Whether tile t takes key block j of the piece
-__device__ __forceinline__ bool tile_takes(const Group& g, int t, int j) {
-  return g.dual ? (j & 1) == t : t ? j >= g.lo1 : j <= g.hi0;
-}
 // First and last block of tile t in the piece (first > last: none), and their distance
 struct TileBlocks { int first, last, step; };
 __device__ __forceinline__ TileBlocks tile_blocks(const Group& g, const ChunkPiece& p, int t) {
@@ -353,41 +346,68 @@ __device__ __forceinline__ TileBlocks tile_blocks(const Group& g, const ChunkPie
 constexpr int kBarBytes = 512, kScaleSlots = 4;
 template <int D, bool kE4M3>
 struct ChunkSmem {
-  static constexpr int kQTileBytes = kTileM * D * 2;
-  static constexpr int kKVTileBytes = kTileN * D * 2;
-  static constexpr int kRawBytes = 64 * D;               // codes of 64 keys
+  static constexpr int kQTileBytes = kTileM * D * 2;                     // e4m3: both terms
+  static constexpr int kKTileBytes = kTileN * D * (kE4M3 ? 1 : 2);
+  static constexpr int kVTileBytes = kTileN * D * 2;
+  static constexpr int kRawBytes = kE4M3 ? kTileN * D : 0;               // codes of V
   static constexpr int kKOff = 2 * kQTileBytes;
-  static constexpr int kVOff = kKOff + kStages * kKVTileBytes;
-  static constexpr int kRawOff = kVOff + kStages * kKVTileBytes;      // K: two halves of a block, V: two
-  static constexpr int kBarOff = kRawOff + (kE4M3 ? 4 * kRawBytes : 0);
+  static constexpr int kVOff = kKOff + kKStages * kKTileBytes;
+  static constexpr int kRawOff = kVOff + kVStages * kVTileBytes;
+  static constexpr int kScaleOff = kRawOff + kVStages * kRawBytes;       // scales of K, by key
+  static constexpr int kBarOff = kScaleOff + (kE4M3 ? kScaleSlots * kTileN * 4 : 0);
   static constexpr int kTotal = kBarOff + kBarBytes + 1024 /* alignment slack */;
 };
 
 struct ChunkBars {
   uint64_t q_full[2];
-  uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
+  uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
   uint64_t s_full[2], p_half[2], p_full[2], o_final[2];
-  uint64_t raw_full[4], raw_empty[4];     // e4m3: halves of K, of V; bf16: raw_full[stage] of V
+  uint64_t raw_full[kVStages], raw_empty[kVStages];      // e4m3: codes of V; bf16: V before the clearing
   uint64_t scale_full[kScaleSlots];
-  float4 k_scale[kScaleSlots], v_exp[kScaleSlots];       // of the 32 keys of each decoding warp: 2^e of K, e of V
+  float4 v_exp[kScaleSlots];                             // exponent of V of the 32 keys of each decoding warp
   uint32_t tmem_base;
   int abort_flag;
 };
 static_assert(sizeof(ChunkBars) <= kBarBytes, "barriers");
 
-// 16 codes times a power of two (two of it) as fp16
+// 16 codes times a power of two as fp16; scale2: 2^8 times it, twice.  Of every four codes 0 and 2 come first, then 1 and 3: the
+// columns of the accumulators are put back in order.
 __device__ __forceinline__ void scaled_codes(const float4& codes, uint32_t scale2, uint32_t (&o)[8]) {
   const uint32_t w[4] = {__float_as_uint(codes.x), __float_as_uint(codes.y), __float_as_uint(codes.z), __float_as_uint(codes.w)};
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const uint32_t h = e4m3x2_to_f16x2(k & 1 ? w[k / 2] >> 16 : w[k / 2] & 0xffffu);
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[k]) : "r"(h), "r"(scale2));
+  for (int k = 0; k < 4; ++k) {
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * k]) : "r"(codes_02_f16(w[k])), "r"(scale2));
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * k + 1]) : "r"(codes_13_f16(w[k])), "r"(scale2));
   }
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+// Two values as the sum of two e4m3 numbers: the nearest, and the nearest to what it leaves
+__device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ void two_terms(float x, float y, uint32_t& first, uint32_t& second) {
+  first = pack_e4m3(x, y);
+  const float2 f = f16x2_to_float2(e4m3x2_to_f16x2(first));
+  second = pack_e4m3(x - f.x, y - f.y);
+}
+// Instruction descriptor, kind::f8f6f4: e4m3 x e4m3 -> fp32, both K-major
+__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N) {
+  return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+}
+__device__ __forceinline__ void mma_ss_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// Descriptor of a K-major operand with rows of 64 bytes, 64-byte swizzle (groups of eight rows 512 bytes apart)
+__device__ __forceinline__ uint64_t smem_desc_sw64(uint32_t saddr) {
+  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | 1ull << 16 | 32ull << 32 | 1ull << 46 | 4ull << 61;
 }
 // Instruction descriptor as idesc_bf16_f32, of fp16 operands
 __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, int a_mn_major, int b_mn_major) {
@@ -396,6 +416,15 @@ __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, int a_mn_majo
 __device__ __forceinline__ void sts128(uint32_t saddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(saddr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
+
+// A soft-max thread's row in a piece
+struct RowOf {
+  TileBlocks tb;
+  int token, head, lo, hi;       // first and last key that it sees
+  int min_hi, max_lo;            // of the tile
+  int slot, first_block, n_blocks;
+  bool valid, seg, complete;     // complete: the piece holds all of the row's keys in this segment
+};
 
 template <int D, bool kE4M3>
 __global__ void __launch_bounds__(kChunkThreads, 1)
@@ -414,6 +443,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
   uint8_t* sK = smem + SM::kKOff;
   uint8_t* sV = smem + SM::kVOff;
   uint8_t* sRaw = smem + SM::kRawOff;
+  float* sScale = reinterpret_cast<float*>(smem + SM::kScaleOff);
   ChunkBars* bar = reinterpret_cast<ChunkBars*>(smem + SM::kBarOff);
   volatile int* abort_flag = &bar->abort_flag;
 
@@ -425,17 +455,17 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       mbar_init(&bar->p_full[t], kTileM);
       mbar_init(&bar->o_final[t], 1);
     }
-    for (int s = 0; s < kStages; ++s) {
-      mbar_init(&bar->k_full[s], kE4M3 ? kConvWarps * 32 : 1);
+    for (int s = 0; s < kKStages; ++s) {
+      mbar_init(&bar->k_full[s], 1);
       mbar_init(&bar->k_empty[s], 1);
+    }
+    for (int s = 0; s < kVStages; ++s) {
       mbar_init(&bar->v_full[s], kConvWarps * 32);
       mbar_init(&bar->v_empty[s], 1);
+      mbar_init(&bar->raw_full[s], 1);
+      mbar_init(&bar->raw_empty[s], kConvWarps);
     }
     for (int i = 0; i < kScaleSlots; ++i) mbar_init(&bar->scale_full[i], kConvWarps);
-    for (int i = 0; i < 4; ++i) {
-      mbar_init(&bar->raw_full[i], 1);
-      mbar_init(&bar->raw_empty[i], kConvWarps / 2);
-    }
     bar->abort_flag = 0;
     fence_mbar_init();
   }
@@ -467,41 +497,44 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     ChunkWalk walk;
     ChunkPiece pc;
     bool ok = walk.init(w);
-    // rows of a copy; a lane copies page `u` (bf16: columns `piece`) of a block, e4m3: of half a block
-    const int rows_shift = min(c.page_shift, kE4M3 ? 6 : 7), rows = 1 << rows_shift;
-    const int copies = (kE4M3 ? 64 : 128) >> rows_shift, u = lane % copies, piece = lane / copies;
+    // a lane copies the rows of page `u` of a block, in bf16 64 columns of them
+    const int rows = 1 << c.page_shift, copies = 128 >> c.page_shift, u = lane % copies, piece = lane / copies;
     const bool active = piece < (kE4M3 ? 1 : D / 64);
     const uint32_t bytes = rows * (kE4M3 ? D : 128);
-    uint32_t it = 0;
+    uint32_t k_slot = 0, k_ph = 1, v_cnt = 0;
     while (ok && walk.next(w, c.Hkv, pc)) {
-      const Group& g = walk.g;
-      const int first_entry = g.key_lo >> c.page_shift, last_entry = g.key_hi >> c.page_shift;
+      const Group& g = w.groups[walk.group];
+      const int b = g.b, key_lo = g.key_lo, key_hi = g.key_hi, step = g.dual ? 2 : 1;
+      const int first_entry = key_lo >> c.page_shift, last_entry = key_hi >> c.page_shift;
       int entry0 = -512, page_ids = -1;
-      for (int j = pc.j0; ok && j <= pc.j1; ++j, ++it) {
-        const int s = it & 1;
-        const uint32_t ph = kE4M3 ? it & 1 : (it >> 1) & 1;
-#pragma unroll
-        for (int i = 0; i < (kE4M3 ? 4 : 2); ++i) {      // e4m3: halves of K, of V; bf16: K, V
-          const bool value = kE4M3 ? i >= 2 : i == 1;
-          const int key = j * kTileN + (kE4M3 ? (i & 1) * 64 : 0) + u * rows, entry = key >> c.page_shift;
-          if (((j * kTileN + kTileN - 1) >> c.page_shift) - entry0 >= 32) {
-            entry0 = (j * kTileN) >> c.page_shift;
-            const int e = entry0 + lane;
-            page_ids = e >= first_entry && e <= last_entry ? cache_page(c, g.b, e << c.page_shift) : -1;
-          }
-          const int page = __shfl_sync(0xffffffffu, page_ids, entry - entry0);
-          const bool load = active && page >= 0 && key <= g.key_hi && key + rows > g.key_lo;
-          const uint32_t expect = __popc(__ballot_sync(0xffffffffu, load)) * bytes;
-          uint64_t* full = kE4M3 ? &bar->raw_full[i] : value ? &bar->raw_full[s] : &bar->k_full[s];
-          uint64_t* empty = kE4M3 ? &bar->raw_empty[i] : value ? &bar->v_empty[s] : &bar->k_empty[s];
-          if (!mbar_wait_warp(empty, ph ^ 1, abort_flag)) { ok = false; break; }
-          if (lane == 0) mbar_expect_tx(full, expect);
-          __syncwarp();
-          if (load) {
-            uint8_t* dst = kE4M3 ? sRaw + i * SM::kRawBytes + u * rows * D
-                                 : (value ? sV : sK) + s * SM::kKVTileBytes + piece * kBoxBytes + u * rows * 128;
-            tma_load_page(dst, value ? &mapV : &mapK, full, kE4M3, piece, key & ((1 << c.page_shift) - 1), pc.head, page);
-          }
+      // pages of block j, 32 of them at a time (a block of V lies `step` blocks behind that of K)
+      auto copy = [&](int j, uint8_t* dst, const CUtensorMap* map, uint64_t* full) {
+        const int key = j * kTileN + u * rows, entry = key >> c.page_shift;
+        if (((j * kTileN) >> c.page_shift) < entry0 || ((j * kTileN + kTileN - 1) >> c.page_shift) - entry0 >= 32) {
+          entry0 = (max(j - step, 0) * kTileN) >> c.page_shift;
+          const int e = entry0 + lane;
+          page_ids = e >= first_entry && e <= last_entry ? cache_page(c, b, e << c.page_shift) : -1;
+        }
+        const int page = __shfl_sync(0xffffffffu, page_ids, entry - entry0);
+        const bool load = active && page >= 0 && key <= key_hi && key + rows > key_lo;
+        const uint32_t expect = __popc(__ballot_sync(0xffffffffu, load)) * bytes;
+        if (lane == 0) mbar_expect_tx(full, expect);
+        __syncwarp();
+        if (load)
+          tma_load_page(dst + (kE4M3 ? u * rows * D : piece * kBoxBytes + u * rows * 128), map, full, kE4M3, piece, 0, pc.head, page);
+      };
+      // in the order in which the products take them
+      for (int j = pc.j0 - step; ok && j <= pc.j1; ++j) {
+        if (j >= pc.j0) {
+          const int s = v_cnt & 1;
+          if (!mbar_wait_warp(kE4M3 ? &bar->raw_empty[s] : &bar->v_empty[s], ((v_cnt >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
+          copy(j, kE4M3 ? sRaw + s * SM::kRawBytes : sV + s * SM::kVTileBytes, &mapV, &bar->raw_full[s]);
+          ++v_cnt;
+        }
+        if (j + step <= pc.j1) {
+          if (!mbar_wait_warp(&bar->k_empty[k_slot], k_ph, abort_flag)) { ok = false; break; }
+          copy(j + step, sK + k_slot * SM::kKTileBytes, &mapK, &bar->k_full[k_slot]);
+          if (++k_slot == kKStages) { k_slot = 0; k_ph ^= 1; }
         }
       }
     }
@@ -510,24 +543,32 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     setmaxnreg_dec<kOtherRegs>();
     if (elect_one()) {
       constexpr uint32_t tmem = 0;   // checked above: TMEM operand addresses are immediates in this loop
-      constexpr uint32_t idesc_qk = kE4M3 ? idesc_f16_f32(kTileM, kTileN, 0, 0) : idesc_bf16_f32(kTileM, kTileN, 0, 0);
+      constexpr uint32_t idesc_qk = kE4M3 ? idesc_e4m3_f32(kTileM, kTileN) : idesc_bf16_f32(kTileM, kTileN, 0, 0);
       constexpr uint32_t idesc_pv = kE4M3 ? idesc_f16_f32(kTileM, D, 0, 1) : idesc_bf16_f32(kTileM, D, 0, 1);
-      const uint64_t dq0 = smem_desc_sw128(smem_u32(sQ), 16, 1024);
-      const uint64_t dq1 = smem_desc_sw128(smem_u32(sQ + SM::kQTileBytes), 16, 1024);
-      const uint64_t dk0 = smem_desc_sw128(smem_u32(sK), 16, 1024);
-      const uint64_t dk1 = smem_desc_sw128(smem_u32(sK + SM::kKVTileBytes), 16, 1024);
+      auto k_major = [](const uint8_t* tile) {
+        return kE4M3 && D == 64 ? smem_desc_sw64(smem_u32(tile)) : smem_desc_sw128(smem_u32(tile), 16, 1024);
+      };
+      const uint64_t dq0 = k_major(sQ), dq1 = k_major(sQ + SM::kQTileBytes), dk0 = k_major(sK);
       const uint64_t dv0 = smem_desc_sw128(smem_u32(sV), kBoxBytes, 1024);
-      const uint64_t dv1 = smem_desc_sw128(smem_u32(sV + SM::kKVTileBytes), kBoxBytes, 1024);
+      const uint64_t dv1 = smem_desc_sw128(smem_u32(sV + SM::kVTileBytes), kBoxBytes, 1024);
       uint32_t p_cnt[2] = {0, 0}, q_cnt[2] = {0, 0};
       bool started[2];
 
       auto issue_qk = [&](int t, int s) {
-        const uint64_t qd = t ? dq1 : dq0, kd = s ? dk1 : dk0;
+        const uint64_t qd = t ? dq1 : dq0, kd = dk0 + s * (SM::kKTileBytes >> 4);
         const uint32_t d = tmem + t * kTileN;
+        if (kE4M3) {
 #pragma unroll
-        for (int kk = 0; kk < kKSteps; ++kk) {
-          const uint32_t o = ((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4;
-          mma_ss(d, qd + o, kd + o, idesc_qk, kk > 0);
+          for (int term = 0; term < 2; ++term)
+#pragma unroll
+            for (int kk = 0; kk < D / 32; ++kk)
+              mma_ss_f8(d, qd + ((term * kTileM * D + kk * 32) >> 4), kd + ((kk * 32) >> 4), idesc_qk, term + kk > 0);
+        } else {
+#pragma unroll
+          for (int kk = 0; kk < kKSteps; ++kk) {
+            const uint32_t o = ((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4;
+            mma_ss(d, qd + o, kd + o, idesc_qk, kk > 0);
+          }
         }
         tc_commit(&bar->s_full[t]);
       };
@@ -539,13 +580,14 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
           mma_ts(d, q + kk * 8, vd + (((half * 4 + kk) * 2048) >> 4), idesc_pv, kk > 0 ? 1u : acc);
       };
 
+      uint32_t k_slot = 0, k_ph = 0;
       ChunkWalk walk;
       ChunkPiece pc;
       bool ok = walk.init(w);
       uint32_t it = 0;
       while (ok && walk.next(w, c.Hkv, pc)) {
-        const TileBlocks tb[2] = {tile_blocks(walk.g, pc, 0), tile_blocks(walk.g, pc, 1)};
-        const bool dual = walk.g.dual;
+        const TileBlocks tb[2] = {tile_blocks(w.groups[walk.group], pc, 0), tile_blocks(w.groups[walk.group], pc, 1)};
+        const bool dual = w.groups[walk.group].dual;
         auto takes = [&](int t, int j) {
           return t ? j >= tb[1].first && j <= tb[1].last && (!dual || (j & 1)) : j >= tb[0].first && j <= tb[0].last && (!dual || !(j & 1));
         };
@@ -563,21 +605,25 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         // Each tile has the scores of one block under way: the next block's, or where the tiles take turns those of
         // the two next blocks.
         const int step = dual ? 2 : 1;
+        auto k_done = [&]() {
+          tc_commit(&bar->k_empty[k_slot]);
+          if (++k_slot == kKStages) { k_slot = 0; k_ph ^= 1; }
+        };
         for (int i = 0; ok && i < step && pc.j0 + i <= pc.j1; ++i) {
-          const int s = (it + i) & 1;
-          if (!mbar_spin(&bar->k_full[s], ((it + i) >> 1) & 1, abort_flag)) { ok = false; break; }
+          if (!mbar_spin(&bar->k_full[k_slot], k_ph, abort_flag)) { ok = false; break; }
           tc_fence_after();
 #pragma unroll
           for (int t = 0; t < 2; ++t)
-            if (ok && takes(t, pc.j0 + i)) scores(t, pc.j0 + i, s);
-          if (ok) tc_commit(&bar->k_empty[s]);
+            if (ok && takes(t, pc.j0 + i)) scores(t, pc.j0 + i, k_slot);
+          if (ok) k_done();
         }
         for (int j = pc.j0; ok && j <= pc.j1; ++j, ++it) {
-          const int s = it & 1, sn = (it + step) & 1;
+          const int s = it & 1;
           const bool more = j + step <= pc.j1;
-          // both operand blocks of this step are waited for ahead of the probabilities
+          // Both operand blocks of this step are waited for ahead of the probabilities (a wait between the products, even one already
+          // satisfied, is part of a tile's serial chain); where the tiles take turns there is time in between.
           if (!mbar_spin(&bar->v_full[s], (it >> 1) & 1, abort_flag)) { ok = false; break; }
-          if (more && !mbar_spin(&bar->k_full[sn], ((it + step) >> 1) & 1, abort_flag)) { ok = false; break; }
+          if (more && !dual && !mbar_spin(&bar->k_full[k_slot], k_ph, abort_flag)) { ok = false; break; }
           tc_fence_after();
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
@@ -592,11 +638,15 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
               issue_pv(t, s, 1, 1u);
               if (j == tb[t].last) tc_commit(&bar->o_final[t]);
             }
-            if (ok && more && takes(t, j + step)) scores(t, j + step, sn);
+            if (ok && more && takes(t, j + step)) {
+              if (dual && !mbar_spin(&bar->k_full[k_slot], k_ph, abort_flag)) { ok = false; break; }
+              tc_fence_after();
+              scores(t, j + step, k_slot);
+            }
           }
           if (!ok) break;
           tc_commit(&bar->v_empty[s]);
-          if (more) tc_commit(&bar->k_empty[sn]);
+          if (more) k_done();
         }
       }
     }
@@ -604,17 +654,18 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
   } else if (warp >= kConvWarp) {
     // =========================================================================== decoding and clearing
     setmaxnreg_dec<kOtherRegs>();
-    const int row = (warp - kConvWarp) * 32 + lane, half = (warp - kConvWarp) >> 1;      // this thread's key of a block
+    const int row = (warp - kConvWarp) * 32 + lane;      // this thread's key of a block
     ChunkWalk walk;
     ChunkPiece pc;
     bool ok = walk.init(w);
     uint32_t it = 0;
     while (ok && walk.next(w, c.Hkv, pc)) {
-      const Group& g = walk.g;
+      const Group& g = w.groups[walk.group];
+      const int b = g.b, key_lo = g.key_lo, key_hi = g.key_hi;
       // page of this thread's key two blocks ahead, the exponents of its rows of K and V one block ahead
       auto page_of = [&](int j) -> int {
         const int key = j * kTileN + row;
-        return kE4M3 && key >= g.key_lo && key <= g.key_hi ? cache_page(c, g.b, key) : -1;
+        return kE4M3 && key >= key_lo && key <= key_hi ? cache_page(c, b, key) : -1;
       };
       auto exponents = [&](int j, int page) -> uint32_t {
         if (page < 0) return 0u;
@@ -626,67 +677,52 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       for (int j = pc.j0; ok && j <= pc.j1; ++j, ++it) {
         const int s = it & 1, key = j * kTileN + row;
         const uint32_t ph = (it >> 1) & 1;
-        const bool seen = key >= g.key_lo && key <= g.key_hi;
+        const bool seen = key >= key_lo && key <= key_hi;
         const uint32_t ahead = exponents(j + 1, page);
         page = page_of(j + 2);
-        uint32_t scale2[2];
+        const uint32_t dst = smem_u32(sV + s * SM::kVTileBytes) + row * 128;
         if (kE4M3) {
-          // A warp's 32 keys get the scale of the largest among them: the codes of the others times a power of two below one, exact in
-          // fp16 down to 2^-24, which is 2^-33 of the largest value.
-          const int e[2] = {(int)(exps & 0xffu), (int)(exps >> 8)};
-          int top[2];
+          // The values of a warp's 32 keys get the scale of the largest among them: the codes of the others times a power of two
+          // below one, exact in fp16 down to 2^-24, which is 2^-33 of the largest value.
+          const int slot = it & (kScaleSlots - 1), e = (int)(exps >> 8);
+          int top = __reduce_max_sync(0xffffffffu, e);
+          if (top == 0) top = 127;
+          sScale[slot * kTileN + row] = scale_of_exponent(exps & 0xffu);
+          if (lane == 0) reinterpret_cast<float*>(&bar->v_exp[slot])[warp - kConvWarp] = (float)(top - 127);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bar->scale_full[slot]);
+          const float f = __uint_as_float((uint32_t)max(e - top + 127 + 8, 0) << 23);
+          const uint32_t scale2 = pack_f16(f, f);
+          if (!mbar_wait_warp(&bar->raw_full[s], ph, abort_flag)) { ok = false; break; }
+          const uint32_t src = smem_u32(sRaw + s * SM::kRawBytes) + row * D;
+          float4 x[D / 16];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            top[i] = __reduce_max_sync(0xffffffffu, e[i]);
-            if (top[i] == 0) top[i] = 127;
-            const float f = __uint_as_float((uint32_t)max(e[i] - top[i] + 127, 0) << 23);
-            scale2[i] = pack_f16(f, f);
-          }
-          if (lane == 0) {
-            const int slot = it & (kScaleSlots - 1);
-            reinterpret_cast<float*>(&bar->k_scale[slot])[warp - kConvWarp] = __uint_as_float((uint32_t)top[0] << 23);
-            reinterpret_cast<float*>(&bar->v_exp[slot])[warp - kConvWarp] = (float)(top[1] - 127);
-            mbar_arrive(&bar->scale_full[slot]);
-          }
-        }
+          for (int k = 0; k < D / 16; ++k) x[k] = lds128(src + ((D == 128 ? k ^ (row & 7) : k ^ ((row >> 1) & 3)) << 4));
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bar->raw_empty[s]);
+          if (!mbar_wait_warp(&bar->v_empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {                    // K, V
-          uint8_t* tile = (i ? sV : sK) + s * SM::kKVTileBytes;
-          const uint32_t dst = smem_u32(tile) + row * 128;
-          if (kE4M3) {
-            const int slot = 2 * i + half;
-            if (!mbar_wait_warp(&bar->raw_full[slot], it & 1, abort_flag)) { ok = false; break; }
-            const uint32_t src = smem_u32(sRaw + slot * SM::kRawBytes) + (row & 63) * D;
-            float4 x[D / 16];
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) x[k] = lds128(src + ((D == 128 ? k ^ (row & 7) : k ^ ((row >> 1) & 3)) << 4));
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bar->raw_empty[slot]);
-            if (!mbar_wait_warp(i ? &bar->v_empty[s] : &bar->k_empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-              uint32_t o[8];
-              scaled_codes(x[k], scale2[i], o);
-              if (!seen) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = 0u;
-              }
-              const uint32_t at = dst + (k >> 2) * kBoxBytes;
-              sts128(at + (((2 * k) & 7 ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
-              sts128(at + (((2 * k + 1) & 7 ^ (row & 7)) << 4), o[4], o[5], o[6], o[7]);
-            }
-            fence_async_smem();
-            mbar_arrive(i ? &bar->v_full[s] : &bar->k_full[s]);
-          } else if (i == 1) {
-            if (!mbar_wait_warp(&bar->raw_full[s], ph, abort_flag)) { ok = false; break; }
+          for (int k = 0; k < D / 16; ++k) {
+            uint32_t o[8];
+            scaled_codes(x[k], scale2, o);
             if (!seen) {
 #pragma unroll
-              for (int k = 0; k < D / 8; ++k) sts128(dst + (k >> 3) * kBoxBytes + ((k & 7) << 4), 0u, 0u, 0u, 0u);
-              fence_async_smem();
+              for (int i = 0; i < 8; ++i) o[i] = 0u;
             }
-            mbar_arrive(&bar->v_full[s]);
+            const uint32_t at = dst + (k >> 2) * kBoxBytes;
+            sts128(at + (((2 * k) & 7 ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
+            sts128(at + (((2 * k + 1) & 7 ^ (row & 7)) << 4), o[4], o[5], o[6], o[7]);
+          }
+          fence_async_smem();
+        } else {
+          if (!mbar_wait_warp(&bar->raw_full[s], ph, abort_flag)) { ok = false; break; }
+          if (!seen) {
+#pragma unroll
+            for (int k = 0; k < D / 8; ++k) sts128(dst + (k >> 3) * kBoxBytes + ((k & 7) << 4), 0u, 0u, 0u, 0u);
+            fence_async_smem();
           }
         }
+        mbar_arrive(&bar->v_full[s]);
         exps = ahead;
       }
     }
@@ -702,81 +738,108 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     const uint32_t o_addr = tmem + lane_base + kOCol0 + t * D;    // its D accumulator columns
     ChunkWalk walk;
     ChunkPiece pc;
-    bool ok = walk.init(w);
-    uint32_t s_cnt = 0, o_cnt = 0, it0 = 0;            // it0: block count of the piece's first block
-    while (ok && walk.next(w, c.Hkv, pc)) {
-      const Group& g = walk.g;
-      const TileBlocks tb = tile_blocks(g, pc, t);
-      const int min_hi = t ? g.min_hi1 : g.min_hi0, max_lo = t ? g.max_lo1 : g.max_lo0;
-      const int tile_row = (g.dual ? 0 : t * kTileM) + r;          // row of the group
-      const bool valid = tile_row < g.n_rows;
-      const bool any = tb.first <= tb.last;
-      int token = g.first, head = 0, row_lo = 0x3fffffff, row_hi = -1;
-      if (valid) {
+    RowOf me;
+    constexpr int kPieces = D / 8, kRowsPerStep = 32 / kPieces;
+    const int piece = lane % kPieces;
+    // The next piece and this thread's row of it
+    auto advance = [&]() -> bool {
+      if (!walk.next(w, c.Hkv, pc)) return false;
+      const Group& g = w.groups[walk.group];
+      me.tb = tile_blocks(g, pc, t);
+      me.min_hi = t ? g.min_hi1 : g.min_hi0;
+      me.max_lo = t ? g.max_lo1 : g.max_lo0;
+      const int dual = g.dual, seg = g.seg, tile_row = (dual ? 0 : t * kTileM) + r;
+      me.valid = tile_row < g.n_rows;
+      me.seg = seg;
+      me.complete = pc.whole && !dual;
+      me.slot = pc.item + blockIdx.x;
+      me.first_block = pc.j0;
+      me.n_blocks = pc.j1 - pc.j0 + 1;
+      me.token = me.head = 0;
+      me.lo = 0x3fffffff;
+      me.hi = -1;
+      if (me.valid) {
         const int x = g.row0 + tile_row, i = x / a.G;
-        token = g.seg ? __ldcg(w.list + g.list + i) : g.first + i;
-        head = pc.head * a.G + x - i * a.G;
-        const int pos = g.off + token - g.first;
-        row_hi = pos - (g.seg ? a.shift : 0);
-        row_lo = g.seg ? 0 : pos - a.window;
+        me.token = seg ? w.list[g.list + i] : g.first + i;
+        me.head = pc.head * a.G + x - i * a.G;
+        const int pos = g.off + me.token - g.first;
+        me.hi = pos - (seg ? a.shift : 0);
+        me.lo = seg ? 0 : pos - a.window;
       }
+      if (me.valid) {
+        const bf16* q = a.q + me.token * a.q_t + (int64_t)me.head * D;
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(q));
+        if (D == 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + 64));
+      }
+      return true;
+    };
+    // The warp's 32 rows of Q, 16-byte pieces, to where the products read them (bf16: as a TMA copy would leave them; e4m3: as the sum of
+    // two terms, the row's largest element scaled to 2^7 .. 2^8).  Returns this thread's row's factor of the scores.
+    auto store_q = [&]() -> float {
+      float factor = a.scale_log2;
+      uint4 qx[kPieces];
+      const bf16* src = me.valid ? a.q + me.token * a.q_t + (int64_t)me.head * D : nullptr;
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k) {
+        const bf16* q = reinterpret_cast<const bf16*>(
+            __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), k * kRowsPerStep + lane / kPieces));
+        qx[k] = q != nullptr ? __ldcg(reinterpret_cast<const uint4*>(q) + piece) : make_uint4(0, 0, 0, 0);
+      }
+      const uint32_t base = smem_u32(sQ + t * SM::kQTileBytes);
+      uint32_t mine = 127;
+#pragma unroll
+      for (int k = 0; k < kPieces; ++k) {
+        const int rr = (warp & 3) * 32 + k * kRowsPerStep + lane / kPieces;
+        if (kE4M3) {
+          const uint32_t u[4] = {qx[k].x, qx[k].y, qx[k].z, qx[k].w};
+          uint32_t top = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = __vmaxu2(top, u[e] & 0x7fff7fffu);
+          top = max(top & 0xffffu, top >> 16);
+#pragma unroll
+          for (int o = kPieces / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+          const int up = min(max(7 + 127 - (int)(top >> 7), -113), 100);
+          const float f = __uint_as_float((uint32_t)(up + 127) << 23);
+          uint32_t first[4], second[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            two_terms(__uint_as_float(u[e] << 16) * f, __uint_as_float(u[e] & 0xffff0000u) * f, first[e], second[e]);
+          const uint32_t dst = base + rr * D + (((piece >> 1) ^ (D == 128 ? rr & 7 : (rr >> 1) & 3)) << 4) + (piece & 1) * 8;
+          asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(dst), "r"(first[0] | first[1] << 16), "r"(first[2] | first[3] << 16) : "memory");
+          asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(dst + kTileM * D), "r"(second[0] | second[1] << 16),
+                       "r"(second[2] | second[3] << 16) : "memory");
+          // this thread's own row, its lane: step lane / kRowsPerStep, lanes of row lane % kRowsPerStep
+          const uint32_t theirs = __shfl_sync(0xffffffffu, (uint32_t)(127 - up), (lane % kRowsPerStep) * kPieces);
+          if (lane / kRowsPerStep == k) mine = theirs;
+        } else {
+          sts128(base + (piece >> 3) * kBoxBytes + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4), qx[k].x, qx[k].y, qx[k].z, qx[k].w);
+        }
+      }
+      if (kE4M3) factor *= __uint_as_float(mine << 23);
+      fence_async_smem();
+      mbar_arrive(&bar->q_full[t]);
+      return factor;
+    };
+
+    bool ok = walk.init(w);
+    bool more = ok && advance();
+    float row_scale = a.scale_log2;
+    if (more && me.tb.first <= me.tb.last) row_scale = store_q();
+    uint32_t s_cnt = 0, o_cnt = 0, it0 = 0;            // it0: block count of the piece's first block
+    while (more) {
+      const RowOf cur = me;
+      const TileBlocks tb = cur.tb;
+      const bool any = tb.first <= tb.last;
       float m_use = -INFINITY;   // reference maximum, exp2 domain
       float l = 0.f;             // row sum
-      float row_scale = a.scale_log2;
       float v_first = 0.f;       // e4m3: exponent of the first values, which the sum's terms are taken relative to
-      if (any) {
-        // ---- the warp's 32 rows of Q, 16-byte pieces, in the layout a TMA copy would leave
-        constexpr int kPieces = D / 8, kRowsPerStep = 32 / kPieces;
-        const bf16* src = valid ? a.q + token * a.q_t + (int64_t)head * D : nullptr;
-        const int piece = lane % kPieces;
-        uint4 x[kPieces];
-#pragma unroll
-        for (int k = 0; k < kPieces; ++k) {
-          const bf16* q = reinterpret_cast<const bf16*>(
-              __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), k * kRowsPerStep + lane / kPieces));
-          x[k] = q != nullptr ? __ldcg(reinterpret_cast<const uint4*>(q) + piece) : make_uint4(0, 0, 0, 0);
-        }
-        if (kE4M3) {
-          // fp16, the row's largest element scaled to 2^14 .. 2^15: the others keep all their bits down to 2^-28 of it
-          uint32_t mine = 0;
-#pragma unroll
-          for (int k = 0; k < kPieces; ++k) {
-            const uint32_t u[4] = {x[k].x, x[k].y, x[k].z, x[k].w};
-            uint32_t top = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) top = __vmaxu2(top, u[e] & 0x7fff7fffu);
-            top = max(top & 0xffffu, top >> 16);
-#pragma unroll
-            for (int o = kPieces / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const int up = min(max(14 + 127 - (int)(top >> 7), -113), 100);
-            const float f = __uint_as_float((uint32_t)(up + 127) << 23);
-            uint32_t h[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = pack_f16(__uint_as_float(u[e] << 16) * f, __uint_as_float(u[e] & 0xffff0000u) * f);
-            x[k] = make_uint4(h[0], h[1], h[2], h[3]);
-            // this thread's own row, its lane: step lane / kRowsPerStep, lanes of row lane % kRowsPerStep
-            const uint32_t theirs = __shfl_sync(0xffffffffu, (uint32_t)(127 - up), (lane % kRowsPerStep) * kPieces);
-            if (lane / kRowsPerStep == k) mine = theirs;
-          }
-          row_scale = a.scale_log2 * __uint_as_float(mine << 23);
-        }
-        const uint32_t dst = smem_u32(sQ + t * SM::kQTileBytes) + (piece >> 3) * kBoxBytes;
-#pragma unroll
-        for (int k = 0; k < kPieces; ++k) {
-          const int rr = (warp & 3) * 32 + k * kRowsPerStep + lane / kPieces;
-          sts128(dst + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4), x[k].x, x[k].y, x[k].z, x[k].w);
-        }
-        fence_async_smem();
-        mbar_arrive(&bar->q_full[t]);
-      }
-
       for (int j = tb.first; j <= tb.last; j += tb.step) {
-        float sc[4], ev[4];      // e4m3, of each 32 keys: factor of the scores, exponent of the values
+        float ev[4];             // e4m3: exponent of the values of each 32 keys
+        const uint32_t it = it0 + (j - cur.first_block);
         if (kE4M3) {
-          const uint32_t it = it0 + (j - pc.j0), slot = it & (kScaleSlots - 1);
+          const uint32_t slot = it & (kScaleSlots - 1);
           if (!mbar_wait_warp(&bar->scale_full[slot], (it / kScaleSlots) & 1, abort_flag)) { ok = false; break; }
-          const float4 x = lds128(smem_u32(&bar->k_scale[slot])), y = lds128(smem_u32(&bar->v_exp[slot]));
-          sc[0] = x.x * row_scale; sc[1] = x.y * row_scale; sc[2] = x.z * row_scale; sc[3] = x.w * row_scale;
+          const float4 y = lds128(smem_u32(&bar->v_exp[slot]));
           ev[0] = y.x; ev[1] = y.y; ev[2] = y.z; ev[3] = y.w;
           if (j == tb.first) v_first = ev[0];
         }
@@ -785,16 +848,30 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         ++s_cnt;
         tc_fence_after();
         const int k0 = j * kTileN;
-        const bool partial = k0 + kTileN - 1 > min_hi || k0 < max_lo;
+        const bool partial = k0 + kTileN - 1 > cur.min_hi || k0 < cur.max_lo;
         uint32_t v[4][32];       // the row's scores of this key block
 #pragma unroll
         for (int q = 0; q < 4; ++q) tmem_ld32(s_addr + q * 32, v[q]);
         tmem_ld_wait();
+        if (kE4M3) {
+          const uint32_t scales = smem_u32(sScale + (it & (kScaleSlots - 1)) * kTileN);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const float4 f = lds128(scales + (q * 32 + e) * 4);
+              const float2 x = __fmul2_rn(make_float2(__uint_as_float(v[q][e]), __uint_as_float(v[q][e + 1])), make_float2(f.x, f.y));
+              const float2 y = __fmul2_rn(make_float2(__uint_as_float(v[q][e + 2]), __uint_as_float(v[q][e + 3])), make_float2(f.z, f.w));
+              v[q][e] = __float_as_uint(x.x); v[q][e + 1] = __float_as_uint(x.y);
+              v[q][e + 2] = __float_as_uint(y.x); v[q][e + 3] = __float_as_uint(y.y);
+            }
+          }
+        }
         if (partial) {
           // the row's visible keys are one range, hence one bit per column; a masked score becomes -inf whatever it was
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const uint32_t visible = bit_range(row_lo - k0 - q * 32, row_hi + 1 - k0 - q * 32);
+            const uint32_t visible = bit_range(cur.lo - k0 - q * 32, cur.hi + 1 - k0 - q * 32);
 #pragma unroll
             for (int e = 0; e < 32; ++e) v[q][e] = (visible >> e) & 1u ? v[q][e] : 0xff800000u;
           }
@@ -806,7 +883,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
           for (int q = 0; q < 4; ++q) mx[q] = fmax3(mx[q], __uint_as_float(v[q][e]), __uint_as_float(v[q][e + 1]));
         }
         float top;
-        if (kE4M3) top = fmaxf(fmaxf(fmaf(mx[0], sc[0], ev[0]), fmaf(mx[1], sc[1], ev[1])), fmaxf(fmaf(mx[2], sc[2], ev[2]), fmaf(mx[3], sc[3], ev[3])));
+        if (kE4M3) top = fmaxf(fmaxf(fmaf(mx[0], row_scale, ev[0]), fmaf(mx[1], row_scale, ev[1])), fmaxf(fmaf(mx[2], row_scale, ev[2]), fmaf(mx[3], row_scale, ev[3])));
         else top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
         const float m_new = fmaxf(m_use, top);
         // rescale the running sum and the TMEM accumulator only when the maximum moved a lot
@@ -833,7 +910,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           uint32_t pk[16];
-          const float mul = kE4M3 ? sc[q] : a.scale_log2, add = kE4M3 ? ev[q] + neg_m : neg_m;
+          const float mul = kE4M3 ? row_scale : a.scale_log2, add = kE4M3 ? ev[q] + neg_m : neg_m;
           float2 part = make_float2(0.f, 0.f);
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
@@ -860,25 +937,29 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         tc_fence_before();
         mbar_arrive(&bar->p_full[t]);
       }
-      it0 += pc.j1 - pc.j0 + 1;
-      if (ok && any) {
-        if (!mbar_wait_warp(&bar->o_final[t], o_cnt & 1, abort_flag)) ok = false;
+      it0 += cur.n_blocks;
+      // The next piece is looked up while this one's last products run, and its rows of Q are in place before this one's results are
+      // stored, so that its first scores are computed meanwhile.
+      if (!ok) break;
+      more = advance();
+      if (any) {
+        if (!mbar_wait_warp(&bar->o_final[t], o_cnt & 1, abort_flag)) { ok = false; break; }
         ++o_cnt;
       }
-      if (!ok) break;
       tc_fence_after();
+      if (more && me.tb.first <= me.tb.last) row_scale = store_q();
 
       // ---- a row that has nothing else to be joined with leaves finished, others go to the piece's slot
-      const bool complete = pc.whole && !g.dual;
-      const bool finished = complete && (g.seg ? !a.local : valid && __ldcg(w.rank + token) < 0);
-      float* slot = w.part + (size_t)(pc.item + blockIdx.x) * slot_floats(D) + t * kTileM * (D + 2);
+      const bool valid = cur.valid;
+      const bool finished = cur.complete && (cur.seg ? !a.local : valid && w.rank[cur.token] < 0);
+      float* slot = w.part + (size_t)cur.slot * slot_floats(D) + t * kTileM * (D + 2);
       bf16* dst = nullptr;
       const float back = kE4M3 ? fast_exp2(v_first) : 1.f;           // the accumulators lack the exponent of the first values
       float inv_l = 0.f;
       if (finished && valid) {
-        const bool routed = a.global && a.d != nullptr && a.d[token] != 0;
-        dst = a.O + token * a.o_t + (int64_t)head * D;
-        inv_l = l > 0.f ? back * (g.seg || !routed ? 1.f : 2.f) / l : 0.f;      // (no key before the window: a = s)
+        const bool routed = a.global && a.d != nullptr && a.d[cur.token] != 0;
+        dst = a.O + cur.token * a.o_t + (int64_t)cur.head * D;
+        inv_l = l > 0.f ? back * (cur.seg || !routed ? 1.f : 2.f) / l : 0.f;      // (no key before the window: a = s)
       }
 #pragma unroll 1
       for (int q = 0; q < D / 32; ++q) {
@@ -886,6 +967,14 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         if (any) {
           tmem_ld32(o_addr + q * 32, o);
           tmem_ld_wait();
+          if (kE4M3) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const uint32_t y = o[e + 1];
+              o[e + 1] = o[e + 2];
+              o[e + 2] = y;
+            }
+          }
         } else {
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0u;                      // no block of this tile: the accumulator was never written
@@ -974,10 +1063,11 @@ __device__ __forceinline__ RowParts row_parts(const ChunkWs& w, const Group& g, 
   return x;
 }
 
-// A CTA takes 32 packed rows of the token axis and one KV head, a thread D / 8 columns of a row.
+// A CTA takes 32 packed rows of the token axis, one KV head and 32 columns, a thread four columns of a row.  Bound by latencies:
+// the loads of kAhead parts are in flight together, maxima, sums and accumulators in one pass.
+constexpr int kAhead = 8;
 template <int D>
 __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
-  constexpr int kCols = D / 8;
   const CacheFwdArgs& a = p.f;
   const ChunkWs& w = p.w;
   __shared__ int starts[kCtas];
@@ -985,9 +1075,8 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
   const int ctas = w.plan->ctas;
   if (threadIdx.x < ctas) starts[threadIdx.x] = w.plan->start[threadIdx.x].at;
   __syncthreads();
-  if (*a.status != 0) return;              // a wait ran out: nothing more is stored
   const int64_t row = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
-  const int col = (threadIdx.x >> 5) * kCols, head = blockIdx.y;
+  const int piece = blockIdx.z * 8 + (threadIdx.x >> 5), head = blockIdx.y;
   const int t = (int)(row / a.G);
   if (t >= a.c.n_tokens) return;
   const int b = w.seq[t];
@@ -1009,55 +1098,60 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
     part[1] = row_parts<D>(w, w.groups[group], group, a.c.Hkv, head, x % kRowsPerCta, starts, ctas, complete[1]);
     if (complete[1] && !a.local) return;
   }
-  // maxima, then sums and accumulators, of the window and of what lies before it
+  if (*a.status != 0) return;              // a wait ran out: nothing more is stored
+  // of the window and of what lies before it
   constexpr size_t kSlot = (size_t)kRowsPerCta * (D + 2), kHalf = (size_t)kTileM * (D + 2);
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, f[2][kCols] = {};
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, f[2][4] = {};
 #pragma unroll
-  for (int s = 0; s < 2; ++s)
-    for (int i = 0; i < part[s].n * part[s].tiles; ++i) {
-      const float* x = part[s].tile + i / part[s].tiles * kSlot + i % part[s].tiles * kHalf + part[s].r;
-      if (x[kTileM * (D + 1)] != 0.f) m[s] = fmaxf(m[s], x[kTileM * D]);
-    }
-  const float m_all = fmaxf(m[0], m[1]);
+  for (int s = 0; s < 2; ++s) {
+    const int n = part[s].n * part[s].tiles, r = part[s].r;
+    for (int i0 = 0; i0 < n; i0 += kAhead) {
+      float ls[kAhead], ms[kAhead], m_new = m[s];
+      float4 v[kAhead];
 #pragma unroll
-  for (int s = 0; s < 2; ++s)
-    for (int i = 0; i < part[s].n * part[s].tiles; ++i) {
-      const float* x = part[s].tile + i / part[s].tiles * kSlot + i % part[s].tiles * kHalf;
-      const float ls = x[kTileM * (D + 1) + part[s].r];
-      if (ls == 0.f) continue;             // no key of that part is visible to the row
-      const float k = fast_exp2(x[kTileM * D + part[s].r] - m[s]);
-      l[s] = fmaf(ls, k, l[s]);
+      for (int u = 0; u < kAhead; ++u) {
+        const int i = min(i0 + u, n - 1);
+        const float* x = part[s].tile + (part[s].tiles == 2 ? (i >> 1) * kSlot + (i & 1) * kHalf : i * kSlot);
+        ms[u] = x[kTileM * D + r];
+        ls[u] = i0 + u < n ? x[kTileM * (D + 1) + r] : 0.f;
+        v[u] = *reinterpret_cast<const float4*>(x + (piece * kTileM + r) * 4);
+      }
 #pragma unroll
-      for (int e = 0; e < kCols / 4; ++e) {
-        const float4 v = *reinterpret_cast<const float4*>(x + ((col / 4 + e) * kTileM + part[s].r) * 4);
-        f[s][4 * e] = fmaf(k, v.x, f[s][4 * e]);
-        f[s][4 * e + 1] = fmaf(k, v.y, f[s][4 * e + 1]);
-        f[s][4 * e + 2] = fmaf(k, v.z, f[s][4 * e + 2]);
-        f[s][4 * e + 3] = fmaf(k, v.w, f[s][4 * e + 3]);
+      for (int u = 0; u < kAhead; ++u)
+        if (ls[u] != 0.f) m_new = fmaxf(m_new, ms[u]);       // (0: no key of that part is visible to the row)
+      if (m_new == -INFINITY) continue;
+      const float old = fast_exp2(m[s] - m_new);
+      l[s] *= old;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[s][e] *= old;
+      m[s] = m_new;
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        if (ls[u] == 0.f) continue;
+        const float k = fast_exp2(ms[u] - m_new);
+        l[s] = fmaf(ls[u], k, l[s]);
+        f[s][0] = fmaf(k, v[u].x, f[s][0]);
+        f[s][1] = fmaf(k, v[u].y, f[s][1]);
+        f[s][2] = fmaf(k, v[u].z, f[s][2]);
+        f[s][3] = fmaf(k, v[u].w, f[s][3]);
       }
     }
+  }
+  const float m_all = fmaxf(m[0], m[1]);
   const float k0 = l[0] > 0.f ? fast_exp2(m[0] - m_all) : 0.f, k1 = l[1] > 0.f ? fast_exp2(m[1] - m_all) : 0.f;
   const float l_all = fmaf(k0, l[0], k1 * l[1]);
   const float g_all = routed && l_all > 0.f ? 1.f / l_all : 0.f;
   const float w0 = (a.local && l[0] > 0.f ? 1.f / l[0] : 0.f) + g_all * k0, w1 = g_all * k1;
-  bf16* dst = a.O + t * a.o_t + (int64_t)(head * a.G + h) * D + col;
+  uint2* dst = reinterpret_cast<uint2*>(a.O + t * a.o_t + (int64_t)(head * a.G + h) * D) + piece;
+  float o[4];
 #pragma unroll
-  for (int q = 0; q < kCols / 8; ++q) {
-    float o[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = fmaf(w0, f[0][8 * q + e], w1 * f[1][8 * q + e]);
-    uint4* d4 = reinterpret_cast<uint4*>(dst) + q;
-    if (a.add) {
-      const uint4 old = *d4;
-      const uint32_t ow[4] = {old.x, old.y, old.z, old.w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        o[2 * e] += __uint_as_float(ow[e] << 16);
-        o[2 * e + 1] += __uint_as_float(ow[e] & 0xffff0000u);
-      }
-    }
-    *d4 = make_uint4(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]), pack_bf16(o[4], o[5]), pack_bf16(o[6], o[7]));
+  for (int e = 0; e < 4; ++e) o[e] = fmaf(w0, f[0][e], w1 * f[1][e]);
+  if (a.add) {
+    const uint2 old = *dst;
+    o[0] += __uint_as_float(old.x << 16); o[1] += __uint_as_float(old.x & 0xffff0000u);
+    o[2] += __uint_as_float(old.y << 16); o[3] += __uint_as_float(old.y & 0xffff0000u);
   }
+  *dst = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -1096,7 +1190,7 @@ cudaError_t launch_chunk(const ChunkArgs& p, const CUtensorMap& mapK, const CUte
   if (e != cudaSuccess) return e;
   e = launch_dependent(cache_chunk_kernel<D, kE4M3>, dim3(kCtas), kChunkThreads, smem, s, true, mapK, mapV, p);
   if (e != cudaSuccess) return e;
-  const dim3 grid((unsigned)(((int64_t)p.f.c.n_tokens * p.f.G + 31) / 32), p.f.c.Hkv);
+  const dim3 grid((unsigned)(((int64_t)p.f.c.n_tokens * p.f.G + 31) / 32), p.f.c.Hkv, D / 32);
   return launch_dependent(cache_join_kernel<D>, grid, 256, 0, s, true, p);
 }
 
@@ -1112,7 +1206,7 @@ cudaError_t launch_cache_chunk(const CacheFwdArgs& a, void* ws, cudaStream_t s) 
   layout(a.c.B, a.c.n_tokens, a.G, a.c.Hkv, a.c.D, static_cast<uint8_t*>(ws), &p.w);
   const bool e4m3 = a.c.kind == L2A_CACHE_E4M3;
   CUtensorMap mapK, mapV;
-  const int rows = std::min(1 << a.c.page_shift, e4m3 ? 64 : 128);
+  const int rows = 1 << a.c.page_shift;
   if (!encode_pool_map(&mapK, a.c, a.c.K, rows, 1) || !encode_pool_map(&mapV, a.c, a.c.V, rows, 1)) return cudaErrorUnknown;
   if (a.c.D == 128) return e4m3 ? launch_chunk<128, true>(p, mapK, mapV, s) : launch_chunk<128, false>(p, mapK, mapV, s);
   return e4m3 ? launch_chunk<64, true>(p, mapK, mapV, s) : launch_chunk<64, false>(p, mapK, mapV, s);

@@ -75,6 +75,10 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t codes) {
   asm("{\n .reg .b16 c;\n cvt.u16.u32 c, %1;\n cvt.rn.f16x2.e4m3x2 %0, c;\n}" : "=r"(r) : "r"(codes));
   return r;
 }
+// The same on the integer pipe, times 2^-8 (the exponent's bits keep their bias of 7): codes 1 and 3, or 0 and 2, of a word.  The
+// conversion instruction runs on the special-function unit, which the exponentials need.
+__device__ __forceinline__ uint32_t codes_13_f16(uint32_t w) { return ((w >> 1) & 0x3f803f80u) | (w & 0x80008000u); }
+__device__ __forceinline__ uint32_t codes_02_f16(uint32_t w) { return ((w << 7) & 0x3f803f80u) | ((w << 8) & 0x80008000u); }
 __device__ __forceinline__ float2 f16x2_to_float2(uint32_t v) {
   float2 f;
   asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}" : "=f"(f.x), "=f"(f.y) : "r"(v));

@@ -333,13 +333,20 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           // largest element to 2^14 .. 2^15: the others keep all their bits down to 2^-28 of it
           const int up = min(max(14 + 127 - (int)(top >> 7), -113), 100);
           const float f = __uint_as_float((uint32_t)(up + 127) << 23);
-          row_scale[x < kHalves ? x : 0] = a.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23);
+          row_scale[x < kHalves ? x : 0] = a.scale_log2 * 256.f * __uint_as_float((uint32_t)(127 - up) << 23);   // (2^8: the codes' bias)
 #pragma unroll
           for (int i = 0; i < kPieces; ++i)
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
               const uint32_t h = pack_f16(__uint_as_float(v[i][k] << 16) * f, __uint_as_float(v[i][k] & 0xffff0000u) * f);
-              qa[i * 4 + k / 2][(k & 1) * 2 + x] = valid ? h : 0u;
+              v[i][k] = valid ? h : 0u;
+            }
+#pragma unroll
+          for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {              // elements 0 and 2 of four, then 1 and 3, as the codes come
+              qa[i * 4 + k][x] = __byte_perm(v[i][2 * k], v[i][2 * k + 1], 0x5410);
+              qa[i * 4 + k][2 + x] = __byte_perm(v[i][2 * k], v[i][2 * k + 1], 0x7632);
             }
         } else {
           row_scale[x < kHalves ? x : 0] = a.scale_log2;
@@ -381,7 +388,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
                 const uint32_t w[4] = {__float_as_uint(y.x), __float_as_uint(y.y), __float_as_uint(y.z), __float_as_uint(y.w)};
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                  mma_16816<true>(sc[x], qa[i * 4 + k], e4m3x2_to_f16x2(w[k] & 0xffffu), e4m3x2_to_f16x2(w[k] >> 16));
+                  mma_16816<true>(sc[x], qa[i * 4 + k], codes_02_f16(w[k]), codes_13_f16(w[k]));
               }
               const uint32_t at = smem_u32(scales) + s * SM::kScaleBytes + r0 + x * 8 + 2 * t4;
               const uint32_t ek = lds16(at);
