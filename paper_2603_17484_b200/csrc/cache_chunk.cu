@@ -51,7 +51,7 @@ struct alignas(16) Group {
   int b, seg, first, off;        // sequence, segment, its first row of the token axis, position of that row
   int list, row0, n_rows, dual;  // segment 1: its list of routed tokens starts here; first packed row; rows; one tile twice
   int key_lo, key_hi, jlo, jhi;  // keys that some row sees, and their blocks (jhi < jlo: none)
-  int base, hi0, lo1, pad;       // first key block of the group's heads in the call; last block of tile 0, first of tile 1
+  int base, blocks, hi0, lo1;    // first key block of the group's heads in the call, blocks of a head; last block of tile 0, first of tile 1
   int min_hi0, min_hi1, max_lo0, max_lo1;      // of each tile: keys from max_lo to min_hi are seen by all its rows
 };
 struct alignas(16) Start { int at, group, head, block; };   // where a CTA's range begins
@@ -61,12 +61,20 @@ struct Plan {
   Start start[kCtas + 1];
 };
 
-// Workspace: plan, groups, then per token: sequence (-1: none here), rank among the routed of its sequence (-1: no
-// keys before its window to see), list of routed tokens; per sequence: first group of both segments, its part of the list.
+// What the join has to know of a token
+struct alignas(16) TokenInfo {
+  int index, rank;         // among the new tokens of its sequence (-1: of none here), among the routed ones that see keys before
+                           // their window (-1: not one)
+  int group[2];            // first group of the sequence in both segments
+};
+
+// Workspace: plan, groups, then per token: its info, list of routed tokens; per sequence: first group of both segments, its part
+// of the list.
 struct ChunkWs {
   Plan* plan;
   Group* groups;
-  int *seq, *rank, *list;
+  TokenInfo* token;
+  int* list;
   int *first_group, *list_start, *list_end;   // [2][B], [B], [B]
   int* group_cost;                 // of the groups before each
   float* part;
@@ -174,8 +182,8 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const ChunkArg
     if (t < c.n_tokens && !bad && (c.cu_new == nullptr || t >= (small ? keep_first[0] : c.cu_new[0]))) b = sequence_of(t, first, n, length);
     const int take = b >= 0 && routed && length - n + (t - first) - a.shift >= 0;
     const int at = base + block_scan(take, 0, sums, all, unused).x - take;
-    if (t < c.n_tokens) { w.seq[t] = b; w.rank[t] = take ? at : -1; }
-    if (b >= 0 && t == first) { list_start[b] = at; w.list_start[b] = at; }
+    if (t < c.n_tokens) w.token[t] = TokenInfo{b >= 0 ? t - first : -1, take ? at : -1, {b, 0}};      // (completed below)
+    if (b >= 0 && t == first) list_start[b] = at;
     if (b >= 0 && t == first + n - 1) list_end[b] = at + take;
     if (take) w.list[at] = t;
     base += all;
@@ -193,13 +201,22 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const ChunkArg
     }
     const int at = base + block_scan(loc + out, 0, sums, all, unused).x - loc - out;
     if (b < c.B) {
-      first_group[b] = w.first_group[b] = at;
-      first_group[c.B + b] = w.first_group[c.B + b] = at + loc;
+      first_group[b] = at;
+      first_group[c.B + b] = at + loc;
     }
     base += all;
   }
   const int n_groups = base;
   __syncthreads();
+  for (int t = tid; t < c.n_tokens; t += kPlanThreads) {
+    TokenInfo x = w.token[t];                          // (written by this thread)
+    if (x.index < 0) continue;
+    const int b = x.group[0];
+    if (x.rank >= 0) x.rank -= list_start[b];
+    x.group[0] = first_group[b];
+    x.group[1] = first_group[c.B + b];
+    w.token[t] = x;
+  }
   // ---- the groups, their key blocks and costs laid end to end
   const bool few_groups = n_groups <= kKeep;
   int* group_cost = few_groups ? keep_cost : w.group_cost;
@@ -244,8 +261,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const ChunkArg
       g.min_hi1 = p2 - shift;
       g.max_lo0 = low(p1);
       g.max_lo1 = low(p3);
-      g.pad = 0;
-      x = g.jhi - g.jlo + 1;
+      x = g.blocks = g.jhi - g.jlo + 1;
     }
     const int blocks = x * c.Hkv, cost = x > 0 ? (x + kItemCost) * c.Hkv : 0;
     int all_cost;
@@ -951,7 +967,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
 
       // ---- a row that has nothing else to be joined with leaves finished, others go to the piece's slot
       const bool valid = cur.valid;
-      const bool finished = cur.complete && (cur.seg ? !a.local : valid && w.rank[cur.token] < 0);
+      const bool finished = cur.complete && (cur.seg ? !a.local : valid && w.token[cur.token].rank < 0);
       float* slot = w.part + (size_t)cur.slot * slot_floats(D) + t * kTileM * (D + 2);
       bf16* dst = nullptr;
       const float back = kE4M3 ? fast_exp2(v_first) : 1.f;           // the accumulators lack the exponent of the first values
@@ -1035,86 +1051,79 @@ struct RowParts {
   const float* tile;     // half of the first slot that has the row,
   int r;                 // its lane
   int n, tiles;          // slots, halves of each
+  bool complete;         // one part only
 };
 template <int D>
-__device__ __forceinline__ RowParts row_parts(const ChunkWs& w, const Group& g, int group, int Hkv, int head, int row,
-                                              const int* starts, int ctas, bool& complete) {
+__device__ __forceinline__ RowParts row_parts(const ChunkWs& w, int group, int Hkv, int head, int row, const int* starts, int ctas) {
   RowParts x;
-  const int n = g.jhi - g.jlo + 1;
-  x.tiles = g.dual ? 2 : 1;
-  x.n = x.r = 0;
-  x.tile = nullptr;
-  complete = false;
-  if (n <= 0) return x;
-  const int lo = g.base + head * n, hi = lo + n - 1;
-  auto cta_of = [&](int at) {              // the last CTA whose range starts at or before this block
-    int i = 0, k = ctas;
-    while (k - i > 1) {
-      const int mid = (i + k) >> 1;
-      if (starts[mid] <= at) i = mid; else k = mid;
-    }
-    return i;
-  };
-  const int c0 = cta_of(lo), c1 = cta_of(hi);
-  x.n = c1 - c0 + 1;
-  complete = x.n == 1 && !g.dual;
+  const int2 g = *reinterpret_cast<const int2*>(&w.groups[group].base);      // first block, blocks of a head
+  const int dual = w.groups[group].dual;
+  x.tiles = dual ? 2 : 1;
   x.r = row % kTileM;
+  x.n = 0;
+  x.tile = nullptr;
+  x.complete = false;
+  if (g.y <= 0) return x;
+  const int lo = g.x + head * g.y, c0 = last_not_above(starts, ctas, lo), c1 = last_not_above(starts, ctas, lo + g.y - 1);
+  x.n = c1 - c0 + 1;
+  x.complete = x.n == 1 && !dual;
   x.tile = w.part + (size_t)(group * Hkv + head + c0) * slot_floats(D) + row / kTileM * (kTileM * (D + 2));
   return x;
 }
 
-// A CTA takes 32 packed rows of the token axis, one KV head and 32 columns, a thread four columns of a row.  Bound by latencies:
-// the loads of kAhead parts are in flight together, maxima, sums and accumulators in one pass.
-constexpr int kAhead = 8;
-template <int D>
+// A CTA takes 32 packed rows of the token axis and one KV head, a thread kPieces times four columns of a row.  Bound by latencies: the
+// loads of several parts are in flight together, maxima, sums and accumulators in one pass.
+template <int D, int kPieces>
 __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
+  constexpr int kAhead = kPieces == 1 ? 8 : 4;
   const CacheFwdArgs& a = p.f;
   const ChunkWs& w = p.w;
   __shared__ int starts[kCtas];
-  dependency_wait();
-  const int ctas = w.plan->ctas;
-  if (threadIdx.x < ctas) starts[threadIdx.x] = w.plan->start[threadIdx.x].at;
-  __syncthreads();
   const int64_t row = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
-  const int piece = blockIdx.z * 8 + (threadIdx.x >> 5), head = blockIdx.y;
-  const int t = (int)(row / a.G);
-  if (t >= a.c.n_tokens) return;
-  const int b = w.seq[t];
-  if (b < 0) return;
-  const int h = (int)(row - (int64_t)t * a.G), rank = w.rank[t];
-  const bool routed = a.global && a.d != nullptr && a.d[t] != 0;
-  if (a.add && !routed) return;
+  const int piece0 = (blockIdx.z * 8 + (threadIdx.x >> 5)) * kPieces, head = blockIdx.y, t = (int)(row / a.G);
+  const int h = (int)(row - (int64_t)t * a.G);
+  const bool inside = t < a.c.n_tokens;
+  dependency_wait();
+  TokenInfo tok = {-1, -1, {0, 0}};
+  bool routed = false;
+  if (inside) {
+    *reinterpret_cast<int4*>(&tok) = *reinterpret_cast<const int4*>(w.token + t);
+    routed = a.global && a.d != nullptr && a.d[t] != 0;
+  }
+  const int ctas = w.plan->ctas, status = *a.status;
+  if (threadIdx.x < kCtas) starts[threadIdx.x] = w.plan->start[threadIdx.x].at;
+  __syncthreads();
+  if (tok.index < 0 || (a.add && !routed)) return;
   RowParts part[2] = {};
-  bool complete[2] = {false, false};
   if (a.local) {
-    int first;
-    cache_new(a.c, b, first);
-    const int x = (t - first) * a.G + h, group = w.first_group[b] + x / kRowsPerCta;
-    part[0] = row_parts<D>(w, w.groups[group], group, a.c.Hkv, head, x % kRowsPerCta, starts, ctas, complete[0]);
-    if (complete[0] && rank < 0) return;
+    const int x = tok.index * a.G + h;
+    part[0] = row_parts<D>(w, tok.group[0] + x / kRowsPerCta, a.c.Hkv, head, x % kRowsPerCta, starts, ctas);
+    if (part[0].complete && tok.rank < 0) return;
   }
-  if (rank >= 0) {
-    const int x = (rank - w.list_start[b]) * a.G + h, group = w.first_group[a.c.B + b] + x / kRowsPerCta;
-    part[1] = row_parts<D>(w, w.groups[group], group, a.c.Hkv, head, x % kRowsPerCta, starts, ctas, complete[1]);
-    if (complete[1] && !a.local) return;
+  if (tok.rank >= 0) {
+    const int x = tok.rank * a.G + h;
+    part[1] = row_parts<D>(w, tok.group[1] + x / kRowsPerCta, a.c.Hkv, head, x % kRowsPerCta, starts, ctas);
+    if (part[1].complete && !a.local) return;
   }
-  if (*a.status != 0) return;              // a wait ran out: nothing more is stored
+  if (status != 0) return;                 // a wait ran out: nothing more is stored
   // of the window and of what lies before it
   constexpr size_t kSlot = (size_t)kRowsPerCta * (D + 2), kHalf = (size_t)kTileM * (D + 2);
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, f[2][4] = {};
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  float4 f[2][kPieces] = {};
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     const int n = part[s].n * part[s].tiles, r = part[s].r;
     for (int i0 = 0; i0 < n; i0 += kAhead) {
       float ls[kAhead], ms[kAhead], m_new = m[s];
-      float4 v[kAhead];
+      float4 v[kAhead][kPieces];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
         const int i = min(i0 + u, n - 1);
         const float* x = part[s].tile + (part[s].tiles == 2 ? (i >> 1) * kSlot + (i & 1) * kHalf : i * kSlot);
         ms[u] = x[kTileM * D + r];
         ls[u] = i0 + u < n ? x[kTileM * (D + 1) + r] : 0.f;
-        v[u] = *reinterpret_cast<const float4*>(x + (piece * kTileM + r) * 4);
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) v[u][k] = *reinterpret_cast<const float4*>(x + ((piece0 + k) * kTileM + r) * 4);
       }
 #pragma unroll
       for (int u = 0; u < kAhead; ++u)
@@ -1123,17 +1132,20 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
       const float old = fast_exp2(m[s] - m_new);
       l[s] *= old;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f[s][e] *= old;
+      for (int k = 0; k < kPieces; ++k) { f[s][k].x *= old; f[s][k].y *= old; f[s][k].z *= old; f[s][k].w *= old; }
       m[s] = m_new;
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
         if (ls[u] == 0.f) continue;
-        const float k = fast_exp2(ms[u] - m_new);
-        l[s] = fmaf(ls[u], k, l[s]);
-        f[s][0] = fmaf(k, v[u].x, f[s][0]);
-        f[s][1] = fmaf(k, v[u].y, f[s][1]);
-        f[s][2] = fmaf(k, v[u].z, f[s][2]);
-        f[s][3] = fmaf(k, v[u].w, f[s][3]);
+        const float g = fast_exp2(ms[u] - m_new);
+        l[s] = fmaf(ls[u], g, l[s]);
+#pragma unroll
+        for (int k = 0; k < kPieces; ++k) {
+          f[s][k].x = fmaf(g, v[u][k].x, f[s][k].x);
+          f[s][k].y = fmaf(g, v[u][k].y, f[s][k].y);
+          f[s][k].z = fmaf(g, v[u][k].z, f[s][k].z);
+          f[s][k].w = fmaf(g, v[u][k].w, f[s][k].w);
+        }
       }
     }
   }
@@ -1142,16 +1154,18 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
   const float l_all = fmaf(k0, l[0], k1 * l[1]);
   const float g_all = routed && l_all > 0.f ? 1.f / l_all : 0.f;
   const float w0 = (a.local && l[0] > 0.f ? 1.f / l[0] : 0.f) + g_all * k0, w1 = g_all * k1;
-  uint2* dst = reinterpret_cast<uint2*>(a.O + t * a.o_t + (int64_t)(head * a.G + h) * D) + piece;
-  float o[4];
+  uint2* dst = reinterpret_cast<uint2*>(a.O + t * a.o_t + (int64_t)(head * a.G + h) * D) + piece0;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = fmaf(w0, f[0][e], w1 * f[1][e]);
-  if (a.add) {
-    const uint2 old = *dst;
-    o[0] += __uint_as_float(old.x << 16); o[1] += __uint_as_float(old.x & 0xffff0000u);
-    o[2] += __uint_as_float(old.y << 16); o[3] += __uint_as_float(old.y & 0xffff0000u);
+  for (int k = 0; k < kPieces; ++k) {
+    float4 o = make_float4(fmaf(w0, f[0][k].x, w1 * f[1][k].x), fmaf(w0, f[0][k].y, w1 * f[1][k].y),
+                           fmaf(w0, f[0][k].z, w1 * f[1][k].z), fmaf(w0, f[0][k].w, w1 * f[1][k].w));
+    if (a.add) {
+      const uint2 old = dst[k];
+      o.x += __uint_as_float(old.x << 16); o.y += __uint_as_float(old.x & 0xffff0000u);
+      o.z += __uint_as_float(old.y << 16); o.w += __uint_as_float(old.y & 0xffff0000u);
+    }
+    dst[k] = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
   }
-  *dst = make_uint2(pack_bf16(o[0], o[1]), pack_bf16(o[2], o[3]));
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -1167,8 +1181,7 @@ size_t layout(int B, int n_tokens, int G, int Hkv, int D, uint8_t* base, ChunkWs
   x.plan = reinterpret_cast<Plan*>(take(sizeof(Plan)));
   x.groups = reinterpret_cast<Group*>(take(groups * sizeof(Group)));
   x.group_cost = reinterpret_cast<int*>(take(groups * 4));
-  x.seq = reinterpret_cast<int*>(take(tokens * 4));
-  x.rank = reinterpret_cast<int*>(take(tokens * 4));
+  x.token = reinterpret_cast<TokenInfo*>(take(tokens * sizeof(TokenInfo)));
   x.list = reinterpret_cast<int*>(take(tokens * 4));
   x.first_group = reinterpret_cast<int*>(take((size_t)B * 8));
   x.list_start = reinterpret_cast<int*>(take((size_t)B * 4));
@@ -1190,8 +1203,10 @@ cudaError_t launch_chunk(const ChunkArgs& p, const CUtensorMap& mapK, const CUte
   if (e != cudaSuccess) return e;
   e = launch_dependent(cache_chunk_kernel<D, kE4M3>, dim3(kCtas), kChunkThreads, smem, s, true, mapK, mapV, p);
   if (e != cudaSuccess) return e;
-  const dim3 grid((unsigned)(((int64_t)p.f.c.n_tokens * p.f.G + 31) / 32), p.f.c.Hkv, D / 32);
-  return launch_dependent(cache_join_kernel<D>, grid, 256, 0, s, true, p);
+  // few rows: their columns over several CTAs
+  const unsigned rows = (unsigned)(((int64_t)p.f.c.n_tokens * p.f.G + 31) / 32), heads = p.f.c.Hkv;
+  if ((int64_t)rows * heads <= kSplitSms) return launch_dependent(cache_join_kernel<D, 1>, dim3(rows, heads, D / 32), 256, 0, s, true, p);
+  return launch_dependent(cache_join_kernel<D, D / 32>, dim3(rows, heads), 256, 0, s, true, p);
 }
 
 }  // namespace
