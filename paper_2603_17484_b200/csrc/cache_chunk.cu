@@ -4,8 +4,9 @@
 //   segment 1: the rows of routed tokens, compacted; keys 0 .. p - W - 1 (with segment 0 what Global Attention sees)
 // so that the scores inside a window are computed once.  s and a are weighted sums of both segments' results.
 //
-// cache_plan_kernel   : one CTA.  Compacts the routed tokens, lists the groups with their key blocks (of 128), and divides the key
-//                       blocks of all groups and KV heads, laid end to end, evenly among the CTAs.
+// cache_prepare_kernel: the plan, by one CTA.  Compacts the routed tokens, lists the groups with their key blocks (of 128), and divides the key
+//                       blocks of all groups and KV heads, laid end to end, evenly among the CTAs.  Other CTAs, where every key is used
+//                       by many rows: an 8-bit cache decoded to bf16 in the workspace, which the rest then reads.
 // cache_chunk_kernel  : one CTA an SM takes its range, a few pieces of (group, KV head).  A row whose piece is all there is leaves
 //                       finished; other rows go to the piece's slot of the workspace, unnormalised.
 // cache_join_kernel   : joins the slots of a row.
@@ -88,6 +89,8 @@ __host__ __device__ constexpr size_t slot_floats(int D) { return (size_t)kRowsPe
 struct ChunkArgs {
   CacheFwdArgs f;
   ChunkWs w;
+  CacheView codes;       // the 8-bit cache that f.c is the decoded copy of
+  int clear;             // no kernel ahead has cleared the status word
 };
 
 // ------------------------------------------------------------------------------------------------------------- plan
@@ -129,7 +132,7 @@ __device__ __forceinline__ int last_not_above(const int* v, int n, int x) {
 
 // Bound by latencies: what is searched lies in shared memory where it fits (kKeep sequences or groups), else in the workspace.
 constexpr int kKeep = 1024;
-__global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const ChunkArgs p) {
+__device__ void make_plan(const ChunkArgs& p) {
   const CacheFwdArgs& a = p.f;
   const CacheView& c = a.c;
   const ChunkWs& w = p.w;
@@ -138,9 +141,6 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const ChunkArg
   __shared__ int keep_cost[kKeep], keep_base[kKeep], keep_blocks[kKeep];
   static_assert(kPlanThreads == 1024, "block_scan");
   const int tid = threadIdx.x;
-  dependency_wait();
-  dependents_release();
-  if (a.G > kFewRows && tid == 0) *a.status = 0;       // (else the kernel of the few rows has)
   const bool small = c.B <= kKeep;
   int* first_group = small ? keep_group : w.first_group;
   int* list_start = small ? keep_start : w.list_start;
@@ -295,6 +295,71 @@ __global__ void __launch_bounds__(kPlanThreads) cache_plan_kernel(const ChunkArg
     }
     w.plan->start[tid] = s;
   }
+}
+
+// Decoded copy: pages of 128 tokens, [page][KV head][128][D] of K and of V.  A lane brings 16 codes, a warp 512 / D keys at a time, 32
+// keys of a head of K or V in all.  HBM-bound: 3 bytes a code, of the keys that some row sees.
+constexpr int kDecodeKeys = 32;
+template <int D>
+__device__ __forceinline__ void decode_cache(const ChunkArgs& p, int item, int b) {
+  constexpr int kLanes = D / 16, kRows = 32 / kLanes, kSteps = kDecodeKeys / kRows;
+  const CacheFwdArgs& a = p.f;
+  const CacheView &c = p.codes, &out = a.c;
+  const int lane = threadIdx.x & 31, sub = lane % kLanes;
+  int first;
+  const int n = cache_new(c, b, first), length = cache_length(c, b);
+  if (!is_chunk(a, n)) return;
+  // all keys where a token is routed, else those of the windows
+  bool routed = false;
+  if (a.global && a.d != nullptr)
+    for (int i = threadIdx.x; i < n; i += kPlanThreads) routed |= a.d[first + i] != 0;
+  routed = __syncthreads_or(routed);
+  const int lo = routed ? 0 : max(0, length - n - a.window);
+  const int value = item & 1, quarter = (item >> 1) & 3, head = (item >> 3) % c.Hkv, block = (item >> 3) / c.Hkv;
+  const int key0 = block * kTileN + quarter * kDecodeKeys;
+  if (key0 >= length || key0 + kDecodeKeys <= lo) return;
+  const uint8_t *src = value ? c.V : c.K, *exps = value ? c.vs : c.ks;
+  uint4 x[kSteps];
+  uint32_t e[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int key = key0 + i * kRows + lane / kLanes, page = key < length && key >= lo ? cache_page(c, b, key) : -1;
+    const int64_t slot = ((int64_t)head << c.page_shift) + (key & ((1 << c.page_shift) - 1));
+    x[i] = page >= 0 ? *reinterpret_cast<const uint4*>(src + page * c.page_bytes + slot * D + sub * 16) : make_uint4(0, 0, 0, 0);
+    e[i] = page >= 0 ? exps[page * c.scale_stride + slot] : 0u;
+  }
+  uint8_t* dst = (value ? out.V : out.K) + (int64_t)(b * out.table_stride + block) * out.page_bytes +
+                 ((int64_t)head * kTileN + quarter * kDecodeKeys) * (2 * D);
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const float s = scale_of_exponent(e[i]);
+    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+    uint32_t o[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 u = f16x2_to_float2(e4m3x2_to_f16x2(w[k] & 0xffffu)), v = f16x2_to_float2(e4m3x2_to_f16x2(w[k] >> 16));
+      o[2 * k] = pack_bf16(u.x * s, u.y * s);
+      o[2 * k + 1] = pack_bf16(v.x * s, v.y * s);
+    }
+    uint4* row = reinterpret_cast<uint4*>(dst + (i * kRows + lane / kLanes) * (2 * D) + sub * 32);
+    row[0] = make_uint4(o[0], o[1], o[2], o[3]);
+    row[1] = make_uint4(o[4], o[5], o[6], o[7]);
+  }
+}
+
+// The first CTA plans; the others, a row of the grid for each sequence, decode.
+template <int D>
+__global__ void __launch_bounds__(kPlanThreads) cache_prepare_kernel(const ChunkArgs p) {
+  dependency_wait();
+  dependents_release();
+  if (blockIdx.x == 0) {
+    if (blockIdx.y != 0) return;
+    if (p.clear && threadIdx.x == 0) *p.f.status = 0;
+    make_plan(p);
+    return;
+  }
+  const int item = (blockIdx.x - 1) * (kPlanThreads / 32) + (threadIdx.x >> 5);
+  decode_cache<D>(p, item, blockIdx.y);
 }
 
 // ------------------------------------------------------------------------------------------------------------- pieces
@@ -1169,6 +1234,13 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
+// An 8-bit cache is decoded once where a sequence can have kDecodeRows rows of a KV head or more: its keys are then used by that many
+// 256-row groups, and each use would decode them again.  Not for copies beyond kMostDecoded bytes.
+constexpr int64_t kDecodeRows = 1024, kMostDecoded = 4ll << 30;
+int decoded_pages(int Lk) { return (Lk + kTileN - 1) / kTileN; }
+int64_t decoded_bytes(int B, int Lk, int Hkv, int D) { return 2ll * B * decoded_pages(Lk) * Hkv * kTileN * D * 2; }
+bool may_decode(int kind, int Lq, int G) { return kind == L2A_CACHE_E4M3 && (int64_t)Lq * G >= kDecodeRows; }
+
 size_t layout(int B, int n_tokens, int G, int Hkv, int D, uint8_t* base, ChunkWs* w) {
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -1191,6 +1263,12 @@ size_t layout(int B, int n_tokens, int G, int Hkv, int D, uint8_t* base, ChunkWs
   return at;
 }
 
+template <int D>
+cudaError_t launch_prepare(const ChunkArgs& p, bool decode, bool first, cudaStream_t s) {
+  const unsigned items = decode ? (unsigned)(p.f.c.table_stride * p.f.c.Hkv * 8) : 0, per = kPlanThreads / 32;
+  return launch_dependent(cache_prepare_kernel<D>, dim3(1 + (items + per - 1) / per, decode ? p.f.c.B : 1), kPlanThreads, 0, s, !first, p);
+}
+
 template <int D, bool kE4M3>
 cudaError_t launch_chunk(const ChunkArgs& p, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t s) {
   constexpr int smem = ChunkSmem<D, kE4M3>::kTotal;
@@ -1198,8 +1276,6 @@ cudaError_t launch_chunk(const ChunkArgs& p, const CUtensorMap& mapK, const CUte
   cudaError_t e = once.run([] {
     return cudaFuncSetAttribute(cache_chunk_kernel<D, kE4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   });
-  if (e != cudaSuccess) return e;
-  e = launch_dependent(cache_plan_kernel, dim3(1), kPlanThreads, 0, s, p.f.G <= kFewRows, p);
   if (e != cudaSuccess) return e;
   e = launch_dependent(cache_chunk_kernel<D, kE4M3>, dim3(kCtas), kChunkThreads, smem, s, true, mapK, mapV, p);
   if (e != cudaSuccess) return e;
@@ -1211,19 +1287,40 @@ cudaError_t launch_chunk(const ChunkArgs& p, const CUtensorMap& mapK, const CUte
 
 }  // namespace
 
-size_t cache_chunk_ws_bytes(const l2a_params* p, int n_tokens) {
-  return layout(p->B, n_tokens, p->Hq / p->Hkv, p->Hkv, p->D, nullptr, nullptr);
+size_t cache_chunk_ws_bytes(const l2a_params* p, int kind, int n_tokens) {
+  const int G = p->Hq / p->Hkv;
+  const int64_t copy = may_decode(kind, p->Lq, G) ? std::min(decoded_bytes(p->B, p->Lk, p->Hkv, p->D), kMostDecoded) : 0;
+  return layout(p->B, n_tokens, G, p->Hkv, p->D, nullptr, nullptr) + (size_t)copy;
 }
 
-cudaError_t launch_cache_chunk(const CacheFwdArgs& a, void* ws, cudaStream_t s) {
+cudaError_t launch_cache_chunk(const CacheFwdArgs& a, bool first, void* ws, cudaStream_t s) {
   ChunkArgs p;
   p.f = a;
-  layout(a.c.B, a.c.n_tokens, a.G, a.c.Hkv, a.c.D, static_cast<uint8_t*>(ws), &p.w);
-  const bool e4m3 = a.c.kind == L2A_CACHE_E4M3;
+  p.clear = first;
+  const size_t at = layout(a.c.B, a.c.n_tokens, a.G, a.c.Hkv, a.c.D, static_cast<uint8_t*>(ws), &p.w);
+  const int64_t copy = decoded_bytes(a.c.B, a.c.max_keys, a.c.Hkv, a.c.D);
+  const bool decode = may_decode(a.c.kind, a.c.Lq, a.G) && copy <= kMostDecoded && a.c.B <= 65535;
+  p.codes = a.c;
+  if (decode) {
+    CacheView& c = p.f.c;
+    c.kind = L2A_CACHE_BF16;
+    c.K = static_cast<uint8_t*>(ws) + at;
+    c.V = c.K + copy / 2;
+    c.ks = c.vs = nullptr;
+    c.page_bytes = (int64_t)c.Hkv * kTileN * c.D * 2;
+    c.page_shift = 7;
+    c.table = nullptr;
+    c.table_stride = decoded_pages(c.max_keys);
+    c.n_pages = c.B * c.table_stride;
+  }
+  const CacheView& c = p.f.c;
+  const bool e4m3 = c.kind == L2A_CACHE_E4M3;
   CUtensorMap mapK, mapV;
-  const int rows = 1 << a.c.page_shift;
-  if (!encode_pool_map(&mapK, a.c, a.c.K, rows, 1) || !encode_pool_map(&mapV, a.c, a.c.V, rows, 1)) return cudaErrorUnknown;
-  if (a.c.D == 128) return e4m3 ? launch_chunk<128, true>(p, mapK, mapV, s) : launch_chunk<128, false>(p, mapK, mapV, s);
+  const int rows = 1 << c.page_shift;
+  if (!encode_pool_map(&mapK, c, c.K, rows, 1) || !encode_pool_map(&mapV, c, c.V, rows, 1)) return cudaErrorUnknown;
+  const cudaError_t e = c.D == 128 ? launch_prepare<128>(p, decode, first, s) : launch_prepare<64>(p, decode, first, s);
+  if (e != cudaSuccess) return e;
+  if (c.D == 128) return e4m3 ? launch_chunk<128, true>(p, mapK, mapV, s) : launch_chunk<128, false>(p, mapK, mapV, s);
   return e4m3 ? launch_chunk<64, true>(p, mapK, mapV, s) : launch_chunk<64, false>(p, mapK, mapV, s);
 }
 

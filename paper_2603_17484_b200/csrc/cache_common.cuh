@@ -33,8 +33,9 @@ __device__ __forceinline__ int cache_new(const CacheView& c, int b, int& first) 
   return first >= 0 && n > 0 && n <= c.Lq && first <= c.n_tokens - n ? n : 0;
 }
 
-// Page of a position of sequence b, -1: none
+// Page of a position of sequence b, -1: none.  Without a table (a copy in the workspace) the pages of a sequence follow each other.
 __device__ __forceinline__ int cache_page(const CacheView& c, int b, int pos) {
+  if (c.table == nullptr) return b * c.table_stride + (pos >> c.page_shift);
   const int page = c.table[(int64_t)b * c.table_stride + (pos >> c.page_shift)];
   return page >= 0 && page < c.n_pages ? page : -1;
 }
@@ -62,8 +63,8 @@ size_t cache_few_ws_bytes(const l2a_params* p);     // plan and parts
 cudaError_t launch_cache_few(CacheFwdArgs& a, void* ws, cudaStream_t s);
 
 // All others: cache_chunk.cu
-size_t cache_chunk_ws_bytes(const l2a_params* p, int n_tokens);
-cudaError_t launch_cache_chunk(const CacheFwdArgs& a, void* ws, cudaStream_t s);
+size_t cache_chunk_ws_bytes(const l2a_params* p, int kind, int n_tokens);
+cudaError_t launch_cache_chunk(const CacheFwdArgs& a, bool first, void* ws, cudaStream_t s);     // first: no kernel of the call ahead
 
 // Tensor map over a pool: {elements of 128 bytes at most, tokens, (pieces of a row,) heads, pages}; one copy brings box_rows
 // tokens of one head of one page, box_pieces * 64 elements of each (bf16) or the whole row of codes.

@@ -37,7 +37,7 @@ extern "C" l2a_status l2a_cache_workspace_bytes(const l2a_params* p, const l2a_c
   const l2a_status st = check_forward(p, c, n_tokens, &v);
   if (st != L2A_OK) return st;
   if (!ws_bytes) return L2A_ERR_INVALID_ARG;
-  *ws_bytes = kWsHeaderBytes + (has_few(p) ? cache_few_ws_bytes(p) : 0) + (has_chunks(p) ? cache_chunk_ws_bytes(p, n_tokens) : 0);
+  *ws_bytes = kWsHeaderBytes + (has_few(p) ? cache_few_ws_bytes(p) : 0) + (has_chunks(p) ? cache_chunk_ws_bytes(p, c->kind, n_tokens) : 0);
   return L2A_OK;
 }
 
@@ -70,10 +70,13 @@ extern "C" l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c,
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   uint8_t* at = static_cast<uint8_t*>(ws) + kWsHeaderBytes;
   cudaError_t e = cudaSuccess;
+  bool first = true;
   if (has_few(p)) {
-    e = launch_cache_few(a, at, s);
+    // (without a list of new tokens every sequence has the same number)
+    first = cu_new == nullptr && has_chunks(p);
+    if (!first) e = launch_cache_few(a, at, s);
     at += cache_few_ws_bytes(p);
   }
-  if (e == cudaSuccess && has_chunks(p)) e = launch_cache_chunk(a, at, s);
+  if (e == cudaSuccess && has_chunks(p)) e = launch_cache_chunk(a, first, at, s);
   return e == cudaSuccess ? L2A_OK : L2A_ERR_CUDA;
 }
