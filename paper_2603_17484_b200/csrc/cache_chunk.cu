@@ -309,25 +309,26 @@ __device__ __forceinline__ void decode_cache(const ChunkArgs& p, int item, int b
   int first;
   const int n = cache_new(c, b, first), length = cache_length(c, b);
   if (!is_chunk(a, n)) return;
-  // all keys where a token is routed, else those of the windows
-  bool routed = false;
-  if (a.global && a.d != nullptr)
-    for (int i = threadIdx.x; i < n; i += kPlanThreads) routed |= a.d[first + i] != 0;
-  routed = __syncthreads_or(routed);
-  const int lo = routed ? 0 : max(0, length - n - a.window);
   const int value = item & 1, quarter = (item >> 1) & 3, head = (item >> 3) % c.Hkv, block = (item >> 3) / c.Hkv;
-  const int key0 = block * kTileN + quarter * kDecodeKeys;
-  if (key0 >= length || key0 + kDecodeKeys <= lo) return;
+  const int key0 = block * kTileN + quarter * kDecodeKeys, window = max(0, length - n - a.window);
+  const bool may_route = a.global && a.d != nullptr, inside = key0 < length && (may_route || key0 + kDecodeKeys > window);
   const uint8_t *src = value ? c.V : c.K, *exps = value ? c.vs : c.ks;
   uint4 x[kSteps];
   uint32_t e[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const int key = key0 + i * kRows + lane / kLanes, page = key < length && key >= lo ? cache_page(c, b, key) : -1;
+    const int key = key0 + i * kRows + lane / kLanes;
+    const int page = inside && key < length && (may_route || key >= window) ? cache_page(c, b, key) : -1;
     const int64_t slot = ((int64_t)head << c.page_shift) + (key & ((1 << c.page_shift) - 1));
     x[i] = page >= 0 ? *reinterpret_cast<const uint4*>(src + page * c.page_bytes + slot * D + sub * 16) : make_uint4(0, 0, 0, 0);
     e[i] = page >= 0 ? exps[page * c.scale_stride + slot] : 0u;
   }
+  // all keys where a token is routed, else those of the windows (looked up while the codes are on their way)
+  bool routed = false;
+  if (may_route)
+    for (int i = threadIdx.x; i < n; i += kPlanThreads) routed |= a.d[first + i] != 0;
+  routed = __syncthreads_or(routed);
+  if (!inside || (!routed && key0 + kDecodeKeys <= window)) return;
   uint8_t* dst = (value ? out.V : out.K) + (int64_t)(b * out.table_stride + block) * out.page_bytes +
                  ((int64_t)head * kTileN + quarter * kDecodeKeys) * (2 * D);
 #pragma unroll
@@ -370,14 +371,21 @@ struct ChunkPiece {
 };
 // The pieces of a CTA's range in order; every warp walks through them by itself, and reads of a group what it needs (few
 // registers: those of the soft-max warps are taken by the scores).
+constexpr int kKeepGroups = 16;
 struct ChunkWalk {
   int at, end, group, head, block, n_groups;
-  __device__ __forceinline__ bool init(const ChunkWs& w) {
+  const Group* kept;       // the first kKeepGroups of the range, in shared memory
+  int kept_from;
+  __device__ __forceinline__ const Group& group_now(const ChunkWs& w) const {
+    return group - kept_from < kKeepGroups ? kept[group - kept_from] : w.groups[group];
+  }
+  __device__ __forceinline__ bool init(const ChunkWs& w, const Group* keep) {
     const int cta = blockIdx.x;
+    kept = keep;
     n_groups = w.plan->n_groups;
     const int4 s = *reinterpret_cast<const int4*>(&w.plan->start[cta]);
     at = s.x;
-    group = s.y;
+    group = kept_from = s.y;
     head = s.z;
     block = s.w;
     end = w.plan->start[cta + 1].at;
@@ -387,7 +395,7 @@ struct ChunkWalk {
     if (at >= end) return false;
     int n, jlo;
     for (;;) {
-      const int2 j = *reinterpret_cast<const int2*>(&w.groups[group].jlo);
+      const int2 j = *reinterpret_cast<const int2*>(&group_now(w).jlo);
       jlo = j.x;
       n = j.y - j.x + 1;
       if (head < Hkv && block < n) break;
@@ -436,7 +444,8 @@ struct ChunkSmem {
   static constexpr int kRawOff = kVOff + kVStages * kVTileBytes;
   static constexpr int kScaleOff = kRawOff + kVStages * kRawBytes;       // scales of K, by key
   static constexpr int kBarOff = kScaleOff + (kE4M3 ? kScaleSlots * kTileN * 4 : 0);
-  static constexpr int kTotal = kBarOff + kBarBytes + 1024 /* alignment slack */;
+  static constexpr int kGroupOff = kBarOff + kBarBytes;
+  static constexpr int kTotal = kGroupOff + kKeepGroups * (int)sizeof(Group) + 1024 /* alignment slack */;
 };
 
 struct ChunkBars {
@@ -504,7 +513,8 @@ struct RowOf {
   int token, head, lo, hi;       // first and last key that it sees
   int min_hi, max_lo;            // of the tile
   int slot, first_block, n_blocks;
-  bool valid, seg, complete;     // complete: the piece holds all of the row's keys in this segment
+  bool valid, seg, finished;     // finished: the piece holds all that the row has to see
+  bool routed;
 };
 
 template <int D, bool kE4M3>
@@ -526,6 +536,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
   uint8_t* sRaw = smem + SM::kRawOff;
   float* sScale = reinterpret_cast<float*>(smem + SM::kScaleOff);
   ChunkBars* bar = reinterpret_cast<ChunkBars*>(smem + SM::kBarOff);
+  Group* sGroups = reinterpret_cast<Group*>(smem + SM::kGroupOff);
   volatile int* abort_flag = &bar->abort_flag;
 
   if (tid == kTmaWarp * 32) {
@@ -556,6 +567,12 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
   }
   dependency_wait();
   dependents_release();
+  {
+    constexpr int kWords = sizeof(Group) / 16;
+    const int from = w.plan->start[blockIdx.x].group, n = min(kKeepGroups, w.plan->n_groups - from);
+    for (int i = tid; i < n * kWords; i += kChunkThreads)
+      reinterpret_cast<uint4*>(sGroups)[i] = reinterpret_cast<const uint4*>(w.groups + from)[i];
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -577,14 +594,14 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     }
     ChunkWalk walk;
     ChunkPiece pc;
-    bool ok = walk.init(w);
+    bool ok = walk.init(w, sGroups);
     // a lane copies the rows of page `u` of a block, in bf16 64 columns of them
     const int rows = 1 << c.page_shift, copies = 128 >> c.page_shift, u = lane % copies, piece = lane / copies;
     const bool active = piece < (kE4M3 ? 1 : D / 64);
     const uint32_t bytes = rows * (kE4M3 ? D : 128);
     uint32_t k_slot = 0, k_ph = 1, v_cnt = 0;
     while (ok && walk.next(w, c.Hkv, pc)) {
-      const Group& g = w.groups[walk.group];
+      const Group& g = walk.group_now(w);
       const int b = g.b, key_lo = g.key_lo, key_hi = g.key_hi, step = g.dual ? 2 : 1;
       const int first_entry = key_lo >> c.page_shift, last_entry = key_hi >> c.page_shift;
       int entry0 = -512, page_ids = -1;
@@ -664,11 +681,11 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       uint32_t k_slot = 0, k_ph = 0;
       ChunkWalk walk;
       ChunkPiece pc;
-      bool ok = walk.init(w);
+      bool ok = walk.init(w, sGroups);
       uint32_t it = 0;
       while (ok && walk.next(w, c.Hkv, pc)) {
-        const TileBlocks tb[2] = {tile_blocks(w.groups[walk.group], pc, 0), tile_blocks(w.groups[walk.group], pc, 1)};
-        const bool dual = w.groups[walk.group].dual;
+        const TileBlocks tb[2] = {tile_blocks(walk.group_now(w), pc, 0), tile_blocks(walk.group_now(w), pc, 1)};
+        const bool dual = walk.group_now(w).dual;
         auto takes = [&](int t, int j) {
           return t ? j >= tb[1].first && j <= tb[1].last && (!dual || (j & 1)) : j >= tb[0].first && j <= tb[0].last && (!dual || !(j & 1));
         };
@@ -738,10 +755,10 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     const int row = (warp - kConvWarp) * 32 + lane;      // this thread's key of a block
     ChunkWalk walk;
     ChunkPiece pc;
-    bool ok = walk.init(w);
+    bool ok = walk.init(w, sGroups);
     uint32_t it = 0;
     while (ok && walk.next(w, c.Hkv, pc)) {
-      const Group& g = w.groups[walk.group];
+      const Group& g = walk.group_now(w);
       const int b = g.b, key_lo = g.key_lo, key_hi = g.key_hi;
       // page of this thread's key two blocks ahead, the exponents of its rows of K and V one block ahead
       auto page_of = [&](int j) -> int {
@@ -825,14 +842,15 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     // The next piece and this thread's row of it
     auto advance = [&]() -> bool {
       if (!walk.next(w, c.Hkv, pc)) return false;
-      const Group& g = w.groups[walk.group];
+      const Group& g = walk.group_now(w);
       me.tb = tile_blocks(g, pc, t);
       me.min_hi = t ? g.min_hi1 : g.min_hi0;
       me.max_lo = t ? g.max_lo1 : g.max_lo0;
       const int dual = g.dual, seg = g.seg, tile_row = (dual ? 0 : t * kTileM) + r;
       me.valid = tile_row < g.n_rows;
       me.seg = seg;
-      me.complete = pc.whole && !dual;
+      me.finished = pc.whole && !dual && (!seg || !a.local);
+      me.routed = false;
       me.slot = pc.item + blockIdx.x;
       me.first_block = pc.j0;
       me.n_blocks = pc.j1 - pc.j0 + 1;
@@ -846,6 +864,10 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         const int pos = g.off + me.token - g.first;
         me.hi = pos - (seg ? a.shift : 0);
         me.lo = seg ? 0 : pos - a.window;
+        if (!seg) {
+          if (w.token[me.token].rank >= 0) me.finished = false;
+          me.routed = a.global && a.d != nullptr && a.d[me.token] != 0;
+        }
       }
       if (me.valid) {
         const bf16* q = a.q + me.token * a.q_t + (int64_t)me.head * D;
@@ -902,7 +924,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       return factor;
     };
 
-    bool ok = walk.init(w);
+    bool ok = walk.init(w, sGroups);
     bool more = ok && advance();
     float row_scale = a.scale_log2;
     if (more && me.tb.first <= me.tb.last) row_scale = store_q();
@@ -1032,16 +1054,15 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
 
       // ---- a row that has nothing else to be joined with leaves finished, others go to the piece's slot
       const bool valid = cur.valid;
-      const bool finished = cur.complete && (cur.seg ? !a.local : valid && w.token[cur.token].rank < 0);
       float* slot = w.part + (size_t)cur.slot * slot_floats(D) + t * kTileM * (D + 2);
-      bf16* dst = nullptr;
+      bf16* dst = cur.finished && valid ? a.O + cur.token * a.o_t + (int64_t)cur.head * D : nullptr;
       const float back = kE4M3 ? fast_exp2(v_first) : 1.f;           // the accumulators lack the exponent of the first values
-      float inv_l = 0.f;
-      if (finished && valid) {
-        const bool routed = a.global && a.d != nullptr && a.d[cur.token] != 0;
-        dst = a.O + cur.token * a.o_t + (int64_t)cur.head * D;
-        inv_l = l > 0.f ? back * (cur.seg || !routed ? 1.f : 2.f) / l : 0.f;      // (no key before the window: a = s)
-      }
+      const float inv_l = l > 0.f ? back * (cur.routed ? 2.f : 1.f) / l : 0.f;      // (finished and routed: no key before the window, a = s)
+      // Four lanes, four rows: each lane stores the same 16 bytes of all four, so that a store covers 64 bytes of a row
+      bf16* rows[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        rows[k] = reinterpret_cast<bf16*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), (lane & ~3) + k));
 #pragma unroll 1
       for (int q = 0; q < D / 32; ++q) {
         uint32_t o[32];
@@ -1060,36 +1081,45 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0u;                      // no block of this tile: the accumulator was never written
         }
-        if (dst != nullptr) {
-          uint4* d4 = reinterpret_cast<uint4*>(dst + q * 32);
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            float f[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(o[8 * x + e]) * inv_l;
-            if (a.add) {
-              const uint4 old = d4[x];
-              const uint32_t ow[4] = {old.x, old.y, old.z, old.w};
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                f[2 * e] += __uint_as_float(ow[e] << 16);
-                f[2 * e + 1] += __uint_as_float(ow[e] & 0xffff0000u);
-              }
-            }
-            d4[x] = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-          }
-        } else if (valid) {
-          if (kE4M3) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * back);
-          }
+        if (valid && !cur.finished) {
 #pragma unroll
           for (int x = 0; x < 8; ++x)
-            *reinterpret_cast<uint4*>(slot + ((q * 8 + x) * kTileM + r) * 4) =
-                make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+            *reinterpret_cast<float4*>(slot + ((q * 8 + x) * kTileM + r) * 4) =
+                make_float4(__uint_as_float(o[4 * x]) * back, __uint_as_float(o[4 * x + 1]) * back, __uint_as_float(o[4 * x + 2]) * back,
+                            __uint_as_float(o[4 * x + 3]) * back);
+        }
+        if (__any_sync(0xffffffffu, dst != nullptr)) {
+          float2 old[16];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const uint4 u = a.add && dst != nullptr ? reinterpret_cast<const uint4*>(dst + q * 32)[x] : make_uint4(0, 0, 0, 0);
+            const uint32_t ow[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) old[4 * x + e] = make_float2(__uint_as_float(ow[e] << 16), __uint_as_float(ow[e] & 0xffff0000u));
+          }
+          uint32_t pk[4][4];
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            pk[e / 4][e % 4] = pack_bf16(fmaf(__uint_as_float(o[2 * e]), inv_l, old[e].x), fmaf(__uint_as_float(o[2 * e + 1]), inv_l, old[e].y));
+#pragma unroll
+          for (int step = 1; step <= 2; step *= 2) {
+            const bool up = lane & step;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              if (x & step) continue;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? pk[x][e] : pk[x + step][e], step);
+                if (up) pk[x][e] = got; else pk[x + step][e] = got;
+              }
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (rows[k] != nullptr) reinterpret_cast<uint4*>(rows[k] + q * 32)[lane & 3] = make_uint4(pk[k][0], pk[k][1], pk[k][2], pk[k][3]);
         }
       }
-      if (dst == nullptr && valid) {
+      if (valid && !cur.finished) {
         slot[kTileM * D + r] = kE4M3 ? m_use - v_first - kWeightTop : m_use;
         slot[kTileM * (D + 1) + r] = any ? l : 0.f;
       }
