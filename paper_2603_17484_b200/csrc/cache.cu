@@ -83,12 +83,6 @@ __device__ __forceinline__ uint32_t finite_magnitudes(uint32_t x) {
   x &= 0x7fff7fffu;
   return __vcmpltu2(x, 0x7f807f80u) & x;
 }
-__device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-
 // A lane holds 16 values of a row, D / 16 lanes a row, a warp 512 / D tokens of one head of K or V at a time, kSteps times: the
 // warps of a CTA take the heads of the same tokens, so that it reads whole token rows, and the exponents of
 // a warp's tokens, neighbours in a page, leave in one sector.
@@ -156,8 +150,8 @@ __global__ void __launch_bounds__(kRowsThreads) cache_append_kernel(const Append
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t u = w[2 * k], v = w[2 * k + 1];
-        code[k] = to_e4m3x2(__uint_as_float(u << 16) * inv, __uint_as_float(u & 0xffff0000u) * inv) |
-                  to_e4m3x2(__uint_as_float(v << 16) * inv, __uint_as_float(v & 0xffff0000u) * inv) << 16;
+        code[k] = pack_e4m3(__uint_as_float(u << 16) * inv, __uint_as_float(u & 0xffff0000u) * inv) |
+                  pack_e4m3(__uint_as_float(v << 16) * inv, __uint_as_float(v & 0xffff0000u) * inv) << 16;
       }
       if (page >= 0) {
         *reinterpret_cast<uint4*>(dst + sub * 16) = make_uint4(code[0], code[1], code[2], code[3]);

@@ -43,9 +43,8 @@ constexpr int kBoxBytes = 128 * 128;       // 128 rows of 128 bytes
 constexpr float kWeightTop = 7.0f;         // e4m3: weights lie at 2^7 and, while the reference lags, up to 2^15 (fp16 operands)
 constexpr int kPlanThreads = 1024;
 constexpr int kCtas = kSplitSms;
-constexpr int kItemCost = 3;               // key blocks' time that a piece costs besides its blocks
-constexpr int kMinCost = 8;                // of a CTA
-constexpr int kMinPiece = 2;
+constexpr int kItemCost = 5;               // key blocks' time that a piece costs besides its blocks
+constexpr int kMinPiece = 1;
 
 // A group of rows
 struct alignas(16) Group {
@@ -277,7 +276,7 @@ __device__ void make_plan(const ChunkArgs& p) {
   }
   __syncthreads();
   // ---- where the CTAs' ranges start
-  const int ctas = max(1, min(kCtas, base_cost / kMinCost));
+  const int ctas = max(1, min(kCtas, base_blocks));
   if (tid == 0) { w.plan->n_groups = n_groups; w.plan->ctas = ctas; }
   if (tid <= kCtas) {
     Start s = {tid == 0 ? 0 : base_blocks, 0, 0, 0};
@@ -460,31 +459,19 @@ struct ChunkBars {
 };
 static_assert(sizeof(ChunkBars) <= kBarBytes, "barriers");
 
-// 16 codes times a power of two as fp16; scale2: 2^8 times it, twice.  Of every four codes 0 and 2 come first, then 1 and 3: the
-// columns of the accumulators are put back in order.
+// 16 codes times a power of two (two of it) as fp16
 __device__ __forceinline__ void scaled_codes(const float4& codes, uint32_t scale2, uint32_t (&o)[8]) {
   const uint32_t w[4] = {__float_as_uint(codes.x), __float_as_uint(codes.y), __float_as_uint(codes.z), __float_as_uint(codes.w)};
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * k]) : "r"(codes_02_f16(w[k])), "r"(scale2));
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * k + 1]) : "r"(codes_13_f16(w[k])), "r"(scale2));
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * k]) : "r"(e4m3x2_to_f16x2(w[k] & 0xffffu)), "r"(scale2));
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * k + 1]) : "r"(e4m3x2_to_f16x2(w[k] >> 16)), "r"(scale2));
   }
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
-}
-// Two values as the sum of two e4m3 numbers: the nearest, and the nearest to what it leaves
-__device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
-  uint16_t r;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-__device__ __forceinline__ void two_terms(float x, float y, uint32_t& first, uint32_t& second) {
-  first = pack_e4m3(x, y);
-  const float2 f = f16x2_to_float2(e4m3x2_to_f16x2(first));
-  second = pack_e4m3(x - f.x, y - f.y);
 }
 // Instruction descriptor, kind::f8f6f4: e4m3 x e4m3 -> fp32, both K-major
 __host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N) {
@@ -760,7 +747,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     while (ok && walk.next(w, c.Hkv, pc)) {
       const Group& g = walk.group_now(w);
       const int b = g.b, key_lo = g.key_lo, key_hi = g.key_hi;
-      // page of this thread's key two blocks ahead, the exponents of its rows of K and V one block ahead
+      // page of this thread's key three blocks ahead, the exponents of its rows of K and V two blocks ahead
       auto page_of = [&](int j) -> int {
         const int key = j * kTileN + row;
         return kE4M3 && key >= key_lo && key <= key_hi ? cache_page(c, b, key) : -1;
@@ -770,27 +757,38 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         const int64_t at = page * c.scale_stride + ((int64_t)pc.head << c.page_shift) + ((j * kTileN + row) & ((1 << c.page_shift) - 1));
         return c.ks[at] | (uint32_t)c.vs[at] << 8;
       };
-      uint32_t exps = exponents(pc.j0, page_of(pc.j0));
-      int page = page_of(pc.j0 + 1);
+      // The values of a warp's 32 keys get the scale of the largest among them: the codes of the others times a power of two below one,
+      // exact in fp16 down to 2^-24, which is 2^-33 of the largest value.  Returns that factor, twice; `at`: the block's count.
+      auto publish = [&](uint32_t exps, uint32_t at) -> uint32_t {
+        const int slot = at & (kScaleSlots - 1), e = (int)(exps >> 8);
+        int top = __reduce_max_sync(0xffffffffu, e);
+        if (top == 0) top = 127;
+        sScale[slot * kTileN + row] = scale_of_exponent(exps & 0xffu);
+        if (lane == 0) reinterpret_cast<float*>(&bar->v_exp[slot])[warp - kConvWarp] = (float)(top - 127);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar->scale_full[slot]);
+        const float f = __uint_as_float((uint32_t)max(e - top + 127, 0) << 23);
+        return pack_f16(f, f);
+      };
+      uint32_t ahead = 0, scale2 = 0, next_scale2 = 0;
+      int page = -1;
+      if (kE4M3) {
+        next_scale2 = publish(exponents(pc.j0, page_of(pc.j0)), it);
+        ahead = exponents(pc.j0 + 1, page_of(pc.j0 + 1));
+        page = page_of(pc.j0 + 2);
+      }
       for (int j = pc.j0; ok && j <= pc.j1; ++j, ++it) {
         const int s = it & 1, key = j * kTileN + row;
         const uint32_t ph = (it >> 1) & 1;
         const bool seen = key >= key_lo && key <= key_hi;
-        const uint32_t ahead = exponents(j + 1, page);
-        page = page_of(j + 2);
+        if (kE4M3) {
+          scale2 = next_scale2;
+          if (j < pc.j1) next_scale2 = publish(ahead, it + 1);
+          ahead = exponents(j + 2, page);
+          page = page_of(j + 3);
+        }
         const uint32_t dst = smem_u32(sV + s * SM::kVTileBytes) + row * 128;
         if (kE4M3) {
-          // The values of a warp's 32 keys get the scale of the largest among them: the codes of the others times a power of two
-          // below one, exact in fp16 down to 2^-24, which is 2^-33 of the largest value.
-          const int slot = it & (kScaleSlots - 1), e = (int)(exps >> 8);
-          int top = __reduce_max_sync(0xffffffffu, e);
-          if (top == 0) top = 127;
-          sScale[slot * kTileN + row] = scale_of_exponent(exps & 0xffu);
-          if (lane == 0) reinterpret_cast<float*>(&bar->v_exp[slot])[warp - kConvWarp] = (float)(top - 127);
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&bar->scale_full[slot]);
-          const float f = __uint_as_float((uint32_t)max(e - top + 127 + 8, 0) << 23);
-          const uint32_t scale2 = pack_f16(f, f);
           if (!mbar_wait_warp(&bar->raw_full[s], ph, abort_flag)) { ok = false; break; }
           const uint32_t src = smem_u32(sRaw + s * SM::kRawBytes) + row * D;
           float4 x[D / 16];
@@ -821,7 +819,6 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
           }
         }
         mbar_arrive(&bar->v_full[s]);
-        exps = ahead;
       }
     }
   } else if (warp > kMmaWarp) {
@@ -906,7 +903,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
           uint32_t first[4], second[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            two_terms(__uint_as_float(u[e] << 16) * f, __uint_as_float(u[e] & 0xffff0000u) * f, first[e], second[e]);
+            two_e4m3_terms(__uint_as_float(u[e] << 16) * f, __uint_as_float(u[e] & 0xffff0000u) * f, first[e], second[e]);
           const uint32_t dst = base + rr * D + (((piece >> 1) ^ (D == 128 ? rr & 7 : (rr >> 1) & 3)) << 4) + (piece & 1) * 8;
           asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(dst), "r"(first[0] | first[1] << 16), "r"(first[2] | first[3] << 16) : "memory");
           asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(dst + kTileM * D), "r"(second[0] | second[1] << 16),
@@ -932,14 +929,14 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     while (more) {
       const RowOf cur = me;
       const TileBlocks tb = cur.tb;
-      const bool any = tb.first <= tb.last;
+      const bool any = tb.first <= tb.last, warp_has_rows = __any_sync(0xffffffffu, cur.valid);
       float m_use = -INFINITY;   // reference maximum, exp2 domain
       float l = 0.f;             // row sum
       float v_first = 0.f;       // e4m3: exponent of the first values, which the sum's terms are taken relative to
       for (int j = tb.first; j <= tb.last; j += tb.step) {
         float ev[4];             // e4m3: exponent of the values of each 32 keys
         const uint32_t it = it0 + (j - cur.first_block);
-        if (kE4M3) {
+        if (kE4M3 && warp_has_rows) {
           const uint32_t slot = it & (kScaleSlots - 1);
           if (!mbar_wait_warp(&bar->scale_full[slot], (it / kScaleSlots) & 1, abort_flag)) { ok = false; break; }
           const float4 y = lds128(smem_u32(&bar->v_exp[slot]));
@@ -950,6 +947,11 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         if (!mbar_wait_warp(&bar->s_full[t], s_cnt & 1, abort_flag)) { ok = false; break; }
         ++s_cnt;
         tc_fence_after();
+        if (!warp_has_rows) {    // nothing of these rows is ever stored
+          mbar_arrive(&bar->p_half[t]);
+          mbar_arrive(&bar->p_full[t]);
+          continue;
+        }
         const int k0 = j * kTileN;
         const bool partial = k0 + kTileN - 1 > cur.min_hi || k0 < cur.max_lo;
         uint32_t v[4][32];       // the row's scores of this key block
@@ -1019,7 +1021,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
           for (int e = 0; e < 16; ++e) {
             const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[q][2 * e]), __uint_as_float(v[q][2 * e + 1])),
                                         make_float2(mul, mul), make_float2(add, add));
-            const float2 z = e % 4 == 3 ? exp2_fma2(y) : make_float2(fast_exp2(y.x), fast_exp2(y.y));
+            const float2 z = !kE4M3 && e % 4 == 3 ? exp2_fma2(y) : make_float2(fast_exp2(y.x), fast_exp2(y.y));
             if (kE4M3) part = __fadd2_rn(part, z);
             else sum2 = __fadd2_rn(sum2, z);
             pk[e] = kE4M3 ? pack_f16(z.x, z.y) : pack_bf16(z.x, z.y);
@@ -1069,14 +1071,6 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         if (any) {
           tmem_ld32(o_addr + q * 32, o);
           tmem_ld_wait();
-          if (kE4M3) {
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              const uint32_t y = o[e + 1];
-              o[e + 1] = o[e + 2];
-              o[e + 2] = y;
-            }
-          }
         } else {
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0u;                      // no block of this tile: the accumulator was never written

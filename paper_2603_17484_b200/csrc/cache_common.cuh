@@ -76,14 +76,21 @@ __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t codes) {
   asm("{\n .reg .b16 c;\n cvt.u16.u32 c, %1;\n cvt.rn.f16x2.e4m3x2 %0, c;\n}" : "=r"(r) : "r"(codes));
   return r;
 }
-// The same on the integer pipe, times 2^-8 (the exponent's bits keep their bias of 7): codes 1 and 3, or 0 and 2, of a word.  The
-// conversion instruction runs on the special-function unit, which the exponentials need.
-__device__ __forceinline__ uint32_t codes_13_f16(uint32_t w) { return ((w >> 1) & 0x3f803f80u) | (w & 0x80008000u); }
-__device__ __forceinline__ uint32_t codes_02_f16(uint32_t w) { return ((w << 7) & 0x3f803f80u) | ((w << 8) & 0x80008000u); }
 __device__ __forceinline__ float2 f16x2_to_float2(uint32_t v) {
   float2 f;
   asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}" : "=f"(f.x), "=f"(f.y) : "r"(v));
   return f;
+}
+// Two values as the sum of two e4m3 numbers each: the nearest, and the nearest to what it leaves
+__device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ void two_e4m3_terms(float x, float y, uint32_t& first, uint32_t& second) {
+  first = pack_e4m3(x, y);
+  const float2 f = f16x2_to_float2(e4m3x2_to_f16x2(first));
+  second = pack_e4m3(x - f.x, y - f.y);
 }
 // Copies from one page: K or V rows of a head; untiled for their exponents (16 bytes or a multiple, 16-byte aligned)
 __device__ __forceinline__ void tma_load_page(void* dst, const CUtensorMap* map, uint64_t* bar, bool e4m3, int piece, int row,

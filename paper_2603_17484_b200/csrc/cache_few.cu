@@ -14,12 +14,14 @@
 //   compute warps : 16 keys of every tile each.  Rows are the 16 rows of mma.sync A fragments.
 //                   bf16: S = Q K^T from ldmatrix'd rows, P rounded to bf16 and the part that is cut off (in rows 8 .. 15 where those
 //                   are free, else in a product of their own) times V from transposed ldmatrix.
-//                   e4m3: codes are fp16 exactly, one conversion for two of them.  A lane loads 16 codes of a key at once and
-//                   takes them as its elements of successive products: the order of the head's elements does not
-//                   matter as long as Q has the same.  V: two keys' codes of a column are put side by side by byte
-//                   permutes.  The keys' scales multiply the scores in fp32, the values' scales go into the weights: w = 2^(s + e - M) with
-//                   a running maximum M of s + e, beside the sum of 2^(s - m) with its own.  fp16 has 11 bits against bf16's 8, but
-//                   less range: Q is scaled by a power of two for each row, w lies at 2^10 .. 2^14 where it counts and is dropped at 2^-38 of that.
+//                   e4m3: the codes of K are operands as they are, beside Q as the sum of two e4m3 numbers (rows 8 .. 15 or a second
+//                   product; 8 bits in two terms of 4 and a sign, below 2^-10 of the row's largest element to 2^-18 of that).  A lane
+//                   loads 16 codes of a key at once and takes them as its elements of successive products: the order of
+//                   the head's elements does not matter as long as Q has the same.  V: two keys' codes of a column are put side by side by
+//                   byte permutes and become fp16, exactly, one conversion for two of them.  The keys' scales multiply the
+//                   scores in fp32, the values' scales go into the weights: w = 2^(s + e - M) with a running maximum M of s + e,
+//                   beside the sum of 2^(s - m) with its own.  fp16 has 11 bits against bf16's 8, but less range: w lies at
+//                   2^10 .. 2^14 where it counts and is dropped at 2^-38 of that.
 #include <math.h>
 
 #include <algorithm>
@@ -44,6 +46,7 @@ struct FewBars {
   int abort_flag;
   int warp_sum[kThreads / 32];
   int found_b, found_base;   // sequence of the CTA's first tile, and that sequence's first
+  int found[8];              // ... and what it takes part with (FewSeq)
 };
 
 // What a sequence takes part with: its new tokens and the tiles of its two segments
@@ -54,6 +57,7 @@ struct FewSeq {
   int hi, n_out;           // last key (-1: none) and tiles before the windows
   __device__ int tiles() const { return n_loc + n_out; }
 };
+static_assert(sizeof(FewSeq) <= sizeof(FewBars::found), "kept in shared memory");
 __device__ __forceinline__ FewSeq few_seq(const CacheFwdArgs& a, int b) {
   FewSeq s;
   s.n = cache_new(a.c, b, s.first);
@@ -87,6 +91,11 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&x)[4],
   else
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(b0), "r"(b1));
+}
+// C += A B, A 16 x 32 (row), B 32 x 8 (col), e4m3 operands, fp32 accumulators
+__device__ __forceinline__ void mma_16832(float (&c)[4], const uint32_t (&x)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
@@ -170,14 +179,27 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
   FewBars* bar = reinterpret_cast<FewBars*>(reinterpret_cast<uint8_t*>(red) + SM::red_bytes(kRows));
   volatile int* abort_flag = &bar->abort_flag;
 
+  if (tid == kThreads - 1) {
+    tma_prefetch_desc(&mapK);
+    tma_prefetch_desc(&mapV);
+    for (int s = 0; s < stages; ++s) {
+      mbar_init(&bar->full[s], 1);
+      mbar_init(&bar->empty[s], kComputeWarps);
+    }
+    bar->abort_flag = (smem_u32(smem) & 1023u) != 0 ? 2 : 0;       // the swizzled tiles need a 1024-byte aligned base
+    fence_mbar_init();
+  }
   // ---- the plan: tiles of every sequence, a CTA's range of them.  The first CTA leaves it for the combination.
   const int mine = blockIdx.x;
   int total = 0, per_cta = 0;
+  FewSeq own = {};                               // the thread's sequence, of the last kThreads ones
   for (int pass = 0; pass < 2; ++pass) {         // sum, then search
     int base = 0;
     if (pass == 1) per_cta = max(kMinTiles, (total + kCtas - 1) / kCtas);
     for (int b0 = 0; b0 < c.B; b0 += kThreads) {
-      const int b = b0 + tid, n = b < c.B ? few_seq(a, b).tiles() * c.Hkv : 0;
+      const int b = b0 + tid;
+      if (b < c.B && (pass == 0 || c.B > kThreads)) own = few_seq(a, b);
+      const int n = b < c.B ? own.tiles() * c.Hkv : 0;
       int x = n;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -194,9 +216,17 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
       }
       x += base;
       if (pass == 1 && b < c.B) {
-        if (mine == 0) a.plan[1 + b] = x - n;
+        if (mine == 0) {
+          // for the combination: tiles before the sequence, and the sequence
+          reinterpret_cast<int4*>(a.plan)[2 + 2 * b] = make_int4(x - n, own.first, own.n, own.n_loc);
+          a.plan[8 + 8 * b + 4] = own.n_out;
+        }
         const int at = mine * per_cta;
-        if (at >= x - n && at < x) { bar->found_b = b; bar->found_base = x - n; }
+        if (at >= x - n && at < x) {
+          bar->found_b = b;
+          bar->found_base = x - n;
+          *reinterpret_cast<FewSeq*>(bar->found) = own;
+        }
       }
       base += all;
       __syncthreads();
@@ -210,26 +240,13 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
   walk.end = min(total, walk.at + per_cta);
   walk.b = bar->found_b;
   walk.base = bar->found_base;
-  walk.s = few_seq(a, walk.b);
+  walk.s = *reinterpret_cast<const FewSeq*>(bar->found);
 
-  if (tid == 0) {
-    for (int s = 0; s < stages; ++s) {
-      mbar_init(&bar->full[s], 1);
-      mbar_init(&bar->empty[s], kComputeWarps);
-    }
-    bar->abort_flag = (smem_u32(smem) & 1023u) != 0 ? 2 : 0;       // the swizzled tiles need a 1024-byte aligned base
-    fence_mbar_init();
-  }
-  __syncthreads();
   bool ok = *abort_flag == 0;
   const int rows_shift = min(c.page_shift, 6), rows = 1 << rows_shift, copies = kTile >> rows_shift;   // of a page, pages of a tile
 
   if (warp == kComputeWarps) {
     // ================================================================= producer
-    if (lane == 0) {
-      tma_prefetch_desc(&mapK);
-      tma_prefetch_desc(&mapV);
-    }
     // lane -> what it copies of a tile: page `u` of K, V, their exponents
     const int what = lane / copies, u = lane % copies;
     const uint32_t bytes = what < 2 ? rows * D * (kE4M3 ? 1 : 2) : what < (kE4M3 ? 4 : 2) ? rows : 0;
@@ -301,18 +318,13 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
       every_lo = __reduce_max_sync(0xffffffffu, every_lo);
       every_hi = __reduce_min_sync(0xffffffffu, every_hi);
 
-      // ---- A fragments of Q
-      uint32_t qa[D / 16][4];
+      // ---- A fragments of Q.  e4m3: rows 8 .. 15 are the second terms of rows 0 .. 7, or with more rows have fragments of their own
+      constexpr int kFrags = kE4M3 ? D / 32 : D / 16;
+      uint32_t qa[kFrags][4], qb[kE4M3 && kHigh ? kFrags : 1][4];
       float row_scale[kHalves];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        if (x >= kHalves) {
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k) qa[k][1] = qa[k][3] = 0u;
-          continue;
-        }
-        const bf16* qrow = a.q + token[x < kHalves ? x : 0] * a.q_t + (int64_t)head[x < kHalves ? x : 0] * D;
-        const bool valid = row_ok[x < kHalves ? x : 0];
+      for (int x = 0; x < kHalves; ++x) {
+        const bf16* qrow = a.q + token[x] * a.q_t + (int64_t)head[x] * D;
         if (kE4M3) {
           // a lane's elements: those of the 16-byte pieces of a key's codes that it loads (below)
           constexpr int kPieces = D / 64;
@@ -330,32 +342,35 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           top = max(top & 0xffffu, top >> 16);
           top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
           top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          // largest element to 2^14 .. 2^15: the others keep all their bits down to 2^-28 of it
-          const int up = min(max(14 + 127 - (int)(top >> 7), -113), 100);
-          const float f = __uint_as_float((uint32_t)(up + 127) << 23);
-          row_scale[x < kHalves ? x : 0] = a.scale_log2 * 256.f * __uint_as_float((uint32_t)(127 - up) << 23);   // (2^8: the codes' bias)
+          // the largest element to 2^7 .. 2^8
+          const int up = min(max(7 + 127 - (int)(top >> 7), -113), 100);
+          const float f = row_ok[x] ? __uint_as_float((uint32_t)(up + 127) << 23) : 0.f;
+          row_scale[x] = a.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23);
 #pragma unroll
           for (int i = 0; i < kPieces; ++i)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              const uint32_t h = pack_f16(__uint_as_float(v[i][k] << 16) * f, __uint_as_float(v[i][k] & 0xffff0000u) * f);
-              v[i][k] = valid ? h : 0u;
-            }
-#pragma unroll
-          for (int i = 0; i < kPieces; ++i)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {              // elements 0 and 2 of four, then 1 and 3, as the codes come
-              qa[i * 4 + k][x] = __byte_perm(v[i][2 * k], v[i][2 * k + 1], 0x5410);
-              qa[i * 4 + k][2 + x] = __byte_perm(v[i][2 * k], v[i][2 * k + 1], 0x7632);
+            for (int k = 0; k < 4; ++k) {                // four elements: registers k & 1 of product 2 i + (k >> 1)
+              uint32_t h0, l0, h1, l1;
+              two_e4m3_terms(__uint_as_float(v[i][2 * k] << 16) * f, __uint_as_float(v[i][2 * k] & 0xffff0000u) * f, h0, l0);
+              two_e4m3_terms(__uint_as_float(v[i][2 * k + 1] << 16) * f, __uint_as_float(v[i][2 * k + 1] & 0xffff0000u) * f, h1, l1);
+              const int frag = 2 * i + (k >> 1), reg = (k & 1) * 2;
+              if (kHigh) {
+                qa[frag][reg + x] = h0 | h1 << 16;
+                qb[kE4M3 && kHigh ? frag : 0][reg + x] = l0 | l1 << 16;
+              } else {
+                qa[frag][reg] = h0 | h1 << 16;
+                qa[frag][reg + 1] = l0 | l1 << 16;
+              }
             }
         } else {
-          row_scale[x < kHalves ? x : 0] = a.scale_log2;
+          row_scale[x] = a.scale_log2;
 #pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
+          for (int k = 0; k < kFrags; ++k) {
             const uint32_t v0 = *reinterpret_cast<const uint32_t*>(qrow + k * 16 + 2 * t4);
             const uint32_t v1 = *reinterpret_cast<const uint32_t*>(qrow + k * 16 + 8 + 2 * t4);
-            qa[k][x] = valid ? v0 : 0u;
-            qa[k][2 + x] = valid ? v1 : 0u;
+            qa[k][x] = row_ok[x] ? v0 : 0u;
+            qa[k][2 + x] = row_ok[x] ? v1 : 0u;
+            if (!kHigh) qa[k][1] = qa[k][3] = 0u;
           }
         }
       }
@@ -387,13 +402,16 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
                 const float4 y = lds128(tK + row * D + ((D == 128 ? piece ^ (row & 7) : piece ^ ((row >> 1) & 3)) << 4));
                 const uint32_t w[4] = {__float_as_uint(y.x), __float_as_uint(y.y), __float_as_uint(y.z), __float_as_uint(y.w)};
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  mma_16816<true>(sc[x], qa[i * 4 + k], codes_02_f16(w[k]), codes_13_f16(w[k]));
+                for (int k = 0; k < 2; ++k) {
+                  mma_16832(sc[x], qa[2 * i + k], w[2 * k], w[2 * k + 1]);
+                  if (kHigh) mma_16832(sc[x], qb[kE4M3 && kHigh ? 2 * i + k : 0], w[2 * k], w[2 * k + 1]);
+                }
               }
               const uint32_t at = smem_u32(scales) + s * SM::kScaleBytes + r0 + x * 8 + 2 * t4;
               const uint32_t ek = lds16(at);
               ev[x] = lds16(at + kTile);
               const float f0 = scale_of_exponent(ek & 0xffu), f1 = scale_of_exponent(ek >> 8);
+              if (!kHigh) { sc[x][0] += sc[x][2]; sc[x][1] += sc[x][3]; }
               sc[x][0] *= f0; sc[x][1] *= f1; sc[x][2] *= f0; sc[x][3] *= f1;
             }
           } else {
@@ -629,9 +647,15 @@ __global__ void __launch_bounds__(kCombineThreads) cache_few_combine_kernel(cons
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, c4 = tid % kLanes, grp = tid / kLanes;
   dependency_wait();
   dependents_release();
-  const FewSeq s = few_seq(a, b);
+  const int per_cta = a.plan[0];
+  const int4 seq = reinterpret_cast<const int4*>(a.plan)[2 + 2 * b];
+  FewSeq s;
+  s.first = seq.y;
+  s.n = seq.z;
+  s.n_loc = seq.w;
+  s.n_out = a.plan[8 + 8 * b + 4];
   if (i >= s.n) return;
-  const int per_cta = a.plan[0], at = a.plan[1 + b] + g * s.tiles();
+  const int at = seq.x + g * s.tiles();
   const int loc0 = at / per_cta, n_loc = s.n_loc ? (at + s.n_loc - 1) / per_cta - loc0 + 1 : 0;
   const int out0 = (at + s.n_loc) / per_cta, n_out = s.n_out ? (at + s.tiles() - 1) / per_cta - out0 + 1 : 0;
   if (n_loc + n_out == 1) return;                      // stored by its only piece
@@ -755,18 +779,18 @@ cudaError_t launch(const CacheFwdArgs& a, const CUtensorMap& mapK, const CUtenso
 }
 
 int slot_rows(const l2a_params* p) { return (int64_t)p->Lq * (p->Hq / p->Hkv) > 8 ? 16 : 8; }
-size_t plan_bytes(const l2a_params* p) { return align_up(((size_t)p->B + 1) * sizeof(int), 256); }
+size_t plan_bytes(int B) { return align_up(((size_t)B + 1) * 8 * sizeof(int), 256); }
 
 }  // namespace
 
 size_t cache_few_ws_bytes(const l2a_params* p) {
-  return plan_bytes(p) + align_up((2 * (size_t)p->B * p->Hkv + kCtas) * slot_rows(p) * (p->D + 4) * sizeof(float), 256);
+  return plan_bytes(p->B) + align_up((2 * (size_t)p->B * p->Hkv + kCtas) * slot_rows(p) * (p->D + 4) * sizeof(float), 256);
 }
 
 cudaError_t launch_cache_few(CacheFwdArgs& a, void* ws, cudaStream_t s) {
   const bool high = (int64_t)a.c.Lq * a.G > 8, e4m3 = a.c.kind == L2A_CACHE_E4M3;
   a.plan = static_cast<int*>(ws);
-  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + align_up(((size_t)a.c.B + 1) * sizeof(int), 256));
+  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + plan_bytes(a.c.B));
   CUtensorMap mapK, mapV;
   const int rows = std::min(1 << a.c.page_shift, kTile);
   if (!encode_pool_map(&mapK, a.c, a.c.K, rows, a.c.D / 64) || !encode_pool_map(&mapV, a.c, a.c.V, rows, a.c.D / 64))
