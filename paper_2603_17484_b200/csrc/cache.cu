@@ -71,6 +71,7 @@ struct AppendArgs {
   CacheView c;
   const bf16 *K, *V;
   int64_t k_t, v_t;
+  int wide, wide_pool;     // 32-byte accesses to K and V, to a bf16 pool
 };
 
 // Biased exponent of the least 2^e with amax <= 448 * 2^e = 1.75 * 2^(8 + e), from the bits of the bf16 amax
@@ -99,13 +100,11 @@ __global__ void __launch_bounds__(kRowsThreads) cache_append_kernel(const Append
   const bf16* src = value ? a.V : a.K;
   const int64_t stride = value ? a.v_t : a.k_t;
   const int sub = lane % kLanes;
-  uint4 x[kSteps][2];
+  uint32_t w[kSteps][8];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int64_t t = t0 + i * kRows + lane / kLanes;
-    const uint4* row = reinterpret_cast<const uint4*>(src + min(t, (int64_t)c.n_tokens - 1) * stride + h * D + sub * 16);
-    x[i][0] = row[0];
-    x[i][1] = row[1];
+    load_32(src + min(t, (int64_t)c.n_tokens - 1) * stride + h * D + sub * 16, a.wide, w[i]);
   }
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
@@ -137,10 +136,9 @@ __global__ void __launch_bounds__(kRowsThreads) cache_append_kernel(const Append
     const int64_t slot = ((int64_t)h << c.page_shift) + (pos & ((1 << c.page_shift) - 1));
     uint8_t* dst = (value ? c.V : c.K) + page * c.page_bytes + slot * (kE4M3 ? D : 2 * D);
     if (kE4M3) {
-      const uint32_t w[8] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w, x[i][1].x, x[i][1].y, x[i][1].z, x[i][1].w};
       uint32_t m = 0;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) m = __vmaxu2(m, finite_magnitudes(w[k]));
+      for (int k = 0; k < 8; ++k) m = __vmaxu2(m, finite_magnitudes(w[i][k]));
       m = max(m & 0xffffu, m >> 16);
 #pragma unroll
       for (int o = kLanes / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -149,7 +147,7 @@ __global__ void __launch_bounds__(kRowsThreads) cache_append_kernel(const Append
       uint32_t code[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const uint32_t u = w[2 * k], v = w[2 * k + 1];
+        const uint32_t u = w[i][2 * k], v = w[i][2 * k + 1];
         code[k] = pack_e4m3(__uint_as_float(u << 16) * inv, __uint_as_float(u & 0xffff0000u) * inv) |
                   pack_e4m3(__uint_as_float(v << 16) * inv, __uint_as_float(v & 0xffff0000u) * inv) << 16;
       }
@@ -158,8 +156,7 @@ __global__ void __launch_bounds__(kRowsThreads) cache_append_kernel(const Append
         if (sub == 0) (value ? c.vs : c.ks)[page * c.scale_stride + slot] = (uint8_t)e;
       }
     } else if (page >= 0) {
-      reinterpret_cast<uint4*>(dst + sub * 32)[0] = x[i][0];
-      reinterpret_cast<uint4*>(dst + sub * 32)[1] = x[i][1];
+      store_32(dst + sub * 32, a.wide_pool, w[i]);
     }
   }
 }
@@ -169,6 +166,7 @@ struct ReadArgs {
   const int32_t* first;
   bf16 *K, *V;
   RowStrides k_st, v_st;
+  int wide, wide_pool;     // 32-byte accesses to K and V, to a bf16 pool
 };
 
 // The same shape for the way back: a lane brings 16 values of a position, a warp 512 / D positions of a head at a time.
@@ -183,13 +181,13 @@ __global__ void __launch_bounds__(kRowsThreads) cache_read_kernel(const ReadArgs
   const int64_t t0 = item / heads * kTokens + lane / kLanes;
   if (item / heads * kTokens >= c.max_keys) return;
   const int start = a.first ? a.first[b] : 0, length = cache_length(c, b);
-  uint4 x[kSteps][kE4M3 ? 1 : 2];
+  uint32_t x[kSteps][8];         // (e4m3: the first four)
   uint32_t e[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int64_t pos = start + t0 + i * kRows;
-    x[i][0] = make_uint4(0, 0, 0, 0);
-    if (!kE4M3) x[i][kE4M3 ? 0 : 1] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[i][k] = 0u;
     e[i] = 127;
     if (pos < 0 || pos >= length) continue;
     const int page = cache_page(c, b, (int)pos);
@@ -197,54 +195,49 @@ __global__ void __launch_bounds__(kRowsThreads) cache_read_kernel(const ReadArgs
     const int64_t slot = ((int64_t)h << c.page_shift) + (pos & ((1 << c.page_shift) - 1));
     const uint8_t* src = (value ? c.V : c.K) + page * c.page_bytes + slot * (kE4M3 ? D : 2 * D);
     if (kE4M3) {
-      x[i][0] = *reinterpret_cast<const uint4*>(src + sub * 16);
+      const uint4 y = *reinterpret_cast<const uint4*>(src + sub * 16);
+      x[i][0] = y.x; x[i][1] = y.y; x[i][2] = y.z; x[i][3] = y.w;
       e[i] = (value ? c.vs : c.ks)[page * c.scale_stride + slot];
     } else {
-      x[i][0] = reinterpret_cast<const uint4*>(src + sub * 32)[0];
-      x[i][kE4M3 ? 0 : 1] = reinterpret_cast<const uint4*>(src + sub * 32)[1];
+      load_32(src + sub * 32, a.wide_pool, x[i]);
     }
   }
+  const RowStrides st = value ? a.v_st : a.k_st;
+  bf16* out = (value ? a.V : a.K) + b * st.b + h * D + sub * 16;
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int64_t t = t0 + i * kRows;
     if (t >= c.max_keys) continue;
-    const RowStrides st = value ? a.v_st : a.k_st;
-    uint4* dst = reinterpret_cast<uint4*>((value ? a.V : a.K) + b * st.b + t * st.t + h * D + sub * 16);
     if (kE4M3) {
-      const float s = scale_of_exponent(e[i]);
-      const uint32_t w[4] = {x[i][0].x, x[i][0].y, x[i][0].z, x[i][0].w};
       uint32_t o[8];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 lo = f16x2_to_float2(e4m3x2_to_f16x2(w[k] & 0xffffu)), hi = f16x2_to_float2(e4m3x2_to_f16x2(w[k] >> 16));
-        o[2 * k] = pack_bf16(lo.x * s, lo.y * s);
-        o[2 * k + 1] = pack_bf16(hi.x * s, hi.y * s);
-      }
-      dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
-      dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+      decode_16(make_uint4(x[i][0], x[i][1], x[i][2], x[i][3]), scale_of_exponent(e[i]), o);
+      store_32(out + t * st.t, a.wide, o);
     } else {
-      dst[0] = x[i][0];
-      dst[1] = x[i][kE4M3 ? 0 : 1];
+      store_32(out + t * st.t, a.wide, x[i]);
     }
   }
 }
 
 template <int D, bool kE4M3>
 cudaError_t launch_append(const AppendArgs& a, cudaStream_t s) {
-  constexpr int kSteps = 2, kTokens = 512 / D * kSteps;
+  constexpr int kSteps = 1, kTokens = 512 / D * kSteps;
   const int64_t warps = ((int64_t)a.c.n_tokens + kTokens - 1) / kTokens * 2 * a.c.Hkv;
   cache_append_kernel<D, kE4M3, kSteps><<<(unsigned)((warps * 32 + kRowsThreads - 1) / kRowsThreads), kRowsThreads, 0, s>>>(a);
   return cudaGetLastError();
 }
 template <int D, bool kE4M3>
 cudaError_t launch_read(const ReadArgs& a, cudaStream_t s) {
-  constexpr int kSteps = 4, kTokens = 512 / D * kSteps;
+  constexpr int kSteps = 2, kTokens = 512 / D * kSteps;
   const int64_t warps = ((int64_t)a.c.max_keys + kTokens - 1) / kTokens * 2 * a.c.Hkv;
   const dim3 grid((unsigned)((warps * 32 + kRowsThreads - 1) / kRowsThreads), a.c.B);
   cache_read_kernel<D, kE4M3, kSteps><<<grid, kRowsThreads, 0, s>>>(a);
   return cudaGetLastError();
 }
 
+// Whether rows of two tensors (of elem bytes, any number of elements of the strides apart) all start at multiples of 32 bytes
+bool all_wide(const void* p, const void* q, int64_t elem, int64_t s0, int64_t s1, int64_t s2 = 0, int64_t s3 = 0) {
+  return ((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & 31) == 0 && ((s0 | s1 | s2 | s3) * elem) % 32 == 0;
+}
 bool misaligned(const void* p, const void* q) { return (reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & 15; }
 
 }  // namespace
@@ -263,6 +256,8 @@ extern "C" l2a_status l2a_cache_append(const l2a_params* p, const l2a_cache* c, 
   if (!K || !V || misaligned(K, V) || a.k_t == 0 || a.v_t == 0) return L2A_ERR_INVALID_ARG;
   a.K = static_cast<const bf16*>(K);
   a.V = static_cast<const bf16*>(V);
+  a.wide = all_wide(K, V, 2, a.k_t, a.v_t);
+  a.wide_pool = all_wide(c->K, c->V, 1, a.c.page_bytes, 0);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool e4m3 = c->kind == L2A_CACHE_E4M3;
   const cudaError_t e = p->D == 128 ? (e4m3 ? launch_append<128, true>(a, s) : launch_append<128, false>(a, s))
@@ -285,6 +280,8 @@ extern "C" l2a_status l2a_cache_read(const l2a_params* p, const l2a_cache* c, co
   a.V = static_cast<bf16*>(V_out);
   a.k_st = resolve_strides(p->k_stride, p->Lk, p->Hkv * p->D);
   a.v_st = resolve_strides(p->v_stride, p->Lk, p->Hkv * p->D);
+  a.wide = all_wide(K_out, V_out, 2, a.k_st.b, a.k_st.t, a.v_st.b, a.v_st.t);
+  a.wide_pool = all_wide(c->K, c->V, 1, a.c.page_bytes, 0);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool e4m3 = c->kind == L2A_CACHE_E4M3;
   const cudaError_t e = p->D == 128 ? (e4m3 ? launch_read<128, true>(a, s) : launch_read<128, false>(a, s))

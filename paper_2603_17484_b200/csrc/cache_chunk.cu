@@ -332,18 +332,9 @@ __device__ __forceinline__ void decode_cache(const ChunkArgs& p, int item, int b
                  ((int64_t)head * kTileN + quarter * kDecodeKeys) * (2 * D);
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const float s = scale_of_exponent(e[i]);
-    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
     uint32_t o[8];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float2 u = f16x2_to_float2(e4m3x2_to_f16x2(w[k] & 0xffffu)), v = f16x2_to_float2(e4m3x2_to_f16x2(w[k] >> 16));
-      o[2 * k] = pack_bf16(u.x * s, u.y * s);
-      o[2 * k + 1] = pack_bf16(v.x * s, v.y * s);
-    }
-    uint4* row = reinterpret_cast<uint4*>(dst + (i * kRows + lane / kLanes) * (2 * D) + sub * 32);
-    row[0] = make_uint4(o[0], o[1], o[2], o[3]);
-    row[1] = make_uint4(o[4], o[5], o[6], o[7]);
+    decode_16(x[i], scale_of_exponent(e[i]), o);
+    store_32(dst + (i * kRows + lane / kLanes) * (2 * D) + sub * 32, true, o);
   }
 }
 

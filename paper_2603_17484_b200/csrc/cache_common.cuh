@@ -109,7 +109,38 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
 }
+// 32 bytes of a lane: one access where the address allows it, so that a warp's access covers whole sectors
+__device__ __forceinline__ void load_32(const void* p, bool wide, uint32_t (&x)[8]) {
+  if (wide) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]), "=r"(x[4]), "=r"(x[5]), "=r"(x[6]), "=r"(x[7]) : "l"(p));
+  } else {
+    const uint4 a = static_cast<const uint4*>(p)[0], b = static_cast<const uint4*>(p)[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+}
+__device__ __forceinline__ void store_32(void* p, bool wide, const uint32_t (&x)[8]) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]), "r"(x[6]), "r"(x[7]) : "memory");
+  } else {
+    static_cast<uint4*>(p)[0] = make_uint4(x[0], x[1], x[2], x[3]);
+    static_cast<uint4*>(p)[1] = make_uint4(x[4], x[5], x[6], x[7]);
+  }
+}
 // 2^e of a stored exponent (0 and 255, which no row is written with, stand for 0 and infinity)
 __device__ __forceinline__ float scale_of_exponent(uint32_t biased) { return __uint_as_float(biased << 23); }
+
+// 16 codes times 2^e as bf16 (exact but for overflow and underflow)
+__device__ __forceinline__ void decode_16(const uint4& codes, float scale, uint32_t (&o)[8]) {
+  const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float2 lo = f16x2_to_float2(e4m3x2_to_f16x2(w[k] & 0xffffu)), hi = f16x2_to_float2(e4m3x2_to_f16x2(w[k] >> 16));
+    o[2 * k] = pack_bf16(lo.x * scale, lo.y * scale);
+    o[2 * k + 1] = pack_bf16(hi.x * scale, hi.y * scale);
+  }
+}
 
 }  // namespace l2a
