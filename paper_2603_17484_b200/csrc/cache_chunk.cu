@@ -455,8 +455,10 @@ __device__ __forceinline__ void scaled_codes(const float4& codes, uint32_t scale
   const uint32_t w[4] = {__float_as_uint(codes.x), __float_as_uint(codes.y), __float_as_uint(codes.z), __float_as_uint(codes.w)};
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * k]) : "r"(e4m3x2_to_f16x2(w[k] & 0xffffu)), "r"(scale2));
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * k + 1]) : "r"(e4m3x2_to_f16x2(w[k] >> 16)), "r"(scale2));
+    uint32_t lo, hi;
+    e4m3x4_to_f16(w[k], lo, hi);
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * k]) : "r"(lo), "r"(scale2));
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * k + 1]) : "r"(hi), "r"(scale2));
   }
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {

@@ -70,11 +70,15 @@ cudaError_t launch_cache_chunk(const CacheFwdArgs& a, bool first, void* ws, cuda
 // tokens of one head of one page, box_pieces * 64 elements of each (bf16) or the whole row of codes.
 bool encode_pool_map(CUtensorMap* map, const CacheView& c, const void* pool, int box_rows, int box_pieces);
 
-// Two e4m3 codes as fp16, exactly
+// e4m3 codes as fp16, exactly: two, or the four of a word
 __device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t codes) {
   uint32_t r;
   asm("{\n .reg .b16 c;\n cvt.u16.u32 c, %1;\n cvt.rn.f16x2.e4m3x2 %0, c;\n}" : "=r"(r) : "r"(codes));
   return r;
+}
+__device__ __forceinline__ void e4m3x4_to_f16(uint32_t codes, uint32_t& lo, uint32_t& hi) {
+  asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}"
+      : "=r"(lo), "=r"(hi) : "r"(codes));
 }
 __device__ __forceinline__ float2 f16x2_to_float2(uint32_t v) {
   float2 f;
@@ -137,7 +141,9 @@ __device__ __forceinline__ void decode_16(const uint4& codes, float scale, uint3
   const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    const float2 lo = f16x2_to_float2(e4m3x2_to_f16x2(w[k] & 0xffffu)), hi = f16x2_to_float2(e4m3x2_to_f16x2(w[k] >> 16));
+    uint32_t l, h;
+    e4m3x4_to_f16(w[k], l, h);
+    const float2 lo = f16x2_to_float2(l), hi = f16x2_to_float2(h);
     o[2 * k] = pack_bf16(lo.x * scale, lo.y * scale);
     o[2 * k + 1] = pack_bf16(hi.x * scale, hi.y * scale);
   }

@@ -14,14 +14,13 @@
 //   compute warps : 16 keys of every tile each.  Rows are the 16 rows of mma.sync A fragments.
 //                   bf16: S = Q K^T from ldmatrix'd rows, P rounded to bf16 and the part that is cut off (in rows 8 .. 15 where those
 //                   are free, else in a product of their own) times V from transposed ldmatrix.
-//                   e4m3: the codes of K are operands as they are, beside Q as the sum of two e4m3 numbers (rows 8 .. 15 or a second
-//                   product; 8 bits in two terms of 4 and a sign, below 2^-10 of the row's largest element to 2^-18 of that).  A lane
-//                   loads 16 codes of a key at once and takes them as its elements of successive products: the order of
-//                   the head's elements does not matter as long as Q has the same.  V: two keys' codes of a column are put side by side by
-//                   byte permutes and become fp16, exactly, one conversion for two of them.  The keys' scales multiply the
+//                   e4m3: codes become fp16, exactly, one conversion for two of them (mma.sync of e4m3 operands is made of the same
+//                   conversions here, those of Q among them).  A lane loads 16 codes of a key at once and takes them as its elements
+//                   of successive products: the order of the head's elements does not matter as long as Q has the same.  V: two
+//                   keys' codes of a column are put side by side by byte permutes.  The keys' scales multiply the
 //                   scores in fp32, the values' scales go into the weights: w = 2^(s + e - M) with a running maximum M of s + e,
-//                   beside the sum of 2^(s - m) with its own.  fp16 has 11 bits against bf16's 8, but less range: w lies at
-//                   2^10 .. 2^14 where it counts and is dropped at 2^-38 of that.
+//                   beside the sum of 2^(s - m) with its own.  fp16 has 11 bits against bf16's 8, but less range: Q is scaled by a
+//                   power of two for each row, w lies at 2^10 .. 2^14 where it counts and is dropped at 2^-38 of that.
 #include <math.h>
 
 #include <algorithm>
@@ -92,11 +91,6 @@ __device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&x)[4],
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(b0), "r"(b1));
 }
-// C += A B, A 16 x 32 (row), B 32 x 8 (col), e4m3 operands, fp32 accumulators
-__device__ __forceinline__ void mma_16832(float (&c)[4], const uint32_t (&x)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -131,6 +125,14 @@ struct Piece {
   int lo, hi;              // keys of the segment
   bool alone;              // the sequence's head has no other piece
 };
+
+// Tiles of a CTA, for `total` tiles of `pairs` sequences and KV heads: an even share, but at least kMinTiles of them or all of a pair
+// (a part more costs the combination about what a tile does), and where it covers several pairs of the average length, whole ones, whose
+// results need no combination.
+__device__ __forceinline__ int tiles_per_cta(int total, int pairs) {
+  const int share = max(1, (total + kCtas - 1) / kCtas), pair = max(1, total / max(pairs, 1));
+  return share >= pair ? (share + pair - 1) / pair * pair : max(share, min(kMinTiles, pair));
+}
 
 // The pieces of a CTA's range of tiles, in order: every warp walks through them by itself.
 struct Walk {
@@ -191,11 +193,11 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
   }
   // ---- the plan: tiles of every sequence, a CTA's range of them.  The first CTA leaves it for the combination.
   const int mine = blockIdx.x;
-  int total = 0, per_cta = 0;
+  int total = 0, per_cta = 0, base_pairs = 0;
   FewSeq own = {};                               // the thread's sequence, of the last kThreads ones
   for (int pass = 0; pass < 2; ++pass) {         // sum, then search
     int base = 0;
-    if (pass == 1) per_cta = max(kMinTiles, (total + kCtas - 1) / kCtas);
+    if (pass == 1) per_cta = tiles_per_cta(total, base_pairs);
     for (int b0 = 0; b0 < c.B; b0 += kThreads) {
       const int b = b0 + tid;
       if (b < c.B && (pass == 0 || c.B > kThreads)) own = few_seq(a, b);
@@ -229,7 +231,8 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
         }
       }
       base += all;
-      __syncthreads();
+      const int some = __syncthreads_count(n > 0);
+      if (pass == 0) base_pairs += some * c.Hkv;
     }
     total = base;
   }
@@ -318,13 +321,19 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
       every_lo = __reduce_max_sync(0xffffffffu, every_lo);
       every_hi = __reduce_min_sync(0xffffffffu, every_hi);
 
-      // ---- A fragments of Q.  e4m3: rows 8 .. 15 are the second terms of rows 0 .. 7, or with more rows have fragments of their own
-      constexpr int kFrags = kE4M3 ? D / 32 : D / 16;
-      uint32_t qa[kFrags][4], qb[kE4M3 && kHigh ? kFrags : 1][4];
+      // ---- A fragments of Q
+      uint32_t qa[D / 16][4];
       float row_scale[kHalves];
 #pragma unroll
-      for (int x = 0; x < kHalves; ++x) {
-        const bf16* qrow = a.q + token[x] * a.q_t + (int64_t)head[x] * D;
+      for (int x = 0; x < 2; ++x) {
+        if (x >= kHalves) {
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) qa[k][1] = qa[k][3] = 0u;
+          continue;
+        }
+        constexpr int kLast = kHalves - 1;
+        const int y = x < kLast ? x : kLast;
+        const bf16* qrow = a.q + token[y] * a.q_t + (int64_t)head[y] * D;
         if (kE4M3) {
           // a lane's elements: those of the 16-byte pieces of a key's codes that it loads (below)
           constexpr int kPieces = D / 64;
@@ -332,45 +341,30 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           uint32_t top = 0;
 #pragma unroll
           for (int i = 0; i < kPieces; ++i) {
-            const uint4* src = reinterpret_cast<const uint4*>(qrow + (t4 * kPieces + i) * 16);
-            const uint4 y0 = src[0], y1 = src[1];
-            v[i][0] = y0.x; v[i][1] = y0.y; v[i][2] = y0.z; v[i][3] = y0.w;
-            v[i][4] = y1.x; v[i][5] = y1.y; v[i][6] = y1.z; v[i][7] = y1.w;
+            load_32(qrow + (t4 * kPieces + i) * 16, false, v[i]);
 #pragma unroll
             for (int k = 0; k < 8; ++k) top = __vmaxu2(top, v[i][k] & 0x7fff7fffu);
           }
           top = max(top & 0xffffu, top >> 16);
           top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
           top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          // the largest element to 2^7 .. 2^8
-          const int up = min(max(7 + 127 - (int)(top >> 7), -113), 100);
-          const float f = row_ok[x] ? __uint_as_float((uint32_t)(up + 127) << 23) : 0.f;
-          row_scale[x] = a.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23);
+          // largest element to 2^14 .. 2^15: the others keep all their bits down to 2^-28 of it
+          const int up = min(max(14 + 127 - (int)(top >> 7), -113), 100);
+          const float f = row_ok[y] ? __uint_as_float((uint32_t)(up + 127) << 23) : 0.f;
+          row_scale[y] = a.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23);
 #pragma unroll
           for (int i = 0; i < kPieces; ++i)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {                // four elements: registers k & 1 of product 2 i + (k >> 1)
-              uint32_t h0, l0, h1, l1;
-              two_e4m3_terms(__uint_as_float(v[i][2 * k] << 16) * f, __uint_as_float(v[i][2 * k] & 0xffff0000u) * f, h0, l0);
-              two_e4m3_terms(__uint_as_float(v[i][2 * k + 1] << 16) * f, __uint_as_float(v[i][2 * k + 1] & 0xffff0000u) * f, h1, l1);
-              const int frag = 2 * i + (k >> 1), reg = (k & 1) * 2;
-              if (kHigh) {
-                qa[frag][reg + x] = h0 | h1 << 16;
-                qb[kE4M3 && kHigh ? frag : 0][reg + x] = l0 | l1 << 16;
-              } else {
-                qa[frag][reg] = h0 | h1 << 16;
-                qa[frag][reg + 1] = l0 | l1 << 16;
-              }
-            }
+            for (int k = 0; k < 8; ++k)
+              qa[i * 4 + k / 2][(k & 1) * 2 + x] = pack_f16(__uint_as_float(v[i][k] << 16) * f, __uint_as_float(v[i][k] & 0xffff0000u) * f);
         } else {
-          row_scale[x] = a.scale_log2;
+          row_scale[y] = a.scale_log2;
 #pragma unroll
-          for (int k = 0; k < kFrags; ++k) {
+          for (int k = 0; k < D / 16; ++k) {
             const uint32_t v0 = *reinterpret_cast<const uint32_t*>(qrow + k * 16 + 2 * t4);
             const uint32_t v1 = *reinterpret_cast<const uint32_t*>(qrow + k * 16 + 8 + 2 * t4);
-            qa[k][x] = row_ok[x] ? v0 : 0u;
-            qa[k][2 + x] = row_ok[x] ? v1 : 0u;
-            if (!kHigh) qa[k][1] = qa[k][3] = 0u;
+            qa[k][x] = row_ok[y] ? v0 : 0u;
+            qa[k][2 + x] = row_ok[y] ? v1 : 0u;
           }
         }
       }
@@ -402,16 +396,16 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
                 const float4 y = lds128(tK + row * D + ((D == 128 ? piece ^ (row & 7) : piece ^ ((row >> 1) & 3)) << 4));
                 const uint32_t w[4] = {__float_as_uint(y.x), __float_as_uint(y.y), __float_as_uint(y.z), __float_as_uint(y.w)};
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                  mma_16832(sc[x], qa[2 * i + k], w[2 * k], w[2 * k + 1]);
-                  if (kHigh) mma_16832(sc[x], qb[kE4M3 && kHigh ? 2 * i + k : 0], w[2 * k], w[2 * k + 1]);
+                for (int k = 0; k < 4; ++k) {
+                  uint32_t lo, hi;
+                  e4m3x4_to_f16(w[k], lo, hi);
+                  mma_16816<true>(sc[x], qa[i * 4 + k], lo, hi);
                 }
               }
               const uint32_t at = smem_u32(scales) + s * SM::kScaleBytes + r0 + x * 8 + 2 * t4;
               const uint32_t ek = lds16(at);
               ev[x] = lds16(at + kTile);
               const float f0 = scale_of_exponent(ek & 0xffu), f1 = scale_of_exponent(ek >> 8);
-              if (!kHigh) { sc[x][0] += sc[x][2]; sc[x][1] += sc[x][3]; }
               sc[x][0] *= f0; sc[x][1] *= f1; sc[x][2] *= f0; sc[x][3] *= f1;
             }
           } else {
@@ -522,10 +516,15 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
             for (int i = 0; i < kWords; ++i) {
               const uint32_t a0 = __byte_perm(w[0][i], w[1][i], 0x5140), a1 = __byte_perm(w[0][i], w[1][i], 0x7362);
               const uint32_t b0 = __byte_perm(w[2][i], w[3][i], 0x5140), b1 = __byte_perm(w[2][i], w[3][i], 0x7362);
-              mma_16816<true>(acc[4 * i], pa, e4m3x2_to_f16x2(a0 & 0xffffu), e4m3x2_to_f16x2(b0 & 0xffffu));
-              mma_16816<true>(acc[4 * i + 1], pa, e4m3x2_to_f16x2(a0 >> 16), e4m3x2_to_f16x2(b0 >> 16));
-              mma_16816<true>(acc[4 * i + 2], pa, e4m3x2_to_f16x2(a1 & 0xffffu), e4m3x2_to_f16x2(b1 & 0xffffu));
-              mma_16816<true>(acc[4 * i + 3], pa, e4m3x2_to_f16x2(a1 >> 16), e4m3x2_to_f16x2(b1 >> 16));
+              uint32_t p0, p1, p2, p3, q0, q1, q2, q3;
+              e4m3x4_to_f16(a0, p0, p1);
+              e4m3x4_to_f16(a1, p2, p3);
+              e4m3x4_to_f16(b0, q0, q1);
+              e4m3x4_to_f16(b1, q2, q3);
+              mma_16816<true>(acc[4 * i], pa, p0, q0);
+              mma_16816<true>(acc[4 * i + 1], pa, p1, q1);
+              mma_16816<true>(acc[4 * i + 2], pa, p2, q2);
+              mma_16816<true>(acc[4 * i + 3], pa, p3, q3);
             }
           } else {
             const int lm = lane >> 3, row = r0 + (lm & 1) * 8 + (lane & 7);
