@@ -93,7 +93,7 @@ struct ChunkArgs {
 };
 
 // ------------------------------------------------------------------------------------------------------------- plan
-__device__ __forceinline__ bool is_chunk(const CacheFwdArgs& a, int n) { return (int64_t)n * a.G > kFewRows || (n > 0 && a.G > kFewRows); }
+__device__ __forceinline__ bool is_chunk(const CacheFwdArgs& a, int n) { return (int64_t)n * a.G > a.few_rows; }
 
 // Inclusive scans of two values over the CTA's threads; all_x, all_y: the sums.  Two barriers.
 __device__ __forceinline__ int2 block_scan(int x, int y, int2* sums, int& all_x, int& all_y) {

@@ -55,10 +55,13 @@ struct CacheFwdArgs {
   int* status;                 // workspace: status word,
   int* plan;                   // few rows: tiles of a CTA, first tile of every sequence;
   float* part;                 // rows of the parts
+  int few_rows;                // most rows of a sequence there, and
+  int row_blocks;              // blocks of rows that it can have
 };
 
-// Sequences whose new tokens have at most kFewRows rows (tokens x heads of a KV group): cache_few.cu
-constexpr int kFewRows = 16;
+// Sequences whose new tokens have at most few_rows rows (tokens x heads of a KV group), one block of rows or kRowBlocks of them:
+// cache_few.cu
+constexpr int kBlockRows = 16, kRowBlocks = 4;
 size_t cache_few_ws_bytes(const l2a_params* p);     // plan and parts
 cudaError_t launch_cache_few(CacheFwdArgs& a, void* ws, cudaStream_t s);
 

@@ -1,5 +1,6 @@
 // Attention over the paged cache for sequences with few query rows: the new tokens of a sequence times the heads of a KV group
-// are at most 16 (decode, a few drafted tokens).  One pass over the keys that some row sees, so HBM-bound.
+// are at most few_rows (decode, a few drafted tokens).  Rows are taken in blocks of 16, each with its own pass over the keys that some row
+// of the sequence sees: HBM-bound with one block, the passes of further blocks find their keys in L2.
 //
 // Keys come in tiles of 64 from position 0 on.  For every sequence and KV head there are up to two segments of tiles: those
 // of Local Attention (from the first row's window on; all rows) and, where a token is routed, those before its window.
@@ -45,7 +46,7 @@ struct FewBars {
   int abort_flag;
   int warp_sum[kThreads / 32];
   int found_b, found_base;   // sequence of the CTA's first tile, and that sequence's first
-  int found[8];              // ... and what it takes part with (FewSeq)
+  int found[9];              // ... and what it takes part with (FewSeq)
 };
 
 // What a sequence takes part with: its new tokens and the tiles of its two segments
@@ -54,13 +55,15 @@ struct FewSeq {
   int length;
   int lo, n_loc;           // first key and tiles of Local Attention
   int hi, n_out;           // last key (-1: none) and tiles before the windows
-  __device__ int tiles() const { return n_loc + n_out; }
+  int blocks;              // of 16 rows
+  __device__ int tiles() const { return n_loc + n_out; }       // of a KV head and block of rows
 };
 static_assert(sizeof(FewSeq) <= sizeof(FewBars::found), "kept in shared memory");
 __device__ __forceinline__ FewSeq few_seq(const CacheFwdArgs& a, int b) {
   FewSeq s;
   s.n = cache_new(a.c, b, s.first);
-  if ((int64_t)s.n * a.G > kFewRows) s.n = 0;
+  if ((int64_t)s.n * a.G > a.few_rows) s.n = 0;
+  s.blocks = (s.n * a.G + kBlockRows - 1) / kBlockRows;
   s.length = cache_length(a.c, b);
   s.lo = max(0, s.length - s.n - a.window);
   s.n_loc = a.local && s.n > 0 && s.length > 0 ? (s.length - 1) / kTile - s.lo / kTile + 1 : 0;
@@ -120,7 +123,7 @@ struct FewSmem {
 
 // A piece: part of one segment
 struct Piece {
-  int b, g, seg;           // seg 0: Local Attention, 1: before the windows
+  int b, g, block, seg;    // KV head, block of rows; seg 0: Local Attention, 1: before the windows
   int t0, t1;              // tiles [t0, t1)
   int lo, hi;              // keys of the segment
   bool alone;              // the sequence's head has no other piece
@@ -142,14 +145,15 @@ struct Walk {
 };
 __device__ __forceinline__ bool next_piece(const CacheFwdArgs& a, Walk& w, Piece& p) {
   if (w.at >= w.end) return false;
-  while (w.at >= w.base + w.s.tiles() * a.c.Hkv) {
-    w.base += w.s.tiles() * a.c.Hkv;
+  while (w.at >= w.base + w.s.tiles() * w.s.blocks * a.c.Hkv) {
+    w.base += w.s.tiles() * w.s.blocks * a.c.Hkv;
     if (++w.b >= a.c.B) return false;
     w.s = few_seq(a, w.b);
   }
   const int per = w.s.tiles(), in = w.at - w.base, x = in % per;
   p.b = w.b;
-  p.g = in / per;
+  p.g = in / per / w.s.blocks;
+  p.block = in / per % w.s.blocks;
   p.seg = x >= w.s.n_loc;
   const int skip = p.seg ? w.s.n_loc : 0, n = p.seg ? w.s.n_out : w.s.n_loc, first = p.seg ? 0 : w.s.lo / kTile;
   const int i0 = x - skip, i1 = min(n, i0 + w.end - w.at);
@@ -201,7 +205,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
     for (int b0 = 0; b0 < c.B; b0 += kThreads) {
       const int b = b0 + tid;
       if (b < c.B && (pass == 0 || c.B > kThreads)) own = few_seq(a, b);
-      const int n = b < c.B ? own.tiles() * c.Hkv : 0;
+      const int n = b < c.B ? own.tiles() * own.blocks * c.Hkv : 0;
       int x = n;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -231,7 +235,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
         }
       }
       base += all;
-      const int some = __syncthreads_count(n > 0);
+      const int some = __syncthreads_count(n > 0);       // (blocks beside the first are not counted: their tiles lengthen the pair)
       if (pass == 0) base_pairs += some * c.Hkv;
     }
     total = base;
@@ -300,7 +304,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
       int every_lo = p.lo, every_hi = p.hi;            // keys that every row sees
 #pragma unroll
       for (int x = 0; x < kHalves; ++x) {
-        const int r = hr + 8 * x, i = r / a.G;
+        const int r = p.block * kBlockRows + hr + 8 * x, i = r / a.G;
         row_ok[x] = i < walk.s.n;
         token[x] = walk.s.first + (row_ok[x] ? i : 0);
         head[x] = p.g * a.G + r % a.G;
@@ -581,7 +585,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
       }
       named_barrier(1, kComputeWarps * 32);
       const bool failed = *abort_flag != 0;
-      const int n_rows = walk.s.n * a.G;
+      const int row0 = p.block * kBlockRows, n_rows = min(kBlockRows, walk.s.n * a.G - row0);
       for (int i = tid; i < n_rows * (D / 4); i += kComputeWarps * 32) {
         const int r = i / (D / 4), c4 = i % (D / 4);
         float M = -INFINITY;
@@ -601,15 +605,16 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           A.x += v.x * f; A.y += v.y * f; A.z += v.z * f; A.w += v.w * f;
         }
         if (!p.alone) {
-          float* slot = a.part + ((int64_t)((p.b * c.Hkv + p.g) * 2 + p.seg) + blockIdx.x) * (kRows * kPitch) + r * kPitch;
+          float* slot = a.part + (((int64_t)(p.b * c.Hkv + p.g) * a.row_blocks + p.block) * 2 + p.seg + blockIdx.x) * (kRows * kPitch) +
+                        r * kPitch;
           *reinterpret_cast<float4*>(slot + c4 * 4) = A;
           if (c4 == 0) *reinterpret_cast<float2*>(slot + D) = make_float2(M, failed ? -1.f : L);
         } else if (!failed) {
-          const int t = walk.s.first + r / a.G;
+          const int t = walk.s.first + (row0 + r) / a.G;
           const bool routed = a.global && a.d != nullptr && a.d[t] != 0;
           if (a.add && !routed) continue;
           const float k = L > 0.f ? (float)((a.local ? 1 : 0) + (routed ? 1 : 0)) / L : 0.f;
-          uint2* dst = reinterpret_cast<uint2*>(a.O + t * a.o_t + (int64_t)(p.g * a.G + r % a.G) * D) + c4;
+          uint2* dst = reinterpret_cast<uint2*>(a.O + t * a.o_t + (int64_t)(p.g * a.G + (row0 + r) % a.G) * D) + c4;
           float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
           if (a.add) {
             const uint2 x = *dst;
@@ -654,7 +659,8 @@ __global__ void __launch_bounds__(kCombineThreads) cache_few_combine_kernel(cons
   s.n_loc = seq.w;
   s.n_out = a.plan[8 + 8 * b + 4];
   if (i >= s.n) return;
-  const int at = seq.x + g * s.tiles();
+  const int row_of = i * a.G + h % a.G, block = row_of / kBlockRows, blocks = (s.n * a.G + kBlockRows - 1) / kBlockRows;
+  const int at = seq.x + (g * blocks + block) * s.tiles();
   const int loc0 = at / per_cta, n_loc = s.n_loc ? (at + s.n_loc - 1) / per_cta - loc0 + 1 : 0;
   const int out0 = (at + s.n_loc) / per_cta, n_out = s.n_out ? (at + s.tiles() - 1) / per_cta - out0 + 1 : 0;
   if (n_loc + n_out == 1) return;                      // stored by its only piece
@@ -662,8 +668,8 @@ __global__ void __launch_bounds__(kCombineThreads) cache_few_combine_kernel(cons
   const bool routed = a.global && a.d != nullptr && a.d[t] != 0;
   if (a.add && !routed) return;
   const int n = n_loc + (routed ? n_out : 0);
-  const int64_t seg = (int64_t)(b * c.Hkv + g) * 2;
-  const float* row = a.part + (i * a.G + h % a.G) * kPitch;
+  const int64_t seg = ((int64_t)(b * c.Hkv + g) * a.row_blocks + block) * 2;
+  const float* row = a.part + row_of % kBlockRows * kPitch;
   auto slot = [&](int k) { return row + (k < n_loc ? seg + loc0 + k : seg + 1 + out0 + k - n_loc) * (kRows * kPitch); };
   float4 v[kAhead];
 #pragma unroll
@@ -773,22 +779,24 @@ cudaError_t launch(const CacheFwdArgs& a, const CUtensorMap& mapK, const CUtenso
   cache_few_kernel<D, kE4M3, kHigh><<<kCtas, kThreads, smem, s>>>(a, mapK, mapV, kStages);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  const dim3 grid(a.Hq, a.c.B, std::max(1, std::min(a.c.Lq, kFewRows / a.G)));
+  const dim3 grid(a.Hq, a.c.B, std::max(1, std::min(a.c.Lq, a.few_rows / a.G)));
   return launch_dependent(cache_few_combine_kernel<D, kRows>, grid, kCombineThreads, 0, s, true, a);
 }
 
-int slot_rows(const l2a_params* p) { return (int64_t)p->Lq * (p->Hq / p->Hkv) > 8 ? 16 : 8; }
+int slot_rows(const l2a_params* p) { return (int64_t)p->Lq * (p->Hq / p->Hkv) > 8 ? kBlockRows : 8; }
+int row_blocks(int64_t rows) { return (int)(std::min<int64_t>(rows, kRowBlocks * kBlockRows) + kBlockRows - 1) / kBlockRows; }
 size_t plan_bytes(int B) { return align_up(((size_t)B + 1) * 8 * sizeof(int), 256); }
 
 }  // namespace
 
 size_t cache_few_ws_bytes(const l2a_params* p) {
-  return plan_bytes(p->B) + align_up((2 * (size_t)p->B * p->Hkv + kCtas) * slot_rows(p) * (p->D + 4) * sizeof(float), 256);
+  return plan_bytes(p->B) + align_up((2 * (size_t)p->B * p->Hkv * row_blocks((int64_t)p->Lq * (p->Hq / p->Hkv)) + kCtas) * slot_rows(p) * (p->D + 4) * sizeof(float), 256);
 }
 
 cudaError_t launch_cache_few(CacheFwdArgs& a, void* ws, cudaStream_t s) {
   const bool high = (int64_t)a.c.Lq * a.G > 8, e4m3 = a.c.kind == L2A_CACHE_E4M3;
   a.plan = static_cast<int*>(ws);
+  a.row_blocks = row_blocks((int64_t)a.c.Lq * a.G);
   a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + plan_bytes(a.c.B));
   CUtensorMap mapK, mapV;
   const int rows = std::min(1 << a.c.page_shift, kTile);

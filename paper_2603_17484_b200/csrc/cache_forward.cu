@@ -1,6 +1,8 @@
 // Attention of the new tokens over the paged cache (l2a_cache_forward): o = s + d * a for every row, both parts from one pass.
 #include <math.h>
 
+#include <algorithm>
+
 #include "cache_common.cuh"
 #include "sm100_prims.cuh"
 
@@ -9,8 +11,19 @@ namespace l2a {
 namespace {
 
 // Workspace: header, then the part of the few rows, then that of the others
-bool has_few(const l2a_params* p) { return p->Hq / p->Hkv <= kFewRows; }
-bool has_chunks(const l2a_params* p) { return (int64_t)p->Lq * (p->Hq / p->Hkv) > kFewRows; }
+bool has_few(const l2a_params* p) { return p->Hq / p->Hkv <= kRowBlocks * kBlockRows; }
+bool has_chunks(const l2a_params* p) { return (int64_t)p->Lq * (p->Hq / p->Hkv) > kBlockRows; }
+// Most rows of a sequence that the kernel of the few rows takes: those of one block, or of kRowBlocks where reading the keys once for each
+// block costs less than the launches of the other path, about 45 us (180 MB at the rate of these passes, less what that path
+// reads itself).  Blocks by the average sequence; keys by the longest.  us with one block / four (28/4 heads, window 4096, a fifth routed): 5 tokens of one
+// sequence of 32K e4m3 54 / 37, of eight 104 / 148, of eight ragged ones (18 tokens in all) 79 / 55; 8 tokens of eight of 8000 (32/8) e4m3 88 /
+// 73, bf16 69 / 87; 16 of one of 100K (32/8) e4m3 107 / 192.
+int few_rows(const l2a_params* p, const l2a_cache* c, int n_tokens) {
+  const int G = p->Hq / p->Hkv;
+  const double blocks = std::max<double>(p->B, (double)n_tokens * G / kBlockRows);
+  const double pass = (double)p->Lk * p->Hkv * p->D * (c->kind == L2A_CACHE_E4M3 ? 2 : 4);
+  return (blocks - 1.15 * p->B) * pass < 180e6 ? kRowBlocks * kBlockRows : kBlockRows;
+}
 
 int64_t row_stride(const int64_t (&s)[2], int row_elems) {
   if (s[0] != 0 || s[1] < 0) return 0;
@@ -71,12 +84,14 @@ extern "C" l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c,
   uint8_t* at = static_cast<uint8_t*>(ws) + kWsHeaderBytes;
   cudaError_t e = cudaSuccess;
   bool first = true;
+  a.few_rows = few_rows(p, c, n_tokens);
+  const bool few = p->Hq / p->Hkv <= a.few_rows, chunks = (int64_t)p->Lq * a.G > a.few_rows;
   if (has_few(p)) {
     // (without a list of new tokens every sequence has the same number)
-    first = cu_new == nullptr && has_chunks(p);
+    first = !few || (cu_new == nullptr && chunks);
     if (!first) e = launch_cache_few(a, at, s);
     at += cache_few_ws_bytes(p);
   }
-  if (e == cudaSuccess && has_chunks(p)) e = launch_cache_chunk(a, first, at, s);
+  if (e == cudaSuccess && chunks) e = launch_cache_chunk(a, first, at, s);
   return e == cudaSuccess ? L2A_OK : L2A_ERR_CUDA;
 }
