@@ -77,6 +77,28 @@ def test_append_writes_the_formats_bits(kind, page, Hkv, D, lengths, new):
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("kind", ["e4m3", "bf16"])
+@pytest.mark.parametrize("Hkv,D,misaligned", [(1, 64, False), (3, 128, True)])
+def test_append_and_read_of_many_tokens(kind, Hkv, D, misaligned):
+    """More tokens than a wave of small CTAs; with tensors that start at 16 bytes, not 32."""
+    lengths, new = [6000, 900], [5001, 0]
+    c = Cache(kind, 64, Hkv, D, lengths, seed=D)
+    N, off = sum(new), 8 if misaligned else 0
+    rows = [torch.randn(N * Hkv * D + off, device="cuda").bfloat16()[off:].view(N, Hkv, D) for _ in "KV"]
+    p = l2a.params(2, 5001, 6000, Hkv, Hkv, D, 0)
+    cu = torch.tensor([0, 5001, 5001], dtype=torch.int32).cuda()
+    l2a.l2a_cache_append(p, c.handle, *rows, cu, N)
+    out = [torch.empty(2 * 6000 * Hkv * D + off, device="cuda", dtype=torch.bfloat16)[off:].view(2, 6000, Hkv, D) for _ in "KV"]
+    l2a.l2a_cache_read(p, c.handle, None, *out)
+    for x, got, old in zip(rows, out, (c.K, c.V)):
+        want = x.double().cpu().numpy()
+        if kind == "e4m3":
+            want = decoded(*quantise(want))
+        assert np.array_equal(got[0, 999:].double().cpu().numpy(), want)
+        assert torch.equal(got[0, :999].double(), old[0][:999]) and torch.equal(got[1, :900].double(), old[1])
+        assert not got[1, 900:].any()
+
+
 def test_append_of_one_length_without_a_list():
     c = Cache("e4m3", 16, 2, 128, [40, 40, 40], seed=1)
     p = l2a.params(3, 4, 40, 2, 2, 128, 8)
