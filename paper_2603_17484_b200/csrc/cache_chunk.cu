@@ -298,7 +298,7 @@ __device__ void make_plan(const ChunkArgs& p) {
 
 // Decoded copy: pages of 128 tokens, [page][KV head][128][D] of K and of V.  A lane brings 16 codes, a warp 512 / D keys at a time, 32
 // keys of a head of K or V in all.  HBM-bound: 3 bytes a code, of the keys that some row sees.
-constexpr int kDecodeKeys = 32;
+constexpr int kDecodeKeys = 32, kDecodeParts = kTileN / kDecodeKeys;
 template <int D>
 __device__ __forceinline__ void decode_cache(const ChunkArgs& p, int item, int b) {
   constexpr int kLanes = D / 16, kRows = 32 / kLanes, kSteps = kDecodeKeys / kRows;
@@ -308,8 +308,8 @@ __device__ __forceinline__ void decode_cache(const ChunkArgs& p, int item, int b
   int first;
   const int n = cache_new(c, b, first), length = cache_length(c, b);
   if (!is_chunk(a, n)) return;
-  const int value = item & 1, quarter = (item >> 1) & 3, head = (item >> 3) % c.Hkv, block = (item >> 3) / c.Hkv;
-  const int key0 = block * kTileN + quarter * kDecodeKeys, window = max(0, length - n - a.window);
+  const int value = item & 1, part = (item >> 1) % kDecodeParts, row = item / (2 * kDecodeParts), head = row % c.Hkv, block = row / c.Hkv;
+  const int key0 = block * kTileN + part * kDecodeKeys, window = max(0, length - n - a.window);
   const bool may_route = a.global && a.d != nullptr, inside = key0 < length && (may_route || key0 + kDecodeKeys > window);
   const uint8_t *src = value ? c.V : c.K, *exps = value ? c.vs : c.ks;
   uint4 x[kSteps];
@@ -329,7 +329,7 @@ __device__ __forceinline__ void decode_cache(const ChunkArgs& p, int item, int b
   routed = __syncthreads_or(routed);
   if (!inside || (!routed && key0 + kDecodeKeys <= window)) return;
   uint8_t* dst = (value ? out.V : out.K) + (int64_t)(b * out.table_stride + block) * out.page_bytes +
-                 ((int64_t)head * kTileN + quarter * kDecodeKeys) * (2 * D);
+                 ((int64_t)head * kTileN + part * kDecodeKeys) * (2 * D);
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     uint32_t o[8];
@@ -338,7 +338,8 @@ __device__ __forceinline__ void decode_cache(const ChunkArgs& p, int item, int b
   }
 }
 
-// The first CTA plans; the others, a row of the grid for each sequence, decode.
+// The first CTA plans; the others, a row of the grid for each sequence, decode: 213 MB in 42 us (35K tokens, 8 heads, D = 128), two CTAs of
+// half the registers an SM 48.
 template <int D>
 __global__ void __launch_bounds__(kPlanThreads) cache_prepare_kernel(const ChunkArgs p) {
   dependency_wait();
@@ -349,8 +350,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_prepare_kernel(const Chunk
     make_plan(p);
     return;
   }
-  const int item = (blockIdx.x - 1) * (kPlanThreads / 32) + (threadIdx.x >> 5);
-  decode_cache<D>(p, item, blockIdx.y);
+  decode_cache<D>(p, (blockIdx.x - 1) * (kPlanThreads / 32) + (threadIdx.x >> 5), blockIdx.y);
 }
 
 // ------------------------------------------------------------------------------------------------------------- pieces
@@ -1050,7 +1050,8 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       // ---- a row that has nothing else to be joined with leaves finished, others go to the piece's slot
       const bool valid = cur.valid;
       float* slot = w.part + (size_t)cur.slot * slot_floats(D) + t * kTileM * (D + 2);
-      bf16* dst = cur.finished && valid ? a.O + cur.token * a.o_t + (int64_t)cur.head * D : nullptr;
+      const bool here = cur.finished && valid && dbg_in_range(cur.token >= 0 && cur.token < c.n_tokens && cur.head < a.Hq, a.status);
+      bf16* dst = here ? a.O + cur.token * a.o_t + (int64_t)cur.head * D : nullptr;
       const float back = kE4M3 ? fast_exp2(v_first) : 1.f;           // the accumulators lack the exponent of the first values
       const float inv_l = l > 0.f ? back * (cur.routed ? 2.f : 1.f) / l : 0.f;      // (finished and routed: no key before the window, a = s)
       // Four lanes, four rows: each lane stores the same 16 bytes of all four, so that a store covers 64 bytes of a row
@@ -1188,6 +1189,7 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
     if (part[1].complete && !a.local) return;
   }
   if (status != 0) return;                 // a wait ran out: nothing more is stored
+  if (!dbg_in_range(tok.index < a.c.Lq && tok.rank < a.c.n_tokens && head * a.G + h < a.Hq, a.status)) return;
   // of the window and of what lies before it
   constexpr size_t kSlot = (size_t)kRowsPerCta * (D + 2), kHalf = (size_t)kTileM * (D + 2);
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
@@ -1251,9 +1253,11 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
-// An 8-bit cache is decoded once where a sequence can have kDecodeRows rows of a KV head or more: its keys are then used by that many
-// 256-row groups, and each use would decode them again.  Not for copies beyond kMostDecoded bytes.
-constexpr int64_t kDecodeRows = 1024, kMostDecoded = 4ll << 30;
+// An 8-bit cache is decoded once where a sequence can have kDecodeRows rows of a KV head or more: each 256 of them would decode its keys
+// again.  us decoded in the products' kernel / once: 560 rows of each of eight sequences of 32K (28/4 heads, window 4096, a fifth routed) 204 /
+// 300, 1050 of one 61 / 69, of four of 16K 110 / 130, 2000 of two of 8000 (32/8, window 1000) 111 / 101, 2100 of one of 32K 82 / 85, 4000 of two
+// of 8000 200 / 157.  Not for copies beyond kMostDecoded bytes.
+constexpr int64_t kDecodeRows = 1536, kMostDecoded = 4ll << 30;
 int decoded_pages(int Lk) { return (Lk + kTileN - 1) / kTileN; }
 int64_t decoded_bytes(int B, int Lk, int Hkv, int D) { return 2ll * B * decoded_pages(Lk) * Hkv * kTileN * D * 2; }
 bool may_decode(int kind, int Lq, int G) { return kind == L2A_CACHE_E4M3 && (int64_t)Lq * G >= kDecodeRows; }
@@ -1282,7 +1286,7 @@ size_t layout(int B, int n_tokens, int G, int Hkv, int D, uint8_t* base, ChunkWs
 
 template <int D>
 cudaError_t launch_prepare(const ChunkArgs& p, bool decode, bool first, cudaStream_t s) {
-  const unsigned items = decode ? (unsigned)(p.f.c.table_stride * p.f.c.Hkv * 8) : 0, per = kPlanThreads / 32;
+  const unsigned items = decode ? (unsigned)(p.f.c.table_stride * p.f.c.Hkv * 2 * kDecodeParts) : 0, per = kPlanThreads / 32;
   return launch_dependent(cache_prepare_kernel<D>, dim3(1 + (items + per - 1) / per, decode ? p.f.c.B : 1), kPlanThreads, 0, s, !first, p);
 }
 

@@ -612,7 +612,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
         } else if (!failed) {
           const int t = walk.s.first + (row0 + r) / a.G;
           const bool routed = a.global && a.d != nullptr && a.d[t] != 0;
-          if (a.add && !routed) continue;
+          if ((a.add && !routed) || !dbg_in_range(t >= 0 && t < c.n_tokens, a.status)) continue;
           const float k = L > 0.f ? (float)((a.local ? 1 : 0) + (routed ? 1 : 0)) / L : 0.f;
           uint2* dst = reinterpret_cast<uint2*>(a.O + t * a.o_t + (int64_t)(p.g * a.G + (row0 + r) % a.G) * D) + c4;
           float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -666,7 +666,7 @@ __global__ void __launch_bounds__(kCombineThreads) cache_few_combine_kernel(cons
   if (n_loc + n_out == 1) return;                      // stored by its only piece
   const int t = s.first + i;
   const bool routed = a.global && a.d != nullptr && a.d[t] != 0;
-  if (a.add && !routed) return;
+  if ((a.add && !routed) || !dbg_in_range(t >= 0 && t < c.n_tokens && n_loc + n_out <= kMaxParts, a.status)) return;
   const int n = n_loc + (routed ? n_out : 0);
   const int64_t seg = ((int64_t)(b * c.Hkv + g) * a.row_blocks + block) * 2;
   const float* row = a.part + row_of % kBlockRows * kPitch;

@@ -87,8 +87,8 @@ extern "C" l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c,
   a.few_rows = few_rows(p, c, n_tokens);
   const bool few = p->Hq / p->Hkv <= a.few_rows, chunks = (int64_t)p->Lq * a.G > a.few_rows;
   if (has_few(p)) {
-    // (without a list of new tokens every sequence has the same number)
-    first = !few || (cu_new == nullptr && chunks);
+    // (with as many tokens as there can be, every sequence has the same number of them)
+    first = !few || ((int64_t)p->B * p->Lq == n_tokens && chunks);
     if (!first) e = launch_cache_few(a, at, s);
     at += cache_few_ws_bytes(p);
   }

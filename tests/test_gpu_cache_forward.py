@@ -55,8 +55,10 @@ def test_one_token_per_sequence(kind, page, heads, W, lengths, density):
     (16, HEADS[4], 4096, [20000], [50], 0.2),
     (32, HEADS[0], 4096, [33000, 9000], [5, 5], 0.3),
     (64, HEADS[1], 300, [9000] * 8, [12] * 8, 0.3),            # four blocks of rows cost more than the path of the chunks
-    (16, HEADS[0], 200, [3000, 2500], [146, 147], 0.5),        # 1022 and 1029 rows: on either side of the decoded copy
+    (16, HEADS[0], 200, [3000, 2500], [146, 147], 0.5),        # 1022 and 1029 rows
     (128, HEADS[1], 200, [3000, 70], [256, 70], 0.3),
+    (64, HEADS[0], 200, [2000, 70], [219, 70], 0.3),           # 1533 rows
+    (64, HEADS[0], 200, [2000, 70], [220, 70], 0.3),           # 1540
     (64, (2, 1, 128), 500, [40 + 7 * i for i in range(40)], [1 + 3 * (i % 5) for i in range(40)], 0.3),
     (16, (4, 1, 64), 64, [3 + i for i in range(1100)], [1 + i % 3 for i in range(1100)], 0.5),      # more sequences than the plans keep on chip
     (64, (40, 1, 128), 64, [600, 20], [1, 20], 0.5),           # 40 heads of a group
