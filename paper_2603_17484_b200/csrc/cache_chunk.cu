@@ -43,8 +43,8 @@ constexpr int kBoxBytes = 128 * 128;       // 128 rows of 128 bytes
 constexpr float kWeightTop = 7.0f;         // e4m3: weights lie at 2^7 and, while the reference lags, up to 2^15 (fp16 operands)
 constexpr int kPlanThreads = 1024;
 constexpr int kCtas = kSplitSms;
-constexpr int kItemCost = 5;               // key blocks' time that a piece costs besides its blocks
-constexpr int kMinPiece = 1;
+// Costs, in eighths of a key block of two tiles (2900 clk): a block that one tile takes (1800), a piece besides its blocks
+constexpr int kBlockCost = 8, kDualCost = 5, kItemCost = 40;
 
 // A group of rows
 struct alignas(16) Group {
@@ -223,6 +223,7 @@ __device__ void make_plan(const ChunkArgs& p) {
   for (int q0 = 0; q0 < n_groups; q0 += kPlanThreads) {
     const int q = q0 + tid;
     Group g;
+    g.dual = 0;
     int x = 0;
     if (q < n_groups) {
       const int b = last_not_above(first_group, c.B, q), out0 = first_group[c.B + b];      // (the last: it has groups)
@@ -262,14 +263,14 @@ __device__ void make_plan(const ChunkArgs& p) {
       g.max_lo1 = low(p3);
       x = g.blocks = g.jhi - g.jlo + 1;
     }
-    const int blocks = x * c.Hkv, cost = x > 0 ? (x + kItemCost) * c.Hkv : 0;
+    const int each = g.dual ? kDualCost : kBlockCost, blocks = x * c.Hkv, cost = x > 0 ? (x * each + kItemCost) * c.Hkv : 0;
     int all_cost;
     const int2 at = block_scan(blocks, cost, sums, all, all_cost);
     if (q < n_groups) {
       g.base = base_blocks + at.x - blocks;
       w.groups[q] = g;
       group_cost[q] = base_cost + at.y - cost;
-      if (few_groups) { keep_base[q] = g.base; keep_blocks[q] = x; }
+      if (few_groups) { keep_base[q] = g.base; keep_blocks[q] = g.dual ? -x : x; }
     }
     base_blocks += all;
     base_cost += all_cost;
@@ -283,14 +284,13 @@ __device__ void make_plan(const ChunkArgs& p) {
     if (tid > 0 && tid < ctas) {
       const int cost = (int)((int64_t)tid * base_cost / ctas);
       s.group = last_not_above(group_cost, n_groups, cost);              // (the last: it has blocks)
-      const int x = few_groups ? keep_blocks[s.group] : w.groups[s.group].jhi - w.groups[s.group].jlo + 1;
+      const int kept = few_groups ? keep_blocks[s.group] : w.groups[s.group].dual ? -w.groups[s.group].blocks : w.groups[s.group].blocks;
+      const int x = abs(kept), each = kept < 0 ? kDualCost : kBlockCost;
       const int first = few_groups ? keep_base[s.group] : w.groups[s.group].base;
-      const int in = cost - group_cost[s.group], per = x + kItemCost;
+      const int in = cost - group_cost[s.group], per = x * each + kItemCost;
       s.head = in / per;
-      s.block = max(0, in % per - kItemCost);
-      if (s.block < kMinPiece) s.block = 0;
-      if (s.block > 0 && x - s.block < kMinPiece) { s.block = 0; ++s.head; }
-      s.at = first + s.head * x + s.block;             // (head Hkv, block 0: the start of the next group)
+      s.block = max(0, in % per - kItemCost) / each;
+      s.at = first + s.head * x + s.block;
     }
     w.plan->start[tid] = s;
   }
@@ -493,8 +493,9 @@ struct RowOf {
   int token, head, lo, hi;       // first and last key that it sees
   int min_hi, max_lo;            // of the tile
   int slot, first_block, n_blocks;
-  bool valid, seg, finished;     // finished: the piece holds all that the row has to see
-  bool routed;
+  bool valid, seg, whole;        // whole: the piece holds all of the row's keys in this segment
+  int rank;                      // segment 0: whether other keys are to be joined (>= 0),
+  uint8_t routed;                // and the routing decision; looked up here, needed at the piece's end
 };
 
 template <int D, bool kE4M3>
@@ -839,8 +840,9 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       const int dual = g.dual, seg = g.seg, tile_row = (dual ? 0 : t * kTileM) + r;
       me.valid = tile_row < g.n_rows;
       me.seg = seg;
-      me.finished = pc.whole && !dual && (!seg || !a.local);
-      me.routed = false;
+      me.whole = pc.whole && !dual;
+      me.rank = seg && a.local ? 0 : -1;
+      me.routed = 0;
       me.slot = pc.item + blockIdx.x;
       me.first_block = pc.j0;
       me.n_blocks = pc.j1 - pc.j0 + 1;
@@ -855,8 +857,8 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         me.hi = pos - (seg ? a.shift : 0);
         me.lo = seg ? 0 : pos - a.window;
         if (!seg) {
-          if (w.token[me.token].rank >= 0) me.finished = false;
-          me.routed = a.global && a.d != nullptr && a.d[me.token] != 0;
+          me.rank = w.token[me.token].rank;
+          if (a.global && a.d != nullptr) me.routed = a.d[me.token];
         }
       }
       if (me.valid) {
@@ -1048,12 +1050,12 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       if (more && me.tb.first <= me.tb.last) row_scale = store_q();
 
       // ---- a row that has nothing else to be joined with leaves finished, others go to the piece's slot
-      const bool valid = cur.valid;
+      const bool valid = cur.valid, finished = cur.whole && cur.rank < 0;
       float* slot = w.part + (size_t)cur.slot * slot_floats(D) + t * kTileM * (D + 2);
-      const bool here = cur.finished && valid && dbg_in_range(cur.token >= 0 && cur.token < c.n_tokens && cur.head < a.Hq, a.status);
+      const bool here = finished && valid && dbg_in_range(cur.token >= 0 && cur.token < c.n_tokens && cur.head < a.Hq, a.status);
       bf16* dst = here ? a.O + cur.token * a.o_t + (int64_t)cur.head * D : nullptr;
       const float back = kE4M3 ? fast_exp2(v_first) : 1.f;           // the accumulators lack the exponent of the first values
-      const float inv_l = l > 0.f ? back * (cur.routed ? 2.f : 1.f) / l : 0.f;      // (finished and routed: no key before the window, a = s)
+      const float inv_l = l > 0.f ? back * (cur.routed != 0 ? 2.f : 1.f) / l : 0.f;      // (finished and routed: no key before the window, a = s)
       // Four lanes, four rows: each lane stores the same 16 bytes of all four, so that a store covers 64 bytes of a row
       bf16* rows[4];
 #pragma unroll
@@ -1069,7 +1071,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
 #pragma unroll
           for (int e = 0; e < 32; ++e) o[e] = 0u;                      // no block of this tile: the accumulator was never written
         }
-        if (valid && !cur.finished) {
+        if (valid && !finished) {
 #pragma unroll
           for (int x = 0; x < 8; ++x)
             *reinterpret_cast<float4*>(slot + ((q * 8 + x) * kTileM + r) * 4) =
@@ -1107,7 +1109,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
             if (rows[k] != nullptr) reinterpret_cast<uint4*>(rows[k] + q * 32)[lane & 3] = make_uint4(pk[k][0], pk[k][1], pk[k][2], pk[k][3]);
         }
       }
-      if (valid && !cur.finished) {
+      if (valid && !finished) {
         slot[kTileM * D + r] = kE4M3 ? m_use - v_first - kWeightTop : m_use;
         slot[kTileM * (D + 1) + r] = any ? l : 0.f;
       }

@@ -14,15 +14,15 @@ namespace {
 bool has_few(const l2a_params* p) { return p->Hq / p->Hkv <= kRowBlocks * kBlockRows; }
 bool has_chunks(const l2a_params* p) { return (int64_t)p->Lq * (p->Hq / p->Hkv) > kBlockRows; }
 // Most rows of a sequence that the kernel of the few rows takes: those of one block, or of kRowBlocks where reading the keys once for each
-// block costs less than the launches of the other path, about 45 us (180 MB at the rate of these passes, less what that path
-// reads itself).  Blocks by the average sequence; keys by the longest.  us with one block / four (28/4 heads, window 4096, a fifth routed): 5 tokens of one
-// sequence of 32K e4m3 54 / 37, of eight 104 / 148, of eight ragged ones (18 tokens in all) 79 / 55; 8 tokens of eight of 8000 (32/8) e4m3 88 /
-// 73, bf16 69 / 87; 16 of one of 100K (32/8) e4m3 107 / 192.
+// block costs less than the launches of the other path (125 MB, less what that path reads itself).  Blocks by the average sequence, keys
+// by the longest.  us with one block / four (window 4096, a fifth routed; 28/4 heads): 5 tokens of one sequence of 32K e4m3 51 / 37, of
+// four 65 / 71, of eight 99 / 148, of eight ragged ones (18 tokens in all) 81 / 56, 9 tokens of one of 9000 42 / 23; (32/8) 8 tokens of eight
+// of 8000 e4m3 81 / 73, bf16 66 / 87; 16 of one of 100K e4m3 101 / 192.
 int few_rows(const l2a_params* p, const l2a_cache* c, int n_tokens) {
   const int G = p->Hq / p->Hkv;
   const double blocks = std::max<double>(p->B, (double)n_tokens * G / kBlockRows);
   const double pass = (double)p->Lk * p->Hkv * p->D * (c->kind == L2A_CACHE_E4M3 ? 2 : 4);
-  return (blocks - 1.15 * p->B) * pass < 180e6 ? kRowBlocks * kBlockRows : kBlockRows;
+  return (blocks - 1.15 * p->B) * pass < 125e6 ? kRowBlocks * kBlockRows : kBlockRows;
 }
 
 int64_t row_stride(const int64_t (&s)[2], int row_elems) {
