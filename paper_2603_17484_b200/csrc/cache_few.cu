@@ -44,7 +44,7 @@ constexpr float kLag = 4.f;                  // the reference follows the maximu
 struct FewBars {
   uint64_t full[kMaxStages], empty[kMaxStages];
   int abort_flag;
-  int warp_sum[kThreads / 32];
+  int warp_sum[kThreads / 32], warp_pairs[kThreads / 32];
   int found_b, found_base;   // sequence of the CTA's first tile, and that sequence's first
   int found[9];              // ... and what it takes part with (FewSeq)
 };
@@ -129,7 +129,7 @@ struct Piece {
   bool alone;              // the sequence's head has no other piece
 };
 
-// Tiles of a CTA, for `total` tiles of `pairs` sequences and KV heads: an even share, but at least kMinTiles of them or all of a pair
+// Tiles of a CTA, for `total` tiles of `pairs` blocks of rows and KV heads: an even share, but at least kMinTiles of them or all of a pair
 // (a part more costs the combination about what a tile does), and where it covers several pairs of the average length, whole ones, whose
 // results need no combination.
 __device__ __forceinline__ int tiles_per_cta(int total, int pairs) {
@@ -197,16 +197,20 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
   }
   // ---- the plan: tiles of every sequence, a CTA's range of them.  The first CTA leaves it for the combination.
   const int mine = blockIdx.x;
-  int total = 0, per_cta = 0, base_pairs = 0;
+  int total = 0, per_cta = 0, all_pairs = 0;
   FewSeq own = {};                               // the thread's sequence, of the last kThreads ones
   for (int pass = 0; pass < 2; ++pass) {         // sum, then search
     int base = 0;
-    if (pass == 1) per_cta = tiles_per_cta(total, base_pairs);
+    if (pass == 1) per_cta = tiles_per_cta(total, all_pairs);
     for (int b0 = 0; b0 < c.B; b0 += kThreads) {
       const int b = b0 + tid;
       if (b < c.B && (pass == 0 || c.B > kThreads)) own = few_seq(a, b);
-      const int n = b < c.B ? own.tiles() * own.blocks * c.Hkv : 0;
+      const int pairs = b < c.B && own.tiles() > 0 ? own.blocks * c.Hkv : 0, n = own.tiles() * pairs;
       int x = n;
+      if (pass == 0) {
+        const int warp_pairs = __reduce_add_sync(0xffffffffu, pairs);
+        if (lane == 0) bar->warp_pairs[warp] = warp_pairs;
+      }
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, x, o);
@@ -219,6 +223,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
       for (int w = 0; w < kThreads / 32; ++w) {
         if (w < warp) x += bar->warp_sum[w];
         all += bar->warp_sum[w];
+        if (pass == 0) all_pairs += bar->warp_pairs[w];
       }
       x += base;
       if (pass == 1 && b < c.B) {
@@ -235,8 +240,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
         }
       }
       base += all;
-      const int some = __syncthreads_count(n > 0);       // (blocks beside the first are not counted: their tiles lengthen the pair)
-      if (pass == 0) base_pairs += some * c.Hkv;
+      __syncthreads();
     }
     total = base;
   }
