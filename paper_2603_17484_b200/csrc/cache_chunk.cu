@@ -1157,16 +1157,14 @@ __device__ __forceinline__ RowParts row_parts(const ChunkWs& w, int group, int H
 }
 
 // A CTA takes 32 packed rows of the token axis and one KV head, a thread kPieces times four columns of a row.  Bound by latencies: the
-// loads of several parts are in flight together, maxima, sums and accumulators in one pass.
-template <int D, int kPieces>
+// loads of kAhead parts are in flight together, maxima, sums and accumulators in one pass.
+template <int D, int kPieces, int kAhead>
 __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
-  constexpr int kAhead = kPieces == 1 ? 8 : 4;
   const CacheFwdArgs& a = p.f;
   const ChunkWs& w = p.w;
   __shared__ int starts[kCtas];
-  const int64_t row = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
-  const int piece0 = (blockIdx.z * 8 + (threadIdx.x >> 5)) * kPieces, head = blockIdx.y, t = (int)(row / a.G);
-  const int h = (int)(row - (int64_t)t * a.G);
+  const int row = blockIdx.x * 32 + (threadIdx.x & 31);
+  const int piece0 = (blockIdx.z * 8 + (threadIdx.x >> 5)) * kPieces, head = blockIdx.y, t = row / a.G, h = row - t * a.G;
   const bool inside = t < a.c.n_tokens;
   dependency_wait();
   TokenInfo tok = {-1, -1, {0, 0}};
@@ -1302,10 +1300,14 @@ cudaError_t launch_chunk(const ChunkArgs& p, const CUtensorMap& mapK, const CUte
   if (e != cudaSuccess) return e;
   e = launch_dependent(cache_chunk_kernel<D, kE4M3>, dim3(kCtas), kChunkThreads, smem, s, true, mapK, mapV, p);
   if (e != cudaSuccess) return e;
-  // few rows: their columns over several CTAs
+  // Few rows have many parts each: their columns over several CTAs, and more parts in flight.  Many rows have two or three parts, and
+  // registers are CTAs that an SM has room for.  Whole call, four parts in flight / two: 2000 tokens on 34K keys (32/8 heads) 363 / 353 us, 290
+  // on 1253 (28/4, two sequences) 33 / 35.
   const unsigned rows = (unsigned)(((int64_t)p.f.c.n_tokens * p.f.G + 31) / 32), heads = p.f.c.Hkv;
-  if ((int64_t)rows * heads <= kSplitSms) return launch_dependent(cache_join_kernel<D, 1>, dim3(rows, heads, D / 32), 256, 0, s, true, p);
-  return launch_dependent(cache_join_kernel<D, D / 32>, dim3(rows, heads), 256, 0, s, true, p);
+  const int64_t ctas = (int64_t)rows * heads;
+  if (ctas <= kSplitSms) return launch_dependent(cache_join_kernel<D, 1, 8>, dim3(rows, heads, D / 32), 256, 0, s, true, p);
+  if (ctas <= 4 * kSplitSms) return launch_dependent(cache_join_kernel<D, D / 32, 4>, dim3(rows, heads), 256, 0, s, true, p);
+  return launch_dependent(cache_join_kernel<D, D / 32, 2>, dim3(rows, heads), 256, 0, s, true, p);
 }
 
 }  // namespace

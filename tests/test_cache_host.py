@@ -95,6 +95,11 @@ def test_flags(flags, ok):
         assert e.value.code == INVALID
 
 
+def test_more_rows_than_32_bits_count():
+    p, c = params(B=1, Lq=1 << 28, Lk=1 << 28), cache(table_stride=1 << 22)
+    assert calls(p, c, n=1 << 28)[2] == UNSUPPORTED          # 2^31 rows
+
+
 def test_no_tokens_are_no_work():
     """Nothing is launched for an empty token axis (this machine has no GPU to launch on)."""
     append, _, forward = calls(params(), cache(), n=0, K=None, V=None, Q=None, O=None)
