@@ -459,8 +459,10 @@ l2a_status l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t
  *   d           in : uint8 [n_tokens], non-zero = routed; NULL = none is.
  *   O           out: bf16 [n_tokens, Hq, D] (token stride o_stride[1]).  Rows at positions below 0 get zeros.
  *   ws             : device workspace of l2a_cache_workspace_bytes, 256-byte aligned, its first word a status
- *                    (l2a_workspace_status).  The size follows from p, page size and n_tokens; it is enough for every smaller
- *                    n_tokens, Lq and Lk (other fields alike).
+ *                    (l2a_workspace_status; after a time-out the rows that need a combination are not stored).  The size follows
+ *                    from p, the cache's kind and n_tokens; it is enough for every smaller n_tokens, Lq and Lk (other fields alike).
+ *                    Up to 64 rows (tokens x heads of a KV group) of a sequence it holds parts only; beyond, 0.13 MB for every 256 rows
+ *                    and KV head, and from 1536 rows on room for a decoded copy of an 8-bit cache (4 * B * Lk * Hkv * D bytes, 4 GB at most).
  *   p->flags       : L2A_FLAG_SKIP_GLOBAL: s only (as d = NULL).  L2A_FLAG_SKIP_LOCAL: o = d * a.  L2A_FLAG_GLOBAL_PHASE: O holds
  *                    s already (from an L2A_FLAG_SKIP_GLOBAL call on another cache, say), and d * a is added for the routed
  *                    rows; others are not touched.  That is the layer whose Global Attention has projections, and so
@@ -470,7 +472,10 @@ l2a_status l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t
  * Global Attention may give those pages back.  Slots without a token may hold anything.  Keys and values that some
  * new token of the sequence attends to must be finite for all of them.
  * Scores, soft-max statistics and sums are fp32.  Results are bit-reproducible; how the keys of a row are divided follows from
- * all the call's lengths, so that the same sequence in another batch can differ by fp32 rounding.
+ * all the call's lengths, so that the same sequence in another batch can differ by fp32 rounding, and by that of the weights to 16
+ * bits against another running maximum.  n_tokens * Hq < 2^31 - 32.  n_tokens = 0 is no work.  Errors: L2A_ERR_INVALID_ARG,
+ * L2A_ERR_UNSUPPORTED (D, page_size, kind, too many rows), L2A_ERR_WORKSPACE, L2A_ERR_CUDA; a bounded device wait that runs out is
+ * reported by the status header, not by the return value.
  */
 l2a_status l2a_cache_workspace_bytes(const l2a_params* p, const l2a_cache* c, int n_tokens, size_t* ws_bytes);
 l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c, const void* Q, const int32_t* cu_new, int n_tokens,

@@ -22,6 +22,13 @@
 //                   scores in fp32, the values' scales go into the weights: w = 2^(s + e - M) with a running maximum M of s + e,
 //                   beside the sum of 2^(s - m) with its own.  fp16 has 11 bits against bf16's 8, but less range: Q is scaled by a
 //                   power of two for each row, w lies at 2^10 .. 2^14 where it counts and is dropped at 2^-38 of that.
+//
+// Measured (captured calls back to back): 16 sequences of 128K keys (32/8 heads, D = 128, four routed) e4m3 196 to 202 us for 1.18 GB = 5.9
+// to 6.0 TB/s, bf16 345 us for 2.35 GB = 6.8 TB/s; 32 ragged ones of up to 8000, a quarter routed, bf16 69 us (394 MB: 5.7 TB/s).  The 8-bit
+// passes are close to the instructions' limit: about 375 a warp for 16 keys of a head, half of them on the integer pipe (47 % of its
+// rate, 47 % of the issue slots), so that they slow down with the clock (236 us in a long loop).  A lone short sequence is latency: launch
+// and plan 4 us, first tile 2, four tiles 2, join of the warps 1, combination 4 (13 us for 9001 keys).  Two chains of products, the loads of V
+// ahead of the soft-max, and rows of Q handed over by the producer: no gain or 1 us lost.
 #include <math.h>
 
 #include <algorithm>
@@ -36,7 +43,7 @@ constexpr int kTile = 64;
 constexpr int kComputeWarps = kTile / 16;
 constexpr int kThreads = (kComputeWarps + 1) * 32;
 constexpr int kMaxStages = 6;
-constexpr int kMinTiles = 4;                 // tiles of a CTA at least
+constexpr int kMinTiles = 4;                 // tiles of a CTA at least (9001 keys, 28/4 heads: 12.6 us; with 2 14.1, 3 13.1, 6 13.8)
 constexpr int kCtas = 2 * kSplitSms;
 constexpr float kWeightTop = 10.f;           // log2 of the largest weight when the reference is new (fp16 operands)
 constexpr float kLag = 4.f;                  // the reference follows the maximum when it is more than this behind
