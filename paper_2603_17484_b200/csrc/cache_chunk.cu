@@ -24,12 +24,11 @@
 // are decoded, times their power of two relative to the largest of 32 keys, which goes into the exponent of the weights.
 //
 // Measured, 2000 tokens on 34768 keys (32/8 heads, D = 128, window 4096, a fifth routed; 21.5K key blocks of two tiles): call 352 us from
-// an 8-bit cache (decoded once: 42 us for 213 MB), 310 from bf16; 329 GFLOP = 0.94 and 1.06 PFLOP/s.  A key block takes 2900 clk, 2048 of them its
-// products: a tile's chain is scores -> soft-max (1600) -> products (1024 and waiting), the tensor pipe is active 62 % of a launch and the
-// special-function unit 46 %.  A piece costs about 9500 clk besides (look-up and last products 2900, rows of Q 2500, results 3600).
-// In a long loop the power cap lowers the clock to 1.4 GHz (409 us).  Decoding in the products' kernel: 2900 to 4500 clk a block, since the soft-max
-// warps share their schedulers with the decoding ones and multiply by the keys' scales; with all keys decoded on the integer pipe
-// (e4m3 to fp16, to bf16) it was 6400 to 8700.
+// an 8-bit cache (decoded once: 42 us for 213 MB), in a shorter run 341 next to 329 from bf16; 329 GFLOP = 0.93 to 1.00 PFLOP/s.  A key block
+// takes 2900 clk, 2048 of them its products; the tensor pipe is active 62 % of a launch and the special-function unit 46 %.  A piece takes
+// about 9600 clk besides: look-up 100, first scores 540, last products 2900, store of Q and results 6050.
+// In a long loop the power cap lowers the clock (388 us at 1.67 of 1.965 GHz; 409 in another run).  Decoding in the products' kernel: 4850 clk a block (6420 before the
+// operands became fp16).
 #include <math.h>
 
 #include <algorithm>
@@ -43,8 +42,8 @@ namespace {
 constexpr int kKStages = 3, kVStages = 2;
 constexpr int kSoftmaxWarps = 8, kTmaWarp = 8, kMmaWarp = 9, kConvWarp = 12, kConvWarps = 4;
 constexpr int kChunkThreads = 512;
-// The launch has 16 warps of 128 registers; the two warpgroups that do not compute rows give most of theirs away (184 and 72: the soft-max
-// spills more than the others gain).
+// The launch has 16 warps of 128 registers; the two warpgroups that do not compute rows give most of theirs away (with 184 and 72 the
+// soft-max spills 136 bytes instead of 16).
 constexpr int kSoftmaxRegs = 200, kOtherRegs = 56;
 static_assert(kSoftmaxWarps * kSoftmaxRegs + 8 * kOtherRegs <= 16 * 128, "register shares exceed the launch allocation");
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
