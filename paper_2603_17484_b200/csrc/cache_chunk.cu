@@ -27,8 +27,8 @@
 // an 8-bit cache (decoded once: 42 us for 213 MB), in a shorter run 341 next to 329 from bf16; 329 GFLOP = 0.93 to 1.00 PFLOP/s.  A key block
 // takes 2900 clk, 2048 of them its products; the tensor pipe is active 62 % of a launch and the special-function unit 46 %.  A piece takes
 // about 9600 clk besides: look-up 100, first scores 540, last products 2900, store of Q and results 6050.
-// In a long loop the power cap lowers the clock (388 us at 1.67 of 1.965 GHz; 409 in another run).  Decoding in the products' kernel: 4850 clk a block (6420 before the
-// operands became fp16).
+// In a long loop the power cap lowers the clock (388 us at 1.67 of 1.965 GHz; 409 in another run).
+// Decoding in the products' kernel: 4850 clk a block (6420 before the operands became fp16).
 #include <math.h>
 
 #include <algorithm>

@@ -26,8 +26,8 @@
 // Measured (captured calls back to back): 16 sequences of 128K keys (32/8 heads, D = 128, four routed) e4m3 196 to 202 us for 1.18 GB = 5.9
 // to 6.0 TB/s, bf16 346 us for 2.35 GB = 6.8 TB/s; 32 ragged ones of up to 8000, a quarter routed, bf16 69 us (394 MB: 5.7 TB/s).  The 8-bit
 // passes take 375 instructions a warp for 16 keys of a head, 176 of them on the integer pipe (48 % of its rate, 47 % of the issue slots; 445
-// with mma.sync of e4m3 operands), and slow down with the clock in a long loop (218 us at 1.83 of 1.965 GHz; 236 in another run).  A lone short sequence is latency (9001 keys: 13.3 us, of
-// which this kernel 9.2).  Tried: two chains of products 206 us against 196; the loads of V ahead of the soft-max, no change; pieces and rows
+// with mma.sync of e4m3 operands), and slow down with the clock in a long loop (218 us at 1.83 of 1.965 GHz; 236 in another run).
+// A lone short sequence is latency (9001 keys: 13.3 us, of which this kernel 9.2).  Tried: two chains of products 206 us against 196; the loads of V ahead of the soft-max, no change; pieces and rows
 // of Q handed over by the producer, 14.2 against 13.0 for 9001 keys.
 #include <math.h>
 
