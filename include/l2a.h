@@ -426,6 +426,7 @@ typedef struct l2a_cache {
  *   cu_new      : device int32 [B + 1], ascending from 0: the new tokens of sequence b are rows cu_new[b] ..
  *                 cu_new[b + 1] - 1 of a token axis of n_tokens rows; a sequence may have none.  NULL: every sequence has
  *                 Lq of them (n_tokens = B * Lq).  New token i of n of sequence b sits at position lengths[b] - n + i.
+ *                 cu_new[B] may be less than n_tokens: the rows from there on are no one's and are left alone.
  * Tensors on the token axis are [n_tokens, H, D] with their token stride in p (k_stride[1] and so on; the batch stride is 0).
  * The lengths, tables and cu_new are read on the device only: a captured call follows them when they change.  Values that break
  * the bounds above give results of no meaning, but no access outside the tensors.

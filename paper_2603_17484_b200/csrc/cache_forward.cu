@@ -88,9 +88,11 @@ extern "C" l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c,
   a.few_rows = few_rows(p, c, n_tokens);
   const bool few = p->Hq / p->Hkv <= a.few_rows, chunks = (int64_t)p->Lq * a.G > a.few_rows;
   if (has_few(p)) {
-    // (with as many tokens as there can be, every sequence has the same number of them)
+    // With as many tokens as there can be no sequence is expected to have few rows: no launch for those.  The list may say otherwise (the
+    // device alone reads it, and the token axis may be longer than what it lists), so the path of the chunks then takes every sequence.
     first = !few || ((int64_t)p->B * p->Lq == n_tokens && chunks);
     if (!first) e = launch_cache_few(a, at, s);
+    else if (few) a.few_rows = 0;
     at += cache_few_ws_bytes(p);
   }
   if (e == cudaSuccess && chunks) e = launch_cache_chunk(a, first, at, s);
