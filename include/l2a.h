@@ -474,8 +474,9 @@ l2a_status l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t
  * new token of the sequence attends to must be finite for all of them.
  * Scores, soft-max statistics and sums are fp32.  Results are bit-reproducible; how the keys of a row are divided follows from
  * all the call's lengths, so that the same sequence in another batch can differ by fp32 rounding, and by that of the weights to 16
- * bits against another running maximum.  n_tokens * Hq < 2^31 - 32.  n_tokens = 0 is no work.  Errors: L2A_ERR_INVALID_ARG,
- * L2A_ERR_UNSUPPORTED (D, page_size, kind, too many rows), L2A_ERR_WORKSPACE, L2A_ERR_CUDA; a bounded device wait that runs out is
+ * bits against another running maximum.  n_tokens * Hq < 2^31 - 32, and where a sequence can have more than 16 rows
+ * 2 (n_tokens * Hq / Hkv / 256 + B) * Hkv * (Lk / 128 + 1) < 2^38.  n_tokens = 0 is no work.  Errors: L2A_ERR_INVALID_ARG,
+ * L2A_ERR_UNSUPPORTED (D, page_size, kind, too many rows or keys), L2A_ERR_WORKSPACE, L2A_ERR_CUDA; a bounded device wait that runs out is
  * reported by the status header, not by the return value.
  */
 l2a_status l2a_cache_workspace_bytes(const l2a_params* p, const l2a_cache* c, int n_tokens, size_t* ws_bytes);

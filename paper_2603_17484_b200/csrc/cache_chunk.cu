@@ -34,6 +34,7 @@
 #include <algorithm>
 
 #include "cache_common.cuh"
+#include "cache_ranges.h"
 
 namespace l2a {
 
@@ -51,22 +52,23 @@ constexpr int kBoxBytes = 128 * 128;       // 128 rows of 128 bytes
 constexpr float kWeightTop = 7.0f;         // e4m3: weights lie at 2^7 and, while the reference lags, up to 2^15 (fp16 operands)
 constexpr int kPlanThreads = 1024;
 constexpr int kCtas = kSplitSms;
-// Costs, in eighths of a key block of two tiles (2900 clk): a block that one tile takes (1800), a piece besides its blocks
-constexpr int kBlockCost = 8, kDualCost = 5, kItemCost = 40;
 
 // A group of rows
 struct alignas(16) Group {
-  int b, seg, first, off;        // sequence, segment, its first row of the token axis, position of that row
-  int list, row0, n_rows, dual;  // segment 1: its list of routed tokens starts here; first packed row; rows; one tile twice
-  int key_lo, key_hi, jlo, jhi;  // keys that some row sees, and their blocks (jhi < jlo: none)
-  int base, blocks, hi0, lo1;    // first key block of the group's heads in the call, blocks of a head; last block of tile 0, first of tile 1
+  int b, seg, dual, first;       // sequence, segment, one tile twice, its first row of the token axis,
+  int off, list, row0, n_rows;   // position of that row; segment 1: its list of routed tokens starts here; first packed row; rows
+  int jlo, jhi, key_lo, key_hi;  // keys that some row sees, and their blocks (jhi < jlo: none)
+  int64_t base;                  // first key block of the group's heads in the call
+  int hi0, lo1;                  // last block of tile 0, first of tile 1
   int min_hi0, min_hi1, max_lo0, max_lo1;      // of each tile: keys from max_lo to min_hi are seen by all its rows
 };
-struct alignas(16) Start { int at, group, head, block; };   // where a CTA's range begins
+static_assert(sizeof(Group) == 80, "copied by 16 bytes");
+struct alignas(16) Start { int blocks, group, head, block; };   // a CTA's range: its key blocks, and where it begins
 
 struct Plan {
   int n_groups, ctas;
-  Start start[kCtas + 1];
+  int64_t at[kCtas + 1];         // first key block, of the call's, of every CTA's range
+  Start start[kCtas];
 };
 
 // What the join has to know of a token
@@ -84,7 +86,7 @@ struct ChunkWs {
   TokenInfo* token;
   int* list;
   int *first_group, *list_start, *list_end;   // [2][B], [B], [B]
-  int* group_cost;                 // of the groups before each
+  int64_t* group_cost;             // of the groups before each
   float* part;
 };
 
@@ -98,37 +100,44 @@ struct ChunkArgs {
   ChunkWs w;
   CacheView codes;       // the 8-bit cache that f.c is the decoded copy of
   int clear;             // no kernel ahead has cleared the status word
+  int wide;              // the call's key blocks may cost more than 32 bits count
 };
 
 // ------------------------------------------------------------------------------------------------------------- plan
 __device__ __forceinline__ bool is_chunk(const CacheFwdArgs& a, int n) { return (int64_t)n * a.G > a.few_rows; }
 
-// Inclusive scans of two values over the CTA's threads; all_x, all_y: the sums.  Two barriers.
-__device__ __forceinline__ int2 block_scan(int x, int y, int2* sums, int& all_x, int& all_y) {
+// Inclusive scans of kN values over the CTA's threads, in place; all: the sums.  Two barriers.
+template <int kN, class T>
+__device__ __forceinline__ void block_scan(T (&x)[kN], T (*sums)[kPlanThreads / 32], T (&all)[kN]) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int u = __shfl_up_sync(0xffffffffu, x, o), v = __shfl_up_sync(0xffffffffu, y, o);
-    if (lane >= o) { x += u; y += v; }
-  }
-  __syncthreads();
-  if (lane == 31) sums[warp] = make_int2(x, y);
-  __syncthreads();
-  const int2 mine = sums[lane];                        // (as many warps as lanes)
-  int u = mine.x, v = mine.y;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int i = __shfl_up_sync(0xffffffffu, u, o), k = __shfl_up_sync(0xffffffffu, v, o);
-    if (lane >= o) { u += i; v += k; }
+    for (int k = 0; k < kN; ++k) {
+      const T u = __shfl_up_sync(0xffffffffu, x[k], o);
+      if (lane >= o) x[k] += u;
+    }
   }
-  all_x = __shfl_sync(0xffffffffu, u, 31);
-  all_y = __shfl_sync(0xffffffffu, v, 31);
-  x += __shfl_sync(0xffffffffu, u - mine.x, warp);
-  y += __shfl_sync(0xffffffffu, v - mine.y, warp);
-  return make_int2(x, y);
+  __syncthreads();
+  if (lane == 31)
+    for (int k = 0; k < kN; ++k) sums[k][warp] = x[k];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kN; ++k) {
+    const T mine = sums[k][lane];                      // (as many warps as lanes)
+    T u = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const T i = __shfl_up_sync(0xffffffffu, u, o);
+      if (lane >= o) u += i;
+    }
+    all[k] = __shfl_sync(0xffffffffu, u, 31);
+    x[k] += __shfl_sync(0xffffffffu, u - mine, warp);
+  }
 }
 // The last i with v[i] <= x, of n > 0 ascending ones with v[0] <= x
-__device__ __forceinline__ int last_not_above(const int* v, int n, int x) {
+template <class T>
+__device__ __forceinline__ int last_not_above(const T* v, int n, T x) {
   int lo = 0;
   while (n - lo > 1) {
     const int mid = (lo + n) >> 1;
@@ -137,21 +146,27 @@ __device__ __forceinline__ int last_not_above(const int* v, int n, int x) {
   return lo;
 }
 
-// Bound by latencies: what is searched lies in shared memory where it fits (kKeep sequences or groups), else in the workspace.
-constexpr int kKeep = 1024;
-__device__ void make_plan(const ChunkArgs& p) {
+// Bound by latencies: what is searched lies in shared memory where it fits (kKeep sequences, kKeepCosts groups), else in the workspace.
+constexpr int kKeep = 1024, kKeepCosts = 512;
+struct PlanSmem {
+  int64_t cost[kKeepCosts], base[kKeepCosts], at[kCtas + 1], sums2[2][kPlanThreads / 32];     // (T)
+  int blocks[kKeepCosts];
+  int first[kKeep], n[kKeep], length[kKeep], group[2 * kKeep], start[kKeep], end[kKeep], sums[1][kPlanThreads / 32];
+};
+// T: what key blocks and costs are summed in
+template <class T>
+__device__ void make_plan(const ChunkArgs& p, PlanSmem& sm) {
   const CacheFwdArgs& a = p.f;
   const CacheView& c = a.c;
   const ChunkWs& w = p.w;
-  __shared__ int2 sums[kPlanThreads / 32];
-  __shared__ int keep_first[kKeep], keep_n[kKeep], keep_length[kKeep], keep_group[2 * kKeep], keep_start[kKeep], keep_end[kKeep];
-  __shared__ int keep_cost[kKeep], keep_base[kKeep], keep_blocks[kKeep];
+  int *keep_first = sm.first, *keep_n = sm.n, *keep_length = sm.length, *keep_blocks = sm.blocks;
+  T *keep_cost = reinterpret_cast<T*>(sm.cost), *keep_base = reinterpret_cast<T*>(sm.base);
   static_assert(kPlanThreads == 1024, "block_scan");
   const int tid = threadIdx.x;
   const bool small = c.B <= kKeep;
-  int* first_group = small ? keep_group : w.first_group;
-  int* list_start = small ? keep_start : w.list_start;
-  int* list_end = small ? keep_end : w.list_end;
+  int* first_group = small ? sm.group : w.first_group;
+  int* list_start = small ? sm.start : w.list_start;
+  int* list_end = small ? sm.end : w.list_end;
   // ---- the sequences.  (Lists of new tokens that do not ascend: no groups, nothing is stored.)
   bool bad = false;
   if (c.cu_new != nullptr)
@@ -181,19 +196,21 @@ __device__ void make_plan(const ChunkArgs& p) {
     return n > 0 && t >= first && t < first + n ? b : -1;
   };
   // ---- compact the routed tokens that see keys before their windows
-  int base = 0, all, unused;
+  int base = 0, x[1], all[1];
   for (int t0 = 0; t0 < c.n_tokens; t0 += kPlanThreads) {
     const int t = t0 + tid;
     int b = -1, first = 0, n = 0, length = 0;
     const bool routed = a.global && a.d != nullptr && t < c.n_tokens && a.d[t] != 0;
     if (t < c.n_tokens && !bad && (c.cu_new == nullptr || t >= (small ? keep_first[0] : c.cu_new[0]))) b = sequence_of(t, first, n, length);
     const int take = b >= 0 && routed && length - n + (t - first) - a.shift >= 0;
-    const int at = base + block_scan(take, 0, sums, all, unused).x - take;
+    x[0] = take;
+    block_scan(x, sm.sums, all);
+    const int at = base + x[0] - take;
     if (t < c.n_tokens) w.token[t] = TokenInfo{b >= 0 ? t - first : -1, take ? at : -1, {b, 0}};      // (completed below)
     if (b >= 0 && t == first) list_start[b] = at;
     if (b >= 0 && t == first + n - 1) list_end[b] = at + take;
     if (take) w.list[at] = t;
-    base += all;
+    base += all[0];
   }
   __syncthreads();
   // ---- groups of both segments, sequence by sequence
@@ -206,12 +223,14 @@ __device__ void make_plan(const ChunkArgs& p) {
       loc = a.local ? (int)compact_groups(n, a.G) : 0;
       out = (int)compact_groups(list_end[b] - list_start[b], a.G);
     }
-    const int at = base + block_scan(loc + out, 0, sums, all, unused).x - loc - out;
+    x[0] = loc + out;
+    block_scan(x, sm.sums, all);
+    const int at = base + x[0] - loc - out;
     if (b < c.B) {
       first_group[b] = at;
       first_group[c.B + b] = at + loc;
     }
-    base += all;
+    base += all[0];
   }
   const int n_groups = base;
   __syncthreads();
@@ -225,9 +244,9 @@ __device__ void make_plan(const ChunkArgs& p) {
     w.token[t] = x;
   }
   // ---- the groups, their key blocks and costs laid end to end
-  const bool few_groups = n_groups <= kKeep;
-  int* group_cost = few_groups ? keep_cost : w.group_cost;
-  int base_blocks = 0, base_cost = 0;
+  const bool few_groups = n_groups <= kKeepCosts;
+  T* cost_before = few_groups ? keep_cost : reinterpret_cast<T*>(w.group_cost);
+  T base_blocks = 0, base_cost = 0;
   for (int q0 = 0; q0 < n_groups; q0 += kPlanThreads) {
     const int q = q0 + tid;
     Group g;
@@ -269,38 +288,45 @@ __device__ void make_plan(const ChunkArgs& p) {
       g.min_hi1 = p2 - shift;
       g.max_lo0 = low(p1);
       g.max_lo1 = low(p3);
-      x = g.blocks = g.jhi - g.jlo + 1;
+      x = g.jhi - g.jlo + 1;
     }
-    const int each = g.dual ? kDualCost : kBlockCost, blocks = x * c.Hkv, cost = x > 0 ? (x * each + kItemCost) * c.Hkv : 0;
-    int all_cost;
-    const int2 at = block_scan(blocks, cost, sums, all, all_cost);
+    const T blocks = (T)x * c.Hkv, cost = (T)group_cost(x, g.dual, c.Hkv);
+    T at[2] = {blocks, cost}, both[2];
+    block_scan(at, reinterpret_cast<T(*)[kPlanThreads / 32]>(sm.sums2), both);
     if (q < n_groups) {
-      g.base = base_blocks + at.x - blocks;
+      g.base = base_blocks + at[0] - blocks;
       w.groups[q] = g;
-      group_cost[q] = base_cost + at.y - cost;
+      cost_before[q] = base_cost + at[1] - cost;
       if (few_groups) { keep_base[q] = g.base; keep_blocks[q] = g.dual ? -x : x; }
     }
-    base_blocks += all;
-    base_cost += all_cost;
+    base_blocks += both[0];
+    base_cost += both[1];
   }
   __syncthreads();
-  // ---- where the CTAs' ranges start
-  const int ctas = max(1, min(kCtas, base_blocks));
+  // ---- the CTAs' ranges
+  const int ctas = (int)max((T)1, min((T)kCtas, base_blocks));
   if (tid == 0) { w.plan->n_groups = n_groups; w.plan->ctas = ctas; }
+  Start start = {0, 0, 0, 0};
+  T* range_at = reinterpret_cast<T*>(sm.at);
   if (tid <= kCtas) {
-    Start s = {tid == 0 ? 0 : base_blocks, 0, 0, 0};
+    T at = tid == 0 ? 0 : base_blocks;
     if (tid > 0 && tid < ctas) {
-      const int cost = (int)((int64_t)tid * base_cost / ctas);
-      s.group = last_not_above(group_cost, n_groups, cost);              // (the last: it has blocks)
-      const int kept = few_groups ? keep_blocks[s.group] : w.groups[s.group].dual ? -w.groups[s.group].blocks : w.groups[s.group].blocks;
-      const int x = abs(kept), each = kept < 0 ? kDualCost : kBlockCost;
-      const int first = few_groups ? keep_base[s.group] : w.groups[s.group].base;
-      const int in = cost - group_cost[s.group], per = x * each + kItemCost;
-      s.head = in / per;
-      s.block = max(0, in % per - kItemCost) / each;
-      s.at = first + s.head * x + s.block;
+      const T cost = (T)range_cost(tid, ctas, base_cost);
+      start.group = last_not_above(cost_before, n_groups, cost);         // (the last: it has blocks)
+      const Group& g = w.groups[start.group];
+      const int kept = few_groups ? keep_blocks[start.group] : (g.jhi - g.jlo + 1) * (g.dual ? -1 : 1);
+      const RangePlace place = range_place(cost - cost_before[start.group], abs(kept), kept < 0);
+      start.head = place.head;
+      start.block = place.block;
+      at = (T)range_first(few_groups ? keep_base[start.group] : g.base, place, abs(kept));
     }
-    w.plan->start[tid] = s;
+    range_at[tid] = at;
+    w.plan->at[tid] = at;
+  }
+  __syncthreads();
+  if (tid < kCtas) {
+    start.blocks = (int)(range_at[tid + 1] - range_at[tid]);
+    w.plan->start[tid] = start;
   }
 }
 
@@ -355,7 +381,9 @@ __global__ void __launch_bounds__(kPlanThreads) cache_prepare_kernel(const Chunk
   if (blockIdx.x == 0) {
     if (blockIdx.y != 0) return;
     if (p.clear && threadIdx.x == 0) *p.f.status = 0;
-    make_plan(p);
+    __shared__ PlanSmem sm;
+    if (p.wide) make_plan<int64_t>(p, sm);
+    else make_plan<int>(p, sm);
     return;
   }
   decode_cache<D>(p, (blockIdx.x - 1) * (kPlanThreads / 32) + (threadIdx.x >> 5), blockIdx.y);
@@ -371,7 +399,7 @@ struct ChunkPiece {
 // registers: those of the soft-max warps are taken by the scores).
 constexpr int kKeepGroups = 16;
 struct ChunkWalk {
-  int at, end, group, head, block, n_groups;
+  int left, group, head, block, n_groups;      // key blocks of the range that are left, and where it has come to
   const Group* kept;       // the first kKeepGroups of the range, in shared memory
   int kept_from;
   __device__ __forceinline__ const Group& group_now(const ChunkWs& w) const {
@@ -382,15 +410,14 @@ struct ChunkWalk {
     kept = keep;
     n_groups = w.plan->n_groups;
     const int4 s = *reinterpret_cast<const int4*>(&w.plan->start[cta]);
-    at = s.x;
+    left = s.x;
     group = kept_from = s.y;
     head = s.z;
     block = s.w;
-    end = w.plan->start[cta + 1].at;
-    return cta < w.plan->ctas && at < end && group < n_groups;
+    return cta < w.plan->ctas && left > 0 && group < n_groups;
   }
   __device__ __forceinline__ bool next(const ChunkWs& w, int Hkv, ChunkPiece& p) {
-    if (at >= end) return false;
+    if (left <= 0) return false;
     int n, jlo;
     for (;;) {
       const int2 j = *reinterpret_cast<const int2*>(&group_now(w).jlo);
@@ -403,13 +430,13 @@ struct ChunkWalk {
         if (++group >= n_groups) return false;
       }
     }
-    const int take = min(n - block, end - at);
+    const int take = min(n - block, left);
     p.head = head;
     p.j0 = jlo + block;
     p.j1 = p.j0 + take - 1;
     p.whole = take == n;
     p.item = group * Hkv + head;
-    at += take;
+    left -= take;
     block += take;
     return true;
   }
@@ -1147,17 +1174,26 @@ struct RowParts {
   bool complete;         // one part only
 };
 template <int D>
-__device__ __forceinline__ RowParts row_parts(const ChunkWs& w, int group, int Hkv, int head, int row, const int* starts, int ctas) {
+__device__ __forceinline__ RowParts row_parts(const ChunkWs& w, int group, int Hkv, int head, int row, const int* starts, int ctas, bool wide) {
   RowParts x;
-  const int2 g = *reinterpret_cast<const int2*>(&w.groups[group].base);      // first block, blocks of a head
-  const int dual = w.groups[group].dual;
+  const int64_t base = w.groups[group].base;
+  const int blocks = w.groups[group].jhi - w.groups[group].jlo + 1, dual = w.groups[group].dual;
   x.tiles = dual ? 2 : 1;
   x.r = row % kTileM;
   x.n = 0;
   x.tile = nullptr;
   x.complete = false;
-  if (g.y <= 0) return x;
-  const int lo = g.x + head * g.y, c0 = last_not_above(starts, ctas, lo), c1 = last_not_above(starts, ctas, lo + g.y - 1);
+  if (blocks <= 0) return x;
+  int c0, c1;
+  if (wide) {
+    const int64_t lo = base + (int64_t)head * blocks;
+    c0 = last_not_above(w.plan->at, ctas, lo);
+    c1 = last_not_above(w.plan->at, ctas, lo + blocks - 1);
+  } else {
+    const int lo = (int)base + head * blocks;
+    c0 = last_not_above(starts, ctas, lo);
+    c1 = last_not_above(starts, ctas, lo + blocks - 1);
+  }
   x.n = c1 - c0 + 1;
   x.complete = x.n == 1 && !dual;
   x.tile = w.part + (size_t)(group * Hkv + head + c0) * slot_floats(D) + row / kTileM * (kTileM * (D + 2));
@@ -1182,18 +1218,18 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
     routed = a.global && a.d != nullptr && a.d[t] != 0;
   }
   const int ctas = w.plan->ctas, status = *a.status;
-  if (threadIdx.x < kCtas) starts[threadIdx.x] = w.plan->start[threadIdx.x].at;
+  if (threadIdx.x < kCtas) starts[threadIdx.x] = (int)w.plan->at[threadIdx.x];
   __syncthreads();
   if (tok.index < 0 || (a.add && !routed)) return;
   RowParts part[2] = {};
   if (a.local) {
     const int x = tok.index * a.G + h;
-    part[0] = row_parts<D>(w, tok.group[0] + x / kRowsPerCta, a.c.Hkv, head, x % kRowsPerCta, starts, ctas);
+    part[0] = row_parts<D>(w, tok.group[0] + x / kRowsPerCta, a.c.Hkv, head, x % kRowsPerCta, starts, ctas, p.wide);
     if (part[0].complete && tok.rank < 0) return;
   }
   if (tok.rank >= 0) {
     const int x = tok.rank * a.G + h;
-    part[1] = row_parts<D>(w, tok.group[1] + x / kRowsPerCta, a.c.Hkv, head, x % kRowsPerCta, starts, ctas);
+    part[1] = row_parts<D>(w, tok.group[1] + x / kRowsPerCta, a.c.Hkv, head, x % kRowsPerCta, starts, ctas, p.wide);
     if (part[1].complete && !a.local) return;
   }
   if (status != 0) return;                 // a wait ran out: nothing more is stored
@@ -1281,7 +1317,7 @@ size_t layout(int B, int n_tokens, int G, int Hkv, int D, uint8_t* base, ChunkWs
   ChunkWs x;
   x.plan = reinterpret_cast<Plan*>(take(sizeof(Plan)));
   x.groups = reinterpret_cast<Group*>(take(groups * sizeof(Group)));
-  x.group_cost = reinterpret_cast<int*>(take(groups * 4));
+  x.group_cost = reinterpret_cast<int64_t*>(take(groups * 8));
   x.token = reinterpret_cast<TokenInfo*>(take(tokens * sizeof(TokenInfo)));
   x.list = reinterpret_cast<int*>(take(tokens * 4));
   x.first_group = reinterpret_cast<int*>(take((size_t)B * 8));
@@ -1326,10 +1362,15 @@ size_t cache_chunk_ws_bytes(const l2a_params* p, int kind, int n_tokens) {
   return layout(p->B, n_tokens, G, p->Hkv, p->D, nullptr, nullptr) + (size_t)copy;
 }
 
+bool cache_chunk_counts(const l2a_params* p, int n_tokens) {
+  return most_blocks(most_groups(n_tokens, p->Hq / p->Hkv, p->B), p->Hkv, p->Lk) < kMostBlocks;
+}
+
 cudaError_t launch_cache_chunk(const CacheFwdArgs& a, bool first, void* ws, cudaStream_t s) {
   ChunkArgs p;
   p.f = a;
   p.clear = first;
+  p.wide = most_cost(most_groups(a.c.n_tokens, a.G, a.c.B), a.c.Hkv, a.c.max_keys) >= (double)(1u << 31);
   const size_t at = layout(a.c.B, a.c.n_tokens, a.G, a.c.Hkv, a.c.D, static_cast<uint8_t*>(ws), &p.w);
   const int64_t copy = decoded_bytes(a.c.B, a.c.max_keys, a.c.Hkv, a.c.D);
   const bool decode = may_decode(a.c.kind, a.c.Lq, a.G) && copy <= kMostDecoded && a.c.B <= 65535;

@@ -67,6 +67,7 @@ cudaError_t launch_cache_few(CacheFwdArgs& a, void* ws, cudaStream_t s);
 
 // All others: cache_chunk.cu
 size_t cache_chunk_ws_bytes(const l2a_params* p, int kind, int n_tokens);
+bool cache_chunk_counts(const l2a_params* p, int n_tokens);      // whether it can count the key blocks of such a call
 cudaError_t launch_cache_chunk(const CacheFwdArgs& a, bool first, void* ws, cudaStream_t s);     // first: no kernel of the call ahead
 
 // Tensor map over a pool: {elements of 128 bytes at most, tokens, (pieces of a row,) heads, pages}; one copy brings box_rows
