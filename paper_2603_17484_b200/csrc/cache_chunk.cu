@@ -966,6 +966,11 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       for (int j = tb.first; j <= tb.last; j += tb.step) {
         float ev[4];             // e4m3: exponent of the values of each 32 keys
         const uint32_t it = it0 + (j - cur.first_block);
+        // warp-uniform outcome: the TMEM loads/stores below are warp-collective
+        if (!mbar_wait_warp(&bar->s_full[t], s_cnt & 1, abort_flag)) { ok = false; break; }
+        ++s_cnt;
+        // Behind the scores: a tile without a block in much of a piece comes here many blocks ahead of the scales, where the slot's phase of
+        // two rounds ago would pass for the one that is meant.  With the scores there, at most two blocks' scales are missing.
         if (kE4M3 && warp_has_rows) {
           const uint32_t slot = it & (kScaleSlots - 1);
           if (!mbar_wait_warp(&bar->scale_full[slot], (it / kScaleSlots) & 1, abort_flag)) { ok = false; break; }
@@ -973,9 +978,6 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
           ev[0] = y.x; ev[1] = y.y; ev[2] = y.z; ev[3] = y.w;
           if (j == tb.first) v_first = ev[0];
         }
-        // warp-uniform outcome: the TMEM loads/stores below are warp-collective
-        if (!mbar_wait_warp(&bar->s_full[t], s_cnt & 1, abort_flag)) { ok = false; break; }
-        ++s_cnt;
         tc_fence_after();
         if (!warp_has_rows) {    // nothing of these rows is ever stored
           mbar_arrive(&bar->p_half[t]);
