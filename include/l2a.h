@@ -445,7 +445,7 @@ l2a_status l2a_cache_append(const l2a_params* p, const l2a_cache* c, const void*
  * Reads the cache back.  Row t of sequence b of the outputs is position first[b] + t (first: device int32 [B], NULL = 0):
  *   K_out, V_out out : bf16 [B, Lk, Hkv, D] (k_stride, v_stride), what the cache stands for, rounded to bf16 (exact unless it
  *                      overflows or underflows); rows of positions below 0 or from lengths[b] on are zeros.
- * HBM-bound.  The layout is that of K and V in l2a_forward and l2a_decode.
+ * HBM-bound.  The layout is that of K and V in l2a_forward and l2a_decode.  B <= 65535 (L2A_ERR_UNSUPPORTED).
  */
 l2a_status l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t* first, void* K_out, void* V_out,
                           void* stream);
@@ -475,7 +475,7 @@ l2a_status l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t
  * Scores, soft-max statistics and sums are fp32.  Results are bit-reproducible; how the keys of a row are divided follows from
  * all the call's lengths, so that the same sequence in another batch can differ by fp32 rounding, and by that of the weights to 16
  * bits against another running maximum.  n_tokens * Hq < 2^31 - 32, and where a sequence can have more than 16 rows
- * 2 (n_tokens * Hq / Hkv / 256 + B) * Hkv * (Lk / 128 + 1) < 2^38.  n_tokens = 0 is no work.  Errors: L2A_ERR_INVALID_ARG,
+ * 2 (n_tokens * Hq / Hkv / 256 + B) * Hkv * (Lk / 128 + 1) < 2^38; Lk * (Hkv + 75) < 2^35 in any case.  n_tokens = 0 is no work.  Errors: L2A_ERR_INVALID_ARG,
  * L2A_ERR_UNSUPPORTED (D, page_size, kind, too many rows or keys), L2A_ERR_WORKSPACE, L2A_ERR_CUDA; a bounded device wait that runs out is
  * reported by the status header, not by the return value.
  */

@@ -57,13 +57,15 @@ struct CacheFwdArgs {
   float* part;                 // rows of the parts
   int few_rows;                // most rows of a sequence there, and
   int row_blocks;              // blocks of rows that it can have
+  int clear;                   // few rows: no launch ahead has cleared the status word
 };
 
 // Sequences whose new tokens have at most few_rows rows (tokens x heads of a KV group), one block of rows or kRowBlocks of them:
 // cache_few.cu
 constexpr int kBlockRows = 16, kRowBlocks = 4;
 size_t cache_few_ws_bytes(const l2a_params* p);     // plan and parts
-cudaError_t launch_cache_few(CacheFwdArgs& a, void* ws, cudaStream_t s);
+bool cache_few_counts(const l2a_params* p);         // whether it can count the tiles of one sequence
+cudaError_t launch_cache_few(const CacheFwdArgs& a, void* ws, cudaStream_t s);
 
 // All others: cache_chunk.cu
 size_t cache_chunk_ws_bytes(const l2a_params* p, int kind, int n_tokens);

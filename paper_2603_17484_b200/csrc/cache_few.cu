@@ -184,7 +184,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
   const CacheView& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   dependents_release();
-  if (blockIdx.x == 0 && tid == 0) *a.status = 0;
+  if (a.clear && blockIdx.x == 0 && tid == 0) *a.status = 0;
 
   extern __shared__ __align__(1024) uint8_t smem[];
   uint8_t* scales = smem + stages * SM::kStageBytes;
@@ -797,6 +797,12 @@ cudaError_t launch(const CacheFwdArgs& a, const CUtensorMap& mapK, const CUtenso
 int slot_rows(const l2a_params* p) { return (int64_t)p->Lq * (p->Hq / p->Hkv) > 8 ? kBlockRows : 8; }
 int row_blocks(int64_t rows) { return (int)(std::min<int64_t>(rows, kRowBlocks * kBlockRows) + kBlockRows - 1) / kBlockRows; }
 size_t plan_bytes(int B) { return align_up(((size_t)B + 1) * 8 * sizeof(int), 256); }
+// Sequences of a launch, 0: not even one.  A launch counts its tiles in 32 bits (up to one more for a segment that begins inside a tile, and
+// up to one pair's more a CTA behind the last range), and the combination has a row of its grid for each.
+int batch_of(int Lk, int Hkv, int blocks) {
+  const int64_t pair = ((int64_t)Lk + kTile - 1) / kTile + 1, one = pair * Hkv * blocks, most = (1ll << 31) - 1 - (kCtas + 1) * (pair + 1);
+  return (int)std::max<int64_t>(0, std::min<int64_t>(65535, most / one));
+}
 
 }  // namespace
 
@@ -804,7 +810,10 @@ size_t cache_few_ws_bytes(const l2a_params* p) {
   return plan_bytes(p->B) + align_up((2 * (size_t)p->B * p->Hkv * row_blocks((int64_t)p->Lq * (p->Hq / p->Hkv)) + kCtas) * slot_rows(p) * (p->D + 4) * sizeof(float), 256);
 }
 
-cudaError_t launch_cache_few(CacheFwdArgs& a, void* ws, cudaStream_t s) {
+bool cache_few_counts(const l2a_params* p) { return batch_of(p->Lk, p->Hkv, row_blocks((int64_t)p->Lq * (p->Hq / p->Hkv))) > 0; }
+
+cudaError_t launch_cache_few(const CacheFwdArgs& args, void* ws, cudaStream_t s) {
+  CacheFwdArgs a = args;
   const bool high = (int64_t)a.c.Lq * a.G > 8, e4m3 = a.c.kind == L2A_CACHE_E4M3;
   a.plan = static_cast<int*>(ws);
   a.row_blocks = row_blocks((int64_t)a.c.Lq * a.G);
@@ -813,12 +822,31 @@ cudaError_t launch_cache_few(CacheFwdArgs& a, void* ws, cudaStream_t s) {
   const int rows = std::min(1 << a.c.page_shift, kTile);
   if (!encode_pool_map(&mapK, a.c, a.c.K, rows, a.c.D / 64) || !encode_pool_map(&mapV, a.c, a.c.V, rows, a.c.D / 64))
     return cudaErrorUnknown;
-  if (a.c.D == 128) {
-    if (e4m3) return high ? launch<128, true, true>(a, mapK, mapV, s) : launch<128, true, false>(a, mapK, mapV, s);
-    return high ? launch<128, false, true>(a, mapK, mapV, s) : launch<128, false, false>(a, mapK, mapV, s);
+  const int B = a.c.B, batch = batch_of(a.c.max_keys, a.c.Hkv, row_blocks(std::min<int64_t>((int64_t)a.c.Lq * a.G, a.few_rows)));
+  cudaError_t e = batch > 0 ? cudaSuccess : cudaErrorInvalidValue;
+  for (int b = 0; e == cudaSuccess && b < B; b += batch) {
+    a.clear = b == 0;
+    a.c.B = std::min(batch, B - b);
+    a.c.table = args.c.table + (int64_t)b * a.c.table_stride;
+    a.c.lengths = args.c.lengths + b;
+    if (a.c.cu_new != nullptr) {
+      a.c.cu_new = args.c.cu_new + b;
+    } else {
+      const int64_t t = (int64_t)b * a.c.Lq;
+      a.c.n_tokens = a.c.B * a.c.Lq;
+      a.q = args.q + t * a.q_t;
+      a.O = args.O + t * a.o_t;
+      if (a.d != nullptr) a.d = args.d + t;
+    }
+    if (a.c.D == 128) {
+      if (e4m3) e = high ? launch<128, true, true>(a, mapK, mapV, s) : launch<128, true, false>(a, mapK, mapV, s);
+      else e = high ? launch<128, false, true>(a, mapK, mapV, s) : launch<128, false, false>(a, mapK, mapV, s);
+    } else {
+      if (e4m3) e = high ? launch<64, true, true>(a, mapK, mapV, s) : launch<64, true, false>(a, mapK, mapV, s);
+      else e = high ? launch<64, false, true>(a, mapK, mapV, s) : launch<64, false, false>(a, mapK, mapV, s);
+    }
   }
-  if (e4m3) return high ? launch<64, true, true>(a, mapK, mapV, s) : launch<64, true, false>(a, mapK, mapV, s);
-  return high ? launch<64, false, true>(a, mapK, mapV, s) : launch<64, false, false>(a, mapK, mapV, s);
+  return e;
 }
 
 }  // namespace l2a

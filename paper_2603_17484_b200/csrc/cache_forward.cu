@@ -39,7 +39,7 @@ l2a_status check_forward(const l2a_params* p, const l2a_cache* c, int n_tokens, 
   const uint32_t modes = p->flags & known & ~L2A_FLAG_SHARED_WINDOW;
   if ((p->flags & ~known) || (modes & (modes - 1))) return L2A_ERR_INVALID_ARG;
   if ((int64_t)n_tokens * p->Hq >= (1ll << 31) - 32) return L2A_ERR_UNSUPPORTED;      // (rows are counted in 32 bits)
-  return !has_chunks(p) || cache_chunk_counts(p, n_tokens) ? L2A_OK : L2A_ERR_UNSUPPORTED;
+  return (!has_few(p) || cache_few_counts(p)) && (!has_chunks(p) || cache_chunk_counts(p, n_tokens)) ? L2A_OK : L2A_ERR_UNSUPPORTED;
 }
 
 }  // namespace

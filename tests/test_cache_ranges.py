@@ -115,3 +115,10 @@ def test_calls_whose_blocks_cannot_be_counted_are_refused():
     assert l2a.l2a_cache_workspace_bytes(half, c, n) > 0
     with pytest.raises(l2a.L2AError):
         l2a.l2a_cache_workspace_bytes(big, c, n)
+
+
+def test_sequences_whose_tiles_cannot_be_counted_are_refused():
+    """One sequence of few rows over 2^31 - 1 keys: 2^25 tiles, which 296 ranges round up past 2^31."""
+    c = cache(table_stride=1 << 24, page_size=128)
+    assert calls(params(B=1, Lq=1, Lk=(1 << 31) - 1, Hq=1, Hkv=1), c, n=1)[2] == UNSUPPORTED
+    assert l2a.l2a_cache_workspace_bytes(params(B=1, Lq=1, Lk=1 << 28, Hq=1, Hkv=1), c, 1) > 0
