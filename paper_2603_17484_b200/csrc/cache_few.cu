@@ -435,9 +435,27 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
               mma_16816<false>(sc[1], qa[k], kb[2], kb[3]);
             }
           }
-          uint32_t pa[4], pb[4];                       // A fragments of the weights, and of what their rounding cut off
+          // e4m3: a lane's share of the codes of one of its four keys' values (key0 + 2 t4 + {0, 1, 8, 9})
+          constexpr int kWords = kCols / 4;
+          auto value_codes = [&](int y, uint32_t (&w)[kWords]) {
+            const int row = r0 + 2 * t4 + (y & 1) + (y >> 1) * 8;
+            if (D == 128) {
+              const float4 z = lds128(tV + row * 128 + ((hr ^ (row & 7)) << 4));
+              w[0] = __float_as_uint(z.x); w[1] = __float_as_uint(z.y);
+              w[kWords - 2] = __float_as_uint(z.z); w[kWords - 1] = __float_as_uint(z.w);
+            } else {
+              const uint32_t at = tV + row * 64 + (((hr >> 1) ^ ((row >> 1) & 3)) << 4) + (hr & 1) * 8;
+              w[0] = lds32(at);
+              w[1] = lds32(at + 4);
+            }
+          };
+          // ---- weights: u is what they are two to the power of, relative to the reference
+          float u[kHalves][4], top[kHalves];
+          auto row_max = [](const float (&y)[4]) {
+            const float z = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), q = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, 1));
+            return fmaxf(q, __shfl_xor_sync(0xffffffffu, q, 2));
+          };
           bool grow = false;
-          float alpha[2] = {1.f, 1.f};
 #pragma unroll
           for (int x = 0; x < kHalves; ++x) {
             float v[4] = {sc[0][2 * x] * row_scale[x], sc[0][2 * x + 1] * row_scale[x], sc[1][2 * x] * row_scale[x],
@@ -450,37 +468,65 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
                 if (j < row_lo[x] || j > row_hi[x]) v[y] = -INFINITY;
               }
             }
-            float top = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            float u[4], w[4];
             if (kE4M3) {
-              const float m_new = fmaxf(m[x], top), base = m_new == -INFINITY ? 0.f : m_new;
+              const float m_new = fmaxf(m[x], row_max(v)), base = m_new == -INFINITY ? 0.f : m_new;
               l[x] = l[x] * fast_exp2(m[x] - base) + ((fast_exp2(v[0] - base) + fast_exp2(v[1] - base)) +
                                                        (fast_exp2(v[2] - base) + fast_exp2(v[3] - base)));
               m[x] = m_new;
-#pragma unroll
-              for (int y = 0; y < 4; ++y) u[y] = v[y] + (float)((int)(y & 1 ? ev[y >> 1] >> 8 : ev[y >> 1] & 0xffu) - 127);
-              top = fmaxf(fmaxf(u[0], u[1]), fmaxf(u[2], u[3]));
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            } else {
-#pragma unroll
-              for (int y = 0; y < 4; ++y) u[y] = v[y];
             }
-            if (top > ref[x] + kLag) {                 // (the same for the four lanes of a row)
-              alpha[x] = fast_exp2(ref[x] - top);      // 0 the first time
-              ref[x] = top;
-              grow = true;
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              u[x][y] = kE4M3 ? v[y] + (float)((int)(y & 1 ? ev[y >> 1] >> 8 : ev[y >> 1] & 0xffu) - 127) : v[y];
+            top[x] = row_max(u[x]);
+            grow |= top[x] > ref[x] + kLag;            // (the same for the four lanes of a row)
+          }
+          uint32_t pa[4], pb[4];                       // A fragments of the weights, and of what their rounding cut off
+          if (__any_sync(0xffffffffu, grow)) {
+            // Values of zeros have exponent 0 however small all others are: they must not become the reference, which would push the
+            // weights of the others out of fp16's range.  They get the least exponent.
+            if (kE4M3 && __any_sync(0xffffffffu, __vcmpeq4(ev[0] | ev[1] << 16, 0x7f7f7f7fu) != 0)) {
+              uint32_t some = 0;                       // bit y: key y has a value that is not zero
+#pragma unroll
+              for (int y = 0; y < 4; ++y) {
+                uint32_t w[kWords], any = 0;
+                value_codes(y, w);
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) any |= w[i] & 0x7f7f7f7fu;
+                some |= any != 0 ? 1u << y : 0u;
+              }
+#pragma unroll
+              for (int o = 4; o < 32; o <<= 1) some |= __shfl_xor_sync(0xffffffffu, some, o);
+#pragma unroll
+              for (int x = 0; x < kHalves; ++x) {
+#pragma unroll
+                for (int y = 0; y < 4; ++y) u[x][y] -= some >> y & 1u ? 0.f : 127.f;
+                top[x] = row_max(u[x]);
+              }
             }
+            float alpha[2] = {1.f, 1.f};
+#pragma unroll
+            for (int x = 0; x < kHalves; ++x) {
+              if (top[x] > ref[x] + kLag) {
+                alpha[x] = fast_exp2(ref[x] - top[x]);           // 0 the first time
+                ref[x] = top[x];
+                if (!kE4M3) l[x] *= alpha[x];
+              }
+            }
+            if (!kHigh) alpha[1] = alpha[0];
+#pragma unroll
+            for (int j = 0; j < D / 8; ++j) { acc[j][0] *= alpha[0]; acc[j][1] *= alpha[0]; acc[j][2] *= alpha[1]; acc[j][3] *= alpha[1]; }
+          }
+#pragma unroll
+          for (int x = 0; x < kHalves; ++x) {
             const float zero = (ref[x] == -INFINITY ? 0.f : ref[x]) - (kE4M3 ? kWeightTop : 0.f);
+            float w[4];
 #pragma unroll
-            for (int y = 0; y < 4; ++y) w[y] = fast_exp2(u[y] - zero);
+            for (int y = 0; y < 4; ++y) w[y] = fast_exp2(u[x][y] - zero);
             if (kE4M3) {
               pa[x] = pack_f16(w[0], w[1]);
               pa[2 + x] = pack_f16(w[2], w[3]);
             } else {
-              l[x] = l[x] * alpha[x] + ((w[0] + w[1]) + (w[2] + w[3]));
+              l[x] += (w[0] + w[1]) + (w[2] + w[3]);
               const uint32_t h0 = pack_bf16(w[0], w[1]), h1 = pack_bf16(w[2], w[3]);
               pa[x] = h0;
               pa[2 + x] = h1;
@@ -493,11 +539,6 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           if (!kHigh) {
             pa[1] = kE4M3 ? 0u : pb[0];
             pa[3] = kE4M3 ? 0u : pb[2];
-            alpha[1] = alpha[0];
-          }
-          if (__any_sync(0xffffffffu, grow)) {
-#pragma unroll
-            for (int j = 0; j < D / 8; ++j) { acc[j][0] *= alpha[0]; acc[j][1] *= alpha[0]; acc[j][2] *= alpha[1]; acc[j][3] *= alpha[1]; }
           }
           // ---- O += P V.  Slots outside the segment's keys may hold anything: their values are made zeros.
           const bool clear = key0 < p.lo || key0 + 15 > p.hi;
@@ -508,20 +549,10 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
             out[y] = j < p.lo || j > p.hi;
           }
           if (kE4M3) {
-            constexpr int kWords = kCols / 4;
             uint32_t w[4][kWords];
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
-              const int row = r0 + 2 * t4 + (y & 1) + (y >> 1) * 8;
-              if (D == 128) {
-                const float4 z = lds128(tV + row * 128 + ((hr ^ (row & 7)) << 4));
-                w[y][0] = __float_as_uint(z.x); w[y][1] = __float_as_uint(z.y);
-                w[y][kWords - 2] = __float_as_uint(z.z); w[y][kWords - 1] = __float_as_uint(z.w);
-              } else {
-                const uint32_t at = tV + row * 64 + (((hr >> 1) ^ ((row >> 1) & 3)) << 4) + (hr & 1) * 8;
-                w[y][0] = lds32(at);
-                w[y][1] = lds32(at + 4);
-              }
+              value_codes(y, w[y]);
               if (clear && out[y]) {
 #pragma unroll
                 for (int i = 0; i < kWords; ++i) w[y][i] = 0u;
