@@ -16,19 +16,21 @@
 //   warps 0-7   : soft-max, correction and epilogue, one thread a row; they also gather the rows of Q
 //   warp 8      : TMA producer, one copy a page (and 64 columns in bf16)
 //   warp 9      : tcgen05 MMA issuer and TMEM owner
-//   warps 12-15 : one thread a key.  e4m3: decode the values to fp16 tiles.  Both kinds: zeros for the values of keys that no row
-//                 of the group sees (their slots may hold anything).
-// e4m3: the codes of K are an operand as they are.  Q is the sum of two e4m3 numbers, exactly (8 bits in two terms of 4 and a sign,
-// elements below 2^-10 of the row's largest to 2^-18 of that), so Q K^T is two products at twice the rate of bf16; the soft-max
-// warps multiply the scores by the keys' scales.  The values' scales would have to be known to the weights, key by key; instead they
-// are decoded, times their power of two relative to the largest of 32 keys, which goes into the exponent of the weights.
+//   warps 12-15 : one thread a key.  e4m3: decode keys and values to the bf16 tiles that the products read, exactly (code * 2^e), so that
+//                 both kinds of caches share all that follows, to the bit.  Both kinds: zeros for the values of keys that no row of the
+//                 group sees (their slots may hold anything).
+// Weights enter the second product as bf16, one term (8 bits; the sum of the weights is taken before), as in l2a_forward: a second term would be
+// half as many products again.
 //
 // Measured, 2000 tokens on 34768 keys (32/8 heads, D = 128, window 4096, a fifth routed; 21.5K key blocks of two tiles): call 352 us from
 // an 8-bit cache (decoded once: 42 us for 213 MB), in a shorter run 341 next to 329 from bf16; 329 GFLOP = 0.93 to 1.00 PFLOP/s.  A key block
 // takes 2900 clk, 2048 of them its products; the tensor pipe is active 62 % of a launch and the special-function unit 46 %.  A piece takes
 // about 9600 clk besides: look-up 100, first scores 540, last products 2900, store of Q and results 6050.
 // In a long loop the power cap lowers the clock (388 us at 1.67 of 1.965 GHz; 409 in another run).
-// Decoding in the products' kernel: 4850 clk a block (6420 before the operands became fp16).
+// Decoding in the products' kernel, four sequences of 16384 keys, 383 tokens each (32/8 heads): 366 us next to 208 from bf16, 262 for an
+// earlier form with K as 8-bit operands (Q in two e4m3 terms) and values relative to the largest of 32 keys in fp16: there a large value
+// took bits from rows that do not see it, and small elements of Q were lost.  Tried for the decoding: codes spread to bf16 by integer
+// operations 446 us, codes in a ring of their own with two stages of K 400, six warps instead of four 353.
 #include <math.h>
 
 #include <algorithm>
@@ -49,7 +51,6 @@ constexpr int kSoftmaxRegs = 200, kOtherRegs = 56;
 static_assert(kSoftmaxWarps * kSoftmaxRegs + 8 * kOtherRegs <= 16 * 128, "register shares exceed the launch allocation");
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
 constexpr int kBoxBytes = 128 * 128;       // 128 rows of 128 bytes
-constexpr float kWeightTop = 7.0f;         // e4m3: weights lie at 2^7 and, while the reference lags, up to 2^15 (fp16 operands)
 constexpr int kPlanThreads = 1024;
 constexpr int kCtas = kSplitSms;
 
@@ -457,18 +458,26 @@ __device__ __forceinline__ TileBlocks tile_blocks(const Group& g, const ChunkPie
   return x;
 }
 
-constexpr int kBarBytes = 512, kScaleSlots = 4;
+constexpr int kBarBytes = 512;
 template <int D, bool kE4M3>
 struct ChunkSmem {
-  static constexpr int kQTileBytes = kTileM * D * 2;                     // e4m3: both terms
-  static constexpr int kKTileBytes = kTileN * D * (kE4M3 ? 1 : 2);
+  static constexpr int kQTileBytes = kTileM * D * 2;
+  static constexpr int kKTileBytes = kTileN * D * 2;
   static constexpr int kVTileBytes = kTileN * D * 2;
-  static constexpr int kRawBytes = kE4M3 ? kTileN * D : 0;               // codes of V
+  // Codes land where their bf16 tile will be: with D = 128 on its second 64 columns, a key's 128 codes on the same 128 bytes that its
+  // values take there, so that a thread finds its row and leaves it without the others.  Rows of 64 codes do not fit that way.
+  static constexpr int kCodes = kTileN * D;
+  static constexpr bool kApart = kE4M3 && D == 64;
   static constexpr int kKOff = 2 * kQTileBytes;
   static constexpr int kVOff = kKOff + kKStages * kKTileBytes;
   static constexpr int kRawOff = kVOff + kVStages * kVTileBytes;
-  static constexpr int kScaleOff = kRawOff + kVStages * kRawBytes;       // scales of K, by key
-  static constexpr int kBarOff = kScaleOff + (kE4M3 ? kScaleSlots * kTileN * 4 : 0);
+  static constexpr int kBarOff = kRawOff + (kApart ? (kKStages + kVStages) * kCodes : 0);
+  static __device__ __forceinline__ uint8_t* k_codes(uint8_t* smem, int s) {
+    return kApart ? smem + kRawOff + s * kCodes : smem + kKOff + s * kKTileBytes + kBoxBytes;
+  }
+  static __device__ __forceinline__ uint8_t* v_codes(uint8_t* smem, int s) {
+    return kApart ? smem + kRawOff + (kKStages + s) * kCodes : smem + kVOff + s * kVTileBytes + kBoxBytes;
+  }
   static constexpr int kGroupOff = kBarOff + kBarBytes;
   static constexpr int kTotal = kGroupOff + kKeepGroups * (int)sizeof(Group) + 1024 /* alignment slack */;
 };
@@ -477,47 +486,12 @@ struct ChunkBars {
   uint64_t q_full[2];
   uint64_t k_full[kKStages], k_empty[kKStages], v_full[kVStages], v_empty[kVStages];
   uint64_t s_full[2], p_half[2], p_full[2], o_final[2];
-  uint64_t raw_full[kVStages], raw_empty[kVStages];      // e4m3: codes of V; bf16: V before the clearing
-  uint64_t scale_full[kScaleSlots];
-  float4 v_exp[kScaleSlots];                             // exponent of V of the 32 keys of each decoding warp
+  uint64_t k_raw[kKStages], v_raw[kVStages];             // e4m3: codes; bf16: V before the clearing
   uint32_t tmem_base;
   int abort_flag;
 };
 static_assert(sizeof(ChunkBars) <= kBarBytes, "barriers");
 
-// 16 codes times a power of two (two of it) as fp16
-__device__ __forceinline__ void scaled_codes(const float4& codes, uint32_t scale2, uint32_t (&o)[8]) {
-  const uint32_t w[4] = {__float_as_uint(codes.x), __float_as_uint(codes.y), __float_as_uint(codes.z), __float_as_uint(codes.w)};
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    uint32_t lo, hi;
-    e4m3x4_to_f16(w[k], lo, hi);
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * k]) : "r"(lo), "r"(scale2));
-    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(o[2 * k + 1]) : "r"(hi), "r"(scale2));
-  }
-}
-__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-// Instruction descriptor, kind::f8f6f4: e4m3 x e4m3 -> fp32, both K-major
-__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N) {
-  return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
-}
-__device__ __forceinline__ void mma_ss_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
-      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
-}
-// Descriptor of a K-major operand with rows of 64 bytes, 64-byte swizzle (groups of eight rows 512 bytes apart)
-__device__ __forceinline__ uint64_t smem_desc_sw64(uint32_t saddr) {
-  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | 1ull << 16 | 32ull << 32 | 1ull << 46 | 4ull << 61;
-}
-// Instruction descriptor as idesc_bf16_f32, of fp16 operands
-__host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N, int a_mn_major, int b_mn_major) {
-  return idesc_bf16_f32(M, N, a_mn_major, b_mn_major) & ~((1u << 7) | (1u << 10));
-}
 __device__ __forceinline__ void sts128(uint32_t saddr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(saddr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
@@ -527,7 +501,7 @@ struct RowOf {
   TileBlocks tb;
   int token, head, lo, hi;       // first and last key that it sees
   int min_hi, max_lo;            // of the tile
-  int slot, first_block, n_blocks;
+  int slot;
   bool valid, seg, whole;        // whole: the piece holds all of the row's keys in this segment
   int rank;                      // segment 0: whether other keys are to be joined (>= 0),
   uint8_t routed;                // and the routing decision; looked up here, needed at the piece's end
@@ -549,8 +523,6 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
   uint8_t* sQ = smem;
   uint8_t* sK = smem + SM::kKOff;
   uint8_t* sV = smem + SM::kVOff;
-  uint8_t* sRaw = smem + SM::kRawOff;
-  float* sScale = reinterpret_cast<float*>(smem + SM::kScaleOff);
   ChunkBars* bar = reinterpret_cast<ChunkBars*>(smem + SM::kBarOff);
   Group* sGroups = reinterpret_cast<Group*>(smem + SM::kGroupOff);
   volatile int* abort_flag = &bar->abort_flag;
@@ -564,16 +536,15 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       mbar_init(&bar->o_final[t], 1);
     }
     for (int s = 0; s < kKStages; ++s) {
-      mbar_init(&bar->k_full[s], 1);
+      mbar_init(&bar->k_raw[s], 1);
+      mbar_init(&bar->k_full[s], kE4M3 ? kConvWarps * 32 : 1);
       mbar_init(&bar->k_empty[s], 1);
     }
     for (int s = 0; s < kVStages; ++s) {
       mbar_init(&bar->v_full[s], kConvWarps * 32);
       mbar_init(&bar->v_empty[s], 1);
-      mbar_init(&bar->raw_full[s], 1);
-      mbar_init(&bar->raw_empty[s], kConvWarps);
+      mbar_init(&bar->v_raw[s], 1);
     }
-    for (int i = 0; i < kScaleSlots; ++i) mbar_init(&bar->scale_full[i], kConvWarps);
     bar->abort_flag = 0;
     fence_mbar_init();
   }
@@ -637,19 +608,24 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         if (load)
           tma_load_page(dst + (kE4M3 ? u * rows * D : piece * kBoxBytes + u * rows * 128), map, full, kE4M3, piece, 0, pc.head, page);
       };
-      // in the order in which the products take them
+      auto copy_v = [&](int j) -> bool {
+        const int s = v_cnt & 1;
+        if (!mbar_wait_warp(&bar->v_empty[s], ((v_cnt >> 1) & 1) ^ 1, abort_flag)) return false;
+        copy(j, kE4M3 ? SM::v_codes(smem, s) : sV + s * SM::kVTileBytes, &mapV, &bar->v_raw[s]);
+        ++v_cnt;
+        return true;
+      };
+      auto copy_k = [&](int j) -> bool {
+        if (!mbar_wait_warp(&bar->k_empty[k_slot], k_ph, abort_flag)) return false;
+        copy(j, kE4M3 ? SM::k_codes(smem, k_slot) : sK + k_slot * SM::kKTileBytes, &mapK, kE4M3 ? &bar->k_raw[k_slot] : &bar->k_full[k_slot]);
+        if (++k_slot == kKStages) { k_slot = 0; k_ph ^= 1; }
+        return true;
+      };
+      // In the order in which the products take them.  e4m3: in that of the decoding, which has K done while V is on its way.
       for (int j = pc.j0 - step; ok && j <= pc.j1; ++j) {
-        if (j >= pc.j0) {
-          const int s = v_cnt & 1;
-          if (!mbar_wait_warp(kE4M3 ? &bar->raw_empty[s] : &bar->v_empty[s], ((v_cnt >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
-          copy(j, kE4M3 ? sRaw + s * SM::kRawBytes : sV + s * SM::kVTileBytes, &mapV, &bar->raw_full[s]);
-          ++v_cnt;
-        }
-        if (j + step <= pc.j1) {
-          if (!mbar_wait_warp(&bar->k_empty[k_slot], k_ph, abort_flag)) { ok = false; break; }
-          copy(j + step, sK + k_slot * SM::kKTileBytes, &mapK, &bar->k_full[k_slot]);
-          if (++k_slot == kKStages) { k_slot = 0; k_ph ^= 1; }
-        }
+        if (!kE4M3 && j >= pc.j0) ok = copy_v(j);
+        if (ok && j + step <= pc.j1) ok = copy_k(j + step);
+        if (kE4M3 && ok && j >= pc.j0) ok = copy_v(j);
       }
     }
   } else if (warp == kMmaWarp) {
@@ -657,11 +633,8 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     setmaxnreg_dec<kOtherRegs>();
     if (elect_one()) {
       constexpr uint32_t tmem = 0;   // checked above: TMEM operand addresses are immediates in this loop
-      constexpr uint32_t idesc_qk = kE4M3 ? idesc_e4m3_f32(kTileM, kTileN) : idesc_bf16_f32(kTileM, kTileN, 0, 0);
-      constexpr uint32_t idesc_pv = kE4M3 ? idesc_f16_f32(kTileM, D, 0, 1) : idesc_bf16_f32(kTileM, D, 0, 1);
-      auto k_major = [](const uint8_t* tile) {
-        return kE4M3 && D == 64 ? smem_desc_sw64(smem_u32(tile)) : smem_desc_sw128(smem_u32(tile), 16, 1024);
-      };
+      constexpr uint32_t idesc_qk = idesc_bf16_f32(kTileM, kTileN, 0, 0), idesc_pv = idesc_bf16_f32(kTileM, D, 0, 1);
+      auto k_major = [](const uint8_t* tile) { return smem_desc_sw128(smem_u32(tile), 16, 1024); };
       const uint64_t dq0 = k_major(sQ), dq1 = k_major(sQ + SM::kQTileBytes), dk0 = k_major(sK);
       const uint64_t dv0 = smem_desc_sw128(smem_u32(sV), kBoxBytes, 1024);
       const uint64_t dv1 = smem_desc_sw128(smem_u32(sV + SM::kVTileBytes), kBoxBytes, 1024);
@@ -671,18 +644,10 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       auto issue_qk = [&](int t, int s) {
         const uint64_t qd = t ? dq1 : dq0, kd = dk0 + s * (SM::kKTileBytes >> 4);
         const uint32_t d = tmem + t * kTileN;
-        if (kE4M3) {
 #pragma unroll
-          for (int term = 0; term < 2; ++term)
-#pragma unroll
-            for (int kk = 0; kk < D / 32; ++kk)
-              mma_ss_f8(d, qd + ((term * kTileM * D + kk * 32) >> 4), kd + ((kk * 32) >> 4), idesc_qk, term + kk > 0);
-        } else {
-#pragma unroll
-          for (int kk = 0; kk < kKSteps; ++kk) {
-            const uint32_t o = ((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4;
-            mma_ss(d, qd + o, kd + o, idesc_qk, kk > 0);
-          }
+        for (int kk = 0; kk < kKSteps; ++kk) {
+          const uint32_t o = ((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4;
+          mma_ss(d, qd + o, kd + o, idesc_qk, kk > 0);
         }
         tc_commit(&bar->s_full[t]);
       };
@@ -772,82 +737,87 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     ChunkWalk walk;
     ChunkPiece pc;
     bool ok = walk.init(w, sGroups);
-    uint32_t it = 0;
+    uint32_t it = 0, k_slot = 0, k_ph = 0;
     while (ok && walk.next(w, c.Hkv, pc)) {
       const Group& g = walk.group_now(w);
-      const int b = g.b, key_lo = g.key_lo, key_hi = g.key_hi;
-      // page of this thread's key three blocks ahead, the exponents of its rows of K and V two blocks ahead
-      auto page_of = [&](int j) -> int {
-        const int key = j * kTileN + row;
-        return kE4M3 && key >= key_lo && key <= key_hi ? cache_page(c, b, key) : -1;
-      };
-      auto exponents = [&](int j, int page) -> uint32_t {
-        if (page < 0) return 0u;
-        const int64_t at = page * c.scale_stride + ((int64_t)pc.head << c.page_shift) + ((j * kTileN + row) & ((1 << c.page_shift) - 1));
-        return c.ks[at] | (uint32_t)c.vs[at] << 8;
-      };
-      // The values of a warp's 32 keys get the scale of the largest among them: the codes of the others times a power of two below one,
-      // exact in fp16 down to 2^-24, which is 2^-33 of the largest value.  Returns that factor, twice; `at`: the block's count.
-      auto publish = [&](uint32_t exps, uint32_t at) -> uint32_t {
-        const int slot = at & (kScaleSlots - 1), e = (int)(exps >> 8);
-        int top = __reduce_max_sync(0xffffffffu, e);
-        if (top == 0) top = 127;
-        sScale[slot * kTileN + row] = scale_of_exponent(exps & 0xffu);
-        if (lane == 0) reinterpret_cast<float*>(&bar->v_exp[slot])[warp - kConvWarp] = (float)(top - 127);
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bar->scale_full[slot]);
-        const float f = __uint_as_float((uint32_t)max(e - top + 127, 0) << 23);
-        return pack_f16(f, f);
-      };
-      uint32_t ahead = 0, scale2 = 0, next_scale2 = 0;
-      int page = -1;
-      if (kE4M3) {
-        next_scale2 = publish(exponents(pc.j0, page_of(pc.j0)), it);
-        ahead = exponents(pc.j0 + 1, page_of(pc.j0 + 1));
-        page = page_of(pc.j0 + 2);
-      }
-      for (int j = pc.j0; ok && j <= pc.j1; ++j, ++it) {
-        const int s = it & 1, key = j * kTileN + row;
-        const uint32_t ph = (it >> 1) & 1;
-        const bool seen = key >= key_lo && key <= key_hi;
-        if (kE4M3) {
-          scale2 = next_scale2;
-          if (j < pc.j1) next_scale2 = publish(ahead, it + 1);
-          ahead = exponents(j + 2, page);
-          page = page_of(j + 3);
-        }
-        const uint32_t dst = smem_u32(sV + s * SM::kVTileBytes) + row * 128;
-        if (kE4M3) {
-          if (!mbar_wait_warp(&bar->raw_full[s], ph, abort_flag)) { ok = false; break; }
-          const uint32_t src = smem_u32(sRaw + s * SM::kRawBytes) + row * D;
-          float4 x[D / 16];
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k) x[k] = lds128(src + ((D == 128 ? k ^ (row & 7) : k ^ ((row >> 1) & 3)) << 4));
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&bar->raw_empty[s]);
-          if (!mbar_wait_warp(&bar->v_empty[s], ph ^ 1, abort_flag)) { ok = false; break; }
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k) {
-            uint32_t o[8];
-            scaled_codes(x[k], scale2, o);
-            if (!seen) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) o[i] = 0u;
-            }
-            const uint32_t at = dst + (k >> 2) * kBoxBytes;
-            sts128(at + (((2 * k) & 7 ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
-            sts128(at + (((2 * k + 1) & 7 ^ (row & 7)) << 4), o[4], o[5], o[6], o[7]);
-          }
-          fence_async_smem();
-        } else {
-          if (!mbar_wait_warp(&bar->raw_full[s], ph, abort_flag)) { ok = false; break; }
-          if (!seen) {
+      const int b = g.b, key_lo = g.key_lo, key_hi = g.key_hi, step = g.dual ? 2 : 1;
+      auto seen = [&](int j) { return j * kTileN + row >= key_lo && j * kTileN + row <= key_hi; };
+      if (!kE4M3) {
+        for (int j = pc.j0; ok && j <= pc.j1; ++j, ++it) {
+          const int s = it & 1;
+          if (!mbar_wait_warp(&bar->v_raw[s], (it >> 1) & 1, abort_flag)) { ok = false; break; }
+          if (!seen(j)) {
+            const uint32_t dst = smem_u32(sV + s * SM::kVTileBytes) + row * 128;
 #pragma unroll
             for (int k = 0; k < D / 8; ++k) sts128(dst + (k >> 3) * kBoxBytes + ((k & 7) << 4), 0u, 0u, 0u, 0u);
             fence_async_smem();
           }
+          mbar_arrive(&bar->v_full[s]);
         }
-        mbar_arrive(&bar->v_full[s]);
+        continue;
+      }
+      // Of this thread's key in block j: its entry of the table (-1: none is needed), and from that the exponents of its rows of K and V.  What
+      // is loaded is looked at a block later.
+      auto entry_of = [&](int j) -> int {
+        return seen(j) ? c.table[(int64_t)b * c.table_stride + ((j * kTileN + row) >> c.page_shift)] : -1;
+      };
+      auto exponents = [&](int j, int entry, uint32_t& k, uint32_t& v) {
+        k = v = 0u;
+        if (entry < 0 || entry >= c.n_pages) return;
+        const int64_t at = entry * c.scale_stride + ((int64_t)pc.head << c.page_shift) + ((j * kTileN + row) & ((1 << c.page_shift) - 1));
+        k = c.ks[at];
+        v = c.vs[at];
+      };
+      // this thread's row of a block of codes, times 2^e, to its tile
+      auto decode = [&](const uint8_t* codes, uint8_t* tile, uint64_t* raw, uint32_t ph, uint64_t* full, uint32_t e, bool zero) -> bool {
+        if (!mbar_wait_warp(raw, ph, abort_flag)) return false;
+        const uint32_t src = smem_u32(codes) + row * D, dst = smem_u32(tile) + row * 128;
+        const float scale = scale_of_exponent(e);
+#pragma unroll 1
+        for (int half = 0; half < D / 64; ++half) {          // (64 columns at a time: the second half of the codes is overwritten last)
+          uint4 x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4 y = lds128(src + ((D == 128 ? (half * 4 + i) ^ (row & 7) : i ^ ((row >> 1) & 3)) << 4));
+            x[i] = zero ? make_uint4(0u, 0u, 0u, 0u)
+                        : make_uint4(__float_as_uint(y.x), __float_as_uint(y.y), __float_as_uint(y.z), __float_as_uint(y.w));
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t o[8];
+            decode_16(x[i], scale, o);
+            const uint32_t at = dst + half * kBoxBytes;
+            sts128(at + (((2 * i) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
+            sts128(at + (((2 * i + 1) ^ (row & 7)) << 4), o[4], o[5], o[6], o[7]);
+          }
+        }
+        fence_async_smem();
+        mbar_arrive(full);
+        return true;
+      };
+      // Pages are looked up three blocks ahead of K, exponents two; those of V wait until its block comes, `step` behind that of K.
+      uint32_t k_now, k_next, v_now, v_next, v_back1 = 0, v_back2 = 0;
+      exponents(pc.j0, entry_of(pc.j0), k_now, v_now);
+      exponents(pc.j0 + 1, entry_of(pc.j0 + 1), k_next, v_next);
+      int entry = entry_of(pc.j0 + 2);
+      for (int j = pc.j0 - step; ok && j <= pc.j1; ++j) {
+        const int x = j + step;
+        if (x <= pc.j1) {
+          ok = decode(SM::k_codes(smem, k_slot), sK + k_slot * SM::kKTileBytes, &bar->k_raw[k_slot], k_ph, &bar->k_full[k_slot], k_now, false);
+          if (++k_slot == kKStages) { k_slot = 0; k_ph ^= 1; }
+        }
+        if (ok && j >= pc.j0) {
+          const int s = it & 1;
+          ok = decode(SM::v_codes(smem, s), sV + s * SM::kVTileBytes, &bar->v_raw[s], (it >> 1) & 1, &bar->v_full[s],
+                      step == 2 ? v_back2 : v_back1, !seen(j));
+          ++it;
+        }
+        v_back2 = v_back1;
+        v_back1 = v_now;
+        k_now = k_next;
+        v_now = v_next;
+        exponents(x + 2, entry, k_next, v_next);
+        entry = entry_of(x + 3);
       }
     }
   } else if (warp > kMmaWarp) {
@@ -879,8 +849,6 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       me.rank = seg && a.local ? 0 : -1;
       me.routed = 0;
       me.slot = pc.item + blockIdx.x;
-      me.first_block = pc.j0;
-      me.n_blocks = pc.j1 - pc.j0 + 1;
       me.token = me.head = 0;
       me.lo = 0x3fffffff;
       me.hi = -1;
@@ -903,10 +871,8 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       }
       return true;
     };
-    // The warp's 32 rows of Q, 16-byte pieces, to where the products read them (bf16: as a TMA copy would leave them; e4m3: as the sum of
-    // two terms, the row's largest element scaled to 2^7 .. 2^8).  Returns this thread's row's factor of the scores.
-    auto store_q = [&]() -> float {
-      float factor = a.scale_log2;
+    // The warp's 32 rows of Q, 16-byte pieces, to where a TMA copy would leave them
+    auto store_q = [&]() {
       uint4 qx[kPieces];
       const bf16* src = me.valid ? a.q + me.token * a.q_t + (int64_t)me.head * D : nullptr;
 #pragma unroll
@@ -916,68 +882,29 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         qx[k] = q != nullptr ? __ldcg(reinterpret_cast<const uint4*>(q) + piece) : make_uint4(0, 0, 0, 0);
       }
       const uint32_t base = smem_u32(sQ + t * SM::kQTileBytes);
-      uint32_t mine = 127;
 #pragma unroll
       for (int k = 0; k < kPieces; ++k) {
         const int rr = (warp & 3) * 32 + k * kRowsPerStep + lane / kPieces;
-        if (kE4M3) {
-          const uint32_t u[4] = {qx[k].x, qx[k].y, qx[k].z, qx[k].w};
-          uint32_t top = 0;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) top = __vmaxu2(top, u[e] & 0x7fff7fffu);
-          top = max(top & 0xffffu, top >> 16);
-#pragma unroll
-          for (int o = kPieces / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-          const int up = min(max(7 + 127 - (int)(top >> 7), -113), 100);
-          const float f = __uint_as_float((uint32_t)(up + 127) << 23);
-          uint32_t first[4], second[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            two_e4m3_terms(__uint_as_float(u[e] << 16) * f, __uint_as_float(u[e] & 0xffff0000u) * f, first[e], second[e]);
-          const uint32_t dst = base + rr * D + (((piece >> 1) ^ (D == 128 ? rr & 7 : (rr >> 1) & 3)) << 4) + (piece & 1) * 8;
-          asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(dst), "r"(first[0] | first[1] << 16), "r"(first[2] | first[3] << 16) : "memory");
-          asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(dst + kTileM * D), "r"(second[0] | second[1] << 16),
-                       "r"(second[2] | second[3] << 16) : "memory");
-          // this thread's own row, its lane: step lane / kRowsPerStep, lanes of row lane % kRowsPerStep
-          const uint32_t theirs = __shfl_sync(0xffffffffu, (uint32_t)(127 - up), (lane % kRowsPerStep) * kPieces);
-          if (lane / kRowsPerStep == k) mine = theirs;
-        } else {
-          sts128(base + (piece >> 3) * kBoxBytes + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4), qx[k].x, qx[k].y, qx[k].z, qx[k].w);
-        }
+        sts128(base + (piece >> 3) * kBoxBytes + rr * 128 + (((piece & 7) ^ (rr & 7)) << 4), qx[k].x, qx[k].y, qx[k].z, qx[k].w);
       }
-      if (kE4M3) factor *= __uint_as_float(mine << 23);
       fence_async_smem();
       mbar_arrive(&bar->q_full[t]);
-      return factor;
     };
 
     bool ok = walk.init(w, sGroups);
     bool more = ok && advance();
-    float row_scale = a.scale_log2;
-    if (more && me.tb.first <= me.tb.last) row_scale = store_q();
-    uint32_t s_cnt = 0, o_cnt = 0, it0 = 0;            // it0: block count of the piece's first block
+    if (more && me.tb.first <= me.tb.last) store_q();
+    uint32_t s_cnt = 0, o_cnt = 0;
     while (more) {
       const RowOf cur = me;
       const TileBlocks tb = cur.tb;
       const bool any = tb.first <= tb.last, warp_has_rows = __any_sync(0xffffffffu, cur.valid);
       float m_use = -INFINITY;   // reference maximum, exp2 domain
       float l = 0.f;             // row sum
-      float v_first = 0.f;       // e4m3: exponent of the first values, which the sum's terms are taken relative to
       for (int j = tb.first; j <= tb.last; j += tb.step) {
-        float ev[4];             // e4m3: exponent of the values of each 32 keys
-        const uint32_t it = it0 + (j - cur.first_block);
         // warp-uniform outcome: the TMEM loads/stores below are warp-collective
         if (!mbar_wait_warp(&bar->s_full[t], s_cnt & 1, abort_flag)) { ok = false; break; }
         ++s_cnt;
-        // Behind the scores: a tile without a block in much of a piece comes here many blocks ahead of the scales, where the slot's phase of
-        // two rounds ago would pass for the one that is meant.  With the scores there, at most two blocks' scales are missing.
-        if (kE4M3 && warp_has_rows) {
-          const uint32_t slot = it & (kScaleSlots - 1);
-          if (!mbar_wait_warp(&bar->scale_full[slot], (it / kScaleSlots) & 1, abort_flag)) { ok = false; break; }
-          const float4 y = lds128(smem_u32(&bar->v_exp[slot]));
-          ev[0] = y.x; ev[1] = y.y; ev[2] = y.z; ev[3] = y.w;
-          if (j == tb.first) v_first = ev[0];
-        }
         tc_fence_after();
         if (!warp_has_rows) {    // nothing of these rows is ever stored
           mbar_arrive(&bar->p_half[t]);
@@ -990,20 +917,6 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
 #pragma unroll
         for (int q = 0; q < 4; ++q) tmem_ld32(s_addr + q * 32, v[q]);
         tmem_ld_wait();
-        if (kE4M3) {
-          const uint32_t scales = smem_u32(sScale + (it & (kScaleSlots - 1)) * kTileN);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              const float4 f = lds128(scales + (q * 32 + e) * 4);
-              const float2 x = __fmul2_rn(make_float2(__uint_as_float(v[q][e]), __uint_as_float(v[q][e + 1])), make_float2(f.x, f.y));
-              const float2 y = __fmul2_rn(make_float2(__uint_as_float(v[q][e + 2]), __uint_as_float(v[q][e + 3])), make_float2(f.z, f.w));
-              v[q][e] = __float_as_uint(x.x); v[q][e + 1] = __float_as_uint(x.y);
-              v[q][e + 2] = __float_as_uint(y.x); v[q][e + 3] = __float_as_uint(y.y);
-            }
-          }
-        }
         if (partial) {
           // the row's visible keys are one range, hence one bit per column; a masked score becomes -inf whatever it was
 #pragma unroll
@@ -1019,10 +932,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
 #pragma unroll
           for (int q = 0; q < 4; ++q) mx[q] = fmax3(mx[q], __uint_as_float(v[q][e]), __uint_as_float(v[q][e + 1]));
         }
-        float top;
-        if (kE4M3) top = fmaxf(fmaxf(fmaf(mx[0], row_scale, ev[0]), fmaf(mx[1], row_scale, ev[1])), fmaxf(fmaf(mx[2], row_scale, ev[2]), fmaf(mx[3], row_scale, ev[3])));
-        else top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
-        const float m_new = fmaxf(m_use, top);
+        const float m_new = fmaxf(m_use, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2);
         // rescale the running sum and the TMEM accumulator only when the maximum moved a lot
         const bool need = j == tb.first ? false : m_new - m_use > kRescaleThreshold;
         if (j == tb.first) m_use = m_new;
@@ -1040,27 +950,20 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
           }
           if (need) m_use = m_new;
         }
-        const float neg_m = (m_use == -INFINITY ? 0.f : -m_use) + (kE4M3 ? kWeightTop : 0.f);
+        const float neg_m = m_use == -INFINITY ? 0.f : -m_use;
         // probabilities; the 16-bit P of keys 64h .. 64h+63 overwrites score columns 64h .. 64h+31, a quarter of the
         // exponentials on the FMA pipe, and the first half is handed over while the second is computed
         float2 sum2 = make_float2(0.f, 0.f);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           uint32_t pk[16];
-          const float mul = kE4M3 ? row_scale : a.scale_log2, add = kE4M3 ? ev[q] + neg_m : neg_m;
-          float2 part = make_float2(0.f, 0.f);
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[q][2 * e]), __uint_as_float(v[q][2 * e + 1])),
-                                        make_float2(mul, mul), make_float2(add, add));
-            const float2 z = !kE4M3 && e % 4 == 3 ? exp2_fma2(y) : make_float2(fast_exp2(y.x), fast_exp2(y.y));
-            if (kE4M3) part = __fadd2_rn(part, z);
-            else sum2 = __fadd2_rn(sum2, z);
-            pk[e] = kE4M3 ? pack_f16(z.x, z.y) : pack_bf16(z.x, z.y);
-          }
-          if (kE4M3) {           // (the weights hold 2^e of the values, their sum must not)
-            const float f = fast_exp2(v_first - ev[q]);
-            sum2 = __ffma2_rn(part, make_float2(f, f), sum2);
+                                        make_float2(a.scale_log2, a.scale_log2), make_float2(neg_m, neg_m));
+            const float2 z = e % 4 == 3 ? exp2_fma2(y) : make_float2(fast_exp2(y.x), fast_exp2(y.y));
+            sum2 = __fadd2_rn(sum2, z);
+            pk[e] = pack_bf16(z.x, z.y);
           }
           tmem_st16(s_addr + (q >> 1) * 64 + (q & 1) * 16, pk);
           if (q == 1) {
@@ -1074,7 +977,6 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         tc_fence_before();
         mbar_arrive(&bar->p_full[t]);
       }
-      it0 += cur.n_blocks;
       // The next piece is looked up while this one's last products run, and its rows of Q are in place before this one's results are
       // stored, so that its first scores are computed meanwhile.
       if (!ok) break;
@@ -1084,15 +986,14 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         ++o_cnt;
       }
       tc_fence_after();
-      if (more && me.tb.first <= me.tb.last) row_scale = store_q();
+      if (more && me.tb.first <= me.tb.last) store_q();
 
       // ---- a row that has nothing else to be joined with leaves finished, others go to the piece's slot
       const bool valid = cur.valid, finished = cur.whole && cur.rank < 0;
       float* slot = w.part + (size_t)cur.slot * slot_floats(D) + t * kTileM * (D + 2);
       const bool here = finished && valid && dbg_in_range(cur.token >= 0 && cur.token < c.n_tokens && cur.head < a.Hq, a.status);
       bf16* dst = here ? a.O + cur.token * a.o_t + (int64_t)cur.head * D : nullptr;
-      const float back = kE4M3 ? fast_exp2(v_first) : 1.f;           // the accumulators lack the exponent of the first values
-      const float inv_l = l > 0.f ? back * (cur.routed != 0 ? 2.f : 1.f) / l : 0.f;      // (finished and routed: no key before the window, a = s)
+      const float inv_l = l > 0.f ? (cur.routed != 0 ? 2.f : 1.f) / l : 0.f;      // (finished and routed: no key before the window, a = s)
       // Four lanes, four rows: each lane stores the same 16 bytes of all four, so that a store covers 64 bytes of a row
       bf16* rows[4];
 #pragma unroll
@@ -1112,8 +1013,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
 #pragma unroll
           for (int x = 0; x < 8; ++x)
             *reinterpret_cast<float4*>(slot + ((q * 8 + x) * kTileM + r) * 4) =
-                make_float4(__uint_as_float(o[4 * x]) * back, __uint_as_float(o[4 * x + 1]) * back, __uint_as_float(o[4 * x + 2]) * back,
-                            __uint_as_float(o[4 * x + 3]) * back);
+                make_float4(__uint_as_float(o[4 * x]), __uint_as_float(o[4 * x + 1]), __uint_as_float(o[4 * x + 2]), __uint_as_float(o[4 * x + 3]));
         }
         if (__any_sync(0xffffffffu, dst != nullptr)) {
           float2 old[16];
@@ -1147,7 +1047,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         }
       }
       if (valid && !finished) {
-        slot[kTileM * D + r] = kE4M3 ? m_use - v_first - kWeightTop : m_use;
+        slot[kTileM * D + r] = m_use;
         slot[kTileM * (D + 1) + r] = any ? l : 0.f;
       }
       tc_fence_before();       // the accumulators have been read; the next piece's products come behind this warp's arrivals
@@ -1300,10 +1200,10 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
 
 // ------------------------------------------------------------------------------------------------------------- host
 // An 8-bit cache is decoded once where a sequence can have kDecodeRows rows of a KV head or more: each 256 of them would decode its keys
-// again.  us decoded in the products' kernel / once: 560 rows of each of eight sequences of 32K (28/4 heads, window 4096, a fifth routed) 204 /
-// 300, 1050 of one 61 / 69, of four of 16K 110 / 130, 2000 of two of 8000 (32/8, window 1000) 111 / 101, 2100 of one of 32K 82 / 85, 4000 of two
-// of 8000 200 / 157.  Not for copies beyond kMostDecoded bytes.
-constexpr int64_t kDecodeRows = 1536, kMostDecoded = 4ll << 30;
+// again.  us decoded in the products' kernel / once (window 4096, a fifth routed): 560 rows of each of eight sequences of 32K (28/4 heads) 246 /
+// 283, 800 of one (32/8) 94 / 97, 1050 of one (28/4) 65 / 67, of four of 16K 120 / 123, of one of 6000 42 / 39, 1200 of four of 4000 (32/8)
+// 127 / 114, 1470 of one of 64K (28/4) 134 / 116, 1532 of four of 16K (32/8) 366 / 269.  Not for copies beyond kMostDecoded bytes.
+constexpr int64_t kDecodeRows = 1024, kMostDecoded = 4ll << 30;
 int decoded_pages(int Lk) { return (Lk + kTileN - 1) / kTileN; }
 int64_t decoded_bytes(int B, int Lk, int Hkv, int D) { return 2ll * B * decoded_pages(Lk) * Hkv * kTileN * D * 2; }
 bool may_decode(int kind, int Lq, int G) { return kind == L2A_CACHE_E4M3 && (int64_t)Lq * G >= kDecodeRows; }

@@ -76,12 +76,7 @@ cudaError_t launch_cache_chunk(const CacheFwdArgs& a, bool first, void* ws, cuda
 // tokens of one head of one page, box_pieces * 64 elements of each (bf16) or the whole row of codes.
 bool encode_pool_map(CUtensorMap* map, const CacheView& c, const void* pool, int box_rows, int box_pieces);
 
-// e4m3 codes as fp16, exactly: two, or the four of a word
-__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t codes) {
-  uint32_t r;
-  asm("{\n .reg .b16 c;\n cvt.u16.u32 c, %1;\n cvt.rn.f16x2.e4m3x2 %0, c;\n}" : "=r"(r) : "r"(codes));
-  return r;
-}
+// The four e4m3 codes of a word as fp16, exactly
 __device__ __forceinline__ void e4m3x4_to_f16(uint32_t codes, uint32_t& lo, uint32_t& hi) {
   asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}"
       : "=r"(lo), "=r"(hi) : "r"(codes));
@@ -91,16 +86,11 @@ __device__ __forceinline__ float2 f16x2_to_float2(uint32_t v) {
   asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, h;\n}" : "=f"(f.x), "=f"(f.y) : "r"(v));
   return f;
 }
-// Two values as the sum of two e4m3 numbers each: the nearest, and the nearest to what it leaves
+// Two values as e4m3, to nearest even
 __device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
   uint16_t r;
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
-}
-__device__ __forceinline__ void two_e4m3_terms(float x, float y, uint32_t& first, uint32_t& second) {
-  first = pack_e4m3(x, y);
-  const float2 f = f16x2_to_float2(e4m3x2_to_f16x2(first));
-  second = pack_e4m3(x - f.x, y - f.y);
 }
 // Copies from one page: K or V rows of a head; untiled for their exponents (16 bytes or a multiple, 16-byte aligned)
 __device__ __forceinline__ void tma_load_page(void* dst, const CUtensorMap* map, uint64_t* bar, bool e4m3, int piece, int row,
@@ -149,9 +139,9 @@ __device__ __forceinline__ void decode_16(const uint4& codes, float scale, uint3
   for (int k = 0; k < 4; ++k) {
     uint32_t l, h;
     e4m3x4_to_f16(w[k], l, h);
-    const float2 lo = f16x2_to_float2(l), hi = f16x2_to_float2(h);
-    o[2 * k] = pack_bf16(lo.x * scale, lo.y * scale);
-    o[2 * k + 1] = pack_bf16(hi.x * scale, hi.y * scale);
+    const float2 both = make_float2(scale, scale), lo = __fmul2_rn(f16x2_to_float2(l), both), hi = __fmul2_rn(f16x2_to_float2(h), both);
+    o[2 * k] = pack_bf16(lo.x, lo.y);
+    o[2 * k + 1] = pack_bf16(hi.x, hi.y);
   }
 }
 
