@@ -993,7 +993,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       float* slot = w.part + (size_t)cur.slot * slot_floats(D) + t * kTileM * (D + 2);
       const bool here = finished && valid && dbg_in_range(cur.token >= 0 && cur.token < c.n_tokens && cur.head < a.Hq, a.status);
       bf16* dst = here ? a.O + cur.token * a.o_t + (int64_t)cur.head * D : nullptr;
-      const float inv_l = l > 0.f ? (cur.routed != 0 ? 2.f : 1.f) / l : 0.f;      // (finished and routed: no key before the window, a = s)
+      const float inv_l = l != 0.f ? (cur.routed != 0 ? 2.f : 1.f) / l : 0.f;      // (finished and routed: no key before the window, a = s)
       // Four lanes, four rows: each lane stores the same 16 bytes of all four, so that a store covers 64 bytes of a row
       bf16* rows[4];
 #pragma unroll
@@ -1158,7 +1158,11 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
 #pragma unroll
       for (int u = 0; u < kAhead; ++u)
         if (ls[u] != 0.f) m_new = fmaxf(m_new, ms[u]);       // (0: no key of that part is visible to the row)
-      if (m_new == -INFINITY) continue;
+      if (m_new == -INFINITY) {                // no key, or scores that are NaN: so is the result then
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) l[s] += ls[u];
+        continue;
+      }
       const float old = fast_exp2(m[s] - m_new);
       l[s] *= old;
 #pragma unroll
@@ -1180,10 +1184,10 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
     }
   }
   const float m_all = fmaxf(m[0], m[1]);
-  const float k0 = l[0] > 0.f ? fast_exp2(m[0] - m_all) : 0.f, k1 = l[1] > 0.f ? fast_exp2(m[1] - m_all) : 0.f;
+  const float k0 = l[0] != 0.f ? fast_exp2(m[0] - m_all) : 0.f, k1 = l[1] != 0.f ? fast_exp2(m[1] - m_all) : 0.f;
   const float l_all = fmaf(k0, l[0], k1 * l[1]);
-  const float g_all = routed && l_all > 0.f ? 1.f / l_all : 0.f;
-  const float w0 = (a.local && l[0] > 0.f ? 1.f / l[0] : 0.f) + g_all * k0, w1 = g_all * k1;
+  const float g_all = routed && l_all != 0.f ? 1.f / l_all : 0.f;
+  const float w0 = (a.local && l[0] != 0.f ? 1.f / l[0] : 0.f) + g_all * k0, w1 = g_all * k1;
   uint2* dst = reinterpret_cast<uint2*>(a.O + t * a.o_t + (int64_t)(head * a.G + h) * D) + piece0;
 #pragma unroll
   for (int k = 0; k < kPieces; ++k) {

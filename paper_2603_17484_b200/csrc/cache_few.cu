@@ -650,12 +650,13 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           float* slot = a.part + (((int64_t)(p.b * c.Hkv + p.g) * a.row_blocks + p.block) * 2 + p.seg + blockIdx.x) * (kRows * kPitch) +
                         r * kPitch;
           *reinterpret_cast<float4*>(slot + c4 * 4) = A;
-          if (c4 == 0) *reinterpret_cast<float2*>(slot + D) = make_float2(M, failed ? -1.f : L);
+          // (a sum of NaN comes with a maximum above all others, so that the combination cannot pass it over)
+          if (c4 == 0) *reinterpret_cast<float2*>(slot + D) = make_float2(isnan(L) ? INFINITY : M, failed ? -1.f : L);
         } else if (!failed) {
           const int t = walk.s.first + (row0 + r) / a.G;
           const bool routed = a.global && a.d != nullptr && a.d[t] != 0;
           if ((a.add && !routed) || !dbg_in_range(t >= 0 && t < c.n_tokens, a.status)) continue;
-          const float k = L > 0.f ? (float)((a.local ? 1 : 0) + (routed ? 1 : 0)) / L : 0.f;
+          const float k = L != 0.f ? (float)((a.local ? 1 : 0) + (routed ? 1 : 0)) / L : 0.f;
           uint2* dst = reinterpret_cast<uint2*>(a.O + t * a.o_t + (int64_t)(p.g * a.G + (row0 + r) % a.G) * D) + c4;
           float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
           if (a.add) {
