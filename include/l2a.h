@@ -463,7 +463,9 @@ l2a_status l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t
  *                    (l2a_workspace_status; after a time-out the rows that need a combination are not stored).  The size follows
  *                    from p, the cache's kind and n_tokens; it is enough for every smaller n_tokens, Lq and Lk (other fields alike).
  *                    It holds partial results; where a sequence can have more than 16 rows (Lq * Hq / Hkv) those of the groups of 256
- *                    rows too, and from 1024 rows on a decoded copy of an 8-bit cache (4 * B * Lk * Hkv * D bytes, 4 GB at most).
+ *                    rows too, and from 1024 rows on a decoded copy of an 8-bit cache (4 * B * Lk * Hkv * D bytes with Lk rounded up to
+ *                    128) where that is 4 GB at most.  The size less the copy (that of a bf16 cache) is taken too: the 8-bit keys are then
+ *                    decoded as they are used, as they are beyond 4 GB; same bits, longer.  Lk decides, so give it no larger than need be.
  *   p->flags       : L2A_FLAG_SKIP_GLOBAL: s only (as d = NULL).  L2A_FLAG_SKIP_LOCAL: o = d * a.  L2A_FLAG_GLOBAL_PHASE: O holds
  *                    s already (from an L2A_FLAG_SKIP_GLOBAL call on another cache, say), and d * a is added for the routed
  *                    rows; others are not touched.  That is the layer whose Global Attention has projections, and so

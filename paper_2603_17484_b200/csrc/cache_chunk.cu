@@ -1210,8 +1210,6 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
 constexpr int64_t kDecodeRows = 1024, kMostDecoded = 4ll << 30;
 int decoded_pages(int Lk) { return (Lk + kTileN - 1) / kTileN; }
 int64_t decoded_bytes(int B, int Lk, int Hkv, int D) { return 2ll * B * decoded_pages(Lk) * Hkv * kTileN * D * 2; }
-bool may_decode(int kind, int Lq, int G) { return kind == L2A_CACHE_E4M3 && (int64_t)Lq * G >= kDecodeRows; }
-
 size_t layout(int B, int n_tokens, int G, int Hkv, int D, uint8_t* base, ChunkWs* w) {
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -1262,30 +1260,32 @@ cudaError_t launch_chunk(const ChunkArgs& p, const CUtensorMap& mapK, const CUte
 
 }  // namespace
 
-size_t cache_chunk_ws_bytes(const l2a_params* p, int kind, int n_tokens) {
-  const int G = p->Hq / p->Hkv;
-  const int64_t copy = may_decode(kind, p->Lq, G) ? std::min(decoded_bytes(p->B, p->Lk, p->Hkv, p->D), kMostDecoded) : 0;
-  return layout(p->B, n_tokens, G, p->Hkv, p->D, nullptr, nullptr) + (size_t)copy;
+size_t cache_chunk_ws_bytes(const l2a_params* p, int n_tokens) {
+  return layout(p->B, n_tokens, p->Hq / p->Hkv, p->Hkv, p->D, nullptr, nullptr);
+}
+
+size_t cache_copy_bytes(const l2a_params* p, int kind) {
+  if (kind != L2A_CACHE_E4M3 || (int64_t)p->Lq * (p->Hq / p->Hkv) < kDecodeRows || p->B > 65535) return 0;
+  const int64_t bytes = decoded_bytes(p->B, p->Lk, p->Hkv, p->D);
+  return bytes <= kMostDecoded ? (size_t)bytes : 0;
 }
 
 bool cache_chunk_counts(const l2a_params* p, int n_tokens) {
   return most_blocks(most_groups(n_tokens, p->Hq / p->Hkv, p->B), p->Hkv, p->Lk) < kMostBlocks;
 }
 
-cudaError_t launch_cache_chunk(const CacheFwdArgs& a, bool first, void* ws, cudaStream_t s) {
+cudaError_t launch_cache_chunk(const CacheFwdArgs& a, bool first, void* ws, bool decode, cudaStream_t s) {
   ChunkArgs p;
   p.f = a;
   p.clear = first;
   p.wide = most_cost(most_groups(a.c.n_tokens, a.G, a.c.B), a.c.Hkv, a.c.max_keys) >= (double)(1u << 31);
   const size_t at = layout(a.c.B, a.c.n_tokens, a.G, a.c.Hkv, a.c.D, static_cast<uint8_t*>(ws), &p.w);
-  const int64_t copy = decoded_bytes(a.c.B, a.c.max_keys, a.c.Hkv, a.c.D);
-  const bool decode = may_decode(a.c.kind, a.c.Lq, a.G) && copy <= kMostDecoded && a.c.B <= 65535;
   p.codes = a.c;
   if (decode) {
     CacheView& c = p.f.c;
     c.kind = L2A_CACHE_BF16;
     c.K = static_cast<uint8_t*>(ws) + at;
-    c.V = c.K + copy / 2;
+    c.V = c.K + decoded_bytes(c.B, c.max_keys, c.Hkv, c.D) / 2;
     c.ks = c.vs = nullptr;
     c.page_bytes = (int64_t)c.Hkv * kTileN * c.D * 2;
     c.page_shift = 7;

@@ -68,9 +68,11 @@ bool cache_few_counts(const l2a_params* p);         // whether it can count the 
 cudaError_t launch_cache_few(const CacheFwdArgs& a, void* ws, cudaStream_t s);
 
 // All others: cache_chunk.cu
-size_t cache_chunk_ws_bytes(const l2a_params* p, int kind, int n_tokens);
+size_t cache_chunk_ws_bytes(const l2a_params* p, int n_tokens);          // plan and parts,
+size_t cache_copy_bytes(const l2a_params* p, int kind);                  // behind them the decoded copy, 0: none is made
 bool cache_chunk_counts(const l2a_params* p, int n_tokens);      // whether it can count the key blocks of such a call
-cudaError_t launch_cache_chunk(const CacheFwdArgs& a, bool first, void* ws, cudaStream_t s);     // first: no kernel of the call ahead
+// first: no kernel of the call ahead; copy: the workspace has room for the decoded copy
+cudaError_t launch_cache_chunk(const CacheFwdArgs& a, bool first, void* ws, bool copy, cudaStream_t s);
 
 // Tensor map over a pool: {elements of 128 bytes at most, tokens, (pieces of a row,) heads, pages}; one copy brings box_rows
 // tokens of one head of one page, box_pieces * 64 elements of each (bf16) or the whole row of codes.

@@ -25,6 +25,11 @@ int few_rows(const l2a_params* p, const l2a_cache* c, int n_tokens) {
   return (blocks - 1.15 * p->B) * pass < 125e6 ? kRowBlocks * kBlockRows : kBlockRows;
 }
 
+// Without the decoded copy of an 8-bit cache, which a smaller workspace does without
+size_t least_ws_bytes(const l2a_params* p, int n_tokens) {
+  return kWsHeaderBytes + (has_few(p) ? cache_few_ws_bytes(p) : 0) + (has_chunks(p) ? cache_chunk_ws_bytes(p, n_tokens) : 0);
+}
+
 int64_t row_stride(const int64_t (&s)[2], int row_elems) {
   if (s[0] != 0 || s[1] < 0) return 0;
   const int64_t t = s[1] ? s[1] : row_elems;
@@ -52,7 +57,7 @@ extern "C" l2a_status l2a_cache_workspace_bytes(const l2a_params* p, const l2a_c
   const l2a_status st = check_forward(p, c, n_tokens, &v);
   if (st != L2A_OK) return st;
   if (!ws_bytes) return L2A_ERR_INVALID_ARG;
-  *ws_bytes = kWsHeaderBytes + (has_few(p) ? cache_few_ws_bytes(p) : 0) + (has_chunks(p) ? cache_chunk_ws_bytes(p, c->kind, n_tokens) : 0);
+  *ws_bytes = least_ws_bytes(p, n_tokens) + cache_copy_bytes(p, c->kind);
   return L2A_OK;
 }
 
@@ -65,9 +70,7 @@ extern "C" l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c,
   a.q_t = row_stride(p->q_stride, p->Hq * p->D);
   a.o_t = row_stride(p->o_stride, p->Hq * p->D);
   if (a.q_t == 0 || a.o_t == 0) return L2A_ERR_INVALID_ARG;
-  size_t need = 0;
-  st = l2a_cache_workspace_bytes(p, c, n_tokens, &need);
-  if (st != L2A_OK) return st;
+  const size_t need = least_ws_bytes(p, n_tokens), copy = cache_copy_bytes(p, c->kind);
   if (!ws || (reinterpret_cast<uintptr_t>(ws) % 256) != 0 || ws_bytes < need) return L2A_ERR_WORKSPACE;
   if (n_tokens == 0) return L2A_OK;
   if (!Q || !O || ((reinterpret_cast<uintptr_t>(Q) | reinterpret_cast<uintptr_t>(O)) & 15)) return L2A_ERR_INVALID_ARG;
@@ -96,6 +99,6 @@ extern "C" l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c,
     else if (few) a.few_rows = 0;
     at += cache_few_ws_bytes(p);
   }
-  if (e == cudaSuccess && chunks) e = launch_cache_chunk(a, first, at, s);
+  if (e == cudaSuccess && chunks) e = launch_cache_chunk(a, first, at, copy > 0 && ws_bytes >= need + copy, s);
   return e == cudaSuccess ? L2A_OK : L2A_ERR_CUDA;
 }
