@@ -138,14 +138,16 @@ def cache(K, V, page_table, lengths, k_scale=None, v_scale=None) -> L2ACache:
         return x.stride(0) if x.shape[0] > 1 else 0
 
     kind = CACHE_BF16 if K.dtype == torch.bfloat16 else CACHE_E4M3
-    if K.dtype != V.dtype or K.element_size() != (2 if kind == CACHE_BF16 else 1):
-        raise ValueError("a cache holds bf16 values or 8-bit codes, K and V alike")
-    if (kind == CACHE_E4M3) != (k_scale is not None and v_scale is not None):
+    if K.dtype not in (torch.bfloat16, torch.float8_e4m3fn, torch.uint8) or K.dtype != V.dtype:
+        raise ValueError("a cache holds bf16 values or e4m3 codes (float8_e4m3fn or uint8), K and V alike")
+    if any((x is not None) != (kind == CACHE_E4M3) for x in (k_scale, v_scale)):
         raise ValueError("8-bit codes need their exponents, bf16 values have none")
     if kind == CACHE_E4M3 and (k_scale.dtype != torch.uint8 or v_scale.dtype != torch.uint8 or k_scale.shape != K.shape[:3]):
         raise ValueError("k_scale, v_scale: uint8 [pages, Hkv, page size]")
-    if page_table.dtype != torch.int32 or lengths.dtype != torch.int32 or page_table.stride(-1) != 1:
+    if page_table.dtype != torch.int32 or lengths.dtype != torch.int32 or page_table.dim() != 2 or lengths.dim() != 1:
         raise ValueError("page_table [B, n] and lengths [B] are int32")
+    if (page_table.stride(1) != 1 and page_table.shape[1] > 1) or (lengths.stride(0) != 1 and lengths.shape[0] > 1):
+        raise ValueError("rows of page_table, and lengths, are dense")
     c = L2ACache(_addr(K), _addr(V), _addr(k_scale), _addr(v_scale), stride(K, V),
                  0 if kind == CACHE_BF16 else stride(k_scale, v_scale), kind, K.shape[0], K.shape[2],
                  page_table.stride(0) if page_table.shape[0] > 1 else page_table.shape[1], _addr(page_table), _addr(lengths))
