@@ -1,7 +1,7 @@
 /*
  * L2A conditional attention layer -- fp64 CPU oracle.  TEST INFRASTRUCTURE ONLY.
  *
- * A plain, slow, obviously-correct restatement of what the layer computes.  It shares no code with
+ * A plain, obviously-correct restatement of what the layer computes.  It shares no code with
  * the CUDA library and must never be called from the product path; only the tests, the smoke check
  * and the benchmark's CPU-baseline leg use it.
  *
@@ -93,15 +93,52 @@ void l2a_oracle_compact(const uint8_t *d, int32_t B, int32_t L, int32_t *q_idx, 
   }
 }
 
+/* The loops over a head's elements, which take nearly all of the time.  Sums over elements may be reordered (fp64 partial sums, as
+ * many as a vector has lanes); the compiler makes a version for each kind of machine and the loader picks one. */
+#if defined(__x86_64__) && defined(__GNUC__) && !defined(__clang__)
+#define VERSIONS __attribute__((target_clones("arch=skylake-avx512", "arch=haswell", "default")))
+#else
+#define VERSIONS
+#endif
+/* sum_e x_e y_e */
+VERSIONS static double dot(const double *x, const in_t *y, int D) {
+  double acc = 0.0;
+#pragma omp simd reduction(+ : acc)
+  for (int e = 0; e < D; ++e) acc += x[e] * LD(y[e]);
+  return acc;
+}
+/* to_e += f y_e */
+VERSIONS static void add_scaled(double *to, double f, const in_t *y, int D) {
+#pragma omp simd
+  for (int e = 0; e < D; ++e) to[e] += f * LD(y[e]);
+}
+/* to_e += f x_e */
+VERSIONS static void add_scaled64(double *to, double f, const double *x, int D) {
+#pragma omp simd
+  for (int e = 0; e < D; ++e) to[e] += f * x[e];
+}
+
 static inline const in_t *q_row(const l2a_oracle_shape *s, const in_t *Q, int b, int t, int h) {
   return Q + (((int64_t)b * s->Lq + t) * s->Hq + h) * s->D;
 }
+/* K and V are read head by head from a copy [B, Hkv, Lk, D] (by_head): key after key lies there without gaps, where the rows of one
+ * head of [B, Lk, Hkv, D] are on a page of memory each at the sizes of the benchmark. */
 static inline const in_t *kv_row(const l2a_oracle_shape *s, const in_t *K, int b, int j, int g) {
-  return K + (((int64_t)b * s->Lk + j) * s->Hkv + g) * s->D;
+  return K + (((int64_t)b * s->Hkv + g) * s->Lk + j) * s->D;
+}
+static in_t *by_head(const l2a_oracle_shape *s, const in_t *K) {
+  const size_t row = sizeof(in_t) * (size_t)s->D;
+  in_t *to = (in_t *)malloc(row * (size_t)s->B * s->Hkv * s->Lk);
+#pragma omp parallel for schedule(static) collapse(2)
+  for (int b = 0; b < s->B; ++b)
+    for (int j = 0; j < s->Lk; ++j)
+      for (int g = 0; g < s->Hkv; ++g)
+        memcpy(to + (((int64_t)b * s->Hkv + g) * s->Lk + j) * s->D, K + (((int64_t)b * s->Lk + j) * s->Hkv + g) * s->D, row);
+  return to;
 }
 
 /* One attention row over keys lo..hi (inclusive) of KV head g:
- * score_j = scale * q.k_j ; lse = log sum exp ; out = sum_j exp(score_j - lse) v_j.
+ * score_j = scale * q.k_j ; lse = log sum exp ; out = sum_j exp(score_j - lse) v_j, the exponentials taken relative to the maximum.
  * p (length hi-lo+1) receives the probabilities when non-NULL. */
 static void attn_row(const l2a_oracle_shape *s, const in_t *q, const in_t *K, const in_t *V,
                      int b, int g, int lo, int hi, double *out, double *lse, double *p) {
@@ -109,24 +146,23 @@ static void attn_row(const l2a_oracle_shape *s, const in_t *q, const in_t *K, co
   const int n = hi - lo + 1;
   double *sc = p ? p : (double *)malloc(sizeof(double) * (size_t)n);
   double m = -INFINITY;
+  double *q64 = (double *)malloc(sizeof(double) * (size_t)D);
+  for (int e = 0; e < D; ++e) q64[e] = LD(q[e]);
   for (int j = lo; j <= hi; ++j) {
-    const in_t *k = kv_row(s, K, b, j, g);
-    double acc = 0.0;
-    for (int e = 0; e < D; ++e) acc += LD(q[e]) * LD(k[e]);
-    acc *= s->scale;
+    const double acc = dot(q64, kv_row(s, K, b, j, g), D) * s->scale;
     sc[j - lo] = acc;
     if (acc > m) m = acc;
   }
   double l = 0.0;
-  for (int j = 0; j < n; ++j) l += exp(sc[j] - m);
+  for (int j = 0; j < n; ++j) l += (sc[j] = exp(sc[j] - m));
   *lse = m + log(l);
   for (int e = 0; e < D; ++e) out[e] = 0.0;
   for (int j = lo; j <= hi; ++j) {
-    const double pj = exp(sc[j - lo] - *lse);
+    const double pj = sc[j - lo] / l;
     sc[j - lo] = pj;
-    const in_t *v = kv_row(s, V, b, j, g);
-    for (int e = 0; e < D; ++e) out[e] += pj * LD(v[e]);
+    add_scaled(out, pj, kv_row(s, V, b, j, g), D);
   }
+  free(q64);
   if (!p) free(sc);
 }
 
@@ -134,10 +170,11 @@ static inline int local_lo(const l2a_oracle_shape *s, int p) { return p - s->win
 
 /* Forward for a list of (b, h, t) rows.  Outputs are [nrows, D] (s, a, o) and [nrows] (lse).
  * For a non-routed row a = 0 and lse_glb = NaN (undefined). */
-void l2a_oracle_forward_rows(const l2a_oracle_shape *s, const in_t *Q, const in_t *K,
-                             const in_t *V, const uint8_t *d, int64_t nrows, const int32_t *rb,
+void l2a_oracle_forward_rows(const l2a_oracle_shape *s, const in_t *Q, const in_t *K_in,
+                             const in_t *V_in, const uint8_t *d, int64_t nrows, const int32_t *rb,
                              const int32_t *rh, const int32_t *rt, double *s_out, double *a_out,
                              double *o_out, double *lse_loc, double *lse_glb) {
+  in_t *K = by_head(s, K_in), *V = by_head(s, V_in);
   const int D = s->D, G = s->Hq / s->Hkv;
 #pragma omp parallel for schedule(dynamic, 4)
   for (int64_t r = 0; r < nrows; ++r) {
@@ -154,6 +191,8 @@ void l2a_oracle_forward_rows(const l2a_oracle_shape *s, const in_t *Q, const in_
     }
     for (int e = 0; e < D; ++e) oo[e] = so[e] + ao[e];
   }
+  free(K);
+  free(V);
 }
 
 /* VJP of one attention row: adds this row's contribution into dq (length D) and, where the
@@ -173,19 +212,15 @@ static void attn_row_bwd(const l2a_oracle_shape *s, const in_t *q, const in_t *K
   for (int j = lo; j <= hi; ++j) {
     const in_t *k = kv_row(s, K, b, j, g);
     const in_t *v = kv_row(s, V, b, j, g);
-    double dp = 0.0;
-    for (int e = 0; e < D; ++e) dp += dout[e] * LD(v[e]);
+    const double dp = dot(dout, v, D);
     const double pj = p[j - lo];
     const double ds = pj * (dp - delta);
-    if (dq)
-      for (int e = 0; e < D; ++e) dq[e] += s->scale * ds * LD(k[e]);
+    if (dq) add_scaled(dq, s->scale * ds, k, D);
     if (dK && (!keep_abs || keep_abs[j])) {
       double *dk = dK + (((int64_t)b * s->Lk + j) * s->Hkv + g) * D;
       double *dv = dV + (((int64_t)b * s->Lk + j) * s->Hkv + g) * D;
-      for (int e = 0; e < D; ++e) {
-        dk[e] += s->scale * ds * LD(q[e]);
-        dv[e] += pj * dout[e];
-      }
+      add_scaled(dk, s->scale * ds, q, D);
+      add_scaled64(dv, pj, dout, D);
     }
   }
   free(p);
@@ -194,9 +229,10 @@ static void attn_row_bwd(const l2a_oracle_shape *s, const in_t *q, const in_t *K
 
 /* Full backward: dQ [B,Lq,Hq,D], dK, dV [B,Lk,Hkv,D] in fp64 (overwritten).  Parallel over
  * (b, KV head) so that no two threads add into the same dK/dV row. */
-void l2a_oracle_backward_full(const l2a_oracle_shape *s, const in_t *Q, const in_t *K,
-                              const in_t *V, const uint8_t *d, const in_t *dO, double *dQ,
+void l2a_oracle_backward_full(const l2a_oracle_shape *s, const in_t *Q, const in_t *K_in,
+                              const in_t *V_in, const uint8_t *d, const in_t *dO, double *dQ,
                               double *dK, double *dV) {
+  in_t *K = by_head(s, K_in), *V = by_head(s, V_in);
   const int D = s->D, G = s->Hq / s->Hkv;
   memset(dQ, 0, sizeof(double) * (size_t)s->B * s->Lq * s->Hq * D);
   memset(dK, 0, sizeof(double) * (size_t)s->B * s->Lk * s->Hkv * D);
@@ -219,12 +255,15 @@ void l2a_oracle_backward_full(const l2a_oracle_shape *s, const in_t *Q, const in
       free(dout);
     }
   }
+  free(K);
+  free(V);
 }
 
 /* dQ for a list of (b, h, t) rows; out [nrows, D]. */
-void l2a_oracle_dq_rows(const l2a_oracle_shape *s, const in_t *Q, const in_t *K, const in_t *V,
+void l2a_oracle_dq_rows(const l2a_oracle_shape *s, const in_t *Q, const in_t *K_in, const in_t *V_in,
                         const uint8_t *d, const in_t *dO, int64_t nrows, const int32_t *rb,
                         const int32_t *rh, const int32_t *rt, double *dq_out) {
+  in_t *K = by_head(s, K_in), *V = by_head(s, V_in);
   const int D = s->D, G = s->Hq / s->Hkv;
 #pragma omp parallel for schedule(dynamic, 4)
   for (int64_t r = 0; r < nrows; ++r) {
@@ -239,13 +278,16 @@ void l2a_oracle_dq_rows(const l2a_oracle_shape *s, const in_t *Q, const in_t *K,
     if (d[(int64_t)b * s->Lq + t]) attn_row_bwd(s, q, K, V, dout, b, g, 0, p, dq, NULL, NULL, NULL);
     free(dout);
   }
+  free(K);
+  free(V);
 }
 
 /* dK, dV for the listed key positions js[0..nj) of one (b, KV head g); out [nj, D] each.
  * Every query row that can see one of those keys is visited, for every query head of the group. */
-void l2a_oracle_dkv_cols(const l2a_oracle_shape *s, const in_t *Q, const in_t *K, const in_t *V,
+void l2a_oracle_dkv_cols(const l2a_oracle_shape *s, const in_t *Q, const in_t *K_in, const in_t *V_in,
                          const uint8_t *d, const in_t *dO, int32_t b, int32_t g, int32_t nj,
                          const int32_t *js, double *dk_out, double *dv_out) {
+  in_t *K = by_head(s, K_in), *V = by_head(s, V_in);
   const int D = s->D, G = s->Hq / s->Hkv;
   uint8_t *keep = (uint8_t *)calloc((size_t)s->Lk, 1);
   int jmin = s->Lk;
@@ -290,14 +332,11 @@ void l2a_oracle_dkv_cols(const l2a_oracle_shape *s, const in_t *Q, const in_t *K
             const int j = js[i];
             if (j < lo || j > pos || slot[j] != i) continue; /* duplicates in js count once */
             const in_t *v = kv_row(s, V, b, j, g);
-            double dp = 0.0;
-            for (int e = 0; e < D; ++e) dp += dout[e] * LD(v[e]);
+            const double dp = dot(dout, v, D);
             const double pj = p[j - lo];
             const double ds = pj * (dp - delta);
-            for (int e = 0; e < D; ++e) {
-              ak[(size_t)i * D + e] += s->scale * ds * LD(q[e]);
-              av[(size_t)i * D + e] += pj * dout[e];
-            }
+            add_scaled(ak + (size_t)i * D, s->scale * ds, q, D);
+            add_scaled64(av + (size_t)i * D, pj, dout, D);
           }
         }
       }
@@ -320,14 +359,17 @@ void l2a_oracle_dkv_cols(const l2a_oracle_shape *s, const in_t *Q, const in_t *K
       }
   }
   free(keep); free(slot); free(acc_k); free(acc_v);
+  free(K);
+  free(V);
 }
 
 /* Straight-through gate gradient by-product (Eq. 7, first term): dgate_t = sum_h dO_{t,h} . a_{t,h}
  * with a the global-attention output of EVERY row (as when global attention is forced for all
  * tokens); rows listed by (b, t); out [nrows]. */
-void l2a_oracle_dgate_rows(const l2a_oracle_shape *s, const in_t *Q, const in_t *K, const in_t *V,
+void l2a_oracle_dgate_rows(const l2a_oracle_shape *s, const in_t *Q, const in_t *K_in, const in_t *V_in,
                            const in_t *dO, int64_t nrows, const int32_t *rb, const int32_t *rt,
                            double *dgate) {
+  in_t *K = by_head(s, K_in), *V = by_head(s, V_in);
   const int D = s->D, G = s->Hq / s->Hkv;
 #pragma omp parallel for schedule(dynamic, 1)
   for (int64_t r = 0; r < nrows; ++r) {
@@ -342,4 +384,6 @@ void l2a_oracle_dgate_rows(const l2a_oracle_shape *s, const in_t *Q, const in_t 
     dgate[r] = acc;
     free(a);
   }
+  free(K);
+  free(V);
 }
