@@ -474,11 +474,15 @@ l2a_status l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t
  * Positions before every window of a sequence whose tokens are not routed are not read, nor are their table entries: a layer without
  * Global Attention may give those pages back.  Slots without a token may hold anything.  Keys and values that some
  * new token of the sequence attends to must be finite for all of them.
- * Scores, soft-max statistics and sums are fp32.  Results are bit-reproducible; how the keys of a row are divided follows from
- * all the call's lengths, so that the same sequence in another batch can differ by fp32 rounding, and by that of the weights to 16
- * bits against another running maximum.  n_tokens * Hq < 2^31 - 32, and where a sequence can have more than 16 rows
- * 2 (n_tokens * Hq / Hkv / 256 + B) * Hkv * (Lk / 128 + 1) < 2^38; Lk * (Hkv + 75) < 2^35 in any case.  n_tokens = 0 is no work.  Errors: L2A_ERR_INVALID_ARG,
- * L2A_ERR_UNSUPPORTED (D, page_size, kind, too many rows or keys), L2A_ERR_WORKSPACE, L2A_ERR_CUDA; a bounded device wait that runs out is
+ * A query row with NaN gives NaN.
+ * Scores, soft-max statistics and sums are fp32; the decoded keys and values are exact.  The weights enter the second product rounded: as
+ * bf16 (8 bits) for sequences of more rows (Lq * Hq / Hkv, see ws), for those of few rows as a pair of bf16 (16 bits) from a bf16 cache, as fp16
+ * from an 8-bit one (11 bits down to 2^-24 of the largest weight times 2^e of the values that the row sees, nothing below 2^-35).  Results are
+ * bit-reproducible; how the keys of a row are divided, and up to 64 rows which of the two ways they take, follows from all the call's
+ * lengths and bounds, so that the same sequence in another batch can differ by such roundings.
+ * Limits: n_tokens * Hq < 2^31 - 32; Lk * (Hkv + 75) < 2^35; where a sequence can have more than 16 rows
+ * 2 (n_tokens * Hq / Hkv / 256 + B) * Hkv * (Lk / 128 + 1) < 2^38.  n_tokens = 0 is no work.  Errors: L2A_ERR_INVALID_ARG,
+ * L2A_ERR_UNSUPPORTED (D, page_size, kind, the limits), L2A_ERR_WORKSPACE, L2A_ERR_CUDA; a bounded device wait that runs out is
  * reported by the status header, not by the return value.
  */
 l2a_status l2a_cache_workspace_bytes(const l2a_params* p, const l2a_cache* c, int n_tokens, size_t* ws_bytes);

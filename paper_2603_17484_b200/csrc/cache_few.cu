@@ -23,12 +23,13 @@
 //                   beside the sum of 2^(s - m) with its own.  fp16 has 11 bits against bf16's 8, but less range: Q is scaled by a
 //                   power of two for each row, w lies at 2^10 .. 2^14 where it counts and is dropped at 2^-38 of that.
 //
-// Measured (captured calls back to back): 16 sequences of 128K keys (32/8 heads, D = 128, four routed) e4m3 196 to 202 us for 1.18 GB = 5.9
-// to 6.0 TB/s, bf16 346 us for 2.35 GB = 6.8 TB/s; 32 ragged ones of up to 8000, a quarter routed, bf16 69 us (394 MB: 5.7 TB/s).  The 8-bit
-// passes take 375 instructions a warp for 16 keys of a head, 176 of them on the integer pipe (48 % of its rate, 47 % of the issue slots; 445
-// with mma.sync of e4m3 operands), and slow down with the clock in a long loop (218 us at 1.83 of 1.965 GHz; 236 in another run).
-// A lone short sequence is latency (9001 keys: 13.3 us, of which this kernel 9.2).  Tried: two chains of products 206 us against 196; the loads of V ahead of the soft-max, no change; pieces and rows
-// of Q handed over by the producer, 14.2 against 13.0 for 9001 keys.
+// Measured (captured calls back to back, milliseconds long): 16 sequences of 128K keys (32/8 heads, D = 128, four routed) e4m3 196 to 202 us for
+// 1.18 GB = 5.9 to 6.0 TB/s, bf16 346 us for 2.35 GB = 6.8 TB/s; 32 ragged ones of up to 8000, a quarter routed, bf16 69 us (394 MB: 5.7 TB/s).
+// The 8-bit passes take 355 instructions a warp for 16 keys of a head, 176 of them on the integer pipe (48 % of its rate, 44 % of the issue
+// slots; 445 with mma.sync of e4m3 operands), and slow down with the clock in a long loop (218 us at 1.83 of 1.965 GHz; 230 to 236 in others).
+// A lone short sequence is latency (9001 keys: 13.3 us, of which this kernel 9.2; the dense l2a_decode, which knows its lengths on the host,
+// takes 7.6 in 16 bits): lists, lengths and decisions are read by every CTA ahead of its first copy.  Tried: two chains of products 206 us
+// against 196; the loads of V ahead of the soft-max, no change; pieces and rows of Q handed over by the producer, 14.2 against 13.0 for 9001 keys.
 #include <math.h>
 
 #include <algorithm>
