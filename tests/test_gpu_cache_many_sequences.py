@@ -62,3 +62,28 @@ def test_tiles_of_the_bounds_pass_32_bits(kind, new):
     torch.cuda.synchronize()
     assert l2a.l2a_workspace_status(ws) == 0
     check(O, *attention(c, Q, new, d, W), f"{kind} bounds of 2^26 tokens")
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "bf16"])
+def test_units_of_work_of_the_bounds_pass_32_bits(kind):
+    """32 sequences of 8 heads, each of at most 2^26 tokens, a chunk of each: the sums of the plan are 64 bits wide, the result that of
+    the call with close bounds."""
+    B, Hq, Hkv, D, W, Lk, new = 32, 32, 8, 64, 40, 1 << 26, 20
+    c = Cache(kind, 128, Hkv, D, [new + b % 90 * 7 for b in range(B)], 7)
+    N = B * new
+    Q = torch.randn((N, Hq, D), generator=torch.Generator().manual_seed(5)).bfloat16().cuda()
+    d = routed(N, 0.5, 1)
+    table = torch.full((B, Lk // 128), -1, dtype=torch.int32, device="cuda")
+    table[:, :c.table.shape[1]] = c.table
+    far = l2a.cache(c.poolK, c.poolV, table, c.length, k_scale=c.ks, v_scale=c.vs)
+    out = []
+    for handle, keys in ((c.handle, max(c.lengths)), (far, Lk)):
+        p = l2a.params(B, new, keys, Hq, Hkv, D, W)
+        ws = torch.empty(l2a.l2a_cache_workspace_bytes(p, handle, N), dtype=torch.uint8, device="cuda")
+        O = torch.full_like(Q, float("nan"))
+        l2a.l2a_cache_forward(p, handle, Q, None, N, d, O, ws)
+        torch.cuda.synchronize()
+        assert l2a.l2a_workspace_status(ws) == 0
+        out.append(O)
+    check(out[0], *attention(c, Q, [new] * B, d, W), kind)
+    assert torch.equal(out[0], out[1])
