@@ -401,13 +401,23 @@ l2a_status l2a_decode(const l2a_params* p, const void* q, const void* K, const v
  */
 #define L2A_CACHE_BF16 0
 #define L2A_CACHE_E4M3 1
+/*
+ * L2A_CACHE_E2M1: a row of D values is held as D e2m1 codes (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives), two a byte, the even
+ * element in the low half; an e4m3 scale s for each block of 16 of them; and one exponent e, the least whole number with max|x| <= 6 * 448 * 2^e
+ * (e >= -126; 0 for a row of zeros).  s = max|x| of the block / 6 / 2^e rounded to e4m3, code_i = x_i / (s 2^e) rounded to e2m1, both to
+ * nearest even (at most 448 and 6; code 0, with x_i's sign, where s is 0).  It stands for code_i * s * 2^e, exact in bf16.  D / 2 + D / 16 + 1
+ * bytes for D values.  A block with a value that is not finite stands for NaN throughout (its other values count for max|x|).
+ * A page's scales lie head by head: the exponents of its tokens, [page_size], then their blocks' scales, [page_size][D / 16].
+ */
+#define L2A_CACHE_E2M1 3
 
 typedef struct l2a_cache {
-  void *K, *V;               /* pools [n_pages, Hkv, page_size, D] of bf16 or e4m3, 16-byte aligned               */
-  uint8_t *k_scale, *v_scale; /* E4M3: [n_pages, Hkv, page_size] exponents e + 127, 16-byte aligned; BF16: NULL     */
+  void *K, *V;               /* pools [n_pages, Hkv, page_size, D] of bf16, e4m3 or e2m1, 16-byte aligned         */
+  uint8_t *k_scale, *v_scale; /* E4M3: [n_pages, Hkv, page_size] exponents e + 127, 16-byte aligned; BF16: NULL;    */
+                             /* E2M1: [n_pages, Hkv, page_size * (1 + D / 16)], exponents + 127, then block scales */
   int64_t page_stride;       /* elements from a page of K (of V) to the next; 0 = Hkv * page_size * D; multiple of   */
                              /* 16 bytes.  K and V may lie in one allocation, page by page                           */
-  int64_t scale_stride;      /* the same for k_scale and v_scale; 0 = Hkv * page_size; multiple of 16                */
+  int64_t scale_stride;      /* the same for k_scale and v_scale, in bytes; 0 = dense; multiple of 16                */
   int32_t kind;              /* L2A_CACHE_*                                                                       */
   int32_t n_pages;
   int32_t page_size;         /* tokens of a page: 16, 32, 64 or 128                                               */

@@ -12,24 +12,25 @@ l2a_status cache_view(const l2a_params* p, const l2a_cache* c, const int32_t* cu
   if (p->Hq % p->Hkv != 0 || p->window < 0 || p->seq_bounds != nullptr) return L2A_ERR_INVALID_ARG;
   if (!(p->softmax_scale >= 0.f) || isinf(p->softmax_scale)) return L2A_ERR_INVALID_ARG;
   if (p->D != 64 && p->D != 128) return L2A_ERR_UNSUPPORTED;
-  if (c->kind != L2A_CACHE_BF16 && c->kind != L2A_CACHE_E4M3) return L2A_ERR_UNSUPPORTED;
+  if (c->kind != L2A_CACHE_BF16 && c->kind != L2A_CACHE_E4M3 && c->kind != L2A_CACHE_E2M1) return L2A_ERR_UNSUPPORTED;
   if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128) return L2A_ERR_UNSUPPORTED;
   if (c->n_pages <= 0 || c->table_stride <= 0 || (int64_t)c->table_stride * c->page_size < p->Lk) return L2A_ERR_INVALID_ARG;
   if (!c->K || !c->V || !c->page_table || !c->lengths) return L2A_ERR_INVALID_ARG;
-  const bool e4m3 = c->kind == L2A_CACHE_E4M3;
-  const int64_t elem = e4m3 ? 1 : 2, page = (int64_t)p->Hkv * c->page_size * p->D, scales = (int64_t)p->Hkv * c->page_size;
+  const bool coded = c->kind != L2A_CACHE_BF16;
+  const int64_t rows = (int64_t)p->Hkv * c->page_size, page = rows * p->D, scales = rows * (coded ? scale_bytes(c->kind, p->D) : 1);
   const int64_t ps = c->page_stride ? c->page_stride : page, ss = c->scale_stride ? c->scale_stride : scales;
-  if (ps < page || ps * elem % 16 != 0 || ss < scales || ss % 16 != 0) return L2A_ERR_INVALID_ARG;
-  uintptr_t bits = reinterpret_cast<uintptr_t>(c->K) | reinterpret_cast<uintptr_t>(c->V);
-  if (e4m3) {
+  const int64_t bits = c->kind == L2A_CACHE_BF16 ? 16 : c->kind == L2A_CACHE_E4M3 ? 8 : 4;
+  if (ps < page || ps > INT64_MAX / 16 || ps * bits % 128 != 0 || ss < scales || ss % 16 != 0) return L2A_ERR_INVALID_ARG;
+  uintptr_t address = reinterpret_cast<uintptr_t>(c->K) | reinterpret_cast<uintptr_t>(c->V);
+  if (coded) {
     if (!c->k_scale || !c->v_scale) return L2A_ERR_INVALID_ARG;
-    bits |= reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale);
+    address |= reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale);
   }
-  if (bits & 15) return L2A_ERR_INVALID_ARG;
+  if (address & 15) return L2A_ERR_INVALID_ARG;
   if (!cu_new && (int64_t)p->B * p->Lq != n_tokens) return L2A_ERR_INVALID_ARG;
   v->K = static_cast<uint8_t*>(c->K); v->V = static_cast<uint8_t*>(c->V);
   v->ks = c->k_scale; v->vs = c->v_scale;
-  v->page_bytes = ps * elem;
+  v->page_bytes = ps * bits / 8;
   v->scale_stride = ss;
   v->kind = c->kind;
   v->n_pages = c->n_pages;
@@ -45,11 +46,12 @@ l2a_status cache_view(const l2a_params* p, const l2a_cache* c, const int32_t* cu
 bool encode_pool_map(CUtensorMap* map, const CacheView& c, const void* pool, int box_rows, int box_pieces) {
   const cuuint64_t page = 1ull << c.page_shift, D = c.D, pages = c.n_pages, stride = c.page_bytes;
   const cuuint32_t rows = box_rows;
-  if (c.kind == L2A_CACHE_E4M3) {
-    const cuuint64_t dims[4] = {D, page, (cuuint64_t)c.Hkv, pages}, strides[3] = {D, page * D, stride};
-    const cuuint32_t box[4] = {(cuuint32_t)c.D, rows, 1, 1};
+  if (c.kind != L2A_CACHE_BF16) {
+    const cuuint64_t row = row_bytes(c.kind, c.D);
+    const cuuint64_t dims[4] = {row, page, (cuuint64_t)c.Hkv, pages}, strides[3] = {row, page * row, stride};
+    const cuuint32_t box[4] = {(cuuint32_t)row, rows, 1, 1};
     return encode_tiled_map(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, pool, dims, strides, box,
-                            c.D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+                            row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B);
   }
   const cuuint64_t dims[5] = {64, page, D / 64, (cuuint64_t)c.Hkv, pages}, strides[4] = {2 * D, 128, 2 * page * D, stride};
   const cuuint32_t box[5] = {64, rows, (cuuint32_t)box_pieces, 1, 1};
@@ -79,6 +81,15 @@ __device__ __forceinline__ uint32_t exponent_for(uint32_t amax) {
   const int e = (int)(amax >> 7) - 8 + ((amax & 0x7fu) > 0x60u ? 1 : 0);
   return amax == 0 ? 127u : (uint32_t)max(e, 1);
 }
+// The same for 6 * 448 * 2^e = 1.3125 * 2^(11 + e)
+__device__ __forceinline__ uint32_t exponent_for_e2m1(uint32_t amax) {
+  const int e = (int)(amax >> 7) - 11 + ((amax & 0x7fu) > 0x28u ? 1 : 0);
+  return amax == 0 ? 127u : (uint32_t)max(e, 1);
+}
+// y / s for the rounding to e2m1, r = 1 / s: exact where the quotient is half-way between two of them.  y has 8 significant bits, s times
+// a point half-way 7 at most, so that a quotient is such a point or 2^-8 of it away: with 16 bits kept the errors of r and of
+// the product are gone, and nothing else gets to such a point.
+__device__ __forceinline__ float quotient_e2m1(float x) { return __uint_as_float((__float_as_uint(x) + 0x80u) & ~0xffu); }
 // The two magnitudes of a bf16 pair, 0 for those that are not finite
 __device__ __forceinline__ uint32_t finite_magnitudes(uint32_t x) {
   x &= 0x7fff7fffu;
@@ -90,9 +101,10 @@ __device__ __forceinline__ uint32_t finite_magnitudes(uint32_t x) {
 // first rows are on their way.  What bounds it then is the instructions of the conversion: 18380 tokens (8 heads, D = 128, e4m3) take
 // 24.8 us (113 MB: 4.6 TB/s), with 16-byte loads, products one by one and indices by division 30.6.
 constexpr int kAppendAhead = 4;
-template <int D, bool kE4M3, int kTokens>
+template <int D, int kKind, int kTokens>
 __global__ void __launch_bounds__(kRowsThreads) cache_append_kernel(const AppendArgs a) {
   constexpr int kLanes = D / 16, kRows = 32 / kLanes, kGroups = kTokens / kRows, kWarps = kRowsThreads / 32;
+  constexpr bool kE4M3 = kKind == L2A_CACHE_E4M3, kE2M1 = kKind == L2A_CACHE_E2M1;
   const CacheView& c = a.c;
   __shared__ int to_page[kTokens], to_slot[kTokens];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % kLanes;
@@ -152,21 +164,50 @@ __global__ void __launch_bounds__(kRowsThreads) cache_append_kernel(const Append
       const bool value = done_hv & 1;
       const int row = done_group * kRows + lane / kLanes, page = to_page[row];
       const int64_t slot = ((int64_t)(done_hv >> 1) << c.page_shift) + to_slot[row];
-      uint8_t* dst = (value ? c.V : c.K) + page * c.page_bytes + slot * (kE4M3 ? D : 2 * D);
+      uint8_t* dst = (value ? c.V : c.K) + page * c.page_bytes + slot * row_bytes(kKind, D);
+      uint8_t* scales = (value ? c.vs : c.ks) + page * c.scale_stride;
+      const int head = done_hv >> 1;
       next(done_hv, done_group);
-      if (kE4M3) {
-        uint32_t m = 0;
+      uint32_t m = 0, e = 0, own = 0;
+      bool finite = true;
+      if (kE4M3 || kE2M1) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) m = __vmaxu2(m, w[i][k] & 0x7fff7fffu);
-        if (__any_sync(0xffffffffu, (m & 0xffffu) >= 0x7f80u || m >= 0x7f800000u)) {      // values that are not finite do not count
+        finite = (m & 0xffffu) < 0x7f80u && m < 0x7f800000u;
+        if (__any_sync(0xffffffffu, !finite)) {      // values that are not finite do not count
           m = 0;
 #pragma unroll
           for (int k = 0; k < 8; ++k) m = __vmaxu2(m, finite_magnitudes(w[i][k]));
         }
-        m = max(m & 0xffffu, m >> 16);
+        own = m = max(m & 0xffffu, m >> 16);
 #pragma unroll
         for (int o = kLanes / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-        const uint32_t e = exponent_for(m);
+        e = kE4M3 ? exponent_for(m) : exponent_for_e2m1(m);
+      }
+      if (kE2M1) {
+        // A lane has a block: its scale, and what is left over that
+        const float f = __uint_as_float((254u - e) << 23);
+        const uint32_t scale = finite ? pack_e4m3(__fdiv_rn(__uint_as_float(own << 16) * f, 6.f), 0.f) : 0x7fu;
+        const float s = e4m3_value(scale), r = s > 0.f ? __frcp_rn(s) : 0.f;
+        uint32_t code[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float2 x[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t u = w[i][4 * k + j];
+            x[j] = __fmul2_rn(make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)), make_float2(f, f));
+            x[j] = __fmul2_rn(x[j], make_float2(r, r));
+            x[j] = make_float2(quotient_e2m1(x[j].x), quotient_e2m1(x[j].y));
+          }
+          code[k] = finite ? pack_e2m1(x) : 0u;
+        }
+        if (page >= 0) {
+          *reinterpret_cast<uint2*>(dst + sub * 8) = make_uint2(code[0], code[1]);
+          scales[blocks_at<D>(c, head, to_slot[row]) + sub] = (uint8_t)scale;
+          if (sub == 0) scales[exponent_at<D, kKind>(c, head, to_slot[row])] = (uint8_t)e;
+        }
+      } else if (kE4M3) {
         const float f = __uint_as_float((254u - e) << 23);         // 2^-e; e + 127 is 1 .. 247
         const float2 inv = make_float2(f, f);
         uint32_t code[4];
@@ -179,7 +220,7 @@ __global__ void __launch_bounds__(kRowsThreads) cache_append_kernel(const Append
         }
         if (page >= 0) {
           *reinterpret_cast<uint4*>(dst + sub * 16) = make_uint4(code[0], code[1], code[2], code[3]);
-          if (sub == 0) (value ? c.vs : c.ks)[page * c.scale_stride + slot] = (uint8_t)e;
+          if (sub == 0) scales[slot] = (uint8_t)e;
         }
       } else if (page >= 0) {
         store_32(dst + sub * 32, a.wide_pool, w[i]);
@@ -198,9 +239,10 @@ struct ReadArgs {
 
 // The same shape for the way back: a lane brings 16 values of a position, a warp 512 / D positions of a head at a time.  HBM-bound: 1.34 GB
 // (eight sequences, 127K tokens of 262K rows, 8 heads, D = 128, e4m3) in 196 us = 6.8 TB/s, with 16-byte accesses 251.
-template <int D, bool kE4M3, int kSteps>
+template <int D, int kKind, int kSteps>
 __global__ void __launch_bounds__(kRowsThreads) cache_read_kernel(const ReadArgs a) {
   constexpr int kLanes = D / 16, kRows = 32 / kLanes, kTokens = kRows * kSteps;
+  constexpr bool kE4M3 = kKind == L2A_CACHE_E4M3, kE2M1 = kKind == L2A_CACHE_E2M1;
   const CacheView& c = a.c;
   const int lane = threadIdx.x & 31, b = blockIdx.y, sub = lane % kLanes;
   const int64_t item = ((int64_t)blockIdx.x * kRowsThreads + threadIdx.x) >> 5;
@@ -209,23 +251,31 @@ __global__ void __launch_bounds__(kRowsThreads) cache_read_kernel(const ReadArgs
   const int64_t t0 = item / heads * kTokens + lane / kLanes;
   if (item / heads * kTokens >= c.max_keys) return;
   const int start = a.first ? a.first[b] : 0, length = cache_length(c, b);
-  uint32_t x[kSteps][8];         // (e4m3: the first four)
-  uint32_t e[kSteps];
+  uint32_t x[kSteps][8];         // (e4m3: the first four, e2m1: two)
+  uint32_t e[kSteps], t[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int64_t pos = start + t0 + i * kRows;
 #pragma unroll
     for (int k = 0; k < 8; ++k) x[i][k] = 0u;
     e[i] = 127;
+    t[i] = 0;
     if (pos < 0 || pos >= length) continue;
     const int page = cache_page(c, b, (int)pos);
     if (page < 0) continue;
     const int64_t slot = ((int64_t)h << c.page_shift) + (pos & ((1 << c.page_shift) - 1));
-    const uint8_t* src = (value ? c.V : c.K) + page * c.page_bytes + slot * (kE4M3 ? D : 2 * D);
-    if (kE4M3) {
+    const uint8_t* src = (value ? c.V : c.K) + page * c.page_bytes + slot * row_bytes(kKind, D);
+    const uint8_t* scales = (value ? c.vs : c.ks) + page * c.scale_stride;
+    if (kE2M1) {
+      const uint2 y = *reinterpret_cast<const uint2*>(src + sub * 8);
+      x[i][0] = y.x; x[i][1] = y.y;
+      const int in_page = (int)(pos & ((1 << c.page_shift) - 1));
+      e[i] = scales[exponent_at<D, kKind>(c, h, in_page)];
+      t[i] = scales[blocks_at<D>(c, h, in_page) + sub];
+    } else if (kE4M3) {
       const uint4 y = *reinterpret_cast<const uint4*>(src + sub * 16);
       x[i][0] = y.x; x[i][1] = y.y; x[i][2] = y.z; x[i][3] = y.w;
-      e[i] = (value ? c.vs : c.ks)[page * c.scale_stride + slot];
+      e[i] = scales[slot];
     } else {
       load_32(src + sub * 32, a.wide_pool, x[i]);
     }
@@ -234,34 +284,51 @@ __global__ void __launch_bounds__(kRowsThreads) cache_read_kernel(const ReadArgs
   bf16* out = (value ? a.V : a.K) + b * st.b + h * D + sub * 16;
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
-    const int64_t t = t0 + i * kRows;
-    if (t >= c.max_keys) continue;
-    if (kE4M3) {
+    const int64_t row = t0 + i * kRows;
+    if (row >= c.max_keys) continue;
+    if (kE2M1) {
+      uint32_t o[8];
+      decode_16(make_uint2(x[i][0], x[i][1]), e4m3_value(t[i]) * scale_of_exponent(e[i]), o);
+      store_32(out + row * st.t, a.wide, o);
+    } else if (kE4M3) {
       uint32_t o[8];
       decode_16(make_uint4(x[i][0], x[i][1], x[i][2], x[i][3]), scale_of_exponent(e[i]), o);
-      store_32(out + t * st.t, a.wide, o);
+      store_32(out + row * st.t, a.wide, o);
     } else {
-      store_32(out + t * st.t, a.wide, x[i]);
+      store_32(out + row * st.t, a.wide, x[i]);
     }
   }
 }
 
-template <int D, bool kE4M3>
+template <int D, int kKind>
 cudaError_t launch_append(const AppendArgs& a, cudaStream_t s) {
   // 16 tokens a CTA, or as many as a warp takes at once up to two waves of CTAs of the former an SM (8 heads, D = 128, e4m3: 32 tokens 5.7 /
   // 3.1 us, 2000 6.1 / 4.6, 4000 7.8 / 7.6, 8000 13.9 / 15.7)
   constexpr int kFew = 512 / D;
-  if (a.c.n_tokens < 2 * 16 * kSplitSms) cache_append_kernel<D, kE4M3, kFew><<<ceil_div(a.c.n_tokens, kFew), kRowsThreads, 0, s>>>(a);
-  else cache_append_kernel<D, kE4M3, 16><<<ceil_div(a.c.n_tokens, 16), kRowsThreads, 0, s>>>(a);
+  if (a.c.n_tokens < 2 * 16 * kSplitSms) cache_append_kernel<D, kKind, kFew><<<ceil_div(a.c.n_tokens, kFew), kRowsThreads, 0, s>>>(a);
+  else cache_append_kernel<D, kKind, 16><<<ceil_div(a.c.n_tokens, 16), kRowsThreads, 0, s>>>(a);
   return cudaGetLastError();
 }
-template <int D, bool kE4M3>
+template <int D, int kKind>
 cudaError_t launch_read(const ReadArgs& a, cudaStream_t s) {
   constexpr int kSteps = 2, kTokens = 512 / D * kSteps;
   const int64_t warps = ((int64_t)a.c.max_keys + kTokens - 1) / kTokens * 2 * a.c.Hkv;
   const dim3 grid((unsigned)((warps * 32 + kRowsThreads - 1) / kRowsThreads), a.c.B);
-  cache_read_kernel<D, kE4M3, kSteps><<<grid, kRowsThreads, 0, s>>>(a);
+  cache_read_kernel<D, kKind, kSteps><<<grid, kRowsThreads, 0, s>>>(a);
   return cudaGetLastError();
+}
+
+template <int D>
+cudaError_t launch_append_kind(const AppendArgs& a, cudaStream_t s) {
+  return a.c.kind == L2A_CACHE_BF16   ? launch_append<D, L2A_CACHE_BF16>(a, s)
+         : a.c.kind == L2A_CACHE_E4M3 ? launch_append<D, L2A_CACHE_E4M3>(a, s)
+                                      : launch_append<D, L2A_CACHE_E2M1>(a, s);
+}
+template <int D>
+cudaError_t launch_read_kind(const ReadArgs& a, cudaStream_t s) {
+  return a.c.kind == L2A_CACHE_BF16   ? launch_read<D, L2A_CACHE_BF16>(a, s)
+         : a.c.kind == L2A_CACHE_E4M3 ? launch_read<D, L2A_CACHE_E4M3>(a, s)
+                                      : launch_read<D, L2A_CACHE_E2M1>(a, s);
 }
 
 // Whether rows of two tensors (of elem bytes, any number of elements of the strides apart) all start at multiples of 32 bytes
@@ -289,9 +356,7 @@ extern "C" l2a_status l2a_cache_append(const l2a_params* p, const l2a_cache* c, 
   a.wide = all_wide(K, V, 2, a.k_t, a.v_t);
   a.wide_pool = all_wide(c->K, c->V, 1, a.c.page_bytes, 0);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const bool e4m3 = c->kind == L2A_CACHE_E4M3;
-  const cudaError_t e = p->D == 128 ? (e4m3 ? launch_append<128, true>(a, s) : launch_append<128, false>(a, s))
-                                    : (e4m3 ? launch_append<64, true>(a, s) : launch_append<64, false>(a, s));
+  const cudaError_t e = p->D == 128 ? launch_append_kind<128>(a, s) : launch_append_kind<64>(a, s);
   return e == cudaSuccess ? L2A_OK : L2A_ERR_CUDA;
 }
 
@@ -313,8 +378,6 @@ extern "C" l2a_status l2a_cache_read(const l2a_params* p, const l2a_cache* c, co
   a.wide = all_wide(K_out, V_out, 2, a.k_st.b, a.k_st.t, a.v_st.b, a.v_st.t);
   a.wide_pool = all_wide(c->K, c->V, 1, a.c.page_bytes, 0);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const bool e4m3 = c->kind == L2A_CACHE_E4M3;
-  const cudaError_t e = p->D == 128 ? (e4m3 ? launch_read<128, true>(a, s) : launch_read<128, false>(a, s))
-                                    : (e4m3 ? launch_read<64, true>(a, s) : launch_read<64, false>(a, s));
+  const cudaError_t e = p->D == 128 ? launch_read_kind<128>(a, s) : launch_read_kind<64>(a, s);
   return e == cudaSuccess ? L2A_OK : L2A_ERR_CUDA;
 }

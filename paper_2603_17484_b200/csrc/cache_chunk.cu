@@ -334,8 +334,9 @@ __device__ void make_plan(const ChunkArgs& p, PlanSmem& sm) {
 // Decoded copy: pages of 128 tokens, [page][KV head][128][D] of K and of V.  A lane brings 16 codes, a warp 512 / D keys at a time, 32
 // keys of a head of K or V in all.  HBM-bound: 3 bytes a code, of the keys that some row sees.
 constexpr int kDecodeKeys = 32, kDecodeParts = kTileN / kDecodeKeys;
-template <int D>
+template <int D, int kKind>
 __device__ __forceinline__ void decode_cache(const ChunkArgs& p, int item, int b) {
+  constexpr bool kE2M1 = kKind == L2A_CACHE_E2M1;
   constexpr int kLanes = D / 16, kRows = 32 / kLanes, kSteps = kDecodeKeys / kRows;
   const CacheFwdArgs& a = p.f;
   const CacheView &c = p.codes, &out = a.c;
@@ -347,15 +348,26 @@ __device__ __forceinline__ void decode_cache(const ChunkArgs& p, int item, int b
   const int key0 = block * kTileN + part * kDecodeKeys, window = max(0, length - n - a.window);
   const bool may_route = a.global && a.d != nullptr, inside = key0 < length && (may_route || key0 + kDecodeKeys > window);
   const uint8_t *src = value ? c.V : c.K, *exps = value ? c.vs : c.ks;
-  uint4 x[kSteps];
-  uint32_t e[kSteps];
+  uint4 x[kSteps];                 // (e2m1: half of it)
+  uint32_t e[kSteps], t[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int key = key0 + i * kRows + lane / kLanes;
     const int page = inside && key < length && (may_route || key >= window) ? cache_page(c, b, key) : -1;
-    const int64_t slot = ((int64_t)head << c.page_shift) + (key & ((1 << c.page_shift) - 1));
-    x[i] = page >= 0 ? *reinterpret_cast<const uint4*>(src + page * c.page_bytes + slot * D + sub * 16) : make_uint4(0, 0, 0, 0);
-    e[i] = page >= 0 ? exps[page * c.scale_stride + slot] : 0u;
+    const int in_page = key & ((1 << c.page_shift) - 1);
+    const int64_t slot = ((int64_t)head << c.page_shift) + in_page;
+    const uint8_t* row = src + page * c.page_bytes + slot * row_bytes(kKind, D);
+    x[i] = make_uint4(0, 0, 0, 0);
+    e[i] = t[i] = 0u;
+    if (page < 0) continue;
+    e[i] = exps[page * c.scale_stride + exponent_at<D, kKind>(c, head, in_page)];
+    if (kE2M1) {
+      const uint2 y = *reinterpret_cast<const uint2*>(row + sub * 8);
+      x[i].x = y.x; x[i].y = y.y;
+      t[i] = exps[page * c.scale_stride + blocks_at<D>(c, head, in_page) + sub];
+    } else {
+      x[i] = *reinterpret_cast<const uint4*>(row + sub * 16);
+    }
   }
   // all keys where a token is routed, else those of the windows (looked up while the codes are on their way)
   bool routed = false;
@@ -368,14 +380,15 @@ __device__ __forceinline__ void decode_cache(const ChunkArgs& p, int item, int b
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     uint32_t o[8];
-    decode_16(x[i], scale_of_exponent(e[i]), o);
+    if (kE2M1) decode_16(make_uint2(x[i].x, x[i].y), e4m3_value(t[i]) * scale_of_exponent(e[i]), o);
+    else decode_16(x[i], scale_of_exponent(e[i]), o);
     store_32(dst + (i * kRows + lane / kLanes) * (2 * D) + sub * 32, true, o);
   }
 }
 
 // The first CTA plans; the others, a row of the grid for each sequence, decode: 213 MB in 42 us (35K tokens, 8 heads, D = 128), two CTAs of
 // half the registers an SM 48.
-template <int D>
+template <int D, int kKind>
 __global__ void __launch_bounds__(kPlanThreads) cache_prepare_kernel(const ChunkArgs p) {
   dependency_wait();
   dependents_release();
@@ -387,7 +400,7 @@ __global__ void __launch_bounds__(kPlanThreads) cache_prepare_kernel(const Chunk
     else make_plan<int>(p, sm);
     return;
   }
-  decode_cache<D>(p, (blockIdx.x - 1) * (kPlanThreads / 32) + (threadIdx.x >> 5), blockIdx.y);
+  decode_cache<D, kKind>(p, (blockIdx.x - 1) * (kPlanThreads / 32) + (threadIdx.x >> 5), blockIdx.y);
 }
 
 // ------------------------------------------------------------------------------------------------------------- pieces
@@ -459,24 +472,26 @@ __device__ __forceinline__ TileBlocks tile_blocks(const Group& g, const ChunkPie
 }
 
 constexpr int kBarBytes = 512;
-template <int D, bool kE4M3>
+template <int D, int kKind>
 struct ChunkSmem {
   static constexpr int kQTileBytes = kTileM * D * 2;
   static constexpr int kKTileBytes = kTileN * D * 2;
   static constexpr int kVTileBytes = kTileN * D * 2;
   // Codes land where their bf16 tile will be: with D = 128 on its second 64 columns, a key's 128 codes on the same 128 bytes that its
-  // values take there, so that a thread finds its row and leaves it without the others.  Rows of 64 codes do not fit that way.
-  static constexpr int kCodes = kTileN * D;
-  static constexpr bool kApart = kE4M3 && D == 64;
+  // values take there, so that a thread finds its row and leaves it without the others.  Rows of 64 codes do not fit that way.  e2m1: the rows,
+  // behind them the scales of their blocks and their exponents; they are read by all threads before the first writes.
+  static constexpr int kCodes = kTileN * row_bytes(kKind, D);
+  static constexpr int kBlocks = kTileN * (D / 16);
+  static constexpr bool kApart = kKind == L2A_CACHE_E4M3 && D == 64;
   static constexpr int kKOff = 2 * kQTileBytes;
   static constexpr int kVOff = kKOff + kKStages * kKTileBytes;
   static constexpr int kRawOff = kVOff + kVStages * kVTileBytes;
   static constexpr int kBarOff = kRawOff + (kApart ? (kKStages + kVStages) * kCodes : 0);
   static __device__ __forceinline__ uint8_t* k_codes(uint8_t* smem, int s) {
-    return kApart ? smem + kRawOff + s * kCodes : smem + kKOff + s * kKTileBytes + kBoxBytes;
+    return kApart ? smem + kRawOff + s * kCodes : smem + kKOff + s * kKTileBytes + (D == 128 ? kBoxBytes : 0);
   }
   static __device__ __forceinline__ uint8_t* v_codes(uint8_t* smem, int s) {
-    return kApart ? smem + kRawOff + (kKStages + s) * kCodes : smem + kVOff + s * kVTileBytes + kBoxBytes;
+    return kApart ? smem + kRawOff + (kKStages + s) * kCodes : smem + kVOff + s * kVTileBytes + (D == 128 ? kBoxBytes : 0);
   }
   static constexpr int kGroupOff = kBarOff + kBarBytes;
   static constexpr int kTotal = kGroupOff + kKeepGroups * (int)sizeof(Group) + 1024 /* alignment slack */;
@@ -507,10 +522,11 @@ struct RowOf {
   uint8_t routed;                // and the routing decision; looked up here, needed at the piece's end
 };
 
-template <int D, bool kE4M3>
+template <int D, int kKind>
 __global__ void __launch_bounds__(kChunkThreads, 1)
 cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV, const ChunkArgs p) {
-  using SM = ChunkSmem<D, kE4M3>;
+  using SM = ChunkSmem<D, kKind>;
+  constexpr bool kCoded = kKind != L2A_CACHE_BF16, kE2M1 = kKind == L2A_CACHE_E2M1;
   constexpr int kKSteps = D / 16;      // MMA k-steps of Q*K^T
   constexpr int kOCol0 = 2 * kTileN;   // first TMEM column of the O accumulators
   const CacheFwdArgs& a = p.f;
@@ -537,7 +553,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     }
     for (int s = 0; s < kKStages; ++s) {
       mbar_init(&bar->k_raw[s], 1);
-      mbar_init(&bar->k_full[s], kE4M3 ? kConvWarps * 32 : 1);
+      mbar_init(&bar->k_full[s], kCoded ? kConvWarps * 32 : 1);
       mbar_init(&bar->k_empty[s], 1);
     }
     for (int s = 0; s < kVStages; ++s) {
@@ -584,8 +600,9 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
     bool ok = walk.init(w, sGroups);
     // a lane copies the rows of page `u` of a block, in bf16 64 columns of them
     const int rows = 1 << c.page_shift, copies = 128 >> c.page_shift, u = lane % copies, piece = lane / copies;
-    const bool active = piece < (kE4M3 ? 1 : D / 64);
-    const uint32_t bytes = rows * (kE4M3 ? D : 128);
+    // (e2m1: the codes, the scales of their blocks, the exponents)
+    const bool active = piece < (kE2M1 ? 3 : kCoded ? 1 : D / 64);
+    const uint32_t bytes = rows * (kE2M1 ? (piece == 0 ? D / 2 : piece == 1 ? D / 16 : 1) : kCoded ? D : 128);
     uint32_t k_slot = 0, k_ph = 1, v_cnt = 0;
     while (ok && walk.next(w, c.Hkv, pc)) {
       const Group& g = walk.group_now(w);
@@ -593,7 +610,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       const int first_entry = key_lo >> c.page_shift, last_entry = key_hi >> c.page_shift;
       int entry0 = -512, page_ids = -1;
       // pages of block j, 32 of them at a time (a block of V lies `step` blocks behind that of K)
-      auto copy = [&](int j, uint8_t* dst, const CUtensorMap* map, uint64_t* full) {
+      auto copy = [&](int j, uint8_t* dst, const CUtensorMap* map, const uint8_t* scales, uint64_t* full) {
         const int key = j * kTileN + u * rows, entry = key >> c.page_shift;
         if (((j * kTileN) >> c.page_shift) < entry0 || ((j * kTileN + kTileN - 1) >> c.page_shift) - entry0 >= 32) {
           entry0 = (max(j - step, 0) * kTileN) >> c.page_shift;
@@ -602,30 +619,36 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
         }
         const int page = __shfl_sync(0xffffffffu, page_ids, entry - entry0);
         const bool load = active && page >= 0 && key <= key_hi && key + rows > key_lo;
-        const uint32_t expect = __popc(__ballot_sync(0xffffffffu, load)) * bytes;
+        const uint32_t expect = kE2M1 ? __reduce_add_sync(0xffffffffu, load ? bytes : 0u) : __popc(__ballot_sync(0xffffffffu, load)) * bytes;
         if (lane == 0) mbar_expect_tx(full, expect);
         __syncwarp();
-        if (load)
-          tma_load_page(dst + (kE4M3 ? u * rows * D : piece * kBoxBytes + u * rows * 128), map, full, kE4M3, piece, 0, pc.head, page);
+        if (!load) return;
+        if (kE2M1 && piece > 0) {
+          const uint8_t* src = scales + page * c.scale_stride + (piece == 1 ? blocks_at<D>(c, pc.head, 0) : exponent_at<D, kKind>(c, pc.head, 0));
+          bulk_load(dst + SM::kCodes + (piece == 1 ? u * rows * (D / 16) : SM::kBlocks + u * rows), src, bytes, full);
+        } else {
+          tma_load_page(dst + (kCoded ? u * rows * row_bytes(kKind, D) : piece * kBoxBytes + u * rows * 128), map, full, kCoded, piece, 0,
+                        pc.head, page);
+        }
       };
       auto copy_v = [&](int j) -> bool {
         const int s = v_cnt & 1;
         if (!mbar_wait_warp(&bar->v_empty[s], ((v_cnt >> 1) & 1) ^ 1, abort_flag)) return false;
-        copy(j, kE4M3 ? SM::v_codes(smem, s) : sV + s * SM::kVTileBytes, &mapV, &bar->v_raw[s]);
+        copy(j, kCoded ? SM::v_codes(smem, s) : sV + s * SM::kVTileBytes, &mapV, c.vs, &bar->v_raw[s]);
         ++v_cnt;
         return true;
       };
       auto copy_k = [&](int j) -> bool {
         if (!mbar_wait_warp(&bar->k_empty[k_slot], k_ph, abort_flag)) return false;
-        copy(j, kE4M3 ? SM::k_codes(smem, k_slot) : sK + k_slot * SM::kKTileBytes, &mapK, kE4M3 ? &bar->k_raw[k_slot] : &bar->k_full[k_slot]);
+        copy(j, kCoded ? SM::k_codes(smem, k_slot) : sK + k_slot * SM::kKTileBytes, &mapK, c.ks, kCoded ? &bar->k_raw[k_slot] : &bar->k_full[k_slot]);
         if (++k_slot == kKStages) { k_slot = 0; k_ph ^= 1; }
         return true;
       };
       // In the order in which the products take them.  e4m3: in that of the decoding, which has K done while V is on its way.
       for (int j = pc.j0 - step; ok && j <= pc.j1; ++j) {
-        if (!kE4M3 && j >= pc.j0) ok = copy_v(j);
+        if (!kCoded && j >= pc.j0) ok = copy_v(j);
         if (ok && j + step <= pc.j1) ok = copy_k(j + step);
-        if (kE4M3 && ok && j >= pc.j0) ok = copy_v(j);
+        if (kCoded && ok && j >= pc.j0) ok = copy_v(j);
       }
     }
   } else if (warp == kMmaWarp) {
@@ -742,7 +765,7 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
       const Group& g = walk.group_now(w);
       const int b = g.b, key_lo = g.key_lo, key_hi = g.key_hi, step = g.dual ? 2 : 1;
       auto seen = [&](int j) { return j * kTileN + row >= key_lo && j * kTileN + row <= key_hi; };
-      if (!kE4M3) {
+      if (!kCoded) {
         for (int j = pc.j0; ok && j <= pc.j1; ++j, ++it) {
           const int s = it & 1;
           if (!mbar_wait_warp(&bar->v_raw[s], (it >> 1) & 1, abort_flag)) { ok = false; break; }
@@ -753,6 +776,62 @@ cache_chunk_kernel(const __grid_constant__ CUtensorMap mapK, const __grid_consta
             fence_async_smem();
           }
           mbar_arrive(&bar->v_full[s]);
+        }
+        continue;
+      }
+      if (kE2M1) {
+        // this thread's row of a block of codes, times its blocks' scales and 2^e, to its tile
+        auto decode = [&](const uint8_t* codes, uint8_t* tile, uint64_t* raw, uint32_t ph, uint64_t* full, bool zero) -> bool {
+          constexpr int kPieces = D / 32;                      // of 32 codes
+          const bool here = mbar_wait_warp(raw, ph, abort_flag);
+          const uint32_t src = smem_u32(codes), dst = smem_u32(tile) + row * 128;
+          uint4 x[kPieces];
+          uint32_t t[2] = {}, e = 0;
+          if (here) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+              const float4 y = lds128(src + row * (D / 2) + ((D == 128 ? i ^ ((row >> 1) & 3) : i ^ ((row >> 2) & 1)) << 4));
+              x[i] = zero ? make_uint4(0u, 0u, 0u, 0u)
+                          : make_uint4(__float_as_uint(y.x), __float_as_uint(y.y), __float_as_uint(y.z), __float_as_uint(y.w));
+            }
+            const uint8_t* scales = codes + SM::kCodes;
+            if (!zero) {
+              t[0] = *reinterpret_cast<const volatile uint32_t*>(scales + row * (D / 16));
+              if (D == 128) t[1] = *reinterpret_cast<const volatile uint32_t*>(scales + row * (D / 16) + 4);
+              e = *reinterpret_cast<const volatile uint8_t*>(scales + SM::kBlocks + row);
+            }
+          }
+          // (all leave together where a wait ran out)
+          if (!named_barrier_all(2, kConvWarps * 32, here)) return false;
+          const float scale = scale_of_exponent(e);
+#pragma unroll
+          for (int i = 0; i < kPieces; ++i) {
+            uint32_t lo, hi;
+            e4m3x4_to_f16(t[i / 2] >> (i % 2) * 16 & 0xffffu, lo, hi);
+            const float2 f = f16x2_to_float2(lo);
+            const uint32_t at = dst + i / 2 * kBoxBytes;
+            uint32_t o[8];
+            decode_16(make_uint2(x[i].x, x[i].y), f.x * scale, o);
+            sts128(at + ((((i & 1) * 4) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
+            sts128(at + ((((i & 1) * 4 + 1) ^ (row & 7)) << 4), o[4], o[5], o[6], o[7]);
+            decode_16(make_uint2(x[i].z, x[i].w), f.y * scale, o);
+            sts128(at + ((((i & 1) * 4 + 2) ^ (row & 7)) << 4), o[0], o[1], o[2], o[3]);
+            sts128(at + ((((i & 1) * 4 + 3) ^ (row & 7)) << 4), o[4], o[5], o[6], o[7]);
+          }
+          fence_async_smem();
+          mbar_arrive(full);
+          return true;
+        };
+        for (int j = pc.j0 - step; ok && j <= pc.j1; ++j) {
+          if (j + step <= pc.j1) {
+            ok = decode(SM::k_codes(smem, k_slot), sK + k_slot * SM::kKTileBytes, &bar->k_raw[k_slot], k_ph, &bar->k_full[k_slot], false);
+            if (++k_slot == kKStages) { k_slot = 0; k_ph ^= 1; }
+          }
+          if (ok && j >= pc.j0) {
+            const int s = it & 1;
+            ok = decode(SM::v_codes(smem, s), sV + s * SM::kVTileBytes, &bar->v_raw[s], (it >> 1) & 1, &bar->v_full[s], !seen(j));
+            ++it;
+          }
         }
         continue;
       }
@@ -1232,21 +1311,21 @@ size_t layout(int B, int n_tokens, int G, int Hkv, int D, uint8_t* base, ChunkWs
   return at;
 }
 
-template <int D>
+template <int D, int kKind>
 cudaError_t launch_prepare(const ChunkArgs& p, bool decode, bool first, cudaStream_t s) {
   const unsigned items = decode ? (unsigned)(p.f.c.table_stride * p.f.c.Hkv * 2 * kDecodeParts) : 0, per = kPlanThreads / 32;
-  return launch_dependent(cache_prepare_kernel<D>, dim3(1 + (items + per - 1) / per, decode ? p.f.c.B : 1), kPlanThreads, 0, s, !first, p);
+  return launch_dependent(cache_prepare_kernel<D, kKind>, dim3(1 + (items + per - 1) / per, decode ? p.f.c.B : 1), kPlanThreads, 0, s, !first, p);
 }
 
-template <int D, bool kE4M3>
+template <int D, int kKind>
 cudaError_t launch_chunk(const ChunkArgs& p, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t s) {
-  constexpr int smem = ChunkSmem<D, kE4M3>::kTotal;
+  constexpr int smem = ChunkSmem<D, kKind>::kTotal;
   static PerDeviceOnce once;
   cudaError_t e = once.run([] {
-    return cudaFuncSetAttribute(cache_chunk_kernel<D, kE4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    return cudaFuncSetAttribute(cache_chunk_kernel<D, kKind>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   });
   if (e != cudaSuccess) return e;
-  e = launch_dependent(cache_chunk_kernel<D, kE4M3>, dim3(kCtas), kChunkThreads, smem, s, true, mapK, mapV, p);
+  e = launch_dependent(cache_chunk_kernel<D, kKind>, dim3(kCtas), kChunkThreads, smem, s, true, mapK, mapV, p);
   if (e != cudaSuccess) return e;
   // Few rows have many parts each: their columns over several CTAs, and more parts in flight.  Many rows have two or three parts, and
   // registers are CTAs that an SM has room for.  Whole call, four parts in flight / two: 2000 tokens on 34K keys (32/8 heads) 363 / 353 us, 290
@@ -1258,6 +1337,16 @@ cudaError_t launch_chunk(const ChunkArgs& p, const CUtensorMap& mapK, const CUte
   return launch_dependent(cache_join_kernel<D, D / 32, 2>, dim3(rows, heads), 256, 0, s, true, p);
 }
 
+template <int D>
+cudaError_t launch_both(const ChunkArgs& p, const CUtensorMap& mapK, const CUtensorMap& mapV, bool decode, bool first, cudaStream_t s) {
+  const cudaError_t e = p.codes.kind == L2A_CACHE_E2M1 ? launch_prepare<D, L2A_CACHE_E2M1>(p, decode, first, s)
+                                                       : launch_prepare<D, L2A_CACHE_E4M3>(p, decode, first, s);
+  if (e != cudaSuccess) return e;
+  return p.f.c.kind == L2A_CACHE_BF16   ? launch_chunk<D, L2A_CACHE_BF16>(p, mapK, mapV, s)
+         : p.f.c.kind == L2A_CACHE_E4M3 ? launch_chunk<D, L2A_CACHE_E4M3>(p, mapK, mapV, s)
+                                        : launch_chunk<D, L2A_CACHE_E2M1>(p, mapK, mapV, s);
+}
+
 }  // namespace
 
 size_t cache_chunk_ws_bytes(const l2a_params* p, int n_tokens) {
@@ -1265,7 +1354,7 @@ size_t cache_chunk_ws_bytes(const l2a_params* p, int n_tokens) {
 }
 
 size_t cache_copy_bytes(const l2a_params* p, int kind) {
-  if (kind != L2A_CACHE_E4M3 || (int64_t)p->Lq * (p->Hq / p->Hkv) < kDecodeRows || p->B > 65535) return 0;
+  if (kind == L2A_CACHE_BF16 || (int64_t)p->Lq * (p->Hq / p->Hkv) < kDecodeRows || p->B > 65535) return 0;
   const int64_t bytes = decoded_bytes(p->B, p->Lk, p->Hkv, p->D);
   return bytes <= kMostDecoded ? (size_t)bytes : 0;
 }
@@ -1294,14 +1383,10 @@ cudaError_t launch_cache_chunk(const CacheFwdArgs& a, bool first, void* ws, bool
     c.n_pages = c.B * c.table_stride;
   }
   const CacheView& c = p.f.c;
-  const bool e4m3 = c.kind == L2A_CACHE_E4M3;
   CUtensorMap mapK, mapV;
   const int rows = 1 << c.page_shift;
   if (!encode_pool_map(&mapK, c, c.K, rows, 1) || !encode_pool_map(&mapV, c, c.V, rows, 1)) return cudaErrorUnknown;
-  const cudaError_t e = c.D == 128 ? launch_prepare<128>(p, decode, first, s) : launch_prepare<64>(p, decode, first, s);
-  if (e != cudaSuccess) return e;
-  if (c.D == 128) return e4m3 ? launch_chunk<128, true>(p, mapK, mapV, s) : launch_chunk<128, false>(p, mapK, mapV, s);
-  return e4m3 ? launch_chunk<64, true>(p, mapK, mapV, s) : launch_chunk<64, false>(p, mapK, mapV, s);
+  return c.D == 128 ? launch_both<128>(p, mapK, mapV, decode, first, s) : launch_both<64>(p, mapK, mapV, decode, first, s);
 }
 
 }  // namespace l2a

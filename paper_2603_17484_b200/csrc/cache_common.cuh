@@ -8,7 +8,7 @@ namespace l2a {
 
 struct CacheView {
   uint8_t *K, *V;              // pools, as bytes
-  uint8_t *ks, *vs;            // exponents + 127 (E4M3)
+  uint8_t *ks, *vs;            // E4M3, E2M1: of a page and head the exponents + 127, [page]; E2M1: behind them block scales, [page][D / 16]
   int64_t page_bytes, scale_stride;
   int kind, n_pages, page_shift, table_stride;
   int max_keys;                // positions that the table and p->Lk allow
@@ -16,6 +16,19 @@ struct CacheView {
   const int32_t* cu_new;       // NULL: every sequence has Lq new tokens
   int B, Lq, Hkv, D, n_tokens;
 };
+
+// Bytes of a row of codes or values, and of the scales of a row
+__host__ __device__ constexpr int row_bytes(int kind, int D) { return kind == L2A_CACHE_BF16 ? 2 * D : kind == L2A_CACHE_E4M3 ? D : D / 2; }
+__host__ __device__ constexpr int scale_bytes(int kind, int D) { return kind == L2A_CACHE_BF16 ? 0 : kind == L2A_CACHE_E4M3 ? 1 : 1 + D / 16; }
+// Offsets, inside a page's scales, of the exponent of a token of a head and of the scales of its blocks (E2M1)
+template <int D, int kKind>
+__device__ __forceinline__ int64_t exponent_at(const CacheView& c, int head, int in_page) {
+  return (((int64_t)head * scale_bytes(kKind, D)) << c.page_shift) + in_page;
+}
+template <int D>
+__device__ __forceinline__ int64_t blocks_at(const CacheView& c, int head, int in_page) {
+  return ((((int64_t)head * scale_bytes(L2A_CACHE_E2M1, D)) + 1) << c.page_shift) + in_page * (D / 16);
+}
 
 // Host side: checks a cache call's parameters and fills the view.
 l2a_status cache_view(const l2a_params* p, const l2a_cache* c, const int32_t* cu_new, int n_tokens, CacheView* v);
@@ -75,7 +88,7 @@ bool cache_chunk_counts(const l2a_params* p, int n_tokens);      // whether it c
 cudaError_t launch_cache_chunk(const CacheFwdArgs& a, bool first, void* ws, bool copy, cudaStream_t s);
 
 // Tensor map over a pool: {elements of 128 bytes at most, tokens, (pieces of a row,) heads, pages}; one copy brings box_rows
-// tokens of one head of one page, box_pieces * 64 elements of each (bf16) or the whole row of codes.
+// tokens of one head of one page, box_pieces * 64 elements of each (bf16) or the whole row of codes (swizzled over the row's bytes).
 bool encode_pool_map(CUtensorMap* map, const CacheView& c, const void* pool, int box_rows, int box_pieces);
 
 // The four e4m3 codes of a word as fp16, exactly
@@ -94,10 +107,30 @@ __device__ __forceinline__ uint32_t pack_e4m3(float lo, float hi) {
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
+// e2m1 codes, two a byte, the even element in the low half.  Those of a word as fp16, exactly
+__device__ __forceinline__ void e2m1x8_to_f16(uint32_t codes, uint32_t (&h)[4]) {
+  asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n"
+      " cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(codes));
+}
+// Eight values as e2m1, to nearest even, at most 6
+__device__ __forceinline__ uint32_t pack_e2m1(const float2 (&x)[4]) {
+  uint32_t r;
+  asm("{\n .reg .b8 a, b, c, d;\n cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+      " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n mov.b32 %0, {a, b, c, d};\n}"
+      : "=r"(r) : "f"(x[0].x), "f"(x[0].y), "f"(x[1].x), "f"(x[1].y), "f"(x[2].x), "f"(x[2].y), "f"(x[3].x), "f"(x[3].y));
+  return r;
+}
+// An e4m3 byte's value
+__device__ __forceinline__ float e4m3_value(uint32_t byte) {
+  uint32_t lo, hi;
+  e4m3x4_to_f16(byte, lo, hi);
+  return f16x2_to_float2(lo).x;
+}
 // Copies from one page: K or V rows of a head; untiled for their exponents (16 bytes or a multiple, 16-byte aligned)
-__device__ __forceinline__ void tma_load_page(void* dst, const CUtensorMap* map, uint64_t* bar, bool e4m3, int piece, int row,
+__device__ __forceinline__ void tma_load_page(void* dst, const CUtensorMap* map, uint64_t* bar, bool codes, int piece, int row,
                                               int head, int page) {
-  if (e4m3) {
+  if (codes) {
     asm volatile(
         "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
         ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(0), "r"(row), "r"(head), "r"(page) : "memory");
@@ -144,6 +177,21 @@ __device__ __forceinline__ void decode_16(const uint4& codes, float scale, uint3
     const float2 both = make_float2(scale, scale), lo = __fmul2_rn(f16x2_to_float2(l), both), hi = __fmul2_rn(f16x2_to_float2(h), both);
     o[2 * k] = pack_bf16(lo.x, lo.y);
     o[2 * k + 1] = pack_bf16(hi.x, hi.y);
+  }
+}
+// 16 e2m1 codes times the scale of their block, 2^e in it, as bf16 (the same)
+__device__ __forceinline__ void decode_16(const uint2& codes, float scale, uint32_t (&o)[8]) {
+  const uint32_t w[2] = {codes.x, codes.y};
+  const float2 both = make_float2(scale, scale);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    uint32_t h[4];
+    e2m1x8_to_f16(w[k], h);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 x = __fmul2_rn(f16x2_to_float2(h[i]), both);
+      o[4 * k + i] = pack_bf16(x.x, x.y);
+    }
   }
 }
 

@@ -112,17 +112,30 @@ __device__ __forceinline__ uint32_t lds32(uint32_t saddr) {
   asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(saddr));
   return v;
 }
+__device__ __forceinline__ void lds64(uint32_t saddr, uint32_t& x, uint32_t& y) {
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(saddr));
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t saddr) {
+  uint16_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=h"(v) : "r"(saddr));
+  return v;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 __device__ __forceinline__ uint32_t lds16(uint32_t saddr) {
   uint16_t v;
   asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(saddr));
   return v;
 }
 
-template <int D, bool kE4M3>
+template <int D, int kKind>
 struct FewSmem {
-  static constexpr int kTileBytes = kTile * D * (kE4M3 ? 1 : 2);
+  static constexpr int kTileBytes = kTile * row_bytes(kKind, D);
   static constexpr int kStageBytes = 2 * kTileBytes;                       // K, then V
-  static constexpr int kScaleBytes = kE4M3 ? 2 * kTile : 0;                // exponents of K, then of V
+  static constexpr int kScaleBytes = 2 * kTile * scale_bytes(kKind, D);    // exponents of K, then of V; e2m1: scales of the blocks of K, then of V
   static __host__ __device__ constexpr int red_bytes(int rows) { return kComputeWarps * rows * (D + 4) * 4; }
   static __host__ __device__ constexpr int total(int stages, int rows) {
     return stages * (kStageBytes + kScaleBytes) + red_bytes(rows) + (int)sizeof(FewBars);
@@ -175,13 +188,14 @@ __device__ __forceinline__ bool next_piece(const CacheFwdArgs& a, Walk& w, Piece
 }
 
 // kHigh: more than eight rows.
-template <int D, bool kE4M3, bool kHigh>
+template <int D, int kKind, bool kHigh>
 __global__ void __launch_bounds__(kThreads, 2)
 cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
                  const int stages) {
-  using SM = FewSmem<D, kE4M3>;
+  using SM = FewSmem<D, kKind>;
   constexpr int kRows = kHigh ? 16 : 8, kHalves = kHigh ? 2 : 1;
-  constexpr int kCols = D / 8;                   // e4m3: columns of V of a lane's group, and column tiles
+  constexpr bool kCoded = kKind != L2A_CACHE_BF16, kE2M1 = kKind == L2A_CACHE_E2M1;
+  constexpr int kCols = D / 8;                   // codes: columns of V of a lane's group, and column tiles
   const CacheView& c = a.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   dependents_release();
@@ -268,7 +282,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
     // ================================================================= producer
     // lane -> what it copies of a tile: page `u` of K, V, their exponents
     const int what = lane / copies, u = lane % copies;
-    const uint32_t bytes = what < 2 ? rows * D * (kE4M3 ? 1 : 2) : what < (kE4M3 ? 4 : 2) ? rows : 0;
+    const uint32_t bytes = what < 2 ? rows * row_bytes(kKind, D) : what < (kCoded ? 4 : 2) ? rows : kE2M1 && what < 6 ? rows * (D / 16) : 0;
     int s = 0, ph = 1;
     Piece p;
     while (ok && next_piece(a, walk, p)) {
@@ -292,11 +306,13 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           const int in_page = key & ((1 << c.page_shift) - 1);
           if (what < 2) {
             tma_load_page(smem + s * SM::kStageBytes + what * SM::kTileBytes + u * (SM::kTileBytes / copies), what ? &mapV : &mapK,
-                          &bar->full[s], kE4M3, 0, in_page, p.g, page);
+                          &bar->full[s], kCoded, 0, in_page, p.g, page);
+          } else if (kE2M1 && what >= 4) {
+            bulk_load(scales + s * SM::kScaleBytes + 2 * kTile + ((what - 4) * kTile + u * rows) * (D / 16),
+                      (what == 4 ? c.ks : c.vs) + page * c.scale_stride + blocks_at<D>(c, p.g, in_page), bytes, &bar->full[s]);
           } else {
             bulk_load(scales + s * SM::kScaleBytes + (what - 2) * kTile + u * rows,
-                      (what == 2 ? c.ks : c.vs) + page * c.scale_stride + ((int64_t)p.g << c.page_shift) + in_page, rows,
-                      &bar->full[s]);
+                      (what == 2 ? c.ks : c.vs) + page * c.scale_stride + exponent_at<D, kKind>(c, p.g, in_page), rows, &bar->full[s]);
           }
         }
         if (++s == stages) { s = 0; ph ^= 1; }
@@ -350,8 +366,8 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
         constexpr int kLast = kHalves - 1;
         const int y = x < kLast ? x : kLast;
         const bf16* qrow = a.q + token[y] * a.q_t + (int64_t)head[y] * D;
-        if (kE4M3) {
-          // a lane's elements: those of the 16-byte pieces of a key's codes that it loads (below)
+        if (kCoded) {
+          // a lane's elements: those of a key's codes that it loads (below)
           constexpr int kPieces = D / 64;
           uint32_t v[kPieces][8];
           uint32_t top = 0;
@@ -401,13 +417,36 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           // ---- S = Q K^T for two times eight keys; this lane's are key0 + 2 t4 + {0, 1, 8, 9}
           float sc[2][4] = {};
           uint32_t ev[2] = {};
-          if (kE4M3) {
+          const uint32_t tScale = smem_u32(scales) + s * SM::kScaleBytes;
+          if (kCoded) {
             constexpr int kPieces = D / 64;
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               const int row = r0 + x * 8 + hr;
+              if (kE2M1) {
+                // a quarter of a key's codes, D / 64 blocks of them, each with its scale (the product has 6 bits at most: exact)
+                uint32_t w[2 * kPieces];
+                if (D == 128) {
+                  const float4 y = lds128(tK + row * 64 + ((t4 ^ ((row >> 1) & 3)) << 4));
+                  w[0] = __float_as_uint(y.x); w[1] = __float_as_uint(y.y);
+                  w[2 * kPieces - 2] = __float_as_uint(y.z); w[2 * kPieces - 1] = __float_as_uint(y.w);
+                } else {
+                  lds64(tK + row * 32 + (((t4 >> 1) ^ ((row >> 2) & 1)) << 4) + (t4 & 1) * 8, w[0], w[1]);
+                }
+                const uint32_t at = tScale + 2 * kTile + row * (D / 16) + t4 * kPieces;
+                uint32_t both, none;
+                e4m3x4_to_f16(D == 128 ? lds16(at) : lds8(at), both, none);
 #pragma unroll
-              for (int i = 0; i < kPieces; ++i) {
+                for (int i = 0; i < 2 * kPieces; ++i) {
+                  const uint32_t f = __byte_perm(both, both, i < 2 ? 0x1010 : 0x3232);
+                  uint32_t h[4];
+                  e2m1x8_to_f16(w[i], h);
+                  mma_16816<true>(sc[x], qa[2 * i], mul_f16x2(h[0], f), mul_f16x2(h[1], f));
+                  mma_16816<true>(sc[x], qa[2 * i + 1], mul_f16x2(h[2], f), mul_f16x2(h[3], f));
+                }
+              }
+#pragma unroll
+              for (int i = 0; i < (kE2M1 ? 0 : kPieces); ++i) {
                 const int piece = t4 * kPieces + i;
                 const float4 y = lds128(tK + row * D + ((D == 128 ? piece ^ (row & 7) : piece ^ ((row >> 1) & 3)) << 4));
                 const uint32_t w[4] = {__float_as_uint(y.x), __float_as_uint(y.y), __float_as_uint(y.z), __float_as_uint(y.w)};
@@ -418,7 +457,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
                   mma_16816<true>(sc[x], qa[i * 4 + k], lo, hi);
                 }
               }
-              const uint32_t at = smem_u32(scales) + s * SM::kScaleBytes + r0 + x * 8 + 2 * t4;
+              const uint32_t at = tScale + r0 + x * 8 + 2 * t4;
               const uint32_t ek = lds16(at);
               ev[x] = lds16(at + kTile);
               const float f0 = scale_of_exponent(ek & 0xffu), f1 = scale_of_exponent(ek >> 8);
@@ -436,18 +475,21 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
               mma_16816<false>(sc[1], qa[k], kb[2], kb[3]);
             }
           }
-          // e4m3: a lane's share of the codes of one of its four keys' values (key0 + 2 t4 + {0, 1, 8, 9})
-          constexpr int kWords = kCols / 4;
+          // codes: a lane's share of those of one of its four keys' values (key0 + 2 t4 + {0, 1, 8, 9})
+          constexpr int kWords = kE2M1 ? kCols / 8 : kCols / 4;
           auto value_codes = [&](int y, uint32_t (&w)[kWords]) {
             const int row = r0 + 2 * t4 + (y & 1) + (y >> 1) * 8;
-            if (D == 128) {
+            if (kE2M1) {
+              if (D == 128) lds64(tV + row * 64 + (((hr >> 1) ^ ((row >> 1) & 3)) << 4) + (hr & 1) * 8, w[0], w[kWords - 1]);
+              else w[0] = lds32(tV + row * 32 + (((hr >> 2) ^ ((row >> 2) & 1)) << 4) + (hr & 3) * 4);
+            } else if (D == 128) {
               const float4 z = lds128(tV + row * 128 + ((hr ^ (row & 7)) << 4));
-              w[0] = __float_as_uint(z.x); w[1] = __float_as_uint(z.y);
-              w[kWords - 2] = __float_as_uint(z.z); w[kWords - 1] = __float_as_uint(z.w);
+              w[0] = __float_as_uint(z.x); w[kWords > 1 ? 1 : 0] = __float_as_uint(z.y);
+              w[kWords > 1 ? kWords - 2 : 0] = __float_as_uint(z.z); w[kWords - 1] = __float_as_uint(z.w);
             } else {
               const uint32_t at = tV + row * 64 + (((hr >> 1) ^ ((row >> 1) & 3)) << 4) + (hr & 1) * 8;
               w[0] = lds32(at);
-              w[1] = lds32(at + 4);
+              w[kWords - 1] = lds32(at + 4);
             }
           };
           // ---- weights: u is what they are two to the power of, relative to the reference
@@ -469,7 +511,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
                 if (j < row_lo[x] || j > row_hi[x]) v[y] = -INFINITY;
               }
             }
-            if (kE4M3) {
+            if (kCoded) {
               const float m_new = fmaxf(m[x], row_max(v)), base = m_new == -INFINITY ? 0.f : m_new;
               l[x] = l[x] * fast_exp2(m[x] - base) + ((fast_exp2(v[0] - base) + fast_exp2(v[1] - base)) +
                                                        (fast_exp2(v[2] - base) + fast_exp2(v[3] - base)));
@@ -477,7 +519,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
             }
 #pragma unroll
             for (int y = 0; y < 4; ++y)
-              u[x][y] = kE4M3 ? v[y] + (float)((int)(y & 1 ? ev[y >> 1] >> 8 : ev[y >> 1] & 0xffu) - 127) : v[y];
+              u[x][y] = kCoded ? v[y] + (float)((int)(y & 1 ? ev[y >> 1] >> 8 : ev[y >> 1] & 0xffu) - 127) : v[y];
             top[x] = row_max(u[x]);
             grow |= top[x] > ref[x] + kLag;            // (the same for the four lanes of a row)
           }
@@ -485,14 +527,14 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           if (__any_sync(0xffffffffu, grow)) {
             // Values of zeros have exponent 0 however small all others are: they must not become the reference, which would push the
             // weights of the others out of fp16's range.  They get the least exponent.
-            if (kE4M3 && __any_sync(0xffffffffu, __vcmpeq4(ev[0] | ev[1] << 16, 0x7f7f7f7fu) != 0)) {
+            if (kCoded && __any_sync(0xffffffffu, __vcmpeq4(ev[0] | ev[1] << 16, 0x7f7f7f7fu) != 0)) {
               uint32_t some = 0;                       // bit y: key y has a value that is not zero
 #pragma unroll
               for (int y = 0; y < 4; ++y) {
                 uint32_t w[kWords], any = 0;
                 value_codes(y, w);
 #pragma unroll
-                for (int i = 0; i < kWords; ++i) any |= w[i] & 0x7f7f7f7fu;
+                for (int i = 0; i < kWords; ++i) any |= w[i] & (kE2M1 ? 0x77777777u : 0x7f7f7f7fu);
                 some |= any != 0 ? 1u << y : 0u;
               }
 #pragma unroll
@@ -510,7 +552,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
               if (top[x] > ref[x] + kLag) {
                 alpha[x] = fast_exp2(ref[x] - top[x]);           // 0 the first time
                 ref[x] = top[x];
-                if (!kE4M3) l[x] *= alpha[x];
+                if (!kCoded) l[x] *= alpha[x];
               }
             }
             if (!kHigh) alpha[1] = alpha[0];
@@ -519,11 +561,11 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           }
 #pragma unroll
           for (int x = 0; x < kHalves; ++x) {
-            const float zero = (ref[x] == -INFINITY ? 0.f : ref[x]) - (kE4M3 ? kWeightTop : 0.f);
+            const float zero = (ref[x] == -INFINITY ? 0.f : ref[x]) - (kCoded ? kWeightTop : 0.f);
             float w[4];
 #pragma unroll
             for (int y = 0; y < 4; ++y) w[y] = fast_exp2(u[x][y] - zero);
-            if (kE4M3) {
+            if (kCoded) {
               pa[x] = pack_f16(w[0], w[1]);
               pa[2 + x] = pack_f16(w[2], w[3]);
             } else {
@@ -538,8 +580,8 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
             }
           }
           if (!kHigh) {
-            pa[1] = kE4M3 ? 0u : pb[0];
-            pa[3] = kE4M3 ? 0u : pb[2];
+            pa[1] = kCoded ? 0u : pb[0];
+            pa[3] = kCoded ? 0u : pb[2];
           }
           // ---- O += P V.  Slots outside the segment's keys may hold anything: their values are made zeros.
           const bool clear = key0 < p.lo || key0 + 15 > p.hi;
@@ -549,7 +591,36 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
             const int j = key0 + 2 * t4 + (y & 1) + (y >> 1) * 8;
             out[y] = j < p.lo || j > p.hi;
           }
-          if (kE4M3) {
+          if (kE2M1) {
+            // Two keys' codes of a column side by side in a byte, their scales in one register
+            uint32_t w[4][kWords], f[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              value_codes(y, w[y]);
+              const int row = r0 + 2 * t4 + (y & 1) + (y >> 1) * 8;
+              f[y] = lds8(tScale + 2 * kTile + (kTile + row) * (D / 16) + (D == 128 ? hr : hr >> 1));
+              if (clear && out[y]) {
+                f[y] = 0u;
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) w[y][i] = 0u;
+              }
+            }
+            uint32_t f01, f23;
+            e4m3x4_to_f16(f[0] | f[1] << 8 | f[2] << 16 | f[3] << 24, f01, f23);
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) {
+              constexpr uint32_t kLow = 0x0f0f0f0fu;
+              uint32_t p[4], q[4];
+              e2m1x8_to_f16((w[0][i] & kLow) | (w[1][i] << 4 & ~kLow), p);
+              e2m1x8_to_f16((w[2][i] & kLow) | (w[3][i] << 4 & ~kLow), q);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) mma_16816<true>(acc[8 * i + 2 * j], pa, mul_f16x2(p[j], f01), mul_f16x2(q[j], f23));
+              e2m1x8_to_f16((w[0][i] >> 4 & kLow) | (w[1][i] & ~kLow), p);
+              e2m1x8_to_f16((w[2][i] >> 4 & kLow) | (w[3][i] & ~kLow), q);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) mma_16816<true>(acc[8 * i + 2 * j + 1], pa, mul_f16x2(p[j], f01), mul_f16x2(q[j], f23));
+            }
+          } else if (kCoded) {
             uint32_t w[4][kWords];
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
@@ -608,16 +679,16 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
         float sum = l[x];
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        if (t4 == 0) { row[D] = kE4M3 ? m[x] : ref[x]; row[D + 1] = sum; row[D + 2] = ref[x]; }
+        if (t4 == 0) { row[D] = kCoded ? m[x] : ref[x]; row[D + 1] = sum; row[D + 2] = ref[x]; }
 #pragma unroll
         for (int j = 0; j < D / 8; ++j) {
           float v0 = acc[j][2 * x], v1 = acc[j][2 * x + 1];
-          if (!kHigh && !kE4M3) {
+          if (!kHigh && !kCoded) {
             // (an infinite value stays what it is: the part cut off may have the other sign or be zero)
             if (isfinite(v0)) v0 += acc[j][2];
             if (isfinite(v1)) v1 += acc[j][3];
           }
-          if (kE4M3) {                                 // column tile j, columns 2 t4 and 2 t4 + 1 of it
+          if (kCoded) {                                 // column tile j, columns 2 t4 and 2 t4 + 1 of it
             row[2 * t4 * kCols + j] = v0;
             row[(2 * t4 + 1) * kCols + j] = v1;
           } else {
@@ -643,7 +714,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           const float mw = row[D], rw = row[D + 2];
           L += row[D + 1] * exp2f(mw - base);
           if (rw == -INFINITY) continue;
-          const float f = exp2f(rw - (kE4M3 ? kWeightTop : 0.f) - base);
+          const float f = exp2f(rw - (kCoded ? kWeightTop : 0.f) - base);
           const float4 v = *reinterpret_cast<const float4*>(row + c4 * 4);
           A.x += v.x * f; A.y += v.y * f; A.z += v.z * f; A.w += v.w * f;
         }
@@ -808,23 +879,30 @@ __global__ void __launch_bounds__(kCombineThreads) cache_few_combine_kernel(cons
 
 constexpr int kSmemPerCta = 113 * 1024;          // two CTAs an SM
 
-template <int D, bool kE4M3, bool kHigh>
+template <int D, int kKind, bool kHigh>
 cudaError_t launch(const CacheFwdArgs& a, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t s) {
-  using SM = FewSmem<D, kE4M3>;
+  using SM = FewSmem<D, kKind>;
   constexpr int kRows = kHigh ? 16 : 8;
   constexpr int kFit = (kSmemPerCta - SM::total(0, kRows)) / (SM::kStageBytes + SM::kScaleBytes);
   constexpr int kStages = kFit < kMaxStages ? kFit : kMaxStages;
   constexpr int smem = SM::total(kStages, kRows);
   static PerDeviceOnce once;
   cudaError_t e = once.run([] {
-    return cudaFuncSetAttribute(cache_few_kernel<D, kE4M3, kHigh>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    return cudaFuncSetAttribute(cache_few_kernel<D, kKind, kHigh>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   });
   if (e != cudaSuccess) return e;
-  cache_few_kernel<D, kE4M3, kHigh><<<kCtas, kThreads, smem, s>>>(a, mapK, mapV, kStages);
+  cache_few_kernel<D, kKind, kHigh><<<kCtas, kThreads, smem, s>>>(a, mapK, mapV, kStages);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   const dim3 grid(a.Hq, a.c.B, std::max(1, std::min(a.c.Lq, a.few_rows / a.G)));
   return launch_dependent(cache_few_combine_kernel<D, kRows>, grid, kCombineThreads, 0, s, true, a);
+}
+
+template <int D, bool kHigh>
+cudaError_t launch_kind(const CacheFwdArgs& a, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t s) {
+  return a.c.kind == L2A_CACHE_BF16   ? launch<D, L2A_CACHE_BF16, kHigh>(a, mapK, mapV, s)
+         : a.c.kind == L2A_CACHE_E4M3 ? launch<D, L2A_CACHE_E4M3, kHigh>(a, mapK, mapV, s)
+                                      : launch<D, L2A_CACHE_E2M1, kHigh>(a, mapK, mapV, s);
 }
 
 int slot_rows(const l2a_params* p) { return (int64_t)p->Lq * (p->Hq / p->Hkv) > 8 ? kBlockRows : 8; }
@@ -847,7 +925,7 @@ bool cache_few_counts(const l2a_params* p) { return batch_of(p->Lk, p->Hkv, row_
 
 cudaError_t launch_cache_few(const CacheFwdArgs& args, void* ws, cudaStream_t s) {
   CacheFwdArgs a = args;
-  const bool high = (int64_t)a.c.Lq * a.G > 8, e4m3 = a.c.kind == L2A_CACHE_E4M3;
+  const bool high = (int64_t)a.c.Lq * a.G > 8;
   a.plan = static_cast<int*>(ws);
   a.row_blocks = row_blocks((int64_t)a.c.Lq * a.G);
   a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + plan_bytes(a.c.B));
@@ -871,13 +949,8 @@ cudaError_t launch_cache_few(const CacheFwdArgs& args, void* ws, cudaStream_t s)
       a.O = args.O + t * a.o_t;
       if (a.d != nullptr) a.d = args.d + t;
     }
-    if (a.c.D == 128) {
-      if (e4m3) e = high ? launch<128, true, true>(a, mapK, mapV, s) : launch<128, true, false>(a, mapK, mapV, s);
-      else e = high ? launch<128, false, true>(a, mapK, mapV, s) : launch<128, false, false>(a, mapK, mapV, s);
-    } else {
-      if (e4m3) e = high ? launch<64, true, true>(a, mapK, mapV, s) : launch<64, true, false>(a, mapK, mapV, s);
-      else e = high ? launch<64, false, true>(a, mapK, mapV, s) : launch<64, false, false>(a, mapK, mapV, s);
-    }
+    if (a.c.D == 128) e = high ? launch_kind<128, true>(a, mapK, mapV, s) : launch_kind<128, false>(a, mapK, mapV, s);
+    else e = high ? launch_kind<64, true>(a, mapK, mapV, s) : launch_kind<64, false>(a, mapK, mapV, s);
   }
   return e;
 }

@@ -21,7 +21,7 @@ bool has_chunks(const l2a_params* p) { return (int64_t)p->Lq * (p->Hq / p->Hkv) 
 int few_rows(const l2a_params* p, const l2a_cache* c, int n_tokens) {
   const int G = p->Hq / p->Hkv;
   const double blocks = std::max<double>(p->B, (double)n_tokens * G / kBlockRows);
-  const double pass = (double)p->Lk * p->Hkv * p->D * (c->kind == L2A_CACHE_E4M3 ? 2 : 4);
+  const double pass = 2.0 * p->Lk * p->Hkv * row_bytes(c->kind, p->D);
   return (blocks - 1.15 * p->B) * pass < 125e6 ? kRowBlocks * kBlockRows : kBlockRows;
 }
 

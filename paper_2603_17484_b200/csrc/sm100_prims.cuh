@@ -216,6 +216,14 @@ __device__ __forceinline__ void named_barrier(int id, int threads) {
   asm volatile("barrier.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
+// The same; whether the predicate holds for all of them
+__device__ __forceinline__ bool named_barrier_all(int id, int threads, bool pred) {
+  uint32_t all;
+  asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %3, 0;\n barrier.red.and.pred q, %1, %2, p;\n selp.u32 %0, 1, 0, q;\n}"
+               : "=r"(all) : "r"(id), "r"(threads), "r"((uint32_t)pred) : "memory");
+  return all != 0;
+}
+
 // Programmatic dependent launch: a grid launched with that attribute may start once every CTA of the grid before it has
 // started (and called release); wait returns when that grid has completed and its writes are visible.  Without the
 // attribute both are no-ops.

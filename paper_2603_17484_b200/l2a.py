@@ -27,6 +27,7 @@ ROUTER_LOGITS_F32 = 1
 ROUTER_LOGITS_BF16 = 2
 CACHE_BF16 = 0
 CACHE_E4M3 = 1
+CACHE_E2M1 = 3
 
 EXPORTS = (
     "l2a_version", "l2a_status_string", "l2a_workspace_bytes", "l2a_workspace_status",
@@ -129,27 +130,33 @@ def params(B, Lq, Lk, Hq, Hkv, D, window, q_pos_offset=None, softmax_scale=0.0, 
 
 def cache(K, V, page_table, lengths, k_scale=None, v_scale=None) -> L2ACache:
     """Description of a paged cache (see include/l2a.h).  K, V: pools [pages, Hkv, page size, D], bf16, or 8-bit codes
-    (torch.float8_e4m3fn or uint8) with the exponents k_scale, v_scale (uint8 [pages, Hkv, page size]); a page itself is dense, the
-    pages may be further apart.  page_table: int32 [B, pages of a sequence], lengths: int32 [B]."""
+    (torch.float8_e4m3fn or uint8) with the exponents k_scale, v_scale (uint8 [pages, Hkv, page size]), or 4-bit codes
+    (torch.float4_e2m1fn_x2 [pages, Hkv, page size, D / 2]) with exponents and block scales (uint8 [pages, Hkv, page size * (1 + D / 16)]:
+    of each head the exponents of its tokens, then D / 16 scales for each); a page itself is dense, the pages may be further apart.
+    page_table: int32 [B, pages of a sequence], lengths: int32 [B]."""
     def stride(x, y):
         dense = tuple(torch.empty(x.shape[1:], device="meta").stride())
         if x.shape != y.shape or x.stride() != y.stride() or x.stride()[1:] != dense:
             raise ValueError("K and V (and their scales) have the same shape and strides, and dense pages")
         return x.stride(0) if x.shape[0] > 1 else 0
 
-    kind = CACHE_BF16 if K.dtype == torch.bfloat16 else CACHE_E4M3
-    if K.dtype not in (torch.bfloat16, torch.float8_e4m3fn, torch.uint8) or K.dtype != V.dtype:
-        raise ValueError("a cache holds bf16 values or e4m3 codes (float8_e4m3fn or uint8), K and V alike")
-    if any((x is not None) != (kind == CACHE_E4M3) for x in (k_scale, v_scale)):
-        raise ValueError("8-bit codes need their exponents, bf16 values have none")
-    if kind == CACHE_E4M3 and (k_scale.dtype != torch.uint8 or v_scale.dtype != torch.uint8 or k_scale.shape != K.shape[:3]):
-        raise ValueError("k_scale, v_scale: uint8 [pages, Hkv, page size]")
+    kind = {torch.bfloat16: CACHE_BF16, torch.float4_e2m1fn_x2: CACHE_E2M1}.get(K.dtype, CACHE_E4M3)
+    if K.dtype not in (torch.bfloat16, torch.float8_e4m3fn, torch.uint8, torch.float4_e2m1fn_x2) or K.dtype != V.dtype:
+        raise ValueError("a cache holds bf16 values, e4m3 codes (float8_e4m3fn or uint8) or e2m1 codes (float4_e2m1fn_x2), K and V alike")
+    if any((x is not None) != (kind != CACHE_BF16) for x in (k_scale, v_scale)):
+        raise ValueError("8-bit and 4-bit codes need their scales, bf16 values have none")
+    if kind != CACHE_BF16 and (k_scale.dtype != torch.uint8 or v_scale.dtype != torch.uint8):
+        raise ValueError("k_scale, v_scale are uint8")
+    if kind == CACHE_E4M3 and k_scale.shape != K.shape[:3]:
+        raise ValueError("k_scale, v_scale of 8-bit codes: [pages, Hkv, page size]")
+    if kind == CACHE_E2M1 and (K.dim() != 4 or k_scale.shape != (*K.shape[:2], K.shape[2] * (1 + K.shape[3] // 8))):
+        raise ValueError("k_scale, v_scale of 4-bit codes: [pages, Hkv, page size * (1 + D / 16)]")
     if page_table.dtype != torch.int32 or lengths.dtype != torch.int32 or page_table.dim() != 2 or lengths.dim() != 1:
         raise ValueError("page_table [B, n] and lengths [B] are int32")
     if (page_table.stride(1) != 1 and page_table.shape[1] > 1) or (lengths.stride(0) != 1 and lengths.shape[0] > 1):
         raise ValueError("rows of page_table, and lengths, are dense")
-    c = L2ACache(_addr(K), _addr(V), _addr(k_scale), _addr(v_scale), stride(K, V),
-                 0 if kind == CACHE_BF16 else stride(k_scale, v_scale), kind, K.shape[0], K.shape[2],
+    c = L2ACache(_addr(K), _addr(V), _addr(k_scale), _addr(v_scale),
+                 stride(K, V) * (2 if kind == CACHE_E2M1 else 1), 0 if kind == CACHE_BF16 else stride(k_scale, v_scale), kind, K.shape[0], K.shape[2],
                  page_table.stride(0) if page_table.shape[0] > 1 else page_table.shape[1], _addr(page_table), _addr(lengths))
     c.tensors = (K, V, k_scale, v_scale, page_table, lengths)
     return c
