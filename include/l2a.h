@@ -500,6 +500,32 @@ l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c, const void
                              const uint8_t* d, void* O, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Eviction: bounds the cache of every sequence.  Of sequence b, n = lengths[b] tokens long, m = min(n, keep[b], p->Lq) stay (keep below 0
+ * is 0), for every KV head its own: the last r = min(recent, m), the first f = min(sinks, m - r), and of those in between the m - f - r of the
+ * highest weights (equal ones from the lowest position on; NaN is below all).  In order, as tokens 0 .. m - 1 of sequence b, they are
+ * written to the pages of another cache: keys, values and scales as they are, and their weights.  The last tokens keep their order and
+ * distance, so that with recent >= window what Local Attention sees is what it saw.  Global Attention sees what has stayed.
+ *
+ *   p           : B, Hkv, D and the rest as elsewhere; Lk = the most tokens of a sequence, Lq = the most that stay of one (bounds for the host).
+ *   c           : the cache.  weights in: fp32 pool [n_pages, Hkv, page_size] of its slots; weight_stride elements from a page to the next, 0 =
+ *                 dense.
+ *   keep        in: int32 [B] device.  sinks, recent >= 0.
+ *   to          : the other cache: kind, Hkv and D of c; its page size, pools and table are its own (Lq <= table_stride * page_size; its
+ *                 lengths are not read).  It may share pools with c, but no page that either has tokens in: the same table in the same pool is
+ *                 refused.
+ *   to_weights out: fp32 pool of its slots.  Slots beyond a sequence's tokens are left alone in all pools.
+ *   to_lengths  out: int32 [B], m.  May be c->lengths or to->lengths.
+ *   kept        out: optional int32 [B, Hkv, Lq]: the positions that stayed, ascending; -1 behind the m of a sequence.
+ *   ws             : device workspace of l2a_cache_evict_workspace_bytes (4 * B * Hkv * Lq and a little), 256-byte aligned.
+ * HBM-bound: the weights are read once, what stays is read and written once.  Bit-reproducible.  Errors: L2A_ERR_INVALID_ARG,
+ * L2A_ERR_UNSUPPORTED (D, page_size, kind, B or Hkv > 65535), L2A_ERR_WORKSPACE, L2A_ERR_CUDA.
+ */
+l2a_status l2a_cache_evict_workspace_bytes(const l2a_params* p, const l2a_cache* c, size_t* ws_bytes);
+l2a_status l2a_cache_evict(const l2a_params* p, const l2a_cache* c, const float* weights, int64_t weight_stride, const int32_t* keep,
+                           int sinks, int recent, const l2a_cache* to, float* to_weights, int64_t to_weight_stride, int32_t* to_lengths,
+                           int32_t* kept, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * One whole step for callers that hold HOST buffers, so that end-to-end time including the
  * transfers can be measured through the C ABI: copies Q, K, V, the router input (and dO) to the
  * device buffers the caller supplies, runs l2a_route_compact + l2a_forward (+ l2a_backward when

@@ -36,6 +36,7 @@ EXPORTS = (
     "l2a_backward_split", "l2a_router_backward", "l2a_forward_routed", "l2a_selftest_wait_timeout",
     "l2a_forward_sets", "l2a_backward_sets", "l2a_pack_sequences", "l2a_step_host_async", "l2a_step_host_wait",
     "l2a_cache_append", "l2a_cache_read", "l2a_cache_workspace_bytes", "l2a_cache_forward",
+    "l2a_cache_evict_workspace_bytes", "l2a_cache_evict",
 )
 
 
@@ -67,8 +68,8 @@ class L2AError(RuntimeError):
         super().__init__(f"{where}: {status_string(code)} ({code})")
 
 
-# argument types of the calls made once per layer or token: p address, i int, f float, z size_t
-_CTYPES = {"p": ctypes.c_void_p, "i": ctypes.c_int, "f": ctypes.c_float, "z": ctypes.c_size_t}
+# argument types of the calls made once per layer or token: p address, i int, l 64-bit int, f float, z size_t
+_CTYPES = {"p": ctypes.c_void_p, "l": ctypes.c_int64, "i": ctypes.c_int, "f": ctypes.c_float, "z": ctypes.c_size_t}
 _SIGNATURES = {
     "l2a_route_compact": "ppif" + "pppp" + "pzp",
     "l2a_pack_sequences": "piipp",
@@ -84,6 +85,8 @@ _SIGNATURES = {
     "l2a_cache_read": "pppppp",
     "l2a_cache_workspace_bytes": "ppip",
     "l2a_cache_forward": "pppp" + "i" + "pp" + "pzp",
+    "l2a_cache_evict_workspace_bytes": "ppp",
+    "l2a_cache_evict": "pppl" + "pii" + "pplpp" + "pzp",
 }
 
 _lib = None
@@ -285,6 +288,32 @@ def l2a_cache_forward(p, cache, Q, cu_new, n_tokens, d, O, ws, stream=None, chec
                                    _addr(ws), _bytes(ws), _raw_stream(stream))
     if check:
         _check(code, "l2a_cache_forward")
+    return code
+
+
+def _weight_stride(weights, cache):
+    """Elements from a page of weights to the next; they are fp32 [pages, Hkv, page size] like the cache's slots, pages dense."""
+    K = cache.tensors[0]
+    if weights.dtype != torch.float32 or weights.shape != K.shape[:3] or weights.stride()[1:] != (K.shape[2], 1):
+        raise ValueError("weights of a cache: fp32 [pages, Hkv, page size], dense pages")
+    return weights.stride(0) if weights.shape[0] > 1 else 0
+
+
+def l2a_cache_evict_workspace_bytes(p, cache) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().l2a_cache_evict_workspace_bytes(ctypes.byref(p), ctypes.byref(cache), ctypes.byref(n)),
+           "l2a_cache_evict_workspace_bytes")
+    return n.value
+
+
+def l2a_cache_evict(p, cache, weights, keep, sinks, recent, to, to_weights, to_lengths, kept, ws, stream=None, check=True) -> int:
+    """Moves the first tokens, the last ones and those of the highest weights of every sequence and KV head, keep[b] in all, into the pages
+    of `to`, with their weights; their numbers into to_lengths, their positions into kept (int32 [B, Hkv, p.Lq], or None)."""
+    code = lib().l2a_cache_evict(ctypes.byref(p), ctypes.byref(cache), _addr(weights), _weight_stride(weights, cache), _addr(keep),
+                                 sinks, recent, ctypes.byref(to), _addr(to_weights), _weight_stride(to_weights, to),
+                                 _addr(to_lengths), _addr(kept), _addr(ws), _bytes(ws), _raw_stream(stream))
+    if check:
+        _check(code, "l2a_cache_evict")
     return code
 
 
