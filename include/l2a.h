@@ -500,6 +500,34 @@ l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c, const void
                              const uint8_t* d, void* O, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Weights of the cached keys, what an eviction goes by (l2a_cache_evict): how much Global Attention has attended to each.  For every KV head g
+ * and key j of a sequence
+ *   W[g][j] += sum over its new tokens i that count, at positions p_i >= j, and the heads h of the group of  exp(s_ihj) / sum over j' <= p_i of
+ *   exp(s_ihj'),  s = softmax_scale q_ih . k_j.
+ * A new token's own slot had no weight, whatever it holds: weights need no clearing when pages change hands, if every token that is appended is
+ * a new token of one call (d of zeros, where none is to count).
+ *
+ *   p, c, cu_new, n_tokens as in l2a_cache_forward (window is not used; flags: none, L2A_FLAG_SHARED_WINDOW is ignored).
+ *   Q           in : bf16 [n_tokens, Hq, D] (token stride q_stride[1]).
+ *   d           in : uint8 [n_tokens], non-zero = the token counts (the routing decisions: the others have no Global Attention); NULL = all do.
+ *   weights in/out : fp32 pool [n_pages, Hkv, page_size] of the cache's slots, 4-byte aligned; weight_stride elements from a page to the next, 0 =
+ *                    dense.  Only slots of keys that some counted token sees, and of new tokens, are touched.
+ *   ws             : device workspace of l2a_cache_weigh_workspace_bytes, 256-byte aligned, its first word a status (l2a_workspace_status; after
+ *                    a time-out the weights are not to be used).  Up to 64 rows a sequence (Lq * Hq / Hkv) it keeps their scores, 4 * B * Hkv * rows *
+ *                    Lk bytes (fewer rows where that would pass 4 GB); beyond, the rows' queries and of an 8- or 4-bit cache the keys in bf16, 2 * B * Lk *
+ *                    Hkv * D bytes with Lk rounded up to 128.  Lk decides, so give it no larger than need be.  It is enough for every smaller
+ *                    n_tokens (other fields alike).
+ * Scores, soft-max statistics and sums are fp32, products of bf16 and decoded keys exact.  Bit-reproducible.  Keys that a counted token sees must be finite; a query
+ * row with NaN makes the weights of the keys that it sees NaN.
+ * Few rows: HBM-bound, keys and weights once.  Many: bound by the exponentials, two for each pair of a row and a key.
+ * Limits: n_tokens * Hq < 2^31 - 32; B, Hkv <= 65535; Lk * (Hkv + 75) < 2^35 and Lk * Hkv < 2^38.  Errors: L2A_ERR_INVALID_ARG, L2A_ERR_UNSUPPORTED (D,
+ * page_size, kind, the limits), L2A_ERR_WORKSPACE, L2A_ERR_CUDA; a bounded device wait that runs out is reported by the status header.
+ */
+l2a_status l2a_cache_weigh_workspace_bytes(const l2a_params* p, const l2a_cache* c, int n_tokens, size_t* ws_bytes);
+l2a_status l2a_cache_weigh(const l2a_params* p, const l2a_cache* c, const void* Q, const int32_t* cu_new, int n_tokens, const uint8_t* d,
+                           float* weights, int64_t weight_stride, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Eviction: bounds the cache of every sequence.  Of sequence b, n = lengths[b] tokens long, m = min(n, keep[b], p->Lq) stay (keep below 0
  * is 0), for every KV head its own: the last r = min(recent, m), the first f = min(sinks, m - r), and of those in between the m - f - r of the
  * highest weights (equal ones from the lowest position on; NaN is below all).  In order, as tokens 0 .. m - 1 of sequence b, they are

@@ -53,7 +53,7 @@ __device__ __forceinline__ int cache_page(const CacheView& c, int b, int pos) {
   return page >= 0 && page < c.n_pages ? page : -1;
 }
 
-// A forward call over the cache.
+// A call of the attention over the cache, or of the weights of its keys.
 struct CacheFwdArgs {
   CacheView c;
   int Hq, G, window;
@@ -71,6 +71,13 @@ struct CacheFwdArgs {
   int few_rows;                // most rows of a sequence there, and
   int row_blocks;              // blocks of rows that it can have
   int clear;                   // few rows: no launch ahead has cleared the status word
+  // the weights of the keys (l2a_cache_weigh); global is set, local and add are not
+  int every;                   // every row counts, whatever d
+  float* weights;              // pool [pages, Hkv, page], w_page elements a page
+  int64_t w_page;
+  float* scores;               // few rows: of a sequence's KV head score_rows rows of score_pitch keys
+  int score_rows;
+  int64_t score_pitch;
 };
 
 // Sequences whose new tokens have at most few_rows rows (tokens x heads of a KV group), one block of rows or kRowBlocks of them:
@@ -80,12 +87,36 @@ size_t cache_few_ws_bytes(const l2a_params* p);     // plan and parts
 bool cache_few_counts(const l2a_params* p);         // whether it can count the tiles of one sequence
 cudaError_t launch_cache_few(const CacheFwdArgs& a, void* ws, cudaStream_t s);
 
+// The weights of the keys from those sequences, up to `rows` rows of each
+size_t cache_few_weigh_ws_bytes(const l2a_params* p, int rows);
+cudaError_t launch_cache_few_weigh(const CacheFwdArgs& a, void* ws, cudaStream_t s);
+
 // All others: cache_chunk.cu
 size_t cache_chunk_ws_bytes(const l2a_params* p, int n_tokens);          // plan and parts,
 size_t cache_copy_bytes(const l2a_params* p, int kind);                  // behind them the decoded copy, 0: none is made
 bool cache_chunk_counts(const l2a_params* p, int n_tokens);      // whether it can count the key blocks of such a call
 // first: no kernel of the call ahead; copy: the workspace has room for the decoded copy
 cudaError_t launch_cache_chunk(const CacheFwdArgs& a, bool first, void* ws, bool copy, cudaStream_t s);
+
+// Adds sum[i] to the weights of keys key .. key + 3 of a sequence's KV head, key a multiple of four; those of its new tokens (from `fresh` on)
+// had none.  Keys behind hi that are not new keep what they have.
+__device__ __forceinline__ void add_weights(const CacheFwdArgs& a, const CacheView& c, int b, int g, int key, int length, int fresh, int hi,
+                                            const float (&sum)[4]) {
+  const int last = min(length - 1, key + 3);
+  if (key > last || (key > hi && last < fresh)) return;
+  const int page = cache_page(c, b, key);              // (a page holds a multiple of four tokens)
+  if (page < 0) return;
+  float* w = a.weights + page * a.w_page + ((int64_t)g << c.page_shift) + (key & ((1 << c.page_shift) - 1));
+  if (last == key + 3 && key + 3 < fresh && (reinterpret_cast<uintptr_t>(w) & 15) == 0) {
+    float4 x = *reinterpret_cast<float4*>(w);
+    x.x += sum[0]; x.y += sum[1]; x.z += sum[2]; x.w += sum[3];
+    *reinterpret_cast<float4*>(w) = x;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (key + i <= last && (key + i <= hi || key + i >= fresh)) w[i] = (key + i < fresh ? w[i] : 0.f) + sum[i];
+}
 
 // Tensor map over a pool: {elements of 128 bytes at most, tokens, (pieces of a row,) heads, pages}; one copy brings box_rows
 // tokens of one head of one page, box_pieces * 64 elements of each (bf16) or the whole row of codes (swizzled over the row's bytes).

@@ -76,9 +76,9 @@ __device__ __forceinline__ FewSeq few_seq(const CacheFwdArgs& a, int b) {
   s.lo = max(0, s.length - s.n - a.window);
   s.n_loc = a.local && s.n > 0 && s.length > 0 ? (s.length - 1) / kTile - s.lo / kTile + 1 : 0;
   s.hi = -1;
-  if (a.global && a.d != nullptr)
+  if (a.global && (a.d != nullptr || a.every))
     for (int i = 0; i < s.n; ++i)
-      if (a.d[s.first + i] != 0) s.hi = s.length - s.n + i - a.shift;
+      if (a.every || a.d[s.first + i] != 0) s.hi = s.length - s.n + i - a.shift;
   s.hi = max(s.hi, -1);
   s.n_out = s.hi / kTile + (s.hi >= 0 ? 1 : 0);
   return s;
@@ -131,12 +131,13 @@ __device__ __forceinline__ uint32_t lds16(uint32_t saddr) {
   return v;
 }
 
-template <int D, int kKind>
+template <int D, int kKind, bool kWeigh>
 struct FewSmem {
+  static constexpr int kTensors = kWeigh ? 1 : 2;                          // K, then V
   static constexpr int kTileBytes = kTile * row_bytes(kKind, D);
-  static constexpr int kStageBytes = 2 * kTileBytes;                       // K, then V
-  static constexpr int kScaleBytes = 2 * kTile * scale_bytes(kKind, D);    // exponents of K, then of V; e2m1: scales of the blocks of K, then of V
-  static __host__ __device__ constexpr int red_bytes(int rows) { return kComputeWarps * rows * (D + 4) * 4; }
+  static constexpr int kStageBytes = kTensors * kTileBytes;
+  static constexpr int kScaleBytes = kTensors * kTile * scale_bytes(kKind, D);    // exponents of K, of V; e2m1: scales of the blocks of K, of V
+  static __host__ __device__ constexpr int red_bytes(int rows) { return kComputeWarps * rows * (kWeigh ? 2 : D + 4) * 4; }
   static __host__ __device__ constexpr int total(int stages, int rows) {
     return stages * (kStageBytes + kScaleBytes) + red_bytes(rows) + (int)sizeof(FewBars);
   }
@@ -156,6 +157,13 @@ struct Piece {
 __device__ __forceinline__ int tiles_per_cta(int total, int pairs) {
   const int share = max(1, (total + kCtas - 1) / kCtas), pair = max(1, total / max(pairs, 1));
   return share >= pair ? (share + pair - 1) / pair * pair : max(share, min(kMinTiles, pair));
+}
+
+// Maximum and sum of a row's weights, two parts of them in one
+__device__ __forceinline__ void join_sums(float& m, float& l, float m2, float l2) {
+  const float M = fmaxf(m, m2), base = M == -INFINITY ? 0.f : M;
+  l = l * fast_exp2(m - base) + l2 * fast_exp2(m2 - base);
+  m = M;
 }
 
 // The pieces of a CTA's range of tiles, in order: every warp walks through them by itself.
@@ -187,12 +195,13 @@ __device__ __forceinline__ bool next_piece(const CacheFwdArgs& a, Walk& w, Piece
   return true;
 }
 
-// kHigh: more than eight rows.
-template <int D, int kKind, bool kHigh>
+// kHigh: more than eight rows.  kWeigh: scores only, times log2(e), for the weights of the keys (cache_weigh.cu): they go to the workspace,
+// a row's keys side by side, and of a piece the maximum and sum of each row.
+template <int D, int kKind, bool kHigh, bool kWeigh>
 __global__ void __launch_bounds__(kThreads, 2)
 cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
                  const int stages) {
-  using SM = FewSmem<D, kKind>;
+  using SM = FewSmem<D, kKind, kWeigh>;
   constexpr int kRows = kHigh ? 16 : 8, kHalves = kHigh ? 2 : 1;
   constexpr bool kCoded = kKind != L2A_CACHE_BF16, kE2M1 = kKind == L2A_CACHE_E2M1;
   constexpr int kCols = D / 8;                   // codes: columns of V of a lane's group, and column tiles
@@ -253,6 +262,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           // for the combination: tiles before the sequence, and the sequence
           reinterpret_cast<int4*>(a.plan)[2 + 2 * b] = make_int4(x - n, own.first, own.n, own.n_loc);
           a.plan[8 + 8 * b + 4] = own.n_out;
+          if (kWeigh) a.plan[8 + 8 * b + 5] = own.hi;
         }
         const int at = mine * per_cta;
         if (at >= x - n && at < x) {
@@ -297,7 +307,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           page_ids = e >= first_entry && e <= last_entry ? cache_page(c, p.b, e << c.page_shift) : -1;
         }
         const int page = __shfl_sync(0xffffffffu, page_ids, entry - entry0);
-        const bool load = bytes > 0 && page >= 0 && key <= p.hi && key + rows > p.lo;
+        const bool load = bytes > 0 && !(kWeigh && (what & 1)) && page >= 0 && key <= p.hi && key + rows > p.lo;
         const uint32_t expect = __reduce_add_sync(0xffffffffu, load ? bytes : 0u);
         if (!mbar_wait_warp(&bar->empty[s], ph, abort_flag)) { ok = false; break; }
         if (lane == 0) mbar_expect_tx(&bar->full[s], expect);
@@ -308,7 +318,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
             tma_load_page(smem + s * SM::kStageBytes + what * SM::kTileBytes + u * (SM::kTileBytes / copies), what ? &mapV : &mapK,
                           &bar->full[s], kCoded, 0, in_page, p.g, page);
           } else if (kE2M1 && what >= 4) {
-            bulk_load(scales + s * SM::kScaleBytes + 2 * kTile + ((what - 4) * kTile + u * rows) * (D / 16),
+            bulk_load(scales + s * SM::kScaleBytes + SM::kTensors * kTile + ((what - 4) * kTile + u * rows) * (D / 16),
                       (what == 4 ? c.ks : c.vs) + page * c.scale_stride + blocks_at<D>(c, p.g, in_page), bytes, &bar->full[s]);
           } else {
             bulk_load(scales + s * SM::kScaleBytes + (what - 2) * kTile + u * rows,
@@ -343,7 +353,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           if (p.seg == 0) {
             row_lo[x] = pos - a.window;
             row_hi[x] = pos;
-          } else if (a.d[token[x]] != 0) {
+          } else if (kWeigh && a.every ? true : a.d[token[x]] != 0) {
             row_hi[x] = pos - a.shift;
           }
           every_lo = max(every_lo, row_lo[x]);
@@ -433,7 +443,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
                 } else {
                   lds64(tK + row * 32 + (((t4 >> 1) ^ ((row >> 2) & 1)) << 4) + (t4 & 1) * 8, w[0], w[1]);
                 }
-                const uint32_t at = tScale + 2 * kTile + row * (D / 16) + t4 * kPieces;
+                const uint32_t at = tScale + SM::kTensors * kTile + row * (D / 16) + t4 * kPieces;
                 uint32_t both, none;
                 e4m3x4_to_f16(D == 128 ? lds16(at) : lds8(at), both, none);
 #pragma unroll
@@ -459,7 +469,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
               }
               const uint32_t at = tScale + r0 + x * 8 + 2 * t4;
               const uint32_t ek = lds16(at);
-              ev[x] = lds16(at + kTile);
+              if (!kWeigh) ev[x] = lds16(at + kTile);
               const float f0 = scale_of_exponent(ek & 0xffu), f1 = scale_of_exponent(ek >> 8);
               sc[x][0] *= f0; sc[x][1] *= f1; sc[x][2] *= f0; sc[x][3] *= f1;
             }
@@ -475,6 +485,29 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
               mma_16816<false>(sc[1], qa[k], kb[2], kb[3]);
             }
           }
+          if constexpr (kWeigh) {
+            const int k = key0 + 2 * t4;
+#pragma unroll
+            for (int x = 0; x < kHalves; ++x) {
+              float v[4];
+#pragma unroll
+              for (int y = 0; y < 4; ++y) {
+                const int j = k + (y & 1) + (y >> 1) * 8;
+                v[y] = sc[y >> 1][2 * x + (y & 1)] * row_scale[x];
+                if (edge && j > row_hi[x]) v[y] = -INFINITY;
+              }
+              if (row_hi[x] >= 0) {
+                float* dst = a.scores + ((int64_t)(p.b * c.Hkv + p.g) * a.score_rows + p.block * kBlockRows + hr + 8 * x) * a.score_pitch + k;
+                *reinterpret_cast<float2*>(dst) = make_float2(v[0], v[1]);
+                *reinterpret_cast<float2*>(dst + 8) = make_float2(v[2], v[3]);
+              }
+              // (each lane by itself: its keys are joined with the others' at the end)
+              const float m_new = fmaxf(m[x], fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]))), base = m_new == -INFINITY ? 0.f : m_new;
+              l[x] = l[x] * fast_exp2(m[x] - base) + ((fast_exp2(v[0] - base) + fast_exp2(v[1] - base)) +
+                                                       (fast_exp2(v[2] - base) + fast_exp2(v[3] - base)));
+              m[x] = m_new;
+            }
+          } else {
           // codes: a lane's share of those of one of its four keys' values (key0 + 2 t4 + {0, 1, 8, 9})
           constexpr int kWords = kE2M1 ? kCols / 8 : kCols / 4;
           auto value_codes = [&](int y, uint32_t (&w)[kWords]) {
@@ -663,12 +696,34 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
               }
             }
           }
+          }
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&bar->empty[s]);
         if (++s == stages) { s = 0; ph ^= 1; }
       }
 
+      if constexpr (kWeigh) {
+        // ---- join the four lanes of a row, and the four warps
+        float2* parts = reinterpret_cast<float2*>(red);
+        named_barrier(1, kComputeWarps * 32);            // the piece before has been read
+#pragma unroll
+        for (int x = 0; x < kHalves; ++x) {
+#pragma unroll
+          for (int o = 1; o < 4; o <<= 1) join_sums(m[x], l[x], __shfl_xor_sync(0xffffffffu, m[x], o), __shfl_xor_sync(0xffffffffu, l[x], o));
+          if (t4 == 0) parts[warp * kRows + hr + 8 * x] = make_float2(m[x], l[x]);
+        }
+        named_barrier(1, kComputeWarps * 32);
+        if (tid < kRows) {
+          float2 y = parts[tid];
+#pragma unroll
+          for (int w = 1; w < kComputeWarps; ++w) join_sums(y.x, y.y, parts[w * kRows + tid].x, parts[w * kRows + tid].y);
+          // (a wait that ran out: the sum is none)
+          if (*abort_flag != 0) y = make_float2(0.f, -1.f);
+          reinterpret_cast<float2*>(a.part)[((int64_t)(p.b * c.Hkv + p.g) * a.row_blocks + p.block + blockIdx.x) * kRows + tid] = y;
+        }
+        continue;
+      }
       // ---- join the four warps, then store the result or the part
       constexpr int kPitch = D + 4;
       float* mine_red = red + warp * kRows * kPitch;
@@ -877,32 +932,88 @@ __global__ void __launch_bounds__(kCombineThreads) cache_few_combine_kernel(cons
   *dst = make_uint2(pack_bf16(o.x, o.y), pack_bf16(o.z, o.w));
 }
 
+// The weights of the keys of one KV head: what a row's soft-max gives them, summed over the rows, onto what they had (the new tokens' own keys
+// had nothing).  Bound by latencies and the scores' way through L2: a thread has four keys, and the rows' loads are in flight together.
+constexpr int kAddThreads = 256, kAddKeys = 4 * kAddThreads, kMaxRows = kRowBlocks * kBlockRows;
+__global__ void __launch_bounds__(kAddThreads) cache_few_add_kernel(const CacheFwdArgs a, const int slot_rows) {
+  __shared__ float lse[kMaxRows];
+  const CacheView& c = a.c;
+  const int g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int64_t k0 = (int64_t)blockIdx.x * kAddKeys;
+  dependency_wait();
+  const int4 seq = reinterpret_cast<const int4*>(a.plan)[2 + 2 * b];
+  const int n = seq.z, n_out = a.plan[8 + 8 * b + 4], hi = a.plan[8 + 8 * b + 5], length = cache_length(c, b);
+  // keys that some row sees, and the new ones
+  if (n == 0 || k0 >= length || (k0 > hi && k0 + kAddKeys <= length - n)) return;
+  const int per_cta = a.plan[0], rows = n * a.G, blocks = (rows + kBlockRows - 1) / kBlockRows;
+  bool failed = false;
+  for (int r = warp; r < rows; r += kAddThreads / 32) {
+    const int block = r / kBlockRows, at = seq.x + (g * blocks + block) * n_out;
+    const bool counts = n_out > 0 && (a.every || a.d[seq.y + r / a.G] != 0);
+    float m = -INFINITY, l = 0.f;
+    if (counts) {
+      const int c0 = at / per_cta, parts = (at + n_out - 1) / per_cta - c0 + 1;
+      const float2* part = reinterpret_cast<const float2*>(a.part) + ((int64_t)(b * c.Hkv + g) * a.row_blocks + block + c0) * slot_rows + r % kBlockRows;
+      for (int k = lane; k < parts; k += 32) {
+        const float2 x = __ldcg(part + (int64_t)k * slot_rows);
+        failed |= x.y < 0.f;
+        join_sums(m, l, x.x, x.y);
+      }
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) join_sums(m, l, __shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, l, o));
+    }
+    if (lane == 0) lse[r] = l != 0.f ? m + log2f(l) : INFINITY;          // (infinity: a row that sees nothing)
+  }
+  if (__syncthreads_or(failed)) return;                // a wait ran out in a part: nothing is stored
+  const int key = (int)k0 + 4 * tid;
+  if (key >= length) return;
+  const float* s = a.scores + (int64_t)(b * c.Hkv + g) * a.score_rows * a.score_pitch + key;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  if (key <= hi) {
+#pragma unroll 4
+    for (int r = 0; r < rows; ++r) {
+      const float z = lse[r];
+      if (z == INFINITY) continue;
+      const float4 v = __ldcs(reinterpret_cast<const float4*>(s + (int64_t)r * a.score_pitch));
+      sum[0] += fast_exp2(v.x - z);
+      sum[1] += key + 1 <= hi ? fast_exp2(v.y - z) : 0.f;
+      sum[2] += key + 2 <= hi ? fast_exp2(v.z - z) : 0.f;
+      sum[3] += key + 3 <= hi ? fast_exp2(v.w - z) : 0.f;
+    }
+  }
+  add_weights(a, c, b, g, key, length, length - n, hi, sum);
+}
+
 constexpr int kSmemPerCta = 113 * 1024;          // two CTAs an SM
 
-template <int D, int kKind, bool kHigh>
+template <int D, int kKind, bool kHigh, bool kWeigh>
 cudaError_t launch(const CacheFwdArgs& a, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t s) {
-  using SM = FewSmem<D, kKind>;
+  using SM = FewSmem<D, kKind, kWeigh>;
   constexpr int kRows = kHigh ? 16 : 8;
   constexpr int kFit = (kSmemPerCta - SM::total(0, kRows)) / (SM::kStageBytes + SM::kScaleBytes);
   constexpr int kStages = kFit < kMaxStages ? kFit : kMaxStages;
   constexpr int smem = SM::total(kStages, kRows);
   static PerDeviceOnce once;
   cudaError_t e = once.run([] {
-    return cudaFuncSetAttribute(cache_few_kernel<D, kKind, kHigh>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    return cudaFuncSetAttribute(cache_few_kernel<D, kKind, kHigh, kWeigh>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   });
   if (e != cudaSuccess) return e;
-  cache_few_kernel<D, kKind, kHigh><<<kCtas, kThreads, smem, s>>>(a, mapK, mapV, kStages);
+  cache_few_kernel<D, kKind, kHigh, kWeigh><<<kCtas, kThreads, smem, s>>>(a, mapK, mapV, kStages);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
+  if constexpr (kWeigh) {
+    const dim3 keys((unsigned)(((int64_t)a.c.max_keys + kAddKeys - 1) / kAddKeys), a.c.Hkv, a.c.B);
+    return launch_dependent(cache_few_add_kernel, keys, kAddThreads, 0, s, true, a, kRows);
+  }
   const dim3 grid(a.Hq, a.c.B, std::max(1, std::min(a.c.Lq, a.few_rows / a.G)));
   return launch_dependent(cache_few_combine_kernel<D, kRows>, grid, kCombineThreads, 0, s, true, a);
 }
 
-template <int D, bool kHigh>
+template <int D, bool kHigh, bool kWeigh>
 cudaError_t launch_kind(const CacheFwdArgs& a, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t s) {
-  return a.c.kind == L2A_CACHE_BF16   ? launch<D, L2A_CACHE_BF16, kHigh>(a, mapK, mapV, s)
-         : a.c.kind == L2A_CACHE_E4M3 ? launch<D, L2A_CACHE_E4M3, kHigh>(a, mapK, mapV, s)
-                                      : launch<D, L2A_CACHE_E2M1, kHigh>(a, mapK, mapV, s);
+  return a.c.kind == L2A_CACHE_BF16   ? launch<D, L2A_CACHE_BF16, kHigh, kWeigh>(a, mapK, mapV, s)
+         : a.c.kind == L2A_CACHE_E4M3 ? launch<D, L2A_CACHE_E4M3, kHigh, kWeigh>(a, mapK, mapV, s)
+                                      : launch<D, L2A_CACHE_E2M1, kHigh, kWeigh>(a, mapK, mapV, s);
 }
 
 int slot_rows(const l2a_params* p) { return (int64_t)p->Lq * (p->Hq / p->Hkv) > 8 ? kBlockRows : 8; }
@@ -923,12 +1034,10 @@ size_t cache_few_ws_bytes(const l2a_params* p) {
 
 bool cache_few_counts(const l2a_params* p) { return batch_of(p->Lk, p->Hkv, row_blocks((int64_t)p->Lq * (p->Hq / p->Hkv))) > 0; }
 
-cudaError_t launch_cache_few(const CacheFwdArgs& args, void* ws, cudaStream_t s) {
+template <bool kWeigh>
+static cudaError_t launch_few(const CacheFwdArgs& args, cudaStream_t s) {
   CacheFwdArgs a = args;
   const bool high = (int64_t)a.c.Lq * a.G > 8;
-  a.plan = static_cast<int*>(ws);
-  a.row_blocks = row_blocks((int64_t)a.c.Lq * a.G);
-  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + plan_bytes(a.c.B));
   CUtensorMap mapK, mapV;
   const int rows = std::min(1 << a.c.page_shift, kTile);
   if (!encode_pool_map(&mapK, a.c, a.c.K, rows, a.c.D / 64) || !encode_pool_map(&mapV, a.c, a.c.V, rows, a.c.D / 64))
@@ -946,13 +1055,42 @@ cudaError_t launch_cache_few(const CacheFwdArgs& args, void* ws, cudaStream_t s)
       const int64_t t = (int64_t)b * a.c.Lq;
       a.c.n_tokens = a.c.B * a.c.Lq;
       a.q = args.q + t * a.q_t;
-      a.O = args.O + t * a.o_t;
+      if (a.O != nullptr) a.O = args.O + t * a.o_t;
       if (a.d != nullptr) a.d = args.d + t;
     }
-    if (a.c.D == 128) e = high ? launch_kind<128, true>(a, mapK, mapV, s) : launch_kind<128, false>(a, mapK, mapV, s);
-    else e = high ? launch_kind<64, true>(a, mapK, mapV, s) : launch_kind<64, false>(a, mapK, mapV, s);
+    if (a.c.D == 128) e = high ? launch_kind<128, true, kWeigh>(a, mapK, mapV, s) : launch_kind<128, false, kWeigh>(a, mapK, mapV, s);
+    else e = high ? launch_kind<64, true, kWeigh>(a, mapK, mapV, s) : launch_kind<64, false, kWeigh>(a, mapK, mapV, s);
   }
   return e;
+}
+
+cudaError_t launch_cache_few(const CacheFwdArgs& args, void* ws, cudaStream_t s) {
+  CacheFwdArgs a = args;
+  a.plan = static_cast<int*>(ws);
+  a.row_blocks = row_blocks((int64_t)a.c.Lq * a.G);
+  a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + plan_bytes(a.c.B));
+  return launch_few<false>(a, s);
+}
+
+// Plan, maxima and sums of the parts, scores
+static int64_t score_pitch(int Lk) { return ((int64_t)Lk + kTile - 1) / kTile * kTile; }
+size_t cache_few_weigh_ws_bytes(const l2a_params* p, int rows) {
+  const size_t pairs = (size_t)p->B * p->Hkv;
+  return plan_bytes(p->B) + align_up((pairs * row_blocks(rows) + kCtas) * kBlockRows * 2 * sizeof(float), 256) +
+         align_up(pairs * rows * score_pitch(p->Lk) * sizeof(float), 256);
+}
+
+cudaError_t launch_cache_few_weigh(const CacheFwdArgs& args, void* ws, cudaStream_t s) {
+  CacheFwdArgs a = args;
+  uint8_t* at = static_cast<uint8_t*>(ws);
+  a.plan = reinterpret_cast<int*>(at);
+  a.score_rows = (int)std::min<int64_t>((int64_t)a.c.Lq * a.G, a.few_rows);
+  a.score_pitch = score_pitch(a.c.max_keys);
+  a.row_blocks = row_blocks(a.score_rows);
+  at += plan_bytes(a.c.B);
+  a.part = reinterpret_cast<float*>(at);
+  a.scores = reinterpret_cast<float*>(at + align_up(((size_t)a.c.B * a.c.Hkv * a.row_blocks + kCtas) * kBlockRows * 2 * sizeof(float), 256));
+  return launch_few<true>(a, s);
 }
 
 }  // namespace l2a

@@ -63,7 +63,7 @@ extern "C" l2a_status l2a_cache_workspace_bytes(const l2a_params* p, const l2a_c
 
 extern "C" l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c, const void* Q, const int32_t* cu_new, int n_tokens,
                                         const uint8_t* d, void* O, void* ws, size_t ws_bytes, void* stream) {
-  CacheFwdArgs a;
+  CacheFwdArgs a = {};
   l2a_status st = check_forward(p, c, n_tokens, &a.c);
   if (st == L2A_OK) st = cache_view(p, c, cu_new, n_tokens, &a.c);
   if (st != L2A_OK) return st;

@@ -1,0 +1,788 @@
+// Weights of the cached keys (l2a_cache_weigh): W_j += sum over the counted new tokens and the heads of a KV group of what the soft-max over all
+// keys up to the token gives key j.  The maximum and sum of a row have to be known before any of its weights is:
+//
+//   sequences of few rows (cache_few.cu): scores to the workspace in one pass over the keys, a second small kernel sums them up.
+//   others, here: the counted rows are compacted, 128 of a KV group to a block, and the products Q K^T are taken twice.
+//
+// weigh_plan_kernel : one CTA lists the counted tokens and the blocks of rows; the others decode the keys of an 8- or 4-bit cache to bf16.
+// weigh_rows_kernel : the blocks' rows of Q side by side.
+// weigh_pass_kernel : tiles of 128 x 128 scores, tcgen05, one operand kept for a piece of work, the other streamed past it; four tiles
+//                     under way in TMEM, two warpgroups take them in turn, a lane of TMEM to a thread.
+//     first pass    : a block of rows is kept, keys pass: a thread has a row, its running maximum and sum.  All tiles of the call, laid end to
+//                     end, are cut into even ranges, one a CTA; what a range leaves of a row is joined by weigh_join_kernel.
+//     second pass   : 128 keys are kept, the blocks that see them pass: a thread has a key and sums the weights of its column.  A key's sum is
+//                     made by one CTA in a fixed order: bit-reproducible.
+// Bound by the exponentials: 16384 a tile, 1024 clk on the special-function unit, next to 512 clk of products; a quarter of them is computed on the
+// FMA pipe.
+#include <math.h>
+
+#include <algorithm>
+
+#include "cache_common.cuh"
+
+namespace l2a {
+
+namespace {
+
+constexpr int kCtas = kSplitSms;
+constexpr int kPlanThreads = 1024;
+constexpr int kSumWarps = 8, kTmaWarp = 8, kMmaWarp = 9, kPassThreads = 10 * 32;
+constexpr int kYStages = 4, kScoreBufs = 4;
+constexpr int kBoxBytes = 128 * 128;         // 128 rows of 128 bytes
+
+// A block of 128 counted rows of a sequence: packed row r is that of token list[list + r / G], head r % G of the group
+struct alignas(16) RowBlock {
+  int b, list, row0, n_rows;
+  int base, tiles, last;         // position = base + token; key tiles that some row sees; position of the last row
+  int first_pos;                 // of the first row: keys up to there are seen by all
+  int64_t units, pad;            // key tiles of the blocks before
+};
+struct WeighPlan { int n_blocks; int64_t units, tiles; };
+
+struct WeighArgs {
+  CacheFwdArgs f;                // f.c: the bf16 cache or the decoded copy
+  CacheView codes;               // the cache itself
+  WeighPlan* plan;
+  RowBlock* blocks;
+  int* list;                     // counted tokens
+  int *list_start, *list_end;    // of a sequence
+  int* block_start;              // first block of a sequence, [B + 1],
+  int64_t* tile_start;           // key tiles of the sequences before it, [B + 1]
+  bf16* rows;                    // [Hkv][most_blocks * 128][D]
+  int* row_pos;                  // [most_blocks * 128], -1: no row
+  float* minus_lse;              // [Hkv][most_blocks * 128], minus infinity: no row
+  float2* part;                  // of a range: maximum and sum of 128 rows, from each warpgroup
+  int most_blocks;
+  int clear;                     // no kernel ahead has cleared the status word
+};
+
+__device__ __forceinline__ bool here(const CacheFwdArgs& a, int n) { return (int64_t)n * a.G > a.few_rows; }
+// New tokens of a sequence, 0 where it is not taken here
+__device__ __forceinline__ int sequence(const CacheFwdArgs& a, int b, int& first, int& length) {
+  const int n = cache_new(a.c, b, first);
+  length = cache_length(a.c, b);
+  return here(a, n) ? n : 0;
+}
+// The last i with v[i] <= x, of n > 0 ascending ones with v[0] <= x
+template <class T>
+__device__ __forceinline__ int last_not_above(const T* v, int n, T x) {
+  int lo = 0;
+  while (n - lo > 1) {
+    const int mid = (lo + n) >> 1;
+    if (v[mid] <= x) lo = mid; else n = mid;
+  }
+  return lo;
+}
+// Inclusive scan over the CTA's threads, in place; returns the sum
+template <class T>
+__device__ __forceinline__ T block_scan(T& x, T* sums) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const T u = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += u;
+  }
+  __syncthreads();
+  if (lane == 31) sums[warp] = x;
+  __syncthreads();
+  T u = sums[lane];                                    // (as many warps as lanes)
+  const T mine = u;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const T y = __shfl_up_sync(0xffffffffu, u, o);
+    if (lane >= o) u += y;
+  }
+  x += __shfl_sync(0xffffffffu, u - mine, warp);
+  return __shfl_sync(0xffffffffu, u, 31);
+}
+
+// ------------------------------------------------------------------------------------------------------------- plan
+__device__ void make_plan(const WeighArgs& p, int* sums, int64_t* sums2) {
+  const CacheFwdArgs& a = p.f;
+  const CacheView& c = a.c;
+  const int tid = threadIdx.x;
+  // (lists of new tokens that do not ascend: nothing is stored)
+  bool bad = false;
+  if (c.cu_new != nullptr)
+    for (int b = tid; b < c.B; b += kPlanThreads) bad |= c.cu_new[b] > c.cu_new[b + 1];
+  bad = __syncthreads_or(bad);
+  // ---- counted tokens
+  int base = 0;
+  for (int64_t t0 = 0; t0 < c.n_tokens; t0 += kPlanThreads) {
+    const int64_t t = t0 + tid;
+    int b = -1, first = 0, n = 0, length = 0;
+    if (t < c.n_tokens && !bad && (c.cu_new == nullptr || t >= c.cu_new[0])) {
+      b = c.cu_new == nullptr ? (int)t / c.Lq : last_not_above(c.cu_new, c.B, (int)t);
+      n = sequence(a, b, first, length);
+      if (n == 0 || t < first || t >= first + n) b = -1;
+    }
+    const int take = b >= 0 && (a.every || a.d[t] != 0) && length - n + (t - first) >= 0;
+    int x = take;
+    const int all = block_scan(x, sums), at = base + x - take;
+    if (take) p.list[at] = (int)t;
+    if (b >= 0 && t == first) p.list_start[b] = at;
+    if (b >= 0 && t == first + n - 1) p.list_end[b] = at + take;
+    base += all;
+  }
+  __syncthreads();
+  // ---- blocks of rows and key tiles of every sequence
+  int block_base = 0;
+  int64_t tile_base = 0;
+  for (int b0 = 0; b0 < c.B; b0 += kPlanThreads) {
+    const int b = b0 + tid;
+    int first, length = 0, n = 0;
+    if (b < c.B && !bad) n = sequence(a, b, first, length);
+    const int blocks = n > 0 ? compact_tiles(p.list_end[b] - p.list_start[b], a.G) : 0;
+    const int tiles = n > 0 ? (length + kTileN - 1) / kTileN : 0;
+    int x = blocks;
+    int64_t y = tiles;
+    const int all = block_scan(x, sums);
+    const int64_t all_tiles = block_scan(y, sums2);
+    if (b < c.B) {
+      p.block_start[b] = block_base + x - blocks;
+      p.tile_start[b] = tile_base + y - tiles;
+    }
+    block_base += all;
+    tile_base += all_tiles;
+  }
+  if (tid == 0) {
+    p.block_start[c.B] = block_base;
+    p.tile_start[c.B] = tile_base;
+  }
+  __syncthreads();
+  // ---- the blocks
+  int64_t units = 0;
+  for (int q0 = 0; q0 < block_base; q0 += kPlanThreads) {
+    const int q = q0 + tid;
+    RowBlock r;
+    r.tiles = 0;
+    if (q < block_base) {
+      int first, length;
+      r.b = last_not_above(p.block_start, c.B, q);     // (the last: it has blocks)
+      const int n = sequence(a, r.b, first, length);
+      r.list = p.list_start[r.b];
+      r.row0 = (q - p.block_start[r.b]) * kTileM;
+      r.n_rows = min(kTileM, (p.list_end[r.b] - r.list) * a.G - r.row0);
+      r.base = length - n - first;
+      r.first_pos = r.base + p.list[r.list + r.row0 / a.G];
+      r.last = r.base + p.list[r.list + (r.row0 + r.n_rows - 1) / a.G];
+      r.tiles = r.last / kTileN + 1;
+    }
+    int64_t x = r.tiles;
+    const int64_t all = block_scan(x, sums2);
+    if (q < block_base) {
+      r.units = units + x - r.tiles;
+      r.pad = 0;
+      p.blocks[q] = r;
+    }
+    units += all;
+  }
+  if (tid == 0) *p.plan = WeighPlan{block_base, units, tile_base};
+}
+
+// Keys of an 8- or 4-bit cache as bf16, pages of 128 tokens [page][KV head][128][D].  A lane brings 16 codes, a warp 512 / D keys at a time, 32
+// keys of a head in all.
+constexpr int kDecodeKeys = 32, kDecodeParts = kTileN / kDecodeKeys;
+template <int D, int kKind>
+__device__ __forceinline__ void decode_keys(const WeighArgs& p, int64_t item, int b) {
+  constexpr bool kE2M1 = kKind == L2A_CACHE_E2M1;
+  constexpr int kLanes = D / 16, kRows = 32 / kLanes, kSteps = kDecodeKeys / kRows;
+  const CacheFwdArgs& a = p.f;
+  const CacheView &c = p.codes, &out = a.c;
+  const int lane = threadIdx.x & 31, sub = lane % kLanes;
+  int first, length;
+  const int n = sequence(a, b, first, length);
+  if (n == 0) return;
+  const int part = (int)(item % kDecodeParts), head = (int)(item / kDecodeParts % c.Hkv);
+  const int64_t block = item / kDecodeParts / c.Hkv, key0 = block * kTileN + part * kDecodeKeys;
+  const bool inside = key0 < length;
+  uint4 x[kSteps];
+  uint32_t e[kSteps], t[kSteps];
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int64_t key = key0 + i * kRows + lane / kLanes;
+    x[i] = make_uint4(0, 0, 0, 0);
+    e[i] = t[i] = 0u;
+    const int page = inside && key < length ? cache_page(c, b, (int)key) : -1;
+    if (page < 0) continue;
+    const int in_page = (int)key & ((1 << c.page_shift) - 1);
+    const uint8_t* row = c.K + page * c.page_bytes + (((int64_t)head << c.page_shift) + in_page) * row_bytes(kKind, D);
+    const uint8_t* scales = c.ks + page * c.scale_stride;
+    e[i] = scales[exponent_at<D, kKind>(c, head, in_page)];
+    if (kE2M1) {
+      const uint2 y = *reinterpret_cast<const uint2*>(row + sub * 8);
+      x[i].x = y.x; x[i].y = y.y;
+      t[i] = scales[blocks_at<D>(c, head, in_page) + sub];
+    } else {
+      x[i] = *reinterpret_cast<const uint4*>(row + sub * 16);
+    }
+  }
+  // (looked up while the codes are on their way)
+  bool counts = a.every;
+  if (!a.every)
+    for (int i = threadIdx.x; i < n; i += kPlanThreads) counts |= a.d[first + i] != 0;
+  counts = __syncthreads_or(counts);
+  if (!inside || !counts) return;
+  uint8_t* dst = out.K + ((int64_t)b * out.table_stride + block) * out.page_bytes + ((int64_t)head * kTileN + part * kDecodeKeys) * (2 * D);
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    uint32_t o[8];
+    if (kE2M1) decode_16(make_uint2(x[i].x, x[i].y), e4m3_value(t[i]) * scale_of_exponent(e[i]), o);
+    else decode_16(x[i], scale_of_exponent(e[i]), o);
+    store_32(dst + (i * kRows + lane / kLanes) * (2 * D) + sub * 32, true, o);
+  }
+}
+
+template <int D, int kKind>
+__global__ void __launch_bounds__(kPlanThreads) weigh_plan_kernel(const WeighArgs p) {
+  dependency_wait();
+  dependents_release();
+  if (blockIdx.x == 0) {
+    if (blockIdx.y != 0) return;
+    __shared__ int sums[kPlanThreads / 32];
+    __shared__ int64_t sums2[kPlanThreads / 32];
+    if (p.clear && threadIdx.x == 0) *p.f.status = 0;
+    make_plan(p, sums, sums2);
+    return;
+  }
+  if (kKind != L2A_CACHE_BF16) decode_keys<D, kKind>(p, (int64_t)(blockIdx.x - 1) * (kPlanThreads / 32) + (threadIdx.x >> 5), blockIdx.y);
+}
+
+// A block of rows of one KV head, 16 bytes a thread and step; zeros behind the last
+constexpr int kRowsThreads = 256;
+template <int D>
+__global__ void __launch_bounds__(kRowsThreads) weigh_rows_kernel(const WeighArgs p) {
+  const CacheFwdArgs& a = p.f;
+  const int q = blockIdx.x, g = blockIdx.y, tid = threadIdx.x;
+  dependency_wait();
+  dependents_release();
+  if (q >= p.plan->n_blocks) return;
+  const RowBlock r = p.blocks[q];
+  constexpr int kPieces = D / 8, kSteps = kTileM * kPieces / kRowsThreads;
+  bf16* dst = p.rows + ((int64_t)g * p.most_blocks + q) * kTileM * D;
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int row = (i * kRowsThreads + tid) / kPieces, piece = tid % kPieces, x = r.row0 + row, token = x / a.G;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (row < r.n_rows) v = reinterpret_cast<const uint4*>(a.q + p.list[r.list + token] * a.q_t + (int64_t)(g * a.G + x - token * a.G) * D)[piece];
+    reinterpret_cast<uint4*>(dst + row * D)[piece] = v;
+  }
+  if (g == 0 && tid < kTileM) p.row_pos[q * kTileM + tid] = tid < r.n_rows ? r.base + p.list[r.list + (r.row0 + tid) / a.G] : -1;
+}
+
+// ------------------------------------------------------------------------------------------------------------- passes
+// A piece of work: a block of rows and some key tiles, or a key tile and some blocks of rows
+struct WeighPiece {
+  int b, g, x, y0, n;      // sequence, KV head, what is kept, the first of the n that pass
+  int slot;                // first pass
+  int length;
+};
+template <bool kSum>
+struct WeighWalk {
+  int64_t at, end, step, units;
+  int q, n_blocks;
+  __device__ __forceinline__ void init(const WeighArgs& p) {
+    const WeighPlan plan = *p.plan;
+    const int Hkv = p.f.c.Hkv;
+    n_blocks = plan.n_blocks;
+    q = -1;
+    if (kSum) {
+      at = blockIdx.x;
+      step = gridDim.x;
+      end = plan.tiles * Hkv;
+    } else {
+      units = plan.units;
+      const int64_t total = units * Hkv, share = (total + gridDim.x - 1) / gridDim.x;
+      at = min(total, blockIdx.x * share);
+      end = min(total, at + share);
+    }
+  }
+  __device__ __forceinline__ bool next(const WeighArgs& p, WeighPiece& w) {
+    const CacheView& c = p.f.c;
+    for (;;) {
+      if (at >= end) return false;
+      if (kSum) {
+        // the key tiles of a head of a sequence follow each other
+        int lo = 0, hi = c.B;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (p.tile_start[mid] * c.Hkv <= at) lo = mid; else hi = mid;
+        }
+        const int64_t before = p.tile_start[lo], tiles = p.tile_start[lo + 1] - before, in = at - before * c.Hkv;
+        w.b = lo;
+        w.g = (int)(in / tiles);
+        w.x = (int)(in % tiles);
+        // the blocks whose last row sees it: positions ascend
+        int first = p.block_start[lo], last = p.block_start[lo + 1];
+        w.n = last;
+        while (first < last) {
+          const int mid = (first + last) >> 1;
+          if (p.blocks[mid].tiles > w.x) last = mid; else first = mid + 1;
+        }
+        w.y0 = first;
+        w.n -= first;
+        w.slot = 0;
+        at += step;
+      } else {
+        const int64_t g = at / units, in = at - g * units;
+        if (q < 0) {
+          int lo = 0, hi = n_blocks;
+          while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (p.blocks[mid].units <= in) lo = mid; else hi = mid;
+          }
+          q = lo;
+        } else if (++q == n_blocks) {
+          q = 0;
+        }
+        const RowBlock& r = p.blocks[q];
+        w.b = r.b;
+        w.g = (int)g;
+        w.x = q;
+        w.y0 = (int)(in - r.units);
+        w.n = (int)min((int64_t)(r.tiles - w.y0), end - at);
+        w.slot = (int)g * n_blocks + q + blockIdx.x;
+        at += w.n;
+      }
+      w.length = cache_length(c, w.b);
+      return true;
+    }
+  }
+};
+
+struct PassBars {
+  uint64_t x_full[2], x_empty[2], y_full[kYStages], y_empty[kYStages], s_full[kScoreBufs], s_empty[kScoreBufs];
+  uint32_t tmem_base;
+  int abort_flag;
+};
+template <int D>
+struct PassSmem {
+  static constexpr int kTileBytes = 128 * D * 2;
+  static constexpr int kYOff = 2 * kTileBytes, kStageOff = kYOff + kYStages * kTileBytes;
+  static constexpr int kSumOff = kStageOff + kSumWarps * 1024;           // a warp's copy of what its columns need
+  static constexpr int kBarOff = kSumOff + 2 * 2 * 128 * 4;
+  static constexpr int kTotal = kBarOff + 256 + 1024 /* alignment slack */;
+};
+static_assert(sizeof(PassBars) <= 256, "barriers");
+
+// kSum: the second pass
+template <int D, bool kSum>
+__global__ void __launch_bounds__(kPassThreads, 1)
+weigh_pass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK, const WeighArgs p) {
+  using SM = PassSmem<D>;
+  const CacheFwdArgs& a = p.f;
+  const CacheView& c = a.c;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  PassBars* bar = reinterpret_cast<PassBars*>(smem + SM::kBarOff);
+  volatile int* abort_flag = &bar->abort_flag;
+  if (tid == kTmaWarp * 32) {
+    for (int i = 0; i < 2; ++i) { mbar_init(&bar->x_full[i], 1); mbar_init(&bar->x_empty[i], 1); }
+    for (int i = 0; i < kYStages; ++i) { mbar_init(&bar->y_full[i], 1); mbar_init(&bar->y_empty[i], 1); }
+    for (int i = 0; i < kScoreBufs; ++i) { mbar_init(&bar->s_full[i], 1); mbar_init(&bar->s_empty[i], 4); }
+    bar->abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == kMmaWarp) {
+    tmem_alloc(&bar->tmem_base, 512);
+    tmem_relinquish();
+  }
+  dependency_wait();
+  dependents_release();
+  const bool lost = kSum && *a.status != 0;      // a wait ran out in the first pass: nothing more is stored
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bar->tmem_base;
+  WeighWalk<kSum> walk;
+  walk.init(p);
+  if (lost) walk.at = walk.end;
+  WeighPiece w;
+  bool ok = true;
+
+  if (warp == kTmaWarp) {
+    // =========================================================================== TMA producer
+    if (lane == 0) {
+      tma_prefetch_desc(&mapQ);
+      tma_prefetch_desc(&mapK);
+    }
+    const int rows = 1 << c.page_shift, copies = 128 >> c.page_shift, u = lane % copies, piece = lane / copies;
+    const uint32_t bytes = rows * 128;
+    uint32_t x_cnt = 0, y_cnt = 0;
+    while (ok && walk.next(p, w)) {
+      if (w.n == 0) continue;
+      int entry0 = -512, page_ids = -1;
+      const int last_entry = (w.length - 1) >> c.page_shift;
+      auto load_k = [&](int tile, uint8_t* dst, uint64_t* full) {
+        const int first = (int)(((int64_t)tile * kTileN) >> c.page_shift), entry = first + u;
+        if (first < entry0 || first + copies - 1 - entry0 >= 32) {
+          entry0 = first;
+          const int e = entry0 + lane;
+          page_ids = e <= last_entry ? cache_page(c, w.b, e << c.page_shift) : -1;
+        }
+        const int page = __shfl_sync(0xffffffffu, page_ids, entry - entry0);
+        const bool load = piece < D / 64 && page >= 0 && entry <= last_entry;
+        const uint32_t expect = __popc(__ballot_sync(0xffffffffu, load)) * bytes;
+        if (lane == 0) mbar_expect_tx(full, expect);
+        __syncwarp();
+        if (load) tma_load_page(dst + piece * kBoxBytes + u * bytes, &mapK, full, false, piece, 0, w.g, page);
+      };
+      auto load_q = [&](int block, uint8_t* dst, uint64_t* full) {
+        if (lane == 0) {
+          mbar_expect_tx(full, SM::kTileBytes);
+          tma_load_4d(dst, &mapQ, full, 0, block * kTileM, 0, w.g);
+        }
+        __syncwarp();
+      };
+      auto load = [&](bool keys, int i, uint8_t* dst, uint64_t* full) {
+        if (keys) load_k(i, dst, full); else load_q(i, dst, full);
+      };
+      ok = mbar_wait_warp(&bar->x_empty[x_cnt & 1], ((x_cnt >> 1) & 1) ^ 1, abort_flag);
+      if (!ok) break;
+      load(kSum, w.x, smem + (x_cnt & 1) * SM::kTileBytes, &bar->x_full[x_cnt & 1]);
+      ++x_cnt;
+      for (int i = 0; i < w.n; ++i, ++y_cnt) {
+        const int s = y_cnt % kYStages;
+        ok = mbar_wait_warp(&bar->y_empty[s], ((y_cnt / kYStages) & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        load(!kSum, w.y0 + i, smem + SM::kYOff + s * SM::kTileBytes, &bar->y_full[s]);
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    // =========================================================================== MMA issuer
+    if (elect_one()) {
+      constexpr uint32_t idesc = idesc_bf16_f32(128, 128, 0, 0);
+      const uint64_t dx = smem_desc_sw128(smem_u32(smem), 16, 1024), dy = smem_desc_sw128(smem_u32(smem + SM::kYOff), 16, 1024);
+      uint32_t x_cnt = 0, cnt = 0;
+      while (ok && walk.next(p, w)) {
+        if (w.n == 0) continue;
+        const uint32_t xs = x_cnt & 1;
+        if (!mbar_spin(&bar->x_full[xs], (x_cnt >> 1) & 1, abort_flag)) break;
+        for (int i = 0; i < w.n; ++i, ++cnt) {
+          const uint32_t s = cnt % kYStages, buf = cnt % kScoreBufs;
+          if (!mbar_spin(&bar->s_empty[buf], ((cnt / kScoreBufs) & 1) ^ 1, abort_flag) ||
+              !mbar_spin(&bar->y_full[s], (cnt / kYStages) & 1, abort_flag)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint32_t o = ((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4;
+            mma_ss(tmem + buf * 128, dx + xs * (SM::kTileBytes >> 4) + o, dy + s * (SM::kTileBytes >> 4) + o, idesc, kk > 0);
+          }
+          tc_commit(&bar->s_full[buf]);
+          tc_commit(&bar->y_empty[s]);
+        }
+        if (!ok) break;
+        tc_commit(&bar->x_empty[xs]);
+        ++x_cnt;
+      }
+    }
+    __syncwarp();
+  } else {
+    // =========================================================================== soft-max
+    const int wg = warp >> 2, r = (warp & 3) * 32 + lane;       // row of the kept operand == TMEM lane
+    const uint32_t s_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    float* stage = reinterpret_cast<float*>(smem + SM::kStageOff + warp * 1024);
+    const int* stage_pos = reinterpret_cast<const int*>(stage + 128);
+    float* sums = reinterpret_cast<float*>(smem + SM::kSumOff);
+    const float2 scale = make_float2(a.scale_log2, a.scale_log2);
+    uint32_t cnt = 0, pieces = 0;
+    while (walk.next(p, w)) {
+      const int pos = kSum ? w.x * kTileN + r : p.row_pos[w.x * kTileM + r];
+      float m = -INFINITY, l = 0.f;
+      for (int i = 0; i < w.n; ++i, ++cnt) {
+        if ((cnt & 1) != wg) continue;
+        const uint32_t buf = cnt % kScoreBufs;
+        bool partial;                        // some pair of the tile is not seen
+        if (kSum) {
+          const int q = w.y0 + i;
+          partial = w.x * kTileN + kTileN - 1 > p.blocks[q].first_pos;
+          __syncwarp();
+          reinterpret_cast<float4*>(stage)[lane] = reinterpret_cast<const float4*>(p.minus_lse + ((int64_t)w.g * p.most_blocks + q) * kTileM)[lane];
+          if (partial) reinterpret_cast<int4*>(stage + 128)[lane] = reinterpret_cast<const int4*>(p.row_pos + q * kTileM)[lane];
+          __syncwarp();
+        } else {
+          partial = __any_sync(0xffffffffu, (w.y0 + i) * kTileN + kTileN - 1 > pos);
+        }
+        if (!mbar_wait_warp(&bar->s_full[buf], (cnt / kScoreBufs) & 1, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        uint32_t v[4][32];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tmem_ld32(s_addr + buf * 128 + q * 32, v[q]);
+        tmem_ld_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar->s_empty[buf]);
+        float2 sum[2] = {};
+        if (kSum) {
+          const uint32_t at = smem_u32(stage);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            if (partial) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) v[q][e] = stage_pos[q * 32 + e] >= pos ? v[q][e] : 0xff800000u;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float4 z = lds128(at + (q * 8 + e) * 16);
+              const float2 y0 = __ffma2_rn(make_float2(__uint_as_float(v[q][4 * e]), __uint_as_float(v[q][4 * e + 1])), scale, make_float2(z.x, z.y));
+              const float2 y1 = __ffma2_rn(make_float2(__uint_as_float(v[q][4 * e + 2]), __uint_as_float(v[q][4 * e + 3])), scale, make_float2(z.z, z.w));
+              sum[0] = __fadd2_rn(sum[0], make_float2(fast_exp2(y0.x), fast_exp2(y0.y)));
+              sum[1] = __fadd2_rn(sum[1], e % 2 ? exp2_fma2(y1) : make_float2(fast_exp2(y1.x), fast_exp2(y1.y)));
+            }
+          }
+          l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+        } else {
+          if (partial) {
+            const int k0 = (w.y0 + i) * kTileN;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const uint32_t visible = bit_range(0, pos + 1 - k0 - q * 32);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) v[q][e] = (visible >> e) & 1u ? v[q][e] : 0xff800000u;
+            }
+          }
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) mx[q] = fmax3(mx[q], __uint_as_float(v[q][e]), __uint_as_float(v[q][e + 1]));
+          }
+          const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2);
+          const float neg = m_new == -INFINITY ? 0.f : -m_new;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[q][2 * e]), __uint_as_float(v[q][2 * e + 1])), scale, make_float2(neg, neg));
+              sum[e & 1] = __fadd2_rn(sum[e & 1], e % 4 == 3 ? exp2_fma2(y) : make_float2(fast_exp2(y.x), fast_exp2(y.y)));
+            }
+          }
+          l = l * fast_exp2(m + neg) + ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
+          m = m_new;
+        }
+      }
+      if (!kSum) {
+        if (!ok) break;
+        p.part[((int64_t)w.slot * 2 + wg) * kTileM + r] = make_float2(m, l);
+        continue;
+      }
+      // ---- both warpgroups' sums, four keys a thread.  (All warps leave together where a wait ran out.)
+      float* mine = sums + (pieces & 1) * 256;
+      ++pieces;
+      mine[wg * 128 + r] = l;
+      if (!named_barrier_all(1, kSumWarps * 32, ok)) break;
+      if (warp == 0) {
+        const float4 x = reinterpret_cast<const float4*>(mine)[lane], y = reinterpret_cast<const float4*>(mine + 128)[lane];
+        const float four[4] = {x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w};
+        int first;
+        const int n = cache_new(c, w.b, first), hi = w.n > 0 ? p.blocks[p.block_start[w.b + 1] - 1].last : -1;
+        add_weights(a, p.codes, w.b, w.g, w.x * kTileN + 4 * lane, w.length, w.length - n, hi, four);
+      }
+    }
+  }
+
+  // ---- teardown
+  tc_fence_before();
+  __syncthreads();
+  if (bar->abort_flag) {
+    // a bounded wait ran out: give copies still in flight time to land before shared memory is released
+    const uint64_t t0 = globaltimer_ns();
+    while (globaltimer_ns() - t0 < 200000ull) __nanosleep(1000);
+    if (tid == 0) atomicExch(a.status, 1);
+    __syncthreads();
+  }
+  if (warp == kMmaWarp) tmem_dealloc(tmem, 512);
+}
+
+// Minus log2 of the sum of a row's weights, from the ranges that have seen a part of its keys
+__global__ void __launch_bounds__(kTileM) weigh_join_kernel(const WeighArgs p) {
+  const int q = blockIdx.x, g = blockIdx.y, r = threadIdx.x;
+  dependency_wait();
+  dependents_release();
+  const WeighPlan plan = *p.plan;
+  if (q >= plan.n_blocks) return;
+  const int64_t total = plan.units * p.f.c.Hkv, share = (total + kCtas - 1) / kCtas;
+  const int64_t at = g * plan.units + p.blocks[q].units, c0 = at / share, c1 = (at + p.blocks[q].tiles - 1) / share;
+  float m = -INFINITY, l = 0.f;
+  for (int64_t cta = c0; cta <= c1; ++cta) {
+    const int64_t slot = (int64_t)g * plan.n_blocks + q + cta;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const float2 x = p.part[(slot * 2 + i) * kTileM + r];
+      const float M = fmaxf(m, x.x), base = M == -INFINITY ? 0.f : M;
+      l = l * fast_exp2(m - base) + x.y * fast_exp2(x.x - base);
+      m = M;
+    }
+  }
+  const bool row = r < p.blocks[q].n_rows;
+  p.minus_lse[((int64_t)g * p.most_blocks + q) * kTileM + r] = row && l != 0.f ? -(m + log2f(l)) : -INFINITY;
+}
+
+// ------------------------------------------------------------------------------------------------------------- host
+int64_t most_blocks(const l2a_params* p, int n_tokens) { return ((int64_t)n_tokens * (p->Hq / p->Hkv) + kTileM - 1) / kTileM + p->B; }
+int64_t key_tiles(int Lk) { return ((int64_t)Lk + kTileN - 1) / kTileN; }
+size_t layout(const l2a_params* p, int kind, int n_tokens, uint8_t* base, WeighArgs* w, uint8_t** copy) {
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    uint8_t* x = base + at;
+    at += align_up(bytes, 256);
+    return x;
+  };
+  const size_t blocks = (size_t)most_blocks(p, n_tokens), B = p->B, Hkv = p->Hkv;
+  WeighArgs x = {};
+  x.plan = reinterpret_cast<WeighPlan*>(take(sizeof(WeighPlan)));
+  x.blocks = reinterpret_cast<RowBlock*>(take(blocks * sizeof(RowBlock)));
+  x.list = reinterpret_cast<int*>(take((size_t)n_tokens * 4));
+  x.list_start = reinterpret_cast<int*>(take(B * 4));
+  x.list_end = reinterpret_cast<int*>(take(B * 4));
+  x.block_start = reinterpret_cast<int*>(take((B + 1) * 4));
+  x.tile_start = reinterpret_cast<int64_t*>(take((B + 1) * 8));
+  x.row_pos = reinterpret_cast<int*>(take(blocks * kTileM * 4));
+  x.minus_lse = reinterpret_cast<float*>(take(Hkv * blocks * kTileM * 4));
+  x.part = reinterpret_cast<float2*>(take((Hkv * blocks + kCtas) * 2 * kTileM * 8));
+  x.rows = reinterpret_cast<bf16*>(take(Hkv * blocks * kTileM * p->D * 2));
+  x.most_blocks = (int)blocks;
+  uint8_t* decoded = take(kind == L2A_CACHE_BF16 ? 0 : B * Hkv * (size_t)key_tiles(p->Lk) * kTileN * p->D * 2);
+  if (w) {
+    *w = x;
+    *copy = decoded;
+  }
+  return at;
+}
+
+// Rows of a sequence up to which its scores are kept: as many as the kernel of the few rows takes, less where the workspace for the scores of all
+// sequences would pass kMostScores.
+constexpr int64_t kMostScores = 4ll << 30;
+int kept_rows(const l2a_params* p) {
+  const int64_t G = p->Hq / p->Hkv, all = (int64_t)p->Lq * G;
+  for (int rows = kRowBlocks * kBlockRows; rows >= kBlockRows; rows -= kBlockRows)
+    if (rows >= G && (double)p->B * p->Hkv * (double)std::min<int64_t>(rows, all) * (p->Lk + 64.0) * 4 <= (double)kMostScores) return rows;
+  return 0;
+}
+int most_kept(const l2a_params* p) { return (int)std::min<int64_t>(kept_rows(p), (int64_t)p->Lq * (p->Hq / p->Hkv)); }
+size_t few_bytes(const l2a_params* p) { return most_kept(p) > 0 ? align_up(cache_few_weigh_ws_bytes(p, most_kept(p)), 256) : 0; }
+bool has_blocks(const l2a_params* p) { return (int64_t)p->Lq * (p->Hq / p->Hkv) > kept_rows(p); }
+
+template <int D, bool kSum>
+cudaError_t launch_pass(const CUtensorMap& mapQ, const CUtensorMap& mapK, const WeighArgs& p, cudaStream_t s) {
+  constexpr int smem = PassSmem<D>::kTotal;
+  static PerDeviceOnce once;
+  const cudaError_t e = once.run([] { return cudaFuncSetAttribute(weigh_pass_kernel<D, kSum>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem); });
+  return e != cudaSuccess ? e : launch_dependent(weigh_pass_kernel<D, kSum>, dim3(kCtas), kPassThreads, smem, s, true, mapQ, mapK, p);
+}
+
+template <int D, int kKind>
+cudaError_t launch_plan(const WeighArgs& p, bool first, cudaStream_t s) {
+  const int64_t items = kKind == L2A_CACHE_BF16 ? 0 : (int64_t)p.f.c.table_stride * p.f.c.Hkv * kDecodeParts, per = kPlanThreads / 32;
+  return launch_dependent(weigh_plan_kernel<D, kKind>, dim3((unsigned)(1 + (items + per - 1) / per), items ? p.f.c.B : 1), kPlanThreads, 0, s, !first, p);
+}
+
+template <int D>
+cudaError_t launch_blocks(const WeighArgs& p, bool first, cudaStream_t s) {
+  CUtensorMap mapQ, mapK;
+  if (!encode_rows_map(&mapQ, p.rows, p.f.c.Hkv, p.most_blocks * kTileM, D, kTileM, D) || !encode_pool_map(&mapK, p.f.c, p.f.c.K, 1 << p.f.c.page_shift, 1))
+    return cudaErrorUnknown;
+  cudaError_t e = p.codes.kind == L2A_CACHE_BF16   ? launch_plan<D, L2A_CACHE_BF16>(p, first, s)
+                  : p.codes.kind == L2A_CACHE_E4M3 ? launch_plan<D, L2A_CACHE_E4M3>(p, first, s)
+                                                   : launch_plan<D, L2A_CACHE_E2M1>(p, first, s);
+  const dim3 grid(p.most_blocks, p.f.c.Hkv);
+  if (e == cudaSuccess) e = launch_dependent(weigh_rows_kernel<D>, grid, kRowsThreads, 0, s, true, p);
+  if (e == cudaSuccess) e = launch_pass<D, false>(mapQ, mapK, p, s);
+  if (e == cudaSuccess) e = launch_dependent(weigh_join_kernel, grid, kTileM, 0, s, true, p);
+  if (e == cudaSuccess) e = launch_pass<D, true>(mapQ, mapK, p, s);
+  return e;
+}
+
+int64_t row_stride(const int64_t (&s)[2], int row_elems) {
+  if (s[0] != 0 || s[1] < 0) return 0;
+  const int64_t t = s[1] ? s[1] : row_elems;
+  return t >= row_elems && t % 8 == 0 ? t : 0;
+}
+
+l2a_status check_weigh(const l2a_params* p, const l2a_cache* c, int n_tokens, CacheView* v) {
+  const int32_t some = 0;
+  const l2a_status st = cache_view(p, c, &some, n_tokens, v);
+  if (st != L2A_OK) return st;
+  if (p->flags & ~L2A_FLAG_SHARED_WINDOW) return L2A_ERR_INVALID_ARG;
+  if ((int64_t)n_tokens * p->Hq >= (1ll << 31) - 32 || p->B > 65535 || p->Hkv > 65535) return L2A_ERR_UNSUPPORTED;
+  if (most_kept(p) > 0 && !cache_few_counts(p)) return L2A_ERR_UNSUPPORTED;
+  // (slots and rows of the blocks are counted in 32 bits, as are the CTAs that decode)
+  if (has_blocks(p) && ((most_blocks(p, n_tokens) * p->Hkv + kCtas) >= (1ll << 31) || most_blocks(p, n_tokens) >= (1ll << 31) / kTileM ||
+                        key_tiles(p->Lk) * p->Hkv >= (1ll << 31)))
+    return L2A_ERR_UNSUPPORTED;
+  return L2A_OK;
+}
+size_t weigh_ws_bytes(const l2a_params* p, int kind, int n_tokens) {
+  return kWsHeaderBytes + few_bytes(p) + (has_blocks(p) ? layout(p, kind, n_tokens, nullptr, nullptr, nullptr) : 0);
+}
+
+}  // namespace
+}  // namespace l2a
+
+using namespace l2a;
+
+extern "C" l2a_status l2a_cache_weigh_workspace_bytes(const l2a_params* p, const l2a_cache* c, int n_tokens, size_t* ws_bytes) {
+  CacheView v;
+  const l2a_status st = check_weigh(p, c, n_tokens, &v);
+  if (st != L2A_OK) return st;
+  if (!ws_bytes) return L2A_ERR_INVALID_ARG;
+  *ws_bytes = weigh_ws_bytes(p, c->kind, n_tokens);
+  return L2A_OK;
+}
+
+extern "C" l2a_status l2a_cache_weigh(const l2a_params* p, const l2a_cache* c, const void* Q, const int32_t* cu_new, int n_tokens,
+                                      const uint8_t* d, float* weights, int64_t weight_stride, void* ws, size_t ws_bytes, void* stream) {
+  CacheFwdArgs a = {};
+  l2a_status st = check_weigh(p, c, n_tokens, &a.c);
+  if (st == L2A_OK) st = cache_view(p, c, cu_new, n_tokens, &a.c);
+  if (st != L2A_OK) return st;
+  a.q_t = row_stride(p->q_stride, p->Hq * p->D);
+  if (a.q_t == 0) return L2A_ERR_INVALID_ARG;
+  const int64_t dense = (int64_t)p->Hkv * c->page_size;
+  a.w_page = weight_stride ? weight_stride : dense;
+  if (a.w_page < dense) return L2A_ERR_INVALID_ARG;
+  if (!ws || (reinterpret_cast<uintptr_t>(ws) % 256) != 0 || ws_bytes < weigh_ws_bytes(p, c->kind, n_tokens)) return L2A_ERR_WORKSPACE;
+  if (n_tokens == 0) return L2A_OK;
+  if (!Q || !weights || (reinterpret_cast<uintptr_t>(Q) & 15) || (reinterpret_cast<uintptr_t>(weights) & 3)) return L2A_ERR_INVALID_ARG;
+  a.Hq = p->Hq;
+  a.G = p->Hq / p->Hkv;
+  a.scale_log2 = (p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->D)) * 1.4426950408889634f;
+  a.global = 1;
+  a.every = d == nullptr;
+  a.q = static_cast<const bf16*>(Q);
+  a.d = d;
+  a.weights = weights;
+  a.status = static_cast<int*>(ws);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  uint8_t* at = static_cast<uint8_t*>(ws) + kWsHeaderBytes;
+  a.few_rows = kept_rows(p);
+  const bool blocks = has_blocks(p);
+  // With as many tokens as there can be no sequence is expected to have few rows (as in l2a_cache_forward)
+  const bool few = a.few_rows > 0 && !(blocks && (int64_t)p->B * p->Lq == n_tokens);
+  if (!few) a.few_rows = 0;
+  cudaError_t e = few ? launch_cache_few_weigh(a, at, s) : cudaSuccess;
+  if (e == cudaSuccess && blocks) {
+    WeighArgs w;
+    uint8_t* copy;
+    layout(p, c->kind, n_tokens, at + few_bytes(p), &w, &copy);
+    w.f = a;
+    w.codes = a.c;
+    w.clear = !few;
+    if (c->kind != L2A_CACHE_BF16) {
+      CacheView& v = w.f.c;
+      v.kind = L2A_CACHE_BF16;
+      v.K = copy;
+      v.page_bytes = (int64_t)v.Hkv * kTileN * v.D * 2;
+      v.page_shift = 7;
+      v.table = nullptr;
+      v.table_stride = (int)key_tiles(p->Lk);
+      v.n_pages = v.B * v.table_stride;
+    }
+    e = p->D == 128 ? launch_blocks<128>(w, !few, s) : launch_blocks<64>(w, !few, s);
+  }
+  return e == cudaSuccess ? L2A_OK : L2A_ERR_CUDA;
+}

@@ -36,7 +36,7 @@ EXPORTS = (
     "l2a_backward_split", "l2a_router_backward", "l2a_forward_routed", "l2a_selftest_wait_timeout",
     "l2a_forward_sets", "l2a_backward_sets", "l2a_pack_sequences", "l2a_step_host_async", "l2a_step_host_wait",
     "l2a_cache_append", "l2a_cache_read", "l2a_cache_workspace_bytes", "l2a_cache_forward",
-    "l2a_cache_evict_workspace_bytes", "l2a_cache_evict",
+    "l2a_cache_weigh_workspace_bytes", "l2a_cache_weigh", "l2a_cache_evict_workspace_bytes", "l2a_cache_evict",
 )
 
 
@@ -85,6 +85,8 @@ _SIGNATURES = {
     "l2a_cache_read": "pppppp",
     "l2a_cache_workspace_bytes": "ppip",
     "l2a_cache_forward": "pppp" + "i" + "pp" + "pzp",
+    "l2a_cache_weigh_workspace_bytes": "ppip",
+    "l2a_cache_weigh": "pppp" + "ippl" + "pzp",
     "l2a_cache_evict_workspace_bytes": "ppp",
     "l2a_cache_evict": "pppl" + "pii" + "pplpp" + "pzp",
 }
@@ -297,6 +299,23 @@ def _weight_stride(weights, cache):
     if weights.dtype != torch.float32 or weights.shape != K.shape[:3] or weights.stride()[1:] != (K.shape[2], 1):
         raise ValueError("weights of a cache: fp32 [pages, Hkv, page size], dense pages")
     return weights.stride(0) if weights.shape[0] > 1 else 0
+
+
+def l2a_cache_weigh_workspace_bytes(p, cache, n_tokens) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().l2a_cache_weigh_workspace_bytes(ctypes.byref(p), ctypes.byref(cache), n_tokens, ctypes.byref(n)),
+           "l2a_cache_weigh_workspace_bytes")
+    return n.value
+
+
+def l2a_cache_weigh(p, cache, Q, cu_new, n_tokens, d, weights, ws, stream=None, check=True) -> int:
+    """Adds to the weights (fp32 [pages, Hkv, page size]) of the cached keys what the Global Attention of the new tokens that count (d; None: all)
+    gives them; those of the new tokens' own keys start at zero."""
+    code = lib().l2a_cache_weigh(ctypes.byref(p), ctypes.byref(cache), _addr(Q), _addr(cu_new), n_tokens, _addr(d), _addr(weights),
+                                 _weight_stride(weights, cache), _addr(ws), _bytes(ws), _raw_stream(stream))
+    if check:
+        _check(code, "l2a_cache_weigh")
+    return code
 
 
 def l2a_cache_evict_workspace_bytes(p, cache) -> int:
