@@ -30,6 +30,7 @@
 // A lone short sequence is latency (9001 keys: 13.3 us, of which this kernel 9.2; the dense l2a_decode, which knows its lengths on the host,
 // takes 7.6 in 16 bits): lists, lengths and decisions are read by every CTA ahead of its first copy.  Tried: two chains of products 206 us
 // against 196; the loads of V ahead of the soft-max, no change; pieces and rows of Q handed over by the producer, 14.2 against 13.0 for 9001 keys.
+#include <cuda_fp16.h>
 #include <math.h>
 
 #include <algorithm>
@@ -45,7 +46,11 @@ constexpr int kComputeWarps = kTile / 16;
 constexpr int kThreads = (kComputeWarps + 1) * 32;
 constexpr int kMaxStages = 6;
 constexpr int kMinTiles = 4;                 // tiles of a CTA at least (9001 keys, 28/4 heads: 12.6 us; with 2 14.1, 3 13.1, 6 13.8)
-constexpr int kCtas = 2 * kSplitSms;
+// CTAs of an SM: registers allow no more (five warps each)
+__host__ __device__ constexpr int ctas_per_sm(int kind, bool high, bool weigh) {
+  return weigh ? (high && kind == L2A_CACHE_E2M1 ? 2 : 3) : kind == L2A_CACHE_E2M1 && !high ? 3 : 2;
+}
+constexpr int kMostCtas = 3 * kSplitSms;
 constexpr float kWeightTop = 10.f;           // log2 of the largest weight when the reference is new (fp16 operands)
 constexpr float kLag = 4.f;                  // the reference follows the maximum when it is more than this behind
 
@@ -154,8 +159,8 @@ struct Piece {
 // Tiles of a CTA, for `total` tiles of `pairs` blocks of rows and KV heads: an even share, but at least kMinTiles of them or all of a pair
 // (a part more costs the combination about what a tile does), and where it covers several pairs of the average length, whole ones, whose
 // results need no combination.
-__device__ __forceinline__ int tiles_per_cta(int total, int pairs) {
-  const int share = max(1, (total + kCtas - 1) / kCtas), pair = max(1, total / max(pairs, 1));
+__device__ __forceinline__ int tiles_per_cta(int total, int pairs, int ctas) {
+  const int share = max(1, (total + ctas - 1) / ctas), pair = max(1, total / max(pairs, 1));
   return share >= pair ? (share + pair - 1) / pair * pair : max(share, min(kMinTiles, pair));
 }
 
@@ -195,10 +200,308 @@ __device__ __forceinline__ bool next_piece(const CacheFwdArgs& a, Walk& w, Piece
   return true;
 }
 
+__device__ __forceinline__ uint32_t move_matrix_t(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+// Both halves of a times the lower (upper) half of f
+__device__ __forceinline__ uint32_t mul_by_half(uint32_t a, __half2 f, bool upper) {
+  const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&a), upper ? __high2half2(f) : __low2half2(f));
+  return *reinterpret_cast<const uint32_t*>(&x);
+}
+
+// The tiles of a piece over an e2m1 cache, for one warp: 16 keys of each.  The keys are the 16 rows of the products' A fragments and the query
+// rows the 8 columns of B, so that up to eight rows take half as many products and accumulators as with the roles of the other kinds; S^T comes out of one
+// product and goes, transposed, into the other:
+//   S^T = K Q^T : a lane takes a quarter of the codes of two keys, consecutive ones, as its elements of successive products (Q has the same order).
+//   O^T = V^T P^T : a lane has a group of D / 8 columns; two keys' codes of a column are put side by side in a byte.
+// A code becomes fp16 and is multiplied by the scale of its block, both exactly (6 bits); exponents are as in the 8-bit kind.  The maxima are
+// followed only where a row is more than kLag above what it had, so that no lane needs another's scores otherwise.
+// red: of this warp [rows][D + 4] sums, maximum, sum of weights, reference; kWeigh: [rows] maximum and sum.
+template <int D, bool kHigh, bool kWeigh>
+__device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewSeq& seq, const Piece& p, const uint8_t* smem, const uint8_t* scales,
+                                               int stages, FewBars* bar, int& s, int& ph, float* red) {
+  using SM = FewSmem<D, L2A_CACHE_E2M1, kWeigh>;
+  constexpr int kHalves = kHigh ? 2 : 1, kCols = D / 8, kVWords = D / 64, kKWords = D / 32;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, hr = lane >> 2, t4 = lane & 3, r0 = warp * 16;
+  volatile int* abort_flag = &bar->abort_flag;
+  // ---- B fragments of Q: row hr (and hr + 8), this lane's quarter of its elements, the largest of the row at 2^14 .. 2^15
+  uint32_t qb[kHalves][D / 16][2];
+  float row_scale[kHalves][2];                 // of the rows 2 t4, 2 t4 + 1 (and + 8)
+#pragma unroll
+  for (int x = 0; x < kHalves; ++x) {
+    const int r = p.block * kBlockRows + hr + 8 * x, i = r / a.G;
+    const bool ok = i < seq.n;
+    const bf16* qrow = a.q + (seq.first + (ok ? i : 0)) * a.q_t + (int64_t)(p.g * a.G + r % a.G) * D;
+    uint32_t v[kVWords][8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int k = 0; k < kVWords; ++k) {
+      load_32(qrow + (t4 * kVWords + k) * 16, false, v[k]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = __vmaxu2(top, v[k][j] & 0x7fff7fffu);
+    }
+    top = max(top & 0xffffu, top >> 16);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int up = min(max(14 + 127 - (int)(top >> 7), -113), 100);
+    const float f = ok ? __uint_as_float((uint32_t)(up + 127) << 23) : 0.f;
+    const float scale = a.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23);
+    row_scale[x][0] = __shfl_sync(0xffffffffu, scale, t4 * 8);
+    row_scale[x][1] = __shfl_sync(0xffffffffu, scale, t4 * 8 + 4);
+#pragma unroll
+    for (int k = 0; k < kVWords; ++k)
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        qb[x][k * 4 + j / 2][j & 1] = pack_f16(__uint_as_float(v[k][j] << 16) * f, __uint_as_float(v[k][j] & 0xffff0000u) * f);
+  }
+  // ---- the keys that each row sees in this segment
+  int row_lo[kHalves][2], row_hi[kHalves][2], every_lo = p.lo, every_hi = p.hi;
+#pragma unroll
+  for (int x = 0; x < kHalves; ++x)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const int i = (p.block * kBlockRows + 2 * t4 + y + 8 * x) / a.G, pos = seq.length - seq.n + i;
+      row_lo[x][y] = 0;
+      row_hi[x][y] = -1;
+      if (i >= seq.n) continue;
+      if (p.seg == 0) {
+        row_lo[x][y] = pos - a.window;
+        row_hi[x][y] = pos;
+      } else if (a.every || a.d[seq.first + i] != 0) {
+        row_hi[x][y] = pos - a.shift;
+      }
+      every_lo = max(every_lo, row_lo[x][y]);
+      every_hi = min(every_hi, row_hi[x][y]);
+    }
+  every_lo = __reduce_max_sync(0xffffffffu, every_lo);
+  every_hi = __reduce_min_sync(0xffffffffu, every_hi);
+
+  float m[kHalves][2], l[kHalves][2], ref[kHalves][2];     // maxima and sums of the weights; references of the accumulators
+  float acc[kHalves][kCols / 2][4];
+#pragma unroll
+  for (int x = 0; x < kHalves; ++x) {
+    m[x][0] = m[x][1] = ref[x][0] = ref[x][1] = -INFINITY;
+    l[x][0] = l[x][1] = 0.f;
+#pragma unroll
+    for (int j = 0; j < kCols / 2; ++j) acc[x][j][0] = acc[x][j][1] = acc[x][j][2] = acc[x][j][3] = 0.f;
+  }
+  bool ok = true;
+  for (int t = p.t0; t < p.t1; ++t) {
+    if (!mbar_wait_warp(&bar->full[s], ph, abort_flag)) { ok = false; break; }
+    const int key0 = t * kTile + r0;               // first key of this warp's 16
+    if (key0 <= p.hi && key0 + 15 >= p.lo) {
+      const uint32_t tK = smem_u32(smem) + s * SM::kStageBytes, tScale = smem_u32(scales) + s * SM::kScaleBytes;
+      const uint32_t tBlocks = tScale + SM::kTensors * kTile;
+      const bool edge = key0 < every_lo || key0 + 15 > every_hi;
+      // ---- S^T
+      float sc[kHalves][4] = {};
+      {
+        uint32_t w[2][kKWords];
+        __half2 f[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int row = r0 + hr + 8 * k;
+          uint32_t both, none;
+          if (D == 128) {
+            const float4 y = lds128(tK + row * 64 + ((t4 ^ ((row >> 1) & 3)) << 4));
+            w[k][0] = __float_as_uint(y.x); w[k][1] = __float_as_uint(y.y);
+            w[k][kKWords - 2] = __float_as_uint(y.z); w[k][kKWords - 1] = __float_as_uint(y.w);
+            e4m3x4_to_f16(lds16(tBlocks + row * 8 + t4 * 2), both, none);
+          } else {
+            lds64(tK + row * 32 + (((t4 >> 1) ^ ((row >> 2) & 1)) << 4) + (t4 & 1) * 8, w[k][0], w[k][1]);
+            e4m3x4_to_f16(lds8(tBlocks + row * 4 + t4), both, none);
+          }
+          f[k] = *reinterpret_cast<const __half2*>(&both);
+        }
+#pragma unroll
+        for (int i = 0; i < kKWords; ++i) {
+          uint32_t h[2][4];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            e2m1x8_to_f16(w[k][i], h[k]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) h[k][j] = mul_by_half(h[k][j], f[k], i >= 2);
+          }
+          const uint32_t a0[4] = {h[0][0], h[1][0], h[0][1], h[1][1]}, a1[4] = {h[0][2], h[1][2], h[0][3], h[1][3]};
+#pragma unroll
+          for (int x = 0; x < kHalves; ++x) {
+            mma_16816<true>(sc[x], a0, qb[x][2 * i][0], qb[x][2 * i][1]);
+            mma_16816<true>(sc[x], a1, qb[x][2 * i + 1][0], qb[x][2 * i + 1][1]);
+          }
+        }
+      }
+      const float fk[2] = {scale_of_exponent(lds8(tScale + r0 + hr)), scale_of_exponent(lds8(tScale + r0 + hr + 8))};
+      float v[kHalves][4];                         // keys hr (0, 1) and hr + 8 (2, 3), rows 2 t4 and 2 t4 + 1
+#pragma unroll
+      for (int x = 0; x < kHalves; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          v[x][y] = sc[x][y] * fk[y >> 1] * row_scale[x][y & 1];
+          const int j = key0 + hr + (y >> 1) * 8;
+          if (edge && (j < row_lo[x][y & 1] || j > row_hi[x][y & 1])) v[x][y] = -INFINITY;
+        }
+      if constexpr (kWeigh) {
+#pragma unroll
+        for (int x = 0; x < kHalves; ++x)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            if (row_hi[x][y] >= 0) {
+              float* dst = a.scores + ((int64_t)(p.b * a.c.Hkv + p.g) * a.score_rows + p.block * kBlockRows + 2 * t4 + y + 8 * x) * a.score_pitch +
+                           key0 + hr;
+              dst[0] = v[x][y];
+              dst[8] = v[x][2 + y];
+            }
+            // (each lane by itself: its keys are joined with the others' at the end)
+            const float m_new = fmaxf(m[x][y], fmaxf(v[x][y], v[x][2 + y])), base = m_new == -INFINITY ? 0.f : m_new;
+            l[x][y] = l[x][y] * fast_exp2(m[x][y] - base) + (fast_exp2(v[x][y] - base) + fast_exp2(v[x][2 + y] - base));
+            m[x][y] = m_new;
+          }
+      } else {
+        // ---- weights: u is what they are two to the power of, relative to the reference
+        const uint32_t tV = tK + SM::kTileBytes;
+        uint32_t ev[2] = {lds8(tScale + kTile + r0 + hr), lds8(tScale + kTile + r0 + hr + 8)};
+        const float vexp[2] = {__uint_as_float(0x4b000000u | ev[0]) - 8388735.f, __uint_as_float(0x4b000000u | ev[1]) - 8388735.f};   // ev - 127
+        float u[kHalves][4];
+        bool grow = false;
+#pragma unroll
+        for (int x = 0; x < kHalves; ++x) {
+#pragma unroll
+          for (int y = 0; y < 4; ++y) u[x][y] = v[x][y] + vexp[y >> 1];
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            grow |= fmaxf(v[x][y], v[x][2 + y]) > m[x][y] + kLag || fmaxf(u[x][y], u[x][2 + y]) > ref[x][y] + kLag;
+        }
+        // a lane's share of the codes of one of its four keys' values (key0 + 2 t4 + {0, 1, 8, 9})
+        auto value_codes = [&](int row, uint32_t (&w)[kVWords]) {
+          if (D == 128) lds64(tV + row * 64 + (((hr >> 1) ^ ((row >> 1) & 3)) << 4) + (hr & 1) * 8, w[0], w[kVWords - 1]);
+          else w[0] = lds32(tV + row * 32 + (((hr >> 2) ^ ((row >> 2) & 1)) << 4) + (hr & 3) * 4);
+        };
+        if (__any_sync(0xffffffffu, grow)) {
+          // Values of zeros have exponent 0 however small all others are: they must not become the reference, which would push the
+          // weights of the others out of fp16's range.  They get the least exponent.
+          if (__any_sync(0xffffffffu, ev[0] == 127u || ev[1] == 127u)) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              uint32_t any = 0;
+              const uint32_t row = tV + (r0 + hr + 8 * k) * (D / 2) + t4 * (D / 8);      // (a quarter of the row's bytes, in whatever order)
+#pragma unroll
+              for (int i = 0; i < kKWords; ++i) any |= lds32(row + 4 * i) & 0x77777777u;
+              any |= __shfl_xor_sync(0xffffffffu, any, 1);
+              any |= __shfl_xor_sync(0xffffffffu, any, 2);
+#pragma unroll
+              for (int x = 0; x < kHalves; ++x)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) u[x][2 * k + y] -= any != 0 ? 0.f : 127.f;
+            }
+          }
+#pragma unroll
+          for (int x = 0; x < kHalves; ++x)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              float top = fmaxf(u[x][y], u[x][2 + y]), m_new = fmaxf(v[x][y], v[x][2 + y]);
+#pragma unroll
+              for (int o = 4; o < 32; o <<= 1) {
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                m_new = fmaxf(m_new, __shfl_xor_sync(0xffffffffu, m_new, o));
+              }
+              if (m_new > m[x][y] + kLag) {
+                l[x][y] *= fast_exp2(m[x][y] - m_new);       // 0 the first time
+                m[x][y] = m_new;
+              }
+              if (top > ref[x][y] + kLag) {
+                const float alpha = fast_exp2(ref[x][y] - top);
+                ref[x][y] = top;
+#pragma unroll
+                for (int j = 0; j < kCols / 2; ++j) {
+                  acc[x][j][y] *= alpha;
+                  acc[x][j][2 + y] *= alpha;
+                }
+              }
+            }
+        }
+        uint32_t pb[kHalves][2];                   // B fragments of P^T
+#pragma unroll
+        for (int x = 0; x < kHalves; ++x) {
+          float w[4];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const float base = m[x][y] == -INFINITY ? 0.f : m[x][y], zero = (ref[x][y] == -INFINITY ? 0.f : ref[x][y]) - kWeightTop;
+            l[x][y] += fast_exp2(v[x][y] - base) + fast_exp2(v[x][2 + y] - base);
+            w[y] = fast_exp2(u[x][y] - zero);
+            w[2 + y] = fast_exp2(u[x][2 + y] - zero);
+          }
+          pb[x][0] = move_matrix_t(pack_f16(w[0], w[1]));
+          pb[x][1] = move_matrix_t(pack_f16(w[2], w[3]));
+        }
+        // ---- O^T += V^T P^T.  Slots outside the segment's keys may hold anything: their scales are made zeros (and codes are finite).
+        uint32_t w[4][kVWords], f[4];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          const int row = r0 + 2 * t4 + (y & 1) + (y >> 1) * 8;
+          value_codes(row, w[y]);
+          f[y] = lds8(tBlocks + (kTile + row) * (D / 16) + (D == 128 ? hr : hr >> 1));
+        }
+        if (key0 < p.lo || key0 + 15 > p.hi) {
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const int j = key0 + 2 * t4 + (y & 1) + (y >> 1) * 8;
+            if (j < p.lo || j > p.hi) f[y] = 0u;
+          }
+        }
+        uint32_t f01, f23;
+        e4m3x4_to_f16(f[0] | f[1] << 8 | f[2] << 16 | f[3] << 24, f01, f23);
+#pragma unroll
+        for (int i = 0; i < kVWords; ++i) {
+          constexpr uint32_t kLow = 0x0f0f0f0fu;
+          uint32_t even01[4], even23[4], odd01[4], odd23[4];
+          e2m1x8_to_f16((w[0][i] & kLow) | (w[1][i] << 4 & ~kLow), even01);
+          e2m1x8_to_f16((w[0][i] >> 4 & kLow) | (w[1][i] & ~kLow), odd01);
+          e2m1x8_to_f16((w[2][i] & kLow) | (w[3][i] << 4 & ~kLow), even23);
+          e2m1x8_to_f16((w[2][i] >> 4 & kLow) | (w[3][i] & ~kLow), odd23);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t av[4] = {mul_f16x2(even01[j], f01), mul_f16x2(odd01[j], f01), mul_f16x2(even23[j], f23), mul_f16x2(odd23[j], f23)};
+#pragma unroll
+            for (int x = 0; x < kHalves; ++x) mma_16816<true>(acc[x][4 * i + j], av, pb[x][0], pb[x][1]);
+          }
+        }
+      }
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&bar->empty[s]);
+    if (++s == stages) { s = 0; ph ^= 1; }
+  }
+  // ---- what this warp has, for the join with the others
+  named_barrier(1, kComputeWarps * 32);            // the piece before has been read
+#pragma unroll
+  for (int x = 0; x < kHalves; ++x)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const int r = 2 * t4 + y + 8 * x;
+      if constexpr (kWeigh) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) join_sums(m[x][y], l[x][y], __shfl_xor_sync(0xffffffffu, m[x][y], o), __shfl_xor_sync(0xffffffffu, l[x][y], o));
+        if (hr == 0) reinterpret_cast<float2*>(red)[r] = make_float2(m[x][y], l[x][y]);
+      } else {
+        float* row = red + r * (D + 4);
+        float sum = l[x][y];
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (hr == 0) { row[D] = m[x][y]; row[D + 1] = sum; row[D + 2] = ref[x][y]; }
+#pragma unroll
+        for (int j = 0; j < kCols / 2; ++j)         // columns 2 j and 2 j + 1 of the lane's
+          *reinterpret_cast<float2*>(row + hr * kCols + 2 * j) = make_float2(acc[x][j][y], acc[x][j][2 + y]);
+      }
+    }
+  return ok;
+}
+
 // kHigh: more than eight rows.  kWeigh: scores only, times log2(e), for the weights of the keys (cache_weigh.cu): they go to the workspace,
 // a row's keys side by side, and of a piece the maximum and sum of each row.
 template <int D, int kKind, bool kHigh, bool kWeigh>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(kKind, kHigh, kWeigh))
 cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
                  const int stages) {
   using SM = FewSmem<D, kKind, kWeigh>;
@@ -232,7 +535,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
   FewSeq own = {};                               // the thread's sequence, of the last kThreads ones
   for (int pass = 0; pass < 2; ++pass) {         // sum, then search
     int base = 0;
-    if (pass == 1) per_cta = tiles_per_cta(total, all_pairs);
+    if (pass == 1) per_cta = tiles_per_cta(total, all_pairs, gridDim.x);
     for (int b0 = 0; b0 < c.B; b0 += kThreads) {
       const int b = b0 + tid;
       if (b < c.B && (pass == 0 || c.B > kThreads)) own = few_seq(a, b);
@@ -335,6 +638,11 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
     int s = 0, ph = 0;
     Piece p;
     while (next_piece(a, walk, p)) {
+      constexpr int kPitch = D + 4;
+      float* mine_red = red + warp * kRows * (kWeigh ? 2 : kPitch);
+      if constexpr (kE2M1) {
+        ok = few_piece_e2m1<D, kHigh, kWeigh>(a, walk.s, p, smem, scales, stages, bar, s, ph, mine_red) && ok;
+      } else {
       // ---- rows: bounds of the keys that each sees in this segment
       int row_lo[kHalves], row_hi[kHalves];
       bool row_ok[kHalves];
@@ -433,30 +741,8 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               const int row = r0 + x * 8 + hr;
-              if (kE2M1) {
-                // a quarter of a key's codes, D / 64 blocks of them, each with its scale (the product has 6 bits at most: exact)
-                uint32_t w[2 * kPieces];
-                if (D == 128) {
-                  const float4 y = lds128(tK + row * 64 + ((t4 ^ ((row >> 1) & 3)) << 4));
-                  w[0] = __float_as_uint(y.x); w[1] = __float_as_uint(y.y);
-                  w[2 * kPieces - 2] = __float_as_uint(y.z); w[2 * kPieces - 1] = __float_as_uint(y.w);
-                } else {
-                  lds64(tK + row * 32 + (((t4 >> 1) ^ ((row >> 2) & 1)) << 4) + (t4 & 1) * 8, w[0], w[1]);
-                }
-                const uint32_t at = tScale + SM::kTensors * kTile + row * (D / 16) + t4 * kPieces;
-                uint32_t both, none;
-                e4m3x4_to_f16(D == 128 ? lds16(at) : lds8(at), both, none);
 #pragma unroll
-                for (int i = 0; i < 2 * kPieces; ++i) {
-                  const uint32_t f = __byte_perm(both, both, i < 2 ? 0x1010 : 0x3232);
-                  uint32_t h[4];
-                  e2m1x8_to_f16(w[i], h);
-                  mma_16816<true>(sc[x], qa[2 * i], mul_f16x2(h[0], f), mul_f16x2(h[1], f));
-                  mma_16816<true>(sc[x], qa[2 * i + 1], mul_f16x2(h[2], f), mul_f16x2(h[3], f));
-                }
-              }
-#pragma unroll
-              for (int i = 0; i < (kE2M1 ? 0 : kPieces); ++i) {
+              for (int i = 0; i < kPieces; ++i) {
                 const int piece = t4 * kPieces + i;
                 const float4 y = lds128(tK + row * D + ((D == 128 ? piece ^ (row & 7) : piece ^ ((row >> 1) & 3)) << 4));
                 const uint32_t w[4] = {__float_as_uint(y.x), __float_as_uint(y.y), __float_as_uint(y.z), __float_as_uint(y.w)};
@@ -509,20 +795,17 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
             }
           } else {
           // codes: a lane's share of those of one of its four keys' values (key0 + 2 t4 + {0, 1, 8, 9})
-          constexpr int kWords = kE2M1 ? kCols / 8 : kCols / 4;
+          constexpr int kWords = kCols / 4;
           auto value_codes = [&](int y, uint32_t (&w)[kWords]) {
             const int row = r0 + 2 * t4 + (y & 1) + (y >> 1) * 8;
-            if (kE2M1) {
-              if (D == 128) lds64(tV + row * 64 + (((hr >> 1) ^ ((row >> 1) & 3)) << 4) + (hr & 1) * 8, w[0], w[kWords - 1]);
-              else w[0] = lds32(tV + row * 32 + (((hr >> 2) ^ ((row >> 2) & 1)) << 4) + (hr & 3) * 4);
-            } else if (D == 128) {
+            if (D == 128) {
               const float4 z = lds128(tV + row * 128 + ((hr ^ (row & 7)) << 4));
-              w[0] = __float_as_uint(z.x); w[kWords > 1 ? 1 : 0] = __float_as_uint(z.y);
-              w[kWords > 1 ? kWords - 2 : 0] = __float_as_uint(z.z); w[kWords - 1] = __float_as_uint(z.w);
+              w[0] = __float_as_uint(z.x); w[1] = __float_as_uint(z.y);
+              w[kWords - 2] = __float_as_uint(z.z); w[kWords - 1] = __float_as_uint(z.w);
             } else {
               const uint32_t at = tV + row * 64 + (((hr >> 1) ^ ((row >> 1) & 3)) << 4) + (hr & 1) * 8;
               w[0] = lds32(at);
-              w[kWords - 1] = lds32(at + 4);
+              w[1] = lds32(at + 4);
             }
           };
           // ---- weights: u is what they are two to the power of, relative to the reference
@@ -567,7 +850,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
                 uint32_t w[kWords], any = 0;
                 value_codes(y, w);
 #pragma unroll
-                for (int i = 0; i < kWords; ++i) any |= w[i] & (kE2M1 ? 0x77777777u : 0x7f7f7f7fu);
+                for (int i = 0; i < kWords; ++i) any |= w[i] & 0x7f7f7f7fu;
                 some |= any != 0 ? 1u << y : 0u;
               }
 #pragma unroll
@@ -624,36 +907,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
             const int j = key0 + 2 * t4 + (y & 1) + (y >> 1) * 8;
             out[y] = j < p.lo || j > p.hi;
           }
-          if (kE2M1) {
-            // Two keys' codes of a column side by side in a byte, their scales in one register
-            uint32_t w[4][kWords], f[4];
-#pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              value_codes(y, w[y]);
-              const int row = r0 + 2 * t4 + (y & 1) + (y >> 1) * 8;
-              f[y] = lds8(tScale + 2 * kTile + (kTile + row) * (D / 16) + (D == 128 ? hr : hr >> 1));
-              if (clear && out[y]) {
-                f[y] = 0u;
-#pragma unroll
-                for (int i = 0; i < kWords; ++i) w[y][i] = 0u;
-              }
-            }
-            uint32_t f01, f23;
-            e4m3x4_to_f16(f[0] | f[1] << 8 | f[2] << 16 | f[3] << 24, f01, f23);
-#pragma unroll
-            for (int i = 0; i < kWords; ++i) {
-              constexpr uint32_t kLow = 0x0f0f0f0fu;
-              uint32_t p[4], q[4];
-              e2m1x8_to_f16((w[0][i] & kLow) | (w[1][i] << 4 & ~kLow), p);
-              e2m1x8_to_f16((w[2][i] & kLow) | (w[3][i] << 4 & ~kLow), q);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) mma_16816<true>(acc[8 * i + 2 * j], pa, mul_f16x2(p[j], f01), mul_f16x2(q[j], f23));
-              e2m1x8_to_f16((w[0][i] >> 4 & kLow) | (w[1][i] & ~kLow), p);
-              e2m1x8_to_f16((w[2][i] >> 4 & kLow) | (w[3][i] & ~kLow), q);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) mma_16816<true>(acc[8 * i + 2 * j + 1], pa, mul_f16x2(p[j], f01), mul_f16x2(q[j], f23));
-            }
-          } else if (kCoded) {
+          if (kCoded) {
             uint32_t w[4][kWords];
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
@@ -703,31 +957,16 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
         if (++s == stages) { s = 0; ph ^= 1; }
       }
 
+      // ---- what this warp has
+      named_barrier(1, kComputeWarps * 32);            // the piece before has been read
       if constexpr (kWeigh) {
-        // ---- join the four lanes of a row, and the four warps
-        float2* parts = reinterpret_cast<float2*>(red);
-        named_barrier(1, kComputeWarps * 32);            // the piece before has been read
 #pragma unroll
         for (int x = 0; x < kHalves; ++x) {
 #pragma unroll
           for (int o = 1; o < 4; o <<= 1) join_sums(m[x], l[x], __shfl_xor_sync(0xffffffffu, m[x], o), __shfl_xor_sync(0xffffffffu, l[x], o));
-          if (t4 == 0) parts[warp * kRows + hr + 8 * x] = make_float2(m[x], l[x]);
+          if (t4 == 0) reinterpret_cast<float2*>(mine_red)[hr + 8 * x] = make_float2(m[x], l[x]);
         }
-        named_barrier(1, kComputeWarps * 32);
-        if (tid < kRows) {
-          float2 y = parts[tid];
-#pragma unroll
-          for (int w = 1; w < kComputeWarps; ++w) join_sums(y.x, y.y, parts[w * kRows + tid].x, parts[w * kRows + tid].y);
-          // (a wait that ran out: the sum is none)
-          if (*abort_flag != 0) y = make_float2(0.f, -1.f);
-          reinterpret_cast<float2*>(a.part)[((int64_t)(p.b * c.Hkv + p.g) * a.row_blocks + p.block + blockIdx.x) * kRows + tid] = y;
-        }
-        continue;
-      }
-      // ---- join the four warps, then store the result or the part
-      constexpr int kPitch = D + 4;
-      float* mine_red = red + warp * kRows * kPitch;
-      named_barrier(1, kComputeWarps * 32);            // the piece before has been read
+      } else {
 #pragma unroll
       for (int x = 0; x < kHalves; ++x) {
         float* row = mine_red + (hr + 8 * x) * kPitch;
@@ -752,7 +991,22 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           }
         }
       }
+      }
+      }
+      // ---- join the four warps, then store the result or the part
       named_barrier(1, kComputeWarps * 32);
+      if constexpr (kWeigh) {
+        const float2* parts = reinterpret_cast<const float2*>(red);
+        if (tid < kRows) {
+          float2 y = parts[tid];
+#pragma unroll
+          for (int w = 1; w < kComputeWarps; ++w) join_sums(y.x, y.y, parts[w * kRows + tid].x, parts[w * kRows + tid].y);
+          // (a wait that ran out: the sum is none)
+          if (*abort_flag != 0) y = make_float2(0.f, -1.f);
+          reinterpret_cast<float2*>(a.part)[((int64_t)(p.b * c.Hkv + p.g) * a.row_blocks + p.block + blockIdx.x) * kRows + tid] = y;
+        }
+        continue;
+      }
       const bool failed = *abort_flag != 0;
       const int row0 = p.block * kBlockRows, n_rows = min(kBlockRows, walk.s.n * a.G - row0);
       for (int i = tid; i < n_rows * (D / 4); i += kComputeWarps * 32) {
@@ -809,7 +1063,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
 // Joins the parts of one head of one new token:
 //   o = sum_loc acc_i 2^(m_i - M_loc) / L_loc + d sum_all acc_i 2^(m_i - M_all) / L_all
 // Bound by latencies: every thread asks for its share of the first kAhead * 128 / (D / 4) parts before the weights are known.
-constexpr int kCombineThreads = 128, kAhead = 12, kMaxParts = kCtas + 2;
+constexpr int kCombineThreads = 128, kAhead = 12, kMaxParts = kMostCtas + 2;
 template <int D, int kRows>
 __global__ void __launch_bounds__(kCombineThreads) cache_few_combine_kernel(const CacheFwdArgs a) {
   constexpr int kLanes = D / 4, kGroups = kCombineThreads / kLanes, kPitch = D + 4;
@@ -984,13 +1238,14 @@ __global__ void __launch_bounds__(kAddThreads) cache_few_add_kernel(const CacheF
   add_weights(a, c, b, g, key, length, length - n, hi, sum);
 }
 
-constexpr int kSmemPerCta = 113 * 1024;          // two CTAs an SM
+constexpr int kSmemPerSm = 228 * 1024;           // 1 KB of each CTA's share is not its own
 
 template <int D, int kKind, bool kHigh, bool kWeigh>
 cudaError_t launch(const CacheFwdArgs& a, const CUtensorMap& mapK, const CUtensorMap& mapV, cudaStream_t s) {
   using SM = FewSmem<D, kKind, kWeigh>;
   constexpr int kRows = kHigh ? 16 : 8;
-  constexpr int kFit = (kSmemPerCta - SM::total(0, kRows)) / (SM::kStageBytes + SM::kScaleBytes);
+  constexpr int kPerSm = ctas_per_sm(kKind, kHigh, kWeigh);
+  constexpr int kFit = (kSmemPerSm / kPerSm - 1024 - SM::total(0, kRows)) / (SM::kStageBytes + SM::kScaleBytes);
   constexpr int kStages = kFit < kMaxStages ? kFit : kMaxStages;
   constexpr int smem = SM::total(kStages, kRows);
   static PerDeviceOnce once;
@@ -998,7 +1253,7 @@ cudaError_t launch(const CacheFwdArgs& a, const CUtensorMap& mapK, const CUtenso
     return cudaFuncSetAttribute(cache_few_kernel<D, kKind, kHigh, kWeigh>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   });
   if (e != cudaSuccess) return e;
-  cache_few_kernel<D, kKind, kHigh, kWeigh><<<kCtas, kThreads, smem, s>>>(a, mapK, mapV, kStages);
+  cache_few_kernel<D, kKind, kHigh, kWeigh><<<kPerSm * kSplitSms, kThreads, smem, s>>>(a, mapK, mapV, kStages);
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   if constexpr (kWeigh) {
@@ -1022,14 +1277,14 @@ size_t plan_bytes(int B) { return align_up(((size_t)B + 1) * 8 * sizeof(int), 25
 // Sequences of a launch, 0: not even one.  A launch counts its tiles in 32 bits (up to one more for a segment that begins inside a tile, and
 // up to one pair's more a CTA behind the last range), and the combination has a row of its grid for each.
 int batch_of(int Lk, int Hkv, int blocks) {
-  const int64_t pair = ((int64_t)Lk + kTile - 1) / kTile + 1, one = pair * Hkv * blocks, most = (1ll << 31) - 1 - (kCtas + 1) * (pair + 1);
+  const int64_t pair = ((int64_t)Lk + kTile - 1) / kTile + 1, one = pair * Hkv * blocks, most = (1ll << 31) - 1 - (kMostCtas + 1) * (pair + 1);
   return (int)std::max<int64_t>(0, std::min<int64_t>(65535, most / one));
 }
 
 }  // namespace
 
 size_t cache_few_ws_bytes(const l2a_params* p) {
-  return plan_bytes(p->B) + align_up((2 * (size_t)p->B * p->Hkv * row_blocks((int64_t)p->Lq * (p->Hq / p->Hkv)) + kCtas) * slot_rows(p) * (p->D + 4) * sizeof(float), 256);
+  return plan_bytes(p->B) + align_up((2 * (size_t)p->B * p->Hkv * row_blocks((int64_t)p->Lq * (p->Hq / p->Hkv)) + kMostCtas) * slot_rows(p) * (p->D + 4) * sizeof(float), 256);
 }
 
 bool cache_few_counts(const l2a_params* p) { return batch_of(p->Lk, p->Hkv, row_blocks((int64_t)p->Lq * (p->Hq / p->Hkv))) > 0; }
@@ -1076,7 +1331,7 @@ cudaError_t launch_cache_few(const CacheFwdArgs& args, void* ws, cudaStream_t s)
 static int64_t score_pitch(int Lk) { return ((int64_t)Lk + kTile - 1) / kTile * kTile; }
 size_t cache_few_weigh_ws_bytes(const l2a_params* p, int rows) {
   const size_t pairs = (size_t)p->B * p->Hkv;
-  return plan_bytes(p->B) + align_up((pairs * row_blocks(rows) + kCtas) * kBlockRows * 2 * sizeof(float), 256) +
+  return plan_bytes(p->B) + align_up((pairs * row_blocks(rows) + kMostCtas) * kBlockRows * 2 * sizeof(float), 256) +
          align_up(pairs * rows * score_pitch(p->Lk) * sizeof(float), 256);
 }
 
@@ -1089,7 +1344,7 @@ cudaError_t launch_cache_few_weigh(const CacheFwdArgs& args, void* ws, cudaStrea
   a.row_blocks = row_blocks(a.score_rows);
   at += plan_bytes(a.c.B);
   a.part = reinterpret_cast<float*>(at);
-  a.scores = reinterpret_cast<float*>(at + align_up(((size_t)a.c.B * a.c.Hkv * a.row_blocks + kCtas) * kBlockRows * 2 * sizeof(float), 256));
+  a.scores = reinterpret_cast<float*>(at + align_up(((size_t)a.c.B * a.c.Hkv * a.row_blocks + kMostCtas) * kBlockRows * 2 * sizeof(float), 256));
   return launch_few<true>(a, s);
 }
 
