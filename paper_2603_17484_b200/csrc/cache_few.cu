@@ -211,7 +211,7 @@ __device__ __forceinline__ uint32_t mul_by_half(uint32_t a, __half2 f, bool uppe
   return *reinterpret_cast<const uint32_t*>(&x);
 }
 
-// The tiles of a piece over an e2m1 cache, for one warp: 16 keys of each.  The keys are the 16 rows of the products' A fragments and the query
+// The tiles of a piece over an e2m1 cache, for one warp: 32 keys of every other.  The keys are the 16 rows of the products' A fragments and the query
 // rows the 8 columns of B, so that up to eight rows take half as many products and accumulators as with the roles of the other kinds; S^T comes out of one
 // product and goes, transposed, into the other:
 //   S^T = K Q^T : a lane takes a quarter of the codes of two keys, consecutive ones, as its elements of successive products (Q has the same order).
@@ -224,7 +224,8 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
                                                int stages, FewBars* bar, int& s, int& ph, float* red) {
   using SM = FewSmem<D, L2A_CACHE_E2M1, kWeigh>;
   constexpr int kHalves = kHigh ? 2 : 1, kCols = D / 8, kVWords = D / 64, kKWords = D / 32;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, hr = lane >> 2, t4 = lane & 3, r0 = warp * 16;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, hr = lane >> 2, t4 = lane & 3;
+  const int pair = warp >> 1, r0 = (warp & 1) * 32;        // which of two tiles this warp takes, its keys of them
   volatile int* abort_flag = &bar->abort_flag;
   // ---- B fragments of Q: row hr (and hr + 8), this lane's quarter of its elements, the largest of the row at 2^14 .. 2^15
   uint32_t qb[kHalves][D / 16][2];
@@ -278,40 +279,58 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
   every_lo = __reduce_max_sync(0xffffffffu, every_lo);
   every_hi = __reduce_min_sync(0xffffffffu, every_hi);
 
-  float m[kHalves][2], l[kHalves][2], ref[kHalves][2];     // maxima and sums of the weights; references of the accumulators
+  // Of the rows: what the weights are relative to and their sum; what those of the accumulators are (zero: less kWeightTop); and where either
+  // has to follow (minus infinity: the row has seen nothing)
+  float base[kHalves][2], l[kHalves][2], zero[kHalves][2], base_top[kHalves][2], zero_top[kHalves][2];
   float acc[kHalves][kCols / 2][4];
 #pragma unroll
   for (int x = 0; x < kHalves; ++x) {
-    m[x][0] = m[x][1] = ref[x][0] = ref[x][1] = -INFINITY;
-    l[x][0] = l[x][1] = 0.f;
+    base_top[x][0] = base_top[x][1] = zero_top[x][0] = zero_top[x][1] = -INFINITY;
+    base[x][0] = base[x][1] = zero[x][0] = zero[x][1] = l[x][0] = l[x][1] = 0.f;
 #pragma unroll
     for (int j = 0; j < kCols / 2; ++j) acc[x][j][0] = acc[x][j][1] = acc[x][j][2] = acc[x][j][3] = 0.f;
   }
+  // ---- where this lane's operands lie in a stage.  (The swizzle exchanges the 16-byte pieces of a row by its number; rows 8 apart have them
+  // in the same order, so that all else is the same distance for every lane.)
+  constexpr int kRowBytes = D / 2, kBlockBytes = D / 16;
+  const int k_row = r0 + hr, v_row = r0 + 2 * t4;
+  const uint32_t k_at = smem_u32(smem) + k_row * kRowBytes +
+                        (D == 128 ? (t4 ^ ((k_row >> 1) & 3)) << 4 : (((t4 >> 1) ^ ((k_row >> 2) & 1)) << 4) + (t4 & 1) * 8);
+  const uint32_t v_at = smem_u32(smem) + SM::kTileBytes + v_row * kRowBytes +
+                        (D == 128 ? (((hr >> 1) ^ ((v_row >> 1) & 3)) << 4) + (hr & 1) * 8 : (((hr >> 2) ^ ((v_row >> 2) & 1)) << 4) + (hr & 3) * 4);
+  const uint32_t exp_at = smem_u32(scales) + k_row;
+  float* score_at = kWeigh ? a.scores + ((int64_t)(p.b * a.c.Hkv + p.g) * a.score_rows + p.block * kBlockRows + 2 * t4) * a.score_pitch + hr : nullptr;
+  const uint32_t k_scale_at = smem_u32(scales) + SM::kTensors * kTile + k_row * kBlockBytes + t4 * kVWords;
+  const uint32_t v_scale_at = smem_u32(scales) + SM::kTensors * kTile + (kTile + v_row) * kBlockBytes + (D == 128 ? hr : hr >> 1);
   bool ok = true;
   for (int t = p.t0; t < p.t1; ++t) {
-    if (!mbar_wait_warp(&bar->full[s], ph, abort_flag)) { ok = false; break; }
-    const int key0 = t * kTile + r0;               // first key of this warp's 16
-    if (key0 <= p.hi && key0 + 15 >= p.lo) {
-      const uint32_t tK = smem_u32(smem) + s * SM::kStageBytes, tScale = smem_u32(scales) + s * SM::kScaleBytes;
-      const uint32_t tBlocks = tScale + SM::kTensors * kTile;
-      const bool edge = key0 < every_lo || key0 + 15 > every_hi;
-      // ---- S^T
-      float sc[kHalves][4] = {};
-      {
+    const int stage = s, phase = ph;
+    if (++s == stages) { s = 0; ph ^= 1; }
+    if ((t & 1) != pair) continue;
+    if (!mbar_wait_warp(&bar->full[stage], phase, abort_flag)) { ok = false; break; }
+    const int key0 = t * kTile + r0;               // first key of this warp's 32
+    if (key0 <= p.hi && key0 + 31 >= p.lo) {
+      const uint32_t tile = stage * SM::kStageBytes, scale = stage * SM::kScaleBytes;
+      const bool edge = key0 < every_lo || key0 + 31 > every_hi;
+      // ---- S^T, 16 keys at a time (i16)
+      float v[2][kHalves][4];                      // keys hr (0, 1) and hr + 8 (2, 3), rows 2 t4 and 2 t4 + 1
+#pragma unroll
+      for (int i16 = 0; i16 < 2; ++i16) {
+        float sc[kHalves][4] = {};
         uint32_t w[2][kKWords];
         __half2 f[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const int row = r0 + hr + 8 * k;
+          const int row = i16 * 16 + k * 8;
           uint32_t both, none;
           if (D == 128) {
-            const float4 y = lds128(tK + row * 64 + ((t4 ^ ((row >> 1) & 3)) << 4));
+            const float4 y = lds128(k_at + tile + row * kRowBytes);
             w[k][0] = __float_as_uint(y.x); w[k][1] = __float_as_uint(y.y);
             w[k][kKWords - 2] = __float_as_uint(y.z); w[k][kKWords - 1] = __float_as_uint(y.w);
-            e4m3x4_to_f16(lds16(tBlocks + row * 8 + t4 * 2), both, none);
+            e4m3x4_to_f16(lds16(k_scale_at + scale + row * kBlockBytes), both, none);
           } else {
-            lds64(tK + row * 32 + (((t4 >> 1) ^ ((row >> 2) & 1)) << 4) + (t4 & 1) * 8, w[k][0], w[k][1]);
-            e4m3x4_to_f16(lds8(tBlocks + row * 4 + t4), both, none);
+            lds64(k_at + tile + row * kRowBytes, w[k][0], w[k][1]);
+            e4m3x4_to_f16(lds8(k_scale_at + scale + row * kBlockBytes), both, none);
           }
           f[k] = *reinterpret_cast<const __half2*>(&both);
         }
@@ -331,88 +350,101 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
             mma_16816<true>(sc[x], a1, qb[x][2 * i + 1][0], qb[x][2 * i + 1][1]);
           }
         }
+        const float fk[2] = {scale_of_exponent(lds8(exp_at + scale + i16 * 16)), scale_of_exponent(lds8(exp_at + scale + i16 * 16 + 8))};
+#pragma unroll
+        for (int x = 0; x < kHalves; ++x)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) v[i16][x][y] = sc[x][y] * fk[y >> 1] * row_scale[x][y & 1];
       }
-      const float fk[2] = {scale_of_exponent(lds8(tScale + r0 + hr)), scale_of_exponent(lds8(tScale + r0 + hr + 8))};
-      float v[kHalves][4];                         // keys hr (0, 1) and hr + 8 (2, 3), rows 2 t4 and 2 t4 + 1
+      if (edge) {
 #pragma unroll
-      for (int x = 0; x < kHalves; ++x)
+        for (int i16 = 0; i16 < 2; ++i16)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          v[x][y] = sc[x][y] * fk[y >> 1] * row_scale[x][y & 1];
-          const int j = key0 + hr + (y >> 1) * 8;
-          if (edge && (j < row_lo[x][y & 1] || j > row_hi[x][y & 1])) v[x][y] = -INFINITY;
-        }
+          for (int x = 0; x < kHalves; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const int j = key0 + i16 * 16 + hr + (y >> 1) * 8;
+              if (j < row_lo[x][y & 1] || j > row_hi[x][y & 1]) v[i16][x][y] = -INFINITY;
+            }
+      }
       if constexpr (kWeigh) {
 #pragma unroll
         for (int x = 0; x < kHalves; ++x)
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
+            const float k4[4] = {v[0][x][y], v[0][x][2 + y], v[1][x][y], v[1][x][2 + y]};
             if (row_hi[x][y] >= 0) {
-              float* dst = a.scores + ((int64_t)(p.b * a.c.Hkv + p.g) * a.score_rows + p.block * kBlockRows + 2 * t4 + y + 8 * x) * a.score_pitch +
-                           key0 + hr;
-              dst[0] = v[x][y];
-              dst[8] = v[x][2 + y];
+              float* dst = score_at + (int64_t)(8 * x + y) * a.score_pitch + key0;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) dst[8 * k] = k4[k];
             }
             // (each lane by itself: its keys are joined with the others' at the end)
-            const float m_new = fmaxf(m[x][y], fmaxf(v[x][y], v[x][2 + y])), base = m_new == -INFINITY ? 0.f : m_new;
-            l[x][y] = l[x][y] * fast_exp2(m[x][y] - base) + (fast_exp2(v[x][y] - base) + fast_exp2(v[x][2 + y] - base));
-            m[x][y] = m_new;
+            const float m_new = fmaxf(base_top[x][y], fmaxf(fmaxf(k4[0], k4[1]), fmaxf(k4[2], k4[3]))), b = m_new == -INFINITY ? 0.f : m_new;
+            l[x][y] = l[x][y] * fast_exp2(base_top[x][y] - b) +
+                      ((fast_exp2(k4[0] - b) + fast_exp2(k4[1] - b)) + (fast_exp2(k4[2] - b) + fast_exp2(k4[3] - b)));
+            base_top[x][y] = m_new;
           }
       } else {
-        // ---- weights: u is what they are two to the power of, relative to the reference
-        const uint32_t tV = tK + SM::kTileBytes;
-        uint32_t ev[2] = {lds8(tScale + kTile + r0 + hr), lds8(tScale + kTile + r0 + hr + 8)};
-        const float vexp[2] = {__uint_as_float(0x4b000000u | ev[0]) - 8388735.f, __uint_as_float(0x4b000000u | ev[1]) - 8388735.f};   // ev - 127
-        float u[kHalves][4];
-        bool grow = false;
+        // ---- weights: v plus the value's exponent is what they are two to the power of, relative to the reference
+        float vexp[2][2];
+        bool zeros = false, grow = false;
 #pragma unroll
-        for (int x = 0; x < kHalves; ++x) {
+        for (int i16 = 0; i16 < 2; ++i16)
 #pragma unroll
-          for (int y = 0; y < 4; ++y) u[x][y] = v[x][y] + vexp[y >> 1];
-#pragma unroll
-          for (int y = 0; y < 2; ++y)
-            grow |= fmaxf(v[x][y], v[x][2 + y]) > m[x][y] + kLag || fmaxf(u[x][y], u[x][2 + y]) > ref[x][y] + kLag;
-        }
-        // a lane's share of the codes of one of its four keys' values (key0 + 2 t4 + {0, 1, 8, 9})
-        auto value_codes = [&](int row, uint32_t (&w)[kVWords]) {
-          if (D == 128) lds64(tV + row * 64 + (((hr >> 1) ^ ((row >> 1) & 3)) << 4) + (hr & 1) * 8, w[0], w[kVWords - 1]);
-          else w[0] = lds32(tV + row * 32 + (((hr >> 2) ^ ((row >> 2) & 1)) << 4) + (hr & 3) * 4);
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t e = lds8(exp_at + scale + kTile + i16 * 16 + k * 8);
+            zeros |= e == 127u;
+            vexp[i16][k] = __uint_as_float(0x4b000000u | e) - 8388735.f;             // e - 127
+          }
+        auto tops = [&](int x, int y, float& m_new, float& top) {
+          m_new = fmaxf(fmaxf(v[0][x][y], v[0][x][2 + y]), fmaxf(v[1][x][y], v[1][x][2 + y]));
+          top = fmaxf(fmaxf(v[0][x][y] + vexp[0][0], v[0][x][2 + y] + vexp[0][1]), fmaxf(v[1][x][y] + vexp[1][0], v[1][x][2 + y] + vexp[1][1]));
         };
+#pragma unroll
+        for (int x = 0; x < kHalves; ++x)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            float m_new, top;
+            tops(x, y, m_new, top);
+            grow |= m_new > base_top[x][y] || top > zero_top[x][y];
+          }
         if (__any_sync(0xffffffffu, grow)) {
           // Values of zeros have exponent 0 however small all others are: they must not become the reference, which would push the
           // weights of the others out of fp16's range.  They get the least exponent.
-          if (__any_sync(0xffffffffu, ev[0] == 127u || ev[1] == 127u)) {
+          if (__any_sync(0xffffffffu, zeros)) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              uint32_t any = 0;
-              const uint32_t row = tV + (r0 + hr + 8 * k) * (D / 2) + t4 * (D / 8);      // (a quarter of the row's bytes, in whatever order)
+            for (int i16 = 0; i16 < 2; ++i16)
 #pragma unroll
-              for (int i = 0; i < kKWords; ++i) any |= lds32(row + 4 * i) & 0x77777777u;
-              any |= __shfl_xor_sync(0xffffffffu, any, 1);
-              any |= __shfl_xor_sync(0xffffffffu, any, 2);
+              for (int k = 0; k < 2; ++k) {
+                uint32_t any = 0;
+                const uint32_t row = smem_u32(smem) + tile + SM::kTileBytes + (k_row + i16 * 16 + 8 * k) * kRowBytes + t4 * (D / 8);
 #pragma unroll
-              for (int x = 0; x < kHalves; ++x)
-#pragma unroll
-                for (int y = 0; y < 2; ++y) u[x][2 * k + y] -= any != 0 ? 0.f : 127.f;
-            }
+                for (int i = 0; i < kKWords; ++i) any |= lds32(row + 4 * i) & 0x77777777u;      // (a quarter of the row, in whatever order)
+                any |= __shfl_xor_sync(0xffffffffu, any, 1);
+                any |= __shfl_xor_sync(0xffffffffu, any, 2);
+                vexp[i16][k] -= any != 0 ? 0.f : 127.f;
+              }
           }
 #pragma unroll
           for (int x = 0; x < kHalves; ++x)
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-              float top = fmaxf(u[x][y], u[x][2 + y]), m_new = fmaxf(v[x][y], v[x][2 + y]);
+              float top, m_new;
+              tops(x, y, m_new, top);
 #pragma unroll
               for (int o = 4; o < 32; o <<= 1) {
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
                 m_new = fmaxf(m_new, __shfl_xor_sync(0xffffffffu, m_new, o));
               }
-              if (m_new > m[x][y] + kLag) {
-                l[x][y] *= fast_exp2(m[x][y] - m_new);       // 0 the first time
-                m[x][y] = m_new;
+              if (m_new > base_top[x][y]) {
+                l[x][y] *= base_top[x][y] == -INFINITY ? 0.f : fast_exp2(base[x][y] - m_new);
+                base[x][y] = m_new;
+                base_top[x][y] = m_new + kLag;
               }
-              if (top > ref[x][y] + kLag) {
-                const float alpha = fast_exp2(ref[x][y] - top);
-                ref[x][y] = top;
+              if (top > zero_top[x][y]) {
+                const float alpha = zero_top[x][y] == -INFINITY ? 0.f : fast_exp2(zero[x][y] + kWeightTop - top);
+                zero[x][y] = top - kWeightTop;
+                zero_top[x][y] = top + kLag;
 #pragma unroll
                 for (int j = 0; j < kCols / 2; ++j) {
                   acc[x][j][y] *= alpha;
@@ -421,57 +453,58 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
               }
             }
         }
-        uint32_t pb[kHalves][2];                   // B fragments of P^T
+        const bool clear = key0 < p.lo || key0 + 31 > p.hi;
 #pragma unroll
-        for (int x = 0; x < kHalves; ++x) {
-          float w[4];
+        for (int i16 = 0; i16 < 2; ++i16) {
+          uint32_t pb[kHalves][2];                 // B fragments of P^T
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const float base = m[x][y] == -INFINITY ? 0.f : m[x][y], zero = (ref[x][y] == -INFINITY ? 0.f : ref[x][y]) - kWeightTop;
-            l[x][y] += fast_exp2(v[x][y] - base) + fast_exp2(v[x][2 + y] - base);
-            w[y] = fast_exp2(u[x][y] - zero);
-            w[2 + y] = fast_exp2(u[x][2 + y] - zero);
+          for (int x = 0; x < kHalves; ++x) {
+            float w[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) w[y] = fast_exp2(v[i16][x][y] + (vexp[i16][y >> 1] - zero[x][y & 1]));
+#pragma unroll
+            for (int y = 0; y < 2; ++y) l[x][y] += fast_exp2(v[i16][x][y] - base[x][y]) + fast_exp2(v[i16][x][2 + y] - base[x][y]);
+            pb[x][0] = move_matrix_t(pack_f16(w[0], w[1]));
+            pb[x][1] = move_matrix_t(pack_f16(w[2], w[3]));
           }
-          pb[x][0] = move_matrix_t(pack_f16(w[0], w[1]));
-          pb[x][1] = move_matrix_t(pack_f16(w[2], w[3]));
-        }
-        // ---- O^T += V^T P^T.  Slots outside the segment's keys may hold anything: their scales are made zeros (and codes are finite).
-        uint32_t w[4][kVWords], f[4];
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          const int row = r0 + 2 * t4 + (y & 1) + (y >> 1) * 8;
-          value_codes(row, w[y]);
-          f[y] = lds8(tBlocks + (kTile + row) * (D / 16) + (D == 128 ? hr : hr >> 1));
-        }
-        if (key0 < p.lo || key0 + 15 > p.hi) {
+          // ---- O^T += V^T P^T.  Slots outside the segment's keys may hold anything: their scales are made zeros (and codes are finite).
+          uint32_t w[4][kVWords], f[4];
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
-            const int j = key0 + 2 * t4 + (y & 1) + (y >> 1) * 8;
-            if (j < p.lo || j > p.hi) f[y] = 0u;
+            const int row = i16 * 16 + (y & 1) + (y >> 1) * 8;
+            if (D == 128) lds64(v_at + tile + row * kRowBytes, w[y][0], w[y][kVWords - 1]);
+            else w[y][0] = lds32(v_at + tile + row * kRowBytes);
+            f[y] = lds8(v_scale_at + scale + row * kBlockBytes);
           }
-        }
-        uint32_t f01, f23;
-        e4m3x4_to_f16(f[0] | f[1] << 8 | f[2] << 16 | f[3] << 24, f01, f23);
+          if (clear) {
 #pragma unroll
-        for (int i = 0; i < kVWords; ++i) {
-          constexpr uint32_t kLow = 0x0f0f0f0fu;
-          uint32_t even01[4], even23[4], odd01[4], odd23[4];
-          e2m1x8_to_f16((w[0][i] & kLow) | (w[1][i] << 4 & ~kLow), even01);
-          e2m1x8_to_f16((w[0][i] >> 4 & kLow) | (w[1][i] & ~kLow), odd01);
-          e2m1x8_to_f16((w[2][i] & kLow) | (w[3][i] << 4 & ~kLow), even23);
-          e2m1x8_to_f16((w[2][i] >> 4 & kLow) | (w[3][i] & ~kLow), odd23);
+            for (int y = 0; y < 4; ++y) {
+              const int j = key0 + i16 * 16 + 2 * t4 + (y & 1) + (y >> 1) * 8;
+              if (j < p.lo || j > p.hi) f[y] = 0u;
+            }
+          }
+          uint32_t f01, f23;
+          e4m3x4_to_f16(f[0] | f[1] << 8 | f[2] << 16 | f[3] << 24, f01, f23);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t av[4] = {mul_f16x2(even01[j], f01), mul_f16x2(odd01[j], f01), mul_f16x2(even23[j], f23), mul_f16x2(odd23[j], f23)};
+          for (int i = 0; i < kVWords; ++i) {
+            constexpr uint32_t kLow = 0x0f0f0f0fu;
+            uint32_t even01[4], even23[4], odd01[4], odd23[4];
+            e2m1x8_to_f16((w[0][i] & kLow) | (w[1][i] << 4 & ~kLow), even01);
+            e2m1x8_to_f16((w[0][i] >> 4 & kLow) | (w[1][i] & ~kLow), odd01);
+            e2m1x8_to_f16((w[2][i] & kLow) | (w[3][i] << 4 & ~kLow), even23);
+            e2m1x8_to_f16((w[2][i] >> 4 & kLow) | (w[3][i] & ~kLow), odd23);
 #pragma unroll
-            for (int x = 0; x < kHalves; ++x) mma_16816<true>(acc[x][4 * i + j], av, pb[x][0], pb[x][1]);
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t av[4] = {mul_f16x2(even01[j], f01), mul_f16x2(odd01[j], f01), mul_f16x2(even23[j], f23), mul_f16x2(odd23[j], f23)};
+#pragma unroll
+              for (int x = 0; x < kHalves; ++x) mma_16816<true>(acc[x][4 * i + j], av, pb[x][0], pb[x][1]);
+            }
           }
         }
       }
     }
     __syncwarp();
-    if (lane == 0) mbar_arrive(&bar->empty[s]);
-    if (++s == stages) { s = 0; ph ^= 1; }
+    if (lane == 0) mbar_arrive(&bar->empty[stage]);
   }
   // ---- what this warp has, for the join with the others
   named_barrier(1, kComputeWarps * 32);            // the piece before has been read
@@ -482,14 +515,18 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
       const int r = 2 * t4 + y + 8 * x;
       if constexpr (kWeigh) {
 #pragma unroll
-        for (int o = 4; o < 32; o <<= 1) join_sums(m[x][y], l[x][y], __shfl_xor_sync(0xffffffffu, m[x][y], o), __shfl_xor_sync(0xffffffffu, l[x][y], o));
-        if (hr == 0) reinterpret_cast<float2*>(red)[r] = make_float2(m[x][y], l[x][y]);
+        for (int o = 4; o < 32; o <<= 1) join_sums(base_top[x][y], l[x][y], __shfl_xor_sync(0xffffffffu, base_top[x][y], o), __shfl_xor_sync(0xffffffffu, l[x][y], o));
+        if (hr == 0) reinterpret_cast<float2*>(red)[r] = make_float2(base_top[x][y], l[x][y]);
       } else {
         float* row = red + r * (D + 4);
         float sum = l[x][y];
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (hr == 0) { row[D] = m[x][y]; row[D + 1] = sum; row[D + 2] = ref[x][y]; }
+        if (hr == 0) {
+          row[D] = base_top[x][y] == -INFINITY ? -INFINITY : base[x][y];
+          row[D + 1] = sum;
+          row[D + 2] = zero_top[x][y] == -INFINITY ? -INFINITY : zero[x][y] + kWeightTop;
+        }
 #pragma unroll
         for (int j = 0; j < kCols / 2; ++j)         // columns 2 j and 2 j + 1 of the lane's
           *reinterpret_cast<float2*>(row + hr * kCols + 2 * j) = make_float2(acc[x][j][y], acc[x][j][2 + y]);
@@ -524,7 +561,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
     tma_prefetch_desc(&mapV);
     for (int s = 0; s < stages; ++s) {
       mbar_init(&bar->full[s], 1);
-      mbar_init(&bar->empty[s], kComputeWarps);
+      mbar_init(&bar->empty[s], kE2M1 ? kComputeWarps / 2 : kComputeWarps);
     }
     bar->abort_flag = (smem_u32(smem) & 1023u) != 0 ? 2 : 0;       // the swizzled tiles need a 1024-byte aligned base
     fence_mbar_init();
