@@ -217,7 +217,7 @@ __device__ __forceinline__ uint32_t mul_by_half(uint32_t a, __half2 f, bool uppe
 //   S^T = K Q^T : a lane takes a quarter of the codes of two keys, consecutive ones, as its elements of successive products (Q has the same order).
 //   O^T = V^T P^T : a lane has a group of D / 8 columns; two keys' codes of a column are put side by side in a byte.
 // A code becomes fp16 and is multiplied by the scale of its block, both exactly (6 bits); exponents are as in the 8-bit kind.  The maxima are
-// followed only where a row is more than kLag above what it had, so that no lane needs another's scores otherwise.
+// followed only where a weight leaves the range of fp16, so that no lane needs another's scores otherwise.
 // red: of this warp [rows][D + 4] sums, maximum, sum of weights, reference; kWeigh: [rows] maximum and sum.
 template <int D, bool kHigh, bool kWeigh>
 __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewSeq& seq, const Piece& p, const uint8_t* smem, const uint8_t* scales,
@@ -279,14 +279,16 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
   every_lo = __reduce_max_sync(0xffffffffu, every_lo);
   every_hi = __reduce_min_sync(0xffffffffu, every_hi);
 
-  // Of the rows: what the weights are relative to and their sum; what those of the accumulators are (zero: less kWeightTop); and where either
-  // has to follow (minus infinity: the row has seen nothing)
-  float base[kHalves][2], l[kHalves][2], zero[kHalves][2], base_top[kHalves][2], zero_top[kHalves][2];
+  // Of the rows: what the weights are relative to (kWeigh: their maximum) and their sum; what those of the accumulators are relative to.  A
+  // row that has seen nothing has kNothing, from which any weight is infinite.
+  constexpr float kNothing = -3e38f;
+  float base[kHalves][2], l[kHalves][2], zero[kHalves][2];
   float acc[kHalves][kCols / 2][4];
 #pragma unroll
   for (int x = 0; x < kHalves; ++x) {
-    base_top[x][0] = base_top[x][1] = zero_top[x][0] = zero_top[x][1] = -INFINITY;
-    base[x][0] = base[x][1] = zero[x][0] = zero[x][1] = l[x][0] = l[x][1] = 0.f;
+    base[x][0] = base[x][1] = kWeigh ? -INFINITY : kNothing;
+    zero[x][0] = zero[x][1] = kNothing;
+    l[x][0] = l[x][1] = 0.f;
 #pragma unroll
     for (int j = 0; j < kCols / 2; ++j) acc[x][j][0] = acc[x][j][1] = acc[x][j][2] = acc[x][j][3] = 0.f;
   }
@@ -313,7 +315,8 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
       const uint32_t tile = stage * SM::kStageBytes, scale = stage * SM::kScaleBytes;
       const bool edge = key0 < every_lo || key0 + 31 > every_hi;
       // ---- S^T, 16 keys at a time (i16)
-      float v[2][kHalves][4];                      // keys hr (0, 1) and hr + 8 (2, 3), rows 2 t4 and 2 t4 + 1
+      // v times row_scale: the scores of keys hr (0, 1) and hr + 8 (2, 3), rows 2 t4 and 2 t4 + 1
+      float v[2][kHalves][4];
 #pragma unroll
       for (int i16 = 0; i16 < 2; ++i16) {
         float sc[kHalves][4] = {};
@@ -354,7 +357,7 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
 #pragma unroll
         for (int x = 0; x < kHalves; ++x)
 #pragma unroll
-          for (int y = 0; y < 4; ++y) v[i16][x][y] = sc[x][y] * fk[y >> 1] * row_scale[x][y & 1];
+          for (int y = 0; y < 4; ++y) v[i16][x][y] = sc[x][y] * fk[y >> 1];
       }
       if (edge) {
 #pragma unroll
@@ -372,79 +375,93 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
         for (int x = 0; x < kHalves; ++x)
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            const float k4[4] = {v[0][x][y], v[0][x][2 + y], v[1][x][y], v[1][x][2 + y]};
+            const float f = row_scale[x][y], k4[4] = {v[0][x][y] * f, v[0][x][2 + y] * f, v[1][x][y] * f, v[1][x][2 + y] * f};
             if (row_hi[x][y] >= 0) {
               float* dst = score_at + (int64_t)(8 * x + y) * a.score_pitch + key0;
 #pragma unroll
               for (int k = 0; k < 4; ++k) dst[8 * k] = k4[k];
             }
             // (each lane by itself: its keys are joined with the others' at the end)
-            const float m_new = fmaxf(base_top[x][y], fmaxf(fmaxf(k4[0], k4[1]), fmaxf(k4[2], k4[3]))), b = m_new == -INFINITY ? 0.f : m_new;
-            l[x][y] = l[x][y] * fast_exp2(base_top[x][y] - b) +
+            const float m_new = fmaxf(base[x][y], fmaxf(fmaxf(k4[0], k4[1]), fmaxf(k4[2], k4[3]))), b = m_new == -INFINITY ? 0.f : m_new;
+            l[x][y] = l[x][y] * fast_exp2(base[x][y] - b) +
                       ((fast_exp2(k4[0] - b) + fast_exp2(k4[1] - b)) + (fast_exp2(k4[2] - b) + fast_exp2(k4[3] - b)));
-            base_top[x][y] = m_new;
+            base[x][y] = m_new;
           }
       } else {
-        // ---- weights: v plus the value's exponent is what they are two to the power of, relative to the reference
-        float vexp[2][2];
-        bool zeros = false, grow = false;
+        // ---- weights: the score plus the value's exponent is what they are two to the power of, relative to `zero`.  They are computed with what the
+        // rows had; where one comes out at 2^15 or more, or the sum above kMostSum, the row follows its new maximum and they are computed again.
+        constexpr float kMostSum = 0x1p64f;
+        float vexp[2][2], sum[kHalves][2];
+        uint32_t pw[2][kHalves][2];                // as fp16, rows 2 t4 and 2 t4 + 1 of a key
 #pragma unroll
         for (int i16 = 0; i16 < 2; ++i16)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const uint32_t e = lds8(exp_at + scale + kTile + i16 * 16 + k * 8);
-            zeros |= e == 127u;
-            vexp[i16][k] = __uint_as_float(0x4b000000u | e) - 8388735.f;             // e - 127
-          }
-        auto tops = [&](int x, int y, float& m_new, float& top) {
-          m_new = fmaxf(fmaxf(v[0][x][y], v[0][x][2 + y]), fmaxf(v[1][x][y], v[1][x][2 + y]));
-          top = fmaxf(fmaxf(v[0][x][y] + vexp[0][0], v[0][x][2 + y] + vexp[0][1]), fmaxf(v[1][x][y] + vexp[1][0], v[1][x][2 + y] + vexp[1][1]));
-        };
+          for (int k = 0; k < 2; ++k)
+            vexp[i16][k] = __uint_as_float(0x4b000000u | lds8(exp_at + scale + kTile + i16 * 16 + k * 8)) - 8388735.f;             // e - 127
+        auto weights = [&]() -> bool {
+          uint32_t top = 0;
+          float most = 0.f;
 #pragma unroll
-        for (int x = 0; x < kHalves; ++x)
+          for (int x = 0; x < kHalves; ++x) {
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            float m_new, top;
-            tops(x, y, m_new, top);
-            grow |= m_new > base_top[x][y] || top > zero_top[x][y];
-          }
-        if (__any_sync(0xffffffffu, grow)) {
-          // Values of zeros have exponent 0 however small all others are: they must not become the reference, which would push the
-          // weights of the others out of fp16's range.  They get the least exponent.
-          if (__any_sync(0xffffffffu, zeros)) {
+            for (int y = 0; y < 2; ++y) sum[x][y] = l[x][y];
 #pragma unroll
             for (int i16 = 0; i16 < 2; ++i16)
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
-                uint32_t any = 0;
-                const uint32_t row = smem_u32(smem) + tile + SM::kTileBytes + (k_row + i16 * 16 + 8 * k) * kRowBytes + t4 * (D / 8);
+                float w[2];
 #pragma unroll
-                for (int i = 0; i < kKWords; ++i) any |= lds32(row + 4 * i) & 0x77777777u;      // (a quarter of the row, in whatever order)
-                any |= __shfl_xor_sync(0xffffffffu, any, 1);
-                any |= __shfl_xor_sync(0xffffffffu, any, 2);
-                vexp[i16][k] -= any != 0 ? 0.f : 127.f;
+                for (int y = 0; y < 2; ++y) {
+                  w[y] = fast_exp2(fmaf(v[i16][x][2 * k + y], row_scale[x][y], vexp[i16][k] - zero[x][y]));
+                  sum[x][y] += fast_exp2(fmaf(v[i16][x][2 * k + y], row_scale[x][y], -base[x][y]));
+                }
+                pw[i16][x][k] = pack_f16(w[0], w[1]);
+                top = __vmaxu2(top, pw[i16][x][k]);
               }
+            most = fmaxf(most, fmaxf(sum[x][0], sum[x][1]));
           }
+          return ((top + 0x08000800u) & 0x80008000u) != 0 || most > kMostSum;
+        };
+        if (__any_sync(0xffffffffu, weights())) {
+          // Values of zeros have exponent 0 however small all others are: they must not become the reference, which would push the
+          // weights of the others out of fp16's range.  They get the least exponent.
+#pragma unroll
+          for (int i16 = 0; i16 < 2; ++i16)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              uint32_t any = 0;
+              const uint32_t row = smem_u32(smem) + tile + SM::kTileBytes + (k_row + i16 * 16 + 8 * k) * kRowBytes + t4 * (D / 8);
+#pragma unroll
+              for (int i = 0; i < kKWords; ++i) any |= lds32(row + 4 * i) & 0x77777777u;      // (a quarter of the row, in whatever order)
+              any |= __shfl_xor_sync(0xffffffffu, any, 1);
+              any |= __shfl_xor_sync(0xffffffffu, any, 2);
+              if (any == 0) vexp[i16][k] = -127.f;
+            }
 #pragma unroll
           for (int x = 0; x < kHalves; ++x)
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
-              float top, m_new;
-              tops(x, y, m_new, top);
+              float m_new = -INFINITY, top = -INFINITY;
+#pragma unroll
+              for (int i16 = 0; i16 < 2; ++i16)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                  const float z = v[i16][x][2 * k + y] * row_scale[x][y];
+                  m_new = fmaxf(m_new, z);
+                  top = fmaxf(top, z + vexp[i16][k]);
+                }
 #pragma unroll
               for (int o = 4; o < 32; o <<= 1) {
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
                 m_new = fmaxf(m_new, __shfl_xor_sync(0xffffffffu, m_new, o));
               }
-              if (m_new > base_top[x][y]) {
-                l[x][y] *= base_top[x][y] == -INFINITY ? 0.f : fast_exp2(base[x][y] - m_new);
+              if (m_new > base[x][y]) {
+                l[x][y] *= fast_exp2(base[x][y] - m_new);        // 0 the first time
                 base[x][y] = m_new;
-                base_top[x][y] = m_new + kLag;
               }
-              if (top > zero_top[x][y]) {
-                const float alpha = zero_top[x][y] == -INFINITY ? 0.f : fast_exp2(zero[x][y] + kWeightTop - top);
+              if (top - kWeightTop > zero[x][y]) {
+                const float alpha = fast_exp2(zero[x][y] + kWeightTop - top);
                 zero[x][y] = top - kWeightTop;
-                zero_top[x][y] = top + kLag;
 #pragma unroll
                 for (int j = 0; j < kCols / 2; ++j) {
                   acc[x][j][y] *= alpha;
@@ -452,20 +469,18 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
                 }
               }
             }
+          weights();
         }
+#pragma unroll
+        for (int x = 0; x < kHalves; ++x) { l[x][0] = sum[x][0]; l[x][1] = sum[x][1]; }
         const bool clear = key0 < p.lo || key0 + 31 > p.hi;
 #pragma unroll
         for (int i16 = 0; i16 < 2; ++i16) {
           uint32_t pb[kHalves][2];                 // B fragments of P^T
 #pragma unroll
           for (int x = 0; x < kHalves; ++x) {
-            float w[4];
-#pragma unroll
-            for (int y = 0; y < 4; ++y) w[y] = fast_exp2(v[i16][x][y] + (vexp[i16][y >> 1] - zero[x][y & 1]));
-#pragma unroll
-            for (int y = 0; y < 2; ++y) l[x][y] += fast_exp2(v[i16][x][y] - base[x][y]) + fast_exp2(v[i16][x][2 + y] - base[x][y]);
-            pb[x][0] = move_matrix_t(pack_f16(w[0], w[1]));
-            pb[x][1] = move_matrix_t(pack_f16(w[2], w[3]));
+            pb[x][0] = move_matrix_t(pw[i16][x][0]);
+            pb[x][1] = move_matrix_t(pw[i16][x][1]);
           }
           // ---- O^T += V^T P^T.  Slots outside the segment's keys may hold anything: their scales are made zeros (and codes are finite).
           uint32_t w[4][kVWords], f[4];
@@ -515,17 +530,17 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
       const int r = 2 * t4 + y + 8 * x;
       if constexpr (kWeigh) {
 #pragma unroll
-        for (int o = 4; o < 32; o <<= 1) join_sums(base_top[x][y], l[x][y], __shfl_xor_sync(0xffffffffu, base_top[x][y], o), __shfl_xor_sync(0xffffffffu, l[x][y], o));
-        if (hr == 0) reinterpret_cast<float2*>(red)[r] = make_float2(base_top[x][y], l[x][y]);
+        for (int o = 4; o < 32; o <<= 1) join_sums(base[x][y], l[x][y], __shfl_xor_sync(0xffffffffu, base[x][y], o), __shfl_xor_sync(0xffffffffu, l[x][y], o));
+        if (hr == 0) reinterpret_cast<float2*>(red)[r] = make_float2(base[x][y], l[x][y]);
       } else {
         float* row = red + r * (D + 4);
         float sum = l[x][y];
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         if (hr == 0) {
-          row[D] = base_top[x][y] == -INFINITY ? -INFINITY : base[x][y];
+          row[D] = base[x][y] == kNothing ? -INFINITY : base[x][y];
           row[D + 1] = sum;
-          row[D + 2] = zero_top[x][y] == -INFINITY ? -INFINITY : zero[x][y] + kWeightTop;
+          row[D + 2] = zero[x][y] == kNothing ? -INFINITY : zero[x][y] + kWeightTop;
         }
 #pragma unroll
         for (int j = 0; j < kCols / 2; ++j)         // columns 2 j and 2 j + 1 of the lane's
@@ -555,12 +570,14 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
   float* red = reinterpret_cast<float*>(scales + stages * SM::kScaleBytes);
   FewBars* bar = reinterpret_cast<FewBars*>(reinterpret_cast<uint8_t*>(red) + SM::red_bytes(kRows));
   volatile int* abort_flag = &bar->abort_flag;
+  // Scales of e2m1 in small pages by copies of the producer's lanes, not TMA (below)
+  const bool own_copies = kE2M1 && c.page_shift < 6;
 
   if (tid == kThreads - 1) {
     tma_prefetch_desc(&mapK);
     tma_prefetch_desc(&mapV);
     for (int s = 0; s < stages; ++s) {
-      mbar_init(&bar->full[s], 1);
+      mbar_init(&bar->full[s], own_copies ? 1 + 32 : 1);
       mbar_init(&bar->empty[s], kE2M1 ? kComputeWarps / 2 : kComputeWarps);
     }
     bar->abort_flag = (smem_u32(smem) & 1023u) != 0 ? 2 : 0;       // the swizzled tiles need a 1024-byte aligned base
@@ -632,7 +649,11 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
     // ================================================================= producer
     // lane -> what it copies of a tile: page `u` of K, V, their exponents
     const int what = lane / copies, u = lane % copies;
-    const uint32_t bytes = what < 2 ? rows * row_bytes(kKind, D) : what < (kCoded ? 4 : 2) ? rows : kE2M1 && what < 6 ? rows * (D / 16) : 0;
+    const uint32_t bytes = what < 2 ? rows * row_bytes(kKind, D) : !kCoded || own_copies ? 0 : what < 4 ? rows : kE2M1 && what < 6 ? rows * (D / 16) : 0;
+    // own_copies: exponents and block scales 16 bytes at a time, since small TMA copies take as long as large ones.  Pages of 16 tokens (24 TMA copies
+    // a tile) 59 / 52 us for 32 sequences of up to 8000, pages of 64 (6) 176 / 180 for 16 of 128K.  Of 16 tokens there are kGroup: their exponents,
+    // then the scales of some.
+    constexpr int kGroup = 1 + D / 16, kScaleCopies = SM::kTensors * kTile / 16 * kGroup, kRounds = kE2M1 ? (kScaleCopies + 31) / 32 : 0;
     int s = 0, ph = 1;
     Piece p;
     while (ok && next_piece(a, walk, p)) {
@@ -664,6 +685,27 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
             bulk_load(scales + s * SM::kScaleBytes + (what - 2) * kTile + u * rows,
                       (what == 2 ? c.ks : c.vs) + page * c.scale_stride + exponent_at<D, kKind>(c, p.g, in_page), rows, &bar->full[s]);
           }
+        }
+        if (own_copies) {
+#pragma unroll
+          for (int round = 0; round < kRounds; ++round) {
+            const int x = round * 32 + lane, tensor = x / (kTile / 16 * kGroup), y = x % (kTile / 16 * kGroup), group = y / kGroup, z = y % kGroup;
+            const int key16 = t * kTile + group * 16;
+            const int page16 = __shfl_sync(0xffffffffu, page_ids, (key16 >> c.page_shift) - entry0);
+            if (x >= kScaleCopies || page16 < 0 || key16 > p.hi || key16 + 16 <= p.lo) continue;
+            const int in_page = key16 & ((1 << c.page_shift) - 1);
+            const uint8_t* src = (tensor ? c.vs : c.ks) + page16 * c.scale_stride;
+            uint8_t* dst = scales + s * SM::kScaleBytes;
+            if (z == 0) {
+              src += exponent_at<D, kKind>(c, p.g, in_page);
+              dst += tensor * kTile + group * 16;
+            } else {
+              src += blocks_at<D>(c, p.g, in_page) + (z - 1) * 16;
+              dst += SM::kTensors * kTile + (tensor * kTile + group * 16) * (D / 16) + (z - 1) * 16;
+            }
+            copy_16(dst, src);
+          }
+          arrive_after_copies(&bar->full[s]);
         }
         if (++s == stages) { s = 0; ph ^= 1; }
       }
