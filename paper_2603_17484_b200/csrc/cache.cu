@@ -86,10 +86,17 @@ __device__ __forceinline__ uint32_t exponent_for_e2m1(uint32_t amax) {
   const int e = (int)(amax >> 7) - 11 + ((amax & 0x7fu) > 0x28u ? 1 : 0);
   return amax == 0 ? 127u : (uint32_t)max(e, 1);
 }
-// y / s for the rounding to e2m1, r = 1 / s: exact where the quotient is half-way between two of them.  y has 8 significant bits, s times
-// a point half-way 7 at most, so that a quotient is such a point or 2^-8 of it away: with 16 bits kept the errors of r and of
-// the product are gone, and nothing else gets to such a point.
-__device__ __forceinline__ float quotient_e2m1(float x) { return __uint_as_float((__float_as_uint(x) + 0x80u) & ~0xffu); }
+// Quotients of the format that lie half-way between two codes or scales have to be that exactly, whatever the errors of a reciprocal (2^-23) and
+// of the product.  x / s and amax / 6 are such points or at least 2^-8 of one away from it: x and amax have 8 significant bits, the point times s (or 6) at
+// most 7.  So rounding to fewer bits first gets to such a point from its neighbourhood only.  Scales: to 16 significant bits; codes, whose
+// points are multiples of 1/4: to multiples of 2^-13, by adding kGrid and taking it away.
+__device__ __forceinline__ float to_16_bits(float x) { return __uint_as_float((__float_as_uint(x) + 0x80u) & ~0xffu); }
+constexpr float kGrid = 1536.f;
+__device__ __forceinline__ float reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 // The two magnitudes of a bf16 pair, 0 for those that are not finite
 __device__ __forceinline__ uint32_t finite_magnitudes(uint32_t x) {
   x &= 0x7fff7fffu;
@@ -102,7 +109,7 @@ __device__ __forceinline__ uint32_t finite_magnitudes(uint32_t x) {
 // 24.8 us (113 MB: 4.6 TB/s), with 16-byte loads, products one by one and indices by division 30.6.
 constexpr int kAppendAhead = 4;
 template <int D, int kKind, int kTokens>
-__global__ void __launch_bounds__(kRowsThreads) cache_append_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(kRowsThreads, 4) cache_append_kernel(const AppendArgs a) {
   constexpr int kLanes = D / 16, kRows = 32 / kLanes, kGroups = kTokens / kRows, kWarps = kRowsThreads / 32;
   constexpr bool kE4M3 = kKind == L2A_CACHE_E4M3, kE2M1 = kKind == L2A_CACHE_E2M1;
   const CacheView& c = a.c;
@@ -186,9 +193,18 @@ __global__ void __launch_bounds__(kRowsThreads) cache_append_kernel(const Append
       }
       if (kE2M1) {
         // A lane has a block: its scale, and what is left over that
-        const float f = __uint_as_float((254u - e) << 23);
-        const uint32_t scale = finite ? pack_e4m3(__fdiv_rn(__uint_as_float(own << 16) * f, 6.f), 0.f) : 0x7fu;
-        const float s = e4m3_value(scale), r = s > 0.f ? __frcp_rn(s) : 0.f;
+        const float f = __uint_as_float((254u - e) << 23);                 // 2^-e
+        const uint32_t scale = finite ? pack_e4m3(to_16_bits(__uint_as_float(own << 16) * f * (1.f / 6.f)), 0.f) : 0x7fu;
+        const float s = e4m3_value(scale), r = s > 0.f ? reciprocal(s) : 0.f;
+        // 2^-e / s is one factor.  Rows of the smallest values, for which it would be more than fp32 holds, are multiplied by 2^64 before.
+        const bool tiny = e <= 16u;
+        if (__any_sync(0xffffffffu, tiny)) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (tiny) w[i][k] = pack_bf16(__uint_as_float(w[i][k] << 16) * 0x1p64f, __uint_as_float(w[i][k] & 0xffff0000u) * 0x1p64f);
+        }
+        const float factor = r * (tiny ? f * 0x1p-64f : f);
+        const float2 g = make_float2(factor, factor);
         uint32_t code[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -196,9 +212,9 @@ __global__ void __launch_bounds__(kRowsThreads) cache_append_kernel(const Append
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const uint32_t u = w[i][4 * k + j];
-            x[j] = __fmul2_rn(make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)), make_float2(f, f));
-            x[j] = __fmul2_rn(x[j], make_float2(r, r));
-            x[j] = make_float2(quotient_e2m1(x[j].x), quotient_e2m1(x[j].y));
+            x[j] = make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+            const float2 y = __fadd2_rn(__ffma2_rn(x[j], g, make_float2(kGrid, kGrid)), make_float2(-kGrid, -kGrid));
+            x[j] = make_float2(copysignf(y.x, x[j].x), copysignf(y.y, x[j].y));
           }
           code[k] = finite ? pack_e2m1(x) : 0u;
         }

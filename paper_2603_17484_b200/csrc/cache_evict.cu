@@ -2,8 +2,8 @@
 // weights in between move, in order, into the pages of another table.
 //
 // cache_select_kernel: a cluster takes a KV head of a sequence, each of its CTAs a range of the positions, whose weights it keeps in shared
-//                      memory as whole numbers of the same order.  The least weight that stays is found digit by digit (8 bits): a CTA
-//                      counts its numbers by digit, and every CTA adds up the counts of all.  Then each lists what stays, at its place.
+//                      memory as whole numbers of the same order.  The least weight that stays is found digit by digit (11, 11 and 10 bits): a
+//                      CTA counts its numbers by digit, and every CTA adds up the counts of all.  Then each lists what stays, at its place.
 //                      Equal weights stay from the lowest position on, whatever the number of CTAs.
 // cache_move_kernel  : 64 rows of a head a CTA (128 of 32 bytes), 16 bytes a thread; nothing is computed.
 #include "cache_common.cuh"
@@ -17,8 +17,8 @@ constexpr int kMostCluster = 8;              // CTAs of a cluster (portable)
 constexpr int kShareKeys = 8192;             // positions of a CTA where the cluster may grow,
 constexpr int kKeepKeys = 48 * 1024;         // and the most that it keeps in shared memory; beyond, weights are read again
 constexpr int kMoveThreads = 256;
-// Rows of a CTA: at least one for four threads, and 16 bytes of a row for each thread
-__host__ __device__ constexpr int move_rows(int row_bytes) { return row_bytes >= 64 ? 64 : 128; }
+// Rows of a CTA: four dependent loads lead to a row, so that a thread has several of them under way
+__host__ __device__ constexpr int move_rows(int row_bytes) { return row_bytes >= 256 ? 64 : row_bytes == 128 ? 128 : 256; }
 
 struct EvictArgs {
   CacheView c, to;
@@ -52,14 +52,16 @@ __device__ __forceinline__ uint32_t remote_u32(const uint32_t* p, uint32_t rank)
   return v;
 }
 
+constexpr int kRounds = 3, kDigits = 2048;
 struct SelectSmem {
-  uint32_t counts[4][256];       // of each digit
+  uint32_t counts[kRounds][kDigits];     // of each digit
+  uint32_t warp_sum[kSelectWarps];
   uint32_t digit, left;
   uint32_t above[kSelectWarps], equal[kSelectWarps];
   uint32_t cta_above, cta_equal;
 };
 
-// Bound by latencies: four rounds of counting with a cluster barrier each.  (The counts of a digit fall into few places, since weights have few
+// Bound by latencies: three rounds of counting with a cluster barrier each.  (The counts of a digit fall into few places, since weights have few
 // exponents; atomics without a result that meet in a warp are one.)
 template <bool kKeep>
 __global__ void __launch_bounds__(kSelectThreads) cache_select_kernel(const EvictArgs a) {
@@ -80,7 +82,7 @@ __global__ void __launch_bounds__(kSelectThreads) cache_select_kernel(const Evic
     else if (i >= k.all - k.last || k.all == k.length) out[i] = k.length - k.all + (int32_t)i;
   }
   if (k.middle == 0 || k.all == k.length) return;          // (the same for the whole cluster)
-  for (int i = tid; i < 4 * 256; i += kSelectThreads) sm.counts[0][i] = 0u;
+  for (int i = tid; i < kRounds * kDigits; i += kSelectThreads) sm.counts[0][i] = 0u;
   // ---- this CTA's range, in parts of 32 positions for each warp
   const int n = to - from, parts = n / 32 + (n % 32 != 0), share = (parts + ctas - 1) / ctas;
   auto edge = [&](int r) { return from + (int)min((int64_t)n, (int64_t)r * share * 32); };
@@ -99,43 +101,40 @@ __global__ void __launch_bounds__(kSelectThreads) cache_select_kernel(const Evic
   // ---- digit by digit: `left` of the numbers that begin with `prefix` stay, and all above them
   uint32_t prefix = 0, left = k.middle;
 #pragma unroll 1
-  for (int round = 0; round < 4; ++round) {
-    const int shift = 24 - 8 * round;
-    const uint32_t mask = round == 0 ? 0u : 0xffffffffu << (shift + 8);
+  for (int round = 0; round < kRounds; ++round) {
+    const int shift = round == 0 ? 21 : round == 1 ? 10 : 0;
+    const uint32_t mask = round == 0 ? 0u : round == 1 ? 0xffe00000u : 0xfffffc00u, digits = round == 2 ? 1023u : 2047u;
     for (int64_t i = tid; i < mine; i += kSelectThreads) {
       const uint32_t x = key((int)i);
-      if (((x ^ prefix) & mask) == 0u) atomicAdd(&sm.counts[round][x >> shift & 255u], 1u);
+      if (((x ^ prefix) & mask) == 0u) atomicAdd(&sm.counts[round][x >> shift & digits], 1u);
     }
     cluster_sync();
-    if (warp == 0) {
-      // a lane has eight digits, the highest first
-      uint32_t v[8], sum = 0;
+    // two digits a thread, the highest first
+    static_assert(kDigits == 2 * kSelectThreads, "two digits a thread");
+    const int d = kDigits - 1 - 2 * tid;
+    uint32_t high = 0, low = 0;
+    for (int r = 0; r < ctas; ++r) {
+      high += remote_u32(&sm.counts[round][d], r);
+      low += remote_u32(&sm.counts[round][d - 1], r);
+    }
+    uint32_t before = high + low;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        v[j] = 0;
-        for (int r = 0; r < ctas; ++r) v[j] += remote_u32(&sm.counts[round][255 - lane * 8 - j], r);
-        sum += v[j];
-      }
-      uint32_t before = sum;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t y = __shfl_up_sync(0xffffffffu, before, o);
-        if (lane >= o) before += y;
-      }
-      before -= sum;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (before < left && left <= before + v[j]) {
-          sm.digit = 255 - lane * 8 - j;
-          sm.left = left - before;
-        }
-        before += v[j];
-      }
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, before, o);
+      if (lane >= o) before += y;
+    }
+    if (lane == 31) sm.warp_sum[warp] = before;
+    before -= high + low;
+    __syncthreads();
+    before += __reduce_add_sync(0xffffffffu, lane < warp ? sm.warp_sum[lane] : 0u);
+    if (before < left && left <= before + high + low) {
+      const bool second = left > before + high;
+      sm.digit = d - second;
+      sm.left = left - before - (second ? high : 0u);
     }
     __syncthreads();
     prefix |= sm.digit << shift;
     left = sm.left;
-    __syncthreads();
   }
   // ---- what each warp's range, then each CTA's, has above the number and equal to it
   const int per = (share + kSelectWarps - 1) / kSelectWarps * 32, w0 = (int)min((int64_t)mine, (int64_t)warp * per), w1 = min(mine - w0, per) + w0;
@@ -218,7 +217,8 @@ __global__ void __launch_bounds__(kMoveThreads) cache_move_kernel(const EvictArg
     to[tid] = y;
   }
   __syncthreads();
-  constexpr int kSteps = kMoveRows * kLanes / kMoveThreads;
+  constexpr int kSteps = kMoveRows * kLanes / kMoveThreads, kRowSteps = (2 * kMoveRows + kMoveThreads - 1) / kMoveThreads;
+  constexpr int kBytes = 1 + kScaleBlocks;                 // of a row's scales
   uint4 k[kSteps], v[kSteps];
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
@@ -229,6 +229,27 @@ __global__ void __launch_bounds__(kMoveThreads) cache_move_kernel(const EvictArg
     k[i] = *reinterpret_cast<const uint4*>(c.K + at);
     v[i] = *reinterpret_cast<const uint4*>(c.V + at);
   }
+  // scales and weights: two threads a row, one for K and the weight, one for V
+  uint32_t exponent[kRowSteps];
+  uint2 blocks[kRowSteps];
+  float weight[kRowSteps];
+#pragma unroll
+  for (int i = 0; i < kRowSteps; ++i) {
+    const int x = i * kMoveThreads + tid, row = x >> 1, value = x & 1;
+    exponent[i] = 0u;
+    blocks[i] = make_uint2(0u, 0u);
+    weight[i] = 0.f;
+    if (row >= kMoveRows || from[row] < 0) continue;
+    const int64_t p = from[row] >> 32;
+    const int in_page = (int)from[row];
+    if (!value) weight[i] = a.w[p * a.w_page + ((int64_t)g << c.page_shift) + in_page];
+    if (kScaleBlocks < 0) continue;
+    const uint8_t* src = (value ? c.vs : c.ks) + p * c.scale_stride + (((int64_t)g * kBytes) << c.page_shift);
+    exponent[i] = src[in_page];
+    src += (1 << c.page_shift) + in_page * kScaleBlocks;
+    if (kScaleBlocks == 8) blocks[i] = *reinterpret_cast<const uint2*>(src);
+    if (kScaleBlocks == 4) blocks[i].x = *reinterpret_cast<const uint32_t*>(src);
+  }
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int x = i * kMoveThreads + tid, row = x / kLanes, piece = x % kLanes;
@@ -237,25 +258,19 @@ __global__ void __launch_bounds__(kMoveThreads) cache_move_kernel(const EvictArg
     *reinterpret_cast<uint4*>(n.K + at) = k[i];
     *reinterpret_cast<uint4*>(n.V + at) = v[i];
   }
-  // ---- weights and scales: four threads a row
-  const int what = tid & 3;
 #pragma unroll
-  for (int row = tid >> 2; row < kMoveRows; row += kMoveThreads / 4) {
-    if (from[row] < 0) continue;
-    const int64_t p = from[row] >> 32, q = to[row] >> 32;
-    const int i = (int)from[row], j = (int)to[row];
-    if (what == 0) {
-      a.w_to[q * a.w_to_page + ((int64_t)g << n.page_shift) + j] = a.w[p * a.w_page + ((int64_t)g << c.page_shift) + i];
-    } else if (what < 3 && kScaleBlocks >= 0) {
-      constexpr int kBytes = 1 + kScaleBlocks;               // of a row
-      const uint8_t* src = (what == 1 ? c.ks : c.vs) + p * c.scale_stride + (((int64_t)g * kBytes) << c.page_shift);
-      uint8_t* dst = (what == 1 ? n.ks : n.vs) + q * n.scale_stride + (((int64_t)g * kBytes) << n.page_shift);
-      dst[j] = src[i];
-      src += (1 << c.page_shift) + i * kScaleBlocks;
-      dst += (1 << n.page_shift) + j * kScaleBlocks;
-      if (kScaleBlocks == 8) *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(src);
-      if (kScaleBlocks == 4) *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(src);
-    }
+  for (int i = 0; i < kRowSteps; ++i) {
+    const int x = i * kMoveThreads + tid, row = x >> 1, value = x & 1;
+    if (row >= kMoveRows || from[row] < 0) continue;
+    const int64_t q = to[row] >> 32;
+    const int in_page = (int)to[row];
+    if (!value) a.w_to[q * a.w_to_page + ((int64_t)g << n.page_shift) + in_page] = weight[i];
+    if (kScaleBlocks < 0) continue;
+    uint8_t* dst = (value ? n.vs : n.ks) + q * n.scale_stride + (((int64_t)g * kBytes) << n.page_shift);
+    dst[in_page] = (uint8_t)exponent[i];
+    dst += (1 << n.page_shift) + in_page * kScaleBlocks;
+    if (kScaleBlocks == 8) *reinterpret_cast<uint2*>(dst) = blocks[i];
+    if (kScaleBlocks == 4) *reinterpret_cast<uint32_t*>(dst) = blocks[i].x;
   }
 }
 

@@ -52,6 +52,9 @@ __host__ __device__ constexpr int ctas_per_sm(int kind, bool high, bool weigh) {
 }
 constexpr int kMostCtas = 3 * kSplitSms;
 constexpr float kWeightTop = 10.f;           // log2 of the largest weight when the reference is new (fp16 operands)
+// e2m1: 16 keys at a time of a tile for each warp; with more, the warps take tiles in turn, and a stage of the ring is held longer.  us for 16
+// sequences of 128K keys: 1 189, 2 176, 4 184.
+constexpr int kE2m1Steps = 2;
 constexpr float kLag = 4.f;                  // the reference follows the maximum when it is more than this behind
 
 struct FewBars {
@@ -211,7 +214,7 @@ __device__ __forceinline__ uint32_t mul_by_half(uint32_t a, __half2 f, bool uppe
   return *reinterpret_cast<const uint32_t*>(&x);
 }
 
-// The tiles of a piece over an e2m1 cache, for one warp: 32 keys of every other.  The keys are the 16 rows of the products' A fragments and the query
+// The tiles of a piece over an e2m1 cache, for one warp: all keys of every fourth, 16 at a time.  The keys are the 16 rows of the products' A fragments and the query
 // rows the 8 columns of B, so that up to eight rows take half as many products and accumulators as with the roles of the other kinds; S^T comes out of one
 // product and goes, transposed, into the other:
 //   S^T = K Q^T : a lane takes a quarter of the codes of two keys, consecutive ones, as its elements of successive products (Q has the same order).
@@ -223,9 +226,8 @@ template <int D, bool kHigh, bool kWeigh>
 __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewSeq& seq, const Piece& p, const uint8_t* smem, const uint8_t* scales,
                                                int stages, FewBars* bar, int& s, int& ph, float* red) {
   using SM = FewSmem<D, L2A_CACHE_E2M1, kWeigh>;
-  constexpr int kHalves = kHigh ? 2 : 1, kCols = D / 8, kVWords = D / 64, kKWords = D / 32;
+  constexpr int kHalves = kHigh ? 2 : 1, kSteps = kE2m1Steps, kWarps = kComputeWarps / kSteps, kCols = D / 8, kVWords = D / 64, kKWords = D / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, hr = lane >> 2, t4 = lane & 3;
-  const int pair = warp >> 1, r0 = (warp & 1) * 32;        // which of two tiles this warp takes, its keys of them
   volatile int* abort_flag = &bar->abort_flag;
   // ---- B fragments of Q: row hr (and hr + 8), this lane's quarter of its elements, the largest of the row at 2^14 .. 2^15
   uint32_t qb[kHalves][D / 16][2];
@@ -295,7 +297,7 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
   // ---- where this lane's operands lie in a stage.  (The swizzle exchanges the 16-byte pieces of a row by its number; rows 8 apart have them
   // in the same order, so that all else is the same distance for every lane.)
   constexpr int kRowBytes = D / 2, kBlockBytes = D / 16;
-  const int k_row = r0 + hr, v_row = r0 + 2 * t4;
+  const int r0 = warp % kWarps * (16 * kSteps), k_row = r0 + hr, v_row = r0 + 2 * t4;       // this warp's keys of a tile
   const uint32_t k_at = smem_u32(smem) + k_row * kRowBytes +
                         (D == 128 ? (t4 ^ ((k_row >> 1) & 3)) << 4 : (((t4 >> 1) ^ ((k_row >> 2) & 1)) << 4) + (t4 & 1) * 8);
   const uint32_t v_at = smem_u32(smem) + SM::kTileBytes + v_row * kRowBytes +
@@ -308,17 +310,17 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
   for (int t = p.t0; t < p.t1; ++t) {
     const int stage = s, phase = ph;
     if (++s == stages) { s = 0; ph ^= 1; }
-    if ((t & 1) != pair) continue;
+    if (t % kSteps != warp / kWarps) continue;
     if (!mbar_wait_warp(&bar->full[stage], phase, abort_flag)) { ok = false; break; }
-    const int key0 = t * kTile + r0;               // first key of this warp's 32
-    if (key0 <= p.hi && key0 + 31 >= p.lo) {
+    const int key0 = t * kTile + r0;
+    if (key0 <= p.hi && key0 + 16 * kSteps > p.lo) {
       const uint32_t tile = stage * SM::kStageBytes, scale = stage * SM::kScaleBytes;
-      const bool edge = key0 < every_lo || key0 + 31 > every_hi;
+      const bool edge = key0 < every_lo || key0 + 16 * kSteps - 1 > every_hi;
       // ---- S^T, 16 keys at a time (i16)
       // v times row_scale: the scores of keys hr (0, 1) and hr + 8 (2, 3), rows 2 t4 and 2 t4 + 1
-      float v[2][kHalves][4];
+      float v[kSteps][kHalves][4];
 #pragma unroll
-      for (int i16 = 0; i16 < 2; ++i16) {
+      for (int i16 = 0; i16 < kSteps; ++i16) {
         float sc[kHalves][4] = {};
         uint32_t w[2][kKWords];
         __half2 f[2];
@@ -361,7 +363,7 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
       }
       if (edge) {
 #pragma unroll
-        for (int i16 = 0; i16 < 2; ++i16)
+        for (int i16 = 0; i16 < kSteps; ++i16)
 #pragma unroll
           for (int x = 0; x < kHalves; ++x)
 #pragma unroll
@@ -375,26 +377,32 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
         for (int x = 0; x < kHalves; ++x)
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            const float f = row_scale[x][y], k4[4] = {v[0][x][y] * f, v[0][x][2 + y] * f, v[1][x][y] * f, v[1][x][2 + y] * f};
+            float z[2 * kSteps], m_new = base[x][y], sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < 2 * kSteps; ++k) {
+              z[k] = v[k / 2][x][(k & 1) * 2 + y] * row_scale[x][y];
+              m_new = fmaxf(m_new, z[k]);
+            }
             if (row_hi[x][y] >= 0) {
               float* dst = score_at + (int64_t)(8 * x + y) * a.score_pitch + key0;
 #pragma unroll
-              for (int k = 0; k < 4; ++k) dst[8 * k] = k4[k];
+              for (int k = 0; k < 2 * kSteps; ++k) dst[8 * k] = z[k];
             }
             // (each lane by itself: its keys are joined with the others' at the end)
-            const float m_new = fmaxf(base[x][y], fmaxf(fmaxf(k4[0], k4[1]), fmaxf(k4[2], k4[3]))), b = m_new == -INFINITY ? 0.f : m_new;
-            l[x][y] = l[x][y] * fast_exp2(base[x][y] - b) +
-                      ((fast_exp2(k4[0] - b) + fast_exp2(k4[1] - b)) + (fast_exp2(k4[2] - b) + fast_exp2(k4[3] - b)));
+            const float b = m_new == -INFINITY ? 0.f : m_new;
+#pragma unroll
+            for (int k = 0; k < 2 * kSteps; ++k) sum += fast_exp2(z[k] - b);
+            l[x][y] = l[x][y] * fast_exp2(base[x][y] - b) + sum;
             base[x][y] = m_new;
           }
       } else {
         // ---- weights: the score plus the value's exponent is what they are two to the power of, relative to `zero`.  They are computed with what the
         // rows had; where one comes out at 2^15 or more, or the sum above kMostSum, the row follows its new maximum and they are computed again.
         constexpr float kMostSum = 0x1p64f;
-        float vexp[2][2], sum[kHalves][2];
-        uint32_t pw[2][kHalves][2];                // as fp16, rows 2 t4 and 2 t4 + 1 of a key
+        float vexp[kSteps][2], sum[kHalves][2];
+        uint32_t pw[kSteps][kHalves][2];                // as fp16, rows 2 t4 and 2 t4 + 1 of a key
 #pragma unroll
-        for (int i16 = 0; i16 < 2; ++i16)
+        for (int i16 = 0; i16 < kSteps; ++i16)
 #pragma unroll
           for (int k = 0; k < 2; ++k)
             vexp[i16][k] = __uint_as_float(0x4b000000u | lds8(exp_at + scale + kTile + i16 * 16 + k * 8)) - 8388735.f;             // e - 127
@@ -406,7 +414,7 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
 #pragma unroll
             for (int y = 0; y < 2; ++y) sum[x][y] = l[x][y];
 #pragma unroll
-            for (int i16 = 0; i16 < 2; ++i16)
+            for (int i16 = 0; i16 < kSteps; ++i16)
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
                 float w[2];
@@ -426,7 +434,7 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
           // Values of zeros have exponent 0 however small all others are: they must not become the reference, which would push the
           // weights of the others out of fp16's range.  They get the least exponent.
 #pragma unroll
-          for (int i16 = 0; i16 < 2; ++i16)
+          for (int i16 = 0; i16 < kSteps; ++i16)
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
               uint32_t any = 0;
@@ -443,7 +451,7 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
             for (int y = 0; y < 2; ++y) {
               float m_new = -INFINITY, top = -INFINITY;
 #pragma unroll
-              for (int i16 = 0; i16 < 2; ++i16)
+              for (int i16 = 0; i16 < kSteps; ++i16)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                   const float z = v[i16][x][2 * k + y] * row_scale[x][y];
@@ -473,9 +481,9 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
         }
 #pragma unroll
         for (int x = 0; x < kHalves; ++x) { l[x][0] = sum[x][0]; l[x][1] = sum[x][1]; }
-        const bool clear = key0 < p.lo || key0 + 31 > p.hi;
+        const bool clear = key0 < p.lo || key0 + 16 * kSteps - 1 > p.hi;
 #pragma unroll
-        for (int i16 = 0; i16 < 2; ++i16) {
+        for (int i16 = 0; i16 < kSteps; ++i16) {
           uint32_t pb[kHalves][2];                 // B fragments of P^T
 #pragma unroll
           for (int x = 0; x < kHalves; ++x) {
@@ -578,7 +586,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
     tma_prefetch_desc(&mapV);
     for (int s = 0; s < stages; ++s) {
       mbar_init(&bar->full[s], own_copies ? 1 + 32 : 1);
-      mbar_init(&bar->empty[s], kE2M1 ? kComputeWarps / 2 : kComputeWarps);
+      mbar_init(&bar->empty[s], kE2M1 ? kComputeWarps / kE2m1Steps : kComputeWarps);
     }
     bar->abort_flag = (smem_u32(smem) & 1023u) != 0 ? 2 : 0;       // the swizzled tiles need a 1024-byte aligned base
     fence_mbar_init();
@@ -1267,7 +1275,7 @@ __global__ void __launch_bounds__(kCombineThreads) cache_few_combine_kernel(cons
 
 // The weights of the keys of one KV head: what a row's soft-max gives them, summed over the rows, onto what they had (the new tokens' own keys
 // had nothing).  Bound by latencies and the scores' way through L2: a thread has four keys, and the rows' loads are in flight together.
-constexpr int kAddThreads = 256, kAddKeys = 4 * kAddThreads, kMaxRows = kRowBlocks * kBlockRows;
+constexpr int kAddThreads = 256, kAddSteps = 1, kAddKeys = 4 * kAddThreads * kAddSteps, kMaxRows = kRowBlocks * kBlockRows;
 __global__ void __launch_bounds__(kAddThreads) cache_few_add_kernel(const CacheFwdArgs a, const int slot_rows) {
   __shared__ float lse[kMaxRows];
   const CacheView& c = a.c;
@@ -1298,23 +1306,27 @@ __global__ void __launch_bounds__(kAddThreads) cache_few_add_kernel(const CacheF
     if (lane == 0) lse[r] = l != 0.f ? m + log2f(l) : INFINITY;          // (infinity: a row that sees nothing)
   }
   if (__syncthreads_or(failed)) return;                // a wait ran out in a part: nothing is stored
-  const int key = (int)k0 + 4 * tid;
-  if (key >= length) return;
-  const float* s = a.scores + (int64_t)(b * c.Hkv + g) * a.score_rows * a.score_pitch + key;
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
-  if (key <= hi) {
+  const float* scores = a.scores + (int64_t)(b * c.Hkv + g) * a.score_rows * a.score_pitch;
+#pragma unroll 1
+  for (int i = 0; i < kAddSteps; ++i) {
+    const int64_t key0 = k0 + (int64_t)i * 4 * kAddThreads + 4 * tid;
+    if (key0 >= length) break;
+    const int key = (int)key0;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if (key <= hi) {
 #pragma unroll 4
-    for (int r = 0; r < rows; ++r) {
-      const float z = lse[r];
-      if (z == INFINITY) continue;
-      const float4 v = __ldcs(reinterpret_cast<const float4*>(s + (int64_t)r * a.score_pitch));
-      sum[0] += fast_exp2(v.x - z);
-      sum[1] += key + 1 <= hi ? fast_exp2(v.y - z) : 0.f;
-      sum[2] += key + 2 <= hi ? fast_exp2(v.z - z) : 0.f;
-      sum[3] += key + 3 <= hi ? fast_exp2(v.w - z) : 0.f;
+      for (int r = 0; r < rows; ++r) {
+        const float z = lse[r];
+        if (z == INFINITY) continue;
+        const float4 v = __ldcs(reinterpret_cast<const float4*>(scores + (int64_t)r * a.score_pitch + key));
+        sum[0] += fast_exp2(v.x - z);
+        sum[1] += key + 1 <= hi ? fast_exp2(v.y - z) : 0.f;
+        sum[2] += key + 2 <= hi ? fast_exp2(v.z - z) : 0.f;
+        sum[3] += key + 3 <= hi ? fast_exp2(v.w - z) : 0.f;
+      }
     }
+    add_weights(a, c, b, g, key, length, length - n, hi, sum);
   }
-  add_weights(a, c, b, g, key, length, length - n, hi, sum);
 }
 
 constexpr int kSmemPerSm = 228 * 1024;           // 1 KB of each CTA's share is not its own
