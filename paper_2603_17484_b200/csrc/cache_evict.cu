@@ -51,10 +51,15 @@ __device__ __forceinline__ uint32_t remote_u32(const uint32_t* p, uint32_t rank)
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(cluster_map(smem_u32(p), rank)));
   return v;
 }
+__device__ __forceinline__ uint2 remote_u64(const uint32_t* p, uint32_t rank) {
+  uint2 v;
+  asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(cluster_map(smem_u32(p), rank)));
+  return v;
+}
 
 constexpr int kRounds = 3, kDigits = 2048;
 struct SelectSmem {
-  uint32_t counts[kRounds][kDigits];     // of each digit
+  alignas(8) uint32_t counts[kRounds][kDigits];     // of each digit
   uint32_t warp_sum[kSelectWarps];
   uint32_t digit, left;
   uint32_t above[kSelectWarps], equal[kSelectWarps];
@@ -112,11 +117,12 @@ __global__ void __launch_bounds__(kSelectThreads) cache_select_kernel(const Evic
     // two digits a thread, the highest first
     static_assert(kDigits == 2 * kSelectThreads, "two digits a thread");
     const int d = kDigits - 1 - 2 * tid;
+    uint2 got[kMostCluster];
+#pragma unroll
+    for (int r = 0; r < kMostCluster; ++r) got[r] = r < ctas ? remote_u64(&sm.counts[round][d - 1], r) : make_uint2(0u, 0u);
     uint32_t high = 0, low = 0;
-    for (int r = 0; r < ctas; ++r) {
-      high += remote_u32(&sm.counts[round][d], r);
-      low += remote_u32(&sm.counts[round][d - 1], r);
-    }
+#pragma unroll
+    for (int r = 0; r < kMostCluster; ++r) { low += got[r].x; high += got[r].y; }
     uint32_t before = high + low;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -362,7 +368,7 @@ extern "C" l2a_status l2a_cache_evict(const l2a_params* p, const l2a_cache* c, c
   a.lengths = to_lengths;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   int ctas = 1;
-  while (ctas < kMostCluster && p->Lk > ctas * kShareKeys) ctas *= 2;
+  while (ctas < kMostCluster && p->Lk > (int64_t)ctas * kShareKeys) ctas *= 2;
   const int64_t share = (((int64_t)p->Lk + 31) / 32 + ctas - 1) / ctas * 32;
   cudaError_t e = share <= kKeepKeys ? launch_select<true>(a, ctas, (size_t)share * 4, s) : launch_select<false>(a, ctas, 0, s);
   if (e == cudaSuccess) e = launch_move_kind(a, s);
