@@ -6,14 +6,16 @@
 //
 // weigh_plan_kernel : one CTA lists the counted tokens and the blocks of rows; the others decode the keys of an 8- or 4-bit cache to bf16.
 // weigh_rows_kernel : the blocks' rows of Q side by side.
-// weigh_pass_kernel : tiles of 128 x 128 scores, tcgen05, one operand kept for a piece of work, the other streamed past it; four tiles
-//                     under way in TMEM, two warpgroups take them in turn, a lane of TMEM to a thread.
-//     first pass    : a block of rows is kept, keys pass: a thread has a row, its running maximum and sum.  All tiles of the call, laid end to
-//                     end, are cut into even ranges, one a CTA; what a range leaves of a row is joined by weigh_join_kernel.
-//     second pass   : 128 keys are kept, the blocks that see them pass: a thread has a key and sums the weights of its column.  A key's sum is
-//                     made by one CTA in a fixed order: bit-reproducible.
+// weigh_pass_kernel : up to four blocks of rows of a KV head stay in shared memory, 128 keys at a time pass and are multiplied with all of them
+//                     (tcgen05, tiles of 128 x 128 scores in TMEM, one for each of four warpgroups, a lane to a thread, 32 columns at a time).
+//     first pass    : S = Q K^T, a thread has a row, its running maximum and sum.
+//     second pass   : S^T = K Q^T, a thread has a key and sums the weights of its column; another warp adds up the blocks' sums.
+//                     The key tiles of the call, laid end to end and weighed by the blocks of their sequence, are cut into even ranges, one a CTA:
+//                     in the first pass a range leaves a part of the rows' sums, which weigh_join_kernel joins; in the second it owns its keys, so
+//                     that a weight is made by one CTA in a fixed order: bit-reproducible.
 // Bound by the exponentials: 16384 a tile, 1024 clk on the special-function unit, next to 512 clk of products; a quarter of them is computed on the
-// FMA pipe.
+// FMA pipe.  With one block kept and keys streamed past it (32 KB from L2 a tile) L2 was the bound: 4 sequences of up to 16384 keys, 400 tokens of
+// the longest, 30 % counted (28/4 heads): 40 and 58 us for the passes.
 #include <math.h>
 
 #include <algorithm>
@@ -26,8 +28,9 @@ namespace {
 
 constexpr int kCtas = kSplitSms;
 constexpr int kPlanThreads = 1024;
-constexpr int kSumWarps = 8, kTmaWarp = 8, kMmaWarp = 9, kPassThreads = 10 * 32;
-constexpr int kYStages = 4, kScoreBufs = 4;
+constexpr int kKept = 4;                     // blocks of rows, and warpgroups
+constexpr int kSumWarps = 4 * kKept, kTmaWarp = kSumWarps, kMmaWarp = kSumWarps + 1, kAddWarp = kSumWarps + 2, kPassThreads = (kSumWarps + 3) * 32;
+constexpr int kKStages = 2, kSumBufs = 2;
 constexpr int kBoxBytes = 128 * 128;         // 128 rows of 128 bytes
 
 // A block of 128 counted rows of a sequence: packed row r is that of token list[list + r / G], head r % G of the group
@@ -35,9 +38,9 @@ struct alignas(16) RowBlock {
   int b, list, row0, n_rows;
   int base, tiles, last;         // position = base + token; key tiles that some row sees; position of the last row
   int first_pos;                 // of the first row: keys up to there are seen by all
-  int64_t units, pad;            // key tiles of the blocks before
 };
-struct WeighPlan { int n_blocks; int64_t units, tiles; };
+// A unit: a key tile, times the blocks of rows of its sequence (one where there are none)
+struct WeighPlan { int n_blocks, most; int64_t units, share; };     // blocks; most of a sequence; units of a KV head; of a CTA
 
 struct WeighArgs {
   CacheFwdArgs f;                // f.c: the bf16 cache or the decoded copy
@@ -47,12 +50,12 @@ struct WeighArgs {
   int* list;                     // counted tokens
   int *list_start, *list_end;    // of a sequence
   int* block_start;              // first block of a sequence, [B + 1],
-  int64_t* tile_start;           // key tiles of the sequences before it, [B + 1]
+  int64_t* unit_start;           // units of the sequences before it, [B + 1]
   bf16* rows;                    // [Hkv][most_blocks * 128][D]
   int* row_pos;                  // [most_blocks * 128], -1: no row
   float* minus_lse;              // [Hkv][most_blocks * 128], minus infinity: no row
-  float2* part;                  // of a range: maximum and sum of 128 rows, from each warpgroup
-  int most_blocks;
+  float2* part;                  // maximum and sum of 128 rows, from a range
+  int most_blocks;               // bound
   int clear;                     // no kernel ahead has cleared the status word
 };
 
@@ -125,59 +128,54 @@ __device__ void make_plan(const WeighArgs& p, int* sums, int64_t* sums2) {
     base += all;
   }
   __syncthreads();
-  // ---- blocks of rows and key tiles of every sequence
-  int block_base = 0;
-  int64_t tile_base = 0;
+  // ---- blocks of rows and units of every sequence
+  int block_base = 0, most = 1;
+  int64_t unit_base = 0;
   for (int b0 = 0; b0 < c.B; b0 += kPlanThreads) {
     const int b = b0 + tid;
     int first, length = 0, n = 0;
     if (b < c.B && !bad) n = sequence(a, b, first, length);
     const int blocks = n > 0 ? compact_tiles(p.list_end[b] - p.list_start[b], a.G) : 0;
-    const int tiles = n > 0 ? (length + kTileN - 1) / kTileN : 0;
+    const int64_t units = n > 0 ? (int64_t)((length + kTileN - 1) / kTileN) * max(blocks, 1) : 0;
     int x = blocks;
-    int64_t y = tiles;
+    int64_t y = units;
     const int all = block_scan(x, sums);
-    const int64_t all_tiles = block_scan(y, sums2);
+    const int64_t all_units = block_scan(y, sums2);
     if (b < c.B) {
       p.block_start[b] = block_base + x - blocks;
-      p.tile_start[b] = tile_base + y - tiles;
+      p.unit_start[b] = unit_base + y - units;
     }
     block_base += all;
-    tile_base += all_tiles;
+    unit_base += all_units;
+    most = max(most, blocks);
   }
+  most = __reduce_max_sync(0xffffffffu, most);
+  __syncthreads();
+  if ((tid & 31) == 0) sums[tid >> 5] = most;
+  __syncthreads();
+  most = __reduce_max_sync(0xffffffffu, sums[tid & 31]);
   if (tid == 0) {
     p.block_start[c.B] = block_base;
-    p.tile_start[c.B] = tile_base;
+    p.unit_start[c.B] = unit_base;
+    // (a CTA has the tiles whose first unit is in its range; with a tile's units or more a range has one wherever it begins)
+    *p.plan = WeighPlan{block_base, most, unit_base, max((int64_t)most, (unit_base * c.Hkv + kCtas - 1) / kCtas)};
   }
   __syncthreads();
   // ---- the blocks
-  int64_t units = 0;
-  for (int q0 = 0; q0 < block_base; q0 += kPlanThreads) {
-    const int q = q0 + tid;
+  for (int q = tid; q < block_base; q += kPlanThreads) {
     RowBlock r;
-    r.tiles = 0;
-    if (q < block_base) {
-      int first, length;
-      r.b = last_not_above(p.block_start, c.B, q);     // (the last: it has blocks)
-      const int n = sequence(a, r.b, first, length);
-      r.list = p.list_start[r.b];
-      r.row0 = (q - p.block_start[r.b]) * kTileM;
-      r.n_rows = min(kTileM, (p.list_end[r.b] - r.list) * a.G - r.row0);
-      r.base = length - n - first;
-      r.first_pos = r.base + p.list[r.list + r.row0 / a.G];
-      r.last = r.base + p.list[r.list + (r.row0 + r.n_rows - 1) / a.G];
-      r.tiles = r.last / kTileN + 1;
-    }
-    int64_t x = r.tiles;
-    const int64_t all = block_scan(x, sums2);
-    if (q < block_base) {
-      r.units = units + x - r.tiles;
-      r.pad = 0;
-      p.blocks[q] = r;
-    }
-    units += all;
+    int first, length;
+    r.b = last_not_above(p.block_start, c.B, q);       // (the last: it has blocks)
+    const int n = sequence(a, r.b, first, length);
+    r.list = p.list_start[r.b];
+    r.row0 = (q - p.block_start[r.b]) * kTileM;
+    r.n_rows = min(kTileM, (p.list_end[r.b] - r.list) * a.G - r.row0);
+    r.base = length - n - first;
+    r.first_pos = r.base + p.list[r.list + r.row0 / a.G];
+    r.last = r.base + p.list[r.list + (r.row0 + r.n_rows - 1) / a.G];
+    r.tiles = r.last / kTileN + 1;
+    p.blocks[q] = r;
   }
-  if (tid == 0) *p.plan = WeighPlan{block_base, units, tile_base};
 }
 
 // Keys of an 8- or 4-bit cache as bf16, pages of 128 tokens [page][KV head][128][D].  A lane brings 16 codes, a warp 512 / D keys at a time, 32
@@ -271,96 +269,70 @@ __global__ void __launch_bounds__(kRowsThreads) weigh_rows_kernel(const WeighArg
 }
 
 // ------------------------------------------------------------------------------------------------------------- passes
-// A piece of work: a block of rows and some key tiles, or a key tile and some blocks of rows
+// A piece of work: some key tiles of a KV head of a sequence, by their places in the line
 struct WeighPiece {
-  int b, g, x, y0, n;      // sequence, KV head, what is kept, the first of the n that pass
-  int slot;                // first pass
-  int length;
+  int b, g, k0, k1;
+  int tiles, length;       // of the sequence
+  int q0, blocks;          // its blocks of rows
 };
-template <bool kSum>
+// Early tiles are seen by all rows, late ones by few: places take them from both ends in turn
+__device__ __forceinline__ int tile_of(const WeighPiece& w, int k) { return k & 1 ? w.tiles - 1 - (k >> 1) : k >> 1; }
+
 struct WeighWalk {
-  int64_t at, end, step, units;
-  int q, n_blocks;
+  int64_t at, end, units;
   __device__ __forceinline__ void init(const WeighArgs& p) {
     const WeighPlan plan = *p.plan;
-    const int Hkv = p.f.c.Hkv;
-    n_blocks = plan.n_blocks;
-    q = -1;
-    if (kSum) {
-      at = blockIdx.x;
-      step = gridDim.x;
-      end = plan.tiles * Hkv;
-    } else {
-      units = plan.units;
-      const int64_t total = units * Hkv, share = (total + gridDim.x - 1) / gridDim.x;
-      at = min(total, blockIdx.x * share);
-      end = min(total, at + share);
-    }
+    units = plan.units;
+    const int64_t total = units * p.f.c.Hkv;
+    at = min(total, blockIdx.x * plan.share);
+    end = min(total, at + plan.share);
   }
   __device__ __forceinline__ bool next(const WeighArgs& p, WeighPiece& w) {
-    const CacheView& c = p.f.c;
-    for (;;) {
-      if (at >= end) return false;
-      if (kSum) {
-        // the key tiles of a head of a sequence follow each other
-        int lo = 0, hi = c.B;
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (p.tile_start[mid] * c.Hkv <= at) lo = mid; else hi = mid;
-        }
-        const int64_t before = p.tile_start[lo], tiles = p.tile_start[lo + 1] - before, in = at - before * c.Hkv;
-        w.b = lo;
-        w.g = (int)(in / tiles);
-        w.x = (int)(in % tiles);
-        // the blocks whose last row sees it: positions ascend
-        int first = p.block_start[lo], last = p.block_start[lo + 1];
-        w.n = last;
-        while (first < last) {
-          const int mid = (first + last) >> 1;
-          if (p.blocks[mid].tiles > w.x) last = mid; else first = mid + 1;
-        }
-        w.y0 = first;
-        w.n -= first;
-        w.slot = 0;
-        at += step;
-      } else {
-        const int64_t g = at / units, in = at - g * units;
-        if (q < 0) {
-          int lo = 0, hi = n_blocks;
-          while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (p.blocks[mid].units <= in) lo = mid; else hi = mid;
-          }
-          q = lo;
-        } else if (++q == n_blocks) {
-          q = 0;
-        }
-        const RowBlock& r = p.blocks[q];
-        w.b = r.b;
-        w.g = (int)g;
-        w.x = q;
-        w.y0 = (int)(in - r.units);
-        w.n = (int)min((int64_t)(r.tiles - w.y0), end - at);
-        w.slot = (int)g * n_blocks + q + blockIdx.x;
-        at += w.n;
-      }
-      w.length = cache_length(c, w.b);
-      return true;
+    while (at < end) {
+      const int64_t in = at % units;
+      w.g = (int)(at / units);
+      w.b = last_not_above(p.unit_start, p.f.c.B, in);                   // (the last: it has units)
+      w.length = cache_length(p.f.c, w.b);
+      w.tiles = (w.length + kTileN - 1) / kTileN;
+      w.q0 = p.block_start[w.b];
+      w.blocks = p.block_start[w.b + 1] - w.q0;
+      const int64_t first = p.unit_start[w.b], last = p.unit_start[w.b + 1], of_tile = max(w.blocks, 1);
+      w.k0 = (int)((in - first + of_tile - 1) / of_tile);
+      w.k1 = (int)((min(in + (end - at), last) - first + of_tile - 1) / of_tile);
+      at += min(end - at, last - in);
+      if (w.k0 < w.k1) return true;
     }
+    return false;
   }
+};
+// The blocks that are kept at a time: n of them from q on.  One tile of keys takes `width` warpgroups (block i: warpgroup i of those), so that `wide` tiles
+// are under way together.
+struct Kept {
+  int q, n, width, wide;
+  int tiles[kKept];        // that each of them sees (ascending; 0: no block)
+  __device__ __forceinline__ Kept(const WeighArgs& p, const WeighPiece& w, int i0) {
+    q = w.q0 + i0;
+    n = min(kKept, w.blocks - i0);
+    width = n <= 1 ? 1 : n == 2 ? 2 : 4;
+    wide = kKept / width;
+#pragma unroll
+    for (int i = 0; i < kKept; ++i) tiles[i] = i < n ? p.blocks[q + i].tiles : 0;
+  }
+  __device__ __forceinline__ int seen() const { return max(max(tiles[0], tiles[1]), max(tiles[2], tiles[3])); }
 };
 
 struct PassBars {
-  uint64_t x_full[2], x_empty[2], y_full[kYStages], y_empty[kYStages], s_full[kScoreBufs], s_empty[kScoreBufs];
+  uint64_t q_full, q_empty, k_full[kKStages], k_empty[kKStages], s_full[kKept], s_empty[kKept], sum_full[kSumBufs], sum_empty[kSumBufs];
   uint32_t tmem_base;
   int abort_flag;
 };
 template <int D>
 struct PassSmem {
   static constexpr int kTileBytes = 128 * D * 2;
-  static constexpr int kYOff = 2 * kTileBytes, kStageOff = kYOff + kYStages * kTileBytes;
-  static constexpr int kSumOff = kStageOff + kSumWarps * 1024;           // a warp's copy of what its columns need
-  static constexpr int kBarOff = kSumOff + 2 * 2 * 128 * 4;
+  static constexpr int kKOff = kKept * kTileBytes, kStageOff = kKOff + kKStages * kTileBytes;
+  static constexpr int kSumOff = kStageOff + kSumWarps * 1024;           // (a warp's copy of what its columns need)
+  static constexpr int kSumBytes = kKept * 128 * 8;                      // first pass: maxima and sums; second: two buffers of sums
+  static constexpr int kBarOff = kSumOff + kSumBytes;
   static constexpr int kTotal = kBarOff + 256 + 1024 /* alignment slack */;
 };
 static_assert(sizeof(PassBars) <= 256, "barriers");
@@ -378,9 +350,11 @@ weigh_pass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
   PassBars* bar = reinterpret_cast<PassBars*>(smem + SM::kBarOff);
   volatile int* abort_flag = &bar->abort_flag;
   if (tid == kTmaWarp * 32) {
-    for (int i = 0; i < 2; ++i) { mbar_init(&bar->x_full[i], 1); mbar_init(&bar->x_empty[i], 1); }
-    for (int i = 0; i < kYStages; ++i) { mbar_init(&bar->y_full[i], 1); mbar_init(&bar->y_empty[i], 1); }
-    for (int i = 0; i < kScoreBufs; ++i) { mbar_init(&bar->s_full[i], 1); mbar_init(&bar->s_empty[i], 4); }
+    mbar_init(&bar->q_full, 1);
+    mbar_init(&bar->q_empty, 1);
+    for (int i = 0; i < kKStages; ++i) { mbar_init(&bar->k_full[i], 1); mbar_init(&bar->k_empty[i], 1); }
+    for (int i = 0; i < kKept; ++i) { mbar_init(&bar->s_full[i], 1); mbar_init(&bar->s_empty[i], 4); }
+    for (int i = 0; i < kSumBufs; ++i) { mbar_init(&bar->sum_full[i], kSumWarps); mbar_init(&bar->sum_empty[i], 1); }
     bar->abort_flag = 0;
     fence_mbar_init();
   }
@@ -395,7 +369,7 @@ weigh_pass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bar->tmem_base;
-  WeighWalk<kSum> walk;
+  WeighWalk walk;
   walk.init(p);
   if (lost) walk.at = walk.end;
   WeighPiece w;
@@ -407,180 +381,228 @@ weigh_pass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
       tma_prefetch_desc(&mapQ);
       tma_prefetch_desc(&mapK);
     }
-    const int rows = 1 << c.page_shift, copies = 128 >> c.page_shift, u = lane % copies, piece = lane / copies;
-    const uint32_t bytes = rows * 128;
-    uint32_t x_cnt = 0, y_cnt = 0;
+    const int copies = 128 >> c.page_shift, u = lane % copies, piece = lane / copies;
+    const uint32_t bytes = (1u << c.page_shift) * 128;
+    uint32_t q_cnt = 0, k_cnt = 0;
     while (ok && walk.next(p, w)) {
-      if (w.n == 0) continue;
-      int entry0 = -512, page_ids = -1;
       const int last_entry = (w.length - 1) >> c.page_shift;
-      auto load_k = [&](int tile, uint8_t* dst, uint64_t* full) {
-        const int first = (int)(((int64_t)tile * kTileN) >> c.page_shift), entry = first + u;
-        if (first < entry0 || first + copies - 1 - entry0 >= 32) {
-          entry0 = first;
-          const int e = entry0 + lane;
-          page_ids = e <= last_entry ? cache_page(c, w.b, e << c.page_shift) : -1;
-        }
-        const int page = __shfl_sync(0xffffffffu, page_ids, entry - entry0);
-        const bool load = piece < D / 64 && page >= 0 && entry <= last_entry;
-        const uint32_t expect = __popc(__ballot_sync(0xffffffffu, load)) * bytes;
-        if (lane == 0) mbar_expect_tx(full, expect);
-        __syncwarp();
-        if (load) tma_load_page(dst + piece * kBoxBytes + u * bytes, &mapK, full, false, piece, 0, w.g, page);
+      auto page_of = [&](int k) -> int {         // of this lane's rows of the tile at place k, -1: none
+        const int entry = (int)(((int64_t)tile_of(w, k) * kTileN) >> c.page_shift) + u;
+        return k < w.k1 && piece < D / 64 && entry <= last_entry ? cache_page(c, w.b, entry << c.page_shift) : -1;
       };
-      auto load_q = [&](int block, uint8_t* dst, uint64_t* full) {
-        if (lane == 0) {
-          mbar_expect_tx(full, SM::kTileBytes);
-          tma_load_4d(dst, &mapQ, full, 0, block * kTileM, 0, w.g);
-        }
-        __syncwarp();
-      };
-      auto load = [&](bool keys, int i, uint8_t* dst, uint64_t* full) {
-        if (keys) load_k(i, dst, full); else load_q(i, dst, full);
-      };
-      ok = mbar_wait_warp(&bar->x_empty[x_cnt & 1], ((x_cnt >> 1) & 1) ^ 1, abort_flag);
-      if (!ok) break;
-      load(kSum, w.x, smem + (x_cnt & 1) * SM::kTileBytes, &bar->x_full[x_cnt & 1]);
-      ++x_cnt;
-      for (int i = 0; i < w.n; ++i, ++y_cnt) {
-        const int s = y_cnt % kYStages;
-        ok = mbar_wait_warp(&bar->y_empty[s], ((y_cnt / kYStages) & 1) ^ 1, abort_flag);
+      for (int i0 = 0; ok && i0 < w.blocks; i0 += kKept) {
+        const Kept kept(p, w, i0);
+        const int seen = kept.seen();
+        ok = mbar_wait_warp(&bar->q_empty, (q_cnt & 1) ^ 1, abort_flag);
         if (!ok) break;
-        load(!kSum, w.y0 + i, smem + SM::kYOff + s * SM::kTileBytes, &bar->y_full[s]);
+        ++q_cnt;
+        if (lane == 0) {
+          mbar_expect_tx(&bar->q_full, kept.n * SM::kTileBytes);
+          for (int i = 0; i < kept.n; ++i) tma_load_4d(smem + i * SM::kTileBytes, &mapQ, &bar->q_full, 0, (kept.q + i) * kTileM, 0, w.g);
+        }
+        __syncwarp();
+        int page = page_of(w.k0), next = page_of(w.k0 + 1);              // (looked up two tiles ahead)
+        for (int k = w.k0; k < w.k1; ++k) {
+          const int later = page_of(k + 2);
+          if (tile_of(w, k) < seen) {
+            const int s = k_cnt % kKStages;
+            ok = mbar_wait_warp(&bar->k_empty[s], ((k_cnt / kKStages) & 1) ^ 1, abort_flag);
+            if (!ok) break;
+            ++k_cnt;
+            const uint32_t expect = __popc(__ballot_sync(0xffffffffu, page >= 0)) * bytes;
+            if (lane == 0) mbar_expect_tx(&bar->k_full[s], expect);
+            __syncwarp();
+            if (page >= 0)
+              tma_load_page(smem + SM::kKOff + s * SM::kTileBytes + piece * kBoxBytes + u * bytes, &mapK, &bar->k_full[s], false, piece, 0, w.g, page);
+          }
+          page = next;
+          next = later;
+        }
       }
     }
   } else if (warp == kMmaWarp) {
     // =========================================================================== MMA issuer
     if (elect_one()) {
       constexpr uint32_t idesc = idesc_bf16_f32(128, 128, 0, 0);
-      const uint64_t dx = smem_desc_sw128(smem_u32(smem), 16, 1024), dy = smem_desc_sw128(smem_u32(smem + SM::kYOff), 16, 1024);
-      uint32_t x_cnt = 0, cnt = 0;
+      const uint64_t dq = smem_desc_sw128(smem_u32(smem), 16, 1024), dk = smem_desc_sw128(smem_u32(smem + SM::kKOff), 16, 1024);
+      uint32_t q_cnt = 0, k_cnt = 0, phases = 0;         // bit wg: phase of its scores' buffer
       while (ok && walk.next(p, w)) {
-        if (w.n == 0) continue;
-        const uint32_t xs = x_cnt & 1;
-        if (!mbar_spin(&bar->x_full[xs], (x_cnt >> 1) & 1, abort_flag)) break;
-        for (int i = 0; i < w.n; ++i, ++cnt) {
-          const uint32_t s = cnt % kYStages, buf = cnt % kScoreBufs;
-          if (!mbar_spin(&bar->s_empty[buf], ((cnt / kScoreBufs) & 1) ^ 1, abort_flag) ||
-              !mbar_spin(&bar->y_full[s], (cnt / kYStages) & 1, abort_flag)) {
-            ok = false;
-            break;
-          }
-          tc_fence_after();
+        for (int i0 = 0; ok && i0 < w.blocks; i0 += kKept) {
+          const Kept kept(p, w, i0);
+          const int seen = kept.seen();
+          if (!mbar_spin(&bar->q_full, q_cnt & 1, abort_flag)) { ok = false; break; }
+          ++q_cnt;
+          for (int k = w.k0; ok && k < w.k1; ++k) {
+            const int t = tile_of(w, k), wg0 = (k - w.k0) % kept.wide * kept.width;
+            if (t >= seen) continue;
+            const uint32_t s = k_cnt % kKStages;
+            if (!mbar_spin(&bar->k_full[s], (k_cnt / kKStages) & 1, abort_flag)) { ok = false; break; }
+            ++k_cnt;
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk) {
-            const uint32_t o = ((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4;
-            mma_ss(tmem + buf * 128, dx + xs * (SM::kTileBytes >> 4) + o, dy + s * (SM::kTileBytes >> 4) + o, idesc, kk > 0);
+            for (int i = 0; i < kKept; ++i) {
+              if (t >= kept.tiles[i]) continue;
+              const int wg = wg0 + i;
+              if (!mbar_spin(&bar->s_empty[wg], ((phases >> wg) & 1) ^ 1, abort_flag)) { ok = false; break; }
+              phases ^= 1u << wg;
+              tc_fence_after();
+              const uint64_t x = dq + i * (SM::kTileBytes >> 4), y = dk + s * (SM::kTileBytes >> 4);
+#pragma unroll
+              for (int kk = 0; kk < D / 16; ++kk) {
+                const uint32_t o = ((kk >> 2) * kBoxBytes + (kk & 3) * 32) >> 4;
+                mma_ss(tmem + wg * 128, (kSum ? y : x) + o, (kSum ? x : y) + o, idesc, kk > 0);
+              }
+              tc_commit(&bar->s_full[wg]);
+            }
+            tc_commit(&bar->k_empty[s]);
           }
-          tc_commit(&bar->s_full[buf]);
-          tc_commit(&bar->y_empty[s]);
+          tc_commit(&bar->q_empty);
         }
-        if (!ok) break;
-        tc_commit(&bar->x_empty[xs]);
-        ++x_cnt;
       }
     }
     __syncwarp();
+  } else if (warp == kAddWarp) {
+    // =========================================================================== second pass: the sums of a tile's blocks onto the keys' weights
+    uint32_t rounds = 0;
+    while (kSum && ok && walk.next(p, w)) {
+      int first;
+      const int fresh = w.length - cache_new(c, w.b, first);
+      for (int i0 = 0; ok && i0 < max(w.blocks, 1); i0 += kKept) {
+        const Kept kept(p, w, i0);
+        const int hi = kept.n > 0 ? p.blocks[kept.q + kept.n - 1].last : -1;
+        for (int k = w.k0; k < w.k1; k += kept.wide, ++rounds) {
+          const int buf = rounds % kSumBufs;
+          if (!mbar_wait_warp(&bar->sum_full[buf], (rounds / kSumBufs) & 1, abort_flag)) { ok = false; break; }
+          const float* sums = reinterpret_cast<const float*>(smem + SM::kSumOff) + buf * (kKept * 128);
+          for (int x = 0; x < kept.wide && k + x < w.k1; ++x) {
+            float four[4] = {};
+            for (int i = 0; i < kept.width; ++i) {
+              const float4 y = reinterpret_cast<const float4*>(sums + (x * kept.width + i) * 128)[lane];
+              four[0] += y.x; four[1] += y.y; four[2] += y.z; four[3] += y.w;
+            }
+            add_weights(a, p.codes, w.b, w.g, tile_of(w, k + x) * kTileN + 4 * lane, w.length, i0 == 0 ? fresh : w.length, hi, four);
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bar->sum_empty[buf]);
+        }
+      }
+    }
   } else {
     // =========================================================================== soft-max
-    const int wg = warp >> 2, r = (warp & 3) * 32 + lane;       // row of the kept operand == TMEM lane
-    const uint32_t s_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+    const int wg = warp >> 2, r = (warp & 3) * 32 + lane;       // row of the A operand == TMEM lane
+    const uint32_t s_addr = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + wg * 128;
     float* stage = reinterpret_cast<float*>(smem + SM::kStageOff + warp * 1024);
     const int* stage_pos = reinterpret_cast<const int*>(stage + 128);
-    float* sums = reinterpret_cast<float*>(smem + SM::kSumOff);
     const float2 scale = make_float2(a.scale_log2, a.scale_log2);
-    uint32_t cnt = 0, pieces = 0;
-    while (walk.next(p, w)) {
-      const int pos = kSum ? w.x * kTileN + r : p.row_pos[w.x * kTileM + r];
-      float m = -INFINITY, l = 0.f;
-      for (int i = 0; i < w.n; ++i, ++cnt) {
-        if ((cnt & 1) != wg) continue;
-        const uint32_t buf = cnt % kScoreBufs;
-        bool partial;                        // some pair of the tile is not seen
-        if (kSum) {
-          const int q = w.y0 + i;
-          partial = w.x * kTileN + kTileN - 1 > p.blocks[q].first_pos;
+    uint32_t s_cnt = 0, rounds = 0;
+    while (ok && walk.next(p, w)) {
+      for (int i0 = 0; ok && i0 < max(w.blocks, kSum ? 1 : 0); i0 += kKept) {
+        const Kept kept(p, w, i0);
+        const int i = wg % kept.width, slot = wg / kept.width, q = kept.q + i;
+        const bool mine = i < kept.n;
+        int seen = 0, row_pos = -1, first_pos = 0;
+#pragma unroll
+        for (int x = 0; x < kKept; ++x) seen = x == i ? kept.tiles[x] : seen;
+        if (mine && !kSum) row_pos = p.row_pos[q * kTileM + r];
+        if (mine && kSum) {
+          first_pos = p.blocks[q].first_pos;
           __syncwarp();
           reinterpret_cast<float4*>(stage)[lane] = reinterpret_cast<const float4*>(p.minus_lse + ((int64_t)w.g * p.most_blocks + q) * kTileM)[lane];
-          if (partial) reinterpret_cast<int4*>(stage + 128)[lane] = reinterpret_cast<const int4*>(p.row_pos + q * kTileM)[lane];
+          reinterpret_cast<int4*>(stage + 128)[lane] = reinterpret_cast<const int4*>(p.row_pos + q * kTileM)[lane];
           __syncwarp();
-        } else {
-          partial = __any_sync(0xffffffffu, (w.y0 + i) * kTileN + kTileN - 1 > pos);
         }
-        if (!mbar_wait_warp(&bar->s_full[buf], (cnt / kScoreBufs) & 1, abort_flag)) { ok = false; break; }
-        tc_fence_after();
-        uint32_t v[4][32];
+        float m = -INFINITY, l = 0.f;
+        for (int k = w.k0; k < w.k1; k += kept.wide) {
+          const int t = k + slot < w.k1 ? tile_of(w, k + slot) : 0x7fffffff;
+          if (kSum) l = 0.f;
+          if (t < seen) {
+            const int pos = kSum ? t * kTileN + r : row_pos;
+            // some pair of the tile is not seen
+            const bool partial = kSum ? t * kTileN + kTileN - 1 > first_pos : __any_sync(0xffffffffu, t * kTileN + kTileN - 1 > pos);
+            if (!mbar_wait_warp(&bar->s_full[wg], s_cnt & 1, abort_flag)) { ok = false; break; }
+            ++s_cnt;
+            tc_fence_after();
+            // 32 columns are computed with while the next ones come
+            uint32_t v[2][32];
+            tmem_ld32(s_addr, v[0]);
+            float2 sum[2] = {};
 #pragma unroll
-        for (int q = 0; q < 4; ++q) tmem_ld32(s_addr + buf * 128 + q * 32, v[q]);
-        tmem_ld_wait();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&bar->s_empty[buf]);
-        float2 sum[2] = {};
-        if (kSum) {
-          const uint32_t at = smem_u32(stage);
+            for (int col = 0; col < 4; ++col) {
+              uint32_t (&x)[32] = v[col & 1];
+              tmem_ld_wait();
+              if (col < 3) {
+                tmem_ld32(s_addr + (col + 1) * 32, v[(col + 1) & 1]);
+              } else {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bar->s_empty[wg]);
+              }
+              if (kSum) {
+                if (partial) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            if (partial) {
+                  for (int e = 0; e < 32; ++e) x[e] = stage_pos[col * 32 + e] >= pos ? x[e] : 0xff800000u;
+                }
+                const uint32_t at = smem_u32(stage) + col * 128;
 #pragma unroll
-              for (int e = 0; e < 32; ++e) v[q][e] = stage_pos[q * 32 + e] >= pos ? v[q][e] : 0xff800000u;
+                for (int e = 0; e < 8; ++e) {
+                  const float4 z = lds128(at + e * 16);
+                  const float2 y0 = __ffma2_rn(make_float2(__uint_as_float(x[4 * e]), __uint_as_float(x[4 * e + 1])), scale, make_float2(z.x, z.y));
+                  const float2 y1 = __ffma2_rn(make_float2(__uint_as_float(x[4 * e + 2]), __uint_as_float(x[4 * e + 3])), scale, make_float2(z.z, z.w));
+                  sum[0] = __fadd2_rn(sum[0], make_float2(fast_exp2(y0.x), fast_exp2(y0.y)));
+                  sum[1] = __fadd2_rn(sum[1], e % 2 ? exp2_fma2(y1) : make_float2(fast_exp2(y1.x), fast_exp2(y1.y)));
+                }
+              } else {
+                if (partial) {
+                  const uint32_t visible = bit_range(0, pos + 1 - t * kTileN - col * 32);
+#pragma unroll
+                  for (int e = 0; e < 32; ++e) x[e] = (visible >> e) & 1u ? x[e] : 0xff800000u;
+                }
+                float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                  mx[0] = fmax3(mx[0], __uint_as_float(x[e]), __uint_as_float(x[e + 1]));
+                  mx[1] = fmax3(mx[1], __uint_as_float(x[e + 2]), __uint_as_float(x[e + 3]));
+                }
+                const float m_new = fmaxf(m, fmaxf(mx[0], mx[1]) * a.scale_log2);
+                const float neg = m_new == -INFINITY ? 0.f : -m_new;
+                sum[0] = sum[1] = make_float2(0.f, 0.f);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                  const float2 y = __ffma2_rn(make_float2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), scale, make_float2(neg, neg));
+                  sum[e & 1] = __fadd2_rn(sum[e & 1], e % 4 == 3 ? exp2_fma2(y) : make_float2(fast_exp2(y.x), fast_exp2(y.y)));
+                }
+                l = l * fast_exp2(m + neg) + ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
+                m = m_new;
+              }
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float4 z = lds128(at + (q * 8 + e) * 16);
-              const float2 y0 = __ffma2_rn(make_float2(__uint_as_float(v[q][4 * e]), __uint_as_float(v[q][4 * e + 1])), scale, make_float2(z.x, z.y));
-              const float2 y1 = __ffma2_rn(make_float2(__uint_as_float(v[q][4 * e + 2]), __uint_as_float(v[q][4 * e + 3])), scale, make_float2(z.z, z.w));
-              sum[0] = __fadd2_rn(sum[0], make_float2(fast_exp2(y0.x), fast_exp2(y0.y)));
-              sum[1] = __fadd2_rn(sum[1], e % 2 ? exp2_fma2(y1) : make_float2(fast_exp2(y1.x), fast_exp2(y1.y)));
-            }
+            if (kSum) l = (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
           }
-          l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-        } else {
-          if (partial) {
-            const int k0 = (w.y0 + i) * kTileN;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const uint32_t visible = bit_range(0, pos + 1 - k0 - q * 32);
-#pragma unroll
-              for (int e = 0; e < 32; ++e) v[q][e] = (visible >> e) & 1u ? v[q][e] : 0xff800000u;
-            }
+          if (kSum) {
+            const int buf = rounds % kSumBufs;
+            if (!mbar_wait_warp(&bar->sum_empty[buf], ((rounds / kSumBufs) & 1) ^ 1, abort_flag)) { ok = false; break; }
+            ++rounds;
+            reinterpret_cast<float*>(smem + SM::kSumOff)[(buf * kKept + wg) * 128 + r] = l;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bar->sum_full[buf]);
           }
-          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) mx[q] = fmax3(mx[q], __uint_as_float(v[q][e]), __uint_as_float(v[q][e + 1]));
-          }
-          const float m_new = fmaxf(m, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2);
-          const float neg = m_new == -INFINITY ? 0.f : -m_new;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[q][2 * e]), __uint_as_float(v[q][2 * e + 1])), scale, make_float2(neg, neg));
-              sum[e & 1] = __fadd2_rn(sum[e & 1], e % 4 == 3 ? exp2_fma2(y) : make_float2(fast_exp2(y.x), fast_exp2(y.y)));
-            }
-          }
-          l = l * fast_exp2(m + neg) + ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
-          m = m_new;
         }
-      }
-      if (!kSum) {
-        if (!ok) break;
-        p.part[((int64_t)w.slot * 2 + wg) * kTileM + r] = make_float2(m, l);
-        continue;
-      }
-      // ---- both warpgroups' sums, four keys a thread.  (All warps leave together where a wait ran out.)
-      float* mine = sums + (pieces & 1) * 256;
-      ++pieces;
-      mine[wg * 128 + r] = l;
-      if (!named_barrier_all(1, kSumWarps * 32, ok)) break;
-      if (warp == 0) {
-        const float4 x = reinterpret_cast<const float4*>(mine)[lane], y = reinterpret_cast<const float4*>(mine + 128)[lane];
-        const float four[4] = {x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w};
-        int first;
-        const int n = cache_new(c, w.b, first), hi = w.n > 0 ? p.blocks[p.block_start[w.b + 1] - 1].last : -1;
-        add_weights(a, p.codes, w.b, w.g, w.x * kTileN + 4 * lane, w.length, w.length - n, hi, four);
+        if (!kSum) {
+          // ---- the warpgroups that had the same rows, in one part.  (All warps leave together where a wait ran out.)
+          float2* sums = reinterpret_cast<float2*>(smem + SM::kSumOff);
+          sums[wg * 128 + r] = make_float2(m, l);
+          ok = named_barrier_all(1, kSumWarps * 32, ok);
+          if (ok && slot == 0 && mine) {
+            for (int x = 1; x < kept.wide; ++x) {
+              const float2 y = sums[(x * kept.width + i) * 128 + r];
+              const float M = fmaxf(m, y.x), base = M == -INFINITY ? 0.f : M;
+              l = l * fast_exp2(m - base) + y.y * fast_exp2(y.x - base);
+              m = M;
+            }
+            // (a range that begins inside the sequence's head is its CTA's first)
+            const int64_t at = w.k0 == 0 ? (int64_t)w.g * p.plan->n_blocks + q : (int64_t)c.Hkv * p.plan->n_blocks + (int64_t)blockIdx.x * p.plan->most + q - w.q0;
+            p.part[at * kTileM + r] = make_float2(m, l);
+          }
+          ok = named_barrier_all(1, kSumWarps * 32, ok);
+        }
       }
     }
   }
@@ -605,18 +627,25 @@ __global__ void __launch_bounds__(kTileM) weigh_join_kernel(const WeighArgs p) {
   dependents_release();
   const WeighPlan plan = *p.plan;
   if (q >= plan.n_blocks) return;
-  const int64_t total = plan.units * p.f.c.Hkv, share = (total + kCtas - 1) / kCtas;
-  const int64_t at = g * plan.units + p.blocks[q].units, c0 = at / share, c1 = (at + p.blocks[q].tiles - 1) / share;
-  float m = -INFINITY, l = 0.f;
-  for (int64_t cta = c0; cta <= c1; ++cta) {
-    const int64_t slot = (int64_t)g * plan.n_blocks + q + cta;
+  const int b = p.blocks[q].b, q0 = p.block_start[b];
+  const int64_t first = g * plan.units + p.unit_start[b], units = p.unit_start[b + 1] - p.unit_start[b], of_tile = p.block_start[b + 1] - q0;
+  const int64_t c0 = first / plan.share, c1 = (first + units - of_tile) / plan.share;
+  float2 x = p.part[((int64_t)g * plan.n_blocks + q) * kTileM + r];
+  float m = x.x, l = x.y;
+  const float2* rest = p.part + ((int64_t)p.f.c.Hkv * plan.n_blocks + q - q0) * kTileM + r;
+  constexpr int kAhead = 8;                // parts under way together
+  for (int64_t cta = c0 + 1; cta <= c1; cta += kAhead) {
+    float2 y[kAhead];
+    float M = m;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float2 x = p.part[(slot * 2 + i) * kTileM + r];
-      const float M = fmaxf(m, x.x), base = M == -INFINITY ? 0.f : M;
-      l = l * fast_exp2(m - base) + x.y * fast_exp2(x.x - base);
-      m = M;
-    }
+    for (int i = 0; i < kAhead; ++i) y[i] = cta + i <= c1 ? rest[(cta + i) * plan.most * kTileM] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) M = fmaxf(M, y[i].x);
+    const float base = M == -INFINITY ? 0.f : M;
+    l *= fast_exp2(m - base);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) l += y[i].y * fast_exp2(y[i].x - base);
+    m = M;
   }
   const bool row = r < p.blocks[q].n_rows;
   p.minus_lse[((int64_t)g * p.most_blocks + q) * kTileM + r] = row && l != 0.f ? -(m + log2f(l)) : -INFINITY;
@@ -624,6 +653,7 @@ __global__ void __launch_bounds__(kTileM) weigh_join_kernel(const WeighArgs p) {
 
 // ------------------------------------------------------------------------------------------------------------- host
 int64_t most_blocks(const l2a_params* p, int n_tokens) { return ((int64_t)n_tokens * (p->Hq / p->Hkv) + kTileM - 1) / kTileM + p->B; }
+int64_t most_of_one(const l2a_params* p) { return ((int64_t)p->Lq * (p->Hq / p->Hkv) + kTileM - 1) / kTileM; }
 int64_t key_tiles(int Lk) { return ((int64_t)Lk + kTileN - 1) / kTileN; }
 size_t layout(const l2a_params* p, int kind, int n_tokens, uint8_t* base, WeighArgs* w, uint8_t** copy) {
   size_t at = 0;
@@ -640,10 +670,10 @@ size_t layout(const l2a_params* p, int kind, int n_tokens, uint8_t* base, WeighA
   x.list_start = reinterpret_cast<int*>(take(B * 4));
   x.list_end = reinterpret_cast<int*>(take(B * 4));
   x.block_start = reinterpret_cast<int*>(take((B + 1) * 4));
-  x.tile_start = reinterpret_cast<int64_t*>(take((B + 1) * 8));
+  x.unit_start = reinterpret_cast<int64_t*>(take((B + 1) * 8));
   x.row_pos = reinterpret_cast<int*>(take(blocks * kTileM * 4));
   x.minus_lse = reinterpret_cast<float*>(take(Hkv * blocks * kTileM * 4));
-  x.part = reinterpret_cast<float2*>(take((Hkv * blocks + kCtas) * 2 * kTileM * 8));
+  x.part = reinterpret_cast<float2*>(take((Hkv * blocks + kCtas * (size_t)most_of_one(p)) * kTileM * 8));
   x.rows = reinterpret_cast<bf16*>(take(Hkv * blocks * kTileM * p->D * 2));
   x.most_blocks = (int)blocks;
   uint8_t* decoded = take(kind == L2A_CACHE_BF16 ? 0 : B * Hkv * (size_t)key_tiles(p->Lk) * kTileN * p->D * 2);
@@ -711,7 +741,7 @@ l2a_status check_weigh(const l2a_params* p, const l2a_cache* c, int n_tokens, Ca
   if ((int64_t)n_tokens * p->Hq >= (1ll << 31) - 32 || p->B > 65535 || p->Hkv > 65535) return L2A_ERR_UNSUPPORTED;
   if (most_kept(p) > 0 && !cache_few_counts(p)) return L2A_ERR_UNSUPPORTED;
   // (slots and rows of the blocks are counted in 32 bits, as are the CTAs that decode)
-  if (has_blocks(p) && ((most_blocks(p, n_tokens) * p->Hkv + kCtas) >= (1ll << 31) || most_blocks(p, n_tokens) >= (1ll << 31) / kTileM ||
+  if (has_blocks(p) && ((most_blocks(p, n_tokens) * p->Hkv) >= (1ll << 31) || most_blocks(p, n_tokens) >= (1ll << 31) / kTileM ||
                         key_tiles(p->Lk) * p->Hkv >= (1ll << 31)))
     return L2A_ERR_UNSUPPORTED;
   return L2A_OK;

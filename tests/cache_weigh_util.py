@@ -5,7 +5,8 @@ log2(e) and the subtraction by a rounding each, 2^-23 of the largest |s| togethe
 off by 2^-22 each, sums of n positive terms by n 2^-24 at most.  Sums are made of partial sums (64 terms of a tile and lane, then the tiles), so
 n is keys / 64 + 300 and rows / 64 + 300.  So each row's weights are off by at most
   2 (D 2^-24 A + 2^-22 A) + 2^-20 + (keys / 64 + rows / 64 + 600) 2^-24  of themselves,  A = max over keys of sum |q_i k_i| scale,
-and the sum with the old weight by one rounding, 2^-24 of it."""
+The old weight is added to for every 512 rows of a KV head (four blocks of 128 whose sums are made apart), with a rounding each time: at most
+ceil(rows / 512) 2^-24 of the new weight, since all summands are positive."""
 import math
 
 import numpy as np
@@ -85,7 +86,8 @@ def weigh(cache, Hq, new, d, Q=None, seed=0, Lk=None, Lq=None, uniform=False, sc
         times = torch.full((len(old), 1), float(calls), device="cuda", dtype=torch.float64)
         times[len(old) - n:] = 1
         want, got = old + times * inc, pool[at, :, slot].double()
-        bound = times * off + times * 2.0 ** -24 * want + 1e-36
+        groups = max(1, math.ceil(int(count[sum(new[:b]):sum(new[:b + 1])].sum()) * (Hq // cache.Hkv) / 512))
+        bound = times * off + times * groups * 2.0 ** -24 * want + 1e-36
         err = (got - want).abs()
         assert torch.isfinite(got).all(), f"sequence {b}: not finite"
         assert bool((err <= bound).all()), f"sequence {b}: {float((err / bound).max()):.3f} times the bound"
