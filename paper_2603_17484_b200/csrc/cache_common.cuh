@@ -152,12 +152,13 @@ __device__ __forceinline__ uint32_t pack_e2m1(const float2 (&x)[4]) {
       : "=r"(r) : "f"(x[0].x), "f"(x[0].y), "f"(x[1].x), "f"(x[1].y), "f"(x[2].x), "f"(x[2].y), "f"(x[3].x), "f"(x[3].y));
   return r;
 }
-// An e4m3 byte's value
-__device__ __forceinline__ float e4m3_value(uint32_t byte) {
-  uint32_t lo, hi;
-  e4m3x4_to_f16(byte, lo, hi);
-  return f16x2_to_float2(lo).x;
+// The two e4m3 bytes of a half as fp16; an e4m3 byte's value
+__device__ __forceinline__ uint32_t e4m3x2_to_f16(uint32_t bytes) {
+  uint32_t r;
+  asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %1;\n cvt.rn.f16x2.e4m3x2 %0, l;\n}" : "=r"(r) : "r"(bytes));
+  return r;
 }
+__device__ __forceinline__ float e4m3_value(uint32_t byte) { return f16x2_to_float2(e4m3x2_to_f16(byte)).x; }
 // Copies from one page: K or V rows of a head; untiled for their exponents (16 bytes or a multiple, 16-byte aligned)
 __device__ __forceinline__ void tma_load_page(void* dst, const CUtensorMap* map, uint64_t* bar, bool codes, int piece, int row,
                                               int head, int page) {

@@ -327,15 +327,15 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           const int row = i16 * 16 + k * 8;
-          uint32_t both, none;
+          uint32_t both;
           if (D == 128) {
             const float4 y = lds128(k_at + tile + row * kRowBytes);
             w[k][0] = __float_as_uint(y.x); w[k][1] = __float_as_uint(y.y);
             w[k][kKWords - 2] = __float_as_uint(y.z); w[k][kKWords - 1] = __float_as_uint(y.w);
-            e4m3x4_to_f16(lds16(k_scale_at + scale + row * kBlockBytes), both, none);
+            both = e4m3x2_to_f16(lds16(k_scale_at + scale + row * kBlockBytes));
           } else {
             lds64(k_at + tile + row * kRowBytes, w[k][0], w[k][1]);
-            e4m3x4_to_f16(lds8(k_scale_at + scale + row * kBlockBytes), both, none);
+            both = e4m3x2_to_f16(lds8(k_scale_at + scale + row * kBlockBytes));
           }
           f[k] = *reinterpret_cast<const __half2*>(&both);
         }
