@@ -1282,11 +1282,13 @@ __global__ void __launch_bounds__(256) cache_join_kernel(const ChunkArgs p) {
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
-// An 8-bit cache is decoded once where a sequence can have kDecodeRows rows of a KV head or more: each 256 of them would decode its keys
-// again.  us decoded in the products' kernel / once (window 4096, a fifth routed): 560 rows of each of eight sequences of 32K (28/4 heads) 246 /
+// A cache of codes is decoded once where a sequence can have kDecodeRows rows of a KV head or more: each 256 of them would decode its keys
+// again.  us decoded in the products' kernel / once (window 4096, a fifth routed), 8 bits: 560 rows of each of eight sequences of 32K (28/4 heads) 246 /
 // 283, 800 of one (32/8) 94 / 97, 1050 of one (28/4) 65 / 67, of four of 16K 120 / 123, of one of 6000 42 / 39, 1200 of four of 4000 (32/8)
 // 127 / 114, 1470 of one of 64K (28/4) 134 / 116, 1532 of four of 16K (32/8) 366 / 269.  Not for copies beyond kMostDecoded bytes.
-constexpr int64_t kDecodeRows = 1024, kMostDecoded = 4ll << 30;
+// 4 bits take longer to decode there, so that the copy is worth it sooner: 280 rows of one of 32K (28/4) 64 / 70, 560 of each of eight 339 / 303, 800 of
+// one (32/8) 123 / 106, 1050 of one of 6000 (28/4) 52 / 45, of four of 16K 182 / 131, 1532 of four (32/8) 472 / 284.
+constexpr int64_t kDecodeRows = 1024, kDecodeRows4 = 512, kMostDecoded = 4ll << 30;
 int decoded_pages(int Lk) { return (Lk + kTileN - 1) / kTileN; }
 int64_t decoded_bytes(int B, int Lk, int Hkv, int D) { return 2ll * B * decoded_pages(Lk) * Hkv * kTileN * D * 2; }
 size_t layout(int B, int n_tokens, int G, int Hkv, int D, uint8_t* base, ChunkWs* w) {
@@ -1354,7 +1356,8 @@ size_t cache_chunk_ws_bytes(const l2a_params* p, int n_tokens) {
 }
 
 size_t cache_copy_bytes(const l2a_params* p, int kind) {
-  if (kind == L2A_CACHE_BF16 || (int64_t)p->Lq * (p->Hq / p->Hkv) < kDecodeRows || p->B > 65535) return 0;
+  const int64_t rows = (int64_t)p->Lq * (p->Hq / p->Hkv), least = kind == L2A_CACHE_E2M1 ? kDecodeRows4 : kDecodeRows;
+  if (kind == L2A_CACHE_BF16 || rows < least || p->B > 65535) return 0;
   const int64_t bytes = decoded_bytes(p->B, p->Lk, p->Hkv, p->D);
   return bytes <= kMostDecoded ? (size_t)bytes : 0;
 }

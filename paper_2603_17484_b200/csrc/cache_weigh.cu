@@ -684,18 +684,24 @@ size_t layout(const l2a_params* p, int kind, int n_tokens, uint8_t* base, WeighA
   return at;
 }
 
-// Rows of a sequence up to which its scores are kept: as many as the kernel of the few rows takes, less where the workspace for the scores of all
-// sequences would pass kMostScores.
+// Rows of a sequence up to which its scores are kept: as many as the kernel of the few rows takes, for bf16, where the blocks need no decoded copy,
+// three quarters; less where the workspace for the scores of all sequences would pass kMostScores.  us scores kept / blocks: 64 rows of each of eight
+// sequences of 32K (32/8 heads, half counted) bf16 448 / 248, e2m1 378 / 406, of one e2m1 99 / 78; 49 rows of four of 16K (28/4) e4m3 63 / 78; 35 of
+// two of 100K e2m1 128 / 188; 28 of eight of 32K bf16 107 / 144.
 constexpr int64_t kMostScores = 4ll << 30;
-int kept_rows(const l2a_params* p) {
+int kept_rows(const l2a_params* p, int kind) {
   const int64_t G = p->Hq / p->Hkv, all = (int64_t)p->Lq * G;
-  for (int rows = kRowBlocks * kBlockRows; rows >= kBlockRows; rows -= kBlockRows)
+  for (int rows = (kind == L2A_CACHE_BF16 ? 3 : kRowBlocks) * kBlockRows; rows >= kBlockRows; rows -= kBlockRows)
     if (rows >= G && (double)p->B * p->Hkv * (double)std::min<int64_t>(rows, all) * (p->Lk + 64.0) * 4 <= (double)kMostScores) return rows;
   return 0;
 }
-int most_kept(const l2a_params* p) { return (int)std::min<int64_t>(kept_rows(p), (int64_t)p->Lq * (p->Hq / p->Hkv)); }
-size_t few_bytes(const l2a_params* p) { return most_kept(p) > 0 ? align_up(cache_few_weigh_ws_bytes(p, most_kept(p)), 256) : 0; }
-bool has_blocks(const l2a_params* p) { return (int64_t)p->Lq * (p->Hq / p->Hkv) > kept_rows(p); }
+static_assert(kRowBlocks == 4, "three quarters");
+int most_kept(const l2a_params* p, int kind) { return (int)std::min<int64_t>(kept_rows(p, kind), (int64_t)p->Lq * (p->Hq / p->Hkv)); }
+size_t few_bytes(const l2a_params* p, int kind) {
+  const int rows = most_kept(p, kind);
+  return rows > 0 ? align_up(cache_few_weigh_ws_bytes(p, rows), 256) : 0;
+}
+bool has_blocks(const l2a_params* p, int kind) { return (int64_t)p->Lq * (p->Hq / p->Hkv) > kept_rows(p, kind); }
 
 template <int D, bool kSum>
 cudaError_t launch_pass(const CUtensorMap& mapQ, const CUtensorMap& mapK, const WeighArgs& p, cudaStream_t s) {
@@ -739,15 +745,15 @@ l2a_status check_weigh(const l2a_params* p, const l2a_cache* c, int n_tokens, Ca
   if (st != L2A_OK) return st;
   if (p->flags & ~L2A_FLAG_SHARED_WINDOW) return L2A_ERR_INVALID_ARG;
   if ((int64_t)n_tokens * p->Hq >= (1ll << 31) - 32 || p->B > 65535 || p->Hkv > 65535) return L2A_ERR_UNSUPPORTED;
-  if (most_kept(p) > 0 && !cache_few_counts(p)) return L2A_ERR_UNSUPPORTED;
+  if (most_kept(p, c->kind) > 0 && !cache_few_counts(p)) return L2A_ERR_UNSUPPORTED;
   // (slots and rows of the blocks are counted in 32 bits, as are the CTAs that decode)
-  if (has_blocks(p) && ((most_blocks(p, n_tokens) * p->Hkv) >= (1ll << 31) || most_blocks(p, n_tokens) >= (1ll << 31) / kTileM ||
+  if (has_blocks(p, c->kind) && ((most_blocks(p, n_tokens) * p->Hkv) >= (1ll << 31) || most_blocks(p, n_tokens) >= (1ll << 31) / kTileM ||
                         key_tiles(p->Lk) * p->Hkv >= (1ll << 31)))
     return L2A_ERR_UNSUPPORTED;
   return L2A_OK;
 }
 size_t weigh_ws_bytes(const l2a_params* p, int kind, int n_tokens) {
-  return kWsHeaderBytes + few_bytes(p) + (has_blocks(p) ? layout(p, kind, n_tokens, nullptr, nullptr, nullptr) : 0);
+  return kWsHeaderBytes + few_bytes(p, kind) + (has_blocks(p, kind) ? layout(p, kind, n_tokens, nullptr, nullptr, nullptr) : 0);
 }
 
 }  // namespace
@@ -789,8 +795,8 @@ extern "C" l2a_status l2a_cache_weigh(const l2a_params* p, const l2a_cache* c, c
   a.status = static_cast<int*>(ws);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   uint8_t* at = static_cast<uint8_t*>(ws) + kWsHeaderBytes;
-  a.few_rows = kept_rows(p);
-  const bool blocks = has_blocks(p);
+  a.few_rows = kept_rows(p, c->kind);
+  const bool blocks = has_blocks(p, c->kind);
   // With as many tokens as there can be no sequence is expected to have few rows (as in l2a_cache_forward)
   const bool few = a.few_rows > 0 && !(blocks && (int64_t)p->B * p->Lq == n_tokens);
   if (!few) a.few_rows = 0;
@@ -798,7 +804,7 @@ extern "C" l2a_status l2a_cache_weigh(const l2a_params* p, const l2a_cache* c, c
   if (e == cudaSuccess && blocks) {
     WeighArgs w;
     uint8_t* copy;
-    layout(p, c->kind, n_tokens, at + few_bytes(p), &w, &copy);
+    layout(p, c->kind, n_tokens, at + few_bytes(p, c->kind), &w, &copy);
     w.f = a;
     w.codes = a.c;
     w.clear = !few;
