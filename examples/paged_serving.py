@@ -3,12 +3,18 @@
 The layer has projections, and so a cache, for each of its two modules.  A step of the server takes some new tokens of every
 active sequence on one token axis and runs
 
-  l2a_cache_append   keys and values of the new tokens into the pages of both caches (8 bits or bf16)
+  l2a_cache_append   keys and values of the new tokens into the pages of both caches (bf16, 8 or 4 bits)
   l2a_cache_forward  SKIP_GLOBAL: Local Attention s from the local cache
   l2a_router_logits  z = w . s + bias; a token is routed where z >= 0
   l2a_cache_forward  GLOBAL_PHASE: o = s + d a from the global cache, routed tokens only
 
-and l2a_cache_read takes a finished sequence out of the pool.  Run: python examples/paged_serving.py
+and l2a_cache_read takes a finished sequence out of the pool.  With a bound on the tokens that a sequence keeps, a step also runs
+
+  l2a_cache_weigh    what Global Attention of the routed tokens gives each key of the global cache, added to its weight
+  l2a_cache_evict    a sequence over the bound: its first tokens, the last of a window and more, and those of the highest weights in between move to
+                     other pages, a shorter cache
+
+Run: python examples/paged_serving.py
 """
 from __future__ import annotations
 
@@ -26,17 +32,25 @@ class Pool:
     """Pages of one cache.  Page numbers are shared by all caches of a server, so the server hands them out."""
 
     def __init__(self, n_pages, Hkv, page, D, bits, table, lengths):
-        shape = (n_pages, Hkv, page, D)
-        dtype = torch.float8_e4m3fn if bits == 8 else torch.bfloat16
+        shape = (n_pages, Hkv, page, D if bits > 4 else D // 2)
+        dtype = {16: torch.bfloat16, 8: torch.float8_e4m3fn, 4: torch.uint8}[bits]
         self.K, self.V = (torch.zeros(shape, dtype=dtype, device="cuda") for _ in "KV")
-        ks, vs = ((torch.zeros(shape[:3], dtype=torch.uint8, device="cuda") for _ in "KV") if bits == 8 else (None, None))
-        self.handle = l2a.cache(self.K, self.V, table, lengths, k_scale=ks, v_scale=vs)
+        if bits == 4:
+            self.K, self.V = self.K.view(torch.float4_e2m1fn_x2), self.V.view(torch.float4_e2m1fn_x2)
+        scales = {16: None, 8: shape[:3], 4: (n_pages, Hkv, page * (1 + D // 16))}[bits]
+        self.scales = [torch.zeros(scales, dtype=torch.uint8, device="cuda") if scales else None for _ in "KV"]
+        self.handle = self.view(table, lengths)
+
+    def view(self, table, lengths):
+        """The cache of some sequences: rows of a table, and their lengths."""
+        return l2a.cache(self.K, self.V, table, lengths, *self.scales)
 
 
 class Layer:
     """One layer of the server: two caches, the router's weights, a workspace for the largest step."""
 
-    def __init__(self, slots, longest, most_new, step_tokens, heads, window, page=64, bits=8, n_pages=None):
+    def __init__(self, slots, longest, most_new, step_tokens, heads, window, page=64, bits=8, n_pages=None, bound=None):
+        """bound: tokens that a sequence keeps; None: all."""
         self.Hq, self.Hkv, self.D = heads
         self.window, self.page, self.slots, self.longest = window, page, slots, longest
         per = -(-longest // page)
@@ -52,6 +66,11 @@ class Layer:
         self.ws = torch.empty(ws, dtype=torch.uint8, device="cuda")
         self.w = torch.zeros(self.Hq * self.D, device="cuda")
         self.bias = 0.0
+        self.bound, self.first = bound, 4
+        if bound is not None:
+            self.weights = torch.zeros((n_pages, self.Hkv, page), device="cuda")
+            self.weigh_ws = torch.empty(l2a.l2a_cache_weigh_workspace_bytes(self._params(most_new), self.glob.handle, step_tokens),
+                                        dtype=torch.uint8, device="cuda")
 
     def _params(self, most_new, flags=0):
         return l2a.params(self.slots, most_new, self.longest, self.Hq, self.Hkv, self.D, self.window, flags=flags)
@@ -77,7 +96,30 @@ class Layer:
         l2a.l2a_router_logits(l2a.params(1, N, N, self.Hq, self.Hkv, self.D, self.window), O, self.w, self.bias, z)
         d = (z[0] >= 0).to(torch.uint8)
         l2a.l2a_cache_forward(self._params(most, l2a.FLAG_GLOBAL_PHASE), self.glob.handle, glob[0], cu, N, d, O, self.ws)
+        if self.bound is not None:
+            l2a.l2a_cache_weigh(p, self.glob.handle, glob[0], cu, N, d, self.weights, self.weigh_ws)
+            for slot, n in enumerate(self.held):
+                if n > self.bound:
+                    self.shrink(slot)
         return O, d
+
+    def shrink(self, slot):
+        """Evicts from both caches of a slot down to three quarters of the bound (at least what Local Attention needs)."""
+        n, room = self.held[slot], max(3 * self.bound // 4, self.window + self.first)
+        keep = min(n, room)
+        pages = [self.free.pop() for _ in range(-(-keep // self.page))]
+        table = torch.tensor([pages], dtype=torch.int32, device="cuda")
+        p = l2a.params(1, keep, n, self.Hq, self.Hkv, self.D, self.window)
+        kept = torch.tensor([keep], dtype=torch.int32, device="cuda")
+        length = torch.empty(1, dtype=torch.int32, device="cuda")
+        for cache in (self.local, self.glob):                    # (the local cache goes by the same weights: only its last tokens matter)
+            old = cache.view(self.table[slot:slot + 1], self.lengths[slot:slot + 1])
+            ws = torch.empty(l2a.l2a_cache_evict_workspace_bytes(p, old), dtype=torch.uint8, device="cuda")
+            l2a.l2a_cache_evict(p, old, self.weights, kept, self.first, self.window, cache.view(table, length), self.weights, length, None, ws)
+        self.free += self.table[slot, :-(-n // self.page)].tolist()
+        self.table[slot, :len(pages)] = table[0]
+        self.held[slot] = keep
+        self.lengths[slot] = keep
 
     def take_out(self, slot):
         """Dense keys and values of both caches of a slot, [tokens, Hkv, D]; its pages go back to the pool."""
@@ -85,9 +127,7 @@ class Layer:
         p = l2a.params(1, 1, max(n, 1), self.Hq, self.Hkv, self.D, self.window)
         got = []
         for cache in (self.local, self.glob):
-            h = cache.handle
-            one = l2a.cache(cache.K, cache.V, self.table[slot:slot + 1], self.lengths[slot:slot + 1],
-                            k_scale=h.tensors[2], v_scale=h.tensors[3])
+            one = cache.view(self.table[slot:slot + 1], self.lengths[slot:slot + 1])
             K, V = (torch.empty((1, max(n, 1), self.Hkv, self.D), dtype=torch.bfloat16, device="cuda") for _ in "KV")
             l2a.l2a_cache_read(p, one, None, K, V)
             got.append((K[0, :n], V[0, :n]))
@@ -98,13 +138,16 @@ class Layer:
         return got
 
 
-def serve(prompts, answer, heads=(28, 4, 128), window=512, chunk=700, bits=8, seed=0):
+def serve(prompts, answer, heads=(28, 4, 128), window=512, chunk=700, bits=8, seed=0, bound=None):
     """Prompts (their lengths) start one step after the other and are taken in chunks, then `answer` single tokens each.  Returns
     the layer's outputs of every sequence, its decisions, and (Q, K, V) of both modules, all [tokens, heads, D]."""
     g = torch.Generator(device="cuda").manual_seed(seed)
     Hq, Hkv, D = heads
     total = [n + answer for n in prompts]
-    layer = Layer(len(prompts), max(total), chunk, chunk * len(prompts), heads, window, bits=bits)
+    page = 64
+    spare = 0 if bound is None else -(-max(total) // page)       # an eviction writes a sequence's next pages before the others are free
+    layer = Layer(len(prompts), max(total), chunk, chunk * len(prompts), heads, window, page=page, bits=bits, bound=bound,
+                  n_pages=len(prompts) * -(-max(total) // page) + spare)
     layer.w.normal_(generator=g)
     layer.bias = -0.8 * float(layer.w.norm()) * 0.06             # about a fifth of the tokens of random inputs
     data = [[[torch.randn((n, h, D), generator=g, device="cuda").bfloat16() for h in (Hq, Hkv, Hkv)] for _ in range(2)] for n in total]
@@ -130,14 +173,14 @@ def serve(prompts, answer, heads=(28, 4, 128), window=512, chunk=700, bits=8, se
 
 def main():
     prompts, answer = [3000, 517, 1800, 64], 20
-    for bits in (16, 8):
+    for bits, bound in ((16, None), (8, None), (4, None), (4, 1500)):
         start, end = (torch.cuda.Event(enable_timing=True) for _ in "ab")
         start.record()
-        layer, out, dec, _ = serve(prompts, answer, bits=bits)
+        layer, out, dec, _ = serve(prompts, answer, bits=bits, bound=bound)
         end.record()
         torch.cuda.synchronize()
         routed = sum(int(d.sum()) for d in dec) / sum(len(d) for d in dec)
-        print(f"{bits}-bit cache: {sum(len(o) for o in out)} tokens of {len(prompts)} sequences, {100 * routed:.0f} % routed, "
+        print(f"{bits}-bit cache{f' of at most {bound} tokens a sequence' if bound else ''}: {sum(len(o) for o in out)} tokens of {len(prompts)} sequences, {100 * routed:.0f} % routed, "
               f"{start.elapsed_time(end):.1f} ms")
         K, V = layer.take_out(0)[0]
         print(f"  sequence 0 taken out: keys {tuple(K.shape)}, {len(layer.free)} pages free")

@@ -473,8 +473,8 @@ l2a_status l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t
  *                    (l2a_workspace_status; after a time-out the rows that need a combination are not stored).  The size follows
  *                    from p, the cache's kind and n_tokens; it is enough for every smaller n_tokens, Lq and Lk (other fields alike).
  *                    It holds partial results; where a sequence can have more than 16 rows (Lq * Hq / Hkv) those of the groups of 256
- *                    rows too, and from 1024 rows on a decoded copy of an 8-bit cache (4 * B * Lk * Hkv * D bytes with Lk rounded up to
- *                    128) where that is 4 GB at most.  The size less the copy (that of a bf16 cache) is taken too: the 8-bit keys are then
+ *                    rows too, and from 1024 rows on a decoded copy of an 8-bit cache, from 512 of a 4-bit one (4 * B * Lk * Hkv * D bytes with Lk rounded
+ *                    up to 128) where that is 4 GB at most.  The size less the copy (that of a bf16 cache) is taken too: the keys are then
  *                    decoded as they are used, as they are beyond 4 GB; same bits, longer.  Lk decides, so give it no larger than need be.
  *   p->flags       : L2A_FLAG_SKIP_GLOBAL: s only (as d = NULL).  L2A_FLAG_SKIP_LOCAL: o = d * a.  L2A_FLAG_GLOBAL_PHASE: O holds
  *                    s already (from an L2A_FLAG_SKIP_GLOBAL call on another cache, say), and d * a is added for the routed
@@ -487,10 +487,10 @@ l2a_status l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t
  * A query row with NaN gives NaN.
  * Scores, soft-max statistics and sums are fp32; the decoded keys and values are exact.  The weights enter the second product rounded: as
  * bf16 (8 bits) for sequences of more rows (Lq * Hq / Hkv, see ws), for those of few rows as a pair of bf16 (16 bits) from a bf16 cache, as fp16
- * from an 8-bit one (11 bits down to 2^-24 of the largest weight times 2^e of the values that the row sees, nothing below 2^-35).  Results are
+ * from one of codes (11 bits down to 2^-24 of the largest weight times 2^e of the values that the row sees, nothing below 2^-35).  Results are
  * bit-reproducible; how the keys of a row are divided, and up to 64 rows which of the two ways they take, follows from all the call's
  * lengths and bounds, so that the same sequence in another batch can differ by such roundings.
- * Limits: n_tokens * Hq < 2^31 - 32; Lk * (Hkv + 75) < 2^35; where a sequence can have more than 16 rows
+ * Limits: n_tokens * Hq < 2^31 - 32; Lk * (Hkv + 75) < 2^35 (4 bits: Lk * (Hkv + 112)); where a sequence can have more than 16 rows
  * 2 (n_tokens * Hq / Hkv / 256 + B) * Hkv * (Lk / 128 + 1) < 2^38.  n_tokens = 0 is no work.  Errors: L2A_ERR_INVALID_ARG,
  * L2A_ERR_UNSUPPORTED (D, page_size, kind, the limits), L2A_ERR_WORKSPACE, L2A_ERR_CUDA; a bounded device wait that runs out is
  * reported by the status header, not by the return value.
@@ -520,7 +520,7 @@ l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c, const void
  * Scores, soft-max statistics and sums are fp32, products of bf16 and decoded keys exact.  Bit-reproducible.  Keys that a counted token sees must be finite; a query
  * row with NaN makes the weights of the keys that it sees NaN.
  * Few rows: HBM-bound, keys and weights once.  Many: bound by the exponentials, two for each pair of a row and a key.
- * Limits: n_tokens * Hq < 2^31 - 32; B, Hkv <= 65535; Lk * (Hkv + 75) < 2^35 and Lk * Hkv < 2^38.  Errors: L2A_ERR_INVALID_ARG, L2A_ERR_UNSUPPORTED (D,
+ * Limits: n_tokens * Hq < 2^31 - 32; B, Hkv <= 65535; Lk * (Hkv + 112) < 2^35 and Lk * Hkv < 2^38.  Errors: L2A_ERR_INVALID_ARG, L2A_ERR_UNSUPPORTED (D,
  * page_size, kind, the limits), L2A_ERR_WORKSPACE, L2A_ERR_CUDA; a bounded device wait that runs out is reported by the status header.
  */
 l2a_status l2a_cache_weigh_workspace_bytes(const l2a_params* p, const l2a_cache* c, int n_tokens, size_t* ws_bytes);

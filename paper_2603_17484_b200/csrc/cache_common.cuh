@@ -84,7 +84,7 @@ struct CacheFwdArgs {
 // cache_few.cu
 constexpr int kBlockRows = 16, kRowBlocks = 4;
 size_t cache_few_ws_bytes(const l2a_params* p);     // plan and parts
-bool cache_few_counts(const l2a_params* p);         // whether it can count the tiles of one sequence
+bool cache_few_counts(const l2a_params* p, int kind, bool weigh);         // whether it can count the tiles of one sequence
 cudaError_t launch_cache_few(const CacheFwdArgs& a, void* ws, cudaStream_t s);
 
 // The weights of the keys from those sequences, up to `rows` rows of each

@@ -1367,8 +1367,8 @@ int row_blocks(int64_t rows) { return (int)(std::min<int64_t>(rows, kRowBlocks *
 size_t plan_bytes(int B) { return align_up(((size_t)B + 1) * 8 * sizeof(int), 256); }
 // Sequences of a launch, 0: not even one.  A launch counts its tiles in 32 bits (up to one more for a segment that begins inside a tile, and
 // up to one pair's more a CTA behind the last range), and the combination has a row of its grid for each.
-int batch_of(int Lk, int Hkv, int blocks) {
-  const int64_t pair = ((int64_t)Lk + kTile - 1) / kTile + 1, one = pair * Hkv * blocks, most = (1ll << 31) - 1 - (kMostCtas + 1) * (pair + 1);
+int batch_of(int Lk, int Hkv, int blocks, int ctas) {
+  const int64_t pair = ((int64_t)Lk + kTile - 1) / kTile + 1, one = pair * Hkv * blocks, most = (1ll << 31) - 1 - (ctas + 1) * (pair + 1);
   return (int)std::max<int64_t>(0, std::min<int64_t>(65535, most / one));
 }
 
@@ -1378,7 +1378,11 @@ size_t cache_few_ws_bytes(const l2a_params* p) {
   return plan_bytes(p->B) + align_up((2 * (size_t)p->B * p->Hkv * row_blocks((int64_t)p->Lq * (p->Hq / p->Hkv)) + kMostCtas) * slot_rows(p) * (p->D + 4) * sizeof(float), 256);
 }
 
-bool cache_few_counts(const l2a_params* p) { return batch_of(p->Lk, p->Hkv, row_blocks((int64_t)p->Lq * (p->Hq / p->Hkv))) > 0; }
+int ctas_of(int kind, int64_t rows, bool weigh) { return kSplitSms * ctas_per_sm(kind, rows > 8, weigh); }
+bool cache_few_counts(const l2a_params* p, int kind, bool weigh) {
+  const int64_t rows = (int64_t)p->Lq * (p->Hq / p->Hkv);
+  return batch_of(p->Lk, p->Hkv, row_blocks(rows), ctas_of(kind, rows, weigh)) > 0;
+}
 
 template <bool kWeigh>
 static cudaError_t launch_few(const CacheFwdArgs& args, cudaStream_t s) {
@@ -1388,7 +1392,8 @@ static cudaError_t launch_few(const CacheFwdArgs& args, cudaStream_t s) {
   const int rows = std::min(1 << a.c.page_shift, kTile);
   if (!encode_pool_map(&mapK, a.c, a.c.K, rows, a.c.D / 64) || !encode_pool_map(&mapV, a.c, a.c.V, rows, a.c.D / 64))
     return cudaErrorUnknown;
-  const int B = a.c.B, batch = batch_of(a.c.max_keys, a.c.Hkv, row_blocks(std::min<int64_t>((int64_t)a.c.Lq * a.G, a.few_rows)));
+  const int B = a.c.B, batch = batch_of(a.c.max_keys, a.c.Hkv, row_blocks(std::min<int64_t>((int64_t)a.c.Lq * a.G, a.few_rows)),
+                                              ctas_of(a.c.kind, (int64_t)a.c.Lq * a.G, kWeigh));
   cudaError_t e = batch > 0 ? cudaSuccess : cudaErrorInvalidValue;
   for (int b = 0; e == cudaSuccess && b < B; b += batch) {
     a.clear = b == 0;

@@ -745,7 +745,7 @@ l2a_status check_weigh(const l2a_params* p, const l2a_cache* c, int n_tokens, Ca
   if (st != L2A_OK) return st;
   if (p->flags & ~L2A_FLAG_SHARED_WINDOW) return L2A_ERR_INVALID_ARG;
   if ((int64_t)n_tokens * p->Hq >= (1ll << 31) - 32 || p->B > 65535 || p->Hkv > 65535) return L2A_ERR_UNSUPPORTED;
-  if (most_kept(p, c->kind) > 0 && !cache_few_counts(p)) return L2A_ERR_UNSUPPORTED;
+  if (most_kept(p, c->kind) > 0 && !cache_few_counts(p, c->kind, true)) return L2A_ERR_UNSUPPORTED;
   // (slots and rows of the blocks are counted in 32 bits, as are the CTAs that decode)
   if (has_blocks(p, c->kind) && ((most_blocks(p, n_tokens) * p->Hkv) >= (1ll << 31) || most_blocks(p, n_tokens) >= (1ll << 31) / kTileM ||
                         key_tiles(p->Lk) * p->Hkv >= (1ll << 31)))

@@ -156,12 +156,88 @@ def test_more_positions_than_shared_memory_keeps():
     run("e4m3", 128, 128, 1, 64, [450000], [200001], 4, 4096, weights=few_values)
 
 
+def test_many_positions_in_shared_memory():
+    run("e2m1", 128, 64, 1, 64, [300000, 1000], [120000, 900], 4, 4096)
+
+
+def test_offsets_beyond_2_31():
+    """Pools of over 2^31 bytes of codes: pages at their ends."""
+    Hkv, page, D, n_pages = 8, 128, 128, 40000                        # 65536 bytes of codes a page
+    small = make_cache("e2m1", page, Hkv, D, [700, 300], 21)
+    codes = [torch.zeros((n_pages, Hkv, page, D // 2), dtype=torch.uint8, device="cuda") for _ in "KV"]
+    scales = [torch.zeros((n_pages, Hkv, page * 9), dtype=torch.uint8, device="cuda") for _ in "KV"]
+    weights = torch.zeros((n_pages, Hkv, page), device="cuda")
+    w = torch.rand(small.poolK.shape[:3], device="cuda")
+    src = torch.tensor([[n_pages - 1, n_pages - 3, n_pages - 2, n_pages - 9, 5, n_pages - 5], [n_pages - 6, 4, n_pages - 7, 0, 0, 0]], device="cuda")
+    for b, n in ((0, 6), (1, 3)):
+        for i in range(n):
+            for big, x in zip(codes + scales + [weights], (small.poolK, small.poolV, small.ks, small.vs, w)):
+                big[src[b, i]] = x[small.table[b, i].long()]
+    dst = torch.tensor([[n_pages - 20, n_pages - 21, n_pages - 22], [n_pages - 23, n_pages - 24, 7]], device="cuda")
+    four = [x.view(torch.float4_e2m1fn_x2) for x in codes]
+    length = torch.zeros(2, dtype=torch.int32, device="cuda")
+    a, b = (l2a.cache(*four, t.int().contiguous(), n, *scales) for t, n in ((src, small.length), (dst, length)))
+    target = Target(small, 384, page)
+    p = l2a.params(2, 384, 700, Hkv, Hkv, D, 8)
+    keep = torch.tensor([384, 200], dtype=torch.int32, device="cuda")
+    ws = torch.empty(l2a.l2a_cache_evict_workspace_bytes(p, a), dtype=torch.uint8, device="cuda")
+    kept = [torch.empty((2, Hkv, 384), dtype=torch.int32, device="cuda") for _ in range(2)]
+    l2a.l2a_cache_evict(p, small.handle, w, keep, 4, 50, target.handle, target.w, target.lengths, kept[0], ws)
+    l2a.l2a_cache_evict(p, a, weights, keep, 4, 50, b, weights, length, kept[1], ws)
+    assert torch.equal(*kept) and length.tolist() == [384, 200]
+    out = [[torch.empty((2, 384, Hkv, D), dtype=torch.bfloat16, device="cuda") for _ in "KV"] for _ in range(2)]
+    pr = l2a.params(2, 1, 384, Hkv, Hkv, D, 0)
+    l2a.l2a_cache_read(pr, target.handle, None, *out[0])
+    l2a.l2a_cache_read(pr, b, None, *out[1])
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1]) and bool(out[0][0].any())
+    # attention and weights from the same places
+    Q = torch.randn((2, 32, D), device="cuda").bfloat16()
+    for new in (1, 40):
+        pa = l2a.params(2, new, 384, 32, Hkv, D, 60)
+        Q = torch.randn((2 * new, 32, D), device="cuda").bfloat16()
+        d = torch.ones(2 * new, dtype=torch.uint8, device="cuda")
+        got = []
+        for h, x in ((target.handle, target.w), (b, weights)):
+            O = torch.empty_like(Q)
+            ws = torch.empty(max(l2a.l2a_cache_workspace_bytes(pa, h, 2 * new), l2a.l2a_cache_weigh_workspace_bytes(pa, h, 2 * new)), dtype=torch.uint8,
+                             device="cuda")
+            l2a.l2a_cache_forward(pa, h, Q, None, 2 * new, d, O, ws)
+            l2a.l2a_cache_weigh(pa, h, Q, None, 2 * new, d, x, ws)
+            table = target.table if h is target.handle else dst
+            got.append((O, [x[table[s, torch.arange(n, device="cuda") // page].long(), :, torch.arange(n, device="cuda") % page]
+                            for s, n in ((0, 384), (1, 200))]))
+        assert torch.equal(got[0][0], got[1][0]) and all(torch.equal(x, y) for x, y in zip(got[0][1], got[1][1]))
+
+
 def test_bounds_above_the_lengths():
     run("bf16", 64, 64, 2, 128, [100, 300], [50, 70], 2, 9, most=100, Lk=60000, with_kept=False)
 
 
 def test_many_sequences():
     run("e2m1", 16, 16, 1, 64, [1 + i % 50 for i in range(300)], [1 + i % 23 for i in range(300)], 1, 3)
+
+
+def test_a_captured_call_of_several_CTAs():
+    c = make_cache("e4m3", 64, 1, 64, [40000], 3)
+    t = Target(c, 9000, 64)
+    w = torch.rand((c.poolK.shape[0], 1, 64), device="cuda")
+    p = l2a.params(1, 9000, 40000, 1, 1, 64, 8)
+    ws = torch.empty(l2a.l2a_cache_evict_workspace_bytes(p, c.handle), dtype=torch.uint8, device="cuda")
+    kept = torch.zeros((1, 1, 9000), dtype=torch.int32, device="cuda")
+    keep = torch.tensor([9000], dtype=torch.int32, device="cuda")
+    l2a.l2a_cache_evict(p, c.handle, w, keep, 4, 100, t.handle, t.w, t.lengths, kept, ws)
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        l2a.l2a_cache_evict(p, c.handle, w, keep, 4, 100, t.handle, t.w, t.lengths, kept, ws)
+    for n in (40000, 20000, 8000):
+        c.length.fill_(n)
+        w.copy_(torch.rand_like(w))
+        g.replay()
+        torch.cuda.synchronize()
+        j = torch.arange(n, device="cuda")
+        want = stays(w[c.table[0, j // 64].long(), 0, j % 64].double().cpu().numpy(), n, 9000, 4, 100, 9000)
+        assert kept[0, 0, :len(want)].tolist() == want and int(t.lengths) == len(want) and bool((kept[0, 0, len(want):] == -1).all())
 
 
 def test_the_same_pools_and_lengths_in_place():
