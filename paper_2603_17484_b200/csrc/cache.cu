@@ -163,18 +163,10 @@ __global__ void __launch_bounds__(kRowsThreads, 4) cache_append_kernel(const App
           to_slot[lane] = pos & ((1 << c.page_shift) - 1);
         }
       }
-      __syncthreads();
     }
+    // ---- codes and scales, in the place of the values; meanwhile the first tokens' places are looked up
 #pragma unroll
     for (int i = 0; i < kAppendAhead; ++i) {
-      if (done_group >= groups) break;
-      const bool value = done_hv & 1;
-      const int row = done_group * kRows + lane / kLanes, page = to_page[row];
-      const int64_t slot = ((int64_t)(done_hv >> 1) << c.page_shift) + to_slot[row];
-      uint8_t* dst = (value ? c.V : c.K) + page * c.page_bytes + slot * row_bytes(kKind, D);
-      uint8_t* scales = (value ? c.vs : c.ks) + page * c.scale_stride;
-      const int head = done_hv >> 1;
-      next(done_hv, done_group);
       uint32_t m = 0, e = 0, own = 0;
       bool finite = true;
       if (kE4M3 || kE2M1) {
@@ -218,27 +210,41 @@ __global__ void __launch_bounds__(kRowsThreads, 4) cache_append_kernel(const App
           }
           code[k] = finite ? pack_e2m1(x) : 0u;
         }
-        if (page >= 0) {
-          *reinterpret_cast<uint2*>(dst + sub * 8) = make_uint2(code[0], code[1]);
-          scales[blocks_at<D>(c, head, to_slot[row]) + sub] = (uint8_t)scale;
-          if (sub == 0) scales[exponent_at<D, kKind>(c, head, to_slot[row])] = (uint8_t)e;
-        }
+        w[i][0] = code[0];
+        w[i][1] = code[1];
+        w[i][4] = e | scale << 8;
       } else if (kE4M3) {
         const float f = __uint_as_float((254u - e) << 23);         // 2^-e; e + 127 is 1 .. 247
         const float2 inv = make_float2(f, f);
-        uint32_t code[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const uint32_t u = w[i][2 * k], v = w[i][2 * k + 1];
           const float2 x = __fmul2_rn(make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)), inv);
           const float2 y = __fmul2_rn(make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)), inv);
-          code[k] = __byte_perm(pack_e4m3(x.x, x.y), pack_e4m3(y.x, y.y), 0x5410);
+          w[i][k] = __byte_perm(pack_e4m3(x.x, x.y), pack_e4m3(y.x, y.y), 0x5410);
         }
-        if (page >= 0) {
-          *reinterpret_cast<uint4*>(dst + sub * 16) = make_uint4(code[0], code[1], code[2], code[3]);
-          if (sub == 0) scales[slot] = (uint8_t)e;
-        }
-      } else if (page >= 0) {
+        w[i][4] = e;
+      }
+    }
+    if (first_batch) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kAppendAhead; ++i) {
+      if (done_group >= groups) break;
+      const bool value = done_hv & 1;
+      const int row = done_group * kRows + lane / kLanes, page = to_page[row], in_page = to_slot[row], head = done_hv >> 1;
+      next(done_hv, done_group);
+      if (page < 0) continue;
+      const int64_t slot = ((int64_t)head << c.page_shift) + in_page;
+      uint8_t* dst = (value ? c.V : c.K) + page * c.page_bytes + slot * row_bytes(kKind, D);
+      uint8_t* scales = (value ? c.vs : c.ks) + page * c.scale_stride;
+      if (kE2M1) {
+        *reinterpret_cast<uint2*>(dst + sub * 8) = make_uint2(w[i][0], w[i][1]);
+        scales[blocks_at<D>(c, head, in_page) + sub] = (uint8_t)(w[i][4] >> 8);
+        if (sub == 0) scales[exponent_at<D, kKind>(c, head, in_page)] = (uint8_t)w[i][4];
+      } else if (kE4M3) {
+        *reinterpret_cast<uint4*>(dst + sub * 16) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+        if (sub == 0) scales[slot] = (uint8_t)w[i][4];
+      } else {
         store_32(dst + sub * 32, a.wide_pool, w[i]);
       }
     }

@@ -357,17 +357,14 @@ __device__ __forceinline__ void decode_cache(const ChunkArgs& p, int item, int b
     const int in_page = key & ((1 << c.page_shift) - 1);
     const int64_t slot = ((int64_t)head << c.page_shift) + in_page;
     const uint8_t* row = src + page * c.page_bytes + slot * row_bytes(kKind, D);
-    x[i] = make_uint4(0, 0, 0, 0);
-    e[i] = t[i] = 0u;
-    if (page < 0) continue;
-    e[i] = exps[page * c.scale_stride + exponent_at<D, kKind>(c, head, in_page)];
     if (kE2M1) {
-      const uint2 y = *reinterpret_cast<const uint2*>(row + sub * 8);
-      x[i].x = y.x; x[i].y = y.y;
-      t[i] = exps[page * c.scale_stride + blocks_at<D>(c, head, in_page) + sub];
+      const uint2 y = page >= 0 ? *reinterpret_cast<const uint2*>(row + sub * 8) : make_uint2(0u, 0u);
+      x[i] = make_uint4(y.x, y.y, 0u, 0u);
+      t[i] = page >= 0 ? exps[page * c.scale_stride + blocks_at<D>(c, head, in_page) + sub] : 0u;
     } else {
-      x[i] = *reinterpret_cast<const uint4*>(row + sub * 16);
+      x[i] = page >= 0 ? *reinterpret_cast<const uint4*>(row + sub * 16) : make_uint4(0, 0, 0, 0);
     }
+    e[i] = page >= 0 ? exps[page * c.scale_stride + exponent_at<D, kKind>(c, head, in_page)] : 0u;
   }
   // all keys where a token is routed, else those of the windows (looked up while the codes are on their way)
   bool routed = false;

@@ -75,6 +75,7 @@ struct FewSeq {
   __device__ int tiles() const { return n_loc + n_out; }       // of a KV head and block of rows
 };
 static_assert(sizeof(FewSeq) <= sizeof(FewBars::found), "kept in shared memory");
+template <bool kWeigh>
 __device__ __forceinline__ FewSeq few_seq(const CacheFwdArgs& a, int b) {
   FewSeq s;
   s.n = cache_new(a.c, b, s.first);
@@ -84,9 +85,9 @@ __device__ __forceinline__ FewSeq few_seq(const CacheFwdArgs& a, int b) {
   s.lo = max(0, s.length - s.n - a.window);
   s.n_loc = a.local && s.n > 0 && s.length > 0 ? (s.length - 1) / kTile - s.lo / kTile + 1 : 0;
   s.hi = -1;
-  if (a.global && (a.d != nullptr || a.every))
+  if (a.global && (a.d != nullptr || (kWeigh && a.every)))
     for (int i = 0; i < s.n; ++i)
-      if (a.every || a.d[s.first + i] != 0) s.hi = s.length - s.n + i - a.shift;
+      if ((kWeigh && a.every) || a.d[s.first + i] != 0) s.hi = s.length - s.n + i - a.shift;
   s.hi = max(s.hi, -1);
   s.n_out = s.hi / kTile + (s.hi >= 0 ? 1 : 0);
   return s;
@@ -180,12 +181,13 @@ struct Walk {
   int b, base;             // sequence and its first tile
   FewSeq s;
 };
+template <bool kWeigh>
 __device__ __forceinline__ bool next_piece(const CacheFwdArgs& a, Walk& w, Piece& p) {
   if (w.at >= w.end) return false;
   while (w.at >= w.base + w.s.tiles() * w.s.blocks * a.c.Hkv) {
     w.base += w.s.tiles() * w.s.blocks * a.c.Hkv;
     if (++w.b >= a.c.B) return false;
-    w.s = few_seq(a, w.b);
+    w.s = few_seq<kWeigh>(a, w.b);
   }
   const int per = w.s.tiles(), in = w.at - w.base, x = in % per;
   p.b = w.b;
@@ -272,7 +274,7 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
       if (p.seg == 0) {
         row_lo[x][y] = pos - a.window;
         row_hi[x][y] = pos;
-      } else if (a.every || a.d[seq.first + i] != 0) {
+      } else if ((kWeigh && a.every) || a.d[seq.first + i] != 0) {
         row_hi[x][y] = pos - a.shift;
       }
       every_lo = max(every_lo, row_lo[x][y]);
@@ -600,7 +602,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
     if (pass == 1) per_cta = tiles_per_cta(total, all_pairs, gridDim.x);
     for (int b0 = 0; b0 < c.B; b0 += kThreads) {
       const int b = b0 + tid;
-      if (b < c.B && (pass == 0 || c.B > kThreads)) own = few_seq(a, b);
+      if (b < c.B && (pass == 0 || c.B > kThreads)) own = few_seq<kWeigh>(a, b);
       const int pairs = b < c.B && own.tiles() > 0 ? own.blocks * c.Hkv : 0, n = own.tiles() * pairs;
       int x = n;
       if (pass == 0) {
@@ -664,7 +666,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
     constexpr int kGroup = 1 + D / 16, kScaleCopies = SM::kTensors * kTile / 16 * kGroup, kRounds = kE2M1 ? (kScaleCopies + 31) / 32 : 0;
     int s = 0, ph = 1;
     Piece p;
-    while (ok && next_piece(a, walk, p)) {
+    while (ok && next_piece<kWeigh>(a, walk, p)) {
       const int last_entry = p.hi >> c.page_shift, first_entry = p.lo >> c.page_shift;
       int entry0 = -64, page_ids = -1;
       for (int t = p.t0; t < p.t1; ++t) {
@@ -724,7 +726,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
     const int r0 = warp * 16;                          // this warp's keys of a tile
     int s = 0, ph = 0;
     Piece p;
-    while (next_piece(a, walk, p)) {
+    while (next_piece<kWeigh>(a, walk, p)) {
       constexpr int kPitch = D + 4;
       float* mine_red = red + warp * kRows * (kWeigh ? 2 : kPitch);
       if constexpr (kE2M1) {
@@ -1150,8 +1152,8 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
 // Joins the parts of one head of one new token:
 //   o = sum_loc acc_i 2^(m_i - M_loc) / L_loc + d sum_all acc_i 2^(m_i - M_all) / L_all
 // Bound by latencies: every thread asks for its share of the first kAhead * 128 / (D / 4) parts before the weights are known.
-constexpr int kCombineThreads = 128, kAhead = 12, kMaxParts = kMostCtas + 2;
-template <int D, int kRows>
+constexpr int kCombineThreads = 128, kAhead = 12;
+template <int D, int kRows, int kMaxParts>
 __global__ void __launch_bounds__(kCombineThreads) cache_few_combine_kernel(const CacheFwdArgs a) {
   constexpr int kLanes = D / 4, kGroups = kCombineThreads / kLanes, kPitch = D + 4;
   __shared__ float weight[kMaxParts];
@@ -1352,7 +1354,7 @@ cudaError_t launch(const CacheFwdArgs& a, const CUtensorMap& mapK, const CUtenso
     return launch_dependent(cache_few_add_kernel, keys, kAddThreads, 0, s, true, a, kRows);
   }
   const dim3 grid(a.Hq, a.c.B, std::max(1, std::min(a.c.Lq, a.few_rows / a.G)));
-  return launch_dependent(cache_few_combine_kernel<D, kRows>, grid, kCombineThreads, 0, s, true, a);
+  return launch_dependent(cache_few_combine_kernel<D, kRows, ctas_per_sm(kKind, kHigh, false) * kSplitSms + 2>, grid, kCombineThreads, 0, s, true, a);
 }
 
 template <int D, bool kHigh, bool kWeigh>

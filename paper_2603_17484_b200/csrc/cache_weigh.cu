@@ -199,21 +199,18 @@ __device__ __forceinline__ void decode_keys(const WeighArgs& p, int64_t item, in
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int64_t key = key0 + i * kRows + lane / kLanes;
-    x[i] = make_uint4(0, 0, 0, 0);
-    e[i] = t[i] = 0u;
     const int page = inside && key < length ? cache_page(c, b, (int)key) : -1;
-    if (page < 0) continue;
     const int in_page = (int)key & ((1 << c.page_shift) - 1);
     const uint8_t* row = c.K + page * c.page_bytes + (((int64_t)head << c.page_shift) + in_page) * row_bytes(kKind, D);
     const uint8_t* scales = c.ks + page * c.scale_stride;
-    e[i] = scales[exponent_at<D, kKind>(c, head, in_page)];
     if (kE2M1) {
-      const uint2 y = *reinterpret_cast<const uint2*>(row + sub * 8);
-      x[i].x = y.x; x[i].y = y.y;
-      t[i] = scales[blocks_at<D>(c, head, in_page) + sub];
+      const uint2 y = page >= 0 ? *reinterpret_cast<const uint2*>(row + sub * 8) : make_uint2(0u, 0u);
+      x[i] = make_uint4(y.x, y.y, 0u, 0u);
+      t[i] = page >= 0 ? scales[blocks_at<D>(c, head, in_page) + sub] : 0u;
     } else {
-      x[i] = *reinterpret_cast<const uint4*>(row + sub * 16);
+      x[i] = page >= 0 ? *reinterpret_cast<const uint4*>(row + sub * 16) : make_uint4(0, 0, 0, 0);
     }
+    e[i] = page >= 0 ? scales[exponent_at<D, kKind>(c, head, in_page)] : 0u;
   }
   // (looked up while the codes are on their way)
   bool counts = a.every;
