@@ -520,7 +520,7 @@ l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c, const void
  * Scores, soft-max statistics and sums are fp32, products of bf16 and decoded keys exact.  Bit-reproducible.  Keys that a counted token sees must be finite; a query
  * row with NaN makes the weights of the keys that it sees NaN.
  * Few rows: HBM-bound, keys and weights once.  Many: bound by the exponentials, two for each pair of a row and a key.
- * Limits: n_tokens * Hq < 2^31 - 32; B, Hkv <= 65535; Lk * (Hkv + 112) < 2^35 and Lk * Hkv < 2^38.  Errors: L2A_ERR_INVALID_ARG, L2A_ERR_UNSUPPORTED (D,
+ * Limits: n_tokens * Hq < 2^31 - 32; B, Hkv <= 65535; Lk * (Hkv + 149) < 2^35 and Lk * Hkv < 2^38.  Errors: L2A_ERR_INVALID_ARG, L2A_ERR_UNSUPPORTED (D,
  * page_size, kind, the limits), L2A_ERR_WORKSPACE, L2A_ERR_CUDA; a bounded device wait that runs out is reported by the status header.
  */
 l2a_status l2a_cache_weigh_workspace_bytes(const l2a_params* p, const l2a_cache* c, int n_tokens, size_t* ws_bytes);

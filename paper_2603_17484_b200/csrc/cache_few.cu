@@ -6,7 +6,7 @@
 // of Local Attention (from the first row's window on; all rows) and, where a token is routed, those before its window.
 // Every key block a routed row sees thus enters one set of partial soft-max results, and s and a are weighted sums of
 // the sets.  All segments of the call, laid end to end, are cut into equal ranges of tiles, one to a CTA (two CTAs
-// an SM), whatever the lengths of the sequences: a range is a few pieces of segments, a piece leaves its rows
+// an SM, three where registers allow), whatever the lengths of the sequences: a range is a few pieces of segments, a piece leaves its rows
 // (acc, max, sum) in a slot of the workspace, and cache_few_combine_kernel joins the slots of a row.  A sequence that is one
 // piece stores its result itself.
 //
@@ -22,6 +22,7 @@
 //                   scores in fp32, the values' scales go into the weights: w = 2^(s + e - M) with a running maximum M of s + e,
 //                   beside the sum of 2^(s - m) with its own.  fp16 has 11 bits against bf16's 8, but less range: Q is scaled by a
 //                   power of two for each row, w lies at 2^10 .. 2^14 where it counts and is dropped at 2^-38 of that.
+//                   e2m1: the roles of the operands are exchanged (few_piece_e2m1).
 //
 // Measured (captured calls back to back, milliseconds long): 16 sequences of 128K keys (32/8 heads, D = 128, four routed) e4m3 196 to 202 us for
 // 1.18 GB = 5.9 to 6.0 TB/s, bf16 346 us for 2.35 GB = 6.8 TB/s; 32 ragged ones of up to 8000, a quarter routed, bf16 69 us (394 MB: 5.7 TB/s).
@@ -30,6 +31,12 @@
 // A lone short sequence is latency (9001 keys: 13.3 us, of which this kernel 9.2; the dense l2a_decode, which knows its lengths on the host,
 // takes 7.6 in 16 bits): lists, lengths and decisions are read by every CTA ahead of its first copy.  Tried: two chains of products 206 us
 // against 196; the loads of V ahead of the soft-max, no change; pieces and rows of Q handed over by the producer, 14.2 against 13.0 for 9001 keys.
+// e2m1, calls one after the other: the 16 sequences of 128K keys 172 us for 671 MB = 3.9 TB/s, the 32 ragged ones (pages of 16) 51 us, 9001 keys 16.4.  Bound
+// by the instructions of the conversions and their latencies with three warps a scheduler: without the loads 162 us, without the computing 122; with Q's
+// operands in registers instead of shared memory 176.
+// 64 of about 340 a warp for 16 keys multiply by block scales (32 us), 64 convert codes.  Tried: scores by tcgen05
+// (kind::f8f6f4 takes e2m1 as it is; queries as three e5m2 numbers, blocks' products kept apart and scaled in fp32) 226 us: fewer conversions,
+// but a chain of 4600 clk a warp for 128 keys.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -46,11 +53,13 @@ constexpr int kComputeWarps = kTile / 16;
 constexpr int kThreads = (kComputeWarps + 1) * 32;
 constexpr int kMaxStages = 6;
 constexpr int kMinTiles = 4;                 // tiles of a CTA at least (9001 keys, 28/4 heads: 12.6 us; with 2 14.1, 3 13.1, 6 13.8)
-// CTAs of an SM: registers allow no more (five warps each)
+// CTAs of an SM: registers allow no more (five warps each).  us of e2m1 with four / three: weights of 16 ragged sequences of 32K 37.6 / 40.2, attention of
+// 16 of 128K (where registers spill with four) 179 / 172.
 __host__ __device__ constexpr int ctas_per_sm(int kind, bool high, bool weigh) {
-  return weigh ? (high && kind == L2A_CACHE_E2M1 ? 2 : 3) : kind == L2A_CACHE_E2M1 && !high ? 3 : 2;
+  const bool more = kind == L2A_CACHE_E2M1 && !high;
+  return weigh ? (more ? 4 : 3) : more ? 3 : 2;
 }
-constexpr int kMostCtas = 3 * kSplitSms;
+constexpr int kMostCtas = 3 * kSplitSms, kMostWeighCtas = 4 * kSplitSms;
 constexpr float kWeightTop = 10.f;           // log2 of the largest weight when the reference is new (fp16 operands)
 // e2m1: 16 keys at a time of a tile for each warp; with more, the warps take tiles in turn, and a stage of the ring is held longer.  us for 16
 // sequences of 128K keys: 1 189, 2 176, 4 184.
@@ -124,6 +133,9 @@ __device__ __forceinline__ uint32_t lds32(uint32_t saddr) {
 __device__ __forceinline__ void lds64(uint32_t saddr, uint32_t& x, uint32_t& y) {
   asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(saddr));
 }
+__device__ __forceinline__ void sts128(uint32_t saddr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(saddr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
 __device__ __forceinline__ uint32_t lds8(uint32_t saddr) {
   uint16_t v;
   asm volatile("ld.shared.u8 %0, [%1];" : "=h"(v) : "r"(saddr));
@@ -146,7 +158,9 @@ struct FewSmem {
   static constexpr int kTileBytes = kTile * row_bytes(kKind, D);
   static constexpr int kStageBytes = kTensors * kTileBytes;
   static constexpr int kScaleBytes = kTensors * kTile * scale_bytes(kKind, D);    // exponents of K, of V; e2m1: scales of the blocks of K, of V
-  static __host__ __device__ constexpr int red_bytes(int rows) { return kComputeWarps * rows * (kWeigh ? 2 : D + 4) * 4; }
+  // floats of a warp's results; e2m1: of its fragments of Q before that
+  static __host__ __device__ constexpr int red_floats(int rows) { return kWeigh ? (kKind == L2A_CACHE_E2M1 ? rows * D / 2 : rows * 2) : rows * (D + 4); }
+  static __host__ __device__ constexpr int red_bytes(int rows) { return kComputeWarps * red_floats(rows) * 4; }
   static __host__ __device__ constexpr int total(int stages, int rows) {
     return stages * (kStageBytes + kScaleBytes) + red_bytes(rows) + (int)sizeof(FewBars);
   }
@@ -231,8 +245,10 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
   constexpr int kHalves = kHigh ? 2 : 1, kSteps = kE2m1Steps, kWarps = kComputeWarps / kSteps, kCols = D / 8, kVWords = D / 64, kKWords = D / 32;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, hr = lane >> 2, t4 = lane & 3;
   volatile int* abort_flag = &bar->abort_flag;
-  // ---- B fragments of Q: row hr (and hr + 8), this lane's quarter of its elements, the largest of the row at 2^14 .. 2^15
-  uint32_t qb[kHalves][D / 16][2];
+  named_barrier(1, kComputeWarps * 32);            // what the piece before left has been read
+  // ---- B fragments of Q: row hr (and hr + 8), this lane's quarter of its elements, the largest of the row at 2^14 .. 2^15.  They wait in shared memory,
+  // where the warp's results will be, for the registers of a CTA more.
+  const uint32_t q_at = smem_u32(red) + lane * 16;
   float row_scale[kHalves][2];                 // of the rows 2 t4, 2 t4 + 1 (and + 8)
 #pragma unroll
   for (int x = 0; x < kHalves; ++x) {
@@ -258,9 +274,14 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
 #pragma unroll
     for (int k = 0; k < kVWords; ++k)
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        qb[x][k * 4 + j / 2][j & 1] = pack_f16(__uint_as_float(v[k][j] << 16) * f, __uint_as_float(v[k][j] & 0xffff0000u) * f);
+      for (int j = 0; j < 8; j += 4) {
+        uint32_t q[4];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) q[z] = pack_f16(__uint_as_float(v[k][j + z] << 16) * f, __uint_as_float(v[k][j + z] & 0xffff0000u) * f);
+        sts128(q_at + (x * kKWords + 2 * k + j / 4) * 512, q[0], q[1], q[2], q[3]);
+      }
   }
+  __syncwarp();
   // ---- the keys that each row sees in this segment
   int row_lo[kHalves][2], row_hi[kHalves][2], every_lo = p.lo, every_hi = p.hi;
 #pragma unroll
@@ -353,8 +374,9 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
           const uint32_t a0[4] = {h[0][0], h[1][0], h[0][1], h[1][1]}, a1[4] = {h[0][2], h[1][2], h[0][3], h[1][3]};
 #pragma unroll
           for (int x = 0; x < kHalves; ++x) {
-            mma_16816<true>(sc[x], a0, qb[x][2 * i][0], qb[x][2 * i][1]);
-            mma_16816<true>(sc[x], a1, qb[x][2 * i + 1][0], qb[x][2 * i + 1][1]);
+            const float4 q = lds128(q_at + (x * kKWords + i) * 512);
+            mma_16816<true>(sc[x], a0, __float_as_uint(q.x), __float_as_uint(q.y));
+            mma_16816<true>(sc[x], a1, __float_as_uint(q.z), __float_as_uint(q.w));
           }
         }
         const float fk[2] = {scale_of_exponent(lds8(exp_at + scale + i16 * 16)), scale_of_exponent(lds8(exp_at + scale + i16 * 16 + 8))};
@@ -532,7 +554,7 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
     if (lane == 0) mbar_arrive(&bar->empty[stage]);
   }
   // ---- what this warp has, for the join with the others
-  named_barrier(1, kComputeWarps * 32);            // the piece before has been read
+  __syncwarp();
 #pragma unroll
   for (int x = 0; x < kHalves; ++x)
 #pragma unroll
@@ -728,7 +750,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
     Piece p;
     while (next_piece<kWeigh>(a, walk, p)) {
       constexpr int kPitch = D + 4;
-      float* mine_red = red + warp * kRows * (kWeigh ? 2 : kPitch);
+      float* mine_red = red + warp * SM::red_floats(kRows);
       if constexpr (kE2M1) {
         ok = few_piece_e2m1<D, kHigh, kWeigh>(a, walk.s, p, smem, scales, stages, bar, s, ph, mine_red) && ok;
       } else {
@@ -1089,7 +1111,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
         if (tid < kRows) {
           float2 y = parts[tid];
 #pragma unroll
-          for (int w = 1; w < kComputeWarps; ++w) join_sums(y.x, y.y, parts[w * kRows + tid].x, parts[w * kRows + tid].y);
+          for (int w = 1; w < kComputeWarps; ++w) join_sums(y.x, y.y, parts[w * (SM::red_floats(kRows) / 2) + tid].x, parts[w * (SM::red_floats(kRows) / 2) + tid].y);
           // (a wait that ran out: the sum is none)
           if (*abort_flag != 0) y = make_float2(0.f, -1.f);
           reinterpret_cast<float2*>(a.part)[((int64_t)(p.b * c.Hkv + p.g) * a.row_blocks + p.block + blockIdx.x) * kRows + tid] = y;
@@ -1429,7 +1451,7 @@ cudaError_t launch_cache_few(const CacheFwdArgs& args, void* ws, cudaStream_t s)
 static int64_t score_pitch(int Lk) { return ((int64_t)Lk + kTile - 1) / kTile * kTile; }
 size_t cache_few_weigh_ws_bytes(const l2a_params* p, int rows) {
   const size_t pairs = (size_t)p->B * p->Hkv;
-  return plan_bytes(p->B) + align_up((pairs * row_blocks(rows) + kMostCtas) * kBlockRows * 2 * sizeof(float), 256) +
+  return plan_bytes(p->B) + align_up((pairs * row_blocks(rows) + kMostWeighCtas) * kBlockRows * 2 * sizeof(float), 256) +
          align_up(pairs * rows * score_pitch(p->Lk) * sizeof(float), 256);
 }
 
@@ -1442,7 +1464,7 @@ cudaError_t launch_cache_few_weigh(const CacheFwdArgs& args, void* ws, cudaStrea
   a.row_blocks = row_blocks(a.score_rows);
   at += plan_bytes(a.c.B);
   a.part = reinterpret_cast<float*>(at);
-  a.scores = reinterpret_cast<float*>(at + align_up(((size_t)a.c.B * a.c.Hkv * a.row_blocks + kMostCtas) * kBlockRows * 2 * sizeof(float), 256));
+  a.scores = reinterpret_cast<float*>(at + align_up(((size_t)a.c.B * a.c.Hkv * a.row_blocks + kMostWeighCtas) * kBlockRows * 2 * sizeof(float), 256));
   return launch_few<true>(a, s);
 }
 
