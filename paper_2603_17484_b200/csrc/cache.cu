@@ -107,7 +107,7 @@ __device__ __forceinline__ uint32_t finite_magnitudes(uint32_t x) {
 // Where the tokens go takes four dependent loads (list, length, table): looked up once for the CTA, by one warp, while the
 // first rows are on their way and are converted.  What bounds it then is the instructions of the conversion: 18380 tokens (8 heads, D = 128,
 // e4m3) take 24.8 us (113 MB: 4.6 TB/s), with 16-byte loads, products one by one and indices by division 30.6.  e2m1: 24K tokens 39 us (126 MB: 3.2 TB/s;
-// with a division for each value and 94 registers 50), issue slots 68 %.
+// with a division for each value and 94 registers 50), issue slots 70 %.
 constexpr int kAppendAhead = 4;
 template <int D, int kKind, int kTokens>
 __global__ void __launch_bounds__(kRowsThreads, 4) cache_append_kernel(const AppendArgs a) {
