@@ -230,7 +230,7 @@ __device__ __forceinline__ uint32_t mul_by_half(uint32_t a, __half2 f, bool uppe
   return *reinterpret_cast<const uint32_t*>(&x);
 }
 
-// The tiles of a piece over an e2m1 cache, for one warp: all keys of every fourth, 16 at a time.  The keys are the 16 rows of the products' A fragments and the query
+// The tiles of a piece over an e2m1 cache, for one warp: 16 kE2m1Steps keys of every kE2m1Steps-th, 16 at a time.  The keys are the 16 rows of the products' A fragments and the query
 // rows the 8 columns of B, so that up to eight rows take half as many products and accumulators as with the roles of the other kinds; S^T comes out of one
 // product and goes, transposed, into the other:
 //   S^T = K Q^T : a lane takes a quarter of the codes of two keys, consecutive ones, as its elements of successive products (Q has the same order).
