@@ -1302,6 +1302,7 @@ __global__ void __launch_bounds__(kCombineThreads) cache_few_combine_kernel(cons
 constexpr int kAddThreads = 256, kAddSteps = 1, kAddKeys = 4 * kAddThreads * kAddSteps, kMaxRows = kRowBlocks * kBlockRows;
 __global__ void __launch_bounds__(kAddThreads) cache_few_add_kernel(const CacheFwdArgs a, const int slot_rows) {
   __shared__ float lse[kMaxRows];
+  __shared__ int nan_seen[kAddThreads / 32];          // last key that a row with NaN sees (of a warp's rows), -1: none
   const CacheView& c = a.c;
   const int g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t k0 = (int64_t)blockIdx.x * kAddKeys;
@@ -1312,6 +1313,7 @@ __global__ void __launch_bounds__(kAddThreads) cache_few_add_kernel(const CacheF
   if (n == 0 || k0 >= length || (k0 > hi && k0 + kAddKeys <= length - n)) return;
   const int per_cta = a.plan[0], rows = n * a.G, blocks = (rows + kBlockRows - 1) / kBlockRows;
   bool failed = false;
+  int nan_last = -1;
   for (int r = warp; r < rows; r += kAddThreads / 32) {
     const int block = r / kBlockRows, at = seq.x + (g * blocks + block) * n_out;
     const bool counts = n_out > 0 && (a.every || a.d[seq.y + r / a.G] != 0);
@@ -1327,9 +1329,14 @@ __global__ void __launch_bounds__(kAddThreads) cache_few_add_kernel(const CacheF
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) join_sums(m, l, __shfl_xor_sync(0xffffffffu, m, o), __shfl_xor_sync(0xffffffffu, l, o));
     }
-    if (lane == 0) lse[r] = l != 0.f ? m + log2f(l) : INFINITY;          // (infinity: a row that sees nothing)
+    // (infinity: a row that sees nothing, or gives NaN to all that it sees)
+    if (isnan(l)) nan_last = max(nan_last, length - n + r / a.G);
+    if (lane == 0) lse[r] = l != 0.f && !isnan(l) ? m + log2f(l) : INFINITY;
   }
+  if (lane == 0) nan_seen[warp] = nan_last;
   if (__syncthreads_or(failed)) return;                // a wait ran out in a part: nothing is stored
+#pragma unroll
+  for (int w = 0; w < kAddThreads / 32; ++w) nan_last = max(nan_last, nan_seen[w]);
   const float* scores = a.scores + (int64_t)(b * c.Hkv + g) * a.score_rows * a.score_pitch;
 #pragma unroll 1
   for (int i = 0; i < kAddSteps; ++i) {
@@ -1348,6 +1355,10 @@ __global__ void __launch_bounds__(kAddThreads) cache_few_add_kernel(const CacheF
         sum[2] += key + 2 <= hi ? fast_exp2(v.z - z) : 0.f;
         sum[3] += key + 3 <= hi ? fast_exp2(v.w - z) : 0.f;
       }
+    }
+    if (key <= nan_last) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) sum[x] = key + x <= nan_last ? NAN : sum[x];
     }
     add_weights(a, c, b, g, key, length, length - n, hi, sum);
   }
