@@ -53,7 +53,8 @@ struct WeighArgs {
   int64_t* unit_start;           // units of the sequences before it, [B + 1]
   bf16* rows;                    // [Hkv][most_blocks * 128][D]
   int* row_pos;                  // [most_blocks * 128], -1: no row
-  float* minus_lse;              // [Hkv][most_blocks * 128], minus infinity: no row
+  float* minus_lse;              // [Hkv][most_blocks * 128], minus infinity: no row, or one whose sum is NaN,
+  int4* nan_last;                // whose position is here: [Hkv][most_blocks], the last one of each 32 rows, -1: none
   float2* part;                  // maximum and sum of 128 rows, from a range
   int most_blocks;               // bound
   int clear;                     // no kernel ahead has cleared the status word
@@ -466,6 +467,11 @@ weigh_pass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
       for (int i0 = 0; ok && i0 < max(w.blocks, 1); i0 += kKept) {
         const Kept kept(p, w, i0);
         const int hi = kept.n > 0 ? p.blocks[kept.q + kept.n - 1].last : -1;
+        int nan_last = -1;
+        for (int i = 0; i < kept.n; ++i) {
+          const int4 x = p.nan_last[(int64_t)w.g * p.most_blocks + kept.q + i];
+          nan_last = max(nan_last, max(max(x.x, x.y), max(x.z, x.w)));
+        }
         for (int k = w.k0; k < w.k1; k += kept.wide, ++rounds) {
           const int buf = rounds % kSumBufs;
           if (!mbar_wait_warp(&bar->sum_full[buf], (rounds / kSumBufs) & 1, abort_flag)) { ok = false; break; }
@@ -476,7 +482,12 @@ weigh_pass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
               const float4 y = reinterpret_cast<const float4*>(sums + (x * kept.width + i) * 128)[lane];
               four[0] += y.x; four[1] += y.y; four[2] += y.z; four[3] += y.w;
             }
-            add_weights(a, p.codes, w.b, w.g, tile_of(w, k + x) * kTileN + 4 * lane, w.length, i0 == 0 ? fresh : w.length, hi, four);
+            const int key = tile_of(w, k + x) * kTileN + 4 * lane;
+            if (key <= nan_last) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) four[i] = key + i <= nan_last ? NAN : four[i];
+            }
+            add_weights(a, p.codes, w.b, w.g, key, w.length, i0 == 0 ? fresh : w.length, hi, four);
           }
           __syncwarp();
           if (lane == 0) mbar_arrive(&bar->sum_empty[buf]);
@@ -645,7 +656,11 @@ __global__ void __launch_bounds__(kTileM) weigh_join_kernel(const WeighArgs p) {
     m = M;
   }
   const bool row = r < p.blocks[q].n_rows;
-  p.minus_lse[((int64_t)g * p.most_blocks + q) * kTileM + r] = row && l != 0.f ? -(m + log2f(l)) : -INFINITY;
+  const int64_t block = (int64_t)g * p.most_blocks + q;
+  // A row with NaN gives it to the keys that it sees, no others: behind its position the second pass is not to meet it
+  const int nan_last = __reduce_max_sync(0xffffffffu, row && isnan(l) ? p.row_pos[q * kTileM + r] : -1);
+  if (r % 32 == 0) reinterpret_cast<int*>(p.nan_last + block)[r / 32] = nan_last;
+  p.minus_lse[block * kTileM + r] = row && l != 0.f && !isnan(l) ? -(m + log2f(l)) : -INFINITY;
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -670,6 +685,7 @@ size_t layout(const l2a_params* p, int kind, int n_tokens, uint8_t* base, WeighA
   x.unit_start = reinterpret_cast<int64_t*>(take((B + 1) * 8));
   x.row_pos = reinterpret_cast<int*>(take(blocks * kTileM * 4));
   x.minus_lse = reinterpret_cast<float*>(take(Hkv * blocks * kTileM * 4));
+  x.nan_last = reinterpret_cast<int4*>(take(Hkv * blocks * sizeof(int4)));
   x.part = reinterpret_cast<float2*>(take((Hkv * blocks + kCtas * (size_t)most_of_one(p)) * kTileM * 8));
   x.rows = reinterpret_cast<bf16*>(take(Hkv * blocks * kTileM * p->D * 2));
   x.most_blocks = (int)blocks;

@@ -46,3 +46,10 @@ def check(kind, page, lengths, new, value):
                                                    ("e2m1", 64, [700, 40], [12, 2]), ("bf16", 64, [12, 40], [12, 2])])
 def test_few_rows(kind, page, lengths, new, value):
     check(kind, page, lengths, new, value)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("kind,page,lengths,new", [("bf16", 16, [500, 100], [90, 30]), ("e4m3", 64, [1000, 40], [200, 2]),
+                                                   ("e2m1", 128, [400, 300], [400, 20])])
+def test_blocks_of_rows(kind, page, lengths, new, value):
+    check(kind, page, lengths, new, value)
