@@ -517,8 +517,11 @@ l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c, const void
  *                    Lk bytes (fewer rows where that would pass 4 GB); beyond, the rows' queries and of an 8- or 4-bit cache the keys in bf16, 2 * B * Lk *
  *                    Hkv * D bytes with Lk rounded up to 128.  Lk decides, so give it no larger than need be.  It is enough for every smaller
  *                    n_tokens (other fields alike).
- * Scores, soft-max statistics and sums are fp32, products of bf16 and decoded keys exact.  Bit-reproducible.  Keys that a counted token sees must be finite; a query
- * row with NaN makes the weights of the keys that it sees NaN.
+ * Scores, soft-max statistics and sums are fp32, products of bf16 and decoded keys exact.  Keys that a counted token sees must be finite; a query
+ * row with NaN makes the weights of the keys that it sees NaN, and no others.
+ * A page that is in the tables of several sequences (a common prompt) gets the weights that all of them give.  The order in which sequences are added
+ * up is then not fixed, so that such a weight can differ in its last bits; all others are bit-reproducible.  The slots of new tokens belong
+ * to one sequence each.
  * Few rows: HBM-bound, keys and weights once.  Many: bound by the exponentials, two for each pair of a row and a key.
  * Limits: n_tokens * Hq < 2^31 - 32; B, Hkv <= 65535; Lk * (Hkv + 149) < 2^35 and Lk * Hkv < 2^38.  Errors: L2A_ERR_INVALID_ARG, L2A_ERR_UNSUPPORTED (D,
  * page_size, kind, the limits), L2A_ERR_WORKSPACE, L2A_ERR_CUDA; a bounded device wait that runs out is reported by the status header.

@@ -99,7 +99,9 @@ bool cache_chunk_counts(const l2a_params* p, int n_tokens);      // whether it c
 cudaError_t launch_cache_chunk(const CacheFwdArgs& a, bool first, void* ws, bool copy, cudaStream_t s);
 
 // Adds sum[i] to the weights of keys key .. key + 3 of a sequence's KV head, key a multiple of four; those of its new tokens (from `fresh` on)
-// had none.  Keys behind hi that are not new keep what they have.
+// had none.  Keys behind hi that are not new keep what they have.  The memory adds: a page may be in the tables of several sequences, whose CTAs
+// know nothing of each other.  (A key's sums of one sequence come from one thread, in order.  Weights of four chunks of 400 on 16K: 101.5 us a call
+// with loads and stores here, 99.3 with this.)
 __device__ __forceinline__ void add_weights(const CacheFwdArgs& a, const CacheView& c, int b, int g, int key, int length, int fresh, int hi,
                                             const float (&sum)[4]) {
   const int last = min(length - 1, key + 3);
@@ -108,14 +110,15 @@ __device__ __forceinline__ void add_weights(const CacheFwdArgs& a, const CacheVi
   if (page < 0) return;
   float* w = a.weights + page * a.w_page + ((int64_t)g << c.page_shift) + (key & ((1 << c.page_shift) - 1));
   if (last == key + 3 && key + 3 < fresh && (reinterpret_cast<uintptr_t>(w) & 15) == 0) {
-    float4 x = *reinterpret_cast<float4*>(w);
-    x.x += sum[0]; x.y += sum[1]; x.z += sum[2]; x.w += sum[3];
-    *reinterpret_cast<float4*>(w) = x;
+    asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(w), "f"(sum[0]), "f"(sum[1]), "f"(sum[2]), "f"(sum[3]) : "memory");
     return;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (key + i <= last && (key + i <= hi || key + i >= fresh)) w[i] = (key + i < fresh ? w[i] : 0.f) + sum[i];
+  for (int i = 0; i < 4; ++i) {
+    if (key + i > last) break;
+    if (key + i >= fresh) w[i] = sum[i];
+    else if (key + i <= hi) atomicAdd(w + i, sum[i]);
+  }
 }
 
 // Tensor map over a pool: {elements of 128 bytes at most, tokens, (pieces of a row,) heads, pages}; one copy brings box_rows
