@@ -516,7 +516,8 @@ l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c, const void
  *                    a time-out the weights are not to be used).  Up to 64 rows a sequence (Lq * Hq / Hkv) it keeps their scores, 4 * B * Hkv * rows *
  *                    Lk bytes (fewer rows where that would pass 4 GB); beyond, the rows' queries and of an 8- or 4-bit cache the keys in bf16, 2 * B * Lk *
  *                    Hkv * D bytes with Lk rounded up to 128.  Lk decides, so give it no larger than need be.  It is enough for every smaller
- *                    n_tokens (other fields alike).
+ *                    n_tokens, Lq and Lk (other fields alike): near 4 GB of scores it can be more than this call takes, for the rows that are kept of
+ *                    shorter sequences.
  * Scores, soft-max statistics and sums are fp32, products of bf16 and decoded keys exact.  Keys that a counted token sees must be finite; a query
  * row with NaN makes the weights of the keys that it sees NaN, and no others.
  * A page that is in the tables of several sequences (a common prompt) gets the weights that all of them give.  The order in which sequences are added

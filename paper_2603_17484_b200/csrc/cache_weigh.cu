@@ -714,6 +714,18 @@ size_t few_bytes(const l2a_params* p, int kind) {
   const int rows = most_kept(p, kind);
   return rows > 0 ? align_up(cache_few_weigh_ws_bytes(p, rows), 256) : 0;
 }
+// The most of them for any smaller Lq and Lk.  More rows are kept of shorter sequences, so that these can need more: for each number of rows as many
+// keys as kMostScores allows.
+size_t most_few_bytes(const l2a_params* p, int kind) {
+  const int64_t G = p->Hq / p->Hkv, top = std::min<int64_t>((kind == L2A_CACHE_BF16 ? 3 : kRowBlocks) * kBlockRows, (int64_t)p->Lq * G);
+  size_t most = 0;
+  for (int64_t rows = G; rows <= top; ++rows) {
+    l2a_params x = *p;
+    x.Lk = (int)std::min<int64_t>(p->Lk, kMostScores / (4 * (int64_t)p->B * p->Hkv * rows) - 64);
+    if (x.Lk > 0) most = std::max(most, align_up(cache_few_weigh_ws_bytes(&x, (int)rows), 256));
+  }
+  return most;
+}
 bool has_blocks(const l2a_params* p, int kind) { return (int64_t)p->Lq * (p->Hq / p->Hkv) > kept_rows(p, kind); }
 
 template <int D, bool kSum>
@@ -765,9 +777,9 @@ l2a_status check_weigh(const l2a_params* p, const l2a_cache* c, int n_tokens, Ca
     return L2A_ERR_UNSUPPORTED;
   return L2A_OK;
 }
-size_t weigh_ws_bytes(const l2a_params* p, int kind, int n_tokens) {
-  return kWsHeaderBytes + few_bytes(p, kind) + (has_blocks(p, kind) ? layout(p, kind, n_tokens, nullptr, nullptr, nullptr) : 0);
-}
+size_t block_bytes(const l2a_params* p, int kind, int n_tokens) { return has_blocks(p, kind) ? layout(p, kind, n_tokens, nullptr, nullptr, nullptr) : 0; }
+// What a call takes
+size_t weigh_ws_bytes(const l2a_params* p, int kind, int n_tokens) { return kWsHeaderBytes + few_bytes(p, kind) + block_bytes(p, kind, n_tokens); }
 
 }  // namespace
 }  // namespace l2a
@@ -779,7 +791,7 @@ extern "C" l2a_status l2a_cache_weigh_workspace_bytes(const l2a_params* p, const
   const l2a_status st = check_weigh(p, c, n_tokens, &v);
   if (st != L2A_OK) return st;
   if (!ws_bytes) return L2A_ERR_INVALID_ARG;
-  *ws_bytes = weigh_ws_bytes(p, c->kind, n_tokens);
+  *ws_bytes = kWsHeaderBytes + most_few_bytes(p, c->kind) + block_bytes(p, c->kind, n_tokens);      // (the blocks' part grows with all three)
   return L2A_OK;
 }
 
