@@ -62,7 +62,7 @@ __host__ __device__ constexpr int ctas_per_sm(int kind, bool high, bool weigh) {
 constexpr int kMostCtas = 3 * kSplitSms, kMostWeighCtas = 4 * kSplitSms;
 constexpr float kWeightTop = 10.f;           // log2 of the largest weight when the reference is new (fp16 operands)
 // e2m1: 16 keys at a time of a tile for each warp; with more, the warps take tiles in turn, and a stage of the ring is held longer.  us for 16
-// sequences of 128K keys: 1 189, 2 176, 4 184.
+// sequences of 128K keys: 1 189, 2 176.
 constexpr int kE2m1Steps = 2;
 constexpr float kLag = 4.f;                  // the reference follows the maximum when it is more than this behind
 
@@ -1372,7 +1372,10 @@ cudaError_t launch(const CacheFwdArgs& a, const CUtensorMap& mapK, const CUtenso
   constexpr int kRows = kHigh ? 16 : 8;
   constexpr int kPerSm = ctas_per_sm(kKind, kHigh, kWeigh);
   constexpr int kFit = (kSmemPerSm / kPerSm - 1024 - SM::total(0, kRows)) / (SM::kStageBytes + SM::kScaleBytes);
-  constexpr int kStages = kFit < kMaxStages ? kFit : kMaxStages;
+  // e2m1: warps take tiles in turn and wait on those alone.  A wait tells a phase of a stage from the next by its parity, so that within a piece a
+  // stage has to come round to the same warps; from piece to piece a barrier of all warps is between them.
+  constexpr int kTurns = kKind == L2A_CACHE_E2M1 ? kE2m1Steps : 1, kMost = kFit < kMaxStages ? kFit : kMaxStages, kStages = kMost - kMost % kTurns;
+  static_assert(kStages >= 2 && kStages % kTurns == 0, "a stage belongs to the same warps");
   constexpr int smem = SM::total(kStages, kRows);
   static PerDeviceOnce once;
   cudaError_t e = once.run([] {
