@@ -83,7 +83,7 @@ struct CacheFwdArgs {
 // Sequences whose new tokens have at most few_rows rows (tokens x heads of a KV group), one block of rows or kRowBlocks of them:
 // cache_few.cu
 constexpr int kBlockRows = 16, kRowBlocks = 4;
-size_t cache_few_ws_bytes(const l2a_params* p);     // plan and parts
+size_t cache_few_ws_bytes(const l2a_params* p, int kind);     // plan and parts
 bool cache_few_counts(const l2a_params* p, int kind, bool weigh);         // whether it can count the tiles of one sequence
 cudaError_t launch_cache_few(const CacheFwdArgs& a, void* ws, cudaStream_t s);
 

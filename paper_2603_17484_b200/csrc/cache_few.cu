@@ -59,7 +59,7 @@ __host__ __device__ constexpr int ctas_per_sm(int kind, bool high, bool weigh) {
   const bool more = kind == L2A_CACHE_E2M1 && !high;
   return weigh ? (more ? 4 : 3) : more ? 3 : 2;
 }
-constexpr int kMostCtas = 3 * kSplitSms, kMostWeighCtas = 4 * kSplitSms;
+constexpr int kMostWeighCtas = 4 * kSplitSms;
 constexpr float kWeightTop = 10.f;           // log2 of the largest weight when the reference is new (fp16 operands)
 // e2m1: 16 keys at a time of a tile for each warp; with more, the warps take tiles in turn, and a stage of the ring is held longer.  us for 16
 // sequences of 128K keys: 1 189, 2 176.
@@ -1412,11 +1412,13 @@ int batch_of(int Lk, int Hkv, int blocks, int ctas) {
 
 }  // namespace
 
-size_t cache_few_ws_bytes(const l2a_params* p) {
-  return plan_bytes(p->B) + align_up((2 * (size_t)p->B * p->Hkv * row_blocks((int64_t)p->Lq * (p->Hq / p->Hkv)) + kMostCtas) * slot_rows(p) * (p->D + 4) * sizeof(float), 256);
+int ctas_of(int kind, int64_t rows, bool weigh) { return kSplitSms * ctas_per_sm(kind, rows > 8, weigh); }
+size_t cache_few_ws_bytes(const l2a_params* p, int kind) {
+  const int64_t rows = (int64_t)p->Lq * (p->Hq / p->Hkv);
+  return plan_bytes(p->B) +
+         align_up((2 * (size_t)p->B * p->Hkv * row_blocks(rows) + ctas_of(kind, rows, false)) * slot_rows(p) * (p->D + 4) * sizeof(float), 256);
 }
 
-int ctas_of(int kind, int64_t rows, bool weigh) { return kSplitSms * ctas_per_sm(kind, rows > 8, weigh); }
 bool cache_few_counts(const l2a_params* p, int kind, bool weigh) {
   const int64_t rows = (int64_t)p->Lq * (p->Hq / p->Hkv);
   return batch_of(p->Lk, p->Hkv, row_blocks(rows), ctas_of(kind, rows, weigh)) > 0;
