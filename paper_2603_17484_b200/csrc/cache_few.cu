@@ -266,7 +266,8 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
     top = max(top & 0xffffu, top >> 16);
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const int up = min(max(14 + 127 - (int)(top >> 7), -113), 100);
+    // (no further up than leaves the row's scale in fp32: unseen keys have scores of minus infinity, times zero NaN)
+    const int up = min(max(14 + 127 - (int)(top >> 7), -113), min(100, (int)(__float_as_uint(a.scale_log2) >> 23) - 1));
     const float f = ok ? __uint_as_float((uint32_t)(up + 127) << 23) : 0.f;
     const float scale = a.scale_log2 * __uint_as_float((uint32_t)(127 - up) << 23);
     row_scale[x][0] = __shfl_sync(0xffffffffu, scale, t4 * 8);
