@@ -548,7 +548,8 @@ l2a_status l2a_cache_weigh(const l2a_params* p, const l2a_cache* c, const void* 
  *   to_weights out: fp32 pool of its slots.  Slots beyond a sequence's tokens are left alone in all pools.
  *   to_lengths  out: int32 [B], m.  May be c->lengths or to->lengths.
  *   kept        out: optional int32 [B, Hkv, Lq]: the positions that stayed, ascending; -1 behind the m of a sequence.
- *   ws             : device workspace of l2a_cache_evict_workspace_bytes (4 * B * Hkv * Lq and a little), 256-byte aligned.
+ *   ws             : device workspace of l2a_cache_evict_workspace_bytes (4 * B * Hkv * Lq and a little), 256-byte aligned, its first word a
+ *                    status (l2a_workspace_status; no wait of this call has a limit, so that it is L2A_OK but for the debug build's checks).
  * HBM-bound: the weights are read once, what stays is read and written once.  Bit-reproducible.  Errors: L2A_ERR_INVALID_ARG,
  * L2A_ERR_UNSUPPORTED (D, page_size, kind, B or Hkv > 65535), L2A_ERR_WORKSPACE, L2A_ERR_CUDA.
  */

@@ -30,6 +30,7 @@ struct EvictArgs {
   const int32_t* keep;
   int sinks, recent, most;       // most: tokens of a sequence that can stay
   int32_t *kept, *count, *lengths;
+  int* status;                   // the workspace's status word
 };
 
 // What stays of a sequence: its first tokens, the last, and the best in between
@@ -80,7 +81,10 @@ __global__ void __launch_bounds__(kSelectThreads) cache_select_kernel(const Evic
   dependents_release();
   const Kept k = kept_of(a, b);
   int32_t* out = a.kept + ((int64_t)b * c.Hkv + g) * a.most;
-  if (rank == 0 && g == 0 && tid == 0) a.count[b] = k.all;
+  if (rank == 0 && g == 0 && tid == 0) {
+    a.count[b] = k.all;
+    if (b == 0) *a.status = 0;
+  }
   // what stays whatever its weight, and no positions behind it
   const int from = k.first, to = k.length - k.last;        // the positions in between
   for (int64_t i = rank * kSelectThreads + tid; i < a.most; i += ctas * kSelectThreads) {
@@ -364,6 +368,7 @@ extern "C" l2a_status l2a_cache_evict(const l2a_params* p, const l2a_cache* c, c
   a.sinks = sinks;
   a.recent = recent;
   a.most = p->Lq;
+  a.status = static_cast<int*>(ws);
   uint8_t* at = static_cast<uint8_t*>(ws) + kWsHeaderBytes;
   a.count = reinterpret_cast<int32_t*>(at);
   a.kept = kept ? kept : reinterpret_cast<int32_t*>(at + count_bytes(p->B));
