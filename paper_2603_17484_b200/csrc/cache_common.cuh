@@ -108,6 +108,7 @@ __device__ __forceinline__ void add_weights(const CacheFwdArgs& a, const CacheVi
   if (key > last || (key > hi && last < fresh)) return;
   const int page = cache_page(c, b, key);              // (a page holds a multiple of four tokens)
   if (page < 0) return;
+  if (!dbg_in_range(key >= 0 && key % 4 == 0 && last < c.max_keys && g < c.Hkv && b < c.B, a.status)) return;
   float* w = a.weights + page * a.w_page + ((int64_t)g << c.page_shift) + (key & ((1 << c.page_shift) - 1));
   if (last == key + 3 && key + 3 < fresh && (reinterpret_cast<uintptr_t>(w) & 15) == 0) {
     asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(w), "f"(sum[0]), "f"(sum[1]), "f"(sum[2]), "f"(sum[3]) : "memory");

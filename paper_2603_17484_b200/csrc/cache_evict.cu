@@ -216,8 +216,10 @@ __global__ void __launch_bounds__(kMoveThreads) cache_move_kernel(const EvictArg
     int64_t x = -1, y = -1;
     if (t0 + tid < count) {
       const int t = (int)t0 + tid;
-      const int pos = a.kept[((int64_t)b * c.Hkv + g) * a.most + t];
-      if (pos >= 0 && pos < c.max_keys) {
+      const int32_t* kept = a.kept + ((int64_t)b * c.Hkv + g) * a.most;
+      const int pos = kept[t];
+      const bool inside = pos >= 0 && pos < c.max_keys;
+      if (dbg_in_range(inside && t < a.most && (t == 0 || kept[t - 1] < pos), a.status) && inside) {
         const int p = cache_page(c, b, pos), q = cache_page(n, b, t);
         if (p >= 0 && q >= 0) {
           x = (int64_t)p << 32 | (pos & ((1 << c.page_shift) - 1));

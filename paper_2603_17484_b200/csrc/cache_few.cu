@@ -219,6 +219,14 @@ __device__ __forceinline__ bool next_piece(const CacheFwdArgs& a, Walk& w, Piece
   return true;
 }
 
+// (index-checking build) Whether a row's score of a key, and a piece's part, have a place in the workspace
+__device__ __forceinline__ bool score_inside(const CacheFwdArgs& a, const Piece& p, int row, int key) {
+  return p.b < a.c.B && p.g < a.c.Hkv && p.block * kBlockRows + row < a.score_rows && key < a.score_pitch;
+}
+__device__ __forceinline__ bool part_inside(const CacheFwdArgs& a, const Piece& p) {
+  return p.b < a.c.B && p.g < a.c.Hkv && p.block < a.row_blocks;
+}
+
 __device__ __forceinline__ uint32_t move_matrix_t(uint32_t x) {
   uint32_t r;
   asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
@@ -408,7 +416,7 @@ __device__ __forceinline__ bool few_piece_e2m1(const CacheFwdArgs& a, const FewS
               z[k] = v[k / 2][x][(k & 1) * 2 + y] * row_scale[x][y];
               m_new = fmaxf(m_new, z[k]);
             }
-            if (row_hi[x][y] >= 0) {
+            if (row_hi[x][y] >= 0 && dbg_in_range(score_inside(a, p, 2 * t4 + y + 8 * x, key0 + hr + 8 * (2 * kSteps - 1)), a.status)) {
               float* dst = score_at + (int64_t)(8 * x + y) * a.score_pitch + key0;
 #pragma unroll
               for (int k = 0; k < 2 * kSteps; ++k) dst[8 * k] = z[k];
@@ -894,7 +902,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
                 v[y] = sc[y >> 1][2 * x + (y & 1)] * row_scale[x];
                 if (edge && j > row_hi[x]) v[y] = -INFINITY;
               }
-              if (row_hi[x] >= 0) {
+              if (row_hi[x] >= 0 && dbg_in_range(score_inside(a, p, hr + 8 * x, k + 9), a.status)) {
                 float* dst = a.scores + ((int64_t)(p.b * c.Hkv + p.g) * a.score_rows + p.block * kBlockRows + hr + 8 * x) * a.score_pitch + k;
                 *reinterpret_cast<float2*>(dst) = make_float2(v[0], v[1]);
                 *reinterpret_cast<float2*>(dst + 8) = make_float2(v[2], v[3]);
@@ -1115,7 +1123,8 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           for (int w = 1; w < kComputeWarps; ++w) join_sums(y.x, y.y, parts[w * (SM::red_floats(kRows) / 2) + tid].x, parts[w * (SM::red_floats(kRows) / 2) + tid].y);
           // (a wait that ran out: the sum is none)
           if (*abort_flag != 0) y = make_float2(0.f, -1.f);
-          reinterpret_cast<float2*>(a.part)[((int64_t)(p.b * c.Hkv + p.g) * a.row_blocks + p.block + blockIdx.x) * kRows + tid] = y;
+          if (dbg_in_range(part_inside(a, p), a.status))
+            reinterpret_cast<float2*>(a.part)[((int64_t)(p.b * c.Hkv + p.g) * a.row_blocks + p.block + blockIdx.x) * kRows + tid] = y;
         }
         continue;
       }
@@ -1140,6 +1149,7 @@ cache_few_kernel(const CacheFwdArgs a, const __grid_constant__ CUtensorMap mapK,
           A.x += v.x * f; A.y += v.y * f; A.z += v.z * f; A.w += v.w * f;
         }
         if (!p.alone) {
+          if (!dbg_in_range(part_inside(a, p), a.status)) continue;
           float* slot = a.part + (((int64_t)(p.b * c.Hkv + p.g) * a.row_blocks + p.block) * 2 + p.seg + blockIdx.x) * (kRows * kPitch) +
                         r * kPitch;
           *reinterpret_cast<float4*>(slot + c4 * 4) = A;
@@ -1313,6 +1323,7 @@ __global__ void __launch_bounds__(kAddThreads) cache_few_add_kernel(const CacheF
   // keys that some row sees, and the new ones
   if (n == 0 || k0 >= length || (k0 > hi && k0 + kAddKeys <= length - n)) return;
   const int per_cta = a.plan[0], rows = n * a.G, blocks = (rows + kBlockRows - 1) / kBlockRows;
+  if (!dbg_in_range(rows <= a.score_rows && rows <= kMaxRows && blocks <= a.row_blocks && seq.y >= 0 && seq.y <= c.n_tokens - n, a.status)) return;
   bool failed = false;
   int nan_last = -1;
   for (int r = warp; r < rows; r += kAddThreads / 32) {

@@ -55,7 +55,8 @@ struct WeighArgs {
   int* row_pos;                  // [most_blocks * 128], -1: no row
   float* minus_lse;              // [Hkv][most_blocks * 128], minus infinity: no row, or one whose sum is NaN,
   int4* nan_last;                // whose position is here: [Hkv][most_blocks], the last one of each 32 rows, -1: none
-  float2* part;                  // maximum and sum of 128 rows, from a range
+  float2* part;                  // maximum and sum of 128 rows, from a range,
+  int64_t parts;                 // bound of them
   int most_blocks;               // bound
   int clear;                     // no kernel ahead has cleared the status word
 };
@@ -123,7 +124,7 @@ __device__ void make_plan(const WeighArgs& p, int* sums, int64_t* sums2) {
     const int take = b >= 0 && (a.every || a.d[t] != 0) && length - n + (t - first) >= 0;
     int x = take;
     const int all = block_scan(x, sums), at = base + x - take;
-    if (take) p.list[at] = (int)t;
+    if (take && dbg_in_range(at < c.n_tokens, a.status)) p.list[at] = (int)t;
     if (b >= 0 && t == first) p.list_start[b] = at;
     if (b >= 0 && t == first + n - 1) p.list_end[b] = at + take;
     base += all;
@@ -175,7 +176,7 @@ __device__ void make_plan(const WeighArgs& p, int* sums, int64_t* sums2) {
     r.first_pos = r.base + p.list[r.list + r.row0 / a.G];
     r.last = r.base + p.list[r.list + (r.row0 + r.n_rows - 1) / a.G];
     r.tiles = r.last / kTileN + 1;
-    p.blocks[q] = r;
+    if (dbg_in_range(q < p.most_blocks && r.n_rows > 0 && r.last < length, a.status)) p.blocks[q] = r;
   }
 }
 
@@ -219,6 +220,7 @@ __device__ __forceinline__ void decode_keys(const WeighArgs& p, int64_t item, in
     for (int i = threadIdx.x; i < n; i += kPlanThreads) counts |= a.d[first + i] != 0;
   counts = __syncthreads_or(counts);
   if (!inside || !counts) return;
+  if (!dbg_in_range(block < out.table_stride && b < out.B, a.status)) return;
   uint8_t* dst = out.K + ((int64_t)b * out.table_stride + block) * out.page_bytes + ((int64_t)head * kTileN + part * kDecodeKeys) * (2 * D);
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
@@ -254,13 +256,16 @@ __global__ void __launch_bounds__(kRowsThreads) weigh_rows_kernel(const WeighArg
   dependents_release();
   if (q >= p.plan->n_blocks) return;
   const RowBlock r = p.blocks[q];
+  if (!dbg_in_range(r.b < a.c.B && r.list + (r.row0 + r.n_rows - 1) / a.G < a.c.n_tokens, a.status)) return;
   constexpr int kPieces = D / 8, kSteps = kTileM * kPieces / kRowsThreads;
   bf16* dst = p.rows + ((int64_t)g * p.most_blocks + q) * kTileM * D;
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
     const int row = (i * kRowsThreads + tid) / kPieces, piece = tid % kPieces, x = r.row0 + row, token = x / a.G;
     uint4 v = make_uint4(0, 0, 0, 0);
-    if (row < r.n_rows) v = reinterpret_cast<const uint4*>(a.q + p.list[r.list + token] * a.q_t + (int64_t)(g * a.G + x - token * a.G) * D)[piece];
+    const int t = row < r.n_rows ? p.list[r.list + token] : 0;
+    if (row < r.n_rows && dbg_in_range(t >= 0 && t < a.c.n_tokens, a.status))
+      v = reinterpret_cast<const uint4*>(a.q + t * a.q_t + (int64_t)(g * a.G + x - token * a.G) * D)[piece];
     reinterpret_cast<uint4*>(dst + row * D)[piece] = v;
   }
   if (g == 0 && tid < kTileM) p.row_pos[q * kTileM + tid] = tid < r.n_rows ? r.base + p.list[r.list + (r.row0 + tid) / a.G] : -1;
@@ -607,7 +612,7 @@ weigh_pass_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constan
             }
             // (a range that begins inside the sequence's head is its CTA's first)
             const int64_t at = w.k0 == 0 ? (int64_t)w.g * p.plan->n_blocks + q : (int64_t)c.Hkv * p.plan->n_blocks + (int64_t)blockIdx.x * p.plan->most + q - w.q0;
-            p.part[at * kTileM + r] = make_float2(m, l);
+            if (dbg_in_range(at < p.parts && q < p.plan->n_blocks && w.g < c.Hkv, a.status)) p.part[at * kTileM + r] = make_float2(m, l);
           }
           ok = named_barrier_all(1, kSumWarps * 32, ok);
         }
@@ -686,7 +691,8 @@ size_t layout(const l2a_params* p, int kind, int n_tokens, uint8_t* base, WeighA
   x.row_pos = reinterpret_cast<int*>(take(blocks * kTileM * 4));
   x.minus_lse = reinterpret_cast<float*>(take(Hkv * blocks * kTileM * 4));
   x.nan_last = reinterpret_cast<int4*>(take(Hkv * blocks * sizeof(int4)));
-  x.part = reinterpret_cast<float2*>(take((Hkv * blocks + kCtas * (size_t)most_of_one(p)) * kTileM * 8));
+  x.parts = (int64_t)(Hkv * blocks + kCtas * (size_t)most_of_one(p));
+  x.part = reinterpret_cast<float2*>(take((size_t)x.parts * kTileM * 8));
   x.rows = reinterpret_cast<bf16*>(take(Hkv * blocks * kTileM * p->D * 2));
   x.most_blocks = (int)blocks;
   uint8_t* decoded = take(kind == L2A_CACHE_BF16 ? 0 : B * Hkv * (size_t)key_tiles(p->Lk) * kTileN * p->D * 2);
