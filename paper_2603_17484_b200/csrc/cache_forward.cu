@@ -18,7 +18,11 @@ bool has_chunks(const l2a_params* p) { return (int64_t)p->Lq * (p->Hq / p->Hkv) 
 // by the longest.  us with one block / four (window 4096, a fifth routed; 28/4 heads): 5 tokens of one sequence of 32K e4m3 51 / 37, of
 // four 65 / 71, of eight 99 / 148, of eight ragged ones (18 tokens in all) 81 / 56, 9 tokens of one of 9000 42 / 23; (32/8) 8 tokens of eight
 // of 8000 e4m3 81 / 73, bf16 66 / 87; 16 of one of 100K e4m3 101 / 192.
+// 4 bits: always those of kRowBlocks, since the other path's decoding costs as much as the further passes, which find their keys in L2.  (28/4) 5 tokens
+// of one of 32K 62 / 37, of eight 199 / 148, 9 of four of 9000 59 / 50, of eight of 100K 571 / 602, of eight ragged ones 227 / 185; (32/8) 6 of four of 100K 668 /
+// 346, 8 of eight of 32K 436 / 241, 12 of eight of 9000 147 / 113, 16 of one of 100K 194 / 182, of eight 1305 / 1343, of eight ragged ones of 32K 169 / 142.
 int few_rows(const l2a_params* p, const l2a_cache* c, int n_tokens) {
+  if (c->kind == L2A_CACHE_E2M1) return kRowBlocks * kBlockRows;
   const int G = p->Hq / p->Hkv;
   const double blocks = std::max<double>(p->B, (double)n_tokens * G / kBlockRows);
   const double pass = 2.0 * p->Lk * p->Hkv * row_bytes(c->kind, p->D);
