@@ -445,7 +445,7 @@ typedef struct l2a_cache {
 /*
  * Writes the keys and values of the new tokens into their pages (and quantises them).
  *   K, V        in : bf16 [n_tokens, Hkv, D] (token strides k_stride[1], v_stride[1]).
- * HBM-bound: one pass over K and V.  n_tokens = 0 is no work.  Two tokens never share a slot; slots of other tokens keep their
+ * One pass over K and V: HBM-bound in bf16, in 8 and 4 bits by the instructions of the conversion.  n_tokens = 0 is no work.  Two tokens never share a slot; slots of other tokens keep their
  * bits.  Errors: L2A_ERR_INVALID_ARG, L2A_ERR_UNSUPPORTED (D, page_size, kind), L2A_ERR_CUDA.
  */
 l2a_status l2a_cache_append(const l2a_params* p, const l2a_cache* c, const void* K, const void* V, const int32_t* cu_new,
@@ -489,7 +489,7 @@ l2a_status l2a_cache_read(const l2a_params* p, const l2a_cache* c, const int32_t
  * bf16 (8 bits) for sequences of more rows (Lq * Hq / Hkv, see ws), for those of few rows as a pair of bf16 (16 bits) from a bf16 cache, as fp16
  * from one of codes (11 bits down to 2^-24 of the largest weight times 2^e of the values that the row sees, nothing below 2^-35).  Results are
  * bit-reproducible; how the keys of a row are divided, and up to 64 rows which of the two ways they take, follows from all the call's
- * lengths and bounds, so that the same sequence in another batch can differ by such roundings.
+ * lengths and bounds, so that the same sequence in another batch can differ by such roundings (4 bits: up to 64 rows always that of the few).
  * Limits: n_tokens * Hq < 2^31 - 32; Lk * (Hkv + 75) < 2^35 (4 bits: Lk * (Hkv + 112)); where a sequence can have more than 16 rows
  * 2 (n_tokens * Hq / Hkv / 256 + B) * Hkv * (Lk / 128 + 1) < 2^38.  n_tokens = 0 is no work.  Errors: L2A_ERR_INVALID_ARG,
  * L2A_ERR_UNSUPPORTED (D, page_size, kind, the limits), L2A_ERR_WORKSPACE, L2A_ERR_CUDA; a bounded device wait that runs out is
@@ -523,7 +523,8 @@ l2a_status l2a_cache_forward(const l2a_params* p, const l2a_cache* c, const void
  * A page that is in the tables of several sequences (a common prompt) gets the weights that all of them give.  The order in which sequences are added
  * up is then not fixed, so that such a weight can differ in its last bits; all others are bit-reproducible.  The slots of new tokens belong
  * to one sequence each.
- * Few rows: HBM-bound, keys and weights once.  Many: bound by the exponentials, two for each pair of a row and a key.
+ * Few rows: keys and weights are read once and the scores pass through the workspace; bf16 is bound by HBM and the scores' way, 8 and 4 bits by the
+ * conversions and by latencies.  Many: bound by the exponentials, two for each pair of a row and a key.
  * Limits: n_tokens * Hq < 2^31 - 32; B, Hkv <= 65535; Lk * (Hkv + 149) < 2^35 and Lk * Hkv < 2^38.  Errors: L2A_ERR_INVALID_ARG, L2A_ERR_UNSUPPORTED (D,
  * page_size, kind, the limits), L2A_ERR_WORKSPACE, L2A_ERR_CUDA; a bounded device wait that runs out is reported by the status header.
  */
@@ -550,7 +551,10 @@ l2a_status l2a_cache_weigh(const l2a_params* p, const l2a_cache* c, const void* 
  *   kept        out: optional int32 [B, Hkv, Lq]: the positions that stayed, ascending; -1 behind the m of a sequence.
  *   ws             : device workspace of l2a_cache_evict_workspace_bytes (4 * B * Hkv * Lq and a little), 256-byte aligned, its first word a
  *                    status (l2a_workspace_status; no wait of this call has a limit, so that it is L2A_OK but for the debug build's checks).
- * HBM-bound: the weights are read once, what stays is read and written once.  Bit-reproducible.  Errors: L2A_ERR_INVALID_ARG,
+ * Positions are places in the cache: keep positions of tokens apart where they matter.  Keys stay as they were appended, any rotation by position in them
+ * included, while lengths[b] shrinks and each KV head keeps tokens of its own; kept says which.
+ * Two kernels: the selection, bound by latencies (three rounds of counting; the weights are read once, beyond 8 * 48K positions in each round again), and
+ * the move, HBM-bound, what stays read and written once.  Bit-reproducible.  Errors: L2A_ERR_INVALID_ARG,
  * L2A_ERR_UNSUPPORTED (D, page_size, kind, B or Hkv > 65535), L2A_ERR_WORKSPACE, L2A_ERR_CUDA.
  */
 l2a_status l2a_cache_evict_workspace_bytes(const l2a_params* p, const l2a_cache* c, size_t* ws_bytes);

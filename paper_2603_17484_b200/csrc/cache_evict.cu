@@ -5,7 +5,7 @@
 //                      memory as whole numbers of the same order.  The least weight that stays is found digit by digit (11, 11 and 10 bits): a
 //                      CTA counts its numbers by digit, and every CTA adds up the counts of all.  Then each lists what stays, at its place.
 //                      Equal weights stay from the lowest position on, whatever the number of CTAs.  Bound by latencies: 32K positions a head, 16 x 8
-//                      heads in clusters of four 30 us, one sequence of 9001 15 (digits of 8 bits: 33 and 21).
+//                      heads in clusters of four 26 to 30 us, one sequence of 9001 15 (digits of 8 bits: 33 and 21).
 // cache_move_kernel  : 64 rows of 256 bytes of a head a CTA (128 of 128, else 256), 16 bytes a thread; nothing is computed.
 //                      16 sequences of up to 32K tokens, 40 % kept (8 heads, D = 128, e2m1): 38 us for 177 MB = 4.7 TB/s; with 64 rows a CTA 53.
 #include "cache_common.cuh"

@@ -31,7 +31,7 @@
 // A lone short sequence is latency (9001 keys: 13.3 us, of which this kernel 9.2; the dense l2a_decode, which knows its lengths on the host,
 // takes 7.6 in 16 bits): lists, lengths and decisions are read by every CTA ahead of its first copy.  Tried: two chains of products 206 us
 // against 196; the loads of V ahead of the soft-max, no change; pieces and rows of Q handed over by the producer, 14.2 against 13.0 for 9001 keys.
-// e2m1, calls one after the other: the 16 sequences of 128K keys 172 us for 671 MB = 3.9 TB/s, the 32 ragged ones (pages of 16) 51 us, 9001 keys 16.4.  Bound
+// e2m1, calls one after the other: the 16 sequences of 128K keys 172 us (179 in other runs) for 671 MB = 3.9 TB/s, the 32 ragged ones (pages of 16) 51 us, 9001 keys 16.4.  Bound
 // by the instructions of the conversions and their latencies with three warps a scheduler: without the loads 162 us, without the computing 122; with Q's
 // operands in registers instead of shared memory 176.
 // 64 of about 340 a warp for 16 keys multiply by block scales (32 us), 64 convert codes.  Tried: scores by tcgen05
